@@ -345,6 +345,141 @@ PMPE_API int pmpe_selftest_wait_timeout(uint32_t *status, int limit_us, void *st
  *     events. */
 PMPE_API int pmpe_moe_forward_noalloc(const pmpe_moe_desc *d, void *stream);
 
+/* ---------------------------------------------- operators around the layer
+ *
+ * The norm of the residual stream before the layer, routing from given logits
+ * where a model's router is not the layer's own, and the clipping of the
+ * gradients that the backward gives.  Pointers need the alignment of their
+ * elements only (16-byte aligned rows are read with wide loads). */
+
+/* Element types. */
+#define PMPE_F32 0
+#define PMPE_BF16 1
+#define PMPE_F16 2
+
+#define PMPE_MAX_NORM_WIDTH 16384
+
+#define PMPE_QUANT_NONE 0
+#define PMPE_QUANT_BLOCK 1 /* e4m3, a scale per row and 128 columns (the last block may be shorter) */
+#define PMPE_QUANT_ROW 2   /* e4m3, a scale per row */
+
+/* Root-mean-square norm with the residual's addition:
+ *   h = round(x + residual)        rounded to `type`; x itself when residual is NULL
+ *   rstd = 1 / sqrt(mean_c h_c^2 + eps)
+ *   y = h rstd weight              rounded to `type`, or in 8 bits:
+ *   s = max(amax |h rstd weight| / 448, 2^-126), y = e4m3(h rstd weight / s)
+ * Sums and products are FP32 (64 bits where squares leave FP32's range).  A
+ * NaN or an infinity stays in its row.  An output may be the same memory as an
+ * input of the same type and row pitch (h on residual, say); other overlaps
+ * are not allowed. */
+typedef struct pmpe_rms_norm_desc {
+    int T, H;              /* rows >= 0, columns 1 .. PMPE_MAX_NORM_WIDTH */
+    int type;              /* of x, residual, h and an unquantised y */
+    int weight_type;       /* `type` or PMPE_F32 */
+    int quant;             /* PMPE_QUANT_* */
+    float eps;             /* >= 1e-20 */
+    const void *x;         /* rows x_ld elements apart, x_ld >= H */
+    const void *residual;  /* optional, rows residual_ld elements apart */
+    const void *weight;    /* [H] */
+    int64_t x_ld, residual_ld;
+    void *h;               /* optional [T, H] */
+    void *y;               /* [T, H]: `type`, or e4m3 bytes */
+    float *scale;          /* [T, ceil(H / 128)] or [T] with a quantised y, else NULL */
+    float *rstd;           /* optional [T], for the backward */
+} pmpe_rms_norm_desc;
+PMPE_API int pmpe_rms_norm(const pmpe_rms_norm_desc *d, void *stream);
+
+/* Its backward, for dy = dL/dy (the 8-bit rounding passes gradients as the
+ * identity) and d_h = dL/dh through the stream's other readers:
+ *   dx = d_h + rstd (dy weight - h rstd^2 mean_c(dy weight h))   (the gradient of x and of residual)
+ *   dw = sum_t dy h rstd
+ * All matrices [T, H] without gaps.  dx may be the same memory as d_h, or as
+ * dy or h of the same type.  The sum over the rows is FP32, in an order that
+ * depends on T and H alone. */
+typedef struct pmpe_rms_norm_backward_desc {
+    int T, H;
+    int type;              /* of h */
+    int weight_type;       /* `type` or PMPE_F32 */
+    int dy_type;           /* `type` or PMPE_F32 */
+    int dx_type;           /* of dx and d_h: `type` or PMPE_F32 */
+    const void *dy, *h, *weight;
+    const float *rstd;     /* [T], the forward's */
+    const void *d_h;       /* optional */
+    void *dx;              /* [T, H] */
+    float *dw;             /* optional [H] FP32, overwritten */
+    void *workspace;       /* >= the size below, 16-byte aligned (unused, may be NULL, without dw) */
+    size_t workspace_bytes;
+} pmpe_rms_norm_backward_desc;
+PMPE_API size_t pmpe_rms_norm_backward_workspace_size(int T, int H); /* 0 for an invalid shape */
+PMPE_API int pmpe_rms_norm_backward(const pmpe_rms_norm_backward_desc *d, void *stream);
+
+#define PMPE_SCORE_SOFTMAX 0
+#define PMPE_SCORE_SIGMOID 1
+#define PMPE_GROUP_MAX 0
+#define PMPE_GROUP_TOP2 1
+
+/* Routing from given logits, each token inside the pool that its policy byte
+ * selects (Sec. 3.1 Eq. 4; only 0x01 selects the private pool):
+ *   eligible: the experts of that pool whose logit is above -inf (NaN is not)
+ *   score:    softmax over the eligible experts, or the sigmoid of the logit
+ *   choice:   score + bias; without a bias the logit (the same order)
+ *   groups:   the pool in `groups` runs of equal length; a group counts its
+ *             largest choice, or the sum of its two largest score + bias; only
+ *             the top_groups best stay in the choice
+ *   selection: the k largest choices, equal ones by the lower id
+ *   weights:  score * scale, divided by the sum of the k scores when
+ *             renormalised (sigmoid: that sum + 1e-20)
+ * The selection is that of exact arithmetic on the given logits and biases,
+ * whatever FP32 rounds to the same value.  A logit of +inf counts as the
+ * largest finite one; an expert with a bias of -inf is never chosen.  Where
+ * fewer than k experts can be chosen, the rest of the row is -1 with weight 0. */
+typedef struct pmpe_route_desc {
+    int T;                 /* tokens >= 0 */
+    int E_pub, E_priv;     /* k <= E_pub <= 256; E_priv 0 (one pool, policy NULL) or k .. 256 */
+    int k;                 /* 1 .. 32 */
+    int logits_type;       /* PMPE_F32, PMPE_BF16, PMPE_F16 */
+    int score;             /* PMPE_SCORE_* */
+    int renormalize;       /* 0 or 1 */
+    int groups_pub, top_groups_pub;    /* 1 .. 32 groups; top_groups of them hold at least k experts */
+    int groups_priv, top_groups_priv;
+    int group_score;       /* PMPE_GROUP_* */
+    float scale;           /* finite */
+    const void *logits;    /* [T, E_pub + E_priv], rows ld elements apart */
+    int64_t ld;
+    const uint8_t *policy; /* [T] or NULL (all DENY) */
+    const float *bias;     /* optional [E_pub + E_priv] */
+    int32_t *topk_idx;     /* [T, k] global ids, best choice first (read by the backward) */
+    float *topk_w;         /* [T, k] (not read by the backward, may be NULL there) */
+    int32_t *load;         /* optional [E_pub + E_priv]: the tokens of each expert are added to it */
+} pmpe_route_desc;
+PMPE_API int pmpe_route(const pmpe_route_desc *d, void *stream);
+
+/* dL/dlogits from dL/dw ([T, k] FP32) for the selection in topk_idx, which is
+ * piecewise constant: d_logits [T, E_pub + E_priv] of logits_type, without
+ * gaps, overwritten (zero for the other pool).  Ids that are -1 or outside
+ * the token's pool contribute nothing; bias, groups and load are not used. */
+PMPE_API int pmpe_route_backward(const pmpe_route_desc *d, const float *dw, void *d_logits, void *stream);
+
+/* One gradient: n elements without gaps. */
+typedef struct pmpe_grad {
+    void *grad;
+    void *out;             /* the clipped gradient's place; NULL or grad: in place */
+    int64_t n;             /* >= 0 */
+    int type;              /* PMPE_F32, PMPE_BF16 or PMPE_F16, of grad and out */
+} pmpe_grad;
+
+/* norm = sqrt(sum over all tensors of g^2), out = g min(1, max_norm / (norm + 1e-6)).
+ * A norm that is not finite clips nothing (out = g): the caller sees it in
+ * *norm and drops the step.  max_norm: >= 0, +inf for the norm alone.  No two
+ * tensors may share memory (PMPE_ERR_INVALID_ARG), whole tensors in place
+ * apart.  `grads` is a host array, read before the call returns; fewer than
+ * 2^31 chunks of 16 KB in all.  norm: device FP32.  workspace: device, 16-byte
+ * aligned, of the size below.  The sums' order depends on the tensors' sizes
+ * and alignment alone. */
+PMPE_API size_t pmpe_clip_workspace_size(int n); /* 0 for n < 0 */
+PMPE_API int pmpe_clip_grad_norm(const pmpe_grad *grads, int n, float max_norm, float *norm, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
 /* Zero the audit buffer (pmpe_audit_words(T, E) words). */
 PMPE_API int pmpe_audit_reset(uint32_t *audit, int T, int E, void *stream);
 

@@ -168,6 +168,17 @@ cudaError_t launch_combine(const Ctx &c);
 // hidden states into the workspace's dispatched-row matrix (a_perm), which the
 // backward's GEMMs read.
 cudaError_t launch_gather_dispatch_rows(const Ctx &c, int g0, int g1);
+// The operators around the layer (k_norm.cu, k_scores.cu, k_clip.cu), their
+// descriptors checked by ops_api.cu.
+cudaError_t launch_rms_norm(const pmpe_rms_norm_desc &d, cudaStream_t st);
+size_t rms_norm_backward_workspace_bytes(int T, int H);
+cudaError_t launch_rms_norm_backward(const pmpe_rms_norm_backward_desc &d, float *part, cudaStream_t st);
+cudaError_t launch_route_scores(const pmpe_route_desc &d, int num_sms, cudaStream_t st);
+cudaError_t launch_route_scores_backward(const pmpe_route_desc &d, const float *dw, void *d_logits, int num_sms,
+                                         cudaStream_t st);
+size_t clip_workspace_bytes(int n);
+int clip_tensors_ok(const pmpe_grad *g, int n);
+cudaError_t launch_clip(const pmpe_grad *g, int n, float max_norm, float *norm_out, double *partial, cudaStream_t st);
 cudaError_t launch_resolve(const uint8_t *policy, int T, uint8_t *tau, cudaStream_t stream);
 cudaError_t launch_policy_from_requests(const uint8_t *req_policy, const int32_t *cu_seqlens, int n_req, int T,
                                         uint8_t *policy_out, cudaStream_t stream);

@@ -7,7 +7,9 @@ has not been built this module raises on import -- there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -101,7 +103,9 @@ EXPORTED = ("pmpe_moe_workspace_size", "pmpe_moe_workspace_layout", "pmpe_audit_
             "pmpe_status_string", "pmpe_moe_forward_noalloc", "pmpe_selftest_wait_timeout",
             "pmpe_policy_from_requests", "pmpe_moe_backward_workspace_size", "pmpe_moe_backward_private",
             "pmpe_moe_backward_input_workspace_size", "pmpe_moe_backward_input",
-            "pmpe_moe_backward_step_workspace_size", "pmpe_moe_backward_step", "pmpe_saved_gu_floats")
+            "pmpe_moe_backward_step_workspace_size", "pmpe_moe_backward_step", "pmpe_saved_gu_floats",
+            "pmpe_rms_norm", "pmpe_rms_norm_backward_workspace_size", "pmpe_rms_norm_backward", "pmpe_route",
+            "pmpe_route_backward", "pmpe_clip_workspace_size", "pmpe_clip_grad_norm")
 
 # Bytes of the library's static scratch array used by pmpe_moe_forward_noalloc.
 STATIC_SCRATCH_BYTES = 32 << 20
@@ -130,6 +134,45 @@ class WorkspaceLayout(ctypes.Structure):
                                                 "tile_counts")]
 
 
+class RmsNormDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int), ("H", ctypes.c_int), ("type", ctypes.c_int), ("weight_type", ctypes.c_int),
+                ("quant", ctypes.c_int), ("eps", ctypes.c_float), ("x", _vp), ("residual", _vp), ("weight", _vp),
+                ("x_ld", ctypes.c_int64), ("residual_ld", ctypes.c_int64), ("h", _vp), ("y", _vp), ("scale", _vp),
+                ("rstd", _vp)]
+
+
+class RmsNormBackwardDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int), ("H", ctypes.c_int), ("type", ctypes.c_int), ("weight_type", ctypes.c_int),
+                ("dy_type", ctypes.c_int), ("dx_type", ctypes.c_int), ("dy", _vp), ("h", _vp), ("weight", _vp),
+                ("rstd", _vp), ("d_h", _vp), ("dx", _vp), ("dw", _vp), ("workspace", _vp),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class RouteDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("T", "E_pub", "E_priv", "k", "logits_type", "score", "renormalize", "groups_pub",
+                                            "top_groups_pub", "groups_priv", "top_groups_priv", "group_score")] + \
+               [("scale", ctypes.c_float), ("logits", _vp), ("ld", ctypes.c_int64), ("policy", _vp), ("bias", _vp),
+                ("topk_idx", _vp), ("topk_w", _vp), ("load", _vp)]
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("grad", _vp), ("out", _vp), ("n", ctypes.c_int64), ("type", ctypes.c_int)]
+
+
+_lib.pmpe_rms_norm.restype = ctypes.c_int
+_lib.pmpe_rms_norm.argtypes = [ctypes.POINTER(RmsNormDesc), _vp]
+_lib.pmpe_rms_norm_backward_workspace_size.restype = ctypes.c_size_t
+_lib.pmpe_rms_norm_backward_workspace_size.argtypes = [ctypes.c_int] * 2
+_lib.pmpe_rms_norm_backward.restype = ctypes.c_int
+_lib.pmpe_rms_norm_backward.argtypes = [ctypes.POINTER(RmsNormBackwardDesc), _vp]
+_lib.pmpe_route.restype = ctypes.c_int
+_lib.pmpe_route.argtypes = [ctypes.POINTER(RouteDesc), _vp]
+_lib.pmpe_route_backward.restype = ctypes.c_int
+_lib.pmpe_route_backward.argtypes = [ctypes.POINTER(RouteDesc), _vp, _vp, _vp]
+_lib.pmpe_clip_workspace_size.restype = ctypes.c_size_t
+_lib.pmpe_clip_workspace_size.argtypes = [ctypes.c_int]
+_lib.pmpe_clip_grad_norm.restype = ctypes.c_int
+_lib.pmpe_clip_grad_norm.argtypes = [ctypes.POINTER(Grad), ctypes.c_int, ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.pmpe_moe_workspace_size.restype = ctypes.c_size_t
 _lib.pmpe_moe_workspace_size.argtypes = [ctypes.c_int] * 7
 _lib.pmpe_moe_workspace_layout.restype = ctypes.c_int
@@ -432,3 +475,253 @@ class MoeLayer:
         _check(_lib.pmpe_moe_backward_input(ctypes.byref(desc), _ptr(dout), _ptr(d_hidden), _ptr(bws), bws.numel(),
                                             _stream(stream)), "pmpe_moe_backward_input")
         return d_hidden
+
+
+# ------------------------------------------- operators around the layer
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_QUANT = {None: 0, "block": 1, "row": 2}
+QUANT_BLOCK = 128  # columns that share a scale with quant="block"
+
+
+def _require(ok, what: str):
+    if not ok:
+        raise PmpeError(ERR_INVALID_ARG, what)
+
+
+def _placed(fn):
+    """Runs ``fn``, whose first argument is a tensor (or a list of them), on
+    that tensor's device and on ``stream``: outputs and scratch are allocated
+    where the kernels run, so the caching allocator reuses them in order."""
+    name = fn.__code__.co_varnames[0]
+
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kw):
+        first = args[0] if args else kw.get(name)
+        t = first[0] if isinstance(first, list) and first else first
+        _require(isinstance(t, torch.Tensor) and t.is_cuda, f"{fn.__name__}: {name}: a CUDA tensor is wanted")
+        if stream is not None:
+            _require(stream.device == t.device, f"{fn.__name__}: the stream is of another device than the tensors")
+            with torch.cuda.stream(stream):
+                return fn(*args, **kw)
+        if t.device.index != torch.cuda.current_device():
+            with torch.cuda.device(t.device):
+                return fn(*args, **kw)
+        return fn(*args, **kw)
+    return call
+
+
+def _stream_of(t) -> int:
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _pitch(t) -> int:
+    """Elements from a row to the next (any value serves a single row)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+class RmsNorm(NamedTuple):
+    y: torch.Tensor             # [T, H], the input's type or float8_e4m3fn
+    scale: torch.Tensor | None  # FP32 [T, ceil(H / 128)] ("block") or [T, 1] ("row") of an 8-bit y
+    h: torch.Tensor             # [T, H], x + residual; x itself without a residual
+    rstd: torch.Tensor          # FP32 [T], for the backward
+
+
+@_placed
+def rms_norm(x, weight, residual=None, eps: float = 1e-6, quant=None, h_out=None) -> RmsNorm:
+    """Root-mean-square norm of ``h = x + residual`` (x without a residual),
+    times ``weight``.
+
+    x and residual: [T, H] of one type (FP32, BF16 or FP16), rows of any pitch;
+    weight: [H] of that type or FP32.  h is rounded to the type, and the norm
+    is that of the rounded h.  ``quant``: None for y in x's type; "block" or
+    "row" for y in e4m3 with an FP32 scale per row and 128 columns or per row
+    (y stands for ``y.float() * scale``).  ``h_out``: where h goes (may be
+    ``residual`` or ``x``).  ``stream``: the stream to run on (default: the
+    current one).  H up to 16384, eps at least 1e-20."""
+    _require(x.dim() == 2 and x.dtype in _TYPES and x.stride(1) == 1 or x.dim() == 2 and x.shape[1] == 1,
+             "rms_norm: x is [T, H] of FP32, BF16 or FP16 with adjacent columns")
+    T, H = x.shape
+    dev, dt = x.device, x.dtype
+    _require(quant in _QUANT, 'rms_norm: quant is None, "block" or "row"')
+    _require(weight.device == dev and weight.dtype in (dt, torch.float32) and weight.shape == (H,) and weight.is_contiguous(),
+             "rms_norm: weight is [H] of x's type or FP32, on x's device")
+    h = x
+    if residual is not None:
+        _require(residual.device == dev and residual.dtype == dt and residual.shape == (T, H) and
+                 (residual.stride(1) == 1 or H == 1), "rms_norm: residual is as x")
+        h = h_out if h_out is not None else torch.empty((T, H), dtype=dt, device=dev)
+        _require(h.device == dev and h.dtype == dt and h.shape == (T, H) and h.is_contiguous(),
+                 "rms_norm: h_out is [T, H] of x's type without gaps")
+    else:
+        _require(h_out is None, "rms_norm: without a residual h is x")
+    y = torch.empty((T, H), dtype=dt if quant is None else torch.float8_e4m3fn, device=dev)
+    scale = None
+    if quant is not None:
+        scale = torch.empty((T, -(-H // QUANT_BLOCK) if quant == "block" else 1), dtype=torch.float32, device=dev)
+    rstd = torch.empty(T, dtype=torch.float32, device=dev)
+    d = RmsNormDesc(T, H, _TYPES[dt], _TYPES[weight.dtype], _QUANT[quant], eps, x.data_ptr(), _at(residual),
+                    weight.data_ptr(), _pitch(x), 0 if residual is None else _pitch(residual),
+                    None if residual is None else h.data_ptr(), y.data_ptr(), _at(scale), rstd.data_ptr())
+    _check(_lib.pmpe_rms_norm(d, _stream_of(x)), "pmpe_rms_norm")
+    return RmsNorm(y, scale, h, rstd)
+
+
+@_placed
+def rms_norm_backward(dy, h, weight, rstd, d_h=None, dx_dtype=None, need_dw: bool = True):
+    """(dx, dw) of ``rms_norm``: dx is the gradient of x and of the residual
+    alike, dw that of the weight (FP32; None unless ``need_dw``).
+
+    dy: [T, H] of h's type or FP32; h and rstd as the forward returned them;
+    d_h: the gradient that reaches h itself, of dx's type.  ``dx_dtype``: h's
+    type (default) or FP32.  Matrices without gaps.  An 8-bit y passes its
+    gradient as the identity."""
+    _require(h.dim() == 2 and h.dtype in _TYPES and h.is_contiguous() and dy.device == h.device,
+             "rms_norm_backward: h is [T, H] of FP32, BF16 or FP16 without gaps")
+    T, H = h.shape
+    dev, dt = h.device, h.dtype
+    xt = dx_dtype if dx_dtype is not None else dt
+    _require(xt in (dt, torch.float32), "rms_norm_backward: dx is of h's type or FP32")
+    _require(dy.dtype in (dt, torch.float32) and dy.shape == (T, H) and dy.is_contiguous(),
+             "rms_norm_backward: dy is [T, H] of h's type or FP32 without gaps")
+    _require(weight.device == dev and weight.dtype in (dt, torch.float32) and weight.shape == (H,) and weight.is_contiguous(),
+             "rms_norm_backward: weight is [H] of h's type or FP32")
+    _require(rstd.device == dev and rstd.dtype == torch.float32 and rstd.shape == (T,) and rstd.is_contiguous(),
+             "rms_norm_backward: rstd is FP32 [T]")
+    _require(d_h is None or (d_h.device == dev and d_h.dtype == xt and d_h.shape == (T, H) and d_h.is_contiguous()),
+             "rms_norm_backward: d_h is [T, H] of dx's type without gaps")
+    dx = torch.empty((T, H), dtype=xt, device=dev)
+    dw = ws = None
+    nb = 0
+    if need_dw:
+        dw = torch.empty(H, dtype=torch.float32, device=dev)
+        nb = _lib.pmpe_rms_norm_backward_workspace_size(T, H)
+        ws = torch.empty(nb, dtype=torch.uint8, device=dev)
+    d = RmsNormBackwardDesc(T, H, _TYPES[dt], _TYPES[weight.dtype], _TYPES[dy.dtype], _TYPES[xt], dy.data_ptr(), h.data_ptr(),
+                            weight.data_ptr(), rstd.data_ptr(), _at(d_h), dx.data_ptr(), _at(dw), _at(ws), nb)
+    _check(_lib.pmpe_rms_norm_backward(d, _stream_of(h)), "pmpe_rms_norm_backward")
+    return dx, dw
+
+
+class Router:
+    """Routing from given logits for models whose router is not the layer's
+    own softmax: softmax or sigmoid scores, a bias for balance, group limits,
+    top-k and weights, each token inside the pool its policy byte selects.
+    ``MoeLayer.forward(route=...)`` runs the experts with the result.
+
+    score: "softmax" (over the token's pool) or "sigmoid".  groups,
+    groups_priv: (groups of the pool, groups kept); group_score: "max" or
+    "top2", the sum of a group's two best.  E_priv = 0: one pool, no policy."""
+
+    def __init__(self, E_pub: int, E_priv: int, k: int, score: str = "softmax", renormalize: bool = True, scale: float = 1.0,
+                 groups=(1, 1), groups_priv=(1, 1), group_score: str = "max"):
+        _require(score in ("softmax", "sigmoid"), 'Router: score is "softmax" or "sigmoid"')
+        _require(group_score in ("max", "top2"), 'Router: group_score is "max" or "top2"')
+        self.E_pub, self.E_priv, self.k, self.E = int(E_pub), int(E_priv), int(k), int(E_pub) + int(E_priv)
+        self._config = (int(score == "sigmoid"), int(bool(renormalize)), int(groups[0]), int(groups[1]), int(groups_priv[0]),
+                        int(groups_priv[1]), int(group_score == "top2"), float(scale))
+        # refuses what the library would refuse, before the first call
+        d = RouteDesc(0, self.E_pub, self.E_priv, self.k, 0, *self._config, None, max(self.E, 0), None, None, None, None, None)
+        _check(_lib.pmpe_route(d, None), "pmpe_route")
+
+    def _desc(self, logits, policy, bias, idx, w, load) -> RouteDesc:
+        T, dev = logits.shape[0], logits.device
+        _require(logits.dim() == 2 and logits.dtype in _TYPES and logits.shape[1] == self.E and
+                 (logits.stride(1) == 1 or self.E == 1), "Router: logits are [T, E] of FP32, BF16 or FP16 with adjacent columns")
+        _require(policy is None or (policy.device == dev and policy.dtype == torch.uint8 and policy.shape == (T,) and
+                                    policy.is_contiguous()), "Router: policy is uint8 [T] on the logits' device")
+        _require(bias is None or (bias.device == dev and bias.dtype == torch.float32 and bias.shape == (self.E,) and
+                                  bias.is_contiguous()), "Router: bias is FP32 [E] on the logits' device")
+        return RouteDesc(T, self.E_pub, self.E_priv, self.k, _TYPES[logits.dtype], *self._config, logits.data_ptr(),
+                         _pitch(logits), _at(policy), _at(bias), idx.data_ptr(), _at(w), _at(load))
+
+    def route(self, logits, policy=None, bias=None, load=None, stream=None):
+        """(idx, w): the k chosen experts of each token (int32 [T, k], global
+        ids, best first, -1 where there is none) and their weights (FP32).
+
+        logits: [T, E_pub + E_priv], rows of any pitch; -inf (or NaN) takes an
+        expert out of a token's choice.  policy: uint8 [T], 0x01 for the
+        private pool (None: all public).  bias: FP32 [E], added to the scores
+        for the choice alone.  load: int32 [E], to which the tokens of each
+        expert are added (for the bias's update)."""
+        return _route(logits, self, policy, bias, load, stream=stream)
+
+    def backward(self, logits, policy, idx, dw, stream=None):
+        """The gradient of the logits ([T, E], their type) from that of the
+        weights (FP32 [T, k]) for the selection ``idx``."""
+        return _route_backward(logits, self, policy, idx, dw, stream=stream)
+
+
+@_placed
+def _route(logits, router, policy, bias, load):
+    dev = logits.device
+    _require(load is None or (load.device == dev and load.dtype == torch.int32 and load.shape == (router.E,) and
+                              load.is_contiguous()), "Router: load is int32 [E] on the logits' device")
+    idx = torch.empty((logits.shape[0], router.k), dtype=torch.int32, device=dev)
+    w = torch.empty((logits.shape[0], router.k), dtype=torch.float32, device=dev)
+    _check(_lib.pmpe_route(router._desc(logits, policy, bias, idx, w, load), _stream_of(logits)), "pmpe_route")
+    return idx, w
+
+
+@_placed
+def _route_backward(logits, router, policy, idx, dw):
+    T, dev = logits.shape[0], logits.device
+    _require(idx.device == dev and idx.dtype == torch.int32 and idx.shape == (T, router.k) and idx.is_contiguous(),
+             "Router: idx is int32 [T, k] on the logits' device")
+    _require(dw.device == dev and dw.dtype == torch.float32 and dw.shape == (T, router.k) and dw.is_contiguous(),
+             "Router: dw is FP32 [T, k] on the logits' device")
+    d_logits = torch.empty((T, router.E), dtype=logits.dtype, device=dev)
+    _check(_lib.pmpe_route_backward(router._desc(logits, policy, None, idx, None, None), dw.data_ptr(), d_logits.data_ptr(),
+                                    _stream_of(logits)), "pmpe_route_backward")
+    return d_logits
+
+
+def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
+    """The global norm of ``grads`` (a list of tensors, or a dict of them as the
+    backward returns it), as an FP32 device scalar; the gradients are scaled in
+    place by min(1, max_norm / (norm + 1e-6)), or into the tensors of ``out``.
+
+    FP32, BF16 and FP16 tensors may be mixed; each lies in memory without gaps.
+    max_norm = inf: the norm alone.  A norm that is not finite clips nothing.
+    No tensor may share memory with another."""
+    if isinstance(grads, dict):
+        _require(out is None or isinstance(out, dict) and out.keys() == grads.keys(), "clip_grad_norm: out is as grads")
+        out = None if out is None else [out[n] for n in grads]
+        grads = list(grads.values())
+    grads = list(grads)
+    _require(grads, "clip_grad_norm: no gradients")
+    return _clip(grads, float(max_norm), None if out is None else list(out), stream=stream)
+
+
+@_placed
+def _clip(grads, max_norm, out):
+    n, dev = len(grads), grads[0].device
+    _require(out is None or len(out) == n, "clip_grad_norm: one output for each gradient")
+    table = (Grad * n)()
+    for i, g in enumerate(grads):
+        o = g if out is None else out[i]
+        _require(g.device == dev and o.device == dev and g.dtype in _TYPES and o.dtype == g.dtype and o.shape == g.shape,
+                 "clip_grad_norm: gradients and outputs are FP32, BF16 or FP16 tensors of one device, outputs as their gradients")
+        if not (g.is_contiguous() and o.is_contiguous()):
+            _require(g.stride() == o.stride() and _dense(g), "clip_grad_norm: a gradient has gaps")
+        table[i] = (g.data_ptr(), o.data_ptr(), g.numel(), _TYPES[g.dtype])
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    nb = _lib.pmpe_clip_workspace_size(n)
+    ws = torch.empty(nb, dtype=torch.uint8, device=dev)
+    _check(_lib.pmpe_clip_grad_norm(table, n, max_norm, norm.data_ptr(), ws.data_ptr(), nb, _stream_of(grads[0])),
+           "pmpe_clip_grad_norm")
+    return norm
+
+
+def _dense(t) -> bool:
+    """Whether the tensor's elements fill a run of memory, in some order."""
+    want = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if stride != want:
+            return False
+        want *= size
+    return True

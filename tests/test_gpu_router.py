@@ -1,0 +1,215 @@
+"""Router.route and Router.backward against 64-bit references.
+
+The selection has to be the reference's exactly.  Weights: an FP32 exponential
+of a difference of logits is off by 2^-24 times that difference (below 40 in
+these inputs' chosen experts) and 2 ulp, a sum of 256 terms by 13 x 2^-24:
+2^-17 relative covers them."""
+import numpy as np
+import pytest
+import torch
+
+import operators_ref as ref
+
+pytestmark = pytest.mark.gpu
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+REL = 2.0 ** -17
+
+
+@pytest.fixture(scope="module")
+def pmpe():
+    from paper_2608_06690_gb300 import pmpe as m
+    return m
+
+
+def make(T, E_pub, E_priv, seed, dtype=F32, bias=False, pitch=None):
+    g = torch.Generator().manual_seed(seed)
+    E = E_pub + E_priv
+    wide = (1.5 * torch.randn((T, pitch or E), generator=g)).to(dtype).cuda()
+    policy = torch.randint(0, 3, (T,), generator=g).to(torch.uint8).cuda() if E_priv else None
+    b = (0.05 * torch.randn((E,), generator=g)).cuda() if bias else None
+    return wide[:, :E], policy, b
+
+
+def n64(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def host(t):
+    return None if t is None else t.cpu().numpy()
+
+
+def check(pmpe, logits, policy, bias, E_pub, E_priv, k, score="softmax", renorm=True, scale=1.0, groups=(1, 1), groups_priv=(1, 1),
+          group_score="max", backward=True, stream=None):
+    r = pmpe.Router(E_pub, E_priv, k, score=score, renormalize=renorm, scale=scale, groups=groups, groups_priv=groups_priv,
+                    group_score=group_score)
+    load = torch.full((E_pub + E_priv,), 3, dtype=torch.int32, device="cuda")
+    idx, w = r.route(logits, policy, bias=bias, load=load)
+    torch.cuda.synchronize()
+    ri, rw = ref.route(n64(logits), host(policy), E_pub, E_priv, k, score == "sigmoid", renorm, scale, n64(bias), groups, groups_priv,
+                       group_score == "top2")
+    got = host(idx)
+    assert np.array_equal(got, ri), (np.argwhere((got != ri).any(1))[:3], got[(got != ri).any(1)][:3], ri[(got != ri).any(1)][:3])
+    gw = n64(w)
+    assert (np.abs(gw - rw) <= REL * np.abs(rw) + 2.0 ** -126).all(), np.abs(gw - rw).max()
+    assert (gw[ri < 0] == 0).all()
+    count = np.bincount(ri[ri >= 0], minlength=E_pub + E_priv)
+    assert np.array_equal(host(load), count + 3)  # added to what was there
+    if not backward:
+        return
+    g = torch.Generator().manual_seed(99)
+    dw = torch.randn(idx.shape, generator=g).cuda()
+    d = r.backward(logits, policy, idx, dw)
+    torch.cuda.synchronize()
+    assert d.dtype == logits.dtype and d.shape == logits.shape
+    rd, size = ref.route_backward(n64(logits), host(policy), ri, n64(dw), E_pub, E_priv, score == "sigmoid", renorm, scale)
+    eps = torch.finfo(logits.dtype)
+    bad = ~(np.abs(n64(d) - rd) <= eps.eps / 2 * np.abs(rd) + 2 * REL * size + eps.smallest_normal * eps.eps / 2)
+    assert not bad.any(), (np.argwhere(bad)[:4], n64(d)[bad][:4], rd[bad][:4])
+
+
+POOLS = [(4, 0, 1), (8, 0, 8), (16, 4, 2), (33, 31, 5), (64, 16, 6), (128, 32, 8), (128, 128, 12), (160, 0, 6), (255, 17, 7),
+         (256, 0, 8), (256, 256, 32), (40, 32, 32)]
+
+
+@pytest.mark.parametrize("E_pub,E_priv,k", POOLS)
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_pools(pmpe, E_pub, E_priv, k, score, dtype):
+    for renorm, bias in ((True, False), (False, True)):
+        z, policy, b = make(37, E_pub, E_priv, E_pub + k, dtype, bias)
+        check(pmpe, z, policy, b, E_pub, E_priv, k, score, renorm, 2.5 if bias else 1.0)
+
+
+@pytest.mark.parametrize("E_pub,groups,k", [(16, (4, 2), 4), (64, (8, 3), 6), (256, (8, 4), 8), (256, (32, 5), 8), (160, (8, 3), 6),
+                                            (96, (3, 1), 5), (30, (10, 7), 3), (7, (7, 3), 2)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("group_score", ["max", "top2"])
+def test_groups(pmpe, E_pub, groups, k, score, group_score):
+    for bias, dtype in ((False, F32), (True, BF16)):
+        z, policy, b = make(41, E_pub, 32, 7, dtype, bias)
+        check(pmpe, z, policy, b, E_pub, 32, k, score, True, 2.5, groups, (4, 2), group_score)
+
+
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 130, 4875])
+def test_tokens(pmpe, T):
+    z, policy, b = make(T, 128, 32, T, F32, True)
+    check(pmpe, z, policy, b, 128, 32, 8, "sigmoid", True, 2.5, (8, 4), (1, 1), "top2")
+
+
+@pytest.mark.parametrize("pitch", [160, 161, 164, 168, 300])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_pitches(pmpe, pitch, dtype):
+    z, policy, _ = make(19, 128, 32, 3, dtype, pitch=pitch)
+    check(pmpe, z, policy, None, 128, 32, 8, renorm=False)
+    check(pmpe, z[1:], policy[1:].clone(), None, 128, 32, 8)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_masked_experts(pmpe, score, renorm):
+    """Rows with fewer eligible experts than k, none, infinities, NaN, the
+    type's lowest value: what is left is chosen and nothing spreads."""
+    z, policy, b = make(12, 16, 8, 5, F32, True)
+    policy[:] = 0
+    policy[6:] = 1
+    z[0] = -np.inf
+    z[1] = -np.inf
+    z[1, 3] = 0.5
+    z[2, 1:] = float("nan")
+    z[3, 5] = np.inf
+    z[4, :16] = torch.finfo(F32).min
+    z[5, ::2] = -np.inf
+    z[6] = float("nan")
+    z[7, 16:20] = -np.inf
+    z[8, :16] = float("nan")  # the other pool of an ALLOW token
+    for bias in (None, b):
+        check(pmpe, z, policy, bias, 16, 8, 4, score, renorm)
+        check(pmpe, z, policy, bias, 16, 8, 4, score, renorm, 1.0, (4, 2), (2, 1), "top2")
+    b[2] = -np.inf  # an expert taken out by its bias
+    check(pmpe, z, policy, b, 16, 8, 4, score, renorm)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_near_ties(pmpe, score):
+    """Logits and biases that FP32 scores cannot tell apart: the selection is
+    that of 64 bits, equal values by the lower id."""
+    g = torch.Generator().manual_seed(11)
+    T, E = 64, 64
+    z = torch.randn((T, 1), generator=g).expand(T, E).clone()
+    z += torch.randint(-3, 4, (T, E), generator=g) * 2.0 ** -23  # a few ulps apart
+    z = z.cuda()
+    check(pmpe, z, None, None, E, 0, 8, score)
+    b = (torch.randint(-2, 3, (E,), generator=g) * 2.0 ** -26).cuda()
+    check(pmpe, z, None, b, E, 0, 8, score)
+    check(pmpe, z, None, b, E, 0, 32, score)
+    check(pmpe, z, None, b, E, 0, 8, score, True, 1.0, (8, 3), (1, 1), "top2")
+    check(pmpe, z, None, None, E, 0, 8, score, True, 1.0, (8, 3), (1, 1), "top2")
+    check(pmpe, z, None, b, E, 0, 8, score, True, 1.0, (8, 3), (1, 1), "max")
+    same = torch.zeros((5, E), device="cuda")
+    check(pmpe, same, None, torch.zeros(E, device="cuda"), E, 0, 8, score)
+    z16 = torch.randn((200, E), generator=g).to(BF16).cuda()  # many true ties
+    check(pmpe, z16, None, torch.zeros(E, device="cuda"), E, 0, 8, score)
+
+
+def test_saturated_sigmoids(pmpe):
+    """Sigmoids that round to 1 in 64 bits too are equal: the lower id."""
+    g = torch.Generator().manual_seed(13)
+    z = (60 * torch.randn((40, 32), generator=g)).cuda()
+    check(pmpe, z, None, torch.zeros(32, device="cuda"), 32, 0, 6, "sigmoid", backward=False)
+
+
+def test_backward_ignores_foreign_ids_and_adds_repeated_ones(pmpe):
+    z, policy, _ = make(6, 16, 8, 2)
+    policy[:] = 0
+    r = pmpe.Router(16, 8, 3, renormalize=False)
+    idx = torch.tensor([[1, 1, 2], [-1, 5, 20], [3, 99, 4], [16, 17, 18], [0, 1, 2], [-7, -1, 15]], dtype=torch.int32).cuda()
+    dw = torch.randn((6, 3), generator=torch.Generator().manual_seed(1)).cuda()
+    d = r.backward(z, policy, idx, dw)
+    torch.cuda.synchronize()
+    rd, size = ref.route_backward(n64(z), host(policy), host(idx), n64(dw), 16, 8, False, False, 1.0)
+    assert (np.abs(n64(d) - rd) <= 2 * REL * size + 1e-30).all()
+
+
+def test_no_tokens_and_refusals(pmpe):
+    r = pmpe.Router(16, 4, 2)
+    z, policy, b = make(3, 16, 4, 1, F32, True)
+    idx, w = r.route(z[:0], policy[:0])
+    assert idx.shape == (0, 2) and w.shape == (0, 2) and r.backward(z[:0], policy[:0], idx, w).shape == (0, 20)
+    good = dict(logits=z, policy=policy, bias=b)
+    for bad in (dict(logits=z[:, :19]), dict(logits=z.double()), dict(logits=z.t().contiguous().t()), dict(policy=policy[:2]),
+                dict(policy=policy.int()), dict(policy=policy.cpu()), dict(bias=b[:19]), dict(bias=b.half()),
+                dict(load=torch.zeros(20, device="cuda")), dict(load=torch.zeros(19, dtype=torch.int32, device="cuda")),
+                dict(logits=z[:1].expand(3, 20))):
+        with pytest.raises(pmpe.PmpeError):
+            r.route(**dict(good, **bad))
+    idx, w = r.route(**good)
+    with pytest.raises(pmpe.PmpeError):
+        r.backward(z, policy, idx.long(), w)
+    with pytest.raises(pmpe.PmpeError):
+        r.backward(z, policy, idx, w[:2])
+    with pytest.raises(pmpe.PmpeError):
+        pmpe.Router(20, 0, 2).route(z, policy)  # a policy without a private pool
+
+
+def test_other_stream_and_graph(pmpe):
+    z, policy, b = make(700, 128, 32, 4, F32, True)
+    r = pmpe.Router(128, 32, 8, score="sigmoid")
+    idx, w = r.route(z, policy, bias=b)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    i2, w2 = r.route(z, policy, bias=b, stream=s)
+    d2 = r.backward(z, policy, i2, w2, stream=s)
+    s.synchronize()
+    assert torch.equal(idx, i2) and torch.equal(w, w2) and torch.equal(d2, r.backward(z, policy, idx, w))
+    load = torch.zeros(160, dtype=torch.int32, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        i3, w3 = r.route(z, policy, bias=b, load=load)
+        d3 = r.backward(z, policy, i3, w3)
+    z.copy_(make(700, 128, 32, 5)[0])
+    g.replay()
+    g.replay()
+    torch.cuda.synchronize()
+    i4, w4 = r.route(z, policy, bias=b)
+    assert torch.equal(i3, i4) and torch.equal(w3, w4) and torch.equal(d3, r.backward(z, policy, i4, w4))
+    assert int(load.sum()) == 2 * 700 * 8

@@ -1,0 +1,213 @@
+"""Refusals of the operators around the layer, and their references' own
+checks: nothing here reaches a CUDA kernel."""
+import ctypes
+import math
+import os
+import shutil
+
+import numpy as np
+import pytest
+import torch
+
+import operators_ref as ref
+
+pytestmark = pytest.mark.skipif(shutil.which("nvcc") is None and not os.path.exists("/usr/local/cuda/bin/nvcc"),
+                                reason="no CUDA toolkit to build the library")
+
+P = 0x10000000  # a device address that is never dereferenced
+
+
+@pytest.fixture(scope="module")
+def pmpe():
+    from paper_2608_06690_gb300 import build
+    build.build()
+    from paper_2608_06690_gb300 import pmpe as m
+    return m
+
+
+def desc(cls, base, **over):
+    d = cls(**dict(base, **over))
+    return ctypes.byref(d)
+
+
+def test_rms_norm_refusals(pmpe):
+    f = pmpe._lib.pmpe_rms_norm
+    base = dict(T=4, H=256, type=1, weight_type=1, quant=0, eps=1e-6, x=P, residual=P, weight=P, x_ld=256, residual_ld=256,
+                h=P, y=P, scale=None, rstd=P)
+
+    def rc(**over):
+        return f(desc(pmpe.RmsNormDesc, base, **over), None)
+
+    assert f(None, None) == pmpe.ERR_INVALID_ARG
+    for bad in (dict(T=-1), dict(H=0), dict(H=-5), dict(type=3), dict(type=-1), dict(weight_type=2), dict(quant=3), dict(quant=-1),
+                dict(eps=0.0), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(x=None), dict(weight=None),
+                dict(y=None), dict(x_ld=255), dict(residual_ld=255), dict(quant=1), dict(scale=P)):
+        assert rc(**bad) == pmpe.ERR_INVALID_ARG, bad
+    for bad in (dict(H=16385, x_ld=16385, residual_ld=16385), dict(x=P + 1), dict(residual=P + 1), dict(h=P + 1), dict(y=P + 1),
+                dict(weight=P + 2, weight_type=0), dict(rstd=P + 2), dict(quant=1, scale=P + 2)):
+        assert rc(**bad) == pmpe.ERR_UNSUPPORTED_SHAPE, bad
+    assert rc(T=0, x=None, weight=None, y=None) == pmpe.OK
+
+
+def test_rms_norm_backward_refusals(pmpe):
+    f, size = pmpe._lib.pmpe_rms_norm_backward, pmpe._lib.pmpe_rms_norm_backward_workspace_size
+    need = size(4, 256)
+    assert need > 0 and size(-1, 256) == 0 and size(4, 0) == 0 and size(4, 16385) == 0 and size(0, 256) > 0
+    assert size(1 << 20, 256) == size(1 << 21, 256)  # bounded: a partial sum a CTA
+    base = dict(T=4, H=256, type=1, weight_type=1, dy_type=0, dx_type=1, dy=P, h=P, weight=P, rstd=P, d_h=P, dx=P, dw=P,
+                workspace=P, workspace_bytes=need)
+
+    def rc(**over):
+        return f(desc(pmpe.RmsNormBackwardDesc, base, **over), None)
+
+    assert f(None, None) == pmpe.ERR_INVALID_ARG
+    for bad in (dict(T=-1), dict(H=0), dict(type=9), dict(weight_type=2), dict(dy_type=2), dict(dx_type=2), dict(dy=None),
+                dict(h=None), dict(weight=None), dict(rstd=None), dict(dx=None)):
+        assert rc(**bad) == pmpe.ERR_INVALID_ARG, bad
+    for bad in (dict(H=16385), dict(dy=P + 2), dict(h=P + 1), dict(d_h=P + 1), dict(dx=P + 1), dict(dw=P + 2), dict(rstd=P + 2)):
+        assert rc(**bad) == pmpe.ERR_UNSUPPORTED_SHAPE, bad
+    for bad in (dict(workspace=None), dict(workspace=P + 8), dict(workspace_bytes=need - 1)):
+        assert rc(**bad) == pmpe.ERR_WORKSPACE, bad
+    assert rc(T=0, dw=None, dy=None, h=None, workspace=None) == pmpe.OK
+
+
+ROUTE = dict(T=4, E_pub=16, E_priv=4, k=2, logits_type=0, score=0, renormalize=1, groups_pub=1, top_groups_pub=1, groups_priv=1,
+             top_groups_priv=1, group_score=0, scale=1.0, logits=P, ld=20, policy=P, bias=P, topk_idx=P, topk_w=P, load=P)
+
+
+def test_route_refusals(pmpe):
+    f = pmpe._lib.pmpe_route
+
+    def rc(**over):
+        return f(desc(pmpe.RouteDesc, ROUTE, **over), None)
+
+    assert f(None, None) == pmpe.ERR_INVALID_ARG
+    for bad in (dict(T=-1), dict(k=0), dict(k=5), dict(E_pub=1), dict(E_priv=-1), dict(E_priv=1), dict(logits_type=3), dict(score=2),
+                dict(score=-1), dict(renormalize=2), dict(scale=math.inf), dict(scale=math.nan), dict(ld=19), dict(logits=None),
+                dict(topk_idx=None), dict(topk_w=None), dict(group_score=2), dict(groups_pub=0), dict(groups_pub=3),
+                dict(groups_pub=4, top_groups_pub=0), dict(groups_pub=4, top_groups_pub=5), dict(groups_pub=33),
+                dict(groups_pub=16, top_groups_pub=1), dict(groups_priv=4, top_groups_priv=1), dict(groups_priv=3),
+                dict(E_priv=0)):  # a policy without a private pool
+        assert rc(**bad) == pmpe.ERR_INVALID_ARG, bad
+    for bad in (dict(E_pub=257, ld=300), dict(E_priv=257, ld=300), dict(E_pub=64, E_priv=64, ld=128, k=33), dict(logits=P + 2),
+                dict(topk_idx=P + 1), dict(topk_w=P + 2), dict(bias=P + 2), dict(load=P + 2)):
+        assert rc(**bad) == pmpe.ERR_UNSUPPORTED_SHAPE, bad
+    assert rc(T=0, logits=None, topk_idx=None, topk_w=None) == pmpe.OK
+    assert rc(T=0, E_priv=0, policy=None, groups_priv=0) == pmpe.OK
+    with pytest.raises(pmpe.PmpeError):
+        pmpe.Router(16, 4, 5)
+    with pytest.raises(pmpe.PmpeError):
+        pmpe.Router(16, 4, 2, score="tanh")
+    with pytest.raises(pmpe.PmpeError):
+        pmpe.Router(16, 4, 2, group_score="mean")
+    with pytest.raises(pmpe.PmpeError):
+        pmpe.Router(16, 4, 2, groups=(5, 1))
+
+
+def test_route_backward_refusals(pmpe):
+    f = pmpe._lib.pmpe_route_backward
+
+    def rc(dw=P, d_logits=P, **over):
+        return f(desc(pmpe.RouteDesc, ROUTE, **over), dw, d_logits, None)
+
+    for bad in (dict(dw=None), dict(d_logits=None), dict(k=0), dict(T=-1), dict(ld=3), dict(topk_idx=None)):
+        assert rc(**bad) == pmpe.ERR_INVALID_ARG, bad
+    for bad in (dict(dw=P + 2), dict(d_logits=P + 2), dict(d_logits=P + 1, logits_type=1)):
+        assert rc(**bad) == pmpe.ERR_UNSUPPORTED_SHAPE, bad
+    assert rc(T=0, dw=None, d_logits=None, logits=None, topk_idx=None) == pmpe.OK
+
+
+def test_clip_refusals(pmpe):
+    f, size = pmpe._lib.pmpe_clip_grad_norm, pmpe._lib.pmpe_clip_workspace_size
+    assert size(-1) == 0 and size(0) > 0 and size(5000) > size(5)
+
+    def rc(tensors, max_norm=1.0, norm=P, ws=P, nb=None, n=None):
+        table = (pmpe.Grad * max(1, len(tensors)))(*tensors)
+        return f(table, len(tensors) if n is None else n, max_norm, norm, ws, size(len(tensors)) if nb is None else nb, None)
+
+    ok = (P, None, 1000, 0)
+    assert f(None, 1, 1.0, P, P, 1 << 20, None) == pmpe.ERR_INVALID_ARG
+    assert rc([ok], n=-1) == pmpe.ERR_INVALID_ARG
+    assert rc([ok], max_norm=-1.0) == pmpe.ERR_INVALID_ARG
+    assert rc([ok], max_norm=math.nan) == pmpe.ERR_INVALID_ARG
+    assert rc([ok], norm=None) == pmpe.ERR_INVALID_ARG
+    assert rc([(P, None, -1, 0)]) == pmpe.ERR_INVALID_ARG
+    assert rc([(P, None, 4, 7)]) == pmpe.ERR_INVALID_ARG
+    assert rc([(None, None, 4, 0)]) == pmpe.ERR_INVALID_ARG
+    assert rc([ok, ok]) == pmpe.ERR_INVALID_ARG                                # the same tensor twice
+    assert rc([ok, (P + 3996, None, 10, 0)]) == pmpe.ERR_INVALID_ARG           # the last element shared
+    assert rc([ok, (P + 8000, P + 400, 10, 0)]) == pmpe.ERR_INVALID_ARG        # an output inside another gradient
+    assert rc([(P, P + 4, 1000, 0)]) == pmpe.ERR_INVALID_ARG                   # an output that overlaps its own gradient
+    assert rc([(P + 2, None, 4, 0)]) == pmpe.ERR_UNSUPPORTED_SHAPE
+    assert rc([(P, P + 0x100001, 4, 1)]) == pmpe.ERR_UNSUPPORTED_SHAPE
+    assert rc([(P, None, 1 << 45, 0)]) == pmpe.ERR_UNSUPPORTED_SHAPE
+    assert rc([(P, None, 1 << 44, 0)]) == pmpe.ERR_INVALID_ARG                 # more chunks than a launch counts
+    assert rc([ok], norm=P + 0x100002) == pmpe.ERR_UNSUPPORTED_SHAPE
+    assert rc([ok], ws=None) == pmpe.ERR_WORKSPACE
+    assert rc([ok], ws=P + 0x100008) == pmpe.ERR_WORKSPACE
+    assert rc([ok], nb=size(1) - 1) == pmpe.ERR_WORKSPACE
+
+
+def test_host_tensors_are_refused(pmpe):
+    x, w = torch.zeros(2, 8), torch.ones(8)
+    for call in (lambda: pmpe.rms_norm(x, w), lambda: pmpe.rms_norm_backward(x, x, w, torch.ones(2)),
+                 lambda: pmpe.Router(8, 0, 2).route(x), lambda: pmpe.clip_grad_norm([x], 1.0), lambda: pmpe.clip_grad_norm([], 1.0),
+                 lambda: pmpe.clip_grad_norm({"a": x}, 1.0, out={"b": x})):
+        with pytest.raises(pmpe.PmpeError):
+            call()
+
+
+# ------------------------------------------------ the references themselves
+
+def test_reference_norm_gradient_against_differences():
+    rng = np.random.default_rng(0)
+    h, w, dy, dh = rng.normal(size=(3, 7)), rng.normal(size=7), rng.normal(size=(3, 7)), rng.normal(size=(3, 7))
+    eps, step = 1e-3, 1e-6
+
+    def loss(h, w):
+        return (ref.rms_norm(h, w, eps)[0] * dy).sum() + (h * dh).sum()
+
+    dx, dw, _, _ = ref.rms_norm_backward(dy, h, w, ref.rms_norm(h, w, eps)[1], dh)
+    for i in np.ndindex(h.shape):
+        e = np.zeros_like(h)
+        e[i] = step
+        assert abs((loss(h + e, w) - loss(h - e, w)) / (2 * step) - dx[i]) < 1e-7  # step^2 f''' / 6 + 2^-52 |f| / step
+    for i in range(7):
+        e = np.zeros_like(w)
+        e[i] = step
+        assert abs((loss(h, w + e) - loss(h, w - e)) / (2 * step) - dw[i]) < 1e-7
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_reference_route_gradient_against_differences(sigmoid, renorm):
+    rng = np.random.default_rng(1)
+    z, policy = rng.normal(size=(3, 9)), np.array([0, 1, 7], np.uint8)
+    idx, _ = ref.route(z, policy, 5, 4, 3, sigmoid, renorm, 2.5)
+    dw = rng.normal(size=(3, 3))
+    d, _ = ref.route_backward(z, policy, idx, dw, 5, 4, sigmoid, renorm, 2.5)
+
+    def loss(z):
+        total = 0.0
+        for t in range(3):
+            lo, hi = ref.pool_of(t, policy, 5, 4)
+            total += (ref.weights(z[t, lo:hi], idx[t] - lo, sigmoid, renorm, 2.5) * dw[t]).sum()
+        return total
+
+    for i in np.ndindex(z.shape):
+        e = np.zeros_like(z)
+        e[i] = 1e-6
+        assert abs((loss(z + e) - loss(z - e)) / 2e-6 - d[i]) < 1e-7
+
+
+def test_reference_route_by_hand():
+    z = np.array([[0.0, 2.0, 2.0, -np.inf, 1.0, 3.0]])
+    idx, w = ref.route(z, None, 6, 0, 3)
+    assert idx.tolist() == [[5, 1, 2]]  # equal logits by the lower id
+    assert np.allclose(w, np.exp([[3, 2, 2]]) / np.exp([3, 2, 2]).sum())
+    idx, _ = ref.route(z, None, 6, 0, 2, groups=(3, 1))  # groups {0, 1}, {2, -}, {1, 3}: the last by its best
+    assert idx.tolist() == [[5, 4]]
+    idx, _ = ref.route(z, None, 6, 0, 2, sigmoid=True, groups=(3, 1), top2=True, bias=np.array([9.0, 0, 0, 0, 0, 0]))
+    assert idx.tolist() == [[0, 1]]
+    idx, w = ref.route(np.full((1, 6), -np.inf), None, 6, 0, 2)
+    assert idx.tolist() == [[-1, -1]] and w.tolist() == [[0.0, 0.0]]
