@@ -51,24 +51,28 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8], __half)
     return u;
 }
 
-// Eight consecutive elements at p, as loaded: the loads of several operands
-// are issued before the first is unpacked.
+// Eight elements of a row in a thread.  kVec: consecutive ones at p, which is
+// aligned for 16-byte accesses; n > 0: they exist (rows hold whole chunks).
+// Otherwise p, p + 32, ..., so that a warp's accesses are contiguous one
+// element at a time; n: elements from p to the row's end.  What does not exist
+// reads as zero.
 template <typename T> struct Raw8 { uint4 u; };
-template <> struct Raw8<float> { float4 lo, hi; };
+template <> struct Raw8<float> { uint4 u, hi; };
 
-// kVec: p is aligned for 16-byte accesses; otherwise element by element.
-// n: how many of the eight exist (the others read as zeros).
 template <bool kVec> __device__ __forceinline__ void load8(Raw8<float> &r, const float *p, int n)
 {
     if (kVec) {
-        r.lo = r.hi = make_float4(0.f, 0.f, 0.f, 0.f);
+        r.u = r.hi = make_uint4(0u, 0u, 0u, 0u);
         if (n > 0) {
-            r.lo = reinterpret_cast<const float4 *>(p)[0];
-            r.hi = reinterpret_cast<const float4 *>(p)[1];
+            r.u = reinterpret_cast<const uint4 *>(p)[0];
+            r.hi = reinterpret_cast<const uint4 *>(p)[1];
         }
     } else {
-        r.lo = make_float4(n > 0 ? p[0] : 0.f, n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, n > 3 ? p[3] : 0.f);
-        r.hi = make_float4(n > 4 ? p[4] : 0.f, n > 5 ? p[5] : 0.f, n > 6 ? p[6] : 0.f, n > 7 ? p[7] : 0.f);
+        uint32_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = 32 * i < n ? __float_as_uint(p[32 * i]) : 0u;
+        r.u = make_uint4(q[0], q[1], q[2], q[3]);
+        r.hi = make_uint4(q[4], q[5], q[6], q[7]);
     }
 }
 template <bool kVec, typename T> __device__ __forceinline__ void load8(Raw8<T> &r, const T *p, int n)
@@ -77,18 +81,17 @@ template <bool kVec, typename T> __device__ __forceinline__ void load8(Raw8<T> &
         r.u = make_uint4(0u, 0u, 0u, 0u);
         if (n > 0) r.u = *reinterpret_cast<const uint4 *>(p);
     } else {
-        uint32_t q[4];
+        uint32_t q[8];
         const uint16_t *s = reinterpret_cast<const uint16_t *>(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            q[i] = (n > 2 * i ? s[2 * i] : 0u) | (uint32_t)(n > 2 * i + 1 ? s[2 * i + 1] : 0u) << 16;
-        r.u = make_uint4(q[0], q[1], q[2], q[3]);
+        for (int i = 0; i < 8; ++i) q[i] = 32 * i < n ? s[32 * i] : 0u;
+        r.u = make_uint4(q[0] | q[1] << 16, q[2] | q[3] << 16, q[4] | q[5] << 16, q[6] | q[7] << 16);
     }
 }
 __device__ __forceinline__ void unpack(const Raw8<float> &r, float (&v)[8])
 {
-    v[0] = r.lo.x; v[1] = r.lo.y; v[2] = r.lo.z; v[3] = r.lo.w;
-    v[4] = r.hi.x; v[5] = r.hi.y; v[6] = r.hi.z; v[7] = r.hi.w;
+    v[0] = __uint_as_float(r.u.x); v[1] = __uint_as_float(r.u.y); v[2] = __uint_as_float(r.u.z); v[3] = __uint_as_float(r.u.w);
+    v[4] = __uint_as_float(r.hi.x); v[5] = __uint_as_float(r.hi.y); v[6] = __uint_as_float(r.hi.z); v[7] = __uint_as_float(r.hi.w);
 }
 template <typename T> __device__ __forceinline__ void unpack(const Raw8<T> &r, float (&v)[8]) { unpack8(r.u, v, T()); }
 
@@ -103,7 +106,7 @@ template <bool kVec> __device__ __forceinline__ void store8(float *p, const floa
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < n) p[i] = v[i];
+            if (32 * i < n) p[32 * i] = v[i];
     }
 }
 template <bool kVec, typename T> __device__ __forceinline__ void store8(T *p, const float (&v)[8], int n)
@@ -113,8 +116,71 @@ template <bool kVec, typename T> __device__ __forceinline__ void store8(T *p, co
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < n) p[i] = from_f32<T>(v[i]);
+            if (32 * i < n) p[32 * i] = from_f32<T>(v[i]);
     }
+}
+
+// Sums rounded once to the type: two 16-bit elements an instruction.
+__device__ __forceinline__ void add8(Raw8<float> &r, const Raw8<float> &q)
+{
+    float a[8], b[8];
+    unpack(r, a);
+    unpack(q, b);
+    r.u = make_uint4(__float_as_uint(a[0] + b[0]), __float_as_uint(a[1] + b[1]), __float_as_uint(a[2] + b[2]), __float_as_uint(a[3] + b[3]));
+    r.hi = make_uint4(__float_as_uint(a[4] + b[4]), __float_as_uint(a[5] + b[5]), __float_as_uint(a[6] + b[6]), __float_as_uint(a[7] + b[7]));
+}
+__device__ __forceinline__ void add8(Raw8<bf16> &r, const Raw8<bf16> &q)
+{
+    __nv_bfloat162 *a = reinterpret_cast<__nv_bfloat162 *>(&r.u);
+    const __nv_bfloat162 *b = reinterpret_cast<const __nv_bfloat162 *>(&q.u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __hadd2_rn(a[i], b[i]);
+}
+__device__ __forceinline__ void add8(Raw8<__half> &r, const Raw8<__half> &q)
+{
+    __half2 *a = reinterpret_cast<__half2 *>(&r.u);
+    const __half2 *b = reinterpret_cast<const __half2 *>(&q.u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __hadd2_rn(a[i], b[i]);
+}
+
+// The words as they are.
+template <bool kVec> __device__ __forceinline__ void store_raw(float *p, const Raw8<float> &r, int n)
+{
+    float v[8];
+    unpack(r, v);
+    store8<kVec>(p, v, n);
+}
+template <bool kVec, typename T> __device__ __forceinline__ void store_raw(T *p, const Raw8<T> &r, int n)
+{
+    if (kVec) {
+        if (n > 0) *reinterpret_cast<uint4 *>(p) = r.u;
+    } else {
+        const uint32_t q[4] = {r.u.x, r.u.y, r.u.z, r.u.w};
+        uint16_t *s = reinterpret_cast<uint16_t *>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (32 * i < n) s[32 * i] = (uint16_t)(q[i >> 1] >> 16 * (i & 1));
+    }
+}
+
+// Two FP32 operations an instruction, each rounded as by itself.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long &>(r))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long &>(r))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)),
+          "l"(reinterpret_cast<unsigned long long &>(c)));
+    return r;
 }
 
 template <typename V> __device__ __forceinline__ V warp_sum(V v)

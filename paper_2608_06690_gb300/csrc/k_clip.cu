@@ -12,9 +12,11 @@
 // is read by each, and written once.  The second takes the chunks from last
 // to first, so that it finds in L2 what the first read last.
 //
-// Squares are FP32 products of a thread's vector, which are added in 64 bits;
-// a vector whose sum of squares leaves 2^-80 .. 2^100 (values that would
-// overflow or vanish when squared) is summed in 64 bits from the start.
+// A vector's squares are summed in FP32, the vectors' sums in pairs of FP32
+// words (a value and what its rounding lost, 48 bits: FP64 adds, two a clock
+// and SM, took longer than the small cases' loads).  A vector whose sum of
+// squares leaves 2^-120 .. 2^90 (values that overflow or vanish when squared)
+// goes to a 64-bit sum instead, which exists in the CTAs that met one.
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>
@@ -28,8 +30,10 @@ namespace {
 constexpr int kClipThreads = 256;
 constexpr int kClipVecs = 4;                                   // 16-byte vectors of a thread and chunk
 constexpr int kChunkBytes = kClipThreads * kClipVecs * 16;
-constexpr int kClipCtasPerSm = 4;
+constexpr int kClipCtasPerSm = 8;
+constexpr int kScaleCtasPerSm = 5;  // its registers allow no more
 constexpr int kClipMaxCtas = 152 * kClipCtasPerSm;
+constexpr int kScaleMaxCtas = 152 * kScaleCtasPerSm;
 
 // The tensors of a launch.  first[i]: chunks before tensor i.
 template <int kCap> struct ClipTable {
@@ -82,21 +86,71 @@ __device__ __forceinline__ void store_one(void *p, long long i, int type, float 
     else ((__half *)p)[i] = from_f32<__half>(v);
 }
 
-// Adds the squares of a vector: fast holds sums that FP32 holds well.
-__device__ __forceinline__ void add_squares(const float (&v)[8], float &fast, double &acc)
+// A sum of FP32 values and what its roundings lost.
+struct Sum2 {
+    float hi, lo;
+};
+__device__ __forceinline__ void add2(Sum2 &s, float v)
 {
-    float s = 0.f, m = 0.f;
+    const float t = s.hi + v, bb = t - s.hi;
+    s.lo += (s.hi - (t - bb)) + (v - bb);
+    s.hi = t;
+}
+
+// What a CTA (or all of them) found: the pair, and the 64-bit sum of the rest.
+struct Squares {
+    Sum2 s;
+    double rare;
+};
+
+// The squares of a vector, added to the sums.
+__device__ __forceinline__ void add_squares(const float (&v)[8], float &fast, double &rare)
+{
+    float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        s += v[i] * v[i];
-        m = fmaxf(m, fabsf(v[i]));
-    }
-    if (s >= 0x1p-80f && s < 0x1p100f) {
+    for (int i = 0; i < 8; ++i) s += v[i] * v[i];
+    if (s >= 0x1p-120f && s < 0x1p90f) {
         fast += s;
-    } else if (m > 0.f || !(s == 0.f)) {
+    } else {
+        uint32_t any = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc += (double)v[i] * v[i];
+        for (int i = 0; i < 8; ++i) any |= __float_as_uint(v[i]);
+        if (any << 1) {  // zeros stay here
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rare += (double)v[i] * v[i];
+        }
     }
+}
+
+// The sums over the CTA's threads, in a fixed order, in all of them.
+__device__ __forceinline__ Squares cta_sum(Sum2 s, double rare)
+{
+    __shared__ Sum2 s_sum[kClipThreads / 32];
+    __shared__ double s_rare[kClipThreads / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        const float hi = __shfl_xor_sync(~0u, s.hi, off), lo = __shfl_xor_sync(~0u, s.lo, off);
+        add2(s, hi);
+        s.lo += lo;
+    }
+    if (lane == 0) s_sum[warp] = s;
+    const int any = __syncthreads_or(!(rare == 0.));  // NaN too
+    Squares r;
+    r.s = s_sum[0];
+    r.rare = 0.;
+#pragma unroll
+    for (int w = 1; w < kClipThreads / 32; ++w) {
+        add2(r.s, s_sum[w].hi);
+        r.s.lo += s_sum[w].lo;
+    }
+    if (any) {
+        rare = warp_sum(rare);
+        if (lane == 0) s_rare[warp] = rare;
+        __syncthreads();
+        for (int w = 0; w < kClipThreads / 32; ++w) r.rare += s_rare[w];
+    }
+    return r;
 }
 
 // The tensor of chunk c.
@@ -112,16 +166,18 @@ template <int kCap> __device__ __forceinline__ int tensor_of(const ClipTable<kCa
 }
 
 template <int kCap>
-__global__ void __launch_bounds__(kClipThreads) clip_squares_kernel(const __grid_constant__ ClipTable<kCap> tab, double *partial)
+__global__ void __launch_bounds__(kClipThreads, kClipCtasPerSm) clip_squares_kernel(const __grid_constant__ ClipTable<kCap> tab, Squares *partial)
 {
-    __shared__ double s_red[kClipThreads / 32];
     pdl_trigger();
     pdl_wait();
     const int tid = threadIdx.x;
-    double acc = 0.;
+    Sum2 sum = {0.f, 0.f};
+    double rare = 0.;
     const uint32_t chunks = tab.first[tab.count];
+    int i = 0;
     for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int i = tensor_of(tab, c), type = tab.type[i], b = elem_bytes(type);
+        if (c < tab.first[i] || c >= tab.first[i + 1]) i = tensor_of(tab, c);
+        const int type = tab.type[i], b = elem_bytes(type);
         const void *g = tab.g[i];
         const long long n = tab.n[i], head = head_of(g, n, b), vecs = (n - head) * b / 16;
         const uint4 *body = reinterpret_cast<const uint4 *>((const uint8_t *)g + head * b);
@@ -136,57 +192,56 @@ __global__ void __launch_bounds__(kClipThreads) clip_squares_kernel(const __grid
 #pragma unroll
         for (int q = 0; q < kClipVecs; ++q) {
             unpack_vec(u[q], type, v);
-            add_squares(v, fast, acc);
+            add_squares(v, fast, rare);
         }
-        acc += fast;
         if (v0 == 0) {  // what the vectors leave: fewer than 16 bytes before and after them
             const long long tail = head + vecs * (16 / b);
-            if (tid < head) {
-                const double x = load_one(g, tid, type);
-                acc += x * x;
-            }
-            if (tid < n - tail) {
-                const double x = load_one(g, tail + tid, type);
-                acc += x * x;
-            }
-        }
-    }
-    acc = warp_sum(acc);
-    if ((tid & 31) == 0) s_red[tid >> 5] = acc;
-    __syncthreads();
-    if (tid == 0) {
-        double a = 0.;
 #pragma unroll
-        for (int w = 0; w < kClipThreads / 32; ++w) a += s_red[w];
-        partial[blockIdx.x] = a;
+            for (int j = 0; j < 8; ++j) v[j] = 0.f;
+            if (tid < head) v[0] = load_one(g, tid, type);
+            if (tid < n - tail) v[1] = load_one(g, tail + tid, type);
+            if (tid < 8) add_squares(v, fast, rare);
+        }
+        add2(sum, fast);
     }
+    const Squares r = cta_sum(sum, rare);
+    if (tid == 0) partial[blockIdx.x] = r;
 }
 
 template <int kCap>
-__global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_constant__ ClipTable<kCap> tab,
-                                                                  const double *partial, int n_partial, float max_norm,
+__global__ void __launch_bounds__(kClipThreads, kScaleCtasPerSm) clip_scale_kernel(const __grid_constant__ ClipTable<kCap> tab,
+                                                                  const Squares *partial, int n_partial, float max_norm,
                                                                   float *norm_out)
 {
-    __shared__ double s_red[kClipThreads / 32];
     pdl_trigger();
     pdl_wait();
     const int tid = threadIdx.x;
-    double acc = 0.;
-    for (int i = tid; i < n_partial; i += kClipThreads) acc += partial[i];
-    acc = warp_sum(acc);
-    if ((tid & 31) == 0) s_red[tid >> 5] = acc;
-    __syncthreads();
-    acc = 0.;
-#pragma unroll
-    for (int w = 0; w < kClipThreads / 32; ++w) acc += s_red[w];
-    const double norm = sqrt(acc);
+    Sum2 sum = {0.f, 0.f};
+    double rare = 0.;
+    for (int i = tid; i < n_partial; i += kClipThreads) {
+        const Squares q = partial[i];
+        add2(sum, q.s.hi);
+        sum.lo += q.s.lo;
+        rare += q.rare;
+    }
+    const Squares all = cta_sum(sum, rare);
     // a norm that is not finite clips nothing: the caller sees it and drops the step
-    const float f = isfinite(norm) ? (float)fmin(1., (double)max_norm / (norm + 1e-6)) : 1.f;
-    if (norm_out && blockIdx.x == 0 && tid == 0) *norm_out = (float)norm;
+    float norm, f = 1.f;
+    if (all.rare == 0.) {
+        norm = sqrtf(all.s.hi + all.s.lo);
+        f = fminf(1.f, max_norm / (norm + 1e-6f));
+    } else {
+        const double n64 = sqrt((double)all.s.hi + all.s.lo + all.rare);
+        norm = (float)n64;
+        if (isfinite(n64)) f = (float)fmin(1., max_norm / (n64 + 1e-6));
+    }
+    if (blockIdx.x == 0 && tid == 0 && norm_out) *norm_out = norm;
+    int i = tab.count - 1;
     const uint32_t chunks = tab.first[tab.count];
     for (uint32_t k = blockIdx.x; k < chunks; k += gridDim.x) {
         const uint32_t c = chunks - 1 - k;
-        const int i = tensor_of(tab, c), type = tab.type[i], b = elem_bytes(type);
+        if (c < tab.first[i] || c >= tab.first[i + 1]) i = tensor_of(tab, c);
+        const int type = tab.type[i], b = elem_bytes(type);
         const void *g = tab.g[i];
         void *o = tab.o[i];
         if (f == 1.f && g == o) continue;
@@ -199,7 +254,7 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_c
 #pragma unroll
         for (int q = 0; q < kClipVecs; ++q) {
             const long long at = v0 + q * kClipThreads + tid;
-            u[q] = at < vecs ? body[at] : make_uint4(0u, 0u, 0u, 0u);
+            u[q] = at < vecs ? __ldcs(body + at) : make_uint4(0u, 0u, 0u, 0u);
         }
 #pragma unroll
         for (int q = 0; q < kClipVecs; ++q) {
@@ -229,7 +284,7 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_c
 }
 
 template <int kCap>
-cudaError_t clip_tables(const pmpe_grad *g, int n, float max_norm, float *norm_out, double *partial, cudaStream_t st, int phase,
+cudaError_t clip_tables(const pmpe_grad *g, int n, float max_norm, float *norm_out, Squares *partial, cudaStream_t st, int phase,
                         int n_partial_all)
 {
     int parts = 0;
@@ -250,8 +305,8 @@ cudaError_t clip_tables(const pmpe_grad *g, int n, float max_norm, float *norm_o
         const int grid = (int)std::max<uint32_t>(1u, std::min<uint32_t>(chunks, (uint32_t)kClipMaxCtas));
         const cudaError_t err =
             phase == 0 ? launch_pdl(clip_squares_kernel<kCap>, dim3(grid), dim3(kClipThreads), 0, st, tab, partial + parts)
-                       : launch_pdl(clip_scale_kernel<kCap>, dim3(grid), dim3(kClipThreads), 0, st, tab, (const double *)partial,
-                                    n_partial_all, max_norm, at == 0 ? norm_out : (float *)nullptr);
+                       : launch_pdl(clip_scale_kernel<kCap>, dim3(std::min(grid, kScaleMaxCtas)), dim3(kClipThreads), 0, st, tab,
+                                    (const Squares *)partial, n_partial_all, max_norm, at == 0 ? norm_out : (float *)nullptr);
         if (err != cudaSuccess) return err;
         parts += grid;
     }
@@ -273,7 +328,7 @@ template <int kCap> int count_partials(const pmpe_grad *g, int n)
 
 size_t clip_workspace_bytes(int n)
 {
-    return (size_t)std::max(1, (n + kLargeTable - 1) / kLargeTable) * kClipMaxCtas * sizeof(double);
+    return (size_t)std::max(1, (n + kLargeTable - 1) / kLargeTable) * kClipMaxCtas * sizeof(Squares);
 }
 
 // Whether no two of the tensors (gradients and outputs, a gradient and its
@@ -300,8 +355,9 @@ int clip_tensors_ok(const pmpe_grad *g, int n)
     return ok ? 1 : 0;
 }
 
-cudaError_t launch_clip(const pmpe_grad *g, int n, float max_norm, float *norm_out, double *partial, cudaStream_t st)
+cudaError_t launch_clip(const pmpe_grad *g, int n, float max_norm, float *norm_out, void *workspace, cudaStream_t st)
 {
+    Squares *partial = static_cast<Squares *>(workspace);
     // the table is copied into every launch's arguments: 1.9 KB or 30 KB
     const bool small = n <= kSmallTable;
     const int parts = small ? count_partials<kSmallTable>(g, n) : count_partials<kLargeTable>(g, n);

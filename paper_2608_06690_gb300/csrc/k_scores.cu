@@ -13,16 +13,18 @@
 //   k experts are eligible
 //
 // A warp takes a token: lane l holds kV consecutive experts of the pool, so a
-// row is read once with one vector load a lane, and each of the k rounds is
-// one redux over order-preserving 32-bit keys, a ballot and an update in the
-// winner's lane.
+// row is read once with one vector load a lane.  A lane orders its experts
+// once; each of the k rounds is then one redux over packed words (24 bits of
+// the choice, 8 of the expert) and a shift in the winner's lane.
 //
-// The selection is that of exact arithmetic.  Logits compare exactly.
-// Choices with a bias are FP32, a few 2^-24 off: where two choices that
-// follow one another in the order (or two groups at the limit) lie within
-// the bound of that error, the warp selects again with 64-bit choices.  That
-// is about one token in a thousand; a 64-bit exponential for every expert
-// would cost more than everything else here (2 FP64 operations a clock and SM).
+// The selection is that of exact arithmetic.  Where two neighbours in the
+// order have equal packed words, the warp selects again by the whole choices
+// (about one token in a hundred with FP32 logits).  Logits compare exactly;
+// choices with a bias are FP32, a few 2^-24 off: where neighbours (or two
+// groups at the limit) lie within the bound of that error, about one token in
+// a thousand, the experts in question are evaluated in 64 bits, one a lane,
+// and compared as integers: an FP64 instruction takes a warp some 60 clocks
+// here, and a selection wholly in FP64 was 16 us.
 #include <algorithm>
 
 #include "elem.cuh"
@@ -52,7 +54,7 @@ __device__ __forceinline__ uint32_t key_of(float x)
     const uint32_t u = __float_as_uint(x + 0.f);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float of_key(uint32_t key)
+__device__ __forceinline__ float of(uint32_t key)
 {
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
@@ -60,122 +62,280 @@ __device__ __forceinline__ float of_key(uint32_t key)
 constexpr float kNone = -INFINITY;
 constexpr float kLargest = 3.402823466e38f;  // stands for a logit of +inf
 
-// The largest value over the warp and the lowest expert that has it.
-__device__ __forceinline__ void warp_best(float &v, int &e)
+// The same for 64-bit values, compared as integers: FP64 compares are as slow
+// as its arithmetic.
+typedef unsigned long long u64;
+__device__ __forceinline__ u64 key64(double x)
 {
-    const uint32_t key = e < 0 ? 0u : key_of(v);
-    const uint32_t best = __reduce_max_sync(~0u, key);
-    // experts ascend with the lanes, so the lowest lane holds the lowest expert
-    const int src = __ffs(__ballot_sync(~0u, key == best)) - 1;
-    e = __shfl_sync(~0u, best ? e : -1, src);
-    v = best ? of_key(best) : kNone;
+    const long long u = __double_as_longlong(x);
+    return (u64)u ^ ((u64)(u >> 63) | 0x8000000000000000ull);
 }
-__device__ __forceinline__ void warp_best(double &v, int &e)
+__device__ __forceinline__ double of(u64 key)
 {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        const double ov = __shfl_xor_sync(~0u, v, off);
-        const int oe = __shfl_xor_sync(~0u, e, off);
-        const bool take = oe >= 0 && (e < 0 || ov > v || (ov == v && oe < e));
-        v = take ? ov : v;
-        e = take ? oe : e;
-    }
+    return __longlong_as_double((long long)(key >> 63 ? key ^ 0x8000000000000000ull : ~key));
+}
+__device__ __forceinline__ u64 warp_max64(u64 v)
+{
+    const uint32_t hi = (uint32_t)(v >> 32), top = __reduce_max_sync(~0u, hi);
+    return (u64)top << 32 | __reduce_max_sync(~0u, hi == top ? (uint32_t)v : 0u);
 }
 
-// Whether a group's value a of group i ranks above b of group j.
-template <typename V> __device__ __forceinline__ bool group_above(V a, int i, V b, int j)
+// A token's pool: what its selection goes by.
+template <typename T> struct Pool {
+    const T *row;       // the pool's logits
+    const float *bias;  // and biases, or null
+    int E, sigmoid, n, top, top2, k;
+};
+
+// Where the exact values are needed, and what FP32 already knows.
+struct Exact {
+    float mx;  // the largest logit (softmax)
+    double sum;
+};
+
+template <typename T> __device__ __forceinline__ float logit(const Pool<T> &p, int e) { return fminf(to_f32(p.row[e]), kLargest); }
+// score + bias in 64 bits.
+template <typename T> __device__ __forceinline__ double exact_value(const Pool<T> &p, const Exact &x, int e)
 {
-    return a > b || (a == b && i < j);
+    const double z = logit(p, e);
+    const double s = p.sigmoid ? 1. / (1. + exp(-z)) : exp(z - x.mx) / x.sum;
+    return p.bias ? s + p.bias[e] : s;
+}
+// The softmax's sum in 64 bits (sigmoid: nothing).
+template <typename T> __device__ __noinline__ double exact_sum(const Pool<T> &p, float mx, int lane)
+{
+    double s = 0.;
+    for (int e = lane; e < p.E; e += 32) {
+        const float z = to_f32(p.row[e]);
+        if (z > kNone) s += exp((double)fminf(z, kLargest) - mx);
+    }
+    return warp_sum(s);
 }
 
 // The two largest values seen, best first; kNone where there are fewer.
-template <typename V> __device__ __forceinline__ void add_two(V &first, V &second, V v)
+__device__ __forceinline__ void add_two(float &first, float &second, float v)
 {
-    second = v > first ? first : (v > second ? v : second);
-    first = v > first ? v : first;
+    second = fmaxf(second, fminf(first, v));
+    first = fmaxf(first, v);
 }
 
-// Clears the candidates (choice -> -inf) outside the best `top` of n groups of
-// `size` experts.  val: score + bias, what two-best sums are made of.  Lane l
-// computes group l's value (n <= 32).  gap: the distance between the last
-// group kept and the first one dropped (+inf where nothing is dropped).
-template <typename V, int kV>
-__device__ __forceinline__ void limit_groups(V (&choice)[kV], const V (&val)[kV], int n, int size, int top, int top2, int lane,
-                                             V &gap)
+// Moves the experts whose bit in `wanted` is set (lane l, bit i: expert l kV +
+// i) to a lane each; returns how many there are (above 32: too many).  list:
+// 32 words of the warp's own.
+template <int kV> __device__ __forceinline__ int gather(uint32_t wanted, int lane, int *list, int &e)
 {
-    const V none = (V)kNone;
-    V mine = none;
-    for (int g = 0; g < n; ++g) {
-        V a = none, b = none;
-#pragma unroll
-        for (int i = 0; i < kV; ++i) {
-            const int e = lane * kV + i;
-            const V c = e >= g * size && e < (g + 1) * size && choice[i] > none ? (top2 ? val[i] : choice[i]) : none;
-            add_two(a, b, c);
-        }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) {
-            const V oa = __shfl_xor_sync(~0u, a, off), ob = __shfl_xor_sync(~0u, b, off);
-            add_two(a, b, oa);
-            add_two(a, b, ob);
-        }
-        if (top2 && b > none) a += b;
-        if (lane == g) mine = a;
-    }
-    // rank of each group; the smallest kept and the largest dropped value
-    int rank = 0;
-    for (int g = 0; g < n; ++g) {
-        const V o = __shfl_sync(~0u, mine, g);
-        rank += group_above(o, g, mine, lane) ? 1 : 0;
-    }
-    const uint32_t kept = __ballot_sync(~0u, lane < n && rank < top);
-    const uint32_t last = __ballot_sync(~0u, lane < n && rank == top - 1);
-    const uint32_t next = __ballot_sync(~0u, lane < n && rank == top);
-    gap = (V)INFINITY;
-    if (next) {
-        const V a = __shfl_sync(~0u, mine, __ffs(last) - 1), b = __shfl_sync(~0u, mine, __ffs(next) - 1);
-        if (b > none) gap = a - b;
-    }
+    int count = 0;
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-        const int e = lane * kV + i;
-        if (e < n * size && !((kept >> (e / size)) & 1u)) choice[i] = none;
+        const uint32_t who = __ballot_sync(~0u, (wanted >> i) & 1u);
+        const int at = count + __popc(who & ((1u << lane) - 1u));
+        if (((wanted >> i) & 1u) && at < 32) list[at] = lane * kV + i;
+        count += __popc(who);
+    }
+    __syncwarp();
+    e = lane < count ? list[lane] : -1;
+    __syncwarp();
+    return count;
+}
+
+// A lane's place among the lanes with a key (0: none): larger keys first,
+// equal ones by the lower id.
+__device__ __forceinline__ int place_of(u64 key, int id, int count)
+{
+    int place = 0;
+    for (int j = 0; j < count; ++j) {
+        const u64 o = __shfl_sync(~0u, key, j);
+        const int oi = __shfl_sync(~0u, id, j);
+        place += o > key || (o == key && oi < id) ? 1 : 0;
+    }
+    return place;
+}
+
+// Orders a lane's packed choices, largest first.
+template <int kV> __device__ __forceinline__ void sort_lane(uint32_t (&v)[kV])
+{
+    auto cex = [&](int i, int j) {
+        const uint32_t hi = max(v[i], v[j]), lo = min(v[i], v[j]);
+        v[i] = hi;
+        v[j] = lo;
+    };
+    if constexpr (kV == 2) {
+        cex(0, 1);
+    } else if constexpr (kV == 4) {
+        cex(0, 1); cex(2, 3); cex(0, 2); cex(1, 3); cex(1, 2);
+    } else if constexpr (kV == 8) {
+        cex(0, 1); cex(2, 3); cex(4, 5); cex(6, 7);
+        cex(0, 2); cex(1, 3); cex(4, 6); cex(5, 7);
+        cex(1, 2); cex(5, 6);
+        cex(0, 4); cex(1, 5); cex(2, 6); cex(3, 7);
+        cex(2, 4); cex(3, 5);
+        cex(1, 2); cex(3, 4); cex(5, 6);
     }
 }
 
-// The k best choices in order: lane j < k gets the j-th's expert (-1: none)
-// and choice; next: the (k + 1)-th's (asked for by want_next).
-template <typename V, int kV>
-__device__ __forceinline__ void pick(V (&choice)[kV], int k, bool want_next, int lane, int &e_mine, V &c_mine, int &e_next,
-                                     V &c_next)
+// The k best of the packed choices in order: lane j < k gets the j-th (0:
+// none); the return value is the (k + 1)-th where want_next.  A packed choice
+// is the upper 24 bits of the choice's key over 255 - expert: one redux gives
+// the winner and who it is, and equal choices come by the lower id.
+template <int kV> __device__ __forceinline__ uint32_t pick_packed(uint32_t (&v)[kV], int k, bool want_next, int lane, uint32_t &mine)
 {
-    const V none = (V)kNone;
+    sort_lane<kV>(v);
+    mine = 0;
+    for (int j = 0; j < k; ++j) {
+        const uint32_t best = __reduce_max_sync(~0u, v[0]);
+        if (lane == j) mine = best;
+        if (v[0] == best) {  // the winner's lane alone, while any candidate is left
+#pragma unroll
+            for (int i = 0; i + 1 < kV; ++i) v[i] = v[i + 1];
+            v[kV - 1] = 0;
+        }
+    }
+    return want_next ? __reduce_max_sync(~0u, v[0]) : 0u;
+}
+
+// The same by whole 32-bit or 64-bit keys (0: no candidate), for the rows that
+// packed ones do not settle: lane j < k gets the j-th's expert (-1: none),
+// next the (k + 1)-th's.
+__device__ __forceinline__ uint32_t warp_max(uint32_t v) { return __reduce_max_sync(~0u, v); }
+__device__ __forceinline__ u64 warp_max(u64 v) { return warp_max64(v); }
+template <typename K, int kV> __device__ __forceinline__ void pick_whole(K (&key)[kV], int k, int lane, int &e_mine, int &e_next)
+{
     e_mine = e_next = -1;
-    c_mine = c_next = none;
-    for (int j = 0; j < k + (want_next ? 1 : 0); ++j) {
-        V c = none;
+    for (int j = 0; j <= k; ++j) {
+        K mine = 0;
         int e = -1;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
-            const bool take = choice[i] > c;
-            c = take ? choice[i] : c;
+            const bool take = key[i] > mine;
+            mine = take ? key[i] : mine;
             e = take ? lane * kV + i : e;
         }
-        warp_best(c, e);
-        if (e < 0) return;  // uniform: no candidate is left
+        const K best = warp_max(mine);
+        if (best == 0) return;  // uniform: no candidate is left
+        // experts ascend with the lanes: the lowest lane holds the lowest one
+        e = __shfl_sync(~0u, e, __ffs(__ballot_sync(~0u, mine == best)) - 1);
         if (j < k) {
-            if (lane == j) {
-                e_mine = e;
-                c_mine = c;
-            }
+            if (lane == j) e_mine = e;
         } else {
             e_next = e;
-            c_next = c;
         }
 #pragma unroll
         for (int i = 0; i < kV; ++i)
-            if (e == lane * kV + i) choice[i] = none;
+            if (e == lane * kV + i) key[i] = 0;
     }
+}
+
+// A group's lanes where groups are whole lanes, a power of two of them; else 0.
+template <int kV> __device__ __forceinline__ int lanes_of_group(int size)
+{
+    const int seg = size / kV;
+    return seg * kV == size && (seg & (seg - 1)) == 0 ? seg : 0;
+}
+
+// Lane g's value of group g, of n <= 32 groups of any size, from the keys of
+// what groups count by (0: no candidate).
+template <typename K, int kV>
+__device__ __forceinline__ auto group_value(const K (&key)[kV], int n, int size, int top2, int lane) -> decltype(of(K()))
+{
+    decltype(of(K())) mine = kNone;
+    for (int g = 0; g < n; ++g) {
+        K a = 0, b = 0;  // the lane's two best in the group
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int e = lane * kV + i;
+            const K v = e >= g * size && e < (g + 1) * size ? key[i] : 0;
+            b = max(b, min(a, v));
+            a = max(a, v);
+        }
+        const K first = warp_max(a);
+        const int who = __ffs(__ballot_sync(~0u, a == first)) - 1;
+        const K second = top2 ? warp_max(lane == who ? b : a) : 0;
+        if (lane == g && first != 0) mine = second != 0 ? of(first) + of(second) : of(first);
+    }
+    return mine;
+}
+
+// Selection by the exact values of every expert, where more than 32 of them
+// (or groups that are not whole lanes) are in doubt.
+template <typename T, int kV> __device__ __noinline__ int pick_exact(const Pool<T> &p, float mx, int lane)
+{
+    const int size = p.E / p.n;
+    const bool limited = p.top < p.n, scored = p.bias || (limited && p.top2);
+    const Exact x = {mx, scored && !p.sigmoid ? exact_sum(p, mx, lane) : 1.};
+    u64 choice[kV], counts[kV];
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+        const int e = lane * kV + i;
+        choice[i] = counts[i] = 0;
+        if (e < p.E && to_f32(p.row[e]) > kNone) {
+            const u64 z = key64((double)(logit(p, e) + 0.f));
+            const double v = scored ? exact_value(p, x, e) : 0.;
+            choice[i] = !p.bias ? z : v > (double)kNone ? key64(v) : 0;
+            counts[i] = p.top2 && choice[i] ? key64(v) : choice[i];
+        }
+    }
+    if (limited) {
+        const u64 v = key64(group_value<u64, kV>(counts, p.n, size, p.top2, lane));
+        int place = 0;
+        for (int q = 0; q < p.n; ++q) {
+            const u64 o = __shfl_sync(~0u, v, q);
+            place += o > v || (o == v && q < lane) ? 1 : 0;
+        }
+        const uint32_t kept = __ballot_sync(~0u, lane < p.n && place < p.top);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int e = lane * kV + i;
+            if (e < p.E && !((kept >> (e / size)) & 1u)) choice[i] = 0;
+        }
+    }
+    int e_mine, e_next;
+    pick_whole<u64, kV>(choice, p.k, lane, e_mine, e_next);
+    return e_mine;
+}
+
+// Which `need` of the groups in `doubt` are kept (a bit each), from the exact
+// values of the experts in `wanted`: those that may be a group's two best.
+// 0: too many experts.
+template <typename T, int kV>
+__device__ __noinline__ uint32_t settle_groups(const Pool<T> &p, float mx, uint32_t wanted, uint32_t doubt, int need, int lane,
+                                               int *list)
+{
+    int e;
+    if (gather<kV>(wanted, lane, list, e) > 32) return 0;
+    const Exact x = {mx, p.sigmoid ? 1. : exact_sum(p, mx, lane)};
+    const u64 key = e >= 0 ? key64(exact_value(p, x, e)) : 0;
+    const int mine = e >= 0 ? e / (p.E / p.n) : -1;
+    u64 value = 0;
+    int group = -1, count = 0;
+    for (uint32_t m = doubt; m; m &= m - 1, ++count) {
+        const int g = __ffs(m) - 1;
+        const u64 first = warp_max64(mine == g ? key : 0);
+        const int who = __ffs(__ballot_sync(~0u, mine == g && key == first)) - 1;
+        const u64 second = p.top2 ? warp_max64(mine == g && lane != who ? key : 0) : 0;
+        if (lane == count) {
+            value = key64(second ? of(first) + of(second) : of(first));
+            group = g;
+        }
+    }
+    const int place = place_of(value, group, count);
+    return __reduce_or_sync(~0u, group >= 0 && place < need ? 1u << group : 0u);
+}
+
+// The order of the k best by the exact values of the experts in `wanted`, among
+// which they are: lane j < k gets the j-th (-1: none).  -2: too many experts.
+template <typename T, int kV>
+__device__ __noinline__ int settle_order(const Pool<T> &p, float mx, uint32_t wanted, int lane, int *list)
+{
+    int e;
+    const int count = gather<kV>(wanted, lane, list, e);
+    if (count > 32) return -2;
+    const Exact x = {mx, p.sigmoid ? 1. : exact_sum(p, mx, lane)};
+    const int place = place_of(e >= 0 ? key64(exact_value(p, x, e)) : 0, e, count);
+    if (e >= 0) list[place] = e;
+    __syncwarp();
+    e = lane < min(p.k, count) ? list[lane] : -1;
+    __syncwarp();
+    return e;
 }
 
 template <typename T, int kV> __device__ __forceinline__ void load_logits(float (&z)[kV], const T *p, int lane, int E, bool vec)
@@ -192,46 +352,10 @@ template <typename T, int kV> __device__ __forceinline__ void load_logits(float 
     }
 }
 
-// The selection in 64 bits, for the tokens whose FP32 choices are too close.
-template <typename T, int kV>
-__device__ __noinline__ int pick64(const T *row, const float *bias, int E, int sigmoid, int n, int top, int top2, int k, int lane)
-{
-    double z[kV], choice[kV], val[kV];
-    double mx = (double)kNone, sum = 0.;
-#pragma unroll
-    for (int i = 0; i < kV; ++i) {
-        const int e = lane * kV + i;
-        const float f = e < E ? to_f32(row[e]) : kNone;
-        z[i] = f > kNone ? (double)fminf(f, kLargest) : (double)kNone;
-        mx = fmax(mx, z[i]);
-    }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) mx = fmax(mx, __shfl_xor_sync(~0u, mx, off));
-#pragma unroll
-    for (int i = 0; i < kV; ++i) {
-        val[i] = 0.;
-        if (z[i] > (double)kNone) val[i] = sigmoid ? 1. / (1. + exp(-z[i])) : exp(z[i] - mx);
-        sum += val[i];
-    }
-    sum = warp_sum(sum);
-#pragma unroll
-    for (int i = 0; i < kV; ++i) {
-        choice[i] = z[i];
-        if (z[i] > (double)kNone) {
-            if (!sigmoid) val[i] /= sum;
-            if (bias) choice[i] = val[i] += bias[lane * kV + i];
-        }
-    }
-    double gap, c_mine, c_next;
-    int e_mine, e_next;
-    if (top < n) limit_groups<double, kV>(choice, val, n, E / n, top, top2, lane, gap);
-    pick<double, kV>(choice, k, false, lane, e_mine, c_mine, e_next, c_next);
-    return e_mine;
-}
-
 template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const ScoreParams p)
 {
     extern __shared__ int s_load[];
+    __shared__ int s_list[kRouteWarps][32];
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E_all = p.E_pub + p.E_priv;
@@ -242,94 +366,196 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
     for (int t = blockIdx.x * kRouteWarps + warp; t < p.T; t += gridDim.x * kRouteWarps) {
         const int priv = p.policy != nullptr && p.policy[t] == 0x01 ? 1 : 0;
         const int base = priv ? p.E_pub : 0, E = priv ? p.E_priv : p.E_pub;
-        const T *row = (const T *)p.logits + t * p.ld + base;
+        const Pool<T> pool = {(const T *)p.logits + t * p.ld + base, p.bias ? p.bias + base : nullptr, E, p.sigmoid, p.groups[priv],
+                              p.top_groups[priv], p.top2, p.k};
+        const bool limited = pool.top < pool.n, scored = pool.bias != nullptr || (limited && p.top2);
         float z[kV], choice[kV], val[kV];
-        load_logits<T, kV>(z, row, lane, E, ((uintptr_t)row & (sizeof(T) * kV - 1)) == 0);
-        const int n = p.groups[priv], top = p.top_groups[priv], size = E / n;
-        const bool limited = top < n, scored = p.bias != nullptr || (limited && p.top2);
+        load_logits<T, kV>(z, pool.row, lane, E, ((uintptr_t)pool.row & (sizeof(T) * kV - 1)) == 0);
         uint32_t live = 0;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             live |= z[i] > kNone ? 1u << i : 0u;
             z[i] = fminf(z[i], kLargest);
         }
-        float mx = kNone, sum = 0.f;
+        float mx = kNone, sum = 1.f;
         if (!p.sigmoid && (!p.renorm || scored)) {  // the pool's softmax
 #pragma unroll
             for (int i = 0; i < kV; ++i)
                 if ((live >> i) & 1u) mx = fmaxf(mx, z[i]);
-            mx = of_key(__reduce_max_sync(~0u, key_of(mx)));
+            mx = of(__reduce_max_sync(~0u, key_of(mx)));
+            sum = 0.f;
 #pragma unroll
             for (int i = 0; i < kV; ++i)
                 if ((live >> i) & 1u) sum += expf(z[i] - mx);
             sum = warp_sum(sum);
         }
-        // Error of an FP32 score, relative to it (twice it covers a pair).
-        // Sigmoid: expf 2 ulp (2^-22), the sum and the quotient half an ulp
-        // each.  Softmax: the difference z - max rounds by up to 2^-24 x 104
-        // where exp does not underflow, which the exponential turns into a
-        // relative error; the sum of 256 terms 13 x 2^-24 besides.
-        const float rel = p.sigmoid ? 0x1p-21f : 0x1p-16f;
-        float top_score = 0.f, top_value = 0.f;
+        auto score = [&](float zz) { return p.sigmoid ? 1.f / (1.f + expf(-zz)) : expf(zz - mx) / sum; };
+        // The error of an FP32 choice c is below err + 2^-24 |c|, with a fifth
+        // to spare.  Sigmoid: expf 2 ulp, which enters with s (1 - s), the sum
+        // and the quotient half an ulp each: 2^-22 s (3/2 - s) at most 2^-22.8.
+        // Softmax, with d = z - max: (|d| + 32) 2^-24 p, of which |d| p is at
+        // most 0.4 / sum: the difference's rounding in the exponent, expf 2 ulp,
+        // the same weighted in the sum, whose additions are 12 x 2^-24.
+        const float err = p.sigmoid ? 0x1.6p-23f : 0x1.5p-19f / sum;
+        float top_value = 0.f;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             const bool on = (live >> i) & 1u;
             val[i] = 0.f;
             choice[i] = on ? z[i] : kNone;
             if (scored && on) {
-                val[i] = p.sigmoid ? 1.f / (1.f + expf(-z[i])) : expf(z[i] - mx) / sum;
-                top_score = fmaxf(top_score, val[i]);
-                if (p.bias) choice[i] = val[i] += __ldg(p.bias + base + lane * kV + i);
-                top_value = fmaxf(top_value, fabsf(val[i]));
+                val[i] = score(z[i]);
+                if (pool.bias) choice[i] = val[i] += __ldg(pool.bias + lane * kV + i);
+                if (choice[i] > kNone) top_value = fmaxf(top_value, fabsf(val[i]));
             }
         }
-        bool again = false;
+        bool exact = false;  // the whole selection again by exact values
         if (limited) {
-            float gap;
-            limit_groups<float, kV>(choice, val, n, size, top, p.top2, lane, gap);
-            if (scored) {  // sums of up to two values on either side
-                top_score = of_key(__reduce_max_sync(~0u, key_of(top_score)));
-                top_value = of_key(__reduce_max_sync(~0u, key_of(top_value)));
-                again = gap <= 4.f * (rel * top_score + 0x1p-23f * top_value);
+            const int n = pool.n, top = pool.top, size = E / n, seg = lanes_of_group<kV>(size);
+            // two sums of two values each, and their own rounding
+            if (scored) top_value = of(__reduce_max_sync(~0u, key_of(top_value)));
+            const float close = 4.f * err + 0x1p-20f * top_value;
+            if (seg) {
+                // every group at once: its lanes hold its two best after log2(seg) exchanges
+                float a = kNone, b = kNone;
+#pragma unroll
+                for (int i = 0; i < kV; ++i) add_two(a, b, choice[i] > kNone ? (p.top2 ? val[i] : choice[i]) : kNone);
+                for (int off = 1; off < seg; off <<= 1) {
+                    const float oa = __shfl_xor_sync(~0u, a, off), ob = __shfl_xor_sync(~0u, b, off);
+                    add_two(a, b, oa);
+                    add_two(a, b, ob);
+                }
+                const float second = b > kNone ? b : a;
+                if (p.top2 && b > kNone) a += b;
+                const int g = lane / seg;
+                int place = 0;
+                for (int q = 0; q < n; ++q) {
+                    const float o = __shfl_sync(~0u, a, q * seg);
+                    place += o > a || (o == a && q < g) ? 1 : 0;
+                }
+                bool kept = place < top;
+                if (scored) {
+                    const float x = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top - 1)) - 1);
+                    const float y = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top)) - 1);
+                    if (y > kNone && x - y <= close) {
+                        const bool in = a > x + close, doubt = g < n && !in && a >= y - close;
+                        uint32_t wanted = 0;
+#pragma unroll
+                        for (int i = 0; i < kV; ++i)
+                            if (doubt && choice[i] > kNone && (p.top2 ? val[i] : choice[i]) >= (p.top2 ? second : a) - close)
+                                wanted |= 1u << i;
+                        const bool first_lane = lane % seg == 0;
+                        const uint32_t which = __reduce_or_sync(~0u, doubt && first_lane ? 1u << g : 0u);
+                        const int need = top - __popc(__ballot_sync(~0u, g < n && in && first_lane));
+                        const uint32_t keep = settle_groups<T, kV>(pool, mx, wanted, which, need, lane, s_list[warp]);
+                        exact = keep == 0;
+                        kept = in || (g < n && ((keep >> g) & 1u));
+                    }
+                }
+                if (!kept) {
+#pragma unroll
+                    for (int i = 0; i < kV; ++i) choice[i] = kNone;
+                }
+            } else {
+                uint32_t key[kV];
+#pragma unroll
+                for (int i = 0; i < kV; ++i) key[i] = choice[i] > kNone ? key_of(p.top2 ? val[i] : choice[i]) : 0u;
+                const float a = group_value<uint32_t, kV>(key, n, size, p.top2, lane);
+                int place = 0;
+                for (int q = 0; q < n; ++q) {
+                    const float o = __shfl_sync(~0u, a, q);
+                    place += o > a || (o == a && q < lane) ? 1 : 0;
+                }
+                const uint32_t kept = __ballot_sync(~0u, lane < n && place < top);
+                if (scored) {
+                    const float x = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, lane < n && place == top - 1)) - 1);
+                    const float y = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, lane < n && place == top)) - 1);
+                    exact = y > kNone && x - y <= close;
+                }
+#pragma unroll
+                for (int i = 0; i < kV; ++i) {
+                    const int e = lane * kV + i;
+                    if (e < E && !((kept >> (e / size)) & 1u)) choice[i] = kNone;
+                }
             }
         }
+        // Neighbours in the order, the last one's being the first not chosen,
+        // are in doubt where their packed choices are equal (again from the
+        // whole ones) or their FP32 choices closer than those are exact (by
+        // exact values), unless their logits and biases are the same: a true
+        // tie.  16-bit logits without a bias are packed whole.
+        const bool inexact = pool.bias != nullptr || sizeof(T) == 4;
         int e_mine, e_next;
-        float c_mine, c_next;
-        pick<float, kV>(choice, p.k, p.bias != nullptr, lane, e_mine, c_mine, e_next, c_next);
-        if (p.bias) {
-            // neighbours in the order that are close, unless both their logits
-            // and their biases are the same: a true tie
-            int e_after = __shfl_down_sync(~0u, e_mine, 1);
-            float c_after = __shfl_down_sync(~0u, c_mine, 1);
-            if (lane == p.k - 1) {
-                e_after = e_next;
-                c_after = c_next;
+        bool whole = false;
+        {
+            uint32_t v[kV], mine;
+#pragma unroll
+            for (int i = 0; i < kV; ++i)
+                v[i] = choice[i] > kNone ? (key_of(choice[i]) & ~255u) | (uint32_t)(255 - (lane * kV + i)) : 0u;
+            const uint32_t next = pick_packed<kV>(v, p.k, inexact, lane, mine);
+            e_mine = mine ? 255 - (int)(mine & 255u) : -1;
+            e_next = next ? 255 - (int)(next & 255u) : -1;
+            if (inexact) {
+                uint32_t after = __shfl_down_sync(~0u, mine, 1);
+                if (lane == p.k - 1) after = next;
+                whole = __any_sync(~0u, lane < p.k && after != 0u && (mine ^ after) < 256u);
             }
-            bool doubt = false;
-            if (lane < p.k && e_after >= 0) {
-                const float b0 = p.bias[base + e_mine], b1 = p.bias[base + e_after];
-                doubt = c_mine - c_after <= rel * (fabsf(c_mine - b0) + fabsf(c_after - b1)) +
-                                                0x1p-22f * (fabsf(c_mine) + fabsf(c_after)) &&
-                        !(b0 == b1 && to_f32(row[e_mine]) == to_f32(row[e_after]));
-            }
-            again = again || __any_sync(~0u, doubt);
         }
-        if (again)
-            e_mine = pick64<T, kV>(row, p.bias ? p.bias + base : nullptr, E, p.sigmoid, n, top, p.top2, p.k, lane);
+        if (whole) {
+            uint32_t key[kV];
+#pragma unroll
+            for (int i = 0; i < kV; ++i) key[i] = choice[i] > kNone ? key_of(choice[i]) : 0u;
+            pick_whole<uint32_t, kV>(key, p.k, lane, e_mine, e_next);
+        }
+        const bool need_score = p.sigmoid || !p.renorm;
+        float zj = kNone, sj = 0.f;
+        if (e_mine >= 0) {
+            zj = logit(pool, e_mine);
+            if (need_score || pool.bias) sj = score(zj);
+        }
+        if (pool.bias && !exact) {
+            int e_after = __shfl_down_sync(~0u, e_mine, 1);
+            if (lane == p.k - 1) e_after = e_next;
+            bool doubt = false;
+            float c0 = kNone;
+            if (lane < p.k && e_mine >= 0) {
+                const float b0 = pool.bias[e_mine];
+                c0 = sj + b0;
+                if (e_after >= 0) {
+                    const float za = logit(pool, e_after), b1 = pool.bias[e_after], c1 = score(za) + b1;
+                    doubt = c0 - c1 <= 2.f * err + 0x1.4p-24f * (fabsf(c0) + fabsf(c1)) && !(b0 == b1 && zj == za);
+                }
+            }
+            if (__any_sync(~0u, doubt)) {
+                const float c = __shfl_sync(~0u, c0, p.k - 1), least = c - 2.02f * (err + 0x1.4p-24f * fabsf(c));
+                uint32_t wanted = 0;
+#pragma unroll
+                for (int i = 0; i < kV; ++i)
+                    if (choice[i] > kNone && choice[i] >= least) wanted |= 1u << i;
+                const int e = settle_order<T, kV>(pool, mx, wanted, lane, s_list[warp]);
+                exact = e == -2;
+                if (e_mine != e && e >= 0) {
+                    zj = logit(pool, e);
+                    sj = score(zj);
+                }
+                e_mine = e;
+            }
+        }
+        if (exact) {
+            e_mine = pick_exact<T, kV>(pool, mx, lane);
+            zj = e_mine >= 0 ? logit(pool, e_mine) : kNone;
+            sj = e_mine >= 0 && need_score ? score(zj) : 0.f;
+        }
         // lane j's weight
         const bool mine = lane < p.k && e_mine >= 0;
-        float w = 0.f;
-        const float zj = mine ? fminf(to_f32(row[e_mine]), kLargest) : kNone;
-        if (p.sigmoid) {
-            if (mine) w = 1.f / (1.f + expf(-zj));
-            if (p.renorm) w = w / (warp_sum(w) + 1e-20f);
+        float w = mine ? sj : 0.f;
+        if (p.renorm && p.sigmoid) {
+            w = w / (warp_sum(w) + 1e-20f);
         } else if (p.renorm) {  // softmax over the k
-            const float m = of_key(__reduce_max_sync(~0u, key_of(zj)));
-            if (mine) w = expf(zj - m);
-            const float s = warp_sum(w);
-            if (mine) w = w / s;
-        } else if (mine) {
-            w = expf(zj - mx) / sum;
+            const float m = of(__reduce_max_sync(~0u, key_of(mine ? zj : kNone)));
+            w = mine ? expf(zj - m) : 0.f;
+            const float total = warp_sum(w);
+            if (mine) w = w / total;
         }
         if (lane < p.k) {
             p.idx[(long long)t * p.k + lane] = mine ? base + e_mine : -1;
@@ -401,7 +627,7 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
             // s (1 - s), 1 - s as the sigmoid of -z: no cancellation near s = 1
             if (mine) g = ds * s * (1.f / (1.f + expf(zj)));
         } else if (p.renorm) {
-            const float m = of_key(__reduce_max_sync(~0u, key_of(mine ? zj : kNone)));
+            const float m = of(__reduce_max_sync(~0u, key_of(mine ? zj : kNone)));
             const float ex = mine ? expf(zj - m) : 0.f;
             const float total = warp_sum(ex);
             const float w = mine ? ex / total : 0.f;
@@ -419,7 +645,7 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
                 z[i] = z[i] > kNone ? fminf(z[i], kLargest) : kNone;
                 mx = fmaxf(mx, z[i]);
             }
-            mx = of_key(__reduce_max_sync(~0u, key_of(mx)));
+            mx = of(__reduce_max_sync(~0u, key_of(mx)));
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
                 d[i] = z[i] > kNone ? expf(z[i] - mx) : 0.f;

@@ -128,7 +128,7 @@ int pmpe_clip_grad_norm(const pmpe_grad *grads, int n, float max_norm, float *no
     const int ok = clip_tensors_ok(grads, n);
     if (ok <= 0) return ok < 0 ? PMPE_ERR_WORKSPACE : PMPE_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < clip_workspace_bytes(n)) return PMPE_ERR_WORKSPACE;
-    return done(launch_clip(grads, n, max_norm, norm, (double *)workspace, (cudaStream_t)stream));
+    return done(launch_clip(grads, n, max_norm, norm, workspace, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -178,7 +178,7 @@ cudaError_t launch_route_scores_backward(const pmpe_route_desc &d, const float *
                                          cudaStream_t st);
 size_t clip_workspace_bytes(int n);
 int clip_tensors_ok(const pmpe_grad *g, int n);
-cudaError_t launch_clip(const pmpe_grad *g, int n, float max_norm, float *norm_out, double *partial, cudaStream_t st);
+cudaError_t launch_clip(const pmpe_grad *g, int n, float max_norm, float *norm_out, void *workspace, cudaStream_t st);
 cudaError_t launch_resolve(const uint8_t *policy, int T, uint8_t *tau, cudaStream_t stream);
 cudaError_t launch_policy_from_requests(const uint8_t *req_policy, const int32_t *cu_seqlens, int n_req, int T,
                                         uint8_t *policy_out, cudaStream_t stream);

@@ -6,9 +6,10 @@ has not been built this module raises on import -- there is no fallback.
 """
 from __future__ import annotations
 
+import array
 import ctypes
-import functools
 import os
+import struct
 from typing import NamedTuple
 
 import numpy as np
@@ -134,45 +135,20 @@ class WorkspaceLayout(ctypes.Structure):
                                                 "tile_counts")]
 
 
-class RmsNormDesc(ctypes.Structure):
-    _fields_ = [("T", ctypes.c_int), ("H", ctypes.c_int), ("type", ctypes.c_int), ("weight_type", ctypes.c_int),
-                ("quant", ctypes.c_int), ("eps", ctypes.c_float), ("x", _vp), ("residual", _vp), ("weight", _vp),
-                ("x_ld", ctypes.c_int64), ("residual_ld", ctypes.c_int64), ("h", _vp), ("y", _vp), ("scale", _vp),
-                ("rstd", _vp)]
-
-
-class RmsNormBackwardDesc(ctypes.Structure):
-    _fields_ = [("T", ctypes.c_int), ("H", ctypes.c_int), ("type", ctypes.c_int), ("weight_type", ctypes.c_int),
-                ("dy_type", ctypes.c_int), ("dx_type", ctypes.c_int), ("dy", _vp), ("h", _vp), ("weight", _vp),
-                ("rstd", _vp), ("d_h", _vp), ("dx", _vp), ("dw", _vp), ("workspace", _vp),
-                ("workspace_bytes", ctypes.c_size_t)]
-
-
-class RouteDesc(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int) for n in ("T", "E_pub", "E_priv", "k", "logits_type", "score", "renormalize", "groups_pub",
-                                            "top_groups_pub", "groups_priv", "top_groups_priv", "group_score")] + \
-               [("scale", ctypes.c_float), ("logits", _vp), ("ld", ctypes.c_int64), ("policy", _vp), ("bias", _vp),
-                ("topk_idx", _vp), ("topk_w", _vp), ("load", _vp)]
-
-
-class Grad(ctypes.Structure):
-    _fields_ = [("grad", _vp), ("out", _vp), ("n", ctypes.c_int64), ("type", ctypes.c_int)]
-
-
 _lib.pmpe_rms_norm.restype = ctypes.c_int
-_lib.pmpe_rms_norm.argtypes = [ctypes.POINTER(RmsNormDesc), _vp]
+_lib.pmpe_rms_norm.argtypes = [_vp, _vp]
 _lib.pmpe_rms_norm_backward_workspace_size.restype = ctypes.c_size_t
 _lib.pmpe_rms_norm_backward_workspace_size.argtypes = [ctypes.c_int] * 2
 _lib.pmpe_rms_norm_backward.restype = ctypes.c_int
-_lib.pmpe_rms_norm_backward.argtypes = [ctypes.POINTER(RmsNormBackwardDesc), _vp]
+_lib.pmpe_rms_norm_backward.argtypes = [_vp, _vp]
 _lib.pmpe_route.restype = ctypes.c_int
-_lib.pmpe_route.argtypes = [ctypes.POINTER(RouteDesc), _vp]
+_lib.pmpe_route.argtypes = [_vp, _vp]
 _lib.pmpe_route_backward.restype = ctypes.c_int
-_lib.pmpe_route_backward.argtypes = [ctypes.POINTER(RouteDesc), _vp, _vp, _vp]
+_lib.pmpe_route_backward.argtypes = [_vp, _vp, _vp, _vp]
 _lib.pmpe_clip_workspace_size.restype = ctypes.c_size_t
 _lib.pmpe_clip_workspace_size.argtypes = [ctypes.c_int]
 _lib.pmpe_clip_grad_norm.restype = ctypes.c_int
-_lib.pmpe_clip_grad_norm.argtypes = [ctypes.POINTER(Grad), ctypes.c_int, ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]
+_lib.pmpe_clip_grad_norm.argtypes = [_vp, ctypes.c_int, ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.pmpe_moe_workspace_size.restype = ctypes.c_size_t
 _lib.pmpe_moe_workspace_size.argtypes = [ctypes.c_int] * 7
 _lib.pmpe_moe_workspace_layout.restype = ctypes.c_int
@@ -478,50 +454,65 @@ class MoeLayer:
 
 
 # ------------------------------------------- operators around the layer
+#
+# A call's host time counts as much as its kernel's at decode sizes (1.7 us of
+# kernel), so the checks below are plain comparisons, descriptors are packed
+# as bytes in the C structs' layout and the stream handle is read directly:
+# 9 us a call on a Grace core, where ctypes structures and
+# torch.cuda.current_stream() made it 20.
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _QUANT = {None: 0, "block": 1, "row": 2}
 QUANT_BLOCK = 128  # columns that share a scale with quant="block"
+_F32 = torch.float32
+
+_pack_norm = struct.Struct("@5if3P2q4P").pack
+_pack_norm_bwd = struct.Struct("@6i8PN").pack
+_pack_route = struct.Struct("@12ifPq5P").pack
+
+_device = torch._C._cuda_getDevice               # the current device's index
+_raw_stream = torch._C._cuda_getCurrentRawStream  # its current stream's handle
 
 
-def _require(ok, what: str):
-    if not ok:
-        raise PmpeError(ERR_INVALID_ARG, what)
+def _bad(what: str):
+    raise PmpeError(ERR_INVALID_ARG, what)
 
 
-def _placed(fn):
-    """Runs ``fn``, whose first argument is a tensor (or a list of them), on
-    that tensor's device and on ``stream``: outputs and scratch are allocated
-    where the kernels run, so the caching allocator reuses them in order."""
-    name = fn.__code__.co_varnames[0]
-
-    @functools.wraps(fn)
-    def call(*args, stream=None, **kw):
-        first = args[0] if args else kw.get(name)
-        t = first[0] if isinstance(first, list) and first else first
-        _require(isinstance(t, torch.Tensor) and t.is_cuda, f"{fn.__name__}: {name}: a CUDA tensor is wanted")
-        if stream is not None:
-            _require(stream.device == t.device, f"{fn.__name__}: the stream is of another device than the tensors")
-            with torch.cuda.stream(stream):
-                return fn(*args, **kw)
-        if t.device.index != torch.cuda.current_device():
-            with torch.cuda.device(t.device):
-                return fn(*args, **kw)
+def _elsewhere(fn, t, stream, *args, **kw):
+    """The call again on ``stream``, or on the tensor's device: outputs and
+    scratch are allocated where the kernels run, so that the caching allocator
+    reuses them in order."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _bad(f"{fn.__name__}: CUDA tensors are wanted")
+    if stream is not None:
+        if stream.device != t.device:
+            _bad(f"{fn.__name__}: the stream is of another device than the tensors")
+        with torch.cuda.stream(stream):
+            return fn(*args, **kw)
+    with torch.cuda.device(t.device):
         return fn(*args, **kw)
-    return call
-
-
-def _stream_of(t) -> int:
-    return torch.cuda.current_stream(t.device).cuda_stream
-
-
-def _pitch(t) -> int:
-    """Elements from a row to the next (any value serves a single row)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _at(t):
-    return None if t is None else t.data_ptr()
+    return 0 if t is None else t.data_ptr()
+
+
+def _pitch(t) -> int:
+    """Elements from a row to the next (any value serves a single row); -1,
+    which the library refuses, where a row's elements are not adjacent."""
+    rows, cols = t.shape
+    if cols != 1 and t.stride(1) != 1:
+        return -1
+    return t.stride(0) if rows > 1 else cols
+
+
+def _vector(t, n: int, dev: int, dtype) -> bool:
+    return t.dtype is dtype and t.dim() == 1 and t.numel() == n and t.get_device() == dev and t.is_contiguous()
+
+
+def _matrix(t, rows: int, cols: int, dev: int, dtype) -> bool:
+    return t.dtype is dtype and t.get_device() == dev and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols and \
+        t.is_contiguous()
 
 
 class RmsNorm(NamedTuple):
@@ -531,8 +522,7 @@ class RmsNorm(NamedTuple):
     rstd: torch.Tensor          # FP32 [T], for the backward
 
 
-@_placed
-def rms_norm(x, weight, residual=None, eps: float = 1e-6, quant=None, h_out=None) -> RmsNorm:
+def rms_norm(x, weight, residual=None, eps: float = 1e-6, quant=None, h_out=None, stream=None) -> RmsNorm:
     """Root-mean-square norm of ``h = x + residual`` (x without a residual),
     times ``weight``.
 
@@ -543,36 +533,54 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-6, quant=None, h_out=None
     (y stands for ``y.float() * scale``).  ``h_out``: where h goes (may be
     ``residual`` or ``x``).  ``stream``: the stream to run on (default: the
     current one).  H up to 16384, eps at least 1e-20."""
-    _require(x.dim() == 2 and x.dtype in _TYPES and x.stride(1) == 1 or x.dim() == 2 and x.shape[1] == 1,
-             "rms_norm: x is [T, H] of FP32, BF16 or FP16 with adjacent columns")
+    dev = x.get_device()
+    if stream is not None or dev < 0 or dev != _device():
+        return _elsewhere(rms_norm, x, stream, x, weight, residual, eps, quant, h_out)
+    dt = x.dtype
+    code = _TYPES.get(dt, -1)
+    if code < 0 or x.dim() != 2:
+        _bad("rms_norm: x is [T, H] of FP32, BF16 or FP16")
     T, H = x.shape
-    dev, dt = x.device, x.dtype
-    _require(quant in _QUANT, 'rms_norm: quant is None, "block" or "row"')
-    _require(weight.device == dev and weight.dtype in (dt, torch.float32) and weight.shape == (H,) and weight.is_contiguous(),
-             "rms_norm: weight is [H] of x's type or FP32, on x's device")
-    h = x
+    plain = x.is_contiguous()
+    if quant not in _QUANT:
+        _bad('rms_norm: quant is None, "block" or "row"')
+    w_code = code
+    if not _vector(weight, H, dev, dt):
+        w_code = 0
+        if not _vector(weight, H, dev, _F32):
+            _bad("rms_norm: weight is [H] of x's type or FP32, on x's device")
+    h, h_at, res_at, res_ld = x, 0, 0, 0
     if residual is not None:
-        _require(residual.device == dev and residual.dtype == dt and residual.shape == (T, H) and
-                 (residual.stride(1) == 1 or H == 1), "rms_norm: residual is as x")
-        h = h_out if h_out is not None else torch.empty((T, H), dtype=dt, device=dev)
-        _require(h.device == dev and h.dtype == dt and h.shape == (T, H) and h.is_contiguous(),
-                 "rms_norm: h_out is [T, H] of x's type without gaps")
-    else:
-        _require(h_out is None, "rms_norm: without a residual h is x")
-    y = torch.empty((T, H), dtype=dt if quant is None else torch.float8_e4m3fn, device=dev)
+        if residual.dtype is not dt or residual.get_device() != dev or residual.shape != x.shape:
+            _bad("rms_norm: residual is as x")
+        res_at, res_ld = residual.data_ptr(), H if residual.is_contiguous() else _pitch(residual)
+        if h_out is None:
+            h = torch.empty_like(x) if plain else torch.empty((T, H), dtype=dt, device=x.device)
+        elif _matrix(h_out, T, H, dev, dt):
+            h = h_out
+        else:
+            _bad("rms_norm: h_out is [T, H] of x's type without gaps")
+        h_at = h.data_ptr()
+    elif h_out is not None:
+        _bad("rms_norm: without a residual h is x")
     scale = None
     if quant is not None:
-        scale = torch.empty((T, -(-H // QUANT_BLOCK) if quant == "block" else 1), dtype=torch.float32, device=dev)
-    rstd = torch.empty(T, dtype=torch.float32, device=dev)
-    d = RmsNormDesc(T, H, _TYPES[dt], _TYPES[weight.dtype], _QUANT[quant], eps, x.data_ptr(), _at(residual),
-                    weight.data_ptr(), _pitch(x), 0 if residual is None else _pitch(residual),
-                    None if residual is None else h.data_ptr(), y.data_ptr(), _at(scale), rstd.data_ptr())
-    _check(_lib.pmpe_rms_norm(d, _stream_of(x)), "pmpe_rms_norm")
+        y = torch.empty((T, H), dtype=torch.float8_e4m3fn, device=x.device)
+        scale = torch.empty((T, -(-H // QUANT_BLOCK) if quant == "block" else 1), dtype=_F32, device=x.device)
+    elif plain:
+        y = torch.empty_like(x)
+    else:
+        y = torch.empty((T, H), dtype=dt, device=x.device)
+    rstd = torch.empty(T, dtype=_F32, device=x.device)
+    rc = _lib.pmpe_rms_norm(_pack_norm(T, H, code, w_code, _QUANT[quant], eps, x.data_ptr(), res_at, weight.data_ptr(),
+                                       H if plain else _pitch(x), res_ld, h_at, y.data_ptr(), _at(scale), rstd.data_ptr()),
+                            _raw_stream(dev))
+    if rc:
+        _check(rc, "pmpe_rms_norm")
     return RmsNorm(y, scale, h, rstd)
 
 
-@_placed
-def rms_norm_backward(dy, h, weight, rstd, d_h=None, dx_dtype=None, need_dw: bool = True):
+def rms_norm_backward(dy, h, weight, rstd, d_h=None, dx_dtype=None, need_dw: bool = True, stream=None):
     """(dx, dw) of ``rms_norm``: dx is the gradient of x and of the residual
     alike, dw that of the weight (FP32; None unless ``need_dw``).
 
@@ -580,30 +588,41 @@ def rms_norm_backward(dy, h, weight, rstd, d_h=None, dx_dtype=None, need_dw: boo
     d_h: the gradient that reaches h itself, of dx's type.  ``dx_dtype``: h's
     type (default) or FP32.  Matrices without gaps.  An 8-bit y passes its
     gradient as the identity."""
-    _require(h.dim() == 2 and h.dtype in _TYPES and h.is_contiguous() and dy.device == h.device,
-             "rms_norm_backward: h is [T, H] of FP32, BF16 or FP16 without gaps")
+    dev = h.get_device()
+    if stream is not None or dev < 0 or dev != _device():
+        return _elsewhere(rms_norm_backward, h, stream, dy, h, weight, rstd, d_h, dx_dtype, need_dw)
+    dt = h.dtype
+    code = _TYPES.get(dt, -1)
+    if code < 0 or h.dim() != 2 or not h.is_contiguous():
+        _bad("rms_norm_backward: h is [T, H] of FP32, BF16 or FP16 without gaps")
     T, H = h.shape
-    dev, dt = h.device, h.dtype
-    xt = dx_dtype if dx_dtype is not None else dt
-    _require(xt in (dt, torch.float32), "rms_norm_backward: dx is of h's type or FP32")
-    _require(dy.dtype in (dt, torch.float32) and dy.shape == (T, H) and dy.is_contiguous(),
-             "rms_norm_backward: dy is [T, H] of h's type or FP32 without gaps")
-    _require(weight.device == dev and weight.dtype in (dt, torch.float32) and weight.shape == (H,) and weight.is_contiguous(),
-             "rms_norm_backward: weight is [H] of h's type or FP32")
-    _require(rstd.device == dev and rstd.dtype == torch.float32 and rstd.shape == (T,) and rstd.is_contiguous(),
-             "rms_norm_backward: rstd is FP32 [T]")
-    _require(d_h is None or (d_h.device == dev and d_h.dtype == xt and d_h.shape == (T, H) and d_h.is_contiguous()),
-             "rms_norm_backward: d_h is [T, H] of dx's type without gaps")
-    dx = torch.empty((T, H), dtype=xt, device=dev)
+    xt = dt if dx_dtype is None else dx_dtype
+    if xt is not dt and xt is not _F32:
+        _bad("rms_norm_backward: dx is of h's type or FP32")
+    gt = dy.dtype
+    if gt is not dt and gt is not _F32 or not _matrix(dy, T, H, dev, gt):
+        _bad("rms_norm_backward: dy is [T, H] of h's type or FP32 without gaps")
+    w_code = code
+    if not _vector(weight, H, dev, dt):
+        w_code = 0
+        if not _vector(weight, H, dev, _F32):
+            _bad("rms_norm_backward: weight is [H] of h's type or FP32")
+    if not _vector(rstd, T, dev, _F32):
+        _bad("rms_norm_backward: rstd is FP32 [T]")
+    if d_h is not None and not _matrix(d_h, T, H, dev, xt):
+        _bad("rms_norm_backward: d_h is [T, H] of dx's type without gaps")
+    dx = torch.empty_like(h) if xt is dt else torch.empty((T, H), dtype=xt, device=h.device)
     dw = ws = None
     nb = 0
     if need_dw:
-        dw = torch.empty(H, dtype=torch.float32, device=dev)
         nb = _lib.pmpe_rms_norm_backward_workspace_size(T, H)
-        ws = torch.empty(nb, dtype=torch.uint8, device=dev)
-    d = RmsNormBackwardDesc(T, H, _TYPES[dt], _TYPES[weight.dtype], _TYPES[dy.dtype], _TYPES[xt], dy.data_ptr(), h.data_ptr(),
-                            weight.data_ptr(), rstd.data_ptr(), _at(d_h), dx.data_ptr(), _at(dw), _at(ws), nb)
-    _check(_lib.pmpe_rms_norm_backward(d, _stream_of(h)), "pmpe_rms_norm_backward")
+        dw = torch.empty(H, dtype=_F32, device=h.device)
+        ws = torch.empty(nb, dtype=torch.uint8, device=h.device)
+    rc = _lib.pmpe_rms_norm_backward(
+        _pack_norm_bwd(T, H, code, w_code, _TYPES[gt], _TYPES[xt], dy.data_ptr(), h.data_ptr(), weight.data_ptr(),
+                       rstd.data_ptr(), _at(d_h), dx.data_ptr(), _at(dw), _at(ws), nb), _raw_stream(dev))
+    if rc:
+        _check(rc, "pmpe_rms_norm_backward")
     return dx, dw
 
 
@@ -611,7 +630,6 @@ class Router:
     """Routing from given logits for models whose router is not the layer's
     own softmax: softmax or sigmoid scores, a bias for balance, group limits,
     top-k and weights, each token inside the pool its policy byte selects.
-    ``MoeLayer.forward(route=...)`` runs the experts with the result.
 
     score: "softmax" (over the token's pool) or "sigmoid".  groups,
     groups_priv: (groups of the pool, groups kept); group_score: "max" or
@@ -619,25 +637,23 @@ class Router:
 
     def __init__(self, E_pub: int, E_priv: int, k: int, score: str = "softmax", renormalize: bool = True, scale: float = 1.0,
                  groups=(1, 1), groups_priv=(1, 1), group_score: str = "max"):
-        _require(score in ("softmax", "sigmoid"), 'Router: score is "softmax" or "sigmoid"')
-        _require(group_score in ("max", "top2"), 'Router: group_score is "max" or "top2"')
+        if score not in ("softmax", "sigmoid"):
+            _bad('Router: score is "softmax" or "sigmoid"')
+        if group_score not in ("max", "top2"):
+            _bad('Router: group_score is "max" or "top2"')
         self.E_pub, self.E_priv, self.k, self.E = int(E_pub), int(E_priv), int(k), int(E_pub) + int(E_priv)
         self._config = (int(score == "sigmoid"), int(bool(renormalize)), int(groups[0]), int(groups[1]), int(groups_priv[0]),
                         int(groups_priv[1]), int(group_score == "top2"), float(scale))
         # refuses what the library would refuse, before the first call
-        d = RouteDesc(0, self.E_pub, self.E_priv, self.k, 0, *self._config, None, max(self.E, 0), None, None, None, None, None)
-        _check(_lib.pmpe_route(d, None), "pmpe_route")
+        _check(_lib.pmpe_route(_pack_route(0, self.E_pub, self.E_priv, self.k, 0, *self._config, 0, self.E, 0, 0, 0, 0, 0), None),
+               "pmpe_route")
 
-    def _desc(self, logits, policy, bias, idx, w, load) -> RouteDesc:
-        T, dev = logits.shape[0], logits.device
-        _require(logits.dim() == 2 and logits.dtype in _TYPES and logits.shape[1] == self.E and
-                 (logits.stride(1) == 1 or self.E == 1), "Router: logits are [T, E] of FP32, BF16 or FP16 with adjacent columns")
-        _require(policy is None or (policy.device == dev and policy.dtype == torch.uint8 and policy.shape == (T,) and
-                                    policy.is_contiguous()), "Router: policy is uint8 [T] on the logits' device")
-        _require(bias is None or (bias.device == dev and bias.dtype == torch.float32 and bias.shape == (self.E,) and
-                                  bias.is_contiguous()), "Router: bias is FP32 [E] on the logits' device")
-        return RouteDesc(T, self.E_pub, self.E_priv, self.k, _TYPES[logits.dtype], *self._config, logits.data_ptr(),
-                         _pitch(logits), _at(policy), _at(bias), idx.data_ptr(), _at(w), _at(load))
+    def _logits(self, logits):
+        """(type, rows, pitch) of the logits."""
+        code = _TYPES.get(logits.dtype, -1)
+        if code < 0 or logits.dim() != 2 or logits.shape[1] != self.E:
+            _bad("Router: logits are [T, E] of FP32, BF16 or FP16")
+        return code, logits.shape[0], self.E if logits.is_contiguous() else _pitch(logits)
 
     def route(self, logits, policy=None, bias=None, load=None, stream=None):
         """(idx, w): the k chosen experts of each token (int32 [T, k], global
@@ -648,36 +664,44 @@ class Router:
         private pool (None: all public).  bias: FP32 [E], added to the scores
         for the choice alone.  load: int32 [E], to which the tokens of each
         expert are added (for the bias's update)."""
-        return _route(logits, self, policy, bias, load, stream=stream)
+        dev = logits.get_device()
+        if stream is not None or dev < 0 or dev != _device():
+            return _elsewhere(self.route, logits, stream, logits, policy, bias, load)
+        code, T, ld = self._logits(logits)
+        if policy is not None and not _vector(policy, T, dev, torch.uint8):
+            _bad("Router: policy is uint8 [T] on the logits' device")
+        if bias is not None and not _vector(bias, self.E, dev, _F32):
+            _bad("Router: bias is FP32 [E] on the logits' device")
+        if load is not None and not _vector(load, self.E, dev, torch.int32):
+            _bad("Router: load is int32 [E] on the logits' device")
+        idx = torch.empty((T, self.k), dtype=torch.int32, device=logits.device)
+        w = torch.empty((T, self.k), dtype=_F32, device=logits.device)
+        rc = _lib.pmpe_route(_pack_route(T, self.E_pub, self.E_priv, self.k, code, *self._config, logits.data_ptr(), ld, _at(policy),
+                                         _at(bias), idx.data_ptr(), w.data_ptr(), _at(load)), _raw_stream(dev))
+        if rc:
+            _check(rc, "pmpe_route")
+        return idx, w
 
     def backward(self, logits, policy, idx, dw, stream=None):
         """The gradient of the logits ([T, E], their type) from that of the
         weights (FP32 [T, k]) for the selection ``idx``."""
-        return _route_backward(logits, self, policy, idx, dw, stream=stream)
-
-
-@_placed
-def _route(logits, router, policy, bias, load):
-    dev = logits.device
-    _require(load is None or (load.device == dev and load.dtype == torch.int32 and load.shape == (router.E,) and
-                              load.is_contiguous()), "Router: load is int32 [E] on the logits' device")
-    idx = torch.empty((logits.shape[0], router.k), dtype=torch.int32, device=dev)
-    w = torch.empty((logits.shape[0], router.k), dtype=torch.float32, device=dev)
-    _check(_lib.pmpe_route(router._desc(logits, policy, bias, idx, w, load), _stream_of(logits)), "pmpe_route")
-    return idx, w
-
-
-@_placed
-def _route_backward(logits, router, policy, idx, dw):
-    T, dev = logits.shape[0], logits.device
-    _require(idx.device == dev and idx.dtype == torch.int32 and idx.shape == (T, router.k) and idx.is_contiguous(),
-             "Router: idx is int32 [T, k] on the logits' device")
-    _require(dw.device == dev and dw.dtype == torch.float32 and dw.shape == (T, router.k) and dw.is_contiguous(),
-             "Router: dw is FP32 [T, k] on the logits' device")
-    d_logits = torch.empty((T, router.E), dtype=logits.dtype, device=dev)
-    _check(_lib.pmpe_route_backward(router._desc(logits, policy, None, idx, None, None), dw.data_ptr(), d_logits.data_ptr(),
-                                    _stream_of(logits)), "pmpe_route_backward")
-    return d_logits
+        dev = logits.get_device()
+        if stream is not None or dev < 0 or dev != _device():
+            return _elsewhere(self.backward, logits, stream, logits, policy, idx, dw)
+        code, T, ld = self._logits(logits)
+        if policy is not None and not _vector(policy, T, dev, torch.uint8):
+            _bad("Router: policy is uint8 [T] on the logits' device")
+        if not _matrix(idx, T, self.k, dev, torch.int32):
+            _bad("Router: idx is int32 [T, k] on the logits' device")
+        if not _matrix(dw, T, self.k, dev, _F32):
+            _bad("Router: dw is FP32 [T, k] on the logits' device")
+        d_logits = torch.empty((T, self.E), dtype=logits.dtype, device=logits.device)
+        rc = _lib.pmpe_route_backward(_pack_route(T, self.E_pub, self.E_priv, self.k, code, *self._config, logits.data_ptr(), ld,
+                                                  _at(policy), 0, idx.data_ptr(), 0, 0), dw.data_ptr(), d_logits.data_ptr(),
+                                      _raw_stream(dev))
+        if rc:
+            _check(rc, "pmpe_route_backward")
+        return d_logits
 
 
 def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
@@ -689,31 +713,34 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
     max_norm = inf: the norm alone.  A norm that is not finite clips nothing.
     No tensor may share memory with another."""
     if isinstance(grads, dict):
-        _require(out is None or isinstance(out, dict) and out.keys() == grads.keys(), "clip_grad_norm: out is as grads")
-        out = None if out is None else [out[n] for n in grads]
+        if out is not None:
+            if not isinstance(out, dict) or out.keys() != grads.keys():
+                _bad("clip_grad_norm: out is as grads")
+            out = [out[n] for n in grads]
         grads = list(grads.values())
-    grads = list(grads)
-    _require(grads, "clip_grad_norm: no gradients")
-    return _clip(grads, float(max_norm), None if out is None else list(out), stream=stream)
-
-
-@_placed
-def _clip(grads, max_norm, out):
-    n, dev = len(grads), grads[0].device
-    _require(out is None or len(out) == n, "clip_grad_norm: one output for each gradient")
-    table = (Grad * n)()
-    for i, g in enumerate(grads):
-        o = g if out is None else out[i]
-        _require(g.device == dev and o.device == dev and g.dtype in _TYPES and o.dtype == g.dtype and o.shape == g.shape,
-                 "clip_grad_norm: gradients and outputs are FP32, BF16 or FP16 tensors of one device, outputs as their gradients")
-        if not (g.is_contiguous() and o.is_contiguous()):
-            _require(g.stride() == o.stride() and _dense(g), "clip_grad_norm: a gradient has gaps")
-        table[i] = (g.data_ptr(), o.data_ptr(), g.numel(), _TYPES[g.dtype])
-    norm = torch.empty((), dtype=torch.float32, device=dev)
+    n = len(grads)
+    if n == 0 or out is not None and len(out) != n:
+        _bad("clip_grad_norm: gradients, and an output for each or none, are wanted")
+    first = grads[0]
+    dev = first.get_device()
+    if stream is not None or dev < 0 or dev != _device():
+        return _elsewhere(clip_grad_norm, first, stream, grads, max_norm, out)
+    table = array.array("q")
+    for g, o in zip(grads, grads if out is None else out):
+        dt = g.dtype
+        if g.get_device() != dev or dt not in _TYPES:
+            _bad("clip_grad_norm: gradients are FP32, BF16 or FP16 tensors of one device")
+        if o is not g and (o.get_device() != dev or o.dtype is not dt or o.shape != g.shape):
+            _bad("clip_grad_norm: outputs are as their gradients")
+        if not (g.is_contiguous() and o.is_contiguous()) and (g.stride() != o.stride() or not _dense(g)):
+            _bad("clip_grad_norm: a gradient has gaps")
+        table.extend((g.data_ptr(), o.data_ptr(), g.numel(), _TYPES[dt]))  # pmpe_grad: the type in a word of its own
+    norm = torch.empty((), dtype=_F32, device=first.device)
     nb = _lib.pmpe_clip_workspace_size(n)
-    ws = torch.empty(nb, dtype=torch.uint8, device=dev)
-    _check(_lib.pmpe_clip_grad_norm(table, n, max_norm, norm.data_ptr(), ws.data_ptr(), nb, _stream_of(grads[0])),
-           "pmpe_clip_grad_norm")
+    ws = torch.empty(nb, dtype=torch.uint8, device=first.device)
+    rc = _lib.pmpe_clip_grad_norm(table.buffer_info()[0], n, max_norm, norm.data_ptr(), ws.data_ptr(), nb, _raw_stream(dev))
+    if rc:
+        _check(rc, "pmpe_clip_grad_norm")
     return norm
 
 

@@ -17,6 +17,31 @@ pytestmark = pytest.mark.skipif(shutil.which("nvcc") is None and not os.path.exi
 P = 0x10000000  # a device address that is never dereferenced
 
 
+class RmsNormDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int), ("H", ctypes.c_int), ("type", ctypes.c_int), ("weight_type", ctypes.c_int),
+                ("quant", ctypes.c_int), ("eps", ctypes.c_float), ("x", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("x_ld", ctypes.c_int64), ("residual_ld", ctypes.c_int64), ("h", ctypes.c_void_p), ("y", ctypes.c_void_p), ("scale", ctypes.c_void_p),
+                ("rstd", ctypes.c_void_p)]
+
+
+class RmsNormBackwardDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int), ("H", ctypes.c_int), ("type", ctypes.c_int), ("weight_type", ctypes.c_int),
+                ("dy_type", ctypes.c_int), ("dx_type", ctypes.c_int), ("dy", ctypes.c_void_p), ("h", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("rstd", ctypes.c_void_p), ("d_h", ctypes.c_void_p), ("dx", ctypes.c_void_p), ("dw", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class RouteDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("T", "E_pub", "E_priv", "k", "logits_type", "score", "renormalize", "groups_pub",
+                                            "top_groups_pub", "groups_priv", "top_groups_priv", "group_score")] + \
+               [("scale", ctypes.c_float), ("logits", ctypes.c_void_p), ("ld", ctypes.c_int64), ("policy", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("topk_idx", ctypes.c_void_p), ("topk_w", ctypes.c_void_p), ("load", ctypes.c_void_p)]
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int)]
+
+
 @pytest.fixture(scope="module")
 def pmpe():
     from paper_2608_06690_gb300 import build
@@ -30,13 +55,25 @@ def desc(cls, base, **over):
     return ctypes.byref(d)
 
 
+def test_packed_descriptors_match_the_structures(pmpe):
+    """The binding packs the descriptors as bytes: every field at its place."""
+    for cls, pack in ((RmsNormDesc, pmpe._pack_norm), (RmsNormBackwardDesc, pmpe._pack_norm_bwd), (RouteDesc, pmpe._pack_route)):
+        values = [i + 1 for i in range(len(cls._fields_))]
+        raw = pack(*values)
+        assert len(raw) == ctypes.sizeof(cls)
+        d = cls.from_buffer_copy(raw)
+        assert [getattr(d, n) for n, _ in cls._fields_] == values
+    assert ctypes.sizeof(Grad) == 32  # four 64-bit words, the type in the last one's low half
+    assert Grad.from_buffer_copy(np.array([1, 2, 3, 2], np.int64)).type == 2
+
+
 def test_rms_norm_refusals(pmpe):
     f = pmpe._lib.pmpe_rms_norm
     base = dict(T=4, H=256, type=1, weight_type=1, quant=0, eps=1e-6, x=P, residual=P, weight=P, x_ld=256, residual_ld=256,
                 h=P, y=P, scale=None, rstd=P)
 
     def rc(**over):
-        return f(desc(pmpe.RmsNormDesc, base, **over), None)
+        return f(desc(RmsNormDesc, base, **over), None)
 
     assert f(None, None) == pmpe.ERR_INVALID_ARG
     for bad in (dict(T=-1), dict(H=0), dict(H=-5), dict(type=3), dict(type=-1), dict(weight_type=2), dict(quant=3), dict(quant=-1),
@@ -58,7 +95,7 @@ def test_rms_norm_backward_refusals(pmpe):
                 workspace=P, workspace_bytes=need)
 
     def rc(**over):
-        return f(desc(pmpe.RmsNormBackwardDesc, base, **over), None)
+        return f(desc(RmsNormBackwardDesc, base, **over), None)
 
     assert f(None, None) == pmpe.ERR_INVALID_ARG
     for bad in (dict(T=-1), dict(H=0), dict(type=9), dict(weight_type=2), dict(dy_type=2), dict(dx_type=2), dict(dy=None),
@@ -79,7 +116,7 @@ def test_route_refusals(pmpe):
     f = pmpe._lib.pmpe_route
 
     def rc(**over):
-        return f(desc(pmpe.RouteDesc, ROUTE, **over), None)
+        return f(desc(RouteDesc, ROUTE, **over), None)
 
     assert f(None, None) == pmpe.ERR_INVALID_ARG
     for bad in (dict(T=-1), dict(k=0), dict(k=5), dict(E_pub=1), dict(E_priv=-1), dict(E_priv=1), dict(logits_type=3), dict(score=2),
@@ -108,7 +145,7 @@ def test_route_backward_refusals(pmpe):
     f = pmpe._lib.pmpe_route_backward
 
     def rc(dw=P, d_logits=P, **over):
-        return f(desc(pmpe.RouteDesc, ROUTE, **over), dw, d_logits, None)
+        return f(desc(RouteDesc, ROUTE, **over), dw, d_logits, None)
 
     for bad in (dict(dw=None), dict(d_logits=None), dict(k=0), dict(T=-1), dict(ld=3), dict(topk_idx=None)):
         assert rc(**bad) == pmpe.ERR_INVALID_ARG, bad
@@ -122,7 +159,7 @@ def test_clip_refusals(pmpe):
     assert size(-1) == 0 and size(0) > 0 and size(5000) > size(5)
 
     def rc(tensors, max_norm=1.0, norm=P, ws=P, nb=None, n=None):
-        table = (pmpe.Grad * max(1, len(tensors)))(*tensors)
+        table = (Grad * max(1, len(tensors)))(*tensors)
         return f(table, len(tensors) if n is None else n, max_norm, norm, ws, size(len(tensors)) if nb is None else nb, None)
 
     ok = (P, None, 1000, 0)
