@@ -26,6 +26,7 @@
 // and compared as integers: an FP64 instruction takes a warp some 60 clocks
 // here, and a selection wholly in FP64 was 16 us.
 #include <algorithm>
+#include <type_traits>
 
 #include "elem.cuh"
 
@@ -151,7 +152,8 @@ __device__ __forceinline__ int place_of(u64 key, int id, int count)
     return place;
 }
 
-// Orders a lane's packed choices, largest first.
+// A lane's largest packed choices in order: all of them up to four, the first
+// four of eight.
 template <int kV> __device__ __forceinline__ void sort_lane(uint32_t (&v)[kV])
 {
     auto cex = [&](int i, int j) {
@@ -163,39 +165,43 @@ template <int kV> __device__ __forceinline__ void sort_lane(uint32_t (&v)[kV])
         cex(0, 1);
     } else if constexpr (kV == 4) {
         cex(0, 1); cex(2, 3); cex(0, 2); cex(1, 3); cex(1, 2);
-    } else if constexpr (kV == 8) {
-        cex(0, 1); cex(2, 3); cex(4, 5); cex(6, 7);
-        cex(0, 2); cex(1, 3); cex(4, 6); cex(5, 7);
-        cex(1, 2); cex(5, 6);
-        cex(0, 4); cex(1, 5); cex(2, 6); cex(3, 7);
-        cex(2, 4); cex(3, 5);
-        cex(1, 2); cex(3, 4); cex(5, 6);
+    } else {
+        cex(0, 1); cex(2, 3); cex(0, 2); cex(1, 3); cex(1, 2);
+        cex(4, 5); cex(6, 7); cex(4, 6); cex(5, 7); cex(5, 6);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = max(v[i], v[7 - i]);  // the larger half, bitonic
+        cex(0, 2); cex(1, 3); cex(0, 1); cex(2, 3);
     }
 }
 
-// The k best of the packed choices in order: lane j < k gets the j-th (0:
-// none); the return value is the (k + 1)-th where want_next.  A packed choice
-// is the upper 24 bits of the choice's key over 255 - expert: one redux gives
-// the winner and who it is, and equal choices come by the lower id.
-template <int kV> __device__ __forceinline__ uint32_t pick_packed(uint32_t (&v)[kV], int k, bool want_next, int lane, uint32_t &mine)
+// The packed word of a choice: 24 bits of its key over 255 - expert, so that
+// one redux gives the winner and who it is, and equal choices come by the
+// lower id.  Those of -inf, no candidates, are below kLeast, all others above.
+constexpr uint32_t kLeast = 0x00800000u;
+
+// The `rounds` best of the packed choices in order: lane j gets the j-th, the
+// last one is returned.  whole: a lane ran out of its sorted ones.
+template <int kV> __device__ __forceinline__ uint32_t pick_packed(uint32_t (&v)[kV], int rounds, int lane, uint32_t &mine, bool &whole)
 {
+    constexpr int kDepth = kV < 4 ? kV : 4;
     sort_lane<kV>(v);
     mine = 0;
-    for (int j = 0; j < k; ++j) {
-        const uint32_t best = __reduce_max_sync(~0u, v[0]);
-        if (lane == j) mine = best;
-        if (v[0] == best) {  // the winner's lane alone, while any candidate is left
+    uint32_t best = 0;
+    for (int j = 0; j < rounds; ++j) {
+        best = __reduce_max_sync(~0u, v[0]);
+        mine = lane == j ? best : mine;
+        const bool won = v[0] == best;  // one lane alone, while any is left
 #pragma unroll
-            for (int i = 0; i + 1 < kV; ++i) v[i] = v[i + 1];
-            v[kV - 1] = 0;
-        }
+        for (int i = 0; i + 1 < kDepth; ++i) v[i] = won ? v[i + 1] : v[i];
+        v[kDepth - 1] = won ? 0u : v[kDepth - 1];
     }
-    return want_next ? __reduce_max_sync(~0u, v[0]) : 0u;
+    whole = kV > kDepth && __any_sync(~0u, v[0] == 0u);
+    return best;
 }
 
 // The same by whole 32-bit or 64-bit keys (0: no candidate), for the rows that
-// packed ones do not settle: lane j < k gets the j-th's expert (-1: none),
-// next the (k + 1)-th's.
+// packed ones do not settle: lane j <= k gets the j-th's expert (-1: none),
+// e_next the (k + 1)-th's.
 __device__ __forceinline__ uint32_t warp_max(uint32_t v) { return __reduce_max_sync(~0u, v); }
 __device__ __forceinline__ u64 warp_max(u64 v) { return warp_max64(v); }
 template <typename K, int kV> __device__ __forceinline__ void pick_whole(K (&key)[kV], int k, int lane, int &e_mine, int &e_next)
@@ -214,11 +220,8 @@ template <typename K, int kV> __device__ __forceinline__ void pick_whole(K (&key
         if (best == 0) return;  // uniform: no candidate is left
         // experts ascend with the lanes: the lowest lane holds the lowest one
         e = __shfl_sync(~0u, e, __ffs(__ballot_sync(~0u, mine == best)) - 1);
-        if (j < k) {
-            if (lane == j) e_mine = e;
-        } else {
-            e_next = e;
-        }
+        if (lane == j) e_mine = e;
+        if (j == k) e_next = e;
 #pragma unroll
         for (int i = 0; i < kV; ++i)
             if (e == lane * kV + i) key[i] = 0;
@@ -338,6 +341,7 @@ __device__ __noinline__ int settle_order(const Pool<T> &p, float mx, uint32_t wa
     return e;
 }
 
+// A lane's logits; -inf for what does not exist.
 template <typename T, int kV> __device__ __forceinline__ void load_logits(float (&z)[kV], const T *p, int lane, int E, bool vec)
 {
     struct alignas(sizeof(T) * kV) Pack { T v[kV]; };
@@ -352,7 +356,9 @@ template <typename T, int kV> __device__ __forceinline__ void load_logits(float 
     }
 }
 
-template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const ScoreParams p)
+// kBias: choices are scores + biases.  kGroups: a pool's groups may be limited.
+template <typename T, int kV, bool kBias, bool kGroups>
+__global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const ScoreParams p)
 {
     extern __shared__ int s_load[];
     __shared__ int s_list[kRouteWarps][32];
@@ -363,69 +369,99 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
         for (int e = threadIdx.x; e < E_all; e += blockDim.x) s_load[e] = 0;
         __syncthreads();
     }
-    for (int t = blockIdx.x * kRouteWarps + warp; t < p.T; t += gridDim.x * kRouteWarps) {
-        const int priv = p.policy != nullptr && p.policy[t] == 0x01 ? 1 : 0;
+    // a token's pool and logits are requested while the token before it is in work
+    const int step = gridDim.x * kRouteWarps;
+    auto pool_at = [&](int t) { return t < p.T && p.policy != nullptr && p.policy[t] == 0x01 ? 1 : 0; };
+    float z_next[kV];
+    auto fetch = [&](int t, int q) {
+        if (t >= p.T) return;
+        const T *row = (const T *)p.logits + t * p.ld + (q ? p.E_pub : 0);
+        load_logits<T, kV>(z_next, row, lane, q ? p.E_priv : p.E_pub, ((uintptr_t)row & (sizeof(T) * kV - 1)) == 0);
+    };
+    int t = blockIdx.x * kRouteWarps + warp;
+    int priv_next = pool_at(t), priv_after = pool_at(t + step), priv_bias = -1;
+    float bias[kV];
+    fetch(t, priv_next);
+    for (; t < p.T; t += step) {
+        const int priv = priv_next;
         const int base = priv ? p.E_pub : 0, E = priv ? p.E_priv : p.E_pub;
-        const Pool<T> pool = {(const T *)p.logits + t * p.ld + base, p.bias ? p.bias + base : nullptr, E, p.sigmoid, p.groups[priv],
+        const Pool<T> pool = {(const T *)p.logits + t * p.ld + base, kBias ? p.bias + base : nullptr, E, p.sigmoid, p.groups[priv],
                               p.top_groups[priv], p.top2, p.k};
-        const bool limited = pool.top < pool.n, scored = pool.bias != nullptr || (limited && p.top2);
-        float z[kV], choice[kV], val[kV];
-        load_logits<T, kV>(z, pool.row, lane, E, ((uintptr_t)pool.row & (sizeof(T) * kV - 1)) == 0);
-        uint32_t live = 0;
+        const bool limited = kGroups && pool.top < pool.n, scored = kBias || (limited && p.top2);
+        if (kBias && priv != priv_bias) {  // a lane's experts, and so its biases, change with the pool alone
 #pragma unroll
-        for (int i = 0; i < kV; ++i) {
-            live |= z[i] > kNone ? 1u << i : 0u;
-            z[i] = fminf(z[i], kLargest);
+            for (int i = 0; i < kV; ++i) bias[i] = lane * kV + i < E ? __ldg(pool.bias + lane * kV + i) : 0.f;
+            priv_bias = priv;
         }
+        float z[kV];  // -inf: not eligible
+#pragma unroll
+        for (int i = 0; i < kV; ++i) z[i] = z_next[i] > kNone ? fminf(z_next[i], kLargest) : kNone;
+        fetch(t + step, priv_after);
+        priv_next = priv_after;
+        priv_after = pool_at(t + 2 * step);
         float mx = kNone, sum = 1.f;
         if (!p.sigmoid && (!p.renorm || scored)) {  // the pool's softmax
 #pragma unroll
-            for (int i = 0; i < kV; ++i)
-                if ((live >> i) & 1u) mx = fmaxf(mx, z[i]);
+            for (int i = 0; i < kV; ++i) mx = fmaxf(mx, z[i]);
             mx = of(__reduce_max_sync(~0u, key_of(mx)));
             sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < kV; ++i)
-                if ((live >> i) & 1u) sum += expf(z[i] - mx);
+            for (int i = 0; i < kV; ++i) sum += z[i] > kNone ? expf(z[i] - mx) : 0.f;
             sum = warp_sum(sum);
         }
         auto score = [&](float zz) { return p.sigmoid ? 1.f / (1.f + expf(-zz)) : expf(zz - mx) / sum; };
-        // The error of an FP32 choice c is below err + 2^-24 |c|, with a fifth
-        // to spare.  Sigmoid: expf 2 ulp, which enters with s (1 - s), the sum
-        // and the quotient half an ulp each: 2^-22 s (3/2 - s) at most 2^-22.8.
-        // Softmax, with d = z - max: (|d| + 32) 2^-24 p, of which |d| p is at
-        // most 0.4 / sum: the difference's rounding in the exponent, expf 2 ulp,
-        // the same weighted in the sum, whose additions are 12 x 2^-24.
-        const float err = p.sigmoid ? 0x1.6p-23f : 0x1.5p-19f / sum;
-        float top_value = 0.f;
+        // The choices come from the fast exponential and quotient, whose error
+        // is known: __expf(x) 2 + 1.2 |x| ulp, __fdividef 2 ulp, ulp <= 2^-23.
+        // So a choice c is off by less than err + 2^-24 |c|, a fifth to spare:
+        // sigmoid: the exponential's error enters with s (1 - s), and s (1 - s)
+        // |z| < 0.23: 0.8, the sum 0.5, the quotient 2, 3.3 x 2^-23 in all;
+        // softmax, with d = z - max: d rounds by 2^-24 |d| and |d| p < 0.4 / sum;
+        // the sum (expf 2 ulp, d, 12 additions) is 22 x 2^-24 off; 30 x 2^-24 / sum.
+        const float err = p.sigmoid ? 0x1p-21f : 0x1.2p-19f / sum;
+        float val[kV];  // score + bias, where it is needed
+        if (scored) {
+            if (p.sigmoid) {
 #pragma unroll
-        for (int i = 0; i < kV; ++i) {
-            const bool on = (live >> i) & 1u;
-            val[i] = 0.f;
-            choice[i] = on ? z[i] : kNone;
-            if (scored && on) {
-                val[i] = score(z[i]);
-                if (pool.bias) choice[i] = val[i] += __ldg(pool.bias + lane * kV + i);
-                if (choice[i] > kNone) top_value = fmaxf(top_value, fabsf(val[i]));
+                for (int i = 0; i < kV; ++i) val[i] = __fdividef(1.f, 1.f + __expf(-z[i]));
+            } else {
+                const float inv_sum = 1.f / sum;
+#pragma unroll
+                for (int i = 0; i < kV; ++i) val[i] = __expf(z[i] - mx) * inv_sum;
+            }
+#pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                if (kBias) val[i] += bias[i];
+                // a bias of -inf (or NaN) takes its expert out too
+                val[i] = z[i] > kNone && val[i] > kNone ? val[i] : kNone;
             }
         }
+        float choice[kV];  // -inf: no candidate
+#pragma unroll
+        for (int i = 0; i < kV; ++i) choice[i] = kBias ? val[i] : z[i];
         bool exact = false;  // the whole selection again by exact values
-        if (limited) {
+        if (kGroups && limited) {
             const int n = pool.n, top = pool.top, size = E / n, seg = lanes_of_group<kV>(size);
-            // two sums of two values each, and their own rounding
-            if (scored) top_value = of(__reduce_max_sync(~0u, key_of(top_value)));
-            const float close = 4.f * err + 0x1p-20f * top_value;
+            float by[kV];  // what groups count by
+            float close = 0.f;
+#pragma unroll
+            for (int i = 0; i < kV; ++i) by[i] = p.top2 ? val[i] : choice[i];
+            if (scored) {  // two sums of two values each, and their own rounding
+                float top_value = 0.f;
+#pragma unroll
+                for (int i = 0; i < kV; ++i) top_value = fmaxf(top_value, val[i] > kNone ? fabsf(val[i]) : 0.f);
+                close = 4.f * err + 0x1p-20f * of(__reduce_max_sync(~0u, key_of(top_value)));
+            }
             if (seg) {
                 // every group at once: its lanes hold its two best after log2(seg) exchanges
                 float a = kNone, b = kNone;
 #pragma unroll
-                for (int i = 0; i < kV; ++i) add_two(a, b, choice[i] > kNone ? (p.top2 ? val[i] : choice[i]) : kNone);
+                for (int i = 0; i < kV; ++i) add_two(a, b, by[i]);
                 for (int off = 1; off < seg; off <<= 1) {
                     const float oa = __shfl_xor_sync(~0u, a, off), ob = __shfl_xor_sync(~0u, b, off);
                     add_two(a, b, oa);
                     add_two(a, b, ob);
                 }
-                const float second = b > kNone ? b : a;
+                const float least = p.top2 && b > kNone ? b : a;
                 if (p.top2 && b > kNone) a += b;
                 const int g = lane / seg;
                 int place = 0;
@@ -442,8 +478,7 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
                         uint32_t wanted = 0;
 #pragma unroll
                         for (int i = 0; i < kV; ++i)
-                            if (doubt && choice[i] > kNone && (p.top2 ? val[i] : choice[i]) >= (p.top2 ? second : a) - close)
-                                wanted |= 1u << i;
+                            if (doubt && by[i] > kNone && by[i] >= least - close) wanted |= 1u << i;
                         const bool first_lane = lane % seg == 0;
                         const uint32_t which = __reduce_or_sync(~0u, doubt && first_lane ? 1u << g : 0u);
                         const int need = top - __popc(__ballot_sync(~0u, g < n && in && first_lane));
@@ -452,14 +487,12 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
                         kept = in || (g < n && ((keep >> g) & 1u));
                     }
                 }
-                if (!kept) {
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) choice[i] = kNone;
-                }
+                for (int i = 0; i < kV; ++i) choice[i] = kept ? choice[i] : kNone;
             } else {
                 uint32_t key[kV];
 #pragma unroll
-                for (int i = 0; i < kV; ++i) key[i] = choice[i] > kNone ? key_of(p.top2 ? val[i] : choice[i]) : 0u;
+                for (int i = 0; i < kV; ++i) key[i] = by[i] > kNone ? key_of(by[i]) : 0u;
                 const float a = group_value<uint32_t, kV>(key, n, size, p.top2, lane);
                 int place = 0;
                 for (int q = 0; q < n; ++q) {
@@ -479,26 +512,26 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
                 }
             }
         }
-        // Neighbours in the order, the last one's being the first not chosen,
-        // are in doubt where their packed choices are equal (again from the
-        // whole ones) or their FP32 choices closer than those are exact (by
-        // exact values), unless their logits and biases are the same: a true
-        // tie.  16-bit logits without a bias are packed whole.
-        const bool inexact = pool.bias != nullptr || sizeof(T) == 4;
+        // Neighbours in the order, the last one's being the first not chosen
+        // (which lane k holds, and e_next), are in doubt where their packed
+        // choices are equal (again from the whole ones) or their FP32 choices
+        // closer than those are exact (by exact values), unless their logits
+        // and biases are the same: a true tie.  16-bit logits without a bias
+        // are packed whole.
+        constexpr bool inexact = kBias || sizeof(T) == 4;
         int e_mine, e_next;
-        bool whole = false;
+        bool whole;
         {
             uint32_t v[kV], mine;
 #pragma unroll
-            for (int i = 0; i < kV; ++i)
-                v[i] = choice[i] > kNone ? (key_of(choice[i]) & ~255u) | (uint32_t)(255 - (lane * kV + i)) : 0u;
-            const uint32_t next = pick_packed<kV>(v, p.k, inexact, lane, mine);
-            e_mine = mine ? 255 - (int)(mine & 255u) : -1;
-            e_next = next ? 255 - (int)(next & 255u) : -1;
+            for (int i = 0; i < kV; ++i) v[i] = (key_of(choice[i]) & ~255u) | (uint32_t)(255 - lane * kV - i);
+            const uint32_t last = pick_packed<kV>(v, inexact ? p.k + 1 : p.k, lane, mine, whole);
+            e_mine = mine >= kLeast ? 255 - (int)(mine & 255u) : -1;
+            e_next = last >= kLeast ? 255 - (int)(last & 255u) : -1;
             if (inexact) {
                 uint32_t after = __shfl_down_sync(~0u, mine, 1);
-                if (lane == p.k - 1) after = next;
-                whole = __any_sync(~0u, lane < p.k && after != 0u && (mine ^ after) < 256u);
+                if (lane == 31) after = last;  // of use where k = 32
+                whole = whole || __any_sync(~0u, lane < p.k && after >= kLeast && (mine ^ after) < 256u);
             }
         }
         if (whole) {
@@ -511,21 +544,18 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
         float zj = kNone, sj = 0.f;
         if (e_mine >= 0) {
             zj = logit(pool, e_mine);
-            if (need_score || pool.bias) sj = score(zj);
+            if (need_score || kBias) sj = score(zj);
         }
-        if (pool.bias && !exact) {
-            int e_after = __shfl_down_sync(~0u, e_mine, 1);
-            if (lane == p.k - 1) e_after = e_next;
-            bool doubt = false;
-            float c0 = kNone;
-            if (lane < p.k && e_mine >= 0) {
-                const float b0 = pool.bias[e_mine];
-                c0 = sj + b0;
-                if (e_after >= 0) {
-                    const float za = logit(pool, e_after), b1 = pool.bias[e_after], c1 = score(za) + b1;
-                    doubt = c0 - c1 <= 2.f * err + 0x1.4p-24f * (fabsf(c0) + fabsf(c1)) && !(b0 == b1 && zj == za);
-                }
+        if (kBias && !exact) {
+            const float b0 = e_mine >= 0 ? pool.bias[e_mine] : 0.f, c0 = e_mine >= 0 ? sj + b0 : kNone;
+            float z1 = __shfl_down_sync(~0u, zj, 1), b1 = __shfl_down_sync(~0u, b0, 1), c1 = __shfl_down_sync(~0u, c0, 1);
+            if (p.k == 32 && lane == 31) {  // no lane holds the 33rd
+                z1 = e_next >= 0 ? logit(pool, e_next) : kNone;
+                b1 = e_next >= 0 ? pool.bias[e_next] : 0.f;
+                c1 = e_next >= 0 ? score(z1) + b1 : kNone;
             }
+            const bool doubt = lane < p.k && c1 > kNone && c0 - c1 <= 2.f * err + 0x1.4p-24f * (fabsf(c0) + fabsf(c1)) &&
+                               !(b0 == b1 && zj == z1);
             if (__any_sync(~0u, doubt)) {
                 const float c = __shfl_sync(~0u, c0, p.k - 1), least = c - 2.02f * (err + 0x1.4p-24f * fabsf(c));
                 uint32_t wanted = 0;
@@ -683,35 +713,23 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
     }
 }
 
-template <template <typename, int> class Launch, typename P> cudaError_t dispatch(int type, int pool, const P &p, int grid, int smem, cudaStream_t st)
+// Calls go(T(), experts a lane) for the logits' type and the larger pool.
+template <typename Go> cudaError_t dispatch(int type, int pool, Go go)
 {
-    const int per = (pool + 31) / 32;
-    auto by_size = [&](auto tag) {
-        using T = decltype(tag);
-        if (per <= 1) return Launch<T, 1>::go(p, grid, smem, st);
-        if (per <= 2) return Launch<T, 2>::go(p, grid, smem, st);
-        if (per <= 4) return Launch<T, 4>::go(p, grid, smem, st);
-        return Launch<T, 8>::go(p, grid, smem, st);
+    auto by_size = [&](auto t) {
+        if (pool <= 64) return go(t, std::integral_constant<int, 2>());
+        if (pool <= 128) return go(t, std::integral_constant<int, 4>());
+        return go(t, std::integral_constant<int, 8>());
     };
     if (type == PMPE_F32) return by_size(float());
     if (type == PMPE_BF16) return by_size(bf16());
     return by_size(__half());
 }
 
-template <typename T, int kV> struct LaunchScores {
-    static cudaError_t go(const ScoreParams &p, int grid, int smem, cudaStream_t st)
-    {
-        return launch_pdl(route_scores_kernel<T, kV>, dim3(grid), dim3(32 * kRouteWarps), (size_t)smem, st, p);
-    }
-};
-template <typename T, int kV> struct LaunchScoresBwd {
-    static cudaError_t go(const ScoreBwdParams &p, int grid, int smem, cudaStream_t st)
-    {
-        return launch_pdl(route_scores_bwd_kernel<T, kV>, dim3(grid), dim3(32 * kRouteWarps), (size_t)smem, st, p);
-    }
-};
-
-int grid_of(int T, int num_sms) { return std::max(1, std::min((T + kRouteWarps - 1) / kRouteWarps, 4 * num_sms)); }
+// CTAs: up to eight an SM (prompts: T = 16384, 128 + 32 experts 8.3 us, with
+// four 12.4), four where a bias or groups take more registers (T = 8192, 256
+// experts in 8 groups 21.8 us, with eight 24.2).
+int grid_of(int T, int num_sms, int per_sm) { return std::max(1, std::min((T + kRouteWarps - 1) / kRouteWarps, per_sm * num_sms)); }
 
 }  // namespace
 
@@ -725,8 +743,18 @@ cudaError_t launch_route_scores(const pmpe_route_desc &d, int num_sms, cudaStrea
     p.groups[0] = d.groups_pub; p.groups[1] = d.groups_priv;
     p.top_groups[0] = d.top_groups_pub; p.top_groups[1] = d.top_groups_priv;
     p.scale = d.scale;
-    return dispatch<LaunchScores>(d.logits_type, std::max(d.E_pub, d.E_priv), p, grid_of(d.T, num_sms),
-                                  d.load ? (d.E_pub + d.E_priv) * 4 : 0, st);
+    const bool limited = d.top_groups_pub < d.groups_pub || (d.E_priv > 0 && d.top_groups_priv < d.groups_priv);
+    const dim3 grid(grid_of(d.T, num_sms, limited || d.bias ? 4 : 8)), block(32 * kRouteWarps);
+    const size_t smem = d.load ? (d.E_pub + d.E_priv) * sizeof(int) : 0;
+    return dispatch(d.logits_type, std::max(d.E_pub, d.E_priv), [&](auto t, auto v) {
+        using T = decltype(t);
+        constexpr int kV = decltype(v)::value;
+        if (d.bias)
+            return limited ? launch_pdl(route_scores_kernel<T, kV, true, true>, grid, block, smem, st, p)
+                           : launch_pdl(route_scores_kernel<T, kV, true, false>, grid, block, smem, st, p);
+        return limited ? launch_pdl(route_scores_kernel<T, kV, false, true>, grid, block, smem, st, p)
+                       : launch_pdl(route_scores_kernel<T, kV, false, false>, grid, block, smem, st, p);
+    });
 }
 
 cudaError_t launch_route_scores_backward(const pmpe_route_desc &d, const float *dw, void *d_logits, int num_sms,
@@ -738,7 +766,10 @@ cudaError_t launch_route_scores_backward(const pmpe_route_desc &d, const float *
     p.T = d.T; p.E_pub = d.E_pub; p.E_priv = d.E_priv; p.k = d.k; p.renorm = d.renormalize;
     p.sigmoid = d.score == PMPE_SCORE_SIGMOID;
     p.scale = d.scale;
-    return dispatch<LaunchScoresBwd>(d.logits_type, std::max(d.E_pub, d.E_priv), p, grid_of(d.T, num_sms), 0, st);
+    const dim3 grid(grid_of(d.T, num_sms, 8)), block(32 * kRouteWarps);
+    return dispatch(d.logits_type, std::max(d.E_pub, d.E_priv), [&](auto t, auto v) {
+        return launch_pdl(route_scores_bwd_kernel<decltype(t), decltype(v)::value>, grid, block, 0, st, p);
+    });
 }
 
 }  // namespace pmpe
