@@ -276,6 +276,18 @@ PMPE_API int pmpe_moe_backward_step(const pmpe_moe_desc *d, const void *dout, fl
                                     float *d_gate_priv, float *d_up_priv, float *d_down_priv, float *d_hidden,
                                     void *bwd_workspace, size_t bwd_workspace_bytes, void *stream);
 
+/* The backward of pmpe_moe_forward_routed(), of the forward just run with the
+ * same descriptor (its topk_idx and topk_w unchanged): the private experts'
+ * gradients and the hidden states' as pmpe_moe_backward_step() gives them, but
+ * without the router's part of either, and dL/dw of the given picks, d_w [T, k]
+ * FP32 (0 for a pick that was not taken), from which the caller's router goes
+ * on (pmpe_route_backward()).  bwd_workspace: of
+ * pmpe_moe_backward_step_workspace_size().  Preconditions, alignment and
+ * errors are those of pmpe_moe_backward_step(). */
+PMPE_API int pmpe_moe_backward_routed(const pmpe_moe_desc *d, const void *dout, float *d_w, float *d_gate_priv,
+                                      float *d_up_priv, float *d_down_priv, float *d_hidden, void *bwd_workspace,
+                                      size_t bwd_workspace_bytes, void *stream);
+
 /* Per-token policy bytes from per-request ones, for callers that carry one
  * trusted authorisation byte per request and the requests' cumulative token
  * offsets (cu_seqlens[0..n_req], device int32) instead of a byte per token.
@@ -299,6 +311,18 @@ PMPE_API int pmpe_policy_from_requests(const uint8_t *req_policy, const int32_t 
  * kernel sets PMPE_STATUS_PIPELINE_TIMEOUT in the status word and returns;
  * the outputs of that call are then not valid. */
 PMPE_API int pmpe_moe_forward(const pmpe_moe_desc *d, void *stream);
+
+/* The layer with a given route in the place of its own router (a model whose
+ * router is another: pmpe_route() below): topk_idx and topk_w are inputs,
+ * [T, k], and the router weights are not used.  The hard mask holds all the
+ * same: a pick outside the pool that the token's policy byte selects, or one
+ * that the token names twice, is not taken, and PMPE_STATUS_BAD_EXPERT_ID is
+ * set in the status word.  Such a pick, and one of -1 (no expert), runs as the
+ * lowest expert of the pool that the token does not name, with weight 0, so
+ * that every token has k rows; the audit counts it as what ran.  Outputs,
+ * audit, workspace and errors are those of pmpe_moe_forward();
+ * unmasked_control must be 0. */
+PMPE_API int pmpe_moe_forward_routed(const pmpe_moe_desc *d, void *stream);
 
 /* Run a subset of the stages (PMPE_STAGE_* bits), in pipeline order.  Each
  * stage reads what the previous stages left in the same workspace, so a

@@ -313,6 +313,32 @@ __global__ void bwd_router_kernel(const uint8_t *tau, const int32_t *idx, const 
     }
 }
 
+// dL/dw of given picks (one warp per token, lane j pick j): the per-32-column
+// partials of the pick's dispatch row, in order; 0 for a pick that was not
+// taken (the forward ran another expert in its place).
+__global__ void bwd_pick_kernel(const int32_t *idx_in, const int32_t *idx, const int32_t *slot_of, const float *gw_part,
+                                int n_part, int T, int k, int R, float *d_w)
+{
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const int warps = gridDim.x * (blockDim.x >> 5);
+    for (int t = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5); t < T; t += warps) {
+        if (lane >= k) continue;
+        const size_t r = (size_t)t * k + lane;
+        const int slot = slot_of[r];
+        float g = 0.f;
+        if (idx_in[r] == idx[r] && (unsigned)slot < (unsigned)R) {
+            const float *gp = gw_part + (size_t)slot * n_part;
+            for (int j = 0; j < n_part; j += 4) {
+                const float4 c = *reinterpret_cast<const float4 *>(gp + j);
+                g += ((c.x + c.y) + c.z) + c.w;
+            }
+        }
+        d_w[r] = g;
+    }
+}
+
 // dW_router[e][c] = sum_t dz[t][e] h[t][c] in FP32, split over the tokens:
 // CTA (x, y, z) owns a 32 x 128 output tile and the z-th token range, staged
 // through shared memory 32 tokens at a time, and writes its partial sum to
@@ -469,6 +495,13 @@ cudaError_t launch_router_dz(const Ctx &c, const float *gw_part, int both_pools,
     return launch_pdl(bwd_router_kernel, dim3(c.num_sms * 4), dim3(256), 0, c.stream, (const uint8_t *)c.tau,
                       (const int32_t *)c.idx, (const float *)c.w, (const int32_t *)c.slot_of, gw_part, s.I / 32, s.T,
                       s.E_pub, s.E_priv, s.k, s.renorm, both_pools, ld, (const float *)logit_part, ksplit, dz);
+}
+
+cudaError_t launch_pick_gradients(const Ctx &c, const int32_t *idx_in, const float *gw_part, float *d_w)
+{
+    const Shape &s = c.s;
+    return launch_pdl(bwd_pick_kernel, dim3(std::min((s.T + 7) / 8, c.num_sms * 8)), dim3(256), 0, c.stream, idx_in,
+                      (const int32_t *)c.idx, (const int32_t *)c.slot_of, gw_part, s.I / 32, s.T, s.k, s.T * s.k, d_w);
 }
 
 cudaError_t launch_router_term(const Ctx &c, const float *dz, int ld, const int32_t *pool_tok, const int *pool_n,

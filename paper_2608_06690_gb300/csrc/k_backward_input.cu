@@ -30,7 +30,7 @@ constexpr int kPadRows = 128;  // the padded row layout of the row launches
 // The sum runs in a fixed order (picks in top-k order, shared experts, the
 // pool's router rows), so the result does not depend on scheduling.  The
 // padded start of every routed expert's rows is rebuilt per CTA from the
-// dispatch offsets.
+// dispatch offsets.  dz null (with renorm 0): no router term.
 __global__ void __launch_bounds__(256) bwd_input_reduce_kernel(
     const bf16 *da, const bf16 *da_sh, const float *dz, int ld, const bf16 *router_pub, const bf16 *router_priv,
     const uint8_t *tau, const int32_t *idx, const int32_t *slot_of, const uint32_t *offsets, int T, int H, int E_pub,
@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(256) bwd_input_reduce_kernel(
         const int priv = tau[t] ? 1 : 0;
         const int e_base = priv ? E_pub : 0, E_pool = priv ? E_priv : E_pub;
         const bf16 *router = priv ? router_priv : router_pub;
-        const float *dzt = dz + (size_t)t * ld;
+        const float *dzt = dz ? dz + (size_t)t * ld : nullptr;
         __syncthreads();  // the previous token's picks are consumed
         if (tid < k) {
             const int e = idx[(size_t)t * k + tid];
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(256) bwd_input_reduce_kernel(
             const int pe = e - e_base;
             const bool in_pool = pe >= 0 && pe < E_pool;
             s_pe[tid] = in_pool ? pe : -1;
-            s_dz[tid] = in_pool ? dzt[pe] : 0.f;
+            s_dz[tid] = in_pool && dzt ? dzt[pe] : 0.f;
         }
         __syncthreads();
         for (int c = tid; c < nv; c += blockDim.x) {
@@ -181,16 +181,17 @@ static InScratch input_scratch(const Shape &s, uint8_t *base)
 // term (dz rows max(E_pub, E_priv) apart): renormalised routing adds the k
 // picks' router rows in the same kernel, the pool softmax its dense term in
 // a tiled GEMM afterwards.
-static cudaError_t launch_input_reduce(const Ctx &c, const InScratch &b, float *d_hidden)
+static cudaError_t launch_input_reduce(const Ctx &c, const InScratch &b, float *d_hidden, bool router = true)
 {
     const Shape &s = c.s;
     const int ld = std::max(s.E_pub, s.E_priv);
+    const float *dz = router ? b.dz : nullptr;
     const cudaError_t err = launch_pdl(bwd_input_reduce_kernel, dim3(std::min(s.T, c.num_sms * 8)), dim3(256), 0, c.stream,
-                      (const bf16 *)b.da, (const bf16 *)b.da_sh, (const float *)b.dz, ld, c.router_pub,
+                      (const bf16 *)b.da, (const bf16 *)b.da_sh, dz, ld, c.router_pub,
                       c.router_priv, (const uint8_t *)c.tau, (const int32_t *)c.idx, (const int32_t *)c.slot_of,
-                      (const uint32_t *)c.offsets, s.T, s.H, s.E_pub, s.E_priv, s.E_sh, s.k, s.T * s.k, s.renorm,
-                      b.tp, d_hidden);
-    if (err != cudaSuccess || s.renorm) return err;
+                      (const uint32_t *)c.offsets, s.T, s.H, s.E_pub, s.E_priv, s.E_sh, s.k, s.T * s.k,
+                      router ? s.renorm : 0, b.tp, d_hidden);
+    if (err != cudaSuccess || s.renorm || !router) return err;
     return launch_router_term(c, b.dz, ld, b.pool_tok, b.pool_n, d_hidden);
 }
 
@@ -268,18 +269,15 @@ size_t backward_step_workspace_bytes(const Shape &s)
     return step_scratch(s, nullptr).bytes;
 }
 
-cudaError_t launch_backward_step(const Ctx &c, const bf16 *dout, float *d_router, float *d_gate, float *d_up,
-                                 float *d_down, float *d_hidden, uint8_t *bws)
+// The row launches of both backwards: Z, [dG | dU], w act and dL/dw partials
+// and dA of the routed experts, the same of the shared ones.
+static cudaError_t launch_step_rows(const Ctx &c, const StepScratch &st, const RowsGroups &g, const bf16 *dout)
 {
     const Shape &s = c.s;
     const int R = s.T * s.k, H = s.H, E = s.E();
-    const StepScratch st = step_scratch(s, bws);
     const InScratch &b = st.in;
-    cudaStream_t stream = c.stream;
-
-    cudaError_t err = launch_gather_rows(dout, c.tok_of_slot, c.offsets, 0, E, R, H, b.dout_rows, c.num_sms, stream);
+    cudaError_t err = launch_gather_rows(dout, c.tok_of_slot, c.offsets, 0, E, R, H, b.dout_rows, c.num_sms, c.stream);
     if (err != cudaSuccess) return err;
-    const RowsGroups g{0, E, 0, b.rp};
     if ((err = launch_rows_z(c, g, b.dout_rows, (uint64_t)R + 64, 1, b.zpad)) != cudaSuccess) return err;
     if ((err = launch_rows_gu(c, g, c.a_perm, (uint64_t)R, b.zpad, b.dgu, st.wact, b.gw_part)) != cudaSuccess)
         return err;
@@ -292,12 +290,38 @@ cudaError_t launch_backward_step(const Ctx &c, const bf16 *dout, float *d_router
             return err;
         if ((err = launch_rows_da(c, gs, b.dgu_sh, b.da_sh)) != cudaSuccess) return err;
     }
+    return cudaSuccess;
+}
+
+cudaError_t launch_backward_step(const Ctx &c, const bf16 *dout, float *d_router, float *d_gate, float *d_up,
+                                 float *d_down, float *d_hidden, uint8_t *bws)
+{
+    const Shape &s = c.s;
+    const StepScratch st = step_scratch(s, bws);
+    const InScratch &b = st.in;
+    const RowsGroups g{0, s.E(), 0, b.rp};
+    cudaError_t err = launch_step_rows(c, st, g, dout);
+    if (err != cudaSuccess) return err;
     const int ld = std::max(s.E_pub, s.E_priv);
     if ((err = launch_router_dz(c, b.gw_part, 1, ld, b.dz, b.pool_tok, b.pool_n, b.logit_part)) != cudaSuccess) return err;
     if ((err = launch_router_wgrad(c, b.dz, ld, st.part, st.active, d_router)) != cudaSuccess) return err;
     if ((err = launch_backward_wgrad(c, b.dout_rows, b.dgu, st.wact, d_gate, d_up, d_down, &g)) != cudaSuccess)
         return err;
     return launch_input_reduce(c, b, d_hidden);
+}
+
+cudaError_t launch_backward_routed(const Ctx &c, const int32_t *idx_in, const bf16 *dout, float *d_w, float *d_gate,
+                                   float *d_up, float *d_down, float *d_hidden, uint8_t *bws)
+{
+    const StepScratch st = step_scratch(c.s, bws);
+    const InScratch &b = st.in;
+    const RowsGroups g{0, c.s.E(), 0, b.rp};
+    cudaError_t err = launch_step_rows(c, st, g, dout);
+    if (err != cudaSuccess) return err;
+    if ((err = launch_pick_gradients(c, idx_in, b.gw_part, d_w)) != cudaSuccess) return err;
+    if ((err = launch_backward_wgrad(c, b.dout_rows, b.dgu, st.wact, d_gate, d_up, d_down, &g)) != cudaSuccess)
+        return err;
+    return launch_input_reduce(c, b, d_hidden, false);
 }
 
 }  // namespace pmpe

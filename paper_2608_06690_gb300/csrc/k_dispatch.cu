@@ -13,6 +13,10 @@
 // status word.  The backward, which reads the dispatched rows as one matrix,
 // fills it with gather_dispatch_rows_kernel.
 //
+// A route given by the caller takes the router's place (adopt_route_kernel):
+// the picks are checked against the policy and written with the tickets and
+// tile counts that the dispatch reads.
+//
 // Combine: out_t = bf16( sum_{j < k} y[slot(t, j)] + y_shared[t] ), summed in
 // FP32 in a fixed order (j ascending, then shared), so the result of a token
 // never depends on the other tokens of the batch.
@@ -114,6 +118,88 @@ __global__ void __launch_bounds__(kDispThreads) dispatch_kernel(const DispatchPa
     }
     for (int r = blockIdx.x * kDispThreads + threadIdx.x; r < p.R; r += gridDim.x * kDispThreads)
         resolve_slot(p, s_off, r);
+}
+
+struct AdoptParams {
+    const int32_t *idx_in;        // [T, k] the caller's picks
+    const float *w_in;
+    const uint8_t *policy;
+    int T, k, E_pub, E_priv, slots4;
+    uint8_t *tau;
+    int32_t *idx, *ticket;        // [T, k] the picks as they run, and their tickets
+    float *w;
+    uint32_t *tile_counts;        // [E][slots4] the column of this CTA's tile
+    uint32_t *status, *route_count, *route_priv_rows;
+};
+
+// The given route in the router's form, a CTA per tile of 128 consecutive
+// tokens and a thread per token.  The hard mask holds for given picks too: one
+// outside the token's pool, or named twice, is not taken (and recorded in the
+// status word); like a pick of -1 (no expert) it runs as the lowest expert of
+// the pool that the token does not name, with weight 0, so that every token
+// keeps k rows.  A row's position among the tile's rows of its expert is its
+// rank by token (a 128-bit token mask per expert: the rank is a popcount), so
+// the dispatch order is the router's: by expert, then by token.
+constexpr int kAdoptTile = 128;
+__global__ void __launch_bounds__(kAdoptTile) adopt_route_kernel(const AdoptParams p)
+{
+    __shared__ uint32_t s_mask[2 * kMaxPool][4];
+    pdl_trigger();
+    pdl_wait();
+    const int E = p.E_pub + p.E_priv, tile = blockIdx.x, t = tile * kAdoptTile + threadIdx.x;
+    for (int i = threadIdx.x; i < 4 * E; i += kAdoptTile) (&s_mask[0][0])[i] = 0u;
+    __syncthreads();
+    const uint32_t bit = 1u << (threadIdx.x & 31);
+    const int word = threadIdx.x >> 5;
+    int base = 0, pool = 0;
+    if (t < p.T) {
+        const bool allow = p.policy != nullptr && p.policy[t] == 0x01;
+        base = allow ? p.E_pub : 0;
+        pool = allow ? p.E_priv : p.E_pub;
+        p.tau[t] = allow ? 1 : 0;
+        const size_t at = (size_t)t * p.k;
+        bool refused = false;
+        int missing = 0;
+        for (int j = 0; j < p.k; ++j) {
+            const int e = p.idx_in[at + j], local = e - base;
+            // this thread alone sets its bit
+            const bool in_pool = local >= 0 && local < pool, taken = in_pool && (s_mask[base + local][word] & bit);
+            if (in_pool && !taken) {
+                atomicOr(&s_mask[base + local][word], bit);
+                p.idx[at + j] = e;
+                p.w[at + j] = p.w_in[at + j];
+            } else {
+                refused = refused || e != -1;
+                p.idx[at + j] = -1;
+                ++missing;
+            }
+        }
+        int free = 0;
+        for (int j = 0; missing > 0 && j < p.k; ++j) {
+            if (p.idx[at + j] >= 0) continue;
+            while (s_mask[base + free][word] & bit) ++free;  // k <= pool: there is one
+            atomicOr(&s_mask[base + free][word], bit);
+            p.idx[at + j] = base + free;
+            p.w[at + j] = 0.f;
+            --missing;
+        }
+        if (refused && p.status) atomicOr(p.status, PMPE_STATUS_BAD_EXPERT_ID);
+        if (p.route_priv_rows) atomicAdd(&p.route_priv_rows[t], allow ? (unsigned)p.k : 0u);
+    }
+    __syncthreads();
+    if (t < p.T) {
+        for (int j = 0; j < p.k; ++j) {
+            const uint32_t *m = s_mask[p.idx[(size_t)t * p.k + j]];
+            int rank = __popc(m[word] & (bit - 1u));
+            for (int i = 0; i < word; ++i) rank += __popc(m[i]);
+            p.ticket[(size_t)t * p.k + j] = kAdoptTile * tile + rank;
+        }
+    }
+    for (int e = threadIdx.x; e < E; e += kAdoptTile) {
+        const uint32_t n = __popc(s_mask[e][0]) + __popc(s_mask[e][1]) + __popc(s_mask[e][2]) + __popc(s_mask[e][3]);
+        p.tile_counts[(size_t)e * p.slots4 + tile] = n;
+        if (n && p.route_count) atomicAdd(&p.route_count[e], n);
+    }
 }
 
 // The token rows of the dispatch slots [offsets[g0], offsets[g1]) copied into
@@ -360,6 +446,18 @@ cudaError_t launch_permute(const Ctx &c)
     p.status = c.audit.status;
     const int grid = std::max(1, std::min((R + kDispThreads - 1) / kDispThreads, 4 * c.num_sms));
     return launch_pdl(dispatch_kernel, dim3(grid), dim3(kDispThreads), 0, c.stream, p);
+}
+
+cudaError_t launch_adopt_route(const Ctx &c, const int32_t *idx, const float *w)
+{
+    const Shape &s = c.s;
+    AdoptParams p;
+    p.idx_in = idx; p.w_in = w; p.policy = c.policy;
+    p.T = s.T; p.k = s.k; p.E_pub = s.E_pub; p.E_priv = s.E_priv; p.slots4 = router_slots4(s.T);
+    p.tau = c.tau; p.idx = c.idx; p.ticket = c.ticket; p.w = c.w; p.tile_counts = c.tile_counts;
+    p.status = c.audit.status; p.route_count = c.audit.route_count; p.route_priv_rows = c.audit.route_priv_rows;
+    // every tile slot's column is written, zeros for those without tokens
+    return launch_pdl(adopt_route_kernel, dim3(router_slots(s.T)), dim3(kAdoptTile), 0, c.stream, p);
 }
 
 cudaError_t launch_combine(const Ctx &c)

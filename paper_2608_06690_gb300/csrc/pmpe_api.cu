@@ -372,6 +372,68 @@ int pmpe_moe_backward_step(const pmpe_moe_desc *d, const void *dout, float *d_ro
                : PMPE_ERR_CUDA;
 }
 
+// The context of a call with a given route: the descriptor's topk_idx and
+// topk_w are inputs, the checked picks live in the workspace.
+static int make_routed_ctx(const pmpe_moe_desc *d, void *stream, Ctx *c)
+{
+    if (!d || d->unmasked_control != 0 || (d->T > 0 && (!d->topk_idx || !d->topk_w))) return PMPE_ERR_INVALID_ARG;
+    const int rc = make_ctx(d, stream, c);
+    if (rc != PMPE_OK) return rc;
+    pmpe_workspace_layout L;
+    compute_layout(c->s, &L);
+    c->idx = (int32_t *)((uint8_t *)d->workspace + L.topk_idx);
+    c->w = (float *)((uint8_t *)d->workspace + L.topk_w);
+    return PMPE_OK;
+}
+
+int pmpe_moe_forward_routed(const pmpe_moe_desc *d, void *stream)
+{
+    Ctx c;
+    const int rc = make_routed_ctx(d, stream, &c);
+    if (rc != PMPE_OK) return rc;
+    if (c.s.T == 0) return PMPE_OK;
+    cudaError_t err = launch_adopt_route(c, d->topk_idx, d->topk_w);
+    if (err == cudaSuccess) err = launch_permute(c);
+    if (err == cudaSuccess) err = launch_experts(c, false, false);  // the dispatch cleared its counters
+    if (err == cudaSuccess) err = launch_combine(c);
+    return err == cudaSuccess ? PMPE_OK : PMPE_ERR_CUDA;
+}
+
+int pmpe_moe_backward_routed(const pmpe_moe_desc *d, const void *dout, float *d_w, float *d_gate_priv, float *d_up_priv,
+                             float *d_down_priv, float *d_hidden, void *bwd_workspace, size_t bwd_workspace_bytes,
+                             void *stream)
+{
+    // every argument is checked before the first CUDA call
+    if (!d) return PMPE_ERR_INVALID_ARG;
+    const Shape s = shape_of(d);
+    const void *need[] = {d_gate_priv, d_up_priv, d_down_priv};
+    for (const void *q : need)
+        if (!q || !aligned16(q)) return PMPE_ERR_INVALID_ARG;
+    const void *rows[] = {dout, d_w, d_hidden};
+    for (const void *q : rows)
+        if (s.T > 0 && (!q || !aligned16(q))) return PMPE_ERR_INVALID_ARG;
+    if (shape_ok(s) && s.T > 0 &&
+        (!bwd_workspace || bwd_workspace_bytes < backward_step_workspace_bytes(s) ||
+         ((uintptr_t)bwd_workspace & 255u)))
+        return PMPE_ERR_WORKSPACE;
+    Ctx c;
+    const int rc = make_routed_ctx(d, stream, &c);
+    if (rc != PMPE_OK) return rc;
+    if (s.T == 0) {  // nothing routed: every parameter gradient is zero
+        cudaStream_t st = (cudaStream_t)stream;
+        const size_t ih = (size_t)s.E_priv * s.I * s.H * sizeof(float);
+        cudaError_t err = cudaMemsetAsync(d_gate_priv, 0, ih, st);
+        if (err == cudaSuccess) err = cudaMemsetAsync(d_up_priv, 0, ih, st);
+        if (err == cudaSuccess) err = cudaMemsetAsync(d_down_priv, 0, ih, st);
+        return err == cudaSuccess ? PMPE_OK : PMPE_ERR_CUDA;
+    }
+    if (launch_gather_dispatch_rows(c, c.saved_gu ? s.E_pub : 0, s.E()) != cudaSuccess) return PMPE_ERR_CUDA;
+    return launch_backward_routed(c, d->topk_idx, (const bf16 *)dout, d_w, d_gate_priv, d_up_priv, d_down_priv, d_hidden,
+                                  (uint8_t *)bwd_workspace) == cudaSuccess
+               ? PMPE_OK
+               : PMPE_ERR_CUDA;
+}
+
 int pmpe_moe_forward(const pmpe_moe_desc *d, void *stream)
 {
     return pmpe_moe_forward_stages(d, PMPE_STAGE_ALL, stream);

@@ -87,6 +87,9 @@ bool route_writes_dispatch(const Ctx &c);
 // Whether launch_route takes the cluster router (no memset before it; the
 // dispatch derives the per-expert counts from tile_counts) or the chunked one.
 bool route_uses_cluster_kernel(const Shape &s, int unmasked, int num_sms);
+// A route given by the caller in the router's place: the checked picks into
+// c.idx and c.w, with what launch_permute reads.
+cudaError_t launch_adopt_route(const Ctx &c, const int32_t *idx, const float *w);
 cudaError_t launch_permute(const Ctx &c);
 cudaError_t launch_gateup(const Ctx &c);
 cudaError_t launch_down(const Ctx &c);
@@ -124,6 +127,11 @@ cudaError_t launch_backward_input(const Ctx &c, const bf16 *dout, float *d_hidde
 size_t backward_step_workspace_bytes(const Shape &s);
 cudaError_t launch_backward_step(const Ctx &c, const bf16 *dout, float *d_router, float *d_gate, float *d_up,
                                  float *d_down, float *d_hidden, uint8_t *bws);
+// The same after a given route: dL/dw of the caller's picks in place of the
+// router's parts (idx_in: those picks).
+cudaError_t launch_backward_routed(const Ctx &c, const int32_t *idx_in, const bf16 *dout, float *d_w, float *d_gate,
+                                   float *d_up, float *d_down, float *d_hidden, uint8_t *bws);
+cudaError_t launch_pick_gradients(const Ctx &c, const int32_t *idx_in, const float *gw_part, float *d_w);
 // Its tensor-core GEMMs (k_backward_tc.cu): rows of the padded layout, the
 // dL/da and gate/up recompute launches, and the weight-gradient launch.
 size_t backward_padded_rows(const Shape &s);

@@ -105,6 +105,7 @@ EXPORTED = ("pmpe_moe_workspace_size", "pmpe_moe_workspace_layout", "pmpe_audit_
             "pmpe_policy_from_requests", "pmpe_moe_backward_workspace_size", "pmpe_moe_backward_private",
             "pmpe_moe_backward_input_workspace_size", "pmpe_moe_backward_input",
             "pmpe_moe_backward_step_workspace_size", "pmpe_moe_backward_step", "pmpe_saved_gu_floats",
+            "pmpe_moe_forward_routed", "pmpe_moe_backward_routed",
             "pmpe_rms_norm", "pmpe_rms_norm_backward_workspace_size", "pmpe_rms_norm_backward", "pmpe_route",
             "pmpe_route_backward", "pmpe_clip_workspace_size", "pmpe_clip_grad_norm")
 
@@ -175,6 +176,10 @@ _lib.pmpe_moe_backward_step_workspace_size.restype = ctypes.c_size_t
 _lib.pmpe_moe_backward_step_workspace_size.argtypes = [ctypes.c_int] * 7
 _lib.pmpe_moe_backward_step.restype = ctypes.c_int
 _lib.pmpe_moe_backward_step.argtypes = [ctypes.POINTER(MoeDesc)] + [_vp] * 7 + [ctypes.c_size_t, _vp]
+_lib.pmpe_moe_forward_routed.restype = ctypes.c_int
+_lib.pmpe_moe_forward_routed.argtypes = [ctypes.POINTER(MoeDesc), _vp]
+_lib.pmpe_moe_backward_routed.restype = ctypes.c_int
+_lib.pmpe_moe_backward_routed.argtypes = [ctypes.POINTER(MoeDesc)] + [_vp] * 7 + [ctypes.c_size_t, _vp]
 _lib.pmpe_saved_gu_floats.restype = ctypes.c_size_t
 _lib.pmpe_saved_gu_floats.argtypes = [ctypes.c_int] * 4
 _lib.pmpe_policy_from_requests.restype = ctypes.c_int
@@ -338,6 +343,7 @@ class MoeLayer:
         self._route_out = (None, None)  # the last forward's caller-owned route outputs
         self._saved_gu = None           # the last forward's saved G | U, when it saved them
         self._saved_buf = None
+        self._given = False             # the last forward ran a given route
 
     def workspace(self, T: int) -> torch.Tensor:
         return self._ws.get(workspace_size(self._shape_T(T)))
@@ -347,8 +353,11 @@ class MoeLayer:
         return LayerShape(T, s.H, s.I, s.E_pub, s.E_priv, s.E_sh, s.k, s.renormalize)
 
     def forward(self, hidden, policy, out=None, topk_idx=None, topk_w=None, audit=None, stages=STAGE_ALL,
-                stream=None, unmasked_control: bool = False, save_for_backward: bool = False):
+                stream=None, unmasked_control: bool = False, save_for_backward: bool = False, route=None):
         """Enqueue the layer on ``stream`` (default: the current stream).
+        ``route``: (idx, w), int32 and FP32 [T, k], as ``Router.route`` gives
+        them, in the place of the layer's own router; its backward is
+        ``backward_routed``.  A pick outside the token's pool is not taken.
         ``unmasked_control`` runs the paper's soft-router control instead of
         the method: routing over the concatenated pool without the hard mask.
         ``save_for_backward`` also keeps the gate and up accumulators of the
@@ -368,12 +377,58 @@ class MoeLayer:
             if self._saved_buf is None or self._saved_buf.numel() < n:
                 self._saved_buf = torch.empty(max(n, 4), dtype=torch.float32, device=hidden.device)
             saved = self._saved_buf
+        if route is not None:
+            if topk_idx is not None or topk_w is not None or unmasked_control or stages != STAGE_ALL:
+                _bad("MoeLayer.forward: a given route takes the place of the route log, the control and the stages")
+            topk_idx, topk_w = route
+            for v, dt in ((topk_idx, torch.int32), (topk_w, torch.float32)):
+                if not _matrix(v, T, s.k, hidden.get_device(), dt):
+                    _bad("MoeLayer.forward: route is (idx, w), int32 and FP32 [T, k] on the layer's device")
         desc = make_desc(s, self.weights, hidden, policy, out, self.workspace(T), topk_idx, topk_w, audit,
                          unmasked_control, saved)
-        forward_desc(desc, stages, stream)
+        if route is not None:
+            _check(_lib.pmpe_moe_forward_routed(ctypes.byref(desc), _stream(stream)), "pmpe_moe_forward_routed")
+        else:
+            forward_desc(desc, stages, stream)
+        self._given = route is not None
         self._route_out = (topk_idx, topk_w)
         self._saved_gu = saved
         return out
+
+    def _own_route(self, what: str):
+        if self._given:
+            _bad(f"MoeLayer.{what}: the last forward ran a given route: backward_routed is its backward")
+
+    def backward_routed(self, hidden, policy, dout, stream=None):
+        """Backward of the forward just run with a given route, the same hidden
+        states and policy on the same stream: (grads, d_hidden, d_w).  grads:
+        the private experts' d_gate, d_up and d_down (FP32); d_hidden: that of
+        the hidden states through the experts (FP32, without the caller's
+        router's part); d_w: that of the route's weights (FP32 [T, k]), for
+        ``Router.backward``."""
+        T = hidden.shape[0]
+        s = self._shape_T(T)
+        if not self._given:
+            _bad("MoeLayer.backward_routed: the last forward ran the layer's own router")
+        assert dout.is_contiguous() and dout.dtype == torch.bfloat16 and dout.shape == (T, s.H)
+        dev = hidden.device
+        g = {n: torch.empty(shp, dtype=torch.float32, device=dev) for n, shp in private_gradient_shapes(s).items()
+             if n != "d_router"}
+        d_hidden = torch.empty((T, s.H), dtype=torch.float32, device=dev)
+        d_w = torch.empty((T, s.k), dtype=torch.float32, device=dev)
+        nb = _lib.pmpe_moe_backward_step_workspace_size(s.T, s.H, s.I, s.E_pub, s.E_priv, s.E_sh, s.k)
+        if nb == 0:
+            raise PmpeError(ERR_UNSUPPORTED_SHAPE, "pmpe_moe_backward_step_workspace_size")
+        if self._bws is None or self._bws.numel() < nb:
+            self._bws = torch.empty(nb, dtype=torch.uint8, device=dev)
+        bws = self._bws
+        topk_idx, topk_w = self._route_out
+        desc = make_desc(s, self.weights, hidden, policy, dout, self.workspace(T), topk_idx, topk_w,
+                         saved_gu=self._saved_gu)
+        _check(_lib.pmpe_moe_backward_routed(ctypes.byref(desc), _ptr(dout), _ptr(d_w), _ptr(g["d_gate"]), _ptr(g["d_up"]),
+                                             _ptr(g["d_down"]), _ptr(d_hidden), _ptr(bws), bws.numel(), _stream(stream)),
+               "pmpe_moe_backward_routed")
+        return g, d_hidden, d_w
 
     def backward_private(self, hidden, policy, dout, topk_idx=None, topk_w=None, stream=None) -> dict:
         """Gradients of sum(dout * out) with respect to the private parameters
@@ -381,6 +436,7 @@ class MoeLayer:
         hidden states and policy on the same stream (its workspace holds the
         route and the activations; the route outputs default to those that
         forward wrote).  The public parameters get none."""
+        self._own_route("backward_private")
         T = hidden.shape[0]
         s = self._shape_T(T)
         assert dout.is_contiguous() and dout.dtype == torch.bfloat16 and dout.shape == (T, s.H)
@@ -407,6 +463,7 @@ class MoeLayer:
         states and policy on the same stream, in one pass: the private
         parameters' gradients (as backward_private) and the gradient of the
         hidden states (as backward_input), each bitwise as those calls give."""
+        self._own_route("backward")
         T = hidden.shape[0]
         s = self._shape_T(T)
         assert dout.is_contiguous() and dout.dtype == torch.bfloat16 and dout.shape == (T, s.H)
@@ -433,6 +490,7 @@ class MoeLayer:
         (FP32), through the frozen layer, for the forward just run with the
         same hidden states and policy on the same stream: the routed experts
         of each token's pool, the shared experts and that pool's router."""
+        self._own_route("backward_input")
         T = hidden.shape[0]
         s = self._shape_T(T)
         assert dout.is_contiguous() and dout.dtype == torch.bfloat16 and dout.shape == (T, s.H)
@@ -630,6 +688,7 @@ class Router:
     """Routing from given logits for models whose router is not the layer's
     own softmax: softmax or sigmoid scores, a bias for balance, group limits,
     top-k and weights, each token inside the pool its policy byte selects.
+    ``MoeLayer.forward(route=...)`` runs the experts with the result.
 
     score: "softmax" (over the token's pool) or "sigmoid".  groups,
     groups_priv: (groups of the pool, groups kept); group_score: "max" or

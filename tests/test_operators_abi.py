@@ -248,3 +248,48 @@ def test_reference_route_by_hand():
     assert idx.tolist() == [[0, 1]]
     idx, w = ref.route(np.full((1, 6), -np.inf), None, 6, 0, 2)
     assert idx.tolist() == [[-1, -1]] and w.tolist() == [[0.0, 0.0]]
+
+
+def test_routed_layer_refusals(pmpe):
+    """A given route needs both of its arrays, and no control."""
+    from paper_2608_06690_gb300.inputs import LayerShape
+
+    class Fake:
+        def __init__(self, addr=P):
+            self.addr = addr
+
+        def data_ptr(self):
+            return self.addr
+
+        def numel(self):
+            return 1 << 40
+
+        def element_size(self):
+            return 1
+
+    p = Fake()
+    W = {n: p for n in ("router_pub", "router_priv", "gate_pub", "up_pub", "down_pub", "gate_priv", "up_priv", "down_priv")}
+    shape = LayerShape(64, 256, 128, 8, 4, 0, 2, True)
+    fwd, bwd = pmpe._lib.pmpe_moe_forward_routed, pmpe._lib.pmpe_moe_backward_routed
+    need = pmpe._lib.pmpe_moe_backward_step_workspace_size(64, 256, 128, 8, 4, 0, 2)
+
+    def d(**over):
+        kw = dict(topk_idx=p, topk_w=p)
+        kw.update(over)
+        return ctypes.byref(pmpe.make_desc(kw.pop("shape", shape), W, p, None, p, kw.pop("workspace", p), **kw))
+
+    def back(desc=None, grads=(P,) * 6, nb=need):
+        return bwd(d() if desc is None else desc, *grads, P, nb, None)
+
+    assert fwd(None, None) == pmpe.ERR_INVALID_ARG and bwd(None, P, P, P, P, P, P, P, need, None) == pmpe.ERR_INVALID_ARG
+    for bad in (dict(topk_idx=None), dict(topk_w=None), dict(unmasked_control=True)):
+        assert fwd(d(**bad), None) == pmpe.ERR_INVALID_ARG, bad
+        assert back(d(**bad)) == pmpe.ERR_INVALID_ARG, bad
+    assert fwd(d(topk_idx=Fake(P + 4)), None) == pmpe.ERR_UNSUPPORTED_SHAPE
+    assert fwd(d(workspace=None), None) == pmpe.ERR_WORKSPACE
+    for i in range(6):  # dout, d_w, d_gate, d_up, d_down, d_hidden
+        for v in (None, P + 4):
+            assert back(grads=tuple(v if j == i else P for j in range(6))) == pmpe.ERR_INVALID_ARG, (i, v)
+    assert back(nb=need - 1) == pmpe.ERR_WORKSPACE
+    empty = LayerShape(0, 256, 128, 8, 4, 0, 2, True)
+    assert fwd(d(shape=empty, topk_idx=None, topk_w=None, workspace=None), None) == pmpe.OK
