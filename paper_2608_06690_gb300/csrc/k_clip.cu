@@ -6,7 +6,8 @@
 // partial sums (every CTA the same way) and scales.  Two launches rather than
 // a grid barrier: no CTA waits for another.  The tensors' pointers travel as
 // kernel arguments, so nothing is copied to the device before the call and a
-// captured graph keeps them.
+// captured graph keeps them.  (One cluster of 16 CTAs for the small cases, its
+// sums exchanged through shared memory, took 13 us where two launches take 5.)
 //
 // A chunk is 16 KB of one tensor.  Bytes bound both launches: every gradient
 // is read by each, and written once.  The second takes the chunks from last
@@ -18,8 +19,6 @@
 // squares leaves 2^-120 .. 2^90 (values that overflow or vanish when squared)
 // goes to a 64-bit sum instead, which exists in the CTAs that met one.
 #include <algorithm>
-#include <cmath>
-#include <cstdlib>
 #include <new>
 
 #include "elem.cuh"
@@ -34,33 +33,38 @@ constexpr int kClipCtasPerSm = 8;
 constexpr int kScaleCtasPerSm = 5;  // its registers allow no more
 constexpr int kClipMaxCtas = 152 * kClipCtasPerSm;
 constexpr int kScaleMaxCtas = 152 * kScaleCtasPerSm;
+// Chunks at the end of the first launch that are left in L2 for the second
+// (72 MB; what comes before them passes through): 604 MB of FP32 283 us, with
+// all of them or none 293; 2500 to 7000 chunks are within a microsecond.
+constexpr uint32_t kKept = 4500;
 
-// The tensors of a launch.  first[i]: chunks before tensor i.
+// The tensors of a launch: their whole 16-byte vectors, and the elements
+// before and after those (fewer than 16 bytes each).  first[i]: chunks before
+// tensor i.
 template <int kCap> struct ClipTable {
-    const void *g[kCap];
-    void *o[kCap];
-    long long n[kCap];
+    const uint4 *body[kCap];
+    uint8_t *out[kCap];  // where the clipped vectors go
+    long long vecs[kCap];
     uint32_t first[kCap + 1];
-    uint8_t type[kCap];
+    uint8_t type[kCap], head[kCap], tail[kCap];
     int count;
 };
 constexpr int kSmallTable = 64, kLargeTable = 1024;
 static_assert(sizeof(ClipTable<kLargeTable>) + 64 <= 32764, "kernel arguments");
 
-__host__ __device__ __forceinline__ int elem_bytes(int type) { return type == PMPE_F32 ? 4 : 2; }
+__host__ __device__ __forceinline__ int elem_shift(int type) { return type == PMPE_F32 ? 2 : 1; }
 // Elements before the first 16-byte boundary of a tensor.
-__host__ __device__ __forceinline__ long long head_of(const void *p, long long n, int bytes)
+inline long long head_of(const void *p, long long n, int type)
 {
-    const long long h = (long long)((16u - ((uintptr_t)p & 15u)) & 15u) / bytes;
-    return h < n ? h : n;
+    const long long h = (long long)((16u - ((uintptr_t)p & 15u)) & 15u) >> elem_shift(type);
+    return std::min(h, n);
 }
 // Chunks of a tensor: its whole vectors, and one at least for what is before and after them.
-__host__ __device__ __forceinline__ long long chunks_of(const void *p, long long n, int type)
+inline long long chunks_of(const pmpe_grad &g)
 {
-    const int b = elem_bytes(type);
-    const long long bytes = (n - head_of(p, n, b)) * b;
+    const long long bytes = (g.n - head_of(g.grad, g.n, g.type)) << elem_shift(g.type);
     const long long c = (bytes + kChunkBytes - 1) / kChunkBytes;
-    return n > 0 && c < 1 ? 1 : c;
+    return g.n > 0 && c < 1 ? 1 : c;
 }
 
 __device__ __forceinline__ void unpack_vec(const uint4 &u, int type, float (&v)[8])
@@ -165,47 +169,115 @@ template <int kCap> __device__ __forceinline__ int tensor_of(const ClipTable<kCa
     return lo;
 }
 
+// A chunk: its tensor's vectors, and with the tensor's first chunk the
+// elements before and after them.
+struct Chunk {
+    const uint4 *body;
+    uint8_t *out;
+    long long vecs, v0;
+    int type, head, tail;
+};
+template <int kCap> __device__ __forceinline__ Chunk chunk_at(const ClipTable<kCap> &tab, uint32_t c, int &i)
+{
+    if (c < tab.first[i] || c >= tab.first[i + 1]) i = tensor_of(tab, c);
+    Chunk k;
+    k.body = tab.body[i];
+    k.out = tab.out[i];
+    k.vecs = tab.vecs[i];
+    k.v0 = (long long)(c - tab.first[i]) * (kChunkBytes / 16);
+    k.type = tab.type[i];
+    k.head = k.v0 == 0 ? tab.head[i] : 0;
+    k.tail = k.v0 == 0 ? tab.tail[i] : 0;
+    return k;
+}
+
+// The chunk's vectors of thread t; zeros past the last one.  kLast: not needed
+// in L2 afterwards.
+template <bool kLast> __device__ __forceinline__ void load_chunk(uint4 (&u)[kClipVecs], const Chunk &k, int t)
+{
+#pragma unroll
+    for (int q = 0; q < kClipVecs; ++q) {
+        const long long at = k.v0 + q * kClipThreads + t;
+        u[q] = at >= k.vecs ? make_uint4(0u, 0u, 0u, 0u) : kLast ? __ldcs(k.body + at) : k.body[at];
+    }
+}
+
+__device__ __forceinline__ void square_chunk(const uint4 (&u)[kClipVecs], const Chunk &k, int t, Sum2 &sum, double &rare)
+{
+    float fast = 0.f, v[8];
+#pragma unroll
+    for (int q = 0; q < kClipVecs; ++q) {
+        unpack_vec(u[q], k.type, v);
+        add_squares(v, fast, rare);
+    }
+    if (t < max(k.head, k.tail)) {  // at most seven of each
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.f;
+        if (t < k.head) v[0] = load_one(k.body, t - k.head, k.type);
+        if (t < k.tail) v[1] = load_one(k.body + k.vecs, t, k.type);
+        add_squares(v, fast, rare);
+    }
+    add2(sum, fast);
+}
+
+__device__ __forceinline__ void scale_chunk(const uint4 (&u)[kClipVecs], const Chunk &k, int t, float f)
+{
+    const int per = 16 >> elem_shift(k.type);
+    const bool vec_out = ((uintptr_t)k.out & 15u) == 0;
+#pragma unroll
+    for (int q = 0; q < kClipVecs; ++q) {
+        const long long at = k.v0 + q * kClipThreads + t;
+        if (at >= k.vecs) continue;
+        float v[8];
+        unpack_vec(u[q], k.type, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= f;
+        if (vec_out) {
+            const uint4 r = k.type == PMPE_F32 ? make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]),
+                                                            __float_as_uint(v[2]), __float_as_uint(v[3]))
+                                               : k.type == PMPE_BF16 ? pack8(v, bf16()) : pack8(v, __half());
+            __stcs(reinterpret_cast<uint4 *>(k.out) + at, r);
+        } else {  // an output that is not aligned as its gradient is
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < per) store_one(k.out, at * per + j, k.type, v[j]);
+        }
+    }
+    if (t < k.head) store_one(k.out, t - k.head, k.type, f * load_one(k.body, t - k.head, k.type));
+    if (t < k.tail) store_one(k.out, k.vecs * per + t, k.type, f * load_one(k.body + k.vecs, t, k.type));
+}
+
+// n and f from the sums of all squares.  A norm that is not finite clips
+// nothing: the caller sees it and drops the step.
+__device__ __forceinline__ float factor_of(const Squares &all, float max_norm, float &norm)
+{
+    if (all.rare == 0.) {
+        norm = sqrtf(all.s.hi + all.s.lo);
+        return fminf(1.f, max_norm / (norm + 1e-6f));
+    }
+    const double n64 = sqrt((double)all.s.hi + all.s.lo + all.rare);
+    norm = (float)n64;
+    return isfinite(n64) ? (float)fmin(1., max_norm / (n64 + 1e-6)) : 1.f;
+}
+
 template <int kCap>
 __global__ void __launch_bounds__(kClipThreads, kClipCtasPerSm) clip_squares_kernel(const __grid_constant__ ClipTable<kCap> tab, Squares *partial)
 {
     pdl_trigger();
     pdl_wait();
-    const int tid = threadIdx.x;
     Sum2 sum = {0.f, 0.f};
     double rare = 0.;
     const uint32_t chunks = tab.first[tab.count];
     int i = 0;
     for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        if (c < tab.first[i] || c >= tab.first[i + 1]) i = tensor_of(tab, c);
-        const int type = tab.type[i], b = elem_bytes(type);
-        const void *g = tab.g[i];
-        const long long n = tab.n[i], head = head_of(g, n, b), vecs = (n - head) * b / 16;
-        const uint4 *body = reinterpret_cast<const uint4 *>((const uint8_t *)g + head * b);
-        const long long v0 = (long long)(c - tab.first[i]) * (kChunkBytes / 16);
+        const Chunk k = chunk_at(tab, c, i);
         uint4 u[kClipVecs];
-#pragma unroll
-        for (int q = 0; q < kClipVecs; ++q) {
-            const long long at = v0 + q * kClipThreads + tid;
-            u[q] = at < vecs ? __ldg(body + at) : make_uint4(0u, 0u, 0u, 0u);
-        }
-        float fast = 0.f, v[8];
-#pragma unroll
-        for (int q = 0; q < kClipVecs; ++q) {
-            unpack_vec(u[q], type, v);
-            add_squares(v, fast, rare);
-        }
-        if (v0 == 0) {  // what the vectors leave: fewer than 16 bytes before and after them
-            const long long tail = head + vecs * (16 / b);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = 0.f;
-            if (tid < head) v[0] = load_one(g, tid, type);
-            if (tid < n - tail) v[1] = load_one(g, tail + tid, type);
-            if (tid < 8) add_squares(v, fast, rare);
-        }
-        add2(sum, fast);
+        if (c + kKept < chunks) load_chunk<true>(u, k, threadIdx.x);
+        else load_chunk<false>(u, k, threadIdx.x);
+        square_chunk(u, k, threadIdx.x, sum, rare);
     }
     const Squares r = cta_sum(sum, rare);
-    if (tid == 0) partial[blockIdx.x] = r;
+    if (threadIdx.x == 0) partial[blockIdx.x] = r;
 }
 
 template <int kCap>
@@ -215,113 +287,76 @@ __global__ void __launch_bounds__(kClipThreads, kScaleCtasPerSm) clip_scale_kern
 {
     pdl_trigger();
     pdl_wait();
-    const int tid = threadIdx.x;
     Sum2 sum = {0.f, 0.f};
     double rare = 0.;
-    for (int i = tid; i < n_partial; i += kClipThreads) {
+    for (int i = threadIdx.x; i < n_partial; i += kClipThreads) {
         const Squares q = partial[i];
         add2(sum, q.s.hi);
         sum.lo += q.s.lo;
         rare += q.rare;
     }
-    const Squares all = cta_sum(sum, rare);
-    // a norm that is not finite clips nothing: the caller sees it and drops the step
-    float norm, f = 1.f;
-    if (all.rare == 0.) {
-        norm = sqrtf(all.s.hi + all.s.lo);
-        f = fminf(1.f, max_norm / (norm + 1e-6f));
-    } else {
-        const double n64 = sqrt((double)all.s.hi + all.s.lo + all.rare);
-        norm = (float)n64;
-        if (isfinite(n64)) f = (float)fmin(1., max_norm / (n64 + 1e-6));
-    }
-    if (blockIdx.x == 0 && tid == 0 && norm_out) *norm_out = norm;
+    float norm;
+    const float f = factor_of(cta_sum(sum, rare), max_norm, norm);
+    if (blockIdx.x == 0 && threadIdx.x == 0 && norm_out) *norm_out = norm;
     int i = tab.count - 1;
     const uint32_t chunks = tab.first[tab.count];
-    for (uint32_t k = blockIdx.x; k < chunks; k += gridDim.x) {
-        const uint32_t c = chunks - 1 - k;
-        if (c < tab.first[i] || c >= tab.first[i + 1]) i = tensor_of(tab, c);
-        const int type = tab.type[i], b = elem_bytes(type);
-        const void *g = tab.g[i];
-        void *o = tab.o[i];
-        if (f == 1.f && g == o) continue;
-        const long long n = tab.n[i], head = head_of(g, n, b), vecs = (n - head) * b / 16, per = 16 / b;
-        const uint4 *body = reinterpret_cast<const uint4 *>((const uint8_t *)g + head * b);
-        uint8_t *out = (uint8_t *)o + head * b;
-        const bool vec_out = ((uintptr_t)out & 15u) == 0;
-        const long long v0 = (long long)(c - tab.first[i]) * (kChunkBytes / 16);
+    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+        const Chunk k = chunk_at(tab, chunks - 1 - c, i);
+        if (f == 1.f && (const uint8_t *)k.body == k.out) continue;
         uint4 u[kClipVecs];
-#pragma unroll
-        for (int q = 0; q < kClipVecs; ++q) {
-            const long long at = v0 + q * kClipThreads + tid;
-            u[q] = at < vecs ? __ldcs(body + at) : make_uint4(0u, 0u, 0u, 0u);
-        }
-#pragma unroll
-        for (int q = 0; q < kClipVecs; ++q) {
-            const long long at = v0 + q * kClipThreads + tid;
-            if (at >= vecs) continue;
-            float v[8];
-            unpack_vec(u[q], type, v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= f;
-            if (vec_out) {
-                const uint4 r = type == PMPE_F32 ? make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]),
-                                                              __float_as_uint(v[2]), __float_as_uint(v[3]))
-                                                 : type == PMPE_BF16 ? pack8(v, bf16()) : pack8(v, __half());
-                __stcs(reinterpret_cast<uint4 *>(out) + at, r);
-            } else {  // an output that is not aligned as its gradient is
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < per) store_one(out, at * per + j, type, v[j]);
-            }
-        }
-        if (v0 == 0) {
-            const long long tail = head + vecs * per;
-            if (tid < head) store_one(o, tid, type, f * load_one(g, tid, type));
-            if (tid < n - tail) store_one(o, tail + tid, type, f * load_one(g, tail + tid, type));
-        }
+        load_chunk<true>(u, k, threadIdx.x);
+        scale_chunk(u, k, threadIdx.x, f);
     }
 }
 
-template <int kCap>
-cudaError_t clip_tables(const pmpe_grad *g, int n, float max_norm, float *norm_out, Squares *partial, cudaStream_t st, int phase,
-                        int n_partial_all)
+template <int kCap> void fill(ClipTable<kCap> &tab, const pmpe_grad *g, int n)
 {
-    int parts = 0;
-    for (int at = 0; at == 0 || at < n; at += kCap) {
-        ClipTable<kCap> tab;
-        tab.count = std::min(kCap, n - at);
-        uint32_t chunks = 0;
-        for (int i = 0; i < tab.count; ++i) {
-            const pmpe_grad &t = g[at + i];
-            tab.g[i] = t.grad;
-            tab.o[i] = t.out ? t.out : t.grad;
-            tab.n[i] = t.n;
-            tab.type[i] = (uint8_t)t.type;
-            tab.first[i] = chunks;
-            chunks += (uint32_t)chunks_of(t.grad, t.n, t.type);
+    tab.count = n;
+    uint32_t chunks = 0;
+    for (int i = 0; i < n; ++i) {
+        const int sh = elem_shift(g[i].type);
+        const long long head = head_of(g[i].grad, g[i].n, g[i].type), vecs = ((g[i].n - head) << sh) / 16;
+        tab.body[i] = (const uint4 *)((const uint8_t *)g[i].grad + (head << sh));
+        tab.out[i] = (uint8_t *)(g[i].out ? g[i].out : g[i].grad) + (head << sh);
+        tab.vecs[i] = vecs;
+        tab.head[i] = (uint8_t)head;
+        tab.tail[i] = (uint8_t)(g[i].n - head - (vecs * 16 >> sh));
+        tab.type[i] = (uint8_t)g[i].type;
+        tab.first[i] = chunks;
+        chunks += (uint32_t)chunks_of(g[i]);
+    }
+    tab.first[n] = chunks;
+}
+
+long long count_chunks(const pmpe_grad *g, int n)
+{
+    long long chunks = 0;
+    for (int i = 0; i < n; ++i) chunks += chunks_of(g[i]);
+    return chunks;
+}
+int ctas_for(long long chunks) { return (int)std::max<long long>(1, std::min<long long>(chunks, kClipMaxCtas)); }
+
+// Both launches for every kCap tensors; all of the first kind come before the second's.
+template <int kCap>
+cudaError_t clip_tables(const pmpe_grad *g, int n, float max_norm, float *norm_out, Squares *partial, cudaStream_t st)
+{
+    int all = 0;
+    for (int phase = 0; phase < 2; ++phase) {
+        int parts = 0;
+        for (int at = 0; at == 0 || at < n; at += kCap) {
+            ClipTable<kCap> tab;
+            fill(tab, g + at, std::min(kCap, n - at));
+            const int grid = ctas_for(tab.first[tab.count]);
+            const cudaError_t err =
+                phase == 0 ? launch_pdl(clip_squares_kernel<kCap>, dim3(grid), dim3(kClipThreads), 0, st, tab, partial + parts)
+                           : launch_pdl(clip_scale_kernel<kCap>, dim3(std::min(grid, kScaleMaxCtas)), dim3(kClipThreads), 0, st, tab,
+                                        (const Squares *)partial, all, max_norm, at == 0 ? norm_out : (float *)nullptr);
+            if (err != cudaSuccess) return err;
+            parts += grid;
         }
-        tab.first[tab.count] = chunks;
-        const int grid = (int)std::max<uint32_t>(1u, std::min<uint32_t>(chunks, (uint32_t)kClipMaxCtas));
-        const cudaError_t err =
-            phase == 0 ? launch_pdl(clip_squares_kernel<kCap>, dim3(grid), dim3(kClipThreads), 0, st, tab, partial + parts)
-                       : launch_pdl(clip_scale_kernel<kCap>, dim3(std::min(grid, kScaleMaxCtas)), dim3(kClipThreads), 0, st, tab,
-                                    (const Squares *)partial, n_partial_all, max_norm, at == 0 ? norm_out : (float *)nullptr);
-        if (err != cudaSuccess) return err;
-        parts += grid;
+        all = parts;
     }
     return cudaSuccess;
-}
-
-template <int kCap> int count_partials(const pmpe_grad *g, int n)
-{
-    int parts = 0;
-    for (int at = 0; at == 0 || at < n; at += kCap) {
-        long long chunks = 0;
-        for (int i = at; i < std::min(n, at + kCap); ++i) chunks += chunks_of(g[i].grad, g[i].n, g[i].type);
-        parts += (int)std::max<long long>(1, std::min<long long>(chunks, kClipMaxCtas));
-    }
-    return parts;
 }
 
 }  // namespace
@@ -340,16 +375,14 @@ int clip_tensors_ok(const pmpe_grad *g, int n)
     Span *s = new (std::nothrow) Span[2 * (size_t)n + 1];
     if (!s) return -1;
     size_t m = 0;
-    long long chunks = 0;
     for (int i = 0; i < n; ++i) {
         if (g[i].n == 0) continue;
-        const uintptr_t bytes = (uintptr_t)g[i].n * elem_bytes(g[i].type);
+        const uintptr_t bytes = (uintptr_t)g[i].n << elem_shift(g[i].type);
         s[m++] = {(uintptr_t)g[i].grad, (uintptr_t)g[i].grad + bytes};
         if (g[i].out && g[i].out != g[i].grad) s[m++] = {(uintptr_t)g[i].out, (uintptr_t)g[i].out + bytes};
-        chunks += chunks_of(g[i].grad, g[i].n, g[i].type);
     }
     std::sort(s, s + m, [](const Span &a, const Span &b) { return a.lo < b.lo; });
-    bool ok = chunks < (1LL << 31);
+    bool ok = count_chunks(g, n) < (1LL << 31);
     for (size_t i = 1; i < m; ++i) ok = ok && s[i - 1].hi <= s[i].lo;
     delete[] s;
     return ok ? 1 : 0;
@@ -358,15 +391,9 @@ int clip_tensors_ok(const pmpe_grad *g, int n)
 cudaError_t launch_clip(const pmpe_grad *g, int n, float max_norm, float *norm_out, void *workspace, cudaStream_t st)
 {
     Squares *partial = static_cast<Squares *>(workspace);
-    // the table is copied into every launch's arguments: 1.9 KB or 30 KB
-    const bool small = n <= kSmallTable;
-    const int parts = small ? count_partials<kSmallTable>(g, n) : count_partials<kLargeTable>(g, n);
-    for (int phase = 0; phase < 2; ++phase) {
-        const cudaError_t err = small ? clip_tables<kSmallTable>(g, n, max_norm, norm_out, partial, st, phase, parts)
-                                      : clip_tables<kLargeTable>(g, n, max_norm, norm_out, partial, st, phase, parts);
-        if (err != cudaSuccess) return err;
-    }
-    return cudaSuccess;
+    // the table travels with every launch: 1.9 KB or 30 KB
+    return n <= kSmallTable ? clip_tables<kSmallTable>(g, n, max_norm, norm_out, partial, st)
+                            : clip_tables<kLargeTable>(g, n, max_norm, norm_out, partial, st);
 }
 
 }  // namespace pmpe

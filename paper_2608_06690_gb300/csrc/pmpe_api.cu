@@ -379,7 +379,7 @@ static int make_routed_ctx(const pmpe_moe_desc *d, void *stream, Ctx *c)
     if (!d || d->unmasked_control != 0 || (d->T > 0 && (!d->topk_idx || !d->topk_w))) return PMPE_ERR_INVALID_ARG;
     const int rc = make_ctx(d, stream, c);
     if (rc != PMPE_OK) return rc;
-    pmpe_workspace_layout L;
+    pmpe_workspace_layout L = {};
     compute_layout(c->s, &L);
     c->idx = (int32_t *)((uint8_t *)d->workspace + L.topk_idx);
     c->w = (float *)((uint8_t *)d->workspace + L.topk_w);
