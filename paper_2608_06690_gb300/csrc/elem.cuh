@@ -52,7 +52,7 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8], __half)
 }
 
 // Eight elements of a row in a thread.  kVec: consecutive ones at p, which is
-// aligned for 16-byte accesses; n > 0: they exist (rows hold whole chunks).
+// aligned to their 16 or 32 bytes; n > 0: they exist (rows hold whole chunks).
 // Otherwise p, p + 32, ..., so that a warp's accesses are contiguous one
 // element at a time; n: elements from p to the row's end.  What does not exist
 // reads as zero.
@@ -63,10 +63,13 @@ template <bool kVec> __device__ __forceinline__ void load8(Raw8<float> &r, const
 {
     if (kVec) {
         r.u = r.hi = make_uint4(0u, 0u, 0u, 0u);
-        if (n > 0) {
-            r.u = reinterpret_cast<const uint4 *>(p)[0];
-            r.hi = reinterpret_cast<const uint4 *>(p)[1];
-        }
+        // one access of 32 bytes: two of 16, each touching every other half
+        // sector, took the norm's backward from 17.5 us to 26.9 with FP32 rows
+        // in the place of BF16 ones
+        if (n > 0)
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(r.u.x), "=r"(r.u.y), "=r"(r.u.z), "=r"(r.u.w), "=r"(r.hi.x), "=r"(r.hi.y), "=r"(r.hi.z), "=r"(r.hi.w)
+                         : "l"(p) : "memory");
     } else {
         uint32_t q[8];
 #pragma unroll
@@ -99,10 +102,10 @@ template <typename T> __device__ __forceinline__ void unpack(const Raw8<T> &r, f
 template <bool kVec> __device__ __forceinline__ void store8(float *p, const float (&v)[8], int n)
 {
     if (kVec) {
-        if (n > 0) {
-            reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        }
+        if (n > 0)
+            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                         "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                         : "memory");
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -162,25 +165,6 @@ template <bool kVec, typename T> __device__ __forceinline__ void store_raw(T *p,
         for (int i = 0; i < 8; ++i)
             if (32 * i < n) s[32 * i] = (uint16_t)(q[i >> 1] >> 16 * (i & 1));
     }
-}
-
-// Two FP32 operations an instruction, each rounded as by itself.
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    float2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;"
-        : "=l"(reinterpret_cast<unsigned long long &>(r))
-        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
-    return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(reinterpret_cast<unsigned long long &>(r))
-        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)),
-          "l"(reinterpret_cast<unsigned long long &>(c)));
-    return r;
 }
 
 template <typename V> __device__ __forceinline__ V warp_sum(V v)
