@@ -22,9 +22,10 @@
 // (about one token in a hundred with FP32 logits).  Logits compare exactly;
 // choices with a bias are FP32, a few 2^-24 off: where neighbours (or two
 // groups at the limit) lie within the bound of that error, about one token in
-// a thousand, the experts in question are evaluated in 64 bits, one a lane,
-// and compared as integers: an FP64 instruction takes a warp some 60 clocks
-// here, and a selection wholly in FP64 was 16 us.
+// a thousand, the token is put aside, and the CTA selects its experts at the
+// end by 64-bit choices, an expert a thread, compared as integers: 4.5 us a
+// token (softmax 8), where one warp alone took 11, as an FP64 instruction
+// occupies a scheduler for some 60 clocks.
 #include <algorithm>
 #include <type_traits>
 
@@ -45,6 +46,7 @@ struct ScoreParams {
     long long ld;
     int T, E_pub, E_priv, k, renorm, sigmoid, top2;
     int groups[2], top_groups[2];  // public, private
+    int tokens;                    // of a CTA at most
     float scale;
 };
 
@@ -88,68 +90,13 @@ template <typename T> struct Pool {
     int E, sigmoid, n, top, top2, k;
 };
 
-// Where the exact values are needed, and what FP32 already knows.
-struct Exact {
-    float mx;  // the largest logit (softmax)
-    double sum;
-};
-
 template <typename T> __device__ __forceinline__ float logit(const Pool<T> &p, int e) { return fminf(to_f32(p.row[e]), kLargest); }
-// score + bias in 64 bits.
-template <typename T> __device__ __forceinline__ double exact_value(const Pool<T> &p, const Exact &x, int e)
-{
-    const double z = logit(p, e);
-    const double s = p.sigmoid ? 1. / (1. + exp(-z)) : exp(z - x.mx) / x.sum;
-    return p.bias ? s + p.bias[e] : s;
-}
-// The softmax's sum in 64 bits (sigmoid: nothing).
-template <typename T> __device__ __noinline__ double exact_sum(const Pool<T> &p, float mx, int lane)
-{
-    double s = 0.;
-    for (int e = lane; e < p.E; e += 32) {
-        const float z = to_f32(p.row[e]);
-        if (z > kNone) s += exp((double)fminf(z, kLargest) - mx);
-    }
-    return warp_sum(s);
-}
 
 // The two largest values seen, best first; kNone where there are fewer.
 __device__ __forceinline__ void add_two(float &first, float &second, float v)
 {
     second = fmaxf(second, fminf(first, v));
     first = fmaxf(first, v);
-}
-
-// Moves the experts whose bit in `wanted` is set (lane l, bit i: expert l kV +
-// i) to a lane each; returns how many there are (above 32: too many).  list:
-// 32 words of the warp's own.
-template <int kV> __device__ __forceinline__ int gather(uint32_t wanted, int lane, int *list, int &e)
-{
-    int count = 0;
-#pragma unroll
-    for (int i = 0; i < kV; ++i) {
-        const uint32_t who = __ballot_sync(~0u, (wanted >> i) & 1u);
-        const int at = count + __popc(who & ((1u << lane) - 1u));
-        if (((wanted >> i) & 1u) && at < 32) list[at] = lane * kV + i;
-        count += __popc(who);
-    }
-    __syncwarp();
-    e = lane < count ? list[lane] : -1;
-    __syncwarp();
-    return count;
-}
-
-// A lane's place among the lanes with a key (0: none): larger keys first,
-// equal ones by the lower id.
-__device__ __forceinline__ int place_of(u64 key, int id, int count)
-{
-    int place = 0;
-    for (int j = 0; j < count; ++j) {
-        const u64 o = __shfl_sync(~0u, key, j);
-        const int oi = __shfl_sync(~0u, id, j);
-        place += o > key || (o == key && oi < id) ? 1 : 0;
-    }
-    return place;
 }
 
 // A lane's largest packed choices in order: all of them up to four, the first
@@ -258,87 +205,100 @@ __device__ __forceinline__ auto group_value(const K (&key)[kV], int n, int size,
     return mine;
 }
 
-// Selection by the exact values of every expert, where more than 32 of them
-// (or groups that are not whole lanes) are in doubt.
-template <typename T, int kV> __device__ __noinline__ int pick_exact(const Pool<T> &p, float mx, int lane)
+// Lane j's weight of its pick: z its logit, s its score where `scored`.  mine:
+// there is a pick.
+__device__ __forceinline__ float weight_of(bool mine, float z, float s, int sigmoid, int renorm)
 {
-    const int size = p.E / p.n;
-    const bool limited = p.top < p.n, scored = p.bias || (limited && p.top2);
-    const Exact x = {mx, scored && !p.sigmoid ? exact_sum(p, mx, lane) : 1.};
-    u64 choice[kV], counts[kV];
-#pragma unroll
-    for (int i = 0; i < kV; ++i) {
-        const int e = lane * kV + i;
-        choice[i] = counts[i] = 0;
-        if (e < p.E && to_f32(p.row[e]) > kNone) {
-            const u64 z = key64((double)(logit(p, e) + 0.f));
-            const double v = scored ? exact_value(p, x, e) : 0.;
-            choice[i] = !p.bias ? z : v > (double)kNone ? key64(v) : 0;
-            counts[i] = p.top2 && choice[i] ? key64(v) : choice[i];
-        }
+    float w = mine ? s : 0.f;
+    if (renorm && sigmoid) {
+        w = w / (warp_sum(w) + 1e-20f);
+    } else if (renorm) {  // softmax over the k
+        const float m = of(__reduce_max_sync(~0u, key_of(mine ? z : kNone)));
+        w = mine ? expf(z - m) : 0.f;
+        const float total = warp_sum(w);
+        if (mine) w = w / total;
     }
-    if (limited) {
-        const u64 v = key64(group_value<u64, kV>(counts, p.n, size, p.top2, lane));
-        int place = 0;
-        for (int q = 0; q < p.n; ++q) {
-            const u64 o = __shfl_sync(~0u, v, q);
-            place += o > v || (o == v && q < lane) ? 1 : 0;
-        }
-        const uint32_t kept = __ballot_sync(~0u, lane < p.n && place < p.top);
+    return w;
+}
+
+template <typename T> __device__ __forceinline__ Pool<T> pool_of(const ScoreParams &p, long long t, int priv)
+{
+    const int base = priv ? p.E_pub : 0;
+    return {(const T *)p.logits + t * p.ld + base, p.bias ? p.bias + base : nullptr, priv ? p.E_priv : p.E_pub, p.sigmoid,
+            p.groups[priv], p.top_groups[priv], p.top2, p.k};
+}
+
+// Selection by 64-bit choices of a token that FP32 does not settle, by the
+// whole CTA: a thread evaluates an expert, warp 0 selects.  s_key: choices, then
+// what groups count by (0: no candidate).
+template <typename T, int kV>
+__device__ __noinline__ void select_exactly(const ScoreParams &p, int t, u64 (&s_key)[2][kMaxPool], int *s_load)
+{
+    __shared__ double s_sum[kRouteWarps];
+    __shared__ uint32_t s_max[kRouteWarps];
+    const int e = threadIdx.x, lane = e & 31, warp = e >> 5;
+    const int priv = p.policy != nullptr && p.policy[t] == 0x01 ? 1 : 0, base = priv ? p.E_pub : 0;
+    const Pool<T> pool = pool_of<T>(p, t, priv);
+    const float raw = e < pool.E ? to_f32(pool.row[e]) : kNone, z = raw > kNone ? fminf(raw, kLargest) + 0.f : kNone;
+    float mx = kNone;
+    double sum = 1., v = 0.;
+    if (p.sigmoid) {
+        if (z > kNone) v = 1. / (1. + exp(-(double)z));
+    } else {
+        const uint32_t top = __reduce_max_sync(~0u, key_of(z));
+        if (lane == 0) s_max[warp] = top;
+        __syncthreads();
+        uint32_t all = 0;
+        for (int q = 0; q < kRouteWarps; ++q) all = max(all, s_max[q]);
+        mx = of(all);
+        if (z > kNone) v = exp((double)z - mx);
+        const double part = warp_sum(v);
+        if (lane == 0) s_sum[warp] = part;
+        __syncthreads();
+        sum = 0.;
+        for (int q = 0; q < kRouteWarps; ++q) sum += s_sum[q];
+        if (z > kNone) v /= sum;
+    }
+    if (pool.bias && z > kNone) v += pool.bias[e];
+    const bool on = z > kNone && v > (double)kNone;  // a bias of -inf (or NaN) takes its expert out
+    s_key[0][e] = !on ? 0 : pool.bias ? key64(v) : key64((double)z);
+    s_key[1][e] = !on ? 0 : p.top2 ? key64(v) : s_key[0][e];
+    __syncthreads();
+    if (warp == 0) {
+        u64 key[kV], by[kV];
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
-            const int e = lane * kV + i;
-            if (e < p.E && !((kept >> (e / size)) & 1u)) choice[i] = 0;
+            key[i] = s_key[0][lane * kV + i];
+            by[i] = s_key[1][lane * kV + i];
+        }
+        if (pool.top < pool.n) {
+            const int size = pool.E / pool.n;
+            const u64 g = key64(group_value<u64, kV>(by, pool.n, size, p.top2, lane));
+            int place = 0;
+            for (int q = 0; q < pool.n; ++q) {
+                const u64 o = __shfl_sync(~0u, g, q);
+                place += o > g || (o == g && q < lane) ? 1 : 0;
+            }
+            const uint32_t kept = __ballot_sync(~0u, lane < pool.n && place < pool.top);
+#pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                const int q = lane * kV + i;
+                if (q < pool.E && !((kept >> (q / size)) & 1u)) key[i] = 0;
+            }
+        }
+        int pick, next;
+        pick_whole<u64, kV>(key, p.k, lane, pick, next);
+        const bool mine = lane < p.k && pick >= 0;
+        const float zj = mine ? logit(pool, pick) : kNone, sum32 = (float)sum;
+        const float sj = !mine ? 0.f : p.sigmoid ? 1.f / (1.f + expf(-zj)) : expf(zj - mx) / sum32;
+        const float w = weight_of(mine, zj, sj, p.sigmoid, p.renorm);
+        if (lane < p.k) {
+            p.idx[(long long)t * p.k + lane] = mine ? base + pick : -1;
+            p.w[(long long)t * p.k + lane] = w * p.scale;
+            if (p.load && mine) atomicAdd(s_load + base + pick, 1);
         }
     }
-    int e_mine, e_next;
-    pick_whole<u64, kV>(choice, p.k, lane, e_mine, e_next);
-    return e_mine;
-}
-
-// Which `need` of the groups in `doubt` are kept (a bit each), from the exact
-// values of the experts in `wanted`: those that may be a group's two best.
-// 0: too many experts.
-template <typename T, int kV>
-__device__ __noinline__ uint32_t settle_groups(const Pool<T> &p, float mx, uint32_t wanted, uint32_t doubt, int need, int lane,
-                                               int *list)
-{
-    int e;
-    if (gather<kV>(wanted, lane, list, e) > 32) return 0;
-    const Exact x = {mx, p.sigmoid ? 1. : exact_sum(p, mx, lane)};
-    const u64 key = e >= 0 ? key64(exact_value(p, x, e)) : 0;
-    const int mine = e >= 0 ? e / (p.E / p.n) : -1;
-    u64 value = 0;
-    int group = -1, count = 0;
-    for (uint32_t m = doubt; m; m &= m - 1, ++count) {
-        const int g = __ffs(m) - 1;
-        const u64 first = warp_max64(mine == g ? key : 0);
-        const int who = __ffs(__ballot_sync(~0u, mine == g && key == first)) - 1;
-        const u64 second = p.top2 ? warp_max64(mine == g && lane != who ? key : 0) : 0;
-        if (lane == count) {
-            value = key64(second ? of(first) + of(second) : of(first));
-            group = g;
-        }
-    }
-    const int place = place_of(value, group, count);
-    return __reduce_or_sync(~0u, group >= 0 && place < need ? 1u << group : 0u);
-}
-
-// The order of the k best by the exact values of the experts in `wanted`, among
-// which they are: lane j < k gets the j-th (-1: none).  -2: too many experts.
-template <typename T, int kV>
-__device__ __noinline__ int settle_order(const Pool<T> &p, float mx, uint32_t wanted, int lane, int *list)
-{
-    int e;
-    const int count = gather<kV>(wanted, lane, list, e);
-    if (count > 32) return -2;
-    const Exact x = {mx, p.sigmoid ? 1. : exact_sum(p, mx, lane)};
-    const int place = place_of(e >= 0 ? key64(exact_value(p, x, e)) : 0, e, count);
-    if (e >= 0) list[place] = e;
-    __syncwarp();
-    e = lane < min(p.k, count) ? list[lane] : -1;
-    __syncwarp();
-    return e;
+    __syncthreads();  // the keys are read
 }
 
 // A lane's logits; -inf for what does not exist.
@@ -357,18 +317,22 @@ template <typename T, int kV> __device__ __forceinline__ void load_logits(float 
 }
 
 // kBias: choices are scores + biases.  kGroups: a pool's groups may be limited.
+// smem: a CTA's tokens (those put aside) where either holds, the loads' counts.
 template <typename T, int kV, bool kBias, bool kGroups>
 __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const ScoreParams p)
 {
-    extern __shared__ int s_load[];
-    __shared__ int s_list[kRouteWarps][32];
+    constexpr bool kAside = kBias || kGroups;
+    extern __shared__ int s_tokens[];
+    __shared__ u64 s_key[kAside ? 2 : 1][kAside ? kMaxPool : 1];
+    __shared__ int s_aside;
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E_all = p.E_pub + p.E_priv;
-    if (p.load) {
+    int *s_load = s_tokens + (kAside ? p.tokens : 0);
+    if (p.load)
         for (int e = threadIdx.x; e < E_all; e += blockDim.x) s_load[e] = 0;
-        __syncthreads();
-    }
+    if (threadIdx.x == 0) s_aside = 0;
+    if (kAside || p.load) __syncthreads();
     // a token's pool and logits are requested while the token before it is in work
     const int step = gridDim.x * kRouteWarps;
     auto pool_at = [&](int t) { return t < p.T && p.policy != nullptr && p.policy[t] == 0x01 ? 1 : 0; };
@@ -383,10 +347,9 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
     float bias[kV];
     fetch(t, priv_next);
     for (; t < p.T; t += step) {
-        const int priv = priv_next;
-        const int base = priv ? p.E_pub : 0, E = priv ? p.E_priv : p.E_pub;
-        const Pool<T> pool = {(const T *)p.logits + t * p.ld + base, kBias ? p.bias + base : nullptr, E, p.sigmoid, p.groups[priv],
-                              p.top_groups[priv], p.top2, p.k};
+        const int priv = priv_next, base = priv ? p.E_pub : 0;
+        const Pool<T> pool = pool_of<T>(p, t, priv);
+        const int E = pool.E;
         const bool limited = kGroups && pool.top < pool.n, scored = kBias || (limited && p.top2);
         if (kBias && priv != priv_bias) {  // a lane's experts, and so its biases, change with the pool alone
 #pragma unroll
@@ -399,26 +362,29 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
         fetch(t + step, priv_after);
         priv_next = priv_after;
         priv_after = pool_at(t + 2 * step);
-        float mx = kNone, sum = 1.f;
+        // The choices come from the fast exponential and quotient, whose error
+        // is known: __expf(x) 2 + 1.2 |x| ulp, __fdividef 2 ulp, ulp <= 2^-23.
+        // So a choice c is off by less than err + 2^-24 |c|, a fifth to spare:
+        // sigmoid: the exponential's error enters with s (1 - s), and s (1 - s)
+        // |z| < 0.23: 0.8, the sum 0.5, the quotient 2, 3.3 x 2^-23 in all;
+        // softmax, with d = z - max, |d| p < 0.4 / sum: the exponential (4 + 2.4
+        // |d|) 2^-24, d's rounding 2^-24 |d|, both again in the sum (|d| weighted
+        // by p is at most ln 256), 12 additions: 43 x 2^-24 / sum.
+        float mx = kNone, sum = 1.f, err = 0x1p-21f;
+        float val[kV];  // score + bias, where it is needed
         if (!p.sigmoid && (!p.renorm || scored)) {  // the pool's softmax
 #pragma unroll
             for (int i = 0; i < kV; ++i) mx = fmaxf(mx, z[i]);
             mx = of(__reduce_max_sync(~0u, key_of(mx)));
             sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < kV; ++i) sum += z[i] > kNone ? expf(z[i] - mx) : 0.f;
+            for (int i = 0; i < kV; ++i) {
+                val[i] = z[i] > kNone ? (kAside ? __expf(z[i] - mx) : expf(z[i] - mx)) : 0.f;
+                sum += val[i];
+            }
             sum = warp_sum(sum);
+            err = 0x1.9p-19f / sum;
         }
-        auto score = [&](float zz) { return p.sigmoid ? 1.f / (1.f + expf(-zz)) : expf(zz - mx) / sum; };
-        // The choices come from the fast exponential and quotient, whose error
-        // is known: __expf(x) 2 + 1.2 |x| ulp, __fdividef 2 ulp, ulp <= 2^-23.
-        // So a choice c is off by less than err + 2^-24 |c|, a fifth to spare:
-        // sigmoid: the exponential's error enters with s (1 - s), and s (1 - s)
-        // |z| < 0.23: 0.8, the sum 0.5, the quotient 2, 3.3 x 2^-23 in all;
-        // softmax, with d = z - max: d rounds by 2^-24 |d| and |d| p < 0.4 / sum;
-        // the sum (expf 2 ulp, d, 12 additions) is 22 x 2^-24 off; 30 x 2^-24 / sum.
-        const float err = p.sigmoid ? 0x1p-21f : 0x1.2p-19f / sum;
-        float val[kV];  // score + bias, where it is needed
         if (scored) {
             if (p.sigmoid) {
 #pragma unroll
@@ -426,7 +392,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
             } else {
                 const float inv_sum = 1.f / sum;
 #pragma unroll
-                for (int i = 0; i < kV; ++i) val[i] = __expf(z[i] - mx) * inv_sum;
+                for (int i = 0; i < kV; ++i) val[i] *= inv_sum;
             }
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
@@ -438,22 +404,17 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
         float choice[kV];  // -inf: no candidate
 #pragma unroll
         for (int i = 0; i < kV; ++i) choice[i] = kBias ? val[i] : z[i];
-        bool exact = false;  // the whole selection again by exact values
+        bool doubt = false;
         if (kGroups && limited) {
             const int n = pool.n, top = pool.top, size = E / n, seg = lanes_of_group<kV>(size);
             float by[kV];  // what groups count by
-            float close = 0.f;
 #pragma unroll
             for (int i = 0; i < kV; ++i) by[i] = p.top2 ? val[i] : choice[i];
-            if (scored) {  // two sums of two values each, and their own rounding
-                float top_value = 0.f;
-#pragma unroll
-                for (int i = 0; i < kV; ++i) top_value = fmaxf(top_value, val[i] > kNone ? fabsf(val[i]) : 0.f);
-                close = 4.f * err + 0x1p-20f * of(__reduce_max_sync(~0u, key_of(top_value)));
-            }
-            if (seg) {
-                // every group at once: its lanes hold its two best after log2(seg) exchanges
-                float a = kNone, b = kNone;
+            float a;       // a group's value: its lanes', or lane g's of group g
+            int g, place = 0;
+            if (seg) {     // every group at once: its lanes hold its two best after log2(seg) exchanges
+                float b = kNone;
+                a = kNone;
 #pragma unroll
                 for (int i = 0; i < kV; ++i) add_two(a, b, by[i]);
                 for (int off = 1; off < seg; off <<= 1) {
@@ -461,63 +422,46 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
                     add_two(a, b, oa);
                     add_two(a, b, ob);
                 }
-                const float least = p.top2 && b > kNone ? b : a;
                 if (p.top2 && b > kNone) a += b;
-                const int g = lane / seg;
-                int place = 0;
+                g = lane / seg;
                 for (int q = 0; q < n; ++q) {
                     const float o = __shfl_sync(~0u, a, q * seg);
                     place += o > a || (o == a && q < g) ? 1 : 0;
                 }
-                bool kept = place < top;
-                if (scored) {
-                    const float x = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top - 1)) - 1);
-                    const float y = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top)) - 1);
-                    if (y > kNone && x - y <= close) {
-                        const bool in = a > x + close, doubt = g < n && !in && a >= y - close;
-                        uint32_t wanted = 0;
 #pragma unroll
-                        for (int i = 0; i < kV; ++i)
-                            if (doubt && by[i] > kNone && by[i] >= least - close) wanted |= 1u << i;
-                        const bool first_lane = lane % seg == 0;
-                        const uint32_t which = __reduce_or_sync(~0u, doubt && first_lane ? 1u << g : 0u);
-                        const int need = top - __popc(__ballot_sync(~0u, g < n && in && first_lane));
-                        const uint32_t keep = settle_groups<T, kV>(pool, mx, wanted, which, need, lane, s_list[warp]);
-                        exact = keep == 0;
-                        kept = in || (g < n && ((keep >> g) & 1u));
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < kV; ++i) choice[i] = kept ? choice[i] : kNone;
+                for (int i = 0; i < kV; ++i) choice[i] = place < top ? choice[i] : kNone;
             } else {
                 uint32_t key[kV];
 #pragma unroll
                 for (int i = 0; i < kV; ++i) key[i] = by[i] > kNone ? key_of(by[i]) : 0u;
-                const float a = group_value<uint32_t, kV>(key, n, size, p.top2, lane);
-                int place = 0;
+                a = group_value<uint32_t, kV>(key, n, size, p.top2, lane);
+                g = lane;
                 for (int q = 0; q < n; ++q) {
                     const float o = __shfl_sync(~0u, a, q);
                     place += o > a || (o == a && q < lane) ? 1 : 0;
                 }
-                const uint32_t kept = __ballot_sync(~0u, lane < n && place < top);
-                if (scored) {
-                    const float x = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, lane < n && place == top - 1)) - 1);
-                    const float y = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, lane < n && place == top)) - 1);
-                    exact = y > kNone && x - y <= close;
-                }
+                const uint32_t kept = __ballot_sync(~0u, g < n && place < top);
 #pragma unroll
                 for (int i = 0; i < kV; ++i) {
                     const int e = lane * kV + i;
                     if (e < E && !((kept >> (e / size)) & 1u)) choice[i] = kNone;
                 }
             }
+            if (scored) {  // the last group kept and the first one dropped: sums of two values each, and their own rounding
+                float top_value = 0.f;
+#pragma unroll
+                for (int i = 0; i < kV; ++i) top_value = fmaxf(top_value, val[i] > kNone ? fabsf(val[i]) : 0.f);
+                top_value = of(__reduce_max_sync(~0u, key_of(top_value)));
+                const float x = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top - 1)) - 1);
+                const float y = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top)) - 1);
+                doubt = y > kNone && x - y <= 4.f * err + 0x1p-20f * top_value;
+            }
         }
         // Neighbours in the order, the last one's being the first not chosen
         // (which lane k holds, and e_next), are in doubt where their packed
         // choices are equal (again from the whole ones) or their FP32 choices
-        // closer than those are exact (by exact values), unless their logits
-        // and biases are the same: a true tie.  16-bit logits without a bias
-        // are packed whole.
+        // closer than those are exact, unless their logits and biases are the
+        // same: a true tie.  16-bit logits without a bias are packed whole.
         constexpr bool inexact = kBias || sizeof(T) == 4;
         int e_mine, e_next;
         bool whole;
@@ -540,13 +484,13 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
             for (int i = 0; i < kV; ++i) key[i] = choice[i] > kNone ? key_of(choice[i]) : 0u;
             pick_whole<uint32_t, kV>(key, p.k, lane, e_mine, e_next);
         }
-        const bool need_score = p.sigmoid || !p.renorm;
+        auto score = [&](float zz) { return p.sigmoid ? 1.f / (1.f + expf(-zz)) : expf(zz - mx) / sum; };
         float zj = kNone, sj = 0.f;
         if (e_mine >= 0) {
             zj = logit(pool, e_mine);
-            if (need_score || kBias) sj = score(zj);
+            if (p.sigmoid || !p.renorm || kBias) sj = score(zj);
         }
-        if (kBias && !exact) {
+        if (kBias) {
             const float b0 = e_mine >= 0 ? pool.bias[e_mine] : 0.f, c0 = e_mine >= 0 ? sj + b0 : kNone;
             float z1 = __shfl_down_sync(~0u, zj, 1), b1 = __shfl_down_sync(~0u, b0, 1), c1 = __shfl_down_sync(~0u, c0, 1);
             if (p.k == 32 && lane == 31) {  // no lane holds the 33rd
@@ -554,44 +498,25 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
                 b1 = e_next >= 0 ? pool.bias[e_next] : 0.f;
                 c1 = e_next >= 0 ? score(z1) + b1 : kNone;
             }
-            const bool doubt = lane < p.k && c1 > kNone && c0 - c1 <= 2.f * err + 0x1.4p-24f * (fabsf(c0) + fabsf(c1)) &&
-                               !(b0 == b1 && zj == z1);
-            if (__any_sync(~0u, doubt)) {
-                const float c = __shfl_sync(~0u, c0, p.k - 1), least = c - 2.02f * (err + 0x1.4p-24f * fabsf(c));
-                uint32_t wanted = 0;
-#pragma unroll
-                for (int i = 0; i < kV; ++i)
-                    if (choice[i] > kNone && choice[i] >= least) wanted |= 1u << i;
-                const int e = settle_order<T, kV>(pool, mx, wanted, lane, s_list[warp]);
-                exact = e == -2;
-                if (e_mine != e && e >= 0) {
-                    zj = logit(pool, e);
-                    sj = score(zj);
-                }
-                e_mine = e;
-            }
+            doubt = doubt || (lane < p.k && c1 > kNone && c0 - c1 <= 2.f * err + 0x1.4p-24f * (fabsf(c0) + fabsf(c1)) &&
+                              !(b0 == b1 && zj == z1));
         }
-        if (exact) {
-            e_mine = pick_exact<T, kV>(pool, mx, lane);
-            zj = e_mine >= 0 ? logit(pool, e_mine) : kNone;
-            sj = e_mine >= 0 && need_score ? score(zj) : 0.f;
+        if (kAside && __any_sync(~0u, doubt)) {
+            if (lane == 0) s_tokens[atomicAdd(&s_aside, 1)] = t;
+            continue;
         }
-        // lane j's weight
         const bool mine = lane < p.k && e_mine >= 0;
-        float w = mine ? sj : 0.f;
-        if (p.renorm && p.sigmoid) {
-            w = w / (warp_sum(w) + 1e-20f);
-        } else if (p.renorm) {  // softmax over the k
-            const float m = of(__reduce_max_sync(~0u, key_of(mine ? zj : kNone)));
-            w = mine ? expf(zj - m) : 0.f;
-            const float total = warp_sum(w);
-            if (mine) w = w / total;
-        }
+        const float w = weight_of(mine, zj, sj, p.sigmoid, p.renorm);
         if (lane < p.k) {
             p.idx[(long long)t * p.k + lane] = mine ? base + e_mine : -1;
             p.w[(long long)t * p.k + lane] = w * p.scale;
             if (p.load && mine) atomicAdd(s_load + base + e_mine, 1);
         }
+    }
+    if constexpr (kAside) {
+        __syncthreads();
+        const int aside = s_aside;  // in any order: each token's result is its own
+        for (int i = 0; i < aside; ++i) select_exactly<T, kV>(p, s_tokens[i], s_key, s_load);
     }
     if (p.load) {  // whole numbers: the order of the additions does not matter
         __syncthreads();
@@ -726,10 +651,14 @@ template <typename Go> cudaError_t dispatch(int type, int pool, Go go)
     return by_size(__half());
 }
 
-// CTAs: up to eight an SM (prompts: T = 16384, 128 + 32 experts 8.3 us, with
-// four 12.4), four where a bias or groups take more registers (T = 8192, 256
-// experts in 8 groups 21.8 us, with eight 24.2).
-int grid_of(int T, int num_sms, int per_sm) { return std::max(1, std::min((T + kRouteWarps - 1) / kRouteWarps, per_sm * num_sms)); }
+// CTAs for T tokens: up to eight an SM (prompts: T = 16384, 128 + 32 experts
+// 8.3 us, with four 12.4), and not more than kMostTokens tokens each.
+constexpr int kMostTokens = 4096;
+int grid_of(int T, int num_sms)
+{
+    const int all = (T + kRouteWarps - 1) / kRouteWarps;
+    return std::max(1, std::min(all, std::max(8 * num_sms, (T + kMostTokens - 1) / kMostTokens)));
+}
 
 }  // namespace
 
@@ -744,8 +673,9 @@ cudaError_t launch_route_scores(const pmpe_route_desc &d, int num_sms, cudaStrea
     p.top_groups[0] = d.top_groups_pub; p.top_groups[1] = d.top_groups_priv;
     p.scale = d.scale;
     const bool limited = d.top_groups_pub < d.groups_pub || (d.E_priv > 0 && d.top_groups_priv < d.groups_priv);
-    const dim3 grid(grid_of(d.T, num_sms, limited || d.bias ? 4 : 8)), block(32 * kRouteWarps);
-    const size_t smem = d.load ? (d.E_pub + d.E_priv) * sizeof(int) : 0;
+    const dim3 grid(grid_of(d.T, num_sms)), block(32 * kRouteWarps);
+    p.tokens = (d.T + (int)grid.x * kRouteWarps - 1) / ((int)grid.x * kRouteWarps) * kRouteWarps;
+    const size_t smem = ((limited || d.bias ? p.tokens : 0) + (d.load ? d.E_pub + d.E_priv : 0)) * sizeof(int);
     return dispatch(d.logits_type, std::max(d.E_pub, d.E_priv), [&](auto t, auto v) {
         using T = decltype(t);
         constexpr int kV = decltype(v)::value;
@@ -766,7 +696,7 @@ cudaError_t launch_route_scores_backward(const pmpe_route_desc &d, const float *
     p.T = d.T; p.E_pub = d.E_pub; p.E_priv = d.E_priv; p.k = d.k; p.renorm = d.renormalize;
     p.sigmoid = d.score == PMPE_SCORE_SIGMOID;
     p.scale = d.scale;
-    const dim3 grid(grid_of(d.T, num_sms, 8)), block(32 * kRouteWarps);
+    const dim3 grid(grid_of(d.T, num_sms)), block(32 * kRouteWarps);
     return dispatch(d.logits_type, std::max(d.E_pub, d.E_priv), [&](auto t, auto v) {
         return launch_pdl(route_scores_bwd_kernel<decltype(t), decltype(v)::value>, grid, block, 0, st, p);
     });
