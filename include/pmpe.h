@@ -373,8 +373,9 @@ PMPE_API int pmpe_moe_forward_noalloc(const pmpe_moe_desc *d, void *stream);
  *
  * The norm of the residual stream before the layer, routing from given logits
  * where a model's router is not the layer's own, and the clipping of the
- * gradients that the backward gives.  Pointers need the alignment of their
- * elements only (16-byte aligned rows are read with wide loads). */
+ * gradients that the backward gives.  At most 2^30 rows.  Pointers need the
+ * alignment of their elements only; rows of a multiple of eight elements that
+ * are aligned to eight elements are read with wide loads. */
 
 /* Element types. */
 #define PMPE_F32 0

@@ -7,6 +7,8 @@
 namespace pmpe {
 namespace {
 
+constexpr int kMaxRows = 1 << 30;  // rows and grid strides past them stay within 32 bits
+
 bool is_type(int t) { return t == PMPE_F32 || t == PMPE_BF16 || t == PMPE_F16; }
 bool fits(const void *p, int type) { return ((uintptr_t)p & (type == PMPE_F32 ? 3u : 1u)) == 0; }
 bool fits4(const void *p) { return ((uintptr_t)p & 3u) == 0; }
@@ -32,7 +34,7 @@ int check_route(const pmpe_route_desc *d)
         (d->renormalize != 0 && d->renormalize != 1) || !std::isfinite(d->scale) || (d->E_priv == 0 && d->policy) ||
         d->ld < (int64_t)d->E_pub + d->E_priv)
         return PMPE_ERR_INVALID_ARG;
-    if (d->k > kMaxTopK || d->E_pub > kMaxPool || d->E_priv > kMaxPool) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    if (d->k > kMaxTopK || d->E_pub > kMaxPool || d->E_priv > kMaxPool || d->T > kMaxRows) return PMPE_ERR_UNSUPPORTED_SHAPE;
     if (d->T > 0 && (!d->logits || !d->topk_idx)) return PMPE_ERR_INVALID_ARG;
     if (!fits(d->logits, d->logits_type) || !fits4(d->topk_idx)) return PMPE_ERR_UNSUPPORTED_SHAPE;
     return PMPE_OK;
@@ -50,7 +52,7 @@ int pmpe_rms_norm(const pmpe_rms_norm_desc *d, void *stream)
     if (!d || d->T < 0 || d->H < 1 || !is_type(d->type) || (d->weight_type != d->type && d->weight_type != PMPE_F32) ||
         d->quant < PMPE_QUANT_NONE || d->quant > PMPE_QUANT_ROW || !(d->eps >= 1e-20f) || !std::isfinite(d->eps))
         return PMPE_ERR_INVALID_ARG;
-    if (d->H > PMPE_MAX_NORM_WIDTH) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    if (d->H > PMPE_MAX_NORM_WIDTH || d->T > kMaxRows) return PMPE_ERR_UNSUPPORTED_SHAPE;
     if (d->x_ld < d->H || (d->residual && d->residual_ld < d->H))
         return PMPE_ERR_INVALID_ARG;
     if (d->T == 0) return PMPE_OK;
@@ -63,7 +65,7 @@ int pmpe_rms_norm(const pmpe_rms_norm_desc *d, void *stream)
 
 size_t pmpe_rms_norm_backward_workspace_size(int T, int H)
 {
-    return T < 0 || H < 1 || H > PMPE_MAX_NORM_WIDTH ? 0 : rms_norm_backward_workspace_bytes(T, H);
+    return T < 0 || T > kMaxRows || H < 1 || H > PMPE_MAX_NORM_WIDTH ? 0 : rms_norm_backward_workspace_bytes(T, H);
 }
 
 int pmpe_rms_norm_backward(const pmpe_rms_norm_backward_desc *d, void *stream)
@@ -71,7 +73,7 @@ int pmpe_rms_norm_backward(const pmpe_rms_norm_backward_desc *d, void *stream)
     if (!d || d->T < 0 || d->H < 1 || !is_type(d->type) || (d->weight_type != d->type && d->weight_type != PMPE_F32) ||
         (d->dy_type != d->type && d->dy_type != PMPE_F32) || (d->dx_type != d->type && d->dx_type != PMPE_F32))
         return PMPE_ERR_INVALID_ARG;
-    if (d->H > PMPE_MAX_NORM_WIDTH) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    if (d->H > PMPE_MAX_NORM_WIDTH || d->T > kMaxRows) return PMPE_ERR_UNSUPPORTED_SHAPE;
     if (!fits4(d->dw)) return PMPE_ERR_UNSUPPORTED_SHAPE;
     if (d->T == 0)  // no rows: the weight's gradient is zero
         return d->dw ? done(cudaMemsetAsync(d->dw, 0, (size_t)d->H * sizeof(float), (cudaStream_t)stream)) : PMPE_OK;

@@ -144,6 +144,15 @@ def test_values_whose_squares_leave_fp32(pmpe, scale, T):
     check(pmpe, randn((T, 512), 1, F32, scale), randn((512,), 2), None, eps=1e-12)
 
 
+@pytest.mark.parametrize("dtype,scale", [(BF16, 2.0 ** -128), (F16, 2.0 ** -18)])
+def test_sums_below_the_types_normal_values(pmpe, dtype, scale):
+    """x + residual is rounded to the type, subnormals included."""
+    x, res = randn((4, 256), 1, dtype, scale), randn((4, 256), 2, dtype, scale)
+    n = pmpe.rms_norm(x, randn((256,), 3, dtype), residual=res, eps=1e-20)
+    torch.cuda.synchronize()
+    assert torch.equal(n.h.cpu().double(), (x.cpu().double() + res.cpu().double()).to(dtype).double())
+
+
 def test_no_rows_and_refusals(pmpe):
     w = randn((64,), 1, BF16)
     n = pmpe.rms_norm(torch.empty((0, 64), dtype=BF16, device="cuda"), w, quant="block")

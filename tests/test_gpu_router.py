@@ -151,6 +151,36 @@ def test_near_ties(pmpe, score):
     check(pmpe, z16, None, torch.zeros(E, device="cuda"), E, 0, 8, score)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("top2", [False, True])
+def test_near_ties_of_many_tokens(pmpe, score, top2):
+    """Most tokens of a long batch in doubt at once, several of each CTA: the
+    selection against a sort of 64-bit choices, with the loads."""
+    T, E, k = 12001, 32, 5
+    g = torch.Generator().manual_seed(17)
+    z = (torch.randn((T, 1), generator=g).expand(T, E) + torch.randint(-3, 4, (T, E), generator=g) * 2.0 ** -22).float().cuda()
+    b = (torch.randint(-2, 3, (E,), generator=g) * 2.0 ** -25).cuda()
+    load = torch.zeros(E, dtype=torch.int32, device="cuda")
+    idx, w = pmpe.Router(E, 0, k, score=score, groups=(4, 2), group_score="top2" if top2 else "max").route(z, bias=b, load=load)
+    torch.cuda.synchronize()
+    s = 1 / (1 + torch.exp(-z.double())) if score == "sigmoid" else torch.softmax(z.double(), 1)
+    c = s + b.double()
+    v = torch.sort(c.view(T, 4, 8), dim=2, descending=True).values
+    v = v[:, :, 0] + v[:, :, 1] if top2 else v[:, :, 0]
+    kept = torch.zeros((T, 4), dtype=torch.bool, device="cuda")
+    kept.scatter_(1, torch.sort(v, dim=1, descending=True, stable=True).indices[:, :2], True)
+    c = torch.where(kept.repeat_interleave(8, 1), c, -1.0)
+    want = torch.sort(c, dim=1, descending=True, stable=True).indices[:, :k]
+    # torch's own softmax and this reference may round a sum differently: 64-bit
+    # choices within 2^-50 of one another have no order to hold to
+    a, d = torch.gather(c, 1, idx.long()), torch.gather(c, 1, want)
+    assert ((a - d).abs() <= 2.0 ** -50).all()
+    assert (idx == want).double().mean() > 0.999
+    assert torch.equal(load, torch.bincount(idx.flatten().long(), minlength=E).int())
+    weights = torch.gather(s, 1, idx.long())
+    assert (w.double() - weights / weights.sum(1, keepdim=True)).abs().max() <= REL
+
+
 def test_saturated_sigmoids(pmpe):
     """Sigmoids that round to 1 in 64 bits too are equal: the lower id."""
     g = torch.Generator().manual_seed(13)

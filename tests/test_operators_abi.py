@@ -80,7 +80,7 @@ def test_rms_norm_refusals(pmpe):
                 dict(eps=0.0), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(x=None), dict(weight=None),
                 dict(y=None), dict(x_ld=255), dict(residual_ld=255), dict(quant=1), dict(scale=P)):
         assert rc(**bad) == pmpe.ERR_INVALID_ARG, bad
-    for bad in (dict(H=16385, x_ld=16385, residual_ld=16385), dict(x=P + 1), dict(residual=P + 1), dict(h=P + 1), dict(y=P + 1),
+    for bad in (dict(T=(1 << 30) + 1), dict(H=16385, x_ld=16385, residual_ld=16385), dict(x=P + 1), dict(residual=P + 1), dict(h=P + 1), dict(y=P + 1),
                 dict(weight=P + 2, weight_type=0), dict(rstd=P + 2), dict(quant=1, scale=P + 2)):
         assert rc(**bad) == pmpe.ERR_UNSUPPORTED_SHAPE, bad
     assert rc(T=0, x=None, weight=None, y=None) == pmpe.OK
@@ -101,7 +101,7 @@ def test_rms_norm_backward_refusals(pmpe):
     for bad in (dict(T=-1), dict(H=0), dict(type=9), dict(weight_type=2), dict(dy_type=2), dict(dx_type=2), dict(dy=None),
                 dict(h=None), dict(weight=None), dict(rstd=None), dict(dx=None)):
         assert rc(**bad) == pmpe.ERR_INVALID_ARG, bad
-    for bad in (dict(H=16385), dict(dy=P + 2), dict(h=P + 1), dict(d_h=P + 1), dict(dx=P + 1), dict(dw=P + 2), dict(rstd=P + 2)):
+    for bad in (dict(T=(1 << 30) + 1), dict(H=16385), dict(dy=P + 2), dict(h=P + 1), dict(d_h=P + 1), dict(dx=P + 1), dict(dw=P + 2), dict(rstd=P + 2)):
         assert rc(**bad) == pmpe.ERR_UNSUPPORTED_SHAPE, bad
     for bad in (dict(workspace=None), dict(workspace=P + 8), dict(workspace_bytes=need - 1)):
         assert rc(**bad) == pmpe.ERR_WORKSPACE, bad
@@ -126,7 +126,7 @@ def test_route_refusals(pmpe):
                 dict(groups_pub=16, top_groups_pub=1), dict(groups_priv=4, top_groups_priv=1), dict(groups_priv=3),
                 dict(E_priv=0)):  # a policy without a private pool
         assert rc(**bad) == pmpe.ERR_INVALID_ARG, bad
-    for bad in (dict(E_pub=257, ld=300), dict(E_priv=257, ld=300), dict(E_pub=64, E_priv=64, ld=128, k=33), dict(logits=P + 2),
+    for bad in (dict(T=(1 << 30) + 1), dict(E_pub=257, ld=300), dict(E_priv=257, ld=300), dict(E_pub=64, E_priv=64, ld=128, k=33), dict(logits=P + 2),
                 dict(topk_idx=P + 1), dict(topk_w=P + 2), dict(bias=P + 2), dict(load=P + 2)):
         assert rc(**bad) == pmpe.ERR_UNSUPPORTED_SHAPE, bad
     assert rc(T=0, logits=None, topk_idx=None, topk_w=None) == pmpe.OK
