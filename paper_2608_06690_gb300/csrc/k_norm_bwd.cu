@@ -7,8 +7,8 @@
 //
 // FP32 throughout.  Bytes bound it, and close to them the instructions of a
 // row, so types are template parameters and a thread's pointers only advance.
-// A CTA takes a row, 8 columns a thread (up to 256 columns a warp does, eight
-// of them a CTA), and goes on to the rows a grid further, the next of which is
+// A CTA takes a row, 8 columns a thread up to 6144 columns (up to 256 columns a
+// warp does, eight of them a CTA), and goes on to the rows a grid further, the next of which is
 // on its way into registers meanwhile.  16 columns a thread need more than 128
 // registers for that and spill (27 us where 8 columns take 20).
 #include <algorithm>
@@ -163,20 +163,24 @@ __global__ void __launch_bounds__(32 * kStrands) rms_norm_dw_kernel(const float 
     if (lane == 0 && blockIdx.x * 32 + strand < H) dw[blockIdx.x * 32 + strand] = a;
 }
 
-// Threads of a CTA, and the CTAs: 768 threads an SM, at 80 registers (T = 4096,
-// 2048 columns, BF16 with an FP32 dy: 18.6 us, with 512 19.9, with 1024 at 64
-// registers 21.3).
-constexpr int kSmThreads = 768;
+// Threads of a CTA, and the CTAs that an SM holds: 768 threads at 80 registers
+// (T = 4096, 2048 columns, BF16 with an FP32 dy: 18.6 us, with 512 19.9, with
+// 1024 at 64 registers 21.3); wider rows' kernels take about 96, from 6145
+// columns on, with 16 columns a thread, 128.  A grid beyond them would run its
+// last CTAs in a second wave.  (T = 3276, 5120 columns, BF16: 32.4 us with 8
+// columns a thread, 43.5 with 16; T = 2340, 7168 columns 37.6 with 16, 35.6 with 8, FP32 30.0
+// and 32.6.)
+int sm_threads(int H) { return H <= 2048 ? 768 : H <= 4096 ? 640 : 512; }
 int threads_for(int H)
 {
     if (H <= 256) return 32 * kWarpRows;
-    const int columns = H <= 4096 ? 256 : 512;  // a warp's
+    const int columns = H <= 6144 ? 256 : 512;  // a warp's
     return (H + columns - 1) / columns * 32;
 }
 int bwd_ctas(int T, int H)
 {
     const int rows = H <= 256 ? kWarpRows : 1;
-    return std::max(1, std::min((T + rows - 1) / rows, kSms * std::max(1, kSmThreads / threads_for(H))));
+    return std::max(1, std::min((T + rows - 1) / rows, kSms * std::max(1, sm_threads(H) / threads_for(H))));
 }
 
 template <typename T, typename G, typename X, bool kVec> cudaError_t launch(const NormBwdParams &p, cudaStream_t st)
@@ -186,6 +190,7 @@ template <typename T, typename G, typename X, bool kVec> cudaError_t launch(cons
     if (p.H <= 256) return go(rms_norm_bwd_kernel<T, G, X, 1, true, kVec, 32 * kWarpRows, 3>);
     if (threads <= 256) return go(rms_norm_bwd_kernel<T, G, X, 1, false, kVec, 256, 3>);
     if (threads <= 512 && p.H <= 4096) return go(rms_norm_bwd_kernel<T, G, X, 1, false, kVec, 512, 1>);
+    if (p.H <= 6144) return go(rms_norm_bwd_kernel<T, G, X, 1, false, kVec, 768, 1>);
     if (threads <= 512) return go(rms_norm_bwd_kernel<T, G, X, 2, false, kVec, 512, 1>);
     return go(rms_norm_bwd_kernel<T, G, X, 2, false, kVec, 1024, 1>);
 }
