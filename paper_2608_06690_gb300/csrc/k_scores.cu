@@ -228,22 +228,38 @@ template <typename T> __device__ __forceinline__ Pool<T> pool_of(const ScorePara
             p.groups[priv], p.top_groups[priv], p.top2, p.k};
 }
 
-// Selection by 64-bit choices of a token that FP32 does not settle, by the
-// whole CTA: a thread evaluates an expert, warp 0 selects.  s_key: choices, then
-// what groups count by (0: no candidate).
+// A token that FP32 does not settle.  kept: its groups where those are settled
+// (0: they are not), and then the FP32 choice below which no expert can be
+// among the k.
+struct Aside {
+    int t;
+    uint32_t kept;
+    float least;
+};
+
+__device__ __forceinline__ float fast_sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+
+// Its selection by 64-bit choices, by the whole CTA: a thread evaluates an
+// expert, warp 0 selects.  s_key: choices, then what groups count by (0: no
+// candidate).
 template <typename T, int kV>
-__device__ __noinline__ void select_exactly(const ScoreParams &p, int t, u64 (&s_key)[2][kMaxPool], int *s_load)
+__device__ __noinline__ void select_exactly(const ScoreParams &p, const Aside &a, u64 (&s_key)[2][kMaxPool], int *s_load)
 {
+    const int t = a.t;
     __shared__ double s_sum[kRouteWarps];
     __shared__ uint32_t s_max[kRouteWarps];
     const int e = threadIdx.x, lane = e & 31, warp = e >> 5;
     const int priv = p.policy != nullptr && p.policy[t] == 0x01 ? 1 : 0, base = priv ? p.E_pub : 0;
     const Pool<T> pool = pool_of<T>(p, t, priv);
     const float raw = e < pool.E ? to_f32(pool.row[e]) : kNone, z = raw > kNone ? fminf(raw, kLargest) + 0.f : kNone;
+    bool on = z > kNone;
+    if (a.kept) on = on && ((a.kept >> (e / (pool.E / pool.n))) & 1u);
     float mx = kNone;
     double sum = 1., v = 0.;
     if (p.sigmoid) {
-        if (z > kNone) v = 1. / (1. + exp(-(double)z));
+        // a warp without a candidate has nothing to evaluate
+        on = on && (!a.kept || fast_sigmoid(z) + pool.bias[e] >= a.least);
+        if (on) v = 1. / (1. + exp(-(double)z));
     } else {
         const uint32_t top = __reduce_max_sync(~0u, key_of(z));
         if (lane == 0) s_max[warp] = top;
@@ -257,10 +273,10 @@ __device__ __noinline__ void select_exactly(const ScoreParams &p, int t, u64 (&s
         __syncthreads();
         sum = 0.;
         for (int q = 0; q < kRouteWarps; ++q) sum += s_sum[q];
-        if (z > kNone) v /= sum;
+        if (on) v /= sum;
     }
-    if (pool.bias && z > kNone) v += pool.bias[e];
-    const bool on = z > kNone && v > (double)kNone;  // a bias of -inf (or NaN) takes its expert out
+    if (pool.bias && on) v += pool.bias[e];
+    on = on && v > (double)kNone;  // a bias of -inf (or NaN) takes its expert out
     s_key[0][e] = !on ? 0 : pool.bias ? key64(v) : key64((double)z);
     s_key[1][e] = !on ? 0 : p.top2 ? key64(v) : s_key[0][e];
     __syncthreads();
@@ -271,7 +287,7 @@ __device__ __noinline__ void select_exactly(const ScoreParams &p, int t, u64 (&s
             key[i] = s_key[0][lane * kV + i];
             by[i] = s_key[1][lane * kV + i];
         }
-        if (pool.top < pool.n) {
+        if (!a.kept) {
             const int size = pool.E / pool.n;
             const u64 g = key64(group_value<u64, kV>(by, pool.n, size, p.top2, lane));
             int place = 0;
@@ -322,13 +338,14 @@ template <typename T, int kV, bool kBias, bool kGroups>
 __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const ScoreParams p)
 {
     constexpr bool kAside = kBias || kGroups;
-    extern __shared__ int s_tokens[];
+    extern __shared__ int s_dynamic[];
     __shared__ u64 s_key[kAside ? 2 : 1][kAside ? kMaxPool : 1];
     __shared__ int s_aside;
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E_all = p.E_pub + p.E_priv;
-    int *s_load = s_tokens + (kAside ? p.tokens : 0);
+    Aside *s_tokens = reinterpret_cast<Aside *>(s_dynamic);
+    int *s_load = s_dynamic + (kAside ? p.tokens * (int)(sizeof(Aside) / sizeof(int)) : 0);
     if (p.load)
         for (int e = threadIdx.x; e < E_all; e += blockDim.x) s_load[e] = 0;
     if (threadIdx.x == 0) s_aside = 0;
@@ -388,7 +405,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
         if (scored) {
             if (p.sigmoid) {
 #pragma unroll
-                for (int i = 0; i < kV; ++i) val[i] = __fdividef(1.f, 1.f + __expf(-z[i]));
+                for (int i = 0; i < kV; ++i) val[i] = fast_sigmoid(z[i]);
             } else {
                 const float inv_sum = 1.f / sum;
 #pragma unroll
@@ -404,15 +421,15 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
         float choice[kV];  // -inf: no candidate
 #pragma unroll
         for (int i = 0; i < kV; ++i) choice[i] = kBias ? val[i] : z[i];
-        bool doubt = false;
+        bool doubt = false, groups_doubt = false;
+        int g = 0, place = 0;  // this lane's group and its place
         if (kGroups && limited) {
             const int n = pool.n, top = pool.top, size = E / n, seg = lanes_of_group<kV>(size);
             float by[kV];  // what groups count by
 #pragma unroll
             for (int i = 0; i < kV; ++i) by[i] = p.top2 ? val[i] : choice[i];
-            float a;       // a group's value: its lanes', or lane g's of group g
-            int g, place = 0;
-            if (seg) {     // every group at once: its lanes hold its two best after log2(seg) exchanges
+            float a;    // a group's value: its lanes', or lane g's of group g
+            if (seg) {  // every group at once: its lanes hold its two best after log2(seg) exchanges
                 float b = kNone;
                 a = kNone;
 #pragma unroll
@@ -454,7 +471,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
                 top_value = of(__reduce_max_sync(~0u, key_of(top_value)));
                 const float x = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top - 1)) - 1);
                 const float y = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top)) - 1);
-                doubt = y > kNone && x - y <= 4.f * err + 0x1p-20f * top_value;
+                groups_doubt = y > kNone && x - y <= 4.f * err + 0x1p-20f * top_value;
             }
         }
         // Neighbours in the order, the last one's being the first not chosen
@@ -485,24 +502,28 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
             pick_whole<uint32_t, kV>(key, p.k, lane, e_mine, e_next);
         }
         auto score = [&](float zz) { return p.sigmoid ? 1.f / (1.f + expf(-zz)) : expf(zz - mx) / sum; };
-        float zj = kNone, sj = 0.f;
+        float zj = kNone, sj = 0.f, c0 = kNone;
         if (e_mine >= 0) {
             zj = logit(pool, e_mine);
             if (p.sigmoid || !p.renorm || kBias) sj = score(zj);
         }
         if (kBias) {
-            const float b0 = e_mine >= 0 ? pool.bias[e_mine] : 0.f, c0 = e_mine >= 0 ? sj + b0 : kNone;
+            const float b0 = e_mine >= 0 ? pool.bias[e_mine] : 0.f;
+            c0 = e_mine >= 0 ? sj + b0 : kNone;
             float z1 = __shfl_down_sync(~0u, zj, 1), b1 = __shfl_down_sync(~0u, b0, 1), c1 = __shfl_down_sync(~0u, c0, 1);
             if (p.k == 32 && lane == 31) {  // no lane holds the 33rd
                 z1 = e_next >= 0 ? logit(pool, e_next) : kNone;
                 b1 = e_next >= 0 ? pool.bias[e_next] : 0.f;
                 c1 = e_next >= 0 ? score(z1) + b1 : kNone;
             }
-            doubt = doubt || (lane < p.k && c1 > kNone && c0 - c1 <= 2.f * err + 0x1.4p-24f * (fabsf(c0) + fabsf(c1)) &&
-                              !(b0 == b1 && zj == z1));
+            doubt = lane < p.k && c1 > kNone && c0 - c1 <= 2.f * err + 0x1.4p-24f * (fabsf(c0) + fabsf(c1)) &&
+                    !(b0 == b1 && zj == z1);
         }
-        if (kAside && __any_sync(~0u, doubt)) {
-            if (lane == 0) s_tokens[atomicAdd(&s_aside, 1)] = t;
+        if (kAside && __any_sync(~0u, doubt || groups_doubt)) {
+            const float c = __shfl_sync(~0u, c0, p.k - 1);  // the k-th choice, off by at most err + 2^-24 |c|, as any other
+            const uint32_t kept = limited ? __reduce_or_sync(~0u, g < pool.n && place < pool.top ? 1u << g : 0u) : ~0u;
+            if (lane == 0)
+                s_tokens[atomicAdd(&s_aside, 1)] = {t, groups_doubt ? 0u : kept, c - 2.02f * (err + 0x1.4p-24f * fabsf(c))};
             continue;
         }
         const bool mine = lane < p.k && e_mine >= 0;
@@ -653,7 +674,7 @@ template <typename Go> cudaError_t dispatch(int type, int pool, Go go)
 
 // CTAs for T tokens: up to eight an SM (prompts: T = 16384, 128 + 32 experts
 // 8.3 us, with four 12.4), and not more than kMostTokens tokens each.
-constexpr int kMostTokens = 4096;
+constexpr int kMostTokens = 1024;
 int grid_of(int T, int num_sms)
 {
     const int all = (T + kRouteWarps - 1) / kRouteWarps;
@@ -675,7 +696,7 @@ cudaError_t launch_route_scores(const pmpe_route_desc &d, int num_sms, cudaStrea
     const bool limited = d.top_groups_pub < d.groups_pub || (d.E_priv > 0 && d.top_groups_priv < d.groups_priv);
     const dim3 grid(grid_of(d.T, num_sms)), block(32 * kRouteWarps);
     p.tokens = (d.T + (int)grid.x * kRouteWarps - 1) / ((int)grid.x * kRouteWarps) * kRouteWarps;
-    const size_t smem = ((limited || d.bias ? p.tokens : 0) + (d.load ? d.E_pub + d.E_priv : 0)) * sizeof(int);
+    const size_t smem = (limited || d.bias ? p.tokens * sizeof(Aside) : 0) + (d.load ? (d.E_pub + d.E_priv) * sizeof(int) : 0);
     return dispatch(d.logits_type, std::max(d.E_pub, d.E_priv), [&](auto t, auto v) {
         using T = decltype(t);
         constexpr int kV = decltype(v)::value;
