@@ -181,5 +181,12 @@ __device__ __forceinline__ float max_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+// The same of two magnitudes; the sign is that of the product.
+__device__ __forceinline__ float max_magnitude(float a, float b)
+{
+    float r;
+    asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 
 }  // namespace pmpe

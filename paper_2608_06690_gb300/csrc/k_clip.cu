@@ -13,11 +13,12 @@
 // is read by each, and written once.  The second takes the chunks from last
 // to first, so that it finds in L2 what the first read last.
 //
-// A vector's squares are summed in FP32, the vectors' sums in pairs of FP32
-// words (a value and what its rounding lost, 48 bits: FP64 adds, two a clock
-// and SM, took longer than the small cases' loads).  A vector whose sum of
-// squares leaves 2^-120 .. 2^90 (values that overflow or vanish when squared)
-// goes to a 64-bit sum instead, which exists in the CTAs that met one.
+// A thread's squares of a chunk are summed in FP32 (four vectors by themselves,
+// then those), the chunks' sums in pairs of FP32 words (a value and what its
+// rounding lost, 48 bits: FP64 adds, two a clock and SM, took longer than the
+// small cases' loads).  Where a thread's sum leaves 2^-120 .. 2^90 (values that
+// overflow or vanish when squared) its vectors go to a 64-bit sum instead,
+// which exists in the CTAs that met one.
 #include <algorithm>
 #include <new>
 
@@ -67,16 +68,32 @@ inline long long chunks_of(const pmpe_grad &g)
     return g.n > 0 && c < 1 ? 1 : c;
 }
 
-__device__ __forceinline__ void unpack_vec(const uint4 &u, int type, float (&v)[8])
+// A vector's elements.
+template <typename T> struct Elems {
+    static constexpr int n = 16 / (int)sizeof(T);
+    float v[n];
+};
+__device__ __forceinline__ Elems<float> elems(const uint4 &u, float)
 {
-    if (type == PMPE_F32) {
-        v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
-        v[4] = v[5] = v[6] = v[7] = 0.f;
-    } else if (type == PMPE_BF16) {
-        unpack8(u, v, bf16());
-    } else {
-        unpack8(u, v, __half());
-    }
+    return {{__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)}};
+}
+template <typename T> __device__ __forceinline__ Elems<T> elems(const uint4 &u, T)
+{
+    Elems<T> e;
+    unpack8(u, e.v, T());
+    return e;
+}
+__device__ __forceinline__ uint4 vector_of(const Elems<float> &e)
+{
+    return make_uint4(__float_as_uint(e.v[0]), __float_as_uint(e.v[1]), __float_as_uint(e.v[2]), __float_as_uint(e.v[3]));
+}
+template <typename T> __device__ __forceinline__ uint4 vector_of(const Elems<T> &e) { return pack8(e.v, T()); }
+// Calls go with an element of the type.
+template <typename Go> __device__ __forceinline__ void by_type(int type, Go go)
+{
+    if (type == PMPE_F32) go(0.f);
+    else if (type == PMPE_BF16) go(bf16());
+    else go(__half());
 }
 __device__ __forceinline__ float load_one(const void *p, long long i, int type)
 {
@@ -106,25 +123,6 @@ struct Squares {
     Sum2 s;
     double rare;
 };
-
-// The squares of a vector, added to the sums.
-__device__ __forceinline__ void add_squares(const float (&v)[8], float &fast, double &rare)
-{
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s += v[i] * v[i];
-    if (s >= 0x1p-120f && s < 0x1p90f) {
-        fast += s;
-    } else {
-        uint32_t any = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) any |= __float_as_uint(v[i]);
-        if (any << 1) {  // zeros stay here
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rare += (double)v[i] * v[i];
-        }
-    }
-}
 
 // The sums over the CTA's threads, in a fixed order, in all of them.
 __device__ __forceinline__ Squares cta_sum(Sum2 s, double rare)
@@ -202,47 +200,77 @@ template <bool kLast> __device__ __forceinline__ void load_chunk(uint4 (&u)[kCli
     }
 }
 
+// The squares of a thread's part of a chunk in 64 bits, from memory again.
+__device__ __forceinline__ double exact_squares(const Chunk &k, int t)
+{
+    double sum = 0.;
+    const int per = 16 >> elem_shift(k.type);
+#pragma unroll 1
+    for (int q = 0; q < kClipVecs; ++q) {
+        const long long at = k.v0 + q * kClipThreads + t;
+#pragma unroll 1
+        for (int j = 0; j < per && at < k.vecs; ++j) {
+            const double x = load_one(k.body, at * per + j, k.type);
+            sum += x * x;
+        }
+    }
+    if (t < k.head) {
+        const double x = load_one(k.body, t - k.head, k.type);
+        sum += x * x;
+    }
+    if (t < k.tail) {
+        const double x = load_one(k.body + k.vecs, t, k.type);
+        sum += x * x;
+    }
+    return sum;
+}
+
 __device__ __forceinline__ void square_chunk(const uint4 (&u)[kClipVecs], const Chunk &k, int t, Sum2 &sum, double &rare)
 {
-    float fast = 0.f, v[8];
-#pragma unroll
-    for (int q = 0; q < kClipVecs; ++q) {
-        unpack_vec(u[q], k.type, v);
-        add_squares(v, fast, rare);
-    }
+    float all = 0.f;
+    uint32_t any = 0;  // zero for zeros alone (a -0 is summed in 64 bits, for nothing)
     if (t < max(k.head, k.tail)) {  // at most seven of each
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.f;
-        if (t < k.head) v[0] = load_one(k.body, t - k.head, k.type);
-        if (t < k.tail) v[1] = load_one(k.body + k.vecs, t, k.type);
-        add_squares(v, fast, rare);
+        const float a = t < k.head ? load_one(k.body, t - k.head, k.type) : 0.f;
+        const float b = t < k.tail ? load_one(k.body + k.vecs, t, k.type) : 0.f;
+        all = a * a + b * b;
+        any = __float_as_uint(a) | __float_as_uint(b);
     }
-    add2(sum, fast);
+#pragma unroll
+    for (int q = 0; q < kClipVecs; ++q) any |= u[q].x | u[q].y | u[q].z | u[q].w;
+    by_type(k.type, [&](auto zero) {
+#pragma unroll
+        for (int q = 0; q < kClipVecs; ++q) {
+            const auto e = elems(u[q], zero);
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < e.n; ++j) s += e.v[j] * e.v[j];
+            all += s;
+        }
+    });
+    if (all >= 0x1p-120f && all < 0x1p90f) add2(sum, all);
+    else if (any) rare += exact_squares(k, t);
 }
 
 __device__ __forceinline__ void scale_chunk(const uint4 (&u)[kClipVecs], const Chunk &k, int t, float f)
 {
     const int per = 16 >> elem_shift(k.type);
     const bool vec_out = ((uintptr_t)k.out & 15u) == 0;
+    by_type(k.type, [&](auto zero) {
 #pragma unroll
-    for (int q = 0; q < kClipVecs; ++q) {
-        const long long at = k.v0 + q * kClipThreads + t;
-        if (at >= k.vecs) continue;
-        float v[8];
-        unpack_vec(u[q], k.type, v);
+        for (int q = 0; q < kClipVecs; ++q) {
+            const long long at = k.v0 + q * kClipThreads + t;
+            if (at >= k.vecs) continue;
+            auto e = elems(u[q], zero);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= f;
-        if (vec_out) {
-            const uint4 r = k.type == PMPE_F32 ? make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]),
-                                                            __float_as_uint(v[2]), __float_as_uint(v[3]))
-                                               : k.type == PMPE_BF16 ? pack8(v, bf16()) : pack8(v, __half());
-            __stcs(reinterpret_cast<uint4 *>(k.out) + at, r);
-        } else {  // an output that is not aligned as its gradient is
+            for (int j = 0; j < e.n; ++j) e.v[j] *= f;
+            if (vec_out) {
+                __stcs(reinterpret_cast<uint4 *>(k.out) + at, vector_of(e));
+            } else {  // an output that is not aligned as its gradient is
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < per) store_one(k.out, at * per + j, k.type, v[j]);
+                for (int j = 0; j < e.n; ++j) store_one(k.out, at * e.n + j, k.type, e.v[j]);
+            }
         }
-    }
+    });
     if (t < k.head) store_one(k.out, t - k.head, k.type, f * load_one(k.body, t - k.head, k.type));
     if (t < k.tail) store_one(k.out, k.vecs * per + t, k.type, f * load_one(k.body + k.vecs, t, k.type));
 }

@@ -46,14 +46,16 @@ constexpr float kMinScale = 1.17549435e-38f;  // 2^-126: the smallest scale, so 
 struct Divide {
     float hi, lo;
 };
-// For values u of a block whose largest is amax and which stand for u m:
-// the scale s = max(amax m / 448, 2^-126) and the factor u -> u m / s.
+// For values u of a block whose largest is amax in magnitude and which stand
+// for u m: the scale s = max(amax m / 448, 2^-126) and the factor u -> u m / s.
 __device__ __forceinline__ Divide divide_by(float amax, float m, float &s)
 {
-    s = max_nan(amax * m / 448.f, kMinScale);
+    amax = fabsf(amax);
+    s = max_nan(amax * m * (1.f / 448.f), kMinScale);
     if (!(s > kMinScale)) return {m * 0x1p126f, 0.f};  // zeros (or NaN)
-    const float hi = 448.f / amax;
-    return {hi, hi > 0.f ? fmaf(-hi, amax, 448.f) / amax : 0.f};
+    // the product's remainder is exact in one fused operation
+    const float inv = __frcp_rn(amax), hi = 448.f * inv;
+    return {hi, hi > 0.f ? fmaf(-hi, amax, 448.f) * inv : 0.f};
 }
 __device__ __forceinline__ uint32_t e4m3x2(float a, float b)
 {
@@ -138,20 +140,20 @@ __global__ void __launch_bounds__(kThreads) rms_norm_kernel(const NormParams p)
             store8<kVec>((T *)p.y + row * p.H + c, v[i], p.H - c);
         } else if (p.quant == PMPE_QUANT_ROW) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) amax = max_nan(amax, fabsf(v[i][j]));
+            for (int j = 0; j < 8; ++j) amax = max_magnitude(amax, v[i][j]);
         }
     }
     if (p.quant == PMPE_QUANT_NONE) return;
     Divide by = {0.f, 0.f};
     if (p.quant == PMPE_QUANT_ROW) {
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) amax = max_nan(amax, __shfl_xor_sync(~0u, amax, off));
+        for (int off = 16; off > 0; off >>= 1) amax = max_magnitude(amax, __shfl_xor_sync(~0u, amax, off));
         if (!kWarpRow) {
             if (lane == 0) s_max[threadIdx.x >> 5] = amax;
             __syncthreads();
             amax = lane < warps ? s_max[lane] : 0.f;
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) amax = max_nan(amax, __shfl_xor_sync(~0u, amax, off));
+            for (int off = 16; off > 0; off >>= 1) amax = max_magnitude(amax, __shfl_xor_sync(~0u, amax, off));
         }
         float s;
         by = divide_by(amax, m, s);
@@ -166,9 +168,9 @@ __global__ void __launch_bounds__(kThreads) rms_norm_kernel(const NormParams p)
             if (p.quant == PMPE_QUANT_BLOCK) {  // 16 threads hold a block; columns past H hold zeros
                 float a = 0.f, s;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) a = max_nan(a, fabsf(v[i][j]));
+                for (int j = 0; j < 8; ++j) a = max_magnitude(a, v[i][j]);
 #pragma unroll
-                for (int off = 8; off > 0; off >>= 1) a = max_nan(a, __shfl_xor_sync(~0u, a, off));
+                for (int off = 8; off > 0; off >>= 1) a = max_magnitude(a, __shfl_xor_sync(~0u, a, off));
                 by = divide_by(a, m, s);
                 if ((at.t & 15) == 0 && n > 0) p.scale[row * nb + c / 128] = s;
             }
@@ -184,9 +186,9 @@ __global__ void __launch_bounds__(kThreads) rms_norm_kernel(const NormParams p)
                 if (p.quant == PMPE_QUANT_BLOCK) {
                     float a = 0.f, s;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) a = max_nan(a, fabsf(v[i][4 * b + j]));
+                    for (int j = 0; j < 4; ++j) a = max_magnitude(a, v[i][4 * b + j]);
 #pragma unroll
-                    for (int off = 16; off > 0; off >>= 1) a = max_nan(a, __shfl_xor_sync(~0u, a, off));
+                    for (int off = 16; off > 0; off >>= 1) a = max_magnitude(a, __shfl_xor_sync(~0u, a, off));
                     by = divide_by(a, m, s);
                     if (lane == 0 && n > 128 * b) p.scale[row * nb + c / 128 + b] = s;
                 }
