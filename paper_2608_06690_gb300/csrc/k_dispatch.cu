@@ -129,6 +129,7 @@ struct AdoptParams {
     int32_t *idx, *ticket;        // [T, k] the picks as they run, and their tickets
     float *w;
     uint32_t *tile_counts;        // [E][slots4] the column of this CTA's tile
+    uint32_t *gemm_bar;           // the expert launch's grid barrier counter, zeroed here
     uint32_t *status, *route_count, *route_priv_rows;
 };
 
@@ -149,6 +150,7 @@ __global__ void __launch_bounds__(kAdoptTile) adopt_route_kernel(const AdoptPara
     const int E = p.E_pub + p.E_priv, tile = blockIdx.x, t = tile * kAdoptTile + threadIdx.x;
     for (int i = threadIdx.x; i < 4 * E; i += kAdoptTile) (&s_mask[0][0])[i] = 0u;
     __syncthreads();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.gemm_bar = 0u;  // read by the expert launch after this grid
     const uint32_t bit = 1u << (threadIdx.x & 31);
     const int word = threadIdx.x >> 5;
     int base = 0, pool = 0;
@@ -455,6 +457,7 @@ cudaError_t launch_adopt_route(const Ctx &c, const int32_t *idx, const float *w)
     p.idx_in = idx; p.w_in = w; p.policy = c.policy;
     p.T = s.T; p.k = s.k; p.E_pub = s.E_pub; p.E_priv = s.E_priv; p.slots4 = router_slots4(s.T);
     p.tau = c.tau; p.idx = c.idx; p.ticket = c.ticket; p.w = c.w; p.tile_counts = c.tile_counts;
+    p.gemm_bar = c.gemm_ready + gemm_ready_words(s) - 1;
     p.status = c.audit.status; p.route_count = c.audit.route_count; p.route_priv_rows = c.audit.route_priv_rows;
     // every tile slot's column is written, zeros for those without tokens
     return launch_pdl(adopt_route_kernel, dim3(router_slots(s.T)), dim3(kAdoptTile), 0, c.stream, p);

@@ -392,9 +392,13 @@ int pmpe_moe_forward_routed(const pmpe_moe_desc *d, void *stream)
     const int rc = make_routed_ctx(d, stream, &c);
     if (rc != PMPE_OK) return rc;
     if (c.s.T == 0) return PMPE_OK;
+    // the dispatch inside the expert launch where it can be (T = 16384: a
+    // kernel of its own takes 32 us), else as a kernel; both clear that
+    // launch's counters
+    const bool fuse = experts_fuse_dispatch(c);
     cudaError_t err = launch_adopt_route(c, d->topk_idx, d->topk_w);
-    if (err == cudaSuccess) err = launch_permute(c);
-    if (err == cudaSuccess) err = launch_experts(c, false, false);  // the dispatch cleared its counters
+    if (err == cudaSuccess && !fuse) err = launch_permute(c);
+    if (err == cudaSuccess) err = launch_experts(c, false, fuse);
     if (err == cudaSuccess) err = launch_combine(c);
     return err == cudaSuccess ? PMPE_OK : PMPE_ERR_CUDA;
 }

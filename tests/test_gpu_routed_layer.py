@@ -17,6 +17,7 @@ SHAPES = {
     "one_token": (LayerShape(T=1, H=256, I=128, E_pub=8, E_priv=4, E_sh=1, k=2, renormalize=True), 13, "allow"),
     "tile_edges": (LayerShape(T=129, H=256, I=128, E_pub=40, E_priv=16, E_sh=0, k=12, renormalize=True), 14, "iid"),
     "no_policy": (LayerShape(T=256, H=256, I=128, E_pub=8, E_priv=4, E_sh=0, k=4, renormalize=True), 15, "none"),
+    "large_experts_decode": (LayerShape(T=70, H=2048, I=768, E_pub=32, E_priv=16, E_sh=1, k=8, renormalize=True), 17, "iid"),
     "large_experts": (LayerShape(T=700, H=2048, I=768, E_pub=128, E_priv=32, E_sh=0, k=8, renormalize=True), 16, "iid"),
 }
 
