@@ -558,14 +558,20 @@ def _bad(what: str):
 def _elsewhere(fn, t, stream, *args, **kw):
     """The call again on ``stream``, or on the tensor's device: outputs and
     scratch are allocated where the kernels run, so that the caching allocator
-    reuses them in order."""
+    reuses them in order, and the arguments' memory is not reused before the
+    stream is done with it.  (The caller orders the streams' work.)"""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _bad(f"{fn.__name__}: CUDA tensors are wanted")
     if stream is not None:
         if stream.device != t.device:
             _bad(f"{fn.__name__}: the stream is of another device than the tensors")
         with torch.cuda.stream(stream):
-            return fn(*args, **kw)
+            result = fn(*args, **kw)
+        for a in args:
+            for v in a if isinstance(a, (list, tuple)) else (a,):
+                if isinstance(v, torch.Tensor):
+                    v.record_stream(stream)
+        return result
     with torch.cuda.device(t.device):
         return fn(*args, **kw)
 

@@ -250,3 +250,22 @@ def test_other_stream_and_graph(pmpe):
         e = pmpe.rms_norm(x, w, residual=res)
         ex, ew = pmpe.rms_norm_backward(dy, e.h, w, e.rstd, d_h=res)
         assert torch.equal(n.y, e.y) and torch.equal(gx, ex) and torch.equal(gw, ew)
+
+
+def test_arguments_freed_while_the_other_stream_has_yet_to_run(pmpe):
+    """The memory of a call's arguments is not handed out again before the
+    stream that it was given is done with them."""
+    w = randn((2048,), 1, BF16)
+    x, res = randn((300, 2048), 2, BF16), randn((300, 2048), 3, BF16)
+    want = pmpe.rms_norm(x, w, residual=res).y.clone()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)  # some 10 ms
+    got = pmpe.rms_norm(x, w, residual=res, stream=s)
+    del x, res
+    other = [torch.full((300, 2048), 7.0, dtype=BF16, device="cuda") for _ in range(4)]
+    y = got.y
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want) and all((o == 7).all() for o in other)
