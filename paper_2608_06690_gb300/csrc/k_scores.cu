@@ -200,7 +200,11 @@ __device__ __forceinline__ auto group_value(const K (&key)[kV], int n, int size,
         const K first = warp_max(a);
         const int who = __ffs(__ballot_sync(~0u, a == first)) - 1;
         const K second = top2 ? warp_max(lane == who ? b : a) : 0;
-        if (lane == g && first != 0) mine = second != 0 ? of(first) + of(second) : of(first);
+        if (lane == g && first != 0) {
+            mine = of(first);
+            if (second != 0) mine += of(second);
+            if constexpr (sizeof(K) == 4) mine = fmaxf(mine, -kLargest);  // two of the lowest value are still candidates
+        }
     }
     return mine;
 }
@@ -258,7 +262,7 @@ __device__ __noinline__ void select_exactly(const ScoreParams &p, const Aside &a
     double sum = 1., v = 0.;
     if (p.sigmoid) {
         // a warp without a candidate has nothing to evaluate
-        on = on && (!a.kept || fast_sigmoid(z) + pool.bias[e] >= a.least);
+        on = on && (!a.kept || !(fast_sigmoid(z) + pool.bias[e] < a.least));
         if (on) v = 1. / (1. + exp(-(double)z));
     } else {
         const uint32_t top = __reduce_max_sync(~0u, key_of(z));
@@ -439,7 +443,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
                     add_two(a, b, oa);
                     add_two(a, b, ob);
                 }
-                if (p.top2 && b > kNone) a += b;
+                if (p.top2 && b > kNone) a = fmaxf(a + b, -kLargest);  // two of the lowest value are still candidates
                 g = lane / seg;
                 for (int q = 0; q < n; ++q) {
                     const float o = __shfl_sync(~0u, a, q * seg);
@@ -471,7 +475,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
                 top_value = of(__reduce_max_sync(~0u, key_of(top_value)));
                 const float x = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top - 1)) - 1);
                 const float y = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top)) - 1);
-                groups_doubt = y > kNone && x - y <= 4.f * err + 0x1p-20f * top_value;
+                groups_doubt = y > kNone && !(x - y > 4.f * err + 0x1p-20f * top_value);
             }
         }
         // Neighbours in the order, the last one's being the first not chosen
@@ -479,6 +483,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
         // choices are equal (again from the whole ones) or their FP32 choices
         // closer than those are exact, unless their logits and biases are the
         // same: a true tie.  16-bit logits without a bias are packed whole.
+        // (Comparisons are written so that an infinite bias means doubt.)
         constexpr bool inexact = kBias || sizeof(T) == 4;
         int e_mine, e_next;
         bool whole;
@@ -516,7 +521,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
                 b1 = e_next >= 0 ? pool.bias[e_next] : 0.f;
                 c1 = e_next >= 0 ? score(z1) + b1 : kNone;
             }
-            doubt = lane < p.k && c1 > kNone && c0 - c1 <= 2.f * err + 0x1.4p-24f * (fabsf(c0) + fabsf(c1)) &&
+            doubt = lane < p.k && c1 > kNone && !(c0 - c1 > 2.f * err + 0x1.4p-24f * (fabsf(c0) + fabsf(c1))) &&
                     !(b0 == b1 && zj == z1);
         }
         if (kAside && __any_sync(~0u, doubt || groups_doubt)) {
@@ -580,8 +585,8 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
         int e = -1;
         float D = 0.f, zj = kNone;
         if (lane < p.k) {
-            e = p.idx[(long long)t * p.k + lane] - base;
-            if (e < 0 || e >= E) e = -1;
+            e = p.idx[(long long)t * p.k + lane];  // any value
+            e = e >= base && e < base + E ? e - base : -1;
             if (e >= 0) {
                 zj = to_f32(row[e]);
                 if (zj > kNone) D = p.dw[(long long)t * p.k + lane] * p.scale;

@@ -130,6 +130,37 @@ def test_masked_experts(pmpe, score, renorm):
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E", [64, 60])  # groups of whole lanes, and others
+@pytest.mark.parametrize("group_score", ["max", "top2"])
+def test_extreme_biases(pmpe, score, E, group_score):
+    """Experts forced by a bias of +inf, masked by the type's lowest value or
+    by -inf, and the largest finite bias: sums of two that pass FP32's range."""
+    z, _, _ = make(9, E, 0, 21)
+    size = E // 4
+    low, high = torch.finfo(F32).min, torch.finfo(F32).max
+    z[1, :size] = -np.inf  # a group without a candidate before those of the lowest value
+    for kind in range(6):
+        b = 0.05 * torch.randn(E, generator=torch.Generator().manual_seed(kind))
+        if kind == 0:  # fewer, as many and more than k
+            b[[3, 17, 40]] = np.inf
+        elif kind == 1:
+            b[[3, 5, 17, 40, 41]] = np.inf
+        elif kind == 2:
+            b[::2] = np.inf
+        elif kind == 3:
+            b[:] = low
+        elif kind == 4:
+            b[size:] = low
+            b[:size:3] = -np.inf
+        else:
+            b[2 * size:] = high
+            b[0] = low
+        b = b.cuda()
+        check(pmpe, z, None, b, E, 0, 5, score, True, backward=False)
+        check(pmpe, z, None, b, E, 0, 5, score, False, 2.5, (4, 2), (1, 1), group_score, backward=False)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_near_ties(pmpe, score):
     """Logits and biases that FP32 scores cannot tell apart: the selection is
     that of 64 bits, equal values by the lower id."""
@@ -192,7 +223,7 @@ def test_backward_ignores_foreign_ids_and_adds_repeated_ones(pmpe):
     z, policy, _ = make(6, 16, 8, 2)
     policy[:] = 0
     r = pmpe.Router(16, 8, 3, renormalize=False)
-    idx = torch.tensor([[1, 1, 2], [-1, 5, 20], [3, 99, 4], [16, 17, 18], [0, 1, 2], [-7, -1, 15]], dtype=torch.int32).cuda()
+    idx = torch.tensor([[1, 1, 2], [-1, 5, 20], [3, 99, 4], [16, 17, 18], [0, 1, 2], [-7, -2 ** 31, 15]], dtype=torch.int32).cuda()
     dw = torch.randn((6, 3), generator=torch.Generator().manual_seed(1)).cuda()
     d = r.backward(z, policy, idx, dw)
     torch.cuda.synchronize()
@@ -243,3 +274,17 @@ def test_other_stream_and_graph(pmpe):
     i4, w4 = r.route(z, policy, bias=b)
     assert torch.equal(i3, i4) and torch.equal(w3, w4) and torch.equal(d3, r.backward(z, policy, i4, w4))
     assert int(load.sum()) == 2 * 700 * 8
+
+
+def test_more_than_2_to_31_logits(pmpe):
+    """Offsets past 32 bits: the last tokens are those of a call on them alone."""
+    T, E = 8_400_000, 256
+    z = torch.empty((T, E), dtype=BF16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    b = 0.05 * torch.randn(E, generator=torch.Generator().manual_seed(2)).cuda()
+    r = pmpe.Router(E, 0, 4, score="sigmoid", groups=(8, 4), group_score="top2")
+    load = torch.zeros(E, dtype=torch.int32, device="cuda")
+    idx, w = r.route(z, bias=b, load=load)
+    few = z[-500:].clone()
+    i2, w2 = r.route(few, bias=b)
+    assert torch.equal(idx[-500:], i2) and torch.equal(w[-500:], w2) and int(load.sum(dtype=torch.int64)) == 4 * T
+    assert torch.equal(r.backward(z, None, idx, w)[-500:], r.backward(few, None, i2, w2))
