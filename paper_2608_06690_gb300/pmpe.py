@@ -411,6 +411,8 @@ class MoeLayer:
         s = self._shape_T(T)
         if not self._given:
             _bad("MoeLayer.backward_routed: the last forward ran the layer's own router")
+        if T != self._route_out[0].shape[0]:
+            _bad("MoeLayer.backward_routed: the last forward ran another number of tokens")
         assert dout.is_contiguous() and dout.dtype == torch.bfloat16 and dout.shape == (T, s.H)
         dev = hidden.device
         g = {n: torch.empty(shp, dtype=torch.float32, device=dev) for n, shp in private_gradient_shapes(s).items()
@@ -822,7 +824,7 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
         whole = whole and all(map(_contiguous, out))
     if not whole:
         for g, o in zip(grads, grads if out is None else out):
-            if g.stride() != o.stride() or not _dense(g):
+            if g.shape != o.shape or g.stride() != o.stride() or not _dense(g):
                 _bad("clip_grad_norm: a gradient has gaps")
     # pmpe_grad: two pointers, the size, the type in a word of its own
     table = struct.pack(f"{4 * n}q", *itertools.chain.from_iterable(zip(at, to, sizes, codes)))

@@ -130,7 +130,9 @@ def test_refusals(pmpe):
                 dict(grads=[a.double()]), dict(grads=[a.cpu()]), dict(grads=[a, b.cpu()]), dict(grads=[a], out=[b]),
                 dict(grads=[a], out=[]), dict(grads=[a], out=[a.half()]), dict(grads=[a], max_norm=-1.0),
                 dict(grads=[a], max_norm=float("nan")), dict(grads=[a], out=[torch.empty_like(a.t())]),
-                dict(grads=[a, b], out=[torch.empty_like(a), a[0]])):
+                dict(grads=[a, b], out=[torch.empty_like(a), a[0]]),
+                # as many elements and the same strides, but not one run of memory
+                dict(grads=[a[:2, :3].contiguous().t().as_strided((2, 3), (1, 2))], out=[b.as_strided((3, 2), (1, 2))])):
         with pytest.raises(pmpe.PmpeError):
             pmpe.clip_grad_norm(**dict(dict(max_norm=1.0), **bad))
 
@@ -160,3 +162,16 @@ def test_other_stream_and_two_graphs(pmpe):
         torch.cuda.synchronize()
         assert torch.equal(n1, na) and torch.equal(n2, nb)
         assert all(torch.equal(a, b) for a, b in zip(outs[0] + outs[1], want + want2))
+
+
+def test_more_than_2_to_31_elements(pmpe):
+    """Offsets past 32 bits, in a tensor that is not aligned to a vector."""
+    n = 2 ** 31 + 1001
+    g = torch.empty(n + 3, dtype=BF16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))[3:]
+    edges = [g[:1000].clone(), g[-3000:].clone()]
+    want = sum(float(g[i:i + 2 ** 28].double().square().sum()) for i in range(0, n, 2 ** 28)) ** 0.5
+    norm = pmpe.clip_grad_norm([g], 0.5 * want)
+    assert abs(float(norm) - want) <= REL * want
+    for got, was in zip((g[:1000], g[-3000:]), edges):
+        r = was.double() * 0.5
+        assert ((got.double() - r).abs() <= (2.0 ** -8 + REL) * r.abs()).all()
