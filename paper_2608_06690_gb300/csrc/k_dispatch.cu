@@ -163,11 +163,11 @@ __global__ void __launch_bounds__(kAdoptTile) adopt_route_kernel(const AdoptPara
         bool refused = false;
         int missing = 0;
         for (int j = 0; j < p.k; ++j) {
-            const int e = p.idx_in[at + j], local = e - base;
+            const int e = p.idx_in[at + j];  // any value
             // this thread alone sets its bit
-            const bool in_pool = local >= 0 && local < pool, taken = in_pool && (s_mask[base + local][word] & bit);
+            const bool in_pool = e >= base && e < base + pool, taken = in_pool && (s_mask[e][word] & bit);
             if (in_pool && !taken) {
-                atomicOr(&s_mask[base + local][word], bit);
+                atomicOr(&s_mask[e][word], bit);
                 p.idx[at + j] = e;
                 p.w[at + j] = p.w_in[at + j];
             } else {

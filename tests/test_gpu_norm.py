@@ -269,3 +269,26 @@ def test_arguments_freed_while_the_other_stream_has_yet_to_run(pmpe):
     s.synchronize()
     torch.cuda.synchronize()
     assert torch.equal(y, want) and all((o == 7).all() for o in other)
+
+
+def test_more_than_2_to_31_elements(pmpe):
+    """Offsets past 32 bits: the last rows are those of a call on them alone."""
+    T, H = 140000, 16384
+    x = torch.empty((T, H), dtype=BF16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    w = randn((H,), 2, F32)
+    few = x[-5:].clone()
+    n, m = pmpe.rms_norm(x, w, residual=x), pmpe.rms_norm(few, w, residual=few)
+    q, r = pmpe.rms_norm(x, w, quant="block"), pmpe.rms_norm(few, w, quant="block")
+    for a, b in ((n.y, m.y), (n.h, m.h), (n.rstd, m.rstd), (q.y.view(torch.uint8), r.y.view(torch.uint8)), (q.scale, r.scale)):
+        assert torch.equal(a[-5:], b)
+    del q
+    dx, dw = pmpe.rms_norm_backward(x, n.h, w, n.rstd, d_h=x)
+    small, _ = pmpe.rms_norm_backward(few, m.h, w, m.rstd, d_h=few)
+    assert torch.equal(dx[-5:], small)
+    want, size = torch.zeros(H, dtype=torch.float64, device="cuda"), torch.zeros(H, dtype=torch.float64, device="cuda")
+    for t in range(0, T, 10000):
+        part = x[t:t + 10000].double() * n.h[t:t + 10000].double() * n.rstd[t:t + 10000, None].double()
+        want += part.sum(0)
+        size += part.abs().sum(0)
+    # a CTA's rows in sequence (140000 / 152), five sums of the CTAs' and the strands' tree
+    assert ((dw.double() - want).abs() <= (140000 / 152 + 20) * 2.0 ** -24 * size).all()

@@ -85,7 +85,7 @@ def test_picks_that_cannot_be_taken():
     def lowest_free(row, base, n, used):
         return next(e for e in range(base, base + n) if e not in row and e not in used)
 
-    edits = {t_deny: [(0, shape.E_pub), (2, 10 ** 9)],   # a private expert for a DENY token, and no expert at all
+    edits = {t_deny: [(0, shape.E_pub), (2, 10 ** 9), (3, -2 ** 31)],   # a private expert for a DENY token, and no expert at all
              t_allow: [(1, 0), (3, -5)]}                 # a public one for an ALLOW token
     twice = int(torch.nonzero(~allow)[1])
     edits[twice] = [(1, int(idx[twice, 0]))]             # the same expert twice
@@ -138,6 +138,8 @@ def test_refusals_and_the_empty_batch():
     with pytest.raises(pmpe.PmpeError):
         layer.backward_routed(h, pol, dout)  # the last forward ran the layer's own router
     layer.forward(h, pol, route=(idx, w))
+    with pytest.raises(pmpe.PmpeError):
+        layer.backward_routed(h[:5], pol[:5], dout[:5])  # another number of tokens than the forward's
     for back in (layer.backward, layer.backward_private, layer.backward_input):
         with pytest.raises(pmpe.PmpeError):
             back(h, pol, dout)
