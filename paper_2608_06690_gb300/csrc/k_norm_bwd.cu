@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(32 * kStrands) rms_norm_dw_kernel(const float 
 }
 
 // Threads of a CTA, and the CTAs that an SM holds: 768 threads at 80 registers
-// (T = 4096, 2048 columns, BF16 with an FP32 dy: 18.6 us, with 512 19.9, with
+// (T = 4096, 2048 columns, BF16 with an FP32 dy: 18.6 us (18.1 now), with 512 19.9, with
 // 1024 at 64 registers 21.3); wider rows' kernels take about 96, from 6145
 // columns on, with 16 columns a thread, 128.  A grid beyond them would run its
 // last CTAs in a second wave.  (T = 3276, 5120 columns, BF16: 32.4 us with 8
