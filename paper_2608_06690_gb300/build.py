@@ -1,6 +1,7 @@
 """Build libpmpe.so in-tree with nvcc for sm_103a (no cmake, no torch
 extension machinery): each .cu under csrc/ compiles to an object in
-parallel, then one shared-library link."""
+parallel, then one shared-library link.  Beside it the Python module _ops
+(csrc/bind_ops.cpp) with g++ against the headers of the installed PyTorch."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -9,11 +10,13 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libpmpe.so")
+OPS_SRC, OPS_OUT = os.path.join(CSRC, "bind_ops.cpp"), os.path.join(PKG, "_ops.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
@@ -37,6 +40,23 @@ def _stale(target: str, deps) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _ops_command():
+    """The command that builds _ops.so, and what it is built for."""
+    import torch
+    cxx = shutil.which("g++") or "g++"
+    home = os.path.dirname(torch.__file__)
+    include = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+               os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include"), sysconfig.get_paths()["include"]]
+    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-Wall", "-fvisibility=hidden", "-shared",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include")]
+    for d in include:
+        cmd += ["-isystem", d]
+    # PyTorch's libraries are in the process by the time the module is loaded
+    cmd += [OPS_SRC, "-o", OPS_OUT + ".tmp", "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cuda", "-ltorch_cpu",
+            "-lc10_cuda", "-lc10"]
+    return cmd, f"{torch.__version__} {sys.version}\n"
+
+
 def build(verbose: bool = False, force: bool = False, ptxas_info: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     nvcc = _nvcc()
@@ -51,6 +71,13 @@ def build(verbose: bool = False, force: bool = False, ptxas_info: bool = False) 
             cmd = [nvcc] + _flags() + (["-Xptxas", "-v"] if ptxas_info else []) + ["-c", src, "-o", obj]
             jobs.append(cmd)
 
+    ops_cmd, built_for = _ops_command()
+    stamp = os.path.join(BUILD_DIR, "_ops.txt")
+    ops = force or _stale(OPS_OUT, [OPS_SRC, os.path.join(ROOT, "include", "pmpe.h")]) or not os.path.exists(stamp) or \
+        open(stamp).read() != built_for
+    if ops:
+        jobs.insert(0, ops_cmd)
+
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
         return cmd, r
@@ -60,8 +87,12 @@ def build(verbose: bool = False, force: bool = False, ptxas_info: bool = False) 
             if verbose or ptxas_info or r.returncode != 0:
                 sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
             if r.returncode != 0:
-                raise RuntimeError(f"nvcc failed on {cmd[-3]}")
-    if force or jobs or _stale(OUT, objs):
+                raise RuntimeError("building _ops.so failed" if cmd is ops_cmd else f"nvcc failed on {cmd[-3]}")
+    if ops:
+        os.replace(OPS_OUT + ".tmp", OPS_OUT)
+        with open(stamp, "w") as f:
+            f.write(built_for)
+    if force or _stale(OUT, objs):
         cmd = [nvcc] + ARCH + ["-shared", "-o", OUT + ".tmp"] + objs
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:

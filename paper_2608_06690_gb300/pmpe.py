@@ -1,16 +1,14 @@
-"""ctypes binding over libpmpe.so (the C ABI of include/pmpe.h).
+"""Binding over libpmpe.so (the C ABI of include/pmpe.h): ctypes for the layer,
+the module _ops for the operators around it.
 
-Argument marshalling only: every step of the layer runs in the library's
-CUDA kernels.  PyTorch supplies device memory and streams.  If the library
+Argument marshalling only: every step runs in the library's CUDA kernels.  PyTorch supplies device memory and streams.  If the library
 has not been built this module raises on import -- there is no fallback.
 """
 from __future__ import annotations
 
 import ctypes
-import itertools
-import operator
+import importlib
 import os
-import struct
 from typing import NamedTuple
 
 import numpy as np
@@ -21,10 +19,14 @@ from .inputs import LayerShape
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpmpe.so")
 
-if not os.path.exists(LIB_PATH):
-    raise ImportError(f"{LIB_PATH} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
+OPS_PATH = os.path.join(_HERE, "_ops.so")
+
+for _path in (LIB_PATH, OPS_PATH):
+    if not os.path.exists(_path):
+        raise ImportError(f"{_path} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
 
 _lib = ctypes.CDLL(LIB_PATH)
+_ops = importlib.import_module("._ops", __package__)
 
 OK = 0
 ERR_INVALID_ARG = -1
@@ -516,83 +518,32 @@ class MoeLayer:
 
 # ------------------------------------------- operators around the layer
 #
-# A call's host time counts as much as its kernel's at decode sizes (1.7 us of
-# kernel), so the checks below are plain comparisons, descriptors are packed
-# as bytes in the C structs' layout, and the stream's handle and the outputs'
-# memory are taken without PyTorch's dispatcher: 8 us a norm on a Grace core,
-# where ctypes structures, torch.cuda.current_stream() and torch.empty() made
-# it 20.
+# Checks, outputs and launches are in _ops (csrc/bind_ops.cpp): a call's host
+# time counts as much as its kernel's at decode sizes.
 
-_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-_QUANT = {None: 0, "block": 1, "row": 2}
 QUANT_BLOCK = 128  # columns that share a scale with quant="block"
-_F32 = torch.float32
-
-_pack_norm = struct.Struct("@5if3P2q4P").pack
-_pack_norm_bwd = struct.Struct("@6i8PN").pack
-_pack_route = struct.Struct("@12ifPq5P").pack
-
-_dtype_of = operator.attrgetter("dtype")
-_device_of, _numel_of, _address_of, _contiguous = (torch.Tensor.get_device, torch.Tensor.numel, torch.Tensor.data_ptr,
-                                                   torch.Tensor.is_contiguous)
-
-_device = torch._C._cuda_getDevice               # the current device's index
-_raw_stream = torch._C._cuda_getCurrentRawStream  # its current stream's handle
-
-
-def _empty_strided(size, stride, dtype):
-    return torch.empty_strided(size, stride, dtype=dtype, device="cuda")
-
-
-# Memory on the current device, as PyTorch's own compiled code takes it: 0.8 us
-# where torch.empty takes 1.4, and the launch after it 2.5 where it takes 5 (the
-# dispatcher's code is not run between launches).
-try:
-    from torch._C._dynamo.guards import _empty_strided_cuda as _empty
-except ImportError:
-    _empty = _empty_strided
 
 
 def _bad(what: str):
     raise PmpeError(ERR_INVALID_ARG, what)
 
 
-def _elsewhere(fn, t, stream, *args, **kw):
-    """The call again on ``stream``, or on the tensor's device: outputs and
-    scratch are allocated where the kernels run, so that the caching allocator
-    reuses them in order, and the arguments' memory is not reused before the
-    stream is done with it.  (The caller orders the streams' work.)"""
+def _on(stream, fn, t, *args):
+    """The call on ``stream``: outputs and scratch are allocated there, so that
+    the caching allocator reuses them in order, and the arguments' memory is
+    not reused before the stream is done with it.  (The caller orders the
+    streams' work.)"""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _bad(f"{fn.__name__}: CUDA tensors are wanted")
-    if stream is not None:
-        if stream.device != t.device:
-            _bad(f"{fn.__name__}: the stream is of another device than the tensors")
-        with torch.cuda.stream(stream):
-            result = fn(*args, **kw)
-        for a in args:
-            for v in a if isinstance(a, (list, tuple)) else (a,):
-                if isinstance(v, torch.Tensor):
-                    v.record_stream(stream)
-        return result
-    with torch.cuda.device(t.device):
-        return fn(*args, **kw)
-
-
-def _at(t):
-    return 0 if t is None else t.data_ptr()
-
-
-def _pitch(t) -> int:
-    """Elements from a row to the next (any value serves a single row); -1,
-    which the library refuses, where a row's elements are not adjacent."""
-    rows, cols = t.shape
-    if cols != 1 and t.stride(1) != 1:
-        return -1
-    return t.stride(0) if rows > 1 else cols
-
-
-def _vector(t, n: int, dev: int, dtype) -> bool:
-    return t.dtype is dtype and t.dim() == 1 and t.numel() == n and t.get_device() == dev and t.is_contiguous()
+    if stream.device != t.device:
+        _bad(f"{fn.__name__}: the stream is of another device than the tensors")
+    with torch.cuda.stream(stream):
+        result = fn(*args)
+    for a in args:
+        for v in a if isinstance(a, (list, tuple)) else (a,):
+            if isinstance(v, torch.Tensor):
+                v.record_stream(stream)
+    return result
 
 
 def _matrix(t, rows: int, cols: int, dev: int, dtype) -> bool:
@@ -618,50 +569,9 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-6, quant=None, h_out=None
     (y stands for ``y.float() * scale``).  ``h_out``: where h goes (may be
     ``residual`` or ``x``).  ``stream``: the stream to run on (default: the
     current one).  H up to 16384, eps at least 1e-20."""
-    dev = x.get_device()
-    if stream is not None or dev < 0 or dev != _device():
-        return _elsewhere(rms_norm, x, stream, x, weight, residual, eps, quant, h_out)
-    dt = x.dtype
-    code = _TYPES.get(dt, -1)
-    if code < 0 or x.dim() != 2:
-        _bad("rms_norm: x is [T, H] of FP32, BF16 or FP16")
-    T, H = x.shape
-    plain = x.is_contiguous()
-    if quant not in _QUANT:
-        _bad('rms_norm: quant is None, "block" or "row"')
-    w_code = code
-    if not _vector(weight, H, dev, dt):
-        w_code = 0
-        if not _vector(weight, H, dev, _F32):
-            _bad("rms_norm: weight is [H] of x's type or FP32, on x's device")
-    h, h_at, res_at, res_ld = x, 0, 0, 0
-    if residual is not None:
-        if residual.dtype is not dt or residual.get_device() != dev or residual.shape != x.shape:
-            _bad("rms_norm: residual is as x")
-        res_at, res_ld = residual.data_ptr(), H if residual.is_contiguous() else _pitch(residual)
-        if h_out is None:
-            h = _empty((T, H), (H, 1), dt)
-        elif _matrix(h_out, T, H, dev, dt):
-            h = h_out
-        else:
-            _bad("rms_norm: h_out is [T, H] of x's type without gaps")
-        h_at = h.data_ptr()
-    elif h_out is not None:
-        _bad("rms_norm: without a residual h is x")
-    scale = None
-    if quant is not None:
-        y = _empty((T, H), (H, 1), torch.float8_e4m3fn)
-        blocks = -(-H // QUANT_BLOCK) if quant == "block" else 1
-        scale = _empty((T, blocks), (blocks, 1), _F32)
-    else:
-        y = _empty((T, H), (H, 1), dt)
-    rstd = _empty((T,), (1,), _F32)
-    rc = _lib.pmpe_rms_norm(_pack_norm(T, H, code, w_code, _QUANT[quant], eps, x.data_ptr(), res_at, weight.data_ptr(),
-                                       H if plain else _pitch(x), res_ld, h_at, y.data_ptr(), _at(scale), rstd.data_ptr()),
-                            _raw_stream(dev))
-    if rc:
-        _check(rc, "pmpe_rms_norm")
-    return RmsNorm(y, scale, h, rstd)
+    if stream is not None:
+        return _on(stream, rms_norm, x, x, weight, residual, eps, quant, h_out)
+    return _ops.rms_norm(x, weight, residual, eps, quant, h_out)
 
 
 def rms_norm_backward(dy, h, weight, rstd, d_h=None, dx_dtype=None, need_dw: bool = True, stream=None):
@@ -672,42 +582,9 @@ def rms_norm_backward(dy, h, weight, rstd, d_h=None, dx_dtype=None, need_dw: boo
     d_h: the gradient that reaches h itself, of dx's type.  ``dx_dtype``: h's
     type (default) or FP32.  Matrices without gaps.  An 8-bit y passes its
     gradient as the identity."""
-    dev = h.get_device()
-    if stream is not None or dev < 0 or dev != _device():
-        return _elsewhere(rms_norm_backward, h, stream, dy, h, weight, rstd, d_h, dx_dtype, need_dw)
-    dt = h.dtype
-    code = _TYPES.get(dt, -1)
-    if code < 0 or h.dim() != 2 or not h.is_contiguous():
-        _bad("rms_norm_backward: h is [T, H] of FP32, BF16 or FP16 without gaps")
-    T, H = h.shape
-    xt = dt if dx_dtype is None else dx_dtype
-    if xt is not dt and xt is not _F32:
-        _bad("rms_norm_backward: dx is of h's type or FP32")
-    gt = dy.dtype
-    if gt is not dt and gt is not _F32 or not _matrix(dy, T, H, dev, gt):
-        _bad("rms_norm_backward: dy is [T, H] of h's type or FP32 without gaps")
-    w_code = code
-    if not _vector(weight, H, dev, dt):
-        w_code = 0
-        if not _vector(weight, H, dev, _F32):
-            _bad("rms_norm_backward: weight is [H] of h's type or FP32")
-    if not _vector(rstd, T, dev, _F32):
-        _bad("rms_norm_backward: rstd is FP32 [T]")
-    if d_h is not None and not _matrix(d_h, T, H, dev, xt):
-        _bad("rms_norm_backward: d_h is [T, H] of dx's type without gaps")
-    dx = _empty((T, H), (H, 1), xt)
-    dw = ws = None
-    nb = 0
-    if need_dw:
-        nb = _lib.pmpe_rms_norm_backward_workspace_size(T, H)
-        dw = _empty((H,), (1,), _F32)
-        ws = _empty((nb,), (1,), torch.uint8)
-    rc = _lib.pmpe_rms_norm_backward(
-        _pack_norm_bwd(T, H, code, w_code, _TYPES[gt], _TYPES[xt], dy.data_ptr(), h.data_ptr(), weight.data_ptr(),
-                       rstd.data_ptr(), _at(d_h), dx.data_ptr(), _at(dw), _at(ws), nb), _raw_stream(dev))
-    if rc:
-        _check(rc, "pmpe_rms_norm_backward")
-    return dx, dw
+    if stream is not None:
+        return _on(stream, rms_norm_backward, h, dy, h, weight, rstd, d_h, dx_dtype, need_dw)
+    return _ops.rms_norm_backward(dy, h, weight, rstd, d_h, dx_dtype, need_dw)
 
 
 class Router:
@@ -727,18 +604,9 @@ class Router:
         if group_score not in ("max", "top2"):
             _bad('Router: group_score is "max" or "top2"')
         self.E_pub, self.E_priv, self.k, self.E = int(E_pub), int(E_priv), int(k), int(E_pub) + int(E_priv)
-        self._config = (int(score == "sigmoid"), int(bool(renormalize)), int(groups[0]), int(groups[1]), int(groups_priv[0]),
-                        int(groups_priv[1]), int(group_score == "top2"), float(scale))
         # refuses what the library would refuse, before the first call
-        _check(_lib.pmpe_route(_pack_route(0, self.E_pub, self.E_priv, self.k, 0, *self._config, 0, self.E, 0, 0, 0, 0, 0), None),
-               "pmpe_route")
-
-    def _logits(self, logits):
-        """(type, rows, pitch) of the logits."""
-        code = _TYPES.get(logits.dtype, -1)
-        if code < 0 or logits.dim() != 2 or logits.shape[1] != self.E:
-            _bad("Router: logits are [T, E] of FP32, BF16 or FP16")
-        return code, logits.shape[0], self.E if logits.is_contiguous() else _pitch(logits)
+        self._desc = _ops.router(self.E_pub, self.E_priv, self.k, int(score == "sigmoid"), int(bool(renormalize)), int(groups[0]),
+                                 int(groups[1]), int(groups_priv[0]), int(groups_priv[1]), int(group_score == "top2"), float(scale))
 
     def route(self, logits, policy=None, bias=None, load=None, stream=None):
         """(idx, w): the k chosen experts of each token (int32 [T, k], global
@@ -749,43 +617,16 @@ class Router:
         private pool (None: all public).  bias: FP32 [E], added to the scores
         for the choice alone.  load: int32 [E], to which the tokens of each
         expert are added (for the bias's update)."""
-        dev = logits.get_device()
-        if stream is not None or dev < 0 or dev != _device():
-            return _elsewhere(self.route, logits, stream, logits, policy, bias, load)
-        code, T, ld = self._logits(logits)
-        if policy is not None and not _vector(policy, T, dev, torch.uint8):
-            _bad("Router: policy is uint8 [T] on the logits' device")
-        if bias is not None and not _vector(bias, self.E, dev, _F32):
-            _bad("Router: bias is FP32 [E] on the logits' device")
-        if load is not None and not _vector(load, self.E, dev, torch.int32):
-            _bad("Router: load is int32 [E] on the logits' device")
-        idx, w = _empty((T, self.k), (self.k, 1), torch.int32), _empty((T, self.k), (self.k, 1), _F32)
-        rc = _lib.pmpe_route(_pack_route(T, self.E_pub, self.E_priv, self.k, code, *self._config, logits.data_ptr(), ld, _at(policy),
-                                         _at(bias), idx.data_ptr(), w.data_ptr(), _at(load)), _raw_stream(dev))
-        if rc:
-            _check(rc, "pmpe_route")
-        return idx, w
+        if stream is not None:
+            return _on(stream, self.route, logits, logits, policy, bias, load)
+        return _ops.route(self._desc, logits, policy, bias, load)
 
     def backward(self, logits, policy, idx, dw, stream=None):
         """The gradient of the logits ([T, E], their type) from that of the
         weights (FP32 [T, k]) for the selection ``idx``."""
-        dev = logits.get_device()
-        if stream is not None or dev < 0 or dev != _device():
-            return _elsewhere(self.backward, logits, stream, logits, policy, idx, dw)
-        code, T, ld = self._logits(logits)
-        if policy is not None and not _vector(policy, T, dev, torch.uint8):
-            _bad("Router: policy is uint8 [T] on the logits' device")
-        if not _matrix(idx, T, self.k, dev, torch.int32):
-            _bad("Router: idx is int32 [T, k] on the logits' device")
-        if not _matrix(dw, T, self.k, dev, _F32):
-            _bad("Router: dw is FP32 [T, k] on the logits' device")
-        d_logits = _empty((T, self.E), (self.E, 1), logits.dtype)
-        rc = _lib.pmpe_route_backward(_pack_route(T, self.E_pub, self.E_priv, self.k, code, *self._config, logits.data_ptr(), ld,
-                                                  _at(policy), 0, idx.data_ptr(), 0, 0), dw.data_ptr(), d_logits.data_ptr(),
-                                      _raw_stream(dev))
-        if rc:
-            _check(rc, "pmpe_route_backward")
-        return d_logits
+        if stream is not None:
+            return _on(stream, self.backward, logits, logits, policy, idx, dw)
+        return _ops.route_backward(self._desc, logits, policy, idx, dw)
 
 
 def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
@@ -802,45 +643,11 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
                 _bad("clip_grad_norm: out is as grads")
             out = [out[n] for n in grads]
         grads = list(grads.values())
-    n = len(grads)
-    if n == 0 or out is not None and len(out) != n:
-        _bad("clip_grad_norm: gradients, and an output for each or none, are wanted")
-    first = grads[0]
-    dev = first.get_device()
-    if stream is not None or dev < 0 or dev != _device():
-        return _elsewhere(clip_grad_norm, first, stream, grads, max_norm, out)
-    # one attribute of all tensors at a time: 0.4 us a tensor, where a loop over them took 0.9
-    codes = list(map(_TYPES.get, map(_dtype_of, grads)))
-    if None in codes or set(map(_device_of, grads)) != {dev}:
-        _bad("clip_grad_norm: gradients are FP32, BF16 or FP16 tensors of one device")
-    sizes, at = list(map(_numel_of, grads)), list(map(_address_of, grads))
-    to = at
-    whole = all(map(_contiguous, grads))
-    if out is not None:
-        if set(map(_device_of, out)) != {dev} or list(map(_TYPES.get, map(_dtype_of, out))) != codes or \
-                list(map(_numel_of, out)) != sizes:
-            _bad("clip_grad_norm: outputs are of their gradients' types and sizes")
-        to = list(map(_address_of, out))
-        whole = whole and all(map(_contiguous, out))
-    if not whole:
-        for g, o in zip(grads, grads if out is None else out):
-            if g.shape != o.shape or g.stride() != o.stride() or not _dense(g):
-                _bad("clip_grad_norm: a gradient has gaps")
-    # pmpe_grad: two pointers, the size, the type in a word of its own
-    table = struct.pack(f"{4 * n}q", *itertools.chain.from_iterable(zip(at, to, sizes, codes)))
-    nb = _lib.pmpe_clip_workspace_size(n)
-    norm, ws = _empty((), (), _F32), _empty((nb,), (1,), torch.uint8)
-    rc = _lib.pmpe_clip_grad_norm(table, n, max_norm, norm.data_ptr(), ws.data_ptr(), nb, _raw_stream(dev))
-    if rc:
-        _check(rc, "pmpe_clip_grad_norm")
-    return norm
+    if stream is not None:
+        return _on(stream, clip_grad_norm, grads[0] if len(grads) else None, grads, max_norm, out)
+    return _ops.clip_grad_norm(grads, max_norm, out)
 
 
-def _dense(t) -> bool:
-    """Whether the tensor's elements fill a run of memory, in some order."""
-    want = 1
-    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
-        if stride != want:
-            return False
-        want *= size
-    return True
+_ops.setup(PmpeError, RmsNorm, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
+    "pmpe_rms_norm", "pmpe_rms_norm_backward_workspace_size", "pmpe_rms_norm_backward", "pmpe_route", "pmpe_route_backward",
+    "pmpe_clip_workspace_size", "pmpe_clip_grad_norm")))

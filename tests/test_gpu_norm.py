@@ -271,6 +271,30 @@ def test_arguments_freed_while_the_other_stream_has_yet_to_run(pmpe):
     assert torch.equal(y, want) and all((o == 7).all() for o in other)
 
 
+def test_two_threads_at_once(pmpe):
+    """Calls of two threads, a stream each, do not disturb one another."""
+    import threading
+    x = [randn((64, 2048), i, BF16) for i in range(2)]
+    w = randn((2048,), 3, BF16)
+    want = [pmpe.rms_norm(v, w, residual=v).y for v in x]
+    torch.cuda.synchronize()
+    same = [False, False]
+
+    def work(i):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            got = [pmpe.rms_norm(x[i], w, residual=x[i]).y for _ in range(300)]
+        s.synchronize()
+        same[i] = all(torch.equal(g, want[i]) for g in got)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert same == [True, True]
+
+
 def test_more_than_2_to_31_elements(pmpe):
     """Offsets past 32 bits: the last rows are those of a call on them alone."""
     T, H = 140000, 16384

@@ -55,18 +55,6 @@ def desc(cls, base, **over):
     return ctypes.byref(d)
 
 
-def test_packed_descriptors_match_the_structures(pmpe):
-    """The binding packs the descriptors as bytes: every field at its place."""
-    for cls, pack in ((RmsNormDesc, pmpe._pack_norm), (RmsNormBackwardDesc, pmpe._pack_norm_bwd), (RouteDesc, pmpe._pack_route)):
-        values = [i + 1 for i in range(len(cls._fields_))]
-        raw = pack(*values)
-        assert len(raw) == ctypes.sizeof(cls)
-        d = cls.from_buffer_copy(raw)
-        assert [getattr(d, n) for n, _ in cls._fields_] == values
-    assert ctypes.sizeof(Grad) == 32  # four 64-bit words, the type in the last one's low half
-    assert Grad.from_buffer_copy(np.array([1, 2, 3, 2], np.int64)).type == 2
-
-
 def test_rms_norm_refusals(pmpe):
     f = pmpe._lib.pmpe_rms_norm
     base = dict(T=4, H=256, type=1, weight_type=1, quant=0, eps=1e-6, x=P, residual=P, weight=P, x_ld=256, residual_ld=256,
@@ -191,6 +179,24 @@ def test_host_tensors_are_refused(pmpe):
                  lambda: pmpe.Router(8, 0, 2).route(x), lambda: pmpe.clip_grad_norm([x], 1.0), lambda: pmpe.clip_grad_norm([], 1.0),
                  lambda: pmpe.clip_grad_norm({"a": x}, 1.0, out={"b": x})):
         with pytest.raises(pmpe.PmpeError):
+            call()
+
+
+def test_arguments_of_other_types_are_refused(pmpe):
+    """Nothing but tensors reaches a tensor's place, and errors of Python's own
+    conversions come through as they are."""
+    x, w, r = torch.zeros(2, 8), torch.ones(8), pmpe.Router(8, 0, 2)
+    for call in (lambda: pmpe.rms_norm(None, w), lambda: pmpe.rms_norm(x, 1.0), lambda: pmpe.rms_norm(x, w, residual=[x]),
+                 lambda: pmpe.rms_norm(x, w, quant="tensor"), lambda: pmpe.rms_norm(x, w, quant=1), lambda: pmpe.rms_norm(x, w, h_out="h"),
+                 lambda: pmpe.rms_norm_backward(x, None, w, w), lambda: pmpe.rms_norm_backward(x, x, w, w, d_h=0),
+                 lambda: r.route([[0.0] * 8]), lambda: r.route(x, policy=1), lambda: r.route(x, load={}), lambda: r.backward(x, None, None, x),
+                 lambda: pmpe.clip_grad_norm(x, 1.0), lambda: pmpe.clip_grad_norm([None], 1.0), lambda: pmpe.clip_grad_norm([x], 1.0, out=x),
+                 lambda: pmpe.clip_grad_norm(iter([x]), 1.0), lambda: pmpe._ops.rms_norm(x, w), lambda: pmpe._ops.route(b"", x, None, None, None),
+                 lambda: pmpe._ops.route_backward(r._desc)):
+        with pytest.raises(pmpe.PmpeError):
+            call()
+    for call in (lambda: pmpe.rms_norm(x, w, eps="small"), lambda: pmpe.clip_grad_norm([x], "1"), lambda: pmpe.Router(8, 0, "two")):
+        with pytest.raises((TypeError, ValueError)):
             call()
 
 
