@@ -4,8 +4,9 @@
 // device.  pmpe.py holds the public functions, their defaults and documents.
 //
 // Why C++: at decode sizes a call is its host time (1.75 us of kernel for one
-// token's norm).  Checks, three allocations and the launch take 8 us a call
-// from Python through ctypes on a Grace core, 4.4 us from here.
+// token's norm).  Checks, three allocations and the launch took 8 us in a loop
+// of calls from Python through ctypes on a Grace core, 4.4 us from here;
+// clipping four tensors 19.8 and 7.9 us.
 #include <Python.h>
 
 #include <algorithm>
