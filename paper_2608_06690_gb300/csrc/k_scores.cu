@@ -586,18 +586,27 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
         float D = 0.f, zj = kNone;
         if (lane < p.k) {
             e = p.idx[(long long)t * p.k + lane];  // any value
-            e = e >= base && e < base + E ? e - base : -1;
-            if (e >= 0) {
-                zj = to_f32(row[e]);
-                if (zj > kNone) D = p.dw[(long long)t * p.k + lane] * p.scale;
-                else e = -1;  // never chosen
-                zj = fminf(zj, kLargest);
-            }
+            D = p.dw[(long long)t * p.k + lane] * p.scale;
         }
+        // the whole row at once, beside the ids, not the picks' logits after them (4.08 us, so 3.9)
+        float z[kV];
+        load_logits<T, kV>(z, row, lane, E, ((uintptr_t)row & (sizeof(T) * kV - 1)) == 0);
+        e = e >= base && e < base + E ? e - base : -1;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {  // a pick's logit from the lane that holds it
+            const float o = __shfl_sync(~0u, z[i], max(e, 0) / kV);
+            if (e >= 0 && e % kV == i) zj = o;
+        }
+        if (!(zj > kNone)) e = -1;  // never chosen
+        if (e < 0) D = 0.f;
+        zj = e >= 0 ? fminf(zj, kLargest) : kNone;
         const bool mine = e >= 0;
         float g = 0.f;  // what lane j adds to its expert's gradient
         float d[kV];
         const bool dense = !p.sigmoid && !p.renorm;
+        // the other pool's logits have no gradient
+        const int other = priv ? 0 : p.E_pub, n_other = priv ? p.E_pub : p.E_priv;
+        for (int i = lane; i < n_other; i += 32) out[other + i] = from_f32<T>(0.f);
         if (p.sigmoid) {
             const float s = mine ? 1.f / (1.f + expf(-zj)) : 0.f;
             float ds = D;
@@ -618,8 +627,6 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
 #pragma unroll
         for (int i = 0; i < kV; ++i) d[i] = 0.f;
         if (dense) {
-            float z[kV];
-            load_logits<T, kV>(z, row, lane, E, ((uintptr_t)row & (sizeof(T) * kV - 1)) == 0);
             float mx = kNone, sum = 0.f;
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
@@ -658,9 +665,6 @@ template <typename T, int kV> __global__ void __launch_bounds__(32 * kRouteWarps
             for (int i = 0; i < kV; ++i)
                 if (lane * kV + i < E) o[i] = from_f32<T>(d[i]);
         }
-        // the other pool's logits have no gradient
-        const int other = priv ? 0 : p.E_pub, n_other = priv ? p.E_pub : p.E_priv;
-        for (int i = lane; i < n_other; i += 32) out[other + i] = from_f32<T>(0.f);
     }
 }
 
