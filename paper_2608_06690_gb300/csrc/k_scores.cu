@@ -210,14 +210,14 @@ __device__ __forceinline__ auto group_value(const K (&key)[kV], int n, int size,
 }
 
 // Lane j's weight of its pick: z its logit, s its score where `scored`.  mine:
-// there is a pick.
-__device__ __forceinline__ float weight_of(bool mine, float z, float s, int sigmoid, int renorm)
+// there is a pick.  ordered: lane 0's logit is the largest.
+__device__ __forceinline__ float weight_of(bool mine, float z, float s, int sigmoid, int renorm, bool ordered)
 {
     float w = mine ? s : 0.f;
     if (renorm && sigmoid) {
         w = w / (warp_sum(w) + 1e-20f);
     } else if (renorm) {  // softmax over the k
-        const float m = of(__reduce_max_sync(~0u, key_of(mine ? z : kNone)));
+        const float m = ordered ? __shfl_sync(~0u, z, 0) : of(__reduce_max_sync(~0u, key_of(mine ? z : kNone)));
         w = mine ? expf(z - m) : 0.f;
         const float total = warp_sum(w);
         if (mine) w = w / total;
@@ -311,7 +311,7 @@ __device__ __noinline__ void select_exactly(const ScoreParams &p, const Aside &a
         const bool mine = lane < p.k && pick >= 0;
         const float zj = mine ? logit(pool, pick) : kNone, sum32 = (float)sum;
         const float sj = !mine ? 0.f : p.sigmoid ? 1.f / (1.f + expf(-zj)) : expf(zj - mx) / sum32;
-        const float w = weight_of(mine, zj, sj, p.sigmoid, p.renorm);
+        const float w = weight_of(mine, zj, sj, p.sigmoid, p.renorm, false);
         if (lane < p.k) {
             p.idx[(long long)t * p.k + lane] = mine ? base + pick : -1;
             p.w[(long long)t * p.k + lane] = w * p.scale;
@@ -379,7 +379,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
         }
         float z[kV];  // -inf: not eligible
 #pragma unroll
-        for (int i = 0; i < kV; ++i) z[i] = z_next[i] > kNone ? fminf(z_next[i], kLargest) : kNone;
+        for (int i = 0; i < kV; ++i) z[i] = fminf(fmaxf(z_next[i], kNone), kLargest);  // the larger of NaN and -inf is -inf
         fetch(t + step, priv_after);
         priv_next = priv_after;
         priv_after = pool_at(t + 2 * step);
@@ -532,7 +532,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
             continue;
         }
         const bool mine = lane < p.k && e_mine >= 0;
-        const float w = weight_of(mine, zj, sj, p.sigmoid, p.renorm);
+        const float w = weight_of(mine, zj, sj, p.sigmoid, p.renorm, !kBias);
         if (lane < p.k) {
             p.idx[(long long)t * p.k + lane] = mine ? base + e_mine : -1;
             p.w[(long long)t * p.k + lane] = w * p.scale;
@@ -681,13 +681,17 @@ template <typename Go> cudaError_t dispatch(int type, int pool, Go go)
     return by_size(__half());
 }
 
-// CTAs for T tokens: up to eight an SM (prompts: T = 16384, 128 + 32 experts
-// 8.2 us, with four 12.4), and not more than kMostTokens tokens each.
+// CTAs for T tokens: up to per_sm an SM, and not more than kMostTokens tokens
+// each.  Eight where a token is short (T = 16384, 128 + 32 experts 8.0 us, with
+// five 8.2); with biases or groups as many as are resident at once, so that no
+// CTA starts late with a token to settle at its end (T = 8192, 256 experts in
+// groups with biases 16.6 us, with eight 17.9; 128 + 32 with biases 14.1, 14.5).
 constexpr int kMostTokens = 1024;
-int grid_of(int T, int num_sms)
+constexpr int kCtasPerSm = 8;
+int grid_of(int T, int num_sms, int per_sm)
 {
     const int all = (T + kRouteWarps - 1) / kRouteWarps;
-    return std::max(1, std::min(all, std::max(8 * num_sms, (T + kMostTokens - 1) / kMostTokens)));
+    return std::max(1, std::min(all, std::max(per_sm * num_sms, (T + kMostTokens - 1) / kMostTokens)));
 }
 
 }  // namespace
@@ -703,7 +707,9 @@ cudaError_t launch_route_scores(const pmpe_route_desc &d, int num_sms, cudaStrea
     p.top_groups[0] = d.top_groups_pub; p.top_groups[1] = d.top_groups_priv;
     p.scale = d.scale;
     const bool limited = d.top_groups_pub < d.groups_pub || (d.E_priv > 0 && d.top_groups_priv < d.groups_priv);
-    const dim3 grid(grid_of(d.T, num_sms)), block(32 * kRouteWarps);
+    // registers: 80 above 128 experts, 64 below
+    const int resident = std::max(d.E_pub, d.E_priv) > 128 ? 3 : 4;
+    const dim3 grid(grid_of(d.T, num_sms, limited || d.bias ? resident : kCtasPerSm)), block(32 * kRouteWarps);
     p.tokens = (d.T + (int)grid.x * kRouteWarps - 1) / ((int)grid.x * kRouteWarps) * kRouteWarps;
     const size_t smem = (limited || d.bias ? p.tokens * sizeof(Aside) : 0) + (d.load ? (d.E_pub + d.E_priv) * sizeof(int) : 0);
     return dispatch(d.logits_type, std::max(d.E_pub, d.E_priv), [&](auto t, auto v) {
@@ -726,7 +732,7 @@ cudaError_t launch_route_scores_backward(const pmpe_route_desc &d, const float *
     p.T = d.T; p.E_pub = d.E_pub; p.E_priv = d.E_priv; p.k = d.k; p.renorm = d.renormalize;
     p.sigmoid = d.score == PMPE_SCORE_SIGMOID;
     p.scale = d.scale;
-    const dim3 grid(grid_of(d.T, num_sms)), block(32 * kRouteWarps);
+    const dim3 grid(grid_of(d.T, num_sms, kCtasPerSm)), block(32 * kRouteWarps);
     return dispatch(d.logits_type, std::max(d.E_pub, d.E_priv), [&](auto t, auto v) {
         return launch_pdl(route_scores_bwd_kernel<decltype(t), decltype(v)::value>, grid, block, 0, st, p);
     });
