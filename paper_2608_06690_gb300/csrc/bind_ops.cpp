@@ -116,7 +116,7 @@ at::Tensor empty(at::Device dev, at::ScalarType type, int64_t rows, int64_t cols
 {
     return at::detail::empty_strided_cuda({rows, cols}, {cols, 1}, type, dev);
 }
-// The library's call, while other threads may run Python.
+// The library's call, which throws nothing, while other threads may run Python.
 template <typename F> void run(const char *what, F f)
 {
     int rc;
@@ -323,8 +323,9 @@ PyObject *route_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         want(is_matrix(dw, d.T, d.k, at.device, at::kFloat), "Router: dw is FP32 [T, k] on the logits' device");
         const at::Tensor d_logits = empty(at.device, logits.scalar_type(), d.T, (int64_t)d.E_pub + d.E_priv);
         d.topk_idx = (int32_t *)idx.data_ptr();
-        run("pmpe_route_backward",
-            [&, s = at.stream()] { return lib_route_backward(&d, (const float *)dw.data_ptr(), d_logits.data_ptr(), s); });
+        run("pmpe_route_backward", [&d, from = (const float *)dw.data_ptr(), to = d_logits.data_ptr(), s = at.stream()] {
+            return lib_route_backward(&d, from, to, s);
+        });
         return THPVariable_Wrap(d_logits);
     });
 }
@@ -381,8 +382,8 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         }
         const size_t bytes = lib_clip_workspace_size((int)n);
         const at::Tensor norm = at::detail::empty_strided_cuda({}, {}, at::kFloat, at.device), ws = empty(at.device, at::kByte, (int64_t)bytes);
-        run("pmpe_clip_grad_norm", [&, s = at.stream()] {
-            return lib_clip_grad_norm(grads.data(), (int)n, narrow(max_norm), (float *)norm.data_ptr(), ws.data_ptr(), bytes, s);
+        run("pmpe_clip_grad_norm", [&, to = (float *)norm.data_ptr(), scratch = ws.data_ptr(), s = at.stream()] {
+            return lib_clip_grad_norm(grads.data(), (int)n, narrow(max_norm), to, scratch, bytes, s);
         });
         return THPVariable_Wrap(norm);
     });
