@@ -385,12 +385,16 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
         priv_after = pool_at(t + 2 * step);
         // The choices come from the fast exponential and quotient, whose error
         // is known: __expf(x) 2 + 1.2 |x| ulp, __fdividef 2 ulp, ulp <= 2^-23.
-        // So a choice c is off by less than err + 2^-24 |c|, a fifth to spare:
-        // sigmoid: the exponential's error enters with s (1 - s), and s (1 - s)
-        // |z| < 0.23: 0.8, the sum 0.5, the quotient 2, 3.3 x 2^-23 in all;
-        // softmax, with d = z - max, |d| p < 0.4 / sum: the exponential (4 + 2.4
-        // |d|) 2^-24, d's rounding 2^-24 |d|, both again in the sum (|d| weighted
-        // by p is at most ln 256), 12 additions: 43 x 2^-24 / sum.
+        // So a choice c is off by F + 2^-24 |c|, and those that expf and a whole
+        // quotient give for the picks by A + 2^-24 |c|, with F + A <= err:
+        // sigmoid, in 2^-23: the exponential's error enters with s (1 - s), and
+        // the sum (0.5) and the quotient (2) with s: F = s (1 - s) (2 + 1.2 |z|)
+        // + 2.5 s < 2.7, A = 2 s (1 - s) + s < 1.2, err 4;
+        // softmax, in 2^-24 / sum, with d = z - max and |d| e^d < 0.4: F = e^d
+        // (4 + 3.4 |d| + 2) < 7.4 (d's rounding with it), A < 5.5, and the sum's
+        // own error, which scales every score alike and so a difference of two
+        // scores by its 4 + 3.4 ln 256 + 12 < 35 (|d| weighted by p is at most
+        // ln 256): err 50.
         float mx = kNone, sum = 1.f, err = 0x1p-21f;
         float val[kV];  // score + bias, where it is needed
         if (!p.sigmoid && (!p.renorm || scored)) {  // the pool's softmax
@@ -487,6 +491,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
         constexpr bool inexact = kBias || sizeof(T) == 4;
         int e_mine, e_next;
         bool whole;
+        float above;  // no choice of the next one's packed word is larger
         {
             uint32_t v[kV], mine;
 #pragma unroll
@@ -494,6 +499,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
             const uint32_t last = pick_packed<kV>(v, inexact ? p.k + 1 : p.k, lane, mine, whole);
             e_mine = mine >= kLeast ? 255 - (int)(mine & 255u) : -1;
             e_next = last >= kLeast ? 255 - (int)(last & 255u) : -1;
+            above = of(last | 255u);
             if (inexact) {
                 uint32_t after = __shfl_down_sync(~0u, mine, 1);
                 if (lane == 31) after = last;  // of use where k = 32
@@ -521,14 +527,33 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
                 b1 = e_next >= 0 ? pool.bias[e_next] : 0.f;
                 c1 = e_next >= 0 ? score(z1) + b1 : kNone;
             }
-            doubt = lane < p.k && c1 > kNone && !(c0 - c1 > 2.f * err + 0x1.4p-24f * (fabsf(c0) + fabsf(c1))) &&
+            // A pick against the next one down, whose own FP32 choice may be low
+            // by as much: twice err, and four roundings.
+            doubt = lane < p.k && c1 > kNone && !(c0 - c1 > 2.f * err + 0x1.8p-23f * (fabsf(c0) + fabsf(c1))) &&
                     !(b0 == b1 && zj == z1);
+            // The k-th against what else may share the next one's packed word.
+            if (!whole && lane == p.k - 1 && e_next >= 0)
+                doubt = doubt || !(c0 - above > err + 0x1.8p-23f * (fabsf(c0) + fabsf(above)));
+            // The k-th and the next one a true tie: against all that is not one.
+            // (From memory again: choices kept for this took 24 registers.)
+            if (__any_sync(~0u, lane == p.k - 1 && c1 > kNone && b0 == b1 && zj == z1)) {
+                const float ck = __shfl_sync(~0u, c0, p.k - 1), zk = __shfl_sync(~0u, zj, p.k - 1), bk = __shfl_sync(~0u, b0, p.k - 1);
+#pragma unroll 1
+                for (int e = lane; e < E; e += 32) {
+                    const float ze = to_f32(pool.row[e]) > kNone ? logit(pool, e) : kNone, be = pool.bias[e];
+                    const float c = (p.sigmoid ? fast_sigmoid(ze) : __expf(ze - mx) * (1.f / sum)) + be;
+                    doubt = doubt || (ze > kNone && c > kNone && !(ze == zk && be == bk) &&
+                                      !(fabsf(ck - c) > err + 0x1.8p-23f * (fabsf(ck) + fabsf(c))));
+                }
+            }
         }
         if (kAside && __any_sync(~0u, doubt || groups_doubt)) {
-            const float c = __shfl_sync(~0u, c0, p.k - 1);  // the k-th choice, off by at most err + 2^-24 |c|, as any other
+            // the k-th choice: an expert further below it than A + 3 F (the picks
+            // before it, itself and that expert) and their roundings is none
+            const float c = __shfl_sync(~0u, c0, p.k - 1);
             const uint32_t kept = limited ? __reduce_or_sync(~0u, g < pool.n && place < pool.top ? 1u << g : 0u) : ~0u;
             if (lane == 0)
-                s_tokens[atomicAdd(&s_aside, 1)] = {t, groups_doubt ? 0u : kept, c - 2.02f * (err + 0x1.4p-24f * fabsf(c))};
+                s_tokens[atomicAdd(&s_aside, 1)] = {t, groups_doubt ? 0u : kept, c - (3.f * err + 0x1.8p-22f * fabsf(c))};
             continue;
         }
         const bool mine = lane < p.k && e_mine >= 0;
@@ -685,7 +710,7 @@ template <typename Go> cudaError_t dispatch(int type, int pool, Go go)
 // each.  Eight where a token is short (T = 16384, 128 + 32 experts 8.0 us, with
 // five 8.2); with biases or groups as many as are resident at once, so that no
 // CTA starts late with a token to settle at its end (T = 8192, 256 experts in
-// groups with biases 16.6 us, with eight 17.9; 128 + 32 with biases 14.1, 14.5).
+// groups with biases 17.0 us, with eight 18.3; 128 + 32 with biases 14.6, 15.0).
 constexpr int kMostTokens = 1024;
 constexpr int kCtasPerSm = 8;
 int grid_of(int T, int num_sms, int per_sm)
@@ -707,7 +732,7 @@ cudaError_t launch_route_scores(const pmpe_route_desc &d, int num_sms, cudaStrea
     p.top_groups[0] = d.top_groups_pub; p.top_groups[1] = d.top_groups_priv;
     p.scale = d.scale;
     const bool limited = d.top_groups_pub < d.groups_pub || (d.E_priv > 0 && d.top_groups_priv < d.groups_priv);
-    // registers: 80 above 128 experts, 64 below
+    // registers: 80 above 128 experts, at most 64 below
     const int resident = std::max(d.E_pub, d.E_priv) > 128 ? 3 : 4;
     const dim3 grid(grid_of(d.T, num_sms, limited || d.bias ? resident : kCtasPerSm)), block(32 * kRouteWarps);
     p.tokens = (d.T + (int)grid.x * kRouteWarps - 1) / ((int)grid.x * kRouteWarps) * kRouteWarps;

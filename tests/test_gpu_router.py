@@ -212,6 +212,25 @@ def test_near_ties_of_many_tokens(pmpe, score, top2):
     assert (w.double() - weights / weights.sum(1, keepdim=True)).abs().max() <= REL
 
 
+@pytest.mark.parametrize("edge", [0.75, 0.5 + 2.0 ** -9, 0.6875])
+def test_choices_at_the_edge_of_a_packed_word(pmpe, edge):
+    """The best two choices within a few ulps on either side of a value where
+    the packed words change, a third one below that shares the second's word:
+    the order is that of 64 bits."""
+    g = torch.Generator().manual_seed(23)
+    T = 100000
+    at = float(np.log(edge / (1 - edge)))
+    close = at + torch.randint(-12, 13, (T, 2), generator=g, dtype=torch.float64) * 2.0 ** -23
+    third = edge - 2.0 ** -16 * torch.rand((T, 1), generator=g, dtype=torch.float64)
+    z = torch.cat([torch.log(third / (1 - third)), close], 1).float().cuda()
+    for order in ([0, 1, 2], [1, 0, 2], [1, 2, 0]):
+        zo = z[:, order].contiguous()
+        want = torch.sort(1 / (1 + torch.exp(-zo.double())), dim=1, descending=True, stable=True).indices
+        for k in (1, 2):
+            idx, _ = pmpe.Router(3, 0, k, score="sigmoid").route(zo, bias=torch.zeros(3, device="cuda"))
+            assert torch.equal(idx.long(), want[:, :k]), (order, k, int((idx.long() != want[:, :k]).any(1).sum()))
+
+
 def test_saturated_sigmoids(pmpe):
     """Sigmoids that round to 1 in 64 bits too are equal: the lower id."""
     g = torch.Generator().manual_seed(13)
