@@ -1,7 +1,7 @@
 """clip_grad_norm against 64-bit references.
 
 Bounds: the square sum of a vector of 8 and four of them in FP32, 12 x 2^-24,
-halved by the root, the rest 64 bits, FP32's rounding of the result: below
+halved by the root, the rest 48 bits or more, FP32's rounding of the result: below
 2^-20 for the norm and the factor; an output adds one rounding of its type."""
 import numpy as np
 import pytest
