@@ -46,7 +46,7 @@ def _ops_command():
     cxx = shutil.which("g++") or "g++"
     home = os.path.dirname(torch.__file__)
     include = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
-               os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include"), sysconfig.get_paths()["include"]]
+               os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(_nvcc()))), "include"), sysconfig.get_paths()["include"]]
     cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-Wall", "-fvisibility=hidden", "-shared",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include")]
     for d in include:

@@ -120,8 +120,12 @@ def test_a_norm_that_is_not_finite_clips_nothing(pmpe, bad):
 
 def test_zero_gradients(pmpe):
     grads = [torch.zeros(5000, device="cuda"), torch.zeros(3, device="cuda")]
+    grads += [torch.full((5001,), -0.0, dtype=t, device="cuda") for t in (F32, BF16, F16)]
     assert float(pmpe.clip_grad_norm(grads, 1.0)) == 0.0
     assert all((g == 0).all() for g in grads)
+    masked = randn((9000,), 3, BF16)
+    masked[:8000] *= -0.0
+    check(pmpe, [masked], 1.0)
 
 
 def test_refusals(pmpe):
