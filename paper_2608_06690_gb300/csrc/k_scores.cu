@@ -480,6 +480,18 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_scores_kernel(const Sc
                 const float x = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top - 1)) - 1);
                 const float y = __shfl_sync(~0u, a, __ffs(__ballot_sync(~0u, g < n && place == top)) - 1);
                 groups_doubt = y > kNone && !(x - y > 4.f * err + 0x1p-20f * top_value);
+                // A row of equal logits (padding) and biases is nothing but true
+                // ties, settled by the ids: T = 8192 of them 24 us, put aside 274.
+                if (groups_doubt) {
+                    bool alike = true;
+#pragma unroll 1
+                    for (int e0 = 0; alike && e0 < E; e0 += 32) {
+                        const int e = min(e0 + lane, E - 1);
+                        const bool same_z = to_f32(pool.row[e]) == to_f32(pool.row[0]), same_b = !kBias || pool.bias[e] == pool.bias[0];
+                        alike = __all_sync(~0u, same_z && same_b);
+                    }
+                    groups_doubt = !alike;
+                }
             }
         }
         // Neighbours in the order, the last one's being the first not chosen

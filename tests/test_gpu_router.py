@@ -231,6 +231,21 @@ def test_choices_at_the_edge_of_a_packed_word(pmpe, edge):
             assert torch.equal(idx.long(), want[:, :k]), (order, k, int((idx.long() != want[:, :k]).any(1).sum()))
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("group_score", ["max", "top2"])
+def test_rows_of_equal_logits(pmpe, score, group_score):
+    """Padding: every choice of a row is the same, or all but one."""
+    z, policy, b = make(24, 64, 30, 31, F32, True)
+    z[::2] = 0.0
+    z[1::4] = -1.5
+    z[2, 5] = 2.0 ** -24
+    z[4, 63] = -np.inf
+    z[6, 64:] = float("nan")
+    z[8] = np.inf
+    for bias in (None, torch.zeros_like(b), torch.full_like(b, 0.3), b):
+        check(pmpe, z, policy, bias, 64, 30, 6, score, True, 1.0, (8, 3), (10, 4), group_score)
+
+
 def test_saturated_sigmoids(pmpe):
     """Sigmoids that round to 1 in 64 bits too are equal: the lower id."""
     g = torch.Generator().manual_seed(13)
