@@ -98,6 +98,13 @@ bool is_matrix(const at::Tensor &t, int64_t rows, int64_t cols, at::Device dev, 
 {
     return t.scalar_type() == type && t.dim() == 2 && t.size(0) == rows && t.size(1) == cols && t.device() == dev && t.is_contiguous();
 }
+// The type of a norm's weight: that of the rows or FP32.
+int weight_type_of(const at::Tensor &w, int64_t H, at::Device dev, at::ScalarType type, const char *what)
+{
+    if (is_vector(w, H, dev, type)) return type_of(type);
+    want(is_vector(w, H, dev, at::kFloat), what);
+    return PMPE_F32;
+}
 // Elements from a row to the next (any value serves a single row); -1, which
 // the library refuses, where a row's elements are not adjacent.
 int64_t pitch(const at::Tensor &t)
@@ -161,7 +168,6 @@ PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
                     : text && PyUnicode_CompareWithASCIIString(a[4], "row") == 0 ? PMPE_QUANT_ROW : -1;
             want(quant > 0, "rms_norm: quant is None, \"block\" or \"row\"");
         }
-        const Where at(x, "rms_norm: x is a CUDA tensor");
         pmpe_rms_norm_desc d = {};
         const at::ScalarType type = x.scalar_type();
         d.type = type_of(type);
@@ -169,8 +175,8 @@ PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int64_t T = x.size(0), H = x.size(1);
         d.T = count(T);
         d.H = count(H);
-        d.weight_type = is_vector(w, H, at.device, type) ? d.type : PMPE_F32;
-        want(d.weight_type == d.type || is_vector(w, H, at.device, at::kFloat), "rms_norm: weight is [H] of x's type or FP32, on x's device");
+        d.weight_type = weight_type_of(w, H, x.device(), type, "rms_norm: weight is [H] of x's type or FP32, on x's device");
+        const Where at(x, "rms_norm: x is a CUDA tensor");
         d.quant = quant;
         d.eps = narrow(eps);
         d.x = x.data_ptr();
@@ -213,7 +219,6 @@ PyObject *rms_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const at::Tensor *d_h = optional(a[4], "rms_norm_backward: d_h is a tensor");
         const int need_dw = PyObject_IsTrue(a[6]);
         if (need_dw < 0) return nullptr;
-        const Where at(h, "rms_norm_backward: h is a CUDA tensor");
         pmpe_rms_norm_backward_desc d = {};
         const at::ScalarType type = h.scalar_type(), gt = dy.scalar_type();
         d.type = type_of(type);
@@ -221,6 +226,8 @@ PyObject *rms_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int64_t T = h.size(0), H = h.size(1);
         d.T = count(T);
         d.H = count(H);
+        d.weight_type = weight_type_of(w, H, h.device(), type, "rms_norm_backward: weight is [H] of h's type or FP32, on h's device");
+        const Where at(h, "rms_norm_backward: h is a CUDA tensor");
         at::ScalarType xt = type;
         if (a[5] != Py_None) {
             want(THPDtype_Check(a[5]), "rms_norm_backward: dx_dtype is a dtype");
@@ -228,8 +235,6 @@ PyObject *rms_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         }
         want(xt == type || xt == at::kFloat, "rms_norm_backward: dx is of h's type or FP32");
         want((gt == type || gt == at::kFloat) && is_matrix(dy, T, H, at.device, gt), "rms_norm_backward: dy is [T, H] of h's type or FP32 without gaps");
-        d.weight_type = is_vector(w, H, at.device, type) ? d.type : PMPE_F32;
-        want(d.weight_type == d.type || is_vector(w, H, at.device, at::kFloat), "rms_norm_backward: weight is [H] of h's type or FP32");
         want(is_vector(rstd, T, at.device, at::kFloat), "rms_norm_backward: rstd is FP32 [T]");
         want(!d_h || is_matrix(*d_h, T, H, at.device, xt), "rms_norm_backward: d_h is [T, H] of dx's type without gaps");
         d.dy_type = type_of(gt);

@@ -165,6 +165,18 @@ def test_no_rows_and_refusals(pmpe):
             pmpe.rms_norm(**dict(dict(x=x, weight=w), **bad))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_weights_that_are_not_the_rows_are_refused(pmpe, dtype):
+    x, w, rstd = randn((4, 64), 2, dtype), randn((64,), 1, dtype), torch.ones(4, device="cuda")
+    other = F16 if dtype is BF16 else BF16
+    for bad in (w.to(other), w.double(), w[:63], w.float()[:63], w.cpu(), w.float().cpu(), w[None], w[:1].expand(64), torch.ones(65, device="cuda"),
+                torch.ones(128, device="cuda")[::2], torch.ones(0, device="cuda")):
+        with pytest.raises(pmpe.PmpeError, match="weight is"):
+            pmpe.rms_norm(x, bad)
+        with pytest.raises(pmpe.PmpeError, match="weight is"):
+            pmpe.rms_norm_backward(x, x, bad, rstd)
+
+
 # ------------------------------------------------------------- backward
 
 def check_backward(pmpe, T, H, dtype, gtype=None, xtype=None, d_h=True, wtype=None, seed=0):

@@ -200,6 +200,25 @@ def test_arguments_of_other_types_are_refused(pmpe):
             call()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_weights_of_another_size_type_or_order_are_refused(pmpe, dtype):
+    """Whatever the rows' type is; the weight is looked at before the device is,
+    so that its own message shows."""
+    x, r = torch.zeros(2, 8, dtype=dtype), torch.ones(2)
+    other = torch.float16 if dtype is torch.bfloat16 else torch.bfloat16
+    for w in (torch.ones(8, dtype=other), torch.ones(8).double(), torch.ones(8, dtype=torch.int32), torch.ones(7, dtype=dtype), torch.ones(7),
+              torch.ones(9), torch.ones(0), torch.ones(1, 8), torch.ones(1).expand(8), torch.ones(16)[::2], torch.ones(())):
+        with pytest.raises(pmpe.PmpeError, match="rms_norm: weight is"):
+            pmpe.rms_norm(x, w)
+        with pytest.raises(pmpe.PmpeError, match="rms_norm_backward: weight is"):
+            pmpe.rms_norm_backward(x, x, w, r)
+    for w in (torch.ones(8, dtype=dtype), torch.ones(8)):  # nothing but the device is wrong
+        with pytest.raises(pmpe.PmpeError, match="x is a CUDA tensor"):
+            pmpe.rms_norm(x, w)
+        with pytest.raises(pmpe.PmpeError, match="h is a CUDA tensor"):
+            pmpe.rms_norm_backward(x, x, w, r)
+
+
 # ------------------------------------------------ the references themselves
 
 def test_reference_norm_gradient_against_differences():
