@@ -494,13 +494,13 @@ typedef struct pmpe_grad {
 } pmpe_grad;
 
 /* norm = sqrt(sum over all tensors of g^2), out = g min(1, max_norm / (norm + 1e-6)).
- * A norm that is not finite clips nothing (out = g): the caller sees it in
- * *norm and drops the step.  max_norm: >= 0, +inf for the norm alone.  No two
- * tensors may share memory (PMPE_ERR_INVALID_ARG), whole tensors in place
- * apart.  `grads` is a host array, read before the call returns; fewer than
- * 2^31 chunks of 16 KB in all.  norm: device FP32.  workspace: device, 16-byte
- * aligned, of the size below.  The sums' order depends on the tensors' sizes
- * and alignment alone. */
+ * A norm that is not finite, or above the largest FP32 value, clips nothing
+ * (out = g): the caller sees infinity or NaN in *norm and drops the step.
+ * max_norm: >= 0, +inf for the norm alone.  No two tensors may share memory
+ * (PMPE_ERR_INVALID_ARG), whole tensors in place apart.  `grads` is a host
+ * array, read before the call returns; fewer than 2^31 chunks of 16 KB in all.
+ * norm: device FP32.  workspace: device, 16-byte aligned, of the size below.
+ * The sums' order depends on the tensors' sizes and alignment alone. */
 PMPE_API size_t pmpe_clip_workspace_size(int n); /* 0 for n < 0 */
 PMPE_API int pmpe_clip_grad_norm(const pmpe_grad *grads, int n, float max_norm, float *norm, void *workspace,
                                  size_t workspace_bytes, void *stream);

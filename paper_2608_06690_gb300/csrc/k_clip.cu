@@ -276,8 +276,8 @@ __device__ __forceinline__ void scale_chunk(const uint4 (&u)[kClipVecs], const C
     if (t < k.tail) store_one(k.out, k.vecs * per + t, k.type, f * load_one(k.body + k.vecs, t, k.type));
 }
 
-// n and f from the sums of all squares.  A norm that is not finite clips
-// nothing: the caller sees it and drops the step.
+// n and f from the sums of all squares.  A norm that is not finite as FP32,
+// as the caller sees it, clips nothing: the step is dropped.
 __device__ __forceinline__ float factor_of(const Squares &all, float max_norm, float &norm)
 {
     if (all.rare == 0.) {
@@ -286,7 +286,7 @@ __device__ __forceinline__ float factor_of(const Squares &all, float max_norm, f
     }
     const double n64 = sqrt((double)all.s.hi + all.s.lo + all.rare);
     norm = (float)n64;
-    return isfinite(n64) ? (float)fmin(1., max_norm / (n64 + 1e-6)) : 1.f;
+    return isfinite(norm) ? (float)fmin(1., max_norm / (n64 + 1e-6)) : 1.f;
 }
 
 template <int kCap>

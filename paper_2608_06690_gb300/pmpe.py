@@ -635,8 +635,8 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
     place by min(1, max_norm / (norm + 1e-6)), or into the tensors of ``out``.
 
     FP32, BF16 and FP16 tensors may be mixed; each lies in memory without gaps.
-    max_norm = inf: the norm alone.  A norm that is not finite clips nothing.
-    No tensor may share memory with another."""
+    max_norm = inf: the norm alone.  A norm that is not finite as FP32
+    clips nothing.  No tensor may share memory with another."""
     if isinstance(grads, dict):
         if out is not None:
             if not isinstance(out, dict) or out.keys() != grads.keys():

@@ -118,6 +118,23 @@ def test_a_norm_that_is_not_finite_clips_nothing(pmpe, bad):
         assert torch.equal(torch.nan_to_num(o.float(), 7.0), torch.nan_to_num(b.float(), 7.0))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_norm_past_fp32_clips_nothing(pmpe, dtype):
+    """Finite gradients whose norm FP32 does not hold: it is reported as
+    infinity, and what is reported decides."""
+    high = torch.finfo(dtype).max
+    for values in ((3e38, 3e38), (high, high, high, 1.0), (high, 2.0 ** 127) * 3000):
+        g = torch.tensor(values).to(dtype).cuda()
+        more, out = randn((500,), 2), [torch.zeros_like(g), torch.zeros(500, device="cuda")]
+        before = [g.clone(), more.clone()]
+        n = [pmpe.clip_grad_norm([g, more], 1.0, out=out), pmpe.clip_grad_norm([g, more], 1.0)]
+        assert all(float(v) == float("inf") for v in n)
+        for a, b, o in zip(before, (g, more), out):
+            assert torch.equal(a, b) and torch.equal(a, o)
+    for values in ((2e38, 2e38), (3.4e38,)):  # within FP32: clipped
+        check(pmpe, [torch.tensor(values).cuda(), torch.tensor([7.0], device="cuda")], 1e30)
+
+
 def test_zero_gradients(pmpe):
     grads = [torch.zeros(5000, device="cuda"), torch.zeros(3, device="cuda")]
     grads += [torch.full((5001,), -0.0, dtype=t, device="cuda") for t in (F32, BF16, F16)]
