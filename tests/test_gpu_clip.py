@@ -135,6 +135,16 @@ def test_a_norm_past_fp32_clips_nothing(pmpe, dtype):
         check(pmpe, [torch.tensor(values).cuda(), torch.tensor([7.0], device="cuda")], 1e30)
 
 
+@pytest.mark.parametrize("dtype,scale", [(F32, 1e35), (F32, 1e30), (BF16, 1e35), (F32, 1e-3)])
+@pytest.mark.parametrize("max_norm", [1e-4, 1e-10, 1e-34])
+def test_factors_below_the_normal_range(pmpe, dtype, scale, max_norm):
+    """Large gradients and a small limit: the factor is below 2^-126, the
+    clipped gradients (of the size max_norm / 70) are not."""
+    grads = [randn((5000,), 1, dtype, scale), randn((33,), 2, dtype, scale)]
+    check(pmpe, grads, max_norm, out=[torch.empty_like(g) for g in grads])
+    check(pmpe, grads, max_norm)
+
+
 def test_zero_gradients(pmpe):
     grads = [torch.zeros(5000, device="cuda"), torch.zeros(3, device="cuda")]
     grads += [torch.full((5001,), -0.0, dtype=t, device="cuda") for t in (F32, BF16, F16)]
