@@ -217,10 +217,17 @@ bool aligned8(const void *q, bool f32) { return ((uintptr_t)q & (f32 ? 31u : 15u
 
 }  // namespace
 
-size_t rms_norm_backward_workspace_bytes(int T, int H) { return (size_t)bwd_ctas(T, H) * H * sizeof(float); }
-
-cudaError_t launch_rms_norm_backward(const pmpe_rms_norm_backward_desc &d, float *part, cudaStream_t st)
+// The partial sums, aligned for eight of them at a time wherever the workspace
+// starts: what is computed how does not depend on its address.
+constexpr size_t kPartAlign = 32, kWorkspaceAlign = 16;
+size_t rms_norm_backward_workspace_bytes(int T, int H)
 {
+    return (size_t)bwd_ctas(T, H) * H * sizeof(float) + (kPartAlign - kWorkspaceAlign);
+}
+
+cudaError_t launch_rms_norm_backward(const pmpe_rms_norm_backward_desc &d, cudaStream_t st)
+{
+    float *part = reinterpret_cast<float *>(((uintptr_t)d.workspace + (kPartAlign - 1)) & ~(uintptr_t)(kPartAlign - 1));
     NormBwdParams p;
     p.h = d.h; p.dy = d.dy; p.d_h = d.d_h; p.w = d.weight; p.rstd = d.rstd; p.dx = d.dx;
     p.part = d.dw ? part : nullptr;
@@ -229,7 +236,7 @@ cudaError_t launch_rms_norm_backward(const pmpe_rms_norm_backward_desc &d, float
     // eight elements an access where every row of every operand allows it
     const bool h32 = d.type == PMPE_F32;
     const bool vec = d.H % 8 == 0 && aligned8(d.dy, g32) && aligned8(d.h, h32) && aligned8(d.weight, p.w_f32) &&
-                     aligned8(d.d_h, x32) && aligned8(d.dx, x32) && aligned8(part, true);
+                     aligned8(d.d_h, x32) && aligned8(d.dx, x32);
     cudaError_t err;
     if (d.type == PMPE_F32) err = vec ? launch<float, float, float, true>(p, st) : launch<float, float, float, false>(p, st);
     else if (d.type == PMPE_BF16) err = vec ? by_types<bf16, true>(p, g32, x32, st) : by_types<bf16, false>(p, g32, x32, st);

@@ -84,7 +84,7 @@ int pmpe_rms_norm_backward(const pmpe_rms_norm_backward_desc *d, void *stream)
     if (d->dw && (!d->workspace || ((uintptr_t)d->workspace & 15u) ||
                   d->workspace_bytes < rms_norm_backward_workspace_bytes(d->T, d->H)))
         return PMPE_ERR_WORKSPACE;
-    return done(launch_rms_norm_backward(*d, (float *)d->workspace, (cudaStream_t)stream));
+    return done(launch_rms_norm_backward(*d, (cudaStream_t)stream));
 }
 
 int pmpe_route(const pmpe_route_desc *d, void *stream)

@@ -180,7 +180,7 @@ cudaError_t launch_gather_dispatch_rows(const Ctx &c, int g0, int g1);
 // descriptors checked by ops_api.cu.
 cudaError_t launch_rms_norm(const pmpe_rms_norm_desc &d, cudaStream_t st);
 size_t rms_norm_backward_workspace_bytes(int T, int H);
-cudaError_t launch_rms_norm_backward(const pmpe_rms_norm_backward_desc &d, float *part, cudaStream_t st);
+cudaError_t launch_rms_norm_backward(const pmpe_rms_norm_backward_desc &d, cudaStream_t st);
 cudaError_t launch_route_scores(const pmpe_route_desc &d, int num_sms, cudaStream_t st);
 cudaError_t launch_route_scores_backward(const pmpe_route_desc &d, const float *dw, void *d_logits, int num_sms,
                                          cudaStream_t st);

@@ -233,6 +233,34 @@ def test_backward_against_differences(pmpe):
     assert abs(quotient - along) <= bound, (quotient, along, bound)
 
 
+@pytest.mark.parametrize("T,H", [(300, 2048), (40, 256), (33, 1001), (500, 8192)])
+def test_backward_does_not_go_by_the_workspaces_address(pmpe, T, H):
+    """Any 16-byte aligned workspace of the size asked for gives the same bits,
+    and so does none where there is no weight's gradient; nothing is written
+    past its end or before it."""
+    from test_operators_abi import RmsNormBackwardDesc, desc
+    h, dy, w = randn((T, H), 1, BF16), randn((T, H), 2, BF16), randn((H,), 3, BF16)
+    rstd = torch.rsqrt(h.double().square().mean(1) + 1e-6).float()
+    need = pmpe._lib.pmpe_rms_norm_backward_workspace_size(T, H)
+    got = []
+    for at in (0, 16, 32, 48, None):
+        ws = torch.full((need + 128,), 77, dtype=torch.uint8, device="cuda")
+        dx, dw = torch.empty_like(h), torch.empty(H, device="cuda")
+        base = dict(T=T, H=H, type=1, weight_type=1, dy_type=1, dx_type=1, dy=dy.data_ptr(), h=h.data_ptr(), weight=w.data_ptr(),
+                    rstd=rstd.data_ptr(), d_h=None, dx=dx.data_ptr(), dw=dw.data_ptr(), workspace=ws.data_ptr() + (at or 0), workspace_bytes=need)
+        if at is None:
+            base.update(dw=None, workspace=ws.data_ptr() + 16, workspace_bytes=0)
+        torch.cuda.synchronize()
+        assert pmpe._lib.pmpe_rms_norm_backward(desc(RmsNormBackwardDesc, base), None) == pmpe.OK
+        torch.cuda.synchronize()
+        assert (ws[:at or 0] == 77).all() and (ws[(at or 0) + need:] == 77).all()
+        assert at is not None or (ws == 77).all()
+        got.append((dx, dw))
+    for dx, dw in got[1:]:
+        assert torch.equal(dx, got[0][0])
+        assert dw is got[-1][1] or torch.equal(dw, got[0][1])
+
+
 def test_backward_no_rows(pmpe):
     e = torch.empty((0, 64), dtype=BF16, device="cuda")
     dx, dw = pmpe.rms_norm_backward(e, e, randn((64,), 1, BF16), torch.empty(0, device="cuda"))
