@@ -228,9 +228,6 @@ template <typename T, bool kVec> cudaError_t dispatch_fwd(const NormParams &p, c
     return p.quant == PMPE_QUANT_NONE ? dispatch_q<T, kVec, false>(p, st) : dispatch_q<T, kVec, true>(p, st);
 }
 
-// Aligned for eight elements at a time.
-bool aligned8(const void *q, bool f32) { return ((uintptr_t)q & (f32 ? 31u : 15u)) == 0; }
-
 }  // namespace
 
 cudaError_t launch_rms_norm(const pmpe_rms_norm_desc &d, cudaStream_t st)

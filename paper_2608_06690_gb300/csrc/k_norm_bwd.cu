@@ -212,9 +212,6 @@ template <typename T, bool kVec> cudaError_t by_types(const NormBwdParams &p, bo
     return x32 ? launch<T, T, float, kVec>(p, st) : launch<T, T, T, kVec>(p, st);
 }
 
-// Aligned for eight elements at a time.
-bool aligned8(const void *q, bool f32) { return ((uintptr_t)q & (f32 ? 31u : 15u)) == 0; }
-
 }  // namespace
 
 // The partial sums, aligned for eight of them at a time wherever the workspace
