@@ -133,6 +133,13 @@ template <typename F> void run(const char *what, F f)
     if (rc != PMPE_OK) throw Refused{rc, what};
 }
 
+// A caller's tensor was written to: autograd refuses a backward that saved it
+// before.  (Tensors of inference mode have no versions.)
+void written(const at::Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // A tuple (or a named one) of tensors; None where there is none.
 PyObject *pack(PyTypeObject *type, std::initializer_list<at::Tensor> all)
 {
@@ -205,6 +212,7 @@ PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         d.y = y.data_ptr();
         d.rstd = (float *)rstd.data_ptr();
         run("pmpe_rms_norm", [&, s = at.stream()] { return lib_rms_norm(&d, s); });
+        if (h_out) written(*h_out);
         return pack(g_rms_norm, {y, scale, h, rstd});
     });
 }
@@ -310,6 +318,7 @@ PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n)
         d.topk_idx = (int32_t *)idx.data_ptr();
         d.topk_w = (float *)w.data_ptr();
         run("pmpe_route", [&, s = at.stream()] { return lib_route(&d, s); });
+        if (load) written(*load);
         return pack(&PyTuple_Type, {idx, w});
     });
 }
@@ -365,6 +374,8 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         PyObject **g = PySequence_Fast_ITEMS(a[0]), **o = apart ? PySequence_Fast_ITEMS(a[2]) : nullptr;
         const Where at(tensor(g[0], "clip_grad_norm: gradients are CUDA tensors"), "clip_grad_norm: gradients are CUDA tensors");
         std::vector<pmpe_grad> grads((size_t)count(n));
+        std::vector<at::Tensor> outputs;  // held: the lists may change while other threads run
+        outputs.reserve((size_t)n);
         for (Py_ssize_t i = 0; i < n; ++i) {
             const at::Tensor &t = tensor(g[i], "clip_grad_norm: gradients are CUDA tensors");
             pmpe_grad &q = grads[(size_t)i];
@@ -384,12 +395,15 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args)
                 }
             }
             want(whole || dense(t), "clip_grad_norm: a gradient has gaps");
+            outputs.push_back(o ? tensor(o[i], "clip_grad_norm: outputs are CUDA tensors") : t);
         }
         const size_t bytes = lib_clip_workspace_size((int)n);
         const at::Tensor norm = at::detail::empty_strided_cuda({}, {}, at::kFloat, at.device), ws = empty(at.device, at::kByte, (int64_t)bytes);
         run("pmpe_clip_grad_norm", [&, to = (float *)norm.data_ptr(), scratch = ws.data_ptr(), s = at.stream()] {
             return lib_clip_grad_norm(grads.data(), (int)n, narrow(max_norm), to, scratch, bytes, s);
         });
+        if (apart || max_norm < INFINITY)  // else the norm alone
+            for (const at::Tensor &t : outputs) written(t);
         return THPVariable_Wrap(norm);
     });
 }

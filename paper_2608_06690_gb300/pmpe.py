@@ -520,6 +520,12 @@ class MoeLayer:
 #
 # Checks, outputs and launches are in _ops (csrc/bind_ops.cpp): a call's host
 # time counts as much as its kernel's at decode sizes.
+#
+# Neither these functions nor MoeLayer record anything for autograd: what they
+# return has no history, whatever the arguments require, and the backward
+# functions are the caller's to call.  What the functions here write to in place
+# (h_out, load, clipped gradients and out) counts up its version, so that
+# autograd refuses a backward that had saved it.
 
 QUANT_BLOCK = 128  # columns that share a scale with quant="block"
 

@@ -155,6 +155,36 @@ def test_zero_gradients(pmpe):
     check(pmpe, [masked], 1.0)
 
 
+def test_what_is_written_in_place_counts_up_its_version(pmpe):
+    """So that autograd does not go on with a tensor that it saved before."""
+    def version(call, t):
+        v = t._version
+        call()
+        return t._version - v
+
+    a, out = randn((300,), 1), [torch.empty(300, device="cuda")]
+    assert version(lambda: pmpe.clip_grad_norm([a], 1.0), a) == 1
+    assert version(lambda: pmpe.clip_grad_norm([a], float("inf")), a) == 0  # the norm alone
+    assert version(lambda: pmpe.clip_grad_norm([a], 1.0, out=out), a) == 0 and out[0]._version == 1
+    assert version(lambda: pmpe.clip_grad_norm([a], float("inf"), out=out), out[0]) == 1
+    x, res, w = randn((4, 64), 2), randn((4, 64), 3), randn((64,), 4)
+    assert version(lambda: pmpe.rms_norm(x, w, residual=res), res) == 0
+    assert version(lambda: pmpe.rms_norm(x, w, residual=res, h_out=res), res) == 1
+    load = torch.zeros(8, dtype=torch.int32, device="cuda")
+    assert version(lambda: pmpe.Router(8, 0, 2).route(randn((4, 8), 5), load=load), load) == 1
+    leaf = randn((4, 64), 6).requires_grad_()
+    saved = leaf * 2
+    loss = saved.square().sum()
+    pmpe.rms_norm(x, w, residual=saved.detach(), h_out=saved.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():  # tensors without versions
+        b = randn((300,), 7)
+        pmpe.clip_grad_norm([b], 1.0)
+        pmpe.rms_norm(x, w, residual=b[:256].view(4, 64), h_out=b[:256].view(4, 64))
+    pmpe.clip_grad_norm([b], 0.5)
+
+
 def test_refusals(pmpe):
     a, b = randn((64, 64), 1), randn((64,), 2)
     for bad in (dict(grads=[a, a]), dict(grads=[a, a[3]]), dict(grads=[a, a.view(-1)[4090:]]), dict(grads=[a[:, :30]]),
