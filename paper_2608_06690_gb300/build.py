@@ -1,7 +1,8 @@
 """Build libpmpe.so in-tree with nvcc for sm_103a (no cmake, no torch
 extension machinery): each .cu under csrc/ compiles to an object in
 parallel, then one shared-library link.  Beside it the Python module _ops
-(csrc/bind_ops.cpp) with g++ against the headers of the installed PyTorch."""
+(csrc/bind_ops.cpp) with g++ against the headers of the installed PyTorch; the
+library needs neither, and is there where that module cannot be built."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -47,7 +48,7 @@ def _ops_command():
     home = os.path.dirname(torch.__file__)
     include = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
                os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(_nvcc()))), "include"), sysconfig.get_paths()["include"]]
-    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-Wall", "-fvisibility=hidden", "-shared",
+    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-Wall", "-fvisibility=hidden", "-shared", f'-DPMPE_BUILT_FOR="{torch.__version__}"',
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include")]
     for d in include:
         cmd += ["-isystem", d]
@@ -71,11 +72,15 @@ def build(verbose: bool = False, force: bool = False, ptxas_info: bool = False) 
             cmd = [nvcc] + _flags() + (["-Xptxas", "-v"] if ptxas_info else []) + ["-c", src, "-o", obj]
             jobs.append(cmd)
 
-    ops_cmd, built_for = _ops_command()
+    ops_cmd = ops_error = built_for = None
     stamp = os.path.join(BUILD_DIR, "_ops.txt")
+    try:
+        ops_cmd, built_for = _ops_command()
+    except Exception as e:  # no PyTorch
+        ops_error = repr(e)
     ops = force or _stale(OPS_OUT, [OPS_SRC, os.path.join(ROOT, "include", "pmpe.h")]) or not os.path.exists(stamp) or \
         open(stamp).read() != built_for
-    if ops:
+    if ops and ops_cmd:
         jobs.insert(0, ops_cmd)
 
     def run(cmd):
@@ -87,8 +92,10 @@ def build(verbose: bool = False, force: bool = False, ptxas_info: bool = False) 
             if verbose or ptxas_info or r.returncode != 0:
                 sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
             if r.returncode != 0:
-                raise RuntimeError("building _ops.so failed" if cmd is ops_cmd else f"nvcc failed on {cmd[-3]}")
-    if ops:
+                if cmd is not ops_cmd:
+                    raise RuntimeError(f"nvcc failed on {cmd[-3]}")
+                ops_error = f"{cmd[0]} returned {r.returncode}"
+    if ops and not ops_error:
         os.replace(OPS_OUT + ".tmp", OPS_OUT)
         with open(stamp, "w") as f:
             f.write(built_for)
@@ -99,6 +106,10 @@ def build(verbose: bool = False, force: bool = False, ptxas_info: bool = False) 
             sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
             raise RuntimeError("link of libpmpe.so failed")
         os.replace(OUT + ".tmp", OUT)
+    if ops_error:
+        if os.path.exists(OPS_OUT):  # of another source or another PyTorch
+            os.remove(OPS_OUT)
+        raise RuntimeError(f"building _ops.so failed ({ops_error}); libpmpe.so is built")
     return OUT
 
 

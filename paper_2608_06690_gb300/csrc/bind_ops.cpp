@@ -436,4 +436,13 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__ops() { return PyModule_Create(&module); }
+// built_for: the PyTorch whose headers this was compiled with.
+PyMODINIT_FUNC PyInit__ops()
+{
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", PMPE_BUILT_FOR) < 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}

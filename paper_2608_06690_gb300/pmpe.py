@@ -2,7 +2,9 @@
 the module _ops for the operators around it.
 
 Argument marshalling only: every step runs in the library's CUDA kernels.  PyTorch supplies device memory and streams.  If the library
-has not been built this module raises on import -- there is no fallback.
+has not been built this module raises on import -- there is no fallback.  Where
+only _ops is missing (it is compiled against one PyTorch) the layer works, and
+the operators raise ImportError when they are called.
 """
 from __future__ import annotations
 
@@ -18,15 +20,35 @@ from .inputs import LayerShape
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpmpe.so")
+_BUILD = "build it with `python -c 'import __graft_entry__ as g; g.build()'`"
 
-OPS_PATH = os.path.join(_HERE, "_ops.so")
-
-for _path in (LIB_PATH, OPS_PATH):
-    if not os.path.exists(_path):
-        raise ImportError(f"{_path} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
+if not os.path.exists(LIB_PATH):
+    raise ImportError(f"{LIB_PATH} is missing: {_BUILD}")
 
 _lib = ctypes.CDLL(LIB_PATH)
-_ops = importlib.import_module("._ops", __package__)
+
+
+class _NoOps:
+    """In the place of _ops where it cannot be loaded: says so at the first use."""
+
+    def __init__(self, why):
+        self.__dict__["why"] = why
+
+    def __getattr__(self, name):
+        raise ImportError(f"the operators around the layer need {os.path.join(_HERE, '_ops.so')} ({self.why}): {_BUILD}")
+
+
+def _load_ops():
+    try:
+        ops = importlib.import_module("._ops", __package__)
+    except ImportError as e:
+        return _NoOps(e)
+    if ops.built_for != torch.__version__:
+        return _NoOps(f"built for PyTorch {ops.built_for}, this is {torch.__version__}")
+    return ops
+
+
+_ops = _load_ops()
 
 OK = 0
 ERR_INVALID_ARG = -1
@@ -654,6 +676,7 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
     return _ops.clip_grad_norm(grads, max_norm, out)
 
 
-_ops.setup(PmpeError, RmsNorm, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
-    "pmpe_rms_norm", "pmpe_rms_norm_backward_workspace_size", "pmpe_rms_norm_backward", "pmpe_route", "pmpe_route_backward",
-    "pmpe_clip_workspace_size", "pmpe_clip_grad_norm")))
+if not isinstance(_ops, _NoOps):
+    _ops.setup(PmpeError, RmsNorm, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
+        "pmpe_rms_norm", "pmpe_rms_norm_backward_workspace_size", "pmpe_rms_norm_backward", "pmpe_route", "pmpe_route_backward",
+        "pmpe_clip_workspace_size", "pmpe_clip_grad_norm")))

@@ -219,6 +219,63 @@ def test_weights_of_another_size_type_or_order_are_refused(pmpe, dtype):
             pmpe.rms_norm_backward(x, x, w, r)
 
 
+WITHOUT_OPS = """
+import sys, torch
+from paper_2608_06690_gb300 import pmpe
+from paper_2608_06690_gb300.inputs import LayerShape
+s = LayerShape(64, 256, 128, 8, 4, 0, 2, True)
+assert pmpe.workspace_size(s) > 0 and pmpe.MoeLayer(s, {}, device="cpu").shape is s
+x = torch.zeros(2, 8)
+for call in (lambda: pmpe.rms_norm(x, x[0]), lambda: pmpe.rms_norm_backward(x, x, x[0], x[:, 0]), lambda: pmpe.Router(8, 0, 2),
+             lambda: pmpe.clip_grad_norm([x], 1.0)):
+    try:
+        call()
+    except ImportError as e:
+        assert "_ops.so" in str(e) and sys.argv[1] in str(e) and "build" in str(e), e
+    else:
+        raise AssertionError("no ImportError")
+"""
+
+
+@pytest.mark.parametrize("kind", ["missing", "broken", "another"])
+def test_the_layer_does_not_need_the_operators_module(pmpe, kind, tmp_path):
+    """Without _ops, with one that does not load or one that was built for
+    another PyTorch, the layer is there and the operators say what is missing."""
+    import subprocess
+    import sys
+    src = os.path.dirname(pmpe.__file__)
+    to = tmp_path / "paper_2608_06690_gb300"
+    to.mkdir()
+    for f in os.listdir(src):
+        if f.endswith(".py") or f == "libpmpe.so":
+            shutil.copy(os.path.join(src, f), to / f)
+    says = "No module named"
+    if kind == "broken":
+        (to / "_ops.so").write_bytes(b"not a library")
+        says = "_ops.so"
+    elif kind == "another":
+        (to / "_ops.py").write_text("built_for = '1.0'")
+        says = "built for PyTorch 1.0"
+    subprocess.run([sys.executable, "-c", WITHOUT_OPS, says], cwd=tmp_path, check=True, env=dict(os.environ, PYTHONPATH=str(tmp_path)))
+
+
+def test_the_library_is_built_where_the_module_cannot_be(pmpe, tmp_path, monkeypatch):
+    from paper_2608_06690_gb300 import build
+
+    def no_torch():
+        raise ImportError("No module named 'torch'")
+
+    for command in (lambda: (["false"], "another"), no_torch):
+        monkeypatch.setattr(build, "OUT", str(tmp_path / "libpmpe.so"))
+        monkeypatch.setattr(build, "OPS_OUT", str(tmp_path / "_ops.so"))
+        monkeypatch.setattr(build, "_ops_command", command)
+        (tmp_path / "_ops.so").write_bytes(b"of another PyTorch")
+        with pytest.raises(RuntimeError, match="building _ops.so failed"):
+            build.build()
+        assert (tmp_path / "libpmpe.so").exists() and not (tmp_path / "_ops.so").exists()
+        os.remove(tmp_path / "libpmpe.so")
+
+
 # ------------------------------------------------ the references themselves
 
 def test_reference_norm_gradient_against_differences():
