@@ -394,6 +394,10 @@ class MoeLayer:
         assert hidden.is_contiguous() and hidden.dtype == torch.bfloat16 and hidden.shape == (T, s.H)
         if policy is not None:
             assert policy.dtype == torch.uint8 and policy.numel() == T and policy.is_contiguous()
+        dev = hidden.get_device()
+        for t in (hidden, policy, out, topk_idx, topk_w, audit):
+            if t is not None and not t.get_device() == dev >= 0:
+                _bad("MoeLayer.forward: CUDA tensors of one device are wanted")
         if out is None:
             out = torch.empty_like(hidden)
         saved = None
@@ -407,7 +411,7 @@ class MoeLayer:
                 _bad("MoeLayer.forward: a given route takes the place of the route log, the control and the stages")
             topk_idx, topk_w = route
             for v, dt in ((topk_idx, torch.int32), (topk_w, torch.float32)):
-                if not _matrix(v, T, s.k, hidden.get_device(), dt):
+                if not _matrix(v, T, s.k, dev, dt):
                     _bad("MoeLayer.forward: route is (idx, w), int32 and FP32 [T, k] on the layer's device")
         desc = make_desc(s, self.weights, hidden, policy, out, self.workspace(T), topk_idx, topk_w, audit,
                          unmasked_control, saved)
@@ -419,6 +423,13 @@ class MoeLayer:
         self._route_out = (topk_idx, topk_w)
         self._saved_gu = saved
         return out
+
+    @staticmethod
+    def _rows(hidden, dout, what: str):
+        """A backward's hidden states are the forward's: BF16 rows as dout's."""
+        if not hidden.is_cuda or hidden.dtype != torch.bfloat16 or not hidden.is_contiguous() or hidden.shape != dout.shape or \
+                hidden.device != dout.device:
+            _bad(f"MoeLayer.{what}: hidden is the forward's, BF16 [T, H] without gaps on dout's CUDA device")
 
     def _own_route(self, what: str):
         if self._given:
@@ -438,6 +449,7 @@ class MoeLayer:
         if T != self._route_out[0].shape[0]:
             _bad("MoeLayer.backward_routed: the last forward ran another number of tokens")
         assert dout.is_contiguous() and dout.dtype == torch.bfloat16 and dout.shape == (T, s.H)
+        self._rows(hidden, dout, "backward_routed")
         dev = hidden.device
         g = {n: torch.empty(shp, dtype=torch.float32, device=dev) for n, shp in private_gradient_shapes(s).items()
              if n != "d_router"}
@@ -467,6 +479,7 @@ class MoeLayer:
         T = hidden.shape[0]
         s = self._shape_T(T)
         assert dout.is_contiguous() and dout.dtype == torch.bfloat16 and dout.shape == (T, s.H)
+        self._rows(hidden, dout, "backward_private")
         dev = hidden.device
         g = {n: torch.empty(shp, dtype=torch.float32, device=dev) for n, shp in private_gradient_shapes(s).items()}
         nb = _lib.pmpe_moe_backward_workspace_size(s.T, s.H, s.I, s.E_pub, s.E_priv, s.E_sh, s.k)
@@ -494,6 +507,7 @@ class MoeLayer:
         T = hidden.shape[0]
         s = self._shape_T(T)
         assert dout.is_contiguous() and dout.dtype == torch.bfloat16 and dout.shape == (T, s.H)
+        self._rows(hidden, dout, "backward")
         dev = hidden.device
         g = {n: torch.empty(shp, dtype=torch.float32, device=dev) for n, shp in private_gradient_shapes(s).items()}
         d_hidden = torch.empty((T, s.H), dtype=torch.float32, device=dev)
@@ -521,6 +535,7 @@ class MoeLayer:
         T = hidden.shape[0]
         s = self._shape_T(T)
         assert dout.is_contiguous() and dout.dtype == torch.bfloat16 and dout.shape == (T, s.H)
+        self._rows(hidden, dout, "backward_input")
         dev = hidden.device
         d_hidden = torch.empty((T, s.H), dtype=torch.float32, device=dev)
         nb = _lib.pmpe_moe_backward_input_workspace_size(s.T, s.H, s.I, s.E_pub, s.E_priv, s.E_sh, s.k)

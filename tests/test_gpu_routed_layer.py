@@ -151,6 +151,27 @@ def test_refusals_and_the_empty_batch():
     assert all((v == 0).all() for v in g.values())
 
 
+def test_tensors_that_are_not_the_layers_rows_are_refused():
+    shape, layer, h, pol, _ = build("tile_edges")
+    _, idx, w = own_route(shape, layer, h, pol)
+    for bad in (dict(policy=pol.cpu()), dict(out=torch.empty_like(h, device="cpu")), dict(topk_idx=idx.cpu()), dict(audit=new_audit(shape).cpu()),
+                dict(route=(idx.cpu(), w)), dict(route=(idx, w.cpu())), dict(hidden=h.cpu())):
+        with pytest.raises(pmpe.PmpeError):
+            layer.forward(**dict(dict(hidden=h, policy=pol), **bad))
+    dout = torch.zeros_like(h)
+    wide = torch.zeros((shape.T, 2 * shape.H), dtype=torch.bfloat16, device="cuda")
+    bad = (h.float(), h[:, :128].contiguous(), wide[:, ::2], wide[:, :shape.H], h.cpu(), h[:5])
+    layer.forward(h, pol)
+    for back in (layer.backward, layer.backward_private, layer.backward_input):
+        for x in bad[:-1]:
+            with pytest.raises(pmpe.PmpeError):
+                back(x, pol, dout)
+    layer.forward(h, pol, route=(idx, w))
+    for x in bad:
+        with pytest.raises(pmpe.PmpeError):
+            layer.backward_routed(x, pol, dout)
+
+
 # ------------------------------------------------------- the block together
 
 def block(layer, router, x, res, wn, wr, bias, policy, dout, max_norm, load):

@@ -219,6 +219,25 @@ def test_weights_of_another_size_type_or_order_are_refused(pmpe, dtype):
             pmpe.rms_norm_backward(x, x, w, r)
 
 
+def test_the_layers_rows_are_checked(pmpe):
+    """Host tensors, and hidden states in a backward that cannot be the
+    forward's, are refused before anything is allocated or launched."""
+    from paper_2608_06690_gb300.inputs import LayerShape
+    layer = pmpe.MoeLayer(LayerShape(6, 256, 128, 8, 4, 0, 2, True), {}, device="cpu")
+    h, pol = torch.zeros(6, 256, dtype=torch.bfloat16), torch.zeros(6, dtype=torch.uint8)
+    idx, w = torch.zeros(6, 2, dtype=torch.int32), torch.zeros(6, 2)
+    for kw in (dict(), dict(route=(idx, w))):
+        with pytest.raises(pmpe.PmpeError, match="MoeLayer.forward: CUDA tensors"):
+            layer.forward(h, pol, **kw)
+    for given in (False, True):
+        layer._given, layer._route_out = given, (idx, w)
+        backs = (layer.backward_routed,) if given else (layer.backward, layer.backward_private, layer.backward_input)
+        for back in backs:
+            for hidden in (h, h.float(), h[:, :128], h.t().contiguous().t(), torch.zeros(6, 512, dtype=torch.bfloat16)[:, ::2]):
+                with pytest.raises(pmpe.PmpeError, match="hidden is the forward's"):
+                    back(hidden, pol, h)
+
+
 WITHOUT_OPS = """
 import sys, torch
 from paper_2608_06690_gb300 import pmpe
