@@ -379,7 +379,8 @@ class MoeLayer:
 
     def forward(self, hidden, policy, out=None, topk_idx=None, topk_w=None, audit=None, stages=STAGE_ALL,
                 stream=None, unmasked_control: bool = False, save_for_backward: bool = False, route=None):
-        """Enqueue the layer on ``stream`` (default: the current stream).
+        """Enqueue the layer on ``stream`` (default: the current stream; the
+        caller orders another one's work after what the current stream has).
         ``route``: (idx, w), int32 and FP32 [T, k], as ``Router.route`` gives
         them, in the place of the layer's own router; its backward is
         ``backward_routed``.  A pick outside the token's pool is not taken.
@@ -395,9 +396,10 @@ class MoeLayer:
         if policy is not None:
             assert policy.dtype == torch.uint8 and policy.numel() == T and policy.is_contiguous()
         dev = hidden.get_device()
-        for t in (hidden, policy, out, topk_idx, topk_w, audit):
-            if t is not None and not t.get_device() == dev >= 0:
-                _bad("MoeLayer.forward: CUDA tensors of one device are wanted")
+        if dev < 0 or policy is not None and policy.get_device() != dev or out is not None and out.get_device() != dev or \
+                topk_idx is not None and topk_idx.get_device() != dev or topk_w is not None and topk_w.get_device() != dev or \
+                audit is not None and audit.get_device() != dev:
+            _bad("MoeLayer.forward: CUDA tensors of one device are wanted")
         if out is None:
             out = torch.empty_like(hidden)
         saved = None
@@ -413,16 +415,28 @@ class MoeLayer:
             for v, dt in ((topk_idx, torch.int32), (topk_w, torch.float32)):
                 if not _matrix(v, T, s.k, dev, dt):
                     _bad("MoeLayer.forward: route is (idx, w), int32 and FP32 [T, k] on the layer's device")
-        desc = make_desc(s, self.weights, hidden, policy, out, self.workspace(T), topk_idx, topk_w, audit,
-                         unmasked_control, saved)
+        ws = self.workspace(T)
+        desc = make_desc(s, self.weights, hidden, policy, out, ws, topk_idx, topk_w, audit, unmasked_control, saved)
         if route is not None:
             _check(_lib.pmpe_moe_forward_routed(ctypes.byref(desc), _stream(stream)), "pmpe_moe_forward_routed")
         else:
             forward_desc(desc, stages, stream)
+        if stream is not None:
+            self._hold(stream, hidden, policy, out, ws, topk_idx, topk_w, audit, saved)
         self._given = route is not None
         self._route_out = (topk_idx, topk_w)
         self._saved_gu = saved
         return out
+
+    @staticmethod
+    def _hold(stream, *tensors):
+        """The memory of a call on a stream of its own (arguments, results and
+        scratch, from the current stream's pool) is not handed out again before
+        that stream is done with it."""
+        if stream.cuda_stream != torch._C._cuda_getCurrentRawStream(stream.device_index):
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
 
     @staticmethod
     def _rows(hidden, dout, what: str):
@@ -460,13 +474,15 @@ class MoeLayer:
             raise PmpeError(ERR_UNSUPPORTED_SHAPE, "pmpe_moe_backward_step_workspace_size")
         if self._bws is None or self._bws.numel() < nb:
             self._bws = torch.empty(nb, dtype=torch.uint8, device=dev)
-        bws = self._bws
+        bws, ws = self._bws, self.workspace(T)
         topk_idx, topk_w = self._route_out
-        desc = make_desc(s, self.weights, hidden, policy, dout, self.workspace(T), topk_idx, topk_w,
+        desc = make_desc(s, self.weights, hidden, policy, dout, ws, topk_idx, topk_w,
                          saved_gu=self._saved_gu)
         _check(_lib.pmpe_moe_backward_routed(ctypes.byref(desc), _ptr(dout), _ptr(d_w), _ptr(g["d_gate"]), _ptr(g["d_up"]),
                                              _ptr(g["d_down"]), _ptr(d_hidden), _ptr(bws), bws.numel(), _stream(stream)),
                "pmpe_moe_backward_routed")
+        if stream is not None:
+            self._hold(stream, hidden, policy, dout, topk_idx, topk_w, self._saved_gu, ws, bws, *g.values(), d_hidden, d_w)
         return g, d_hidden, d_w
 
     def backward_private(self, hidden, policy, dout, topk_idx=None, topk_w=None, stream=None) -> dict:
@@ -487,15 +503,17 @@ class MoeLayer:
             raise PmpeError(ERR_UNSUPPORTED_SHAPE, "pmpe_moe_backward_workspace_size")
         if self._bws is None or self._bws.numel() < nb:
             self._bws = torch.empty(nb, dtype=torch.uint8, device=dev)
-        bws = self._bws
+        bws, ws = self._bws, self.workspace(T)
         if topk_idx is None and topk_w is None:
             topk_idx, topk_w = self._route_out
         # the descriptor's output pointer is never written by the backward
-        desc = make_desc(s, self.weights, hidden, policy, dout, self.workspace(T), topk_idx, topk_w,
+        desc = make_desc(s, self.weights, hidden, policy, dout, ws, topk_idx, topk_w,
                          saved_gu=self._saved_gu)
         _check(_lib.pmpe_moe_backward_private(ctypes.byref(desc), _ptr(dout), _ptr(g["d_router"]), _ptr(g["d_gate"]),
                                               _ptr(g["d_up"]), _ptr(g["d_down"]), _ptr(bws), bws.numel(),
                                               _stream(stream)), "pmpe_moe_backward_private")
+        if stream is not None:
+            self._hold(stream, hidden, policy, dout, topk_idx, topk_w, self._saved_gu, ws, bws, *g.values())
         return g
 
     def backward(self, hidden, policy, dout, topk_idx=None, topk_w=None, stream=None):
@@ -516,14 +534,16 @@ class MoeLayer:
             raise PmpeError(ERR_UNSUPPORTED_SHAPE, "pmpe_moe_backward_step_workspace_size")
         if self._bws is None or self._bws.numel() < nb:
             self._bws = torch.empty(nb, dtype=torch.uint8, device=dev)
-        bws = self._bws
+        bws, ws = self._bws, self.workspace(T)
         if topk_idx is None and topk_w is None:
             topk_idx, topk_w = self._route_out
-        desc = make_desc(s, self.weights, hidden, policy, dout, self.workspace(T), topk_idx, topk_w,
+        desc = make_desc(s, self.weights, hidden, policy, dout, ws, topk_idx, topk_w,
                          saved_gu=self._saved_gu)
         _check(_lib.pmpe_moe_backward_step(ctypes.byref(desc), _ptr(dout), _ptr(g["d_router"]), _ptr(g["d_gate"]),
                                            _ptr(g["d_up"]), _ptr(g["d_down"]), _ptr(d_hidden), _ptr(bws),
                                            bws.numel(), _stream(stream)), "pmpe_moe_backward_step")
+        if stream is not None:
+            self._hold(stream, hidden, policy, dout, topk_idx, topk_w, self._saved_gu, ws, bws, *g.values(), d_hidden)
         return g, d_hidden
 
     def backward_input(self, hidden, policy, dout, topk_idx=None, topk_w=None, stream=None) -> torch.Tensor:
@@ -543,13 +563,15 @@ class MoeLayer:
             raise PmpeError(ERR_UNSUPPORTED_SHAPE, "pmpe_moe_backward_input_workspace_size")
         if self._bws is None or self._bws.numel() < nb:
             self._bws = torch.empty(nb, dtype=torch.uint8, device=dev)
-        bws = self._bws
+        bws, ws = self._bws, self.workspace(T)
         if topk_idx is None and topk_w is None:
             topk_idx, topk_w = self._route_out
-        desc = make_desc(s, self.weights, hidden, policy, dout, self.workspace(T), topk_idx, topk_w,
+        desc = make_desc(s, self.weights, hidden, policy, dout, ws, topk_idx, topk_w,
                          saved_gu=self._saved_gu)
         _check(_lib.pmpe_moe_backward_input(ctypes.byref(desc), _ptr(dout), _ptr(d_hidden), _ptr(bws), bws.numel(),
                                             _stream(stream)), "pmpe_moe_backward_input")
+        if stream is not None:
+            self._hold(stream, hidden, policy, dout, topk_idx, topk_w, self._saved_gu, ws, bws, d_hidden)
         return d_hidden
 
 

@@ -172,6 +172,39 @@ def test_tensors_that_are_not_the_layers_rows_are_refused():
             layer.backward_routed(x, pol, dout)
 
 
+@pytest.mark.parametrize("given", [False, True])
+def test_memory_freed_while_the_other_stream_has_yet_to_run(given):
+    """Neither a call's arguments nor its results are handed out again before
+    the stream that it was given is done with them, nor scratch that a larger
+    call replaced."""
+    shape, layer, h, pol, seed = build("large_experts_decode")
+    want, idx, w = own_route(shape, layer, h, pol)
+    dout = torch.randn((shape.T, shape.H), generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).cuda()
+    route = dict(route=(idx, w)) if given else {}
+    back = layer.backward_routed if given else layer.backward
+    layer.forward(h, pol, **route)
+    grads, dh = back(h, pol, dout)[:2]
+    layer._bws = None  # a scratch of this call's own
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(40_000_000)  # some 20 ms
+    a, b, c = h.clone(), pol.clone(), dout.clone()
+    kept = torch.empty_like(a)
+    torch.cuda.current_stream().synchronize()
+    layer.forward(a, b, stream=s, **route)                # the result is dropped at once
+    layer.forward(a, b, out=kept, stream=s, **route)
+    got = back(a, b, c, stream=s)
+    g, d = got[0]["d_gate"], got[1]
+    layer._bws = None
+    del a, b, c, got
+    other = [torch.full_like(h, 7.0) for _ in range(6)] + [torch.full((1 << 20,), 7.0, device="cuda") for _ in range(64)]
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(kept, want) and torch.equal(g, grads["d_gate"]) and torch.equal(d, dh)
+    assert all((o == 7).all() for o in other)
+
+
 # ------------------------------------------------------- the block together
 
 def block(layer, router, x, res, wn, wr, bias, policy, dout, max_norm, load):
