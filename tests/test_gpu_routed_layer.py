@@ -75,6 +75,45 @@ def test_the_layers_own_route_given_back(name, saved):
     assert (d[allow][:, :shape.E_pub] == 0).all() and (d[~allow][:, shape.E_pub:] == 0).all()
 
 
+LARGE = {
+    "prefill": LayerShape(T=4096, H=2048, I=768, E_pub=128, E_priv=32, E_sh=0, k=8, renormalize=True),
+    "largest_prefill": LayerShape(T=16384, H=2048, I=768, E_pub=128, E_priv=32, E_sh=0, k=8, renormalize=True),
+    "shared_pool_softmax": LayerShape(T=8191, H=2048, I=1408, E_pub=64, E_priv=16, E_sh=2, k=6, renormalize=False),
+    "small_experts": LayerShape(T=5001, H=256, I=128, E_pub=40, E_priv=16, E_sh=1, k=6, renormalize=True),
+}
+
+
+@pytest.mark.parametrize("name", list(LARGE) + ["large_experts_decode", "one_token"])
+def test_a_given_route_after_another_batch(name):
+    """Prompt batches of up to 129 router tiles, and small ones: with the
+    workspace as another batch left it, the own route given back gives the
+    layer's output, audit and private gradients bit by bit."""
+    from paper_2608_06690_gb300 import inputs as inp
+    shape = LARGE[name] if name in LARGE else SHAPES[name][0]
+    layer = pmpe.MoeLayer(shape, inp.make_weights(shape, 21, device="cuda"))
+    h, other = (inp.make_hidden(shape, seed, device="cuda") for seed in (21, 22))
+    pol = inp.policy_iid_mixed(shape.T, 23).cuda()
+    dout = torch.randn((shape.T, shape.H), generator=torch.Generator().manual_seed(24)).to(torch.bfloat16).cuda()
+    a, b = new_audit(shape), new_audit(shape)
+    want, idx, w = own_route(shape, layer, h, pol, a)
+    grads, _ = layer.backward(h, pol, dout)
+    _, idx2, w2 = own_route(shape, layer, other, (pol != 1).to(torch.uint8))  # the other pool of most tokens
+    assert not torch.equal(idx, idx2)
+    got = layer.forward(h, pol, route=(idx, w), audit=b)
+    g, dh, dw = layer.backward_routed(h, pol, dout)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(a, b)
+    for n in ("d_gate", "d_up", "d_down"):
+        assert torch.equal(g[n], grads[n]), n
+    assert torch.isfinite(dh).all() and torch.isfinite(dw).all()
+    # d_w: the picks' outputs along dout, from what the forward kept of them
+    y = (got.double() * dout.double()).sum(1)
+    if shape.E_sh == 0:  # out = sum_j w_j y_j: BF16 rows and output, 2^-8 each of the terms
+        total, size = (dw.double() * w.double()).sum(1), (dw.double() * w.double()).abs().sum(1)
+        scale = (got.double().abs() * dout.double().abs()).sum(1)
+        assert ((total - y).abs() <= 2.0 ** -7 * (size + scale)).all()
+
+
 def test_picks_that_cannot_be_taken():
     shape, layer, h, pol, _ = build("renorm")
     _, idx, w = own_route(shape, layer, h, pol)
