@@ -420,7 +420,8 @@ PMPE_API int pmpe_rms_norm(const pmpe_rms_norm_desc *d, void *stream);
  *   dw = sum_t dy h rstd
  * All matrices [T, H] without gaps.  dx may be the same memory as d_h, or as
  * dy or h of the same type.  The sum over the rows is FP32, in an order that
- * depends on T and H alone. */
+ * depends on T and H alone; its error does not grow with T (310 x 2^-24 of the
+ * terms' magnitudes at most). */
 typedef struct pmpe_rms_norm_backward_desc {
     int T, H;
     int type;              /* of h */

@@ -147,8 +147,12 @@ __global__ void __launch_bounds__(kThreads, kCtas) rms_norm_bwd_kernel(const Nor
 // columns a CTA spread the sums over the SMs (T = 4096, 2048 columns, the whole
 // backward: 17.2 us, with 32 columns 17.9, with 8 17.2; a loop that loads one
 // row after another where fewer than kDeep are left 18.1).
+// pair: null, or [2, H], the sum of the earlier row blocks and what its
+// roundings lost, to which this block's sum is added; dw then is written with
+// the last block.
 constexpr int kDwCols = 16, kStrands = 1024 / kDwCols, kDeep = 8;
-__global__ void __launch_bounds__(kDwCols * kStrands) rms_norm_dw_kernel(const float *part, int n, int H, float *dw)
+__global__ void __launch_bounds__(kDwCols * kStrands) rms_norm_dw_kernel(const float *part, int n, int H, float *dw, float *pair,
+                                                                       int first, int last)
 {
     __shared__ float s[kStrands][kDwCols + 1];
     pdl_trigger();
@@ -170,7 +174,17 @@ __global__ void __launch_bounds__(kDwCols * kStrands) rms_norm_dw_kernel(const f
 #pragma unroll
         for (int q = 0; q < kStrands; q += 32) a += s[q + lane][warp];
         a = warp_sum(a);
-        if (lane == 0 && blockIdx.x * kDwCols + warp < H) dw[blockIdx.x * kDwCols + warp] = a;
+        const int at = blockIdx.x * kDwCols + warp;
+        if (lane == 0 && at < H) {
+            if (pair) {
+                const float hi = first ? 0.f : pair[at], lo = first ? 0.f : pair[H + at];
+                const float sum = hi + a, bb = sum - hi, lost = lo + ((hi - (sum - bb)) + (a - bb));
+                a = sum + lost;
+                pair[at] = sum;
+                pair[H + at] = lost;
+            }
+            if (last) dw[at] = a;
+        }
     }
 }
 
@@ -194,6 +208,13 @@ int bwd_ctas(int T, int H)
     return std::max(1, std::min((T + rows - 1) / rows, kSms * std::max(1, sm_threads(H) / threads_for(H))));
 }
 
+// Rows of a launch at most: a thread sums its rows' part of dw one after
+// another, kChain of them, so that dw's error does not grow with T.  (Pairs
+// kept in the row kernel, joined every 64 rows, took its registers: 60000 x
+// 2048 194 -> 208 us, 1000 x 16384 77 -> 88.)
+constexpr int kChain = 256;
+long long block_rows(int H) { return (long long)kChain * bwd_ctas(1 << 30, H) * (H <= 256 ? kWarpRows : 1); }
+
 template <typename T, typename G, typename X, bool kVec> cudaError_t launch(const NormBwdParams &p, cudaStream_t st)
 {
     const int threads = threads_for(p.H), grid = bwd_ctas(p.T, p.H);
@@ -215,32 +236,40 @@ template <typename T, bool kVec> cudaError_t by_types(const NormBwdParams &p, bo
 }  // namespace
 
 // The partial sums, aligned for eight of them at a time wherever the workspace
-// starts: what is computed how does not depend on its address.
+// starts (what is computed how does not depend on its address), and the row
+// blocks' pair.
 constexpr size_t kPartAlign = 32, kWorkspaceAlign = 16;
 size_t rms_norm_backward_workspace_bytes(int T, int H)
 {
-    return (size_t)bwd_ctas(T, H) * H * sizeof(float) + (kPartAlign - kWorkspaceAlign);
+    return ((size_t)bwd_ctas(T, H) + (T > block_rows(H) ? 2 : 0)) * H * sizeof(float) + (kPartAlign - kWorkspaceAlign);
 }
 
 cudaError_t launch_rms_norm_backward(const pmpe_rms_norm_backward_desc &d, cudaStream_t st)
 {
     float *part = reinterpret_cast<float *>(((uintptr_t)d.workspace + (kPartAlign - 1)) & ~(uintptr_t)(kPartAlign - 1));
-    NormBwdParams p;
-    p.h = d.h; p.dy = d.dy; p.d_h = d.d_h; p.w = d.weight; p.rstd = d.rstd; p.dx = d.dx;
-    p.part = d.dw ? part : nullptr;
-    p.T = d.T; p.H = d.H; p.w_f32 = d.weight_type == PMPE_F32;
-    const bool g32 = d.dy_type == PMPE_F32, x32 = d.dx_type == PMPE_F32;
+    const bool g32 = d.dy_type == PMPE_F32, x32 = d.dx_type == PMPE_F32, h32 = d.type == PMPE_F32, w32 = d.weight_type == PMPE_F32;
     // eight elements an access where every row of every operand allows it
-    const bool h32 = d.type == PMPE_F32;
-    const bool vec = d.H % 8 == 0 && aligned8(d.dy, g32) && aligned8(d.h, h32) && aligned8(d.weight, p.w_f32) &&
-                     aligned8(d.d_h, x32) && aligned8(d.dx, x32);
-    cudaError_t err;
-    if (d.type == PMPE_F32) err = vec ? launch<float, float, float, true>(p, st) : launch<float, float, float, false>(p, st);
-    else if (d.type == PMPE_BF16) err = vec ? by_types<bf16, true>(p, g32, x32, st) : by_types<bf16, false>(p, g32, x32, st);
-    else err = vec ? by_types<__half, true>(p, g32, x32, st) : by_types<__half, false>(p, g32, x32, st);
-    if (err != cudaSuccess || !d.dw) return err;
-    return launch_pdl(rms_norm_dw_kernel, dim3((d.H + kDwCols - 1) / kDwCols), dim3(kDwCols * kStrands), 0, st, (const float *)part,
-                      bwd_ctas(d.T, d.H), d.H, d.dw);
+    const bool vec = d.H % 8 == 0 && aligned8(d.dy, g32) && aligned8(d.h, h32) && aligned8(d.weight, w32) && aligned8(d.d_h, x32) &&
+                     aligned8(d.dx, x32);
+    const long long rows = d.dw ? std::min<long long>(d.T, block_rows(d.H)) : d.T;
+    float *pair = rows < d.T ? part + (size_t)bwd_ctas(d.T, d.H) * d.H : nullptr;
+    for (long long t = 0; t < d.T; t += rows) {
+        auto from = [&](auto *p, bool f32) { return p ? (decltype(p))((uintptr_t)p + (size_t)t * d.H * (f32 ? 4 : 2)) : p; };
+        NormBwdParams p;
+        p.h = from(d.h, h32); p.dy = from(d.dy, g32); p.d_h = from(d.d_h, x32); p.dx = from(d.dx, x32);
+        p.w = d.weight; p.rstd = d.rstd + t;
+        p.part = d.dw ? part : nullptr;
+        p.T = (int)std::min<long long>(rows, d.T - t); p.H = d.H; p.w_f32 = w32;
+        cudaError_t err;
+        if (d.type == PMPE_F32) err = vec ? launch<float, float, float, true>(p, st) : launch<float, float, float, false>(p, st);
+        else if (d.type == PMPE_BF16) err = vec ? by_types<bf16, true>(p, g32, x32, st) : by_types<bf16, false>(p, g32, x32, st);
+        else err = vec ? by_types<__half, true>(p, g32, x32, st) : by_types<__half, false>(p, g32, x32, st);
+        if (err == cudaSuccess && d.dw)
+            err = launch_pdl(rms_norm_dw_kernel, dim3((d.H + kDwCols - 1) / kDwCols), dim3(kDwCols * kStrands), 0, st, (const float *)part,
+                             bwd_ctas(p.T, d.H), d.H, d.dw, pair, t == 0 ? 1 : 0, t + rows >= d.T ? 1 : 0);
+        if (err != cudaSuccess) return err;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace pmpe

@@ -261,6 +261,26 @@ def test_backward_does_not_go_by_the_workspaces_address(pmpe, T, H):
         assert dw is got[-1][1] or torch.equal(dw, got[0][1])
 
 
+@pytest.mark.parametrize("T,H", [(400_000, 4104), (2 * 38_912 + 77, 8200), (466_945, 300), (2 * 933_888 + 5, 8), (933_888, 8), (38_912, 4104)])
+def test_backward_weights_sum_over_many_rows(pmpe, T, H):
+    """The weight gradient's error does not grow with the rows: 256 of a thread
+    in sequence, eight warps, 29 partials a strand, seven steps of their tree,
+    four of the pairs, two roundings of a term: 306 x 2^-24 of the terms'
+    magnitudes.  Terms of one size and sign are the worst case for a sequence."""
+    g = torch.Generator("cuda").manual_seed(T)
+    h = torch.ones((T, H), dtype=BF16, device="cuda")
+    rstd = torch.full((T,), 0.7, device="cuda")
+    w = torch.ones(H, dtype=BF16, device="cuda")
+    for dy in (torch.full((T, H), 1.1, dtype=BF16, device="cuda"), torch.rand((T, H), generator=g, device="cuda", dtype=BF16) - 0.25):
+        dx, dw = pmpe.rms_norm_backward(dy, h, w, rstd)
+        want, size = (sum(f(p.double()).sum(0) for p in dy.split(20000)) * float(rstd[0]) for f in (lambda v: v, torch.abs))
+        assert ((dw.double() - want).abs() <= 306 * 2.0 ** -24 * size).all(), float(((dw.double() - want).abs() / size).max() * 2 ** 24)
+        tail, _ = pmpe.rms_norm_backward(dy[-9:].contiguous(), h[-9:].contiguous(), w, rstd[-9:].contiguous())
+        assert torch.equal(dx[-9:], tail)
+        only, none = pmpe.rms_norm_backward(dy, h, w, rstd, need_dw=False)
+        assert none is None and torch.equal(only, dx)
+
+
 def test_backward_no_rows(pmpe):
     e = torch.empty((0, 64), dtype=BF16, device="cuda")
     dx, dw = pmpe.rms_norm_backward(e, e, randn((64,), 1, BF16), torch.empty(0, device="cuda"))
