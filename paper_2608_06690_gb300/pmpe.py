@@ -43,8 +43,9 @@ def _load_ops():
         ops = importlib.import_module("._ops", __package__)
     except ImportError as e:
         return _NoOps(e)
-    if ops.built_for != torch.__version__:
-        return _NoOps(f"built for PyTorch {ops.built_for}, this is {torch.__version__}")
+    built_for = getattr(ops, "built_for", "of another version")
+    if built_for != torch.__version__:
+        return _NoOps(f"built for PyTorch {built_for}, this is {torch.__version__}")
     return ops
 
 

@@ -256,7 +256,7 @@ for call in (lambda: pmpe.rms_norm(x, x[0]), lambda: pmpe.rms_norm_backward(x, x
 """
 
 
-@pytest.mark.parametrize("kind", ["missing", "broken", "another"])
+@pytest.mark.parametrize("kind", ["missing", "broken", "another", "older"])
 def test_the_layer_does_not_need_the_operators_module(pmpe, kind, tmp_path):
     """Without _ops, with one that does not load or one that was built for
     another PyTorch, the layer is there and the operators say what is missing."""
@@ -275,6 +275,9 @@ def test_the_layer_does_not_need_the_operators_module(pmpe, kind, tmp_path):
     elif kind == "another":
         (to / "_ops.py").write_text("built_for = '1.0'")
         says = "built for PyTorch 1.0"
+    elif kind == "older":
+        (to / "_ops.py").write_text("")
+        says = "of another version"
     subprocess.run([sys.executable, "-c", WITHOUT_OPS, says], cwd=tmp_path, check=True, env=dict(os.environ, PYTHONPATH=str(tmp_path)))
 
 
