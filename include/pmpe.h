@@ -396,7 +396,7 @@ PMPE_API int pmpe_moe_forward_noalloc(const pmpe_moe_desc *d, void *stream);
  * Sums and products are FP32 (64 bits where squares leave FP32's range).  A
  * NaN or an infinity stays in its row.  An output may be the same memory as an
  * input of the same type and row pitch (h on residual, say); other overlaps
- * are not allowed. */
+ * of h and y are refused. */
 typedef struct pmpe_rms_norm_desc {
     int T, H;              /* rows >= 0, columns 1 .. PMPE_MAX_NORM_WIDTH */
     int type;              /* of x, residual, h and an unquantised y */

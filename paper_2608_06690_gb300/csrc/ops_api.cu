@@ -21,6 +21,26 @@ int sm_count(int *n)
     return done(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
 }
 
+// Rows of `bytes` bytes each, `pitch` bytes apart.
+struct Rows {
+    const void *at;
+    int64_t n, bytes, pitch;
+};
+// Whether a run of memory holds a byte of the rows.
+bool meets(const void *p, int64_t bytes, const Rows &r)
+{
+    if (!p || !r.at || r.n == 0) return false;
+    const int64_t lo = (int64_t)((uintptr_t)p - (uintptr_t)r.at), hi = lo + bytes;
+    const int64_t i = lo < r.bytes ? 0 : (lo - r.bytes) / r.pitch + 1;  // the first row that ends after lo
+    return i < r.n && i * r.pitch < hi;
+}
+// Whether an output without gaps is apart from the rows, or is those rows,
+// each of which is read before it is written.
+bool may_write(const void *p, int64_t bytes, const Rows &r)
+{
+    return !meets(p, bytes, r) || (p == r.at && bytes == r.n * r.bytes && (r.n == 1 || r.pitch == r.bytes));
+}
+
 bool groups_ok(int pool, int groups, int top, int k)
 {
     return groups >= 1 && groups <= 32 && pool % groups == 0 && top >= 1 && top <= groups && top * (pool / groups) >= k;
@@ -60,6 +80,16 @@ int pmpe_rms_norm(const pmpe_rms_norm_desc *d, void *stream)
     if (!fits(d->x, d->type) || !fits(d->residual, d->type) || !fits(d->weight, d->weight_type) || !fits(d->h, d->type) ||
         (d->quant == PMPE_QUANT_NONE && !fits(d->y, d->type)) || !fits4(d->scale) || !fits4(d->rstd))
         return PMPE_ERR_UNSUPPORTED_SHAPE;
+    const int64_t T = d->T, H = d->H, e = d->type == PMPE_F32 ? 4 : 2;
+    const int64_t h_bytes = T * H * e, y_bytes = d->quant == PMPE_QUANT_NONE ? h_bytes : T * H;
+    const Rows x = {d->x, T, H * e, T > 1 ? d->x_ld * e : H * e}, res = {d->residual, T, H * e, T > 1 ? d->residual_ld * e : H * e};
+    const Rows w = {d->weight, 1, H * (d->weight_type == PMPE_F32 ? 4 : 2), 1}, h = {d->h, 1, h_bytes, 1};
+    // (8-bit rows are another type's, on none of the inputs)
+    const bool y_ok = d->quant == PMPE_QUANT_NONE ? may_write(d->y, y_bytes, x) && may_write(d->y, y_bytes, res)
+                                                  : !meets(d->y, y_bytes, x) && !meets(d->y, y_bytes, res);
+    if (!y_ok || !may_write(d->h, h_bytes, x) || !may_write(d->h, h_bytes, res) || meets(d->h, h_bytes, w) || meets(d->y, y_bytes, w) ||
+        meets(d->y, y_bytes, h))
+        return PMPE_ERR_INVALID_ARG;
     return done(launch_rms_norm(*d, (cudaStream_t)stream));
 }
 

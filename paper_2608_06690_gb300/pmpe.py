@@ -633,7 +633,7 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-6, quant=None, h_out=None
     is that of the rounded h.  ``quant``: None for y in x's type; "block" or
     "row" for y in e4m3 with an FP32 scale per row and 128 columns or per row
     (y stands for ``y.float() * scale``).  ``h_out``: where h goes (may be
-    ``residual`` or ``x``).  ``stream``: the stream to run on (default: the
+    ``residual`` or ``x``; anything else that shares their memory is refused).  ``stream``: the stream to run on (default: the
     current one).  H up to 16384, eps at least 1e-20."""
     if stream is not None:
         return _on(stream, rms_norm, x, x, weight, residual, eps, quant, h_out)

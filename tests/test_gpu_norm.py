@@ -117,6 +117,29 @@ def test_h_in_place(pmpe, where, T):
     assert got.h.data_ptr() == (b if where == "residual" else a).data_ptr()
 
 
+def test_h_beside_its_inputs(pmpe):
+    """h_out in the same buffer: refused where it shares memory in another
+    order, taken where it lies between rows or after them."""
+    w = randn((64,), 1, F32)
+    flat = randn((4096,), 2, F32)
+    x = flat.as_strided((3, 64), (1000, 1))
+    res = randn((3, 64), 3, F32)
+    want = pmpe.rms_norm(x, w, residual=res)
+    for at in (64, 500, 1000 - 192, 2064, 3000):
+        got = pmpe.rms_norm(x, w, residual=res, h_out=flat[at:at + 192].view(3, 64))
+        assert torch.equal(got.h, want.h) and torch.equal(got.y, want.y)
+    for at in (0, 63, 1000 - 191, 1000, 1063, 2063):
+        with pytest.raises(pmpe.PmpeError):
+            pmpe.rms_norm(x, w, residual=res, h_out=flat[at:at + 192].view(3, 64))
+    rows = randn((4, 64), 4, F32)
+    for a, b in ((rows[:3], rows[1:]), (rows[1:], rows[:3])):
+        with pytest.raises(pmpe.PmpeError):
+            pmpe.rms_norm(res, w, residual=a, h_out=b)
+    one = flat.as_strided((1, 64), (1, 1))
+    n = pmpe.rms_norm(one, w, residual=res[:1], h_out=flat[64:128].view(1, 64))
+    assert torch.equal(n.h, one + res[:1])
+
+
 @pytest.mark.parametrize("quant", [None, "block", "row"])
 @pytest.mark.parametrize("T,H", [(6, 384), (1200, 256)])
 def test_rows_of_zeros_infinities_and_nans_stay_in_their_rows(pmpe, T, H, quant):

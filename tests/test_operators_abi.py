@@ -74,6 +74,23 @@ def test_rms_norm_refusals(pmpe):
     assert rc(T=0, x=None, weight=None, y=None) == pmpe.OK
 
 
+def test_rms_norm_outputs_that_share_memory_are_refused(pmpe):
+    """Rows of 256 BF16 values (512 bytes), four of them, 600 elements apart."""
+    f = pmpe._lib.pmpe_rms_norm
+    far = 1 << 20
+    base = dict(T=4, H=256, type=1, weight_type=1, quant=0, eps=1e-6, x=P, residual=P + far, weight=P + 2 * far, x_ld=600, residual_ld=256,
+                h=P + 3 * far, y=P + 4 * far, scale=None, rstd=P + 5 * far)
+    bad = [dict(h=P), dict(y=P),                                          # on rows of another pitch
+           dict(h=P - 2046), dict(h=P + 510), dict(h=P + 3600 + 510), dict(y=P + 1000), dict(y=P + far + 512), dict(h=P + far + 2),
+           dict(h=P + far - 2), dict(y=P + far + 2046), dict(h=P + 2 * far), dict(y=P + 2 * far + 510), dict(y=P + 2 * far - 2046),
+           dict(h=P + 4 * far), dict(h=P + 4 * far + 2046), dict(h=P + far, x=P + far + 512, x_ld=256)]
+    for quant in (1, 2):
+        bad += [dict(quant=quant, scale=P + 6 * far, y=P + far), dict(quant=quant, scale=P + 6 * far, y=P + far - 1023),
+                dict(quant=quant, scale=P + 6 * far, y=P + far + 2047)]
+    for over in bad:
+        assert f(desc(RmsNormDesc, base, **over), None) == pmpe.ERR_INVALID_ARG, over
+
+
 def test_rms_norm_backward_refusals(pmpe):
     f, size = pmpe._lib.pmpe_rms_norm_backward, pmpe._lib.pmpe_rms_norm_backward_workspace_size
     need = size(4, 256)
