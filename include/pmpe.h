@@ -393,6 +393,7 @@ PMPE_API int pmpe_moe_forward_noalloc(const pmpe_moe_desc *d, void *stream);
  *   rstd = 1 / sqrt(mean_c h_c^2 + eps)
  *   y = h rstd weight              rounded to `type`, or in 8 bits:
  *   s = max(amax |h rstd weight| / 448, 2^-126), y = e4m3(h rstd weight / s)
+ *                                  with s before its own rounding to FP32
  * Sums and products are FP32 (64 bits where squares leave FP32's range).  A
  * NaN or an infinity stays in its row.  An output may be the same memory as an
  * input of the same type and row pitch (h on residual, say); other overlaps
@@ -455,10 +456,15 @@ PMPE_API int pmpe_rms_norm_backward(const pmpe_rms_norm_backward_desc *d, void *
  *   selection: the k largest choices, equal ones by the lower id
  *   weights:  score * scale, divided by the sum of the k scores when
  *             renormalised (sigmoid: that sum + 1e-20)
- * The selection is that of exact arithmetic on the given logits and biases,
- * whatever FP32 rounds to the same value.  A logit of +inf counts as the
- * largest finite one; an expert with a bias of -inf is never chosen.  Where
- * fewer than k experts can be chosen, the rest of the row is -1 with weight 0. */
+ * Without a bias the selection compares the logits themselves.  With one, and
+ * where groups count sums, it is that of choices evaluated in 64 bits, whatever
+ * FP32 rounds to the same value: equal 64-bit choices go by the lower id (two
+ * sigmoids above 37 or so, scores that vanish beside an equal bias), and those
+ * within a 64-bit rounding of one another have no order of their own.  A logit
+ * of +inf counts as the largest finite one; an expert with a bias of -inf is
+ * never chosen.  Where fewer than k experts can be chosen, the rest of the row
+ * is -1 with weight 0.  In the weights and the gradient, which are FP32, a
+ * sigmoid of a logit below -88 is 0. */
 typedef struct pmpe_route_desc {
     int T;                 /* tokens >= 0 */
     int E_pub, E_priv;     /* k <= E_pub <= 256; E_priv 0 (one pool, policy NULL) or k .. 256 */

@@ -4,7 +4,8 @@
 //   h = round(x + residual)            (x itself without a residual)
 //   r = 1 / sqrt(mean_c h_c^2 + eps)
 //   y = h r w                          in the input's type, or
-//   s = max(amax |y| / 448, 2^-126),  q = e4m3(y / s)   per 128 columns or per row
+//   s = max(amax |y| / 448, 2^-126),  q = e4m3(y / s)   per 128 columns or per row,
+//   the quotient by s before its rounding to FP32
 //
 // h is rounded to its type before the norm, so that the backward, which reads
 // the stored h, differentiates what the forward computed.  Everything between

@@ -10,7 +10,11 @@
 // A CTA takes a row, 8 columns a thread up to 6144 columns (up to 256 columns a
 // warp does, eight of them a CTA), and goes on to the rows a grid further, the next of which is
 // on its way into registers meanwhile.  16 columns a thread need more than 128
-// registers for that and spill (27 us where 8 columns take 20).
+// registers for that and spill (27 us where 8 columns take 20).  Bytes that a
+// thread spills: up to 256 columns 0 to 32 (48 to 84 where accesses are element
+// by element and a type is FP32), from 6145 columns 0 to 64 (8 to 144), above
+// 8192, where 1024 threads have 64 registers each, 476 to 700; FP32 rows of odd
+// width 16 elsewhere.
 #include <algorithm>
 
 #include "norm_rows.cuh"
@@ -189,12 +193,16 @@ __global__ void __launch_bounds__(kDwCols * kStrands) rms_norm_dw_kernel(const f
 }
 
 // Threads of a CTA, and the CTAs that an SM holds: 768 threads at 80 registers
-// (T = 4096, 2048 columns, BF16 with an FP32 dy: 18.6 us (18.1 now), with 512 19.9, with
+// (T = 4096, 2048 columns, BF16 with an FP32 dy: 18.6 us (17.2 now), with 512 19.9, with
 // 1024 at 64 registers 21.3); wider rows' kernels take about 96, from 6145
 // columns on, with 16 columns a thread, 128.  A grid beyond them would run its
-// last CTAs in a second wave.  (T = 3276, 5120 columns, BF16: 32.4 us with 8
-// columns a thread, 43.5 with 16; T = 2340, 7168 columns 37.6 with 16, 35.6 with 8, FP32 30.0
-// and 32.6.)
+// last CTAs in a second wave.  T = 3276, 5120 columns, BF16: 32.4 us
+// with 8 columns, 43.5 with 16 (now, with 8 columns and d_h, 34.5 with an FP32
+// dy and 42.7 with a BF16 one).  At 6400 to 8192 columns, 16 columns against 8
+// (1024 threads at 64 registers): FP32 rows 55 to 58 us against 60 to 63 (45 to 48
+// and 49 to 50 without d_h), BF16 rows 27 to 28 against 29 to 30 without d_h, but
+// 35 to 36 against 32 to 33 with it (FP32 dy 40 to 42, 38 to 39): one rule for
+// all, as the kernels of 8 columns would be as many again.
 int sm_threads(int H) { return H <= 2048 ? 768 : H <= 4096 ? 640 : 512; }
 int threads_for(int H)
 {
