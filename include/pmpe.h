@@ -373,9 +373,9 @@ PMPE_API int pmpe_moe_forward_noalloc(const pmpe_moe_desc *d, void *stream);
  *
  * The norm of the residual stream before the layer, routing from given logits
  * where a model's router is not the layer's own, and the clipping of the
- * gradients that the backward gives.  At most 2^30 rows.  Pointers need the
- * alignment of their elements only; rows of a multiple of eight elements that
- * are aligned to eight elements are read with wide loads. */
+ * gradients that the backward gives.  At most 2^30 rows or tensors.  Pointers
+ * need the alignment of their elements only; rows of a multiple of eight
+ * elements that are aligned to eight elements are read with wide loads. */
 
 /* Element types. */
 #define PMPE_F32 0
@@ -508,7 +508,7 @@ typedef struct pmpe_grad {
  * array, read before the call returns; fewer than 2^31 chunks of 16 KB in all.
  * norm: device FP32.  workspace: device, 16-byte aligned, of the size below.
  * The sums' order depends on the tensors' sizes and alignment alone. */
-PMPE_API size_t pmpe_clip_workspace_size(int n); /* 0 for n < 0 */
+PMPE_API size_t pmpe_clip_workspace_size(int n); /* 0 for n < 0 or above 2^30 */
 PMPE_API int pmpe_clip_grad_norm(const pmpe_grad *grads, int n, float max_norm, float *norm, void *workspace,
                                  size_t workspace_bytes, void *stream);
 

@@ -144,12 +144,13 @@ int pmpe_route_backward(const pmpe_route_desc *d, const float *dw, void *d_logit
     return done(launch_route_scores_backward(*d, dw, d_logits, sms, (cudaStream_t)stream));
 }
 
-size_t pmpe_clip_workspace_size(int n) { return n < 0 ? 0 : clip_workspace_bytes(n); }
+size_t pmpe_clip_workspace_size(int n) { return n < 0 || n > kMaxRows ? 0 : clip_workspace_bytes(n); }
 
 int pmpe_clip_grad_norm(const pmpe_grad *grads, int n, float max_norm, float *norm, void *workspace, size_t workspace_bytes,
                         void *stream)
 {
     if (n < 0 || (n > 0 && !grads) || !(max_norm >= 0.f) || !norm) return PMPE_ERR_INVALID_ARG;
+    if (n > kMaxRows) return PMPE_ERR_UNSUPPORTED_SHAPE;
     for (int i = 0; i < n; ++i) {
         const pmpe_grad &g = grads[i];
         if (g.n < 0 || !is_type(g.type) || (g.n > 0 && !g.grad)) return PMPE_ERR_INVALID_ARG;

@@ -190,6 +190,15 @@ def test_clip_refusals(pmpe):
     assert rc([ok], nb=size(1) - 1) == pmpe.ERR_WORKSPACE
 
 
+def test_clip_refuses_more_tensors_than_it_counts(pmpe):
+    f, size = pmpe._lib.pmpe_clip_grad_norm, pmpe._lib.pmpe_clip_workspace_size
+    per = size(1)  # of a launch's 1024 tensors
+    assert size(1024) == per and size(1025) == 2 * per and size(1 << 30) == per << 20
+    for n in ((1 << 30) + 1, 2 ** 31 - 1000, 2 ** 31 - 1):
+        assert size(n) == 0
+        assert f(P, n, 1.0, P, P, 1 << 40, None) == pmpe.ERR_UNSUPPORTED_SHAPE  # before the host array is read
+
+
 def test_host_tensors_are_refused(pmpe):
     x, w = torch.zeros(2, 8), torch.ones(8)
     for call in (lambda: pmpe.rms_norm(x, w), lambda: pmpe.rms_norm_backward(x, x, w, torch.ones(2)),
