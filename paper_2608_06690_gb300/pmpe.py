@@ -384,7 +384,9 @@ class MoeLayer:
         caller orders another one's work after what the current stream has).
         ``route``: (idx, w), int32 and FP32 [T, k], as ``Router.route`` gives
         them, in the place of the layer's own router; its backward is
-        ``backward_routed``.  A pick outside the token's pool is not taken.
+        ``backward_routed``.  A pick outside the token's pool, or of -1, is
+        not taken (another expert runs in its place with weight 0, so padding
+        should hold finite numbers).
         ``unmasked_control`` runs the paper's soft-router control instead of
         the method: routing over the concatenated pool without the hard mask.
         ``save_for_backward`` also keeps the gate and up accumulators of the
