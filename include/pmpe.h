@@ -321,8 +321,8 @@ PMPE_API int pmpe_moe_forward(const pmpe_moe_desc *d, void *stream);
  * lowest expert of the pool that the token does not name, with weight 0, so
  * that every token has k rows; the audit counts it as what ran.  (A row that
  * is not finite is NaN in the gradients of the experts that it runs as, weight
- * 0 or not, as 0 x NaN is: hidden states of padding should be finite.)  Outputs,
- * audit, workspace and errors are those of pmpe_moe_forward();
+ * 0 or not, as 0 x NaN is: hidden states of padding should be finite.)
+ * Outputs, audit, workspace and errors are those of pmpe_moe_forward();
  * unmasked_control must be 0. */
 PMPE_API int pmpe_moe_forward_routed(const pmpe_moe_desc *d, void *stream);
 
