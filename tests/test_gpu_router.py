@@ -212,6 +212,56 @@ def test_near_ties_of_many_tokens(pmpe, score, top2):
     assert (w.double() - weights / weights.sum(1, keepdim=True)).abs().max() <= REL
 
 
+def choices64(z, bias, score, groups=None, top2=False):
+    """64-bit choices of one pool; the experts of the groups left out at -inf."""
+    s = 1 / (1 + torch.exp(-z.double())) if score == "sigmoid" else torch.softmax(z.double(), 1)
+    c = s + bias.double()
+    if groups:
+        v = torch.sort(c.unflatten(1, (groups[0], -1)), dim=2, descending=True).values
+        v = v[:, :, 0] + v[:, :, 1] if top2 else v[:, :, 0]
+        kept = torch.zeros(v.shape, dtype=torch.bool, device="cuda")
+        kept.scatter_(1, torch.sort(v, dim=1, descending=True, stable=True).indices[:, :groups[1]], True)
+        c = torch.where(kept.repeat_interleave(z.shape[1] // groups[0], 1), c, -torch.inf)
+    return c
+
+
+def same_choices(idx, c, k):
+    """The k largest in order, equal ones by the lower id; choices that 64 bits
+    hardly tell apart (torch's own sums may round them another way) as they come."""
+    want = torch.sort(c, dim=1, descending=True, stable=True).indices[:, :k]
+    a, d = torch.gather(c, 1, idx.long()), torch.gather(c, 1, want)
+    off = idx.long() != want
+    assert ((a - d).abs() <= 2.0 ** -50)[off].all(), (int(off.any(1).sum()), float((a - d).abs().max()))
+    assert off.any(1).double().mean() < 1e-3
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("std,mean", [(3.0, 0.0), (5.0, 0.0), (8.0, 0.0), (1.5, -15.0)])
+@pytest.mark.parametrize("bias", [0.0, 0.3])
+def test_wide_logits_with_equal_biases(pmpe, score, std, mean, bias):
+    """Where most scores are small, or saturated, most tokens are settled in 64 bits."""
+    T, E, k = 3001, 256, 8
+    z = (std * torch.randn((T, E), generator=torch.Generator().manual_seed(int(std * 10))) + mean).cuda()
+    b = torch.full((E,), bias, device="cuda")
+    idx, _ = pmpe.Router(E, 0, k, score=score).route(z, bias=b)
+    same_choices(idx, choices64(z, b, score), k)
+
+
+@pytest.mark.parametrize("mask", [-100.0, -1e4, -1e9, torch.finfo(F32).min, -np.inf])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_groups_with_masked_biases(pmpe, score, mask):
+    """One expert in sixteen masked by its bias, at a prompt's size: the bound on
+    the groups' sums goes by the largest choice, the result does not."""
+    T, E, k = 8192, 256, 8
+    g = torch.Generator().manual_seed(5)
+    z, b = (1.5 * torch.randn((T, E), generator=g)).to(BF16).cuda(), (0.05 * torch.randn(E, generator=g)).cuda()
+    b[::16] = mask
+    idx, _ = pmpe.Router(E, 0, k, score=score, groups=(8, 4), group_score="top2").route(z, bias=b)
+    c = choices64(z, b, score, (8, 4), True)
+    same_choices(idx, torch.where(c > mask / 2, c, -torch.inf), k)  # no masked one is among them
+    assert (idx % 16 != 0).all()
+
+
 @pytest.mark.parametrize("edge", [0.75, 0.5 + 2.0 ** -9, 0.6875])
 def test_choices_at_the_edge_of_a_packed_word(pmpe, edge):
     """The best two choices within a few ulps on either side of a value where
