@@ -205,9 +205,11 @@ def _inputs(case, seed):
         rows = (1.5 * _randn((case["B"], wide), seed, 5)).to(DTYPES[case["dtype"]])
         st["q"] = rows[:, :case["heads"] * case["head_dim"]].view(case["B"], case["heads"], case["head_dim"])
         return st
-    new = _shuffled(_news(case), seed, 6)
-    before = _shuffled(_spread(case["B"], 0, case["before"]), seed, 7)
-    st = _plan(case, seed, torch.where(new > 0, before + new, before))
+    # (the same pairs of old and new positions for every seed, so that the pool's size is)
+    new, before = torch.tensor(_news(case)), _shuffled(_spread(case["B"], 0, case["before"]), 0, 7)
+    order = _shuffled(list(range(case["B"])), seed, 6)
+    new, before = new[order], before[order]
+    st = _plan(case, seed, before + new)
     st.update(_pools(case, st["pages"], seed))
     st["cu"] = torch.cat([torch.zeros(1, dtype=torch.int64), torch.cumsum(new, 0)]).to(torch.int32).cuda()
     st["rows"] = int(new.sum())
