@@ -383,6 +383,7 @@ PMPE_API int pmpe_moe_forward_noalloc(const pmpe_moe_desc *d, void *stream);
 #define PMPE_F32 0
 #define PMPE_BF16 1
 #define PMPE_F16 2
+#define PMPE_E4M3 3 /* of a cache: 8 bits with FP32 scales */
 
 #define PMPE_MAX_NORM_WIDTH 16384
 
@@ -513,6 +514,92 @@ typedef struct pmpe_grad {
 PMPE_API size_t pmpe_clip_workspace_size(int n); /* 0 for n < 0 or above 2^30 */
 PMPE_API int pmpe_clip_grad_norm(const pmpe_grad *grads, int n, float max_norm, float *norm, void *workspace,
                                  size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------- a decoding loop around it
+ *
+ * What a model that answers token by token needs beside the layer: the cache
+ * of its attention's keys and values in pages, the attention that reads it,
+ * and the choice of the next token. */
+
+#define PMPE_MAX_HEAD_DIM 256
+#define PMPE_MAX_PAGE_SIZE 4096
+
+/* A cache of keys and values: pages of page_size positions, of each of which
+ * it holds kv_heads keys and as many values of head_dim elements.  In 8 bits
+ * an entry is e4m3 with an FP32 scale per position and head. */
+typedef struct pmpe_kv_cache {
+    int pages, page_size;  /* 1 .. 2^30, 1 .. PMPE_MAX_PAGE_SIZE */
+    int kv_heads;          /* 1 .. 65535 */
+    int head_dim;          /* 8 .. PMPE_MAX_HEAD_DIM, a multiple of 8 (in 8 bits of 16) */
+    int type;              /* PMPE_BF16, PMPE_F16 or PMPE_E4M3 */
+    void *k, *v;           /* [pages, kv_heads, page_size, head_dim], 16-byte aligned */
+    float *k_scale, *v_scale; /* [pages, kv_heads, page_size] in 8 bits, else NULL */
+} pmpe_kv_cache;
+
+/* The sequences of a call.  Position p of sequence b lies in page
+ * table[b][p / page_size], place p % page_size.  A sequence holds lengths[b]
+ * positions, those of the call included; a length is taken as between 0 and
+ * table_width * page_size.  A table entry outside [0, pages) is no page: its
+ * positions are not written, read as zeros and not attended.  Entries that no
+ * position below the length needs are not read. */
+typedef struct pmpe_kv_sequences {
+    int B;                 /* 0 .. 65535 */
+    int table_width;       /* >= 1 entries of a sequence, table_width * page_size <= 2^30 */
+    const int32_t *table;  /* [B, table_width], rows table_ld >= table_width entries apart */
+    int64_t table_ld;
+    const int32_t *lengths;    /* [B] */
+    const int32_t *cu_seqlens; /* [B + 1]: rows cu[b] .. cu[b + 1] - 1 are sequence b's; NULL: row b is.  Where
+                                  they decrease, which sequence a row is of is not defined.  Not used by the attention */
+} pmpe_kv_sequences;
+
+/* Rows of new keys and values into the cache: the rows of sequence b are its
+ * last positions, in order.  Rows past the last sequence's, and those whose
+ * position would be negative or past the table, are not written.
+ *   16 bits: rounded to the cache's type
+ *   8 bits: s = max(amax / 448, 2^-126) over the head's elements, e4m3(x / s),
+ *           with s before its own rounding to FP32
+ * A NaN or an infinity stays in its position and head.  Sequences may share
+ * pages that the call does not write to; where two sequences write to the same
+ * position, what it holds is one of the two, or elements of both.  k and v may
+ * not share memory with the cache. */
+typedef struct pmpe_kv_append_desc {
+    int T;                 /* rows >= 0 (without cu_seqlens: B) */
+    int type;              /* of k and v: PMPE_F32, PMPE_BF16, PMPE_F16 */
+    const void *k, *v;     /* [T, kv_heads, head_dim]: heads ..._head_ld elements apart, rows ..._ld */
+    int64_t k_ld, k_head_ld, v_ld, v_head_ld;
+} pmpe_kv_append_desc;
+PMPE_API int pmpe_kv_append(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, const pmpe_kv_append_desc *d, void *stream);
+
+/* The way back: k and v [T, kv_heads, head_dim] of `type` (PMPE_F32, PMPE_BF16
+ * or PMPE_F16) without gaps, rows as an append with the same sequences takes
+ * them, rounded once.  Rows that an append would not write are zeros. */
+PMPE_API int pmpe_kv_read(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, int T, int type, void *k, void *v, void *stream);
+
+/* Attention of one query of each sequence over the sequence's positions:
+ *   s_p = scale q . k_p,  a = softmax of s over the positions seen
+ *   out = sum_p a_p v_p,  lse = ln sum_p exp(s_p)
+ * for the last `window` positions (0: all).  Query head i uses the keys and
+ * values of head i / (heads / kv_heads).  Products are exact in FP32, sums FP32;
+ * a weight enters the sum over the values in two 16-bit words (16 bits or
+ * more).  A sequence that sees nothing gives out = 0, lse = -inf.  What the
+ * cache holds at positions that are not seen, NaN say, does not matter.  The
+ * order of the sums goes by the lengths of all sequences of the call, so the same
+ * call gives the same bits.  With 8 bits a value whose scale is below 2^-24 of
+ * the largest seen loses bits. */
+typedef struct pmpe_kv_attend_desc {
+    int heads;             /* a multiple of kv_heads, at most 65535 */
+    int type;              /* of q and out: the cache's; over 8 bits PMPE_BF16 or PMPE_F16 */
+    int window;            /* >= 0 */
+    float scale;           /* finite */
+    const void *q;         /* [B, heads, head_dim]: heads q_head_ld elements apart, rows q_ld */
+    int64_t q_ld, q_head_ld;
+    void *out;             /* [B, heads, head_dim] */
+    float *lse;            /* optional [B, heads] */
+    void *workspace;       /* of the size below, 16-byte aligned */
+    size_t workspace_bytes;
+} pmpe_kv_attend_desc;
+PMPE_API size_t pmpe_kv_attend_workspace_size(int B, int heads, int kv_heads, int head_dim); /* 0 for an invalid shape */
+PMPE_API int pmpe_kv_attend(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, const pmpe_kv_attend_desc *d, void *stream);
 
 /* Zero the audit buffer (pmpe_audit_words(T, E) words). */
 PMPE_API int pmpe_audit_reset(uint32_t *audit, int T, int E, void *stream);

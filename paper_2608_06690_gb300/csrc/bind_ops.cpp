@@ -15,6 +15,7 @@
 #include <cmath>
 #include <cstring>
 #include <initializer_list>
+#include <type_traits>
 #include <utility>
 #include <vector>
 
@@ -37,8 +38,12 @@ decltype(&pmpe_route) lib_route;
 decltype(&pmpe_route_backward) lib_route_backward;
 decltype(&pmpe_clip_workspace_size) lib_clip_workspace_size;
 decltype(&pmpe_clip_grad_norm) lib_clip_grad_norm;
-PyObject *g_error;         // PmpeError(code, what)
-PyTypeObject *g_rms_norm;  // RmsNorm, a named tuple
+decltype(&pmpe_kv_append) lib_kv_append;
+decltype(&pmpe_kv_read) lib_kv_read;
+decltype(&pmpe_kv_attend_workspace_size) lib_kv_attend_workspace_size;
+decltype(&pmpe_kv_attend) lib_kv_attend;
+PyObject *g_error;           // PmpeError(code, what)
+PyTypeObject *g_rms_norm, *g_attention;  // RmsNorm and Attention, named tuples
 
 struct Refused {
     int code;
@@ -408,28 +413,203 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     });
 }
 
-// (PmpeError, RmsNorm, the library's functions' addresses in the order above)
+// The cache of the arguments k, v, k_scale, v_scale (scales: None but in 8 bits).
+pmpe_kv_cache cache_of(PyObject *const *a)
+{
+    const at::Tensor &k = tensor(a[0], "KvCache: k is a CUDA tensor"), &v = tensor(a[1], "KvCache: v is a CUDA tensor");
+    const at::Tensor *ks = optional(a[2], "KvCache: k_scale is a tensor"), *vs = optional(a[3], "KvCache: v_scale is a tensor");
+    const at::ScalarType type = k.scalar_type();
+    pmpe_kv_cache c = {};
+    c.type = type == at::kBFloat16 ? PMPE_BF16 : type == at::kHalf ? PMPE_F16 : type == at::kFloat8_e4m3fn ? PMPE_E4M3 : -1;
+    want(c.type >= 0 && k.dim() == 4 && k.is_contiguous(), "KvCache: k is [pages, kv_heads, page_size, head_dim] of BF16, FP16 or e4m3 without gaps");
+    want(v.scalar_type() == type && v.sizes() == k.sizes() && v.device() == k.device() && v.is_contiguous(), "KvCache: v is as k");
+    for (const at::Tensor *s : {ks, vs}) {
+        want((c.type == PMPE_E4M3) == (s != nullptr), "KvCache: 8-bit keys and values have scales, others none");
+        want(!s || (s->scalar_type() == at::kFloat && s->dim() == 3 && s->size(0) == k.size(0) && s->size(1) == k.size(1) &&
+                    s->size(2) == k.size(2) && s->device() == k.device() && s->is_contiguous()),
+             "KvCache: scales are FP32 [pages, kv_heads, page_size] on k's device without gaps");
+    }
+    c.pages = count(k.size(0));
+    c.kv_heads = count(k.size(1));
+    c.page_size = count(k.size(2));
+    c.head_dim = count(k.size(3));
+    c.k = k.data_ptr();
+    c.v = v.data_ptr();
+    c.k_scale = ks ? (float *)ks->data_ptr() : nullptr;
+    c.v_scale = vs ? (float *)vs->data_ptr() : nullptr;
+    return c;
+}
+pmpe_kv_sequences sequences_of(PyObject *table_, PyObject *lengths_, PyObject *cu_, at::Device dev)
+{
+    const at::Tensor &table = tensor(table_, "KvCache: table is a tensor"), &lengths = tensor(lengths_, "KvCache: lengths are a tensor");
+    const at::Tensor *cu = optional(cu_, "KvCache: cu_seqlens is a tensor");
+    want(table.scalar_type() == at::kInt && table.dim() == 2 && table.device() == dev, "KvCache: table is int32 [B, width] on the cache's device");
+    pmpe_kv_sequences s = {};
+    s.B = count(table.size(0));
+    s.table_width = count(table.size(1));
+    s.table = (const int32_t *)table.data_ptr();
+    s.table_ld = pitch(table);
+    want(is_vector(lengths, s.B, dev, at::kInt), "KvCache: lengths are int32 [B] on the cache's device");
+    want(!cu || is_vector(*cu, (int64_t)s.B + 1, dev, at::kInt), "KvCache: cu_seqlens is int32 [B + 1] on the cache's device");
+    s.lengths = (const int32_t *)lengths.data_ptr();
+    s.cu_seqlens = cu ? (const int32_t *)cu->data_ptr() : nullptr;
+    return s;
+}
+// Whether t is [rows, heads, dim] with adjacent elements; where its rows and heads are.
+bool is_rows(const at::Tensor &t, int64_t heads, int64_t dim, at::Device dev, at::ScalarType type, int64_t &ld, int64_t &head_ld)
+{
+    if (t.scalar_type() != type || t.dim() != 3 || t.size(1) != heads || t.size(2) != dim || t.device() != dev || t.stride(2) != 1) return false;
+    ld = t.size(0) > 1 ? t.stride(0) : 0;
+    head_ld = heads > 1 ? t.stride(1) : 0;
+    return true;
+}
+
+// (k, v, k_scale, v_scale): refuses what the library would refuse.
+PyObject *kv_cache(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        arguments(n, 4);
+        const pmpe_kv_cache c = cache_of(a);
+        want(THPVariable_Unpack(a[0]).is_cuda(), "KvCache: k is a CUDA tensor");
+        pmpe_kv_sequences s = {};
+        s.table_width = 1;
+        pmpe_kv_append_desc d = {};
+        run("pmpe_kv_append", [&] { return lib_kv_append(&c, &s, &d, nullptr); });
+        Py_RETURN_NONE;
+    });
+}
+
+// (k, v, k_scale, v_scale, new_k, new_v, table, lengths, cu_seqlens)
+PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        arguments(n, 9);
+        const pmpe_kv_cache c = cache_of(a);
+        const Where at(THPVariable_Unpack(a[0]), "KvCache: k is a CUDA tensor");
+        const at::Tensor &k = tensor(a[4], "KvCache.append: k is a tensor"), &v = tensor(a[5], "KvCache.append: v is a tensor");
+        const pmpe_kv_sequences s = sequences_of(a[6], a[7], a[8], at.device);
+        pmpe_kv_append_desc d = {};
+        d.type = type_of(k.scalar_type());
+        want(d.type >= 0 && is_rows(k, c.kv_heads, c.head_dim, at.device, k.scalar_type(), d.k_ld, d.k_head_ld),
+             "KvCache.append: k is [T, kv_heads, head_dim] of FP32, BF16 or FP16, its last axis without gaps, on the cache's device");
+        want(is_rows(v, c.kv_heads, c.head_dim, at.device, k.scalar_type(), d.v_ld, d.v_head_ld) && v.size(0) == k.size(0),
+             "KvCache.append: v has k's sizes and type");
+        d.T = count(k.size(0));
+        want(s.cu_seqlens || d.T == s.B, "KvCache.append: without cu_seqlens there is a row for each sequence");
+        d.k = k.data_ptr();
+        d.v = v.data_ptr();
+        run("pmpe_kv_append", [&, st = at.stream()] { return lib_kv_append(&c, &s, &d, st); });
+        for (int i = 0; i < (c.type == PMPE_E4M3 ? 4 : 2); ++i) written(THPVariable_Unpack(a[i]));
+        Py_RETURN_NONE;
+    });
+}
+
+// (k, v, k_scale, v_scale, table, lengths, cu_seqlens, rows, dtype)
+PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        arguments(n, 9);
+        const pmpe_kv_cache c = cache_of(a);
+        const Where at(THPVariable_Unpack(a[0]), "KvCache: k is a CUDA tensor");
+        const pmpe_kv_sequences s = sequences_of(a[4], a[5], a[6], at.device);
+        int64_t rows = s.B;
+        if (a[7] != Py_None) {
+            rows = PyLong_AsLongLong(a[7]);
+            if (rows == -1 && PyErr_Occurred()) return nullptr;
+            want(rows >= 0, "KvCache.read: rows are counted from 0");
+        }
+        want(s.cu_seqlens ? a[7] != Py_None : rows == s.B, "KvCache.read: rows says how many there are with cu_seqlens, without them one a sequence");
+        want(THPDtype_Check(a[8]), "KvCache.read: dtype is a dtype");
+        const at::ScalarType type = ((THPDtype *)a[8])->scalar_type;
+        want(type_of(type) >= 0, "KvCache.read: dtype is FP32, BF16 or FP16");
+        const int T = count(rows);
+        const at::Tensor k = at::detail::empty_strided_cuda({T, c.kv_heads, c.head_dim}, {(int64_t)c.kv_heads * c.head_dim, c.head_dim, 1}, type, at.device),
+                         v = at::detail::empty_strided_cuda({T, c.kv_heads, c.head_dim}, {(int64_t)c.kv_heads * c.head_dim, c.head_dim, 1}, type, at.device);
+        run("pmpe_kv_read", [&, to_k = k.data_ptr(), to_v = v.data_ptr(), st = at.stream()] {
+            return lib_kv_read(&c, &s, T, type_of(type), to_k, to_v, st);
+        });
+        return pack(&PyTuple_Type, {k, v});
+    });
+}
+
+// (k, v, k_scale, v_scale, q, table, lengths, scale or None, window)
+PyObject *kv_attend(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        arguments(n, 9);
+        const pmpe_kv_cache c = cache_of(a);
+        const Where at(THPVariable_Unpack(a[0]), "KvCache: k is a CUDA tensor");
+        const at::Tensor &q = tensor(a[4], "KvCache.attend: q is a tensor");
+        const pmpe_kv_sequences s = sequences_of(a[5], a[6], Py_None, at.device);
+        pmpe_kv_attend_desc d = {};
+        double scale = 1. / std::sqrt((double)c.head_dim);
+        if (a[7] != Py_None) {
+            scale = PyFloat_AsDouble(a[7]);
+            if (scale == -1. && PyErr_Occurred()) return nullptr;
+        }
+        const int64_t window = PyLong_AsLongLong(a[8]);
+        if (window == -1 && PyErr_Occurred()) return nullptr;
+        want(window >= 0, "KvCache.attend: window counts positions from 0");
+        d.window = (int)std::min<int64_t>(window, INT_MAX);
+        d.scale = narrow(scale);
+        const at::ScalarType type = q.scalar_type();
+        d.type = type_of(type);
+        want(c.type == PMPE_E4M3 ? d.type == PMPE_BF16 || d.type == PMPE_F16 : d.type == c.type,
+             "KvCache.attend: q is of the cache's type, over 8 bits of BF16 or FP16");
+        want(q.dim() == 3 && q.size(0) == s.B && q.size(1) >= 1 && q.size(1) % c.kv_heads == 0 &&
+                 is_rows(q, q.size(1), c.head_dim, at.device, type, d.q_ld, d.q_head_ld),
+             "KvCache.attend: q is [B, heads, head_dim], heads a multiple of kv_heads, its last axis without gaps, on the cache's device");
+        d.heads = count(q.size(1));
+        d.q = q.data_ptr();
+        const at::Tensor out = at::detail::empty_strided_cuda({s.B, d.heads, c.head_dim}, {(int64_t)d.heads * c.head_dim, c.head_dim, 1}, type, at.device),
+                         lse = empty(at.device, at::kFloat, s.B, d.heads);
+        d.workspace_bytes = lib_kv_attend_workspace_size(s.B, d.heads, c.kv_heads, c.head_dim);
+        const at::Tensor ws = empty(at.device, at::kByte, (int64_t)d.workspace_bytes);
+        d.out = out.data_ptr();
+        d.lse = (float *)lse.data_ptr();
+        d.workspace = ws.data_ptr();
+        run("pmpe_kv_attend", [&, st = at.stream()] { return lib_kv_attend(&c, &s, &d, st); });
+        return pack(g_attention, {out, lse});
+    });
+}
+
+// (PmpeError, RmsNorm, Attention, the library's functions' addresses in the order below)
 PyObject *setup(PyObject *, PyObject *args)
 {
-    unsigned long long f[7];
-    PyObject *error, *norm;
-    if (!PyArg_ParseTuple(args, "OO!KKKKKKK", &error, &PyType_Type, &norm, f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6)) return nullptr;
-    Py_INCREF(error);
-    Py_INCREF(norm);
+    PyObject *error, *norm, *attention, *at;
+    if (!PyArg_ParseTuple(args, "OO!O!O!", &error, &PyType_Type, &norm, &PyType_Type, &attention, &PyTuple_Type, &at)) return nullptr;
+    Py_ssize_t i = 0;
+    auto next = [&](auto &f) {
+        const unsigned long long v = i < PyTuple_GET_SIZE(at) ? PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(at, i)) : 0;
+        ++i;
+        f = (std::remove_reference_t<decltype(f)>)v;
+    };
+    next(lib_rms_norm);
+    next(lib_rms_norm_backward_workspace_size);
+    next(lib_rms_norm_backward);
+    next(lib_route);
+    next(lib_route_backward);
+    next(lib_clip_workspace_size);
+    next(lib_clip_grad_norm);
+    next(lib_kv_append);
+    next(lib_kv_read);
+    next(lib_kv_attend_workspace_size);
+    next(lib_kv_attend);
+    if (PyErr_Occurred()) return nullptr;
+    if (i != PyTuple_GET_SIZE(at)) {
+        PyErr_SetString(PyExc_TypeError, "setup: another number of functions");
+        return nullptr;
+    }
+    for (PyObject *o : {error, norm, attention}) Py_INCREF(o);
     g_error = error;
     g_rms_norm = (PyTypeObject *)norm;
-    lib_rms_norm = (decltype(lib_rms_norm))f[0];
-    lib_rms_norm_backward_workspace_size = (decltype(lib_rms_norm_backward_workspace_size))f[1];
-    lib_rms_norm_backward = (decltype(lib_rms_norm_backward))f[2];
-    lib_route = (decltype(lib_route))f[3];
-    lib_route_backward = (decltype(lib_route_backward))f[4];
-    lib_clip_workspace_size = (decltype(lib_clip_workspace_size))f[5];
-    lib_clip_grad_norm = (decltype(lib_clip_grad_norm))f[6];
+    g_attention = (PyTypeObject *)attention;
     Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void *)name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(rms_norm), FAST(rms_norm_backward), FAST(route), FAST(route_backward), FAST(clip_grad_norm),
+                         FAST(kv_cache), FAST(kv_append), FAST(kv_read), FAST(kv_attend),
                          {"router", router, METH_VARARGS, nullptr}, {"setup", setup, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods};

@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cuda_fp16.h>
+#include <cuda_fp8.h>
 
 #include "pmpe_internal.cuh"
 
@@ -167,6 +168,9 @@ template <bool kVec, typename T> __device__ __forceinline__ void store_raw(T *p,
     }
 }
 
+// Aligned for eight elements at a time.
+inline bool aligned8(const void *q, bool f32) { return ((uintptr_t)q & (f32 ? 31u : 15u)) == 0; }
+
 template <typename V> __device__ __forceinline__ V warp_sum(V v)
 {
 #pragma unroll
@@ -187,6 +191,35 @@ __device__ __forceinline__ float max_magnitude(float a, float b)
     float r;
     asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
+}
+
+// Eight bits: e4m3 with a scale.
+constexpr float kMinScale = 1.17549435e-38f;  // 2^-126: the smallest scale, so that its reciprocal is finite
+
+// A factor in two words: v times 448 / amax with one rounding in all, so that
+// a value goes to the e4m3 neighbour of the exact quotient but within 2^-24 of
+// the middle between two.
+struct Divide {
+    float hi, lo;
+};
+// For values u of a block whose largest is amax in magnitude and which stand
+// for u m: the scale s = max(amax m / 448, 2^-126) and the factor u -> u m / s.
+__device__ __forceinline__ Divide divide_by(float amax, float m, float &s)
+{
+    amax = fabsf(amax);
+    s = max_nan(amax * m * (1.f / 448.f), kMinScale);
+    if (!(s > kMinScale)) return {m * 0x1p126f, 0.f};  // zeros (or NaN)
+    // the product's remainder is exact in one fused operation
+    const float inv = __frcp_rn(amax), hi = 448.f * inv;
+    return {hi, hi > 0.f ? fmaf(-hi, amax, 448.f) * inv : 0.f};
+}
+__device__ __forceinline__ uint32_t e4m3x2(float a, float b)
+{
+    return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ float2 e4m3x2_to_f32(uint32_t two)
+{
+    return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3)));
 }
 
 }  // namespace pmpe

@@ -20,8 +20,6 @@
 // took 14.6 to 17.7 us for the 12.6.)
 #include <algorithm>
 
-#include <cuda_fp8.h>
-
 #include "norm_rows.cuh"
 
 namespace pmpe {
@@ -40,30 +38,6 @@ template <bool kWarpRow, typename V> __device__ __forceinline__ V row_sum(V v, V
     if (lane == 0) s_red[threadIdx.x >> 5] = v;
     __syncthreads();
     return warp_sum(lane < warps ? s_red[lane] : V(0));
-}
-
-constexpr float kMinScale = 1.17549435e-38f;  // 2^-126: the smallest scale, so that its reciprocal is finite
-
-// A factor in two words: v times 448 / amax with one rounding in all, so that
-// a value goes to the e4m3 neighbour of the exact quotient but within 2^-24 of
-// the middle between two.
-struct Divide {
-    float hi, lo;
-};
-// For values u of a block whose largest is amax in magnitude and which stand
-// for u m: the scale s = max(amax m / 448, 2^-126) and the factor u -> u m / s.
-__device__ __forceinline__ Divide divide_by(float amax, float m, float &s)
-{
-    amax = fabsf(amax);
-    s = max_nan(amax * m * (1.f / 448.f), kMinScale);
-    if (!(s > kMinScale)) return {m * 0x1p126f, 0.f};  // zeros (or NaN)
-    // the product's remainder is exact in one fused operation
-    const float inv = __frcp_rn(amax), hi = 448.f * inv;
-    return {hi, hi > 0.f ? fmaf(-hi, amax, 448.f) * inv : 0.f};
-}
-__device__ __forceinline__ uint32_t e4m3x2(float a, float b)
-{
-    return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
 
 struct NormParams {

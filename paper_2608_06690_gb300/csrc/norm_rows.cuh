@@ -1,5 +1,5 @@
-// What the norm and its backward share: a thread's place in a row, typed loads
-// of eight elements, and the host's check of their alignment.
+// What the norm and its backward share: a thread's place in a row, and
+// typed loads of eight elements.
 #pragma once
 
 #include "elem.cuh"
@@ -14,9 +14,6 @@ template <bool kWarpRow, bool kVec> struct Place {
         : G(kWarpRow ? 32 : (int)blockDim.x), t(kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x) {}
     __device__ __forceinline__ int col(int i) const { return kVec ? 8 * (i * G + t) : 256 * (i * (G >> 5) + (t >> 5)) + (t & 31); }
 };
-
-// Aligned for eight elements at a time.
-inline bool aligned8(const void *q, bool f32) { return ((uintptr_t)q & (f32 ? 31u : 15u)) == 0; }
 
 // Eight elements of T or FP32, as loaded.
 template <bool kVec, typename T> __device__ __forceinline__ void load_any(Raw8<float> &r, const void *p, int f32, long long at, int n)

@@ -1,6 +1,7 @@
 // C ABI of the operators around the layer: checks of the descriptors, then
-// the launches of k_norm.cu, k_scores.cu and k_clip.cu.
+// the launches of k_norm.cu, k_scores.cu, k_clip.cu, k_cache.cu and k_attend.cu.
 #include <cmath>
+#include <initializer_list>
 
 #include "pmpe_internal.cuh"
 
@@ -58,6 +59,53 @@ int check_route(const pmpe_route_desc *d)
     if (d->T > 0 && (!d->logits || !d->topk_idx)) return PMPE_ERR_INVALID_ARG;
     if (!fits(d->logits, d->logits_type) || !fits4(d->topk_idx)) return PMPE_ERR_UNSUPPORTED_SHAPE;
     return PMPE_OK;
+}
+
+constexpr int kMaxSequences = 65535, kMaxHeads = 65535;
+constexpr int64_t kMaxCacheElements = (int64_t)1 << 46;
+
+bool is_head_dim(int d) { return d >= 8 && d <= PMPE_MAX_HEAD_DIM && d % 8 == 0; }
+bool apart(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
+{
+    return !a || !b || (uintptr_t)a + (uint64_t)a_bytes <= (uintptr_t)b || (uintptr_t)b + (uint64_t)b_bytes <= (uintptr_t)a;
+}
+// A cache's entries, and the bytes of one head's.
+int64_t entries(const pmpe_kv_cache &c) { return (int64_t)c.pages * c.page_size * c.kv_heads; }
+int64_t entry_bytes(const pmpe_kv_cache &c) { return (int64_t)c.head_dim * (c.type == PMPE_E4M3 ? 1 : 2); }
+
+int check_cache(const pmpe_kv_cache *c)
+{
+    if (!c || c->pages < 1 || c->page_size < 1 || c->kv_heads < 1 || c->head_dim < 1 ||
+        (c->type != PMPE_BF16 && c->type != PMPE_F16 && c->type != PMPE_E4M3) || !c->k || !c->v)
+        return PMPE_ERR_INVALID_ARG;
+    if ((c->type == PMPE_E4M3) != (c->k_scale != nullptr) || (c->type == PMPE_E4M3) != (c->v_scale != nullptr)) return PMPE_ERR_INVALID_ARG;
+    if (c->pages > kMaxRows || c->page_size > PMPE_MAX_PAGE_SIZE || c->kv_heads > kMaxHeads || !is_head_dim(c->head_dim) ||
+        (c->type == PMPE_E4M3 && c->head_dim % 16) || (((uintptr_t)c->k | (uintptr_t)c->v) & 15u) || !fits4(c->k_scale) || !fits4(c->v_scale) ||
+        (int64_t)c->pages * c->page_size > kMaxCacheElements / ((int64_t)c->kv_heads * c->head_dim))
+        return PMPE_ERR_UNSUPPORTED_SHAPE;
+    const int64_t n = entries(*c), b = n * entry_bytes(*c);
+    const bool ok = apart(c->k, b, c->v, b) && apart(c->k_scale, 4 * n, c->v_scale, 4 * n) && apart(c->k, b, c->k_scale, 4 * n) &&
+                    apart(c->k, b, c->v_scale, 4 * n) && apart(c->v, b, c->k_scale, 4 * n) && apart(c->v, b, c->v_scale, 4 * n);
+    return ok ? PMPE_OK : PMPE_ERR_INVALID_ARG;
+}
+bool apart_from_cache(const void *p, int64_t bytes, const pmpe_kv_cache &c)
+{
+    const int64_t n = entries(c), b = n * entry_bytes(c);
+    return apart(p, bytes, c.k, b) && apart(p, bytes, c.v, b) && apart(p, bytes, c.k_scale, 4 * n) && apart(p, bytes, c.v_scale, 4 * n);
+}
+
+int check_sequences(const pmpe_kv_sequences *s, const pmpe_kv_cache &c)
+{
+    if (!s || s->B < 0 || s->table_width < 1) return PMPE_ERR_INVALID_ARG;
+    if (s->B > kMaxSequences || (int64_t)s->table_width * c.page_size > kMaxRows) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    if (s->B > 0 && (!s->table || !s->lengths || s->table_ld < s->table_width)) return PMPE_ERR_INVALID_ARG;
+    return fits4(s->table) && fits4(s->lengths) && fits4(s->cu_seqlens) ? PMPE_OK : PMPE_ERR_UNSUPPORTED_SHAPE;
+}
+// The rows of an append or a read.
+int check_rows(const pmpe_kv_sequences &s, int T)
+{
+    if (T < 0 || (!s.cu_seqlens && T != s.B)) return PMPE_ERR_INVALID_ARG;
+    return T > kMaxRows ? PMPE_ERR_UNSUPPORTED_SHAPE : PMPE_OK;
 }
 
 }  // namespace
@@ -162,6 +210,69 @@ int pmpe_clip_grad_norm(const pmpe_grad *grads, int n, float max_norm, float *no
     if (ok <= 0) return ok < 0 ? PMPE_ERR_WORKSPACE : PMPE_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < clip_workspace_bytes(n)) return PMPE_ERR_WORKSPACE;
     return done(launch_clip(grads, n, max_norm, norm, workspace, (cudaStream_t)stream));
+}
+
+int pmpe_kv_append(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, const pmpe_kv_append_desc *d, void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != PMPE_OK || (rc = check_sequences(seqs, *cache)) != PMPE_OK) return rc;
+    if (!d || !is_type(d->type)) return PMPE_ERR_INVALID_ARG;
+    if ((rc = check_rows(*seqs, d->T)) != PMPE_OK) return rc;
+    if (d->T == 0 || seqs->B == 0) return PMPE_OK;
+    if (!d->k || !d->v || d->k_ld < 0 || d->v_ld < 0 || d->k_head_ld < 0 || d->v_head_ld < 0) return PMPE_ERR_INVALID_ARG;
+    if (!fits(d->k, d->type) || !fits(d->v, d->type)) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    const int64_t most = (int64_t)1 << 60, last = d->T - 1, heads = cache->kv_heads - 1, e = d->type == PMPE_F32 ? 4 : 2;
+    for (int64_t ld : {d->k_ld, d->v_ld, d->k_head_ld, d->v_head_ld})
+        if (ld > most / (4 * (last + heads + 1))) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    if (!apart_from_cache(d->k, (last * d->k_ld + heads * d->k_head_ld + cache->head_dim) * e, *cache) ||
+        !apart_from_cache(d->v, (last * d->v_ld + heads * d->v_head_ld + cache->head_dim) * e, *cache))
+        return PMPE_ERR_INVALID_ARG;
+    return done(launch_kv_append(*cache, *seqs, *d, (cudaStream_t)stream));
+}
+
+int pmpe_kv_read(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, int T, int type, void *k, void *v, void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != PMPE_OK || (rc = check_sequences(seqs, *cache)) != PMPE_OK) return rc;
+    if (!is_type(type)) return PMPE_ERR_INVALID_ARG;
+    if ((rc = check_rows(*seqs, T)) != PMPE_OK) return rc;
+    if (T == 0) return PMPE_OK;
+    if (!k || !v) return PMPE_ERR_INVALID_ARG;
+    if (!fits(k, type) || !fits(v, type)) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    const int64_t bytes = (int64_t)T * cache->kv_heads * cache->head_dim * (type == PMPE_F32 ? 4 : 2);
+    if (!apart(k, bytes, v, bytes) || !apart_from_cache(k, bytes, *cache) || !apart_from_cache(v, bytes, *cache)) return PMPE_ERR_INVALID_ARG;
+    return done(launch_kv_read(*cache, *seqs, T, type, k, v, (cudaStream_t)stream));
+}
+
+size_t pmpe_kv_attend_workspace_size(int B, int heads, int kv_heads, int head_dim)
+{
+    if (B < 0 || B > kMaxSequences || kv_heads < 1 || heads < kv_heads || heads > kMaxHeads || heads % kv_heads || !is_head_dim(head_dim)) return 0;
+    return kv_attend_workspace_bytes(B, heads, kv_heads, head_dim);
+}
+
+int pmpe_kv_attend(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, const pmpe_kv_attend_desc *d, void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != PMPE_OK || (rc = check_sequences(seqs, *cache)) != PMPE_OK) return rc;
+    if (!d || d->heads < 1 || d->heads % cache->kv_heads || d->window < 0 || !std::isfinite(d->scale) ||
+        (cache->type == PMPE_E4M3 ? d->type != PMPE_BF16 && d->type != PMPE_F16 : d->type != cache->type))
+        return PMPE_ERR_INVALID_ARG;
+    if (d->heads > kMaxHeads) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    if (seqs->B == 0) return PMPE_OK;
+    if (!d->q || !d->out || d->q_ld < 0 || d->q_head_ld < 0) return PMPE_ERR_INVALID_ARG;
+    if (!fits(d->q, d->type) || !fits(d->out, d->type) || !fits4(d->lse)) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    const int64_t most = (int64_t)1 << 60, out = (int64_t)seqs->B * d->heads * cache->head_dim * 2, lse = (int64_t)seqs->B * d->heads * 4;
+    if (d->q_ld > most / (4 * (int64_t)seqs->B) || d->q_head_ld > most / (4 * (int64_t)d->heads)) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    const int64_t q = ((seqs->B - 1) * d->q_ld + (d->heads - 1) * d->q_head_ld + cache->head_dim) * 2;
+    // (sequences' outputs are written while others' queries are still read)
+    if (!apart(d->out, out, d->q, q) || !apart(d->lse, lse, d->q, q) || !apart(d->out, out, d->lse, lse) || !apart_from_cache(d->out, out, *cache) ||
+        !apart_from_cache(d->lse, lse, *cache))
+        return PMPE_ERR_INVALID_ARG;
+    const size_t need = kv_attend_workspace_bytes(seqs->B, d->heads, cache->kv_heads, cache->head_dim);
+    if (!d->workspace || ((uintptr_t)d->workspace & 15u) || d->workspace_bytes < need) return PMPE_ERR_WORKSPACE;
+    int sms = 0;
+    if ((rc = sm_count(&sms)) != PMPE_OK) return rc;
+    return done(launch_kv_attend(*cache, *seqs, *d, sms, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -133,7 +133,8 @@ EXPORTED = ("pmpe_moe_workspace_size", "pmpe_moe_workspace_layout", "pmpe_audit_
             "pmpe_moe_backward_step_workspace_size", "pmpe_moe_backward_step", "pmpe_saved_gu_floats",
             "pmpe_moe_forward_routed", "pmpe_moe_backward_routed",
             "pmpe_rms_norm", "pmpe_rms_norm_backward_workspace_size", "pmpe_rms_norm_backward", "pmpe_route",
-            "pmpe_route_backward", "pmpe_clip_workspace_size", "pmpe_clip_grad_norm")
+            "pmpe_route_backward", "pmpe_clip_workspace_size", "pmpe_clip_grad_norm",
+            "pmpe_kv_append", "pmpe_kv_read", "pmpe_kv_attend_workspace_size", "pmpe_kv_attend")
 
 # Bytes of the library's static scratch array used by pmpe_moe_forward_noalloc.
 STATIC_SCRATCH_BYTES = 32 << 20
@@ -176,6 +177,14 @@ _lib.pmpe_clip_workspace_size.restype = ctypes.c_size_t
 _lib.pmpe_clip_workspace_size.argtypes = [ctypes.c_int]
 _lib.pmpe_clip_grad_norm.restype = ctypes.c_int
 _lib.pmpe_clip_grad_norm.argtypes = [_vp, ctypes.c_int, ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]
+_lib.pmpe_kv_append.restype = ctypes.c_int
+_lib.pmpe_kv_append.argtypes = [_vp, _vp, _vp, _vp]
+_lib.pmpe_kv_read.restype = ctypes.c_int
+_lib.pmpe_kv_read.argtypes = [_vp, _vp, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp]
+_lib.pmpe_kv_attend_workspace_size.restype = ctypes.c_size_t
+_lib.pmpe_kv_attend_workspace_size.argtypes = [ctypes.c_int] * 4
+_lib.pmpe_kv_attend.restype = ctypes.c_int
+_lib.pmpe_kv_attend.argtypes = [_vp, _vp, _vp, _vp]
 _lib.pmpe_moe_workspace_size.restype = ctypes.c_size_t
 _lib.pmpe_moe_workspace_size.argtypes = [ctypes.c_int] * 7
 _lib.pmpe_moe_workspace_layout.restype = ctypes.c_int
@@ -716,7 +725,92 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
     return _ops.clip_grad_norm(grads, max_norm, out)
 
 
+class Attention(NamedTuple):
+    out: torch.Tensor  # [B, heads, head_dim], the queries' type
+    lse: torch.Tensor  # FP32 [B, heads], ln of the sum of exp(scores)
+
+
+class KvCache:
+    """A paged cache of attention keys and values, in 16 bits or in e4m3 with a
+    scale per position and head: ``append`` writes new tokens, ``attend`` is the
+    attention of one new token over it, ``read`` gives positions back.
+
+    k, v: [pages, kv_heads, page_size, head_dim] without gaps, BF16, FP16 or
+    float8_e4m3fn; k_scale, v_scale: FP32 [pages, kv_heads, page_size], in 8 bits
+    only (an entry stands for ``k.float() * k_scale[..., None]``).  The cache
+    works on the caller's tensors; ``empty`` makes them.  page_size 1 to 4096,
+    head_dim a multiple of 8 (in 8 bits of 16) up to 256.
+
+    A call's sequences are ``table``, int32 [B, width] (position p of sequence b
+    lies in page table[b, p // page_size]; rows of any pitch), and ``lengths``,
+    int32 [B]: the positions that each holds, those of the call included.  Which
+    pages are whose is the caller's business; an entry outside [0, pages) is no
+    page: its positions are not written, read as zeros and not attended, and
+    lengths are taken as between 0 and width * page_size."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        _ops.kv_cache(k, v, k_scale, v_scale)
+        self._held = (k, v, k_scale, v_scale)
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda") -> "KvCache":
+        """A cache of zeros."""
+        shape = (pages, kv_heads, page_size, head_dim)
+        k, v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
+        if dtype != torch.float8_e4m3fn:
+            return cls(k, v)
+        return cls(k, v, *(torch.zeros(shape[:3], dtype=torch.float32, device=device) for _ in range(2)))
+
+    k = property(lambda self: self._held[0])
+    v = property(lambda self: self._held[1])
+    k_scale = property(lambda self: self._held[2])
+    v_scale = property(lambda self: self._held[3])
+
+    def _on(self, stream, fn, *args):
+        result = _on(stream, fn, self.k, *args)
+        for t in self._held:
+            if t is not None:
+                t.record_stream(stream)
+        return result
+
+    def append(self, k, v, table, lengths, cu_seqlens=None, stream=None) -> None:
+        """Writes the rows k and v, [T, kv_heads, head_dim] of FP32, BF16 or
+        FP16 (rows and heads of any pitch, as slices of a fused projection are):
+        rows cu_seqlens[b] to cu_seqlens[b + 1] - 1 (int32 [B + 1]; None: row b)
+        are the last positions of sequence b, in order.  Rows past the last
+        sequence's are padding and not written.
+
+        No two sequences should write to the same page."""
+        if stream is not None:
+            return self._on(stream, self.append, k, v, table, lengths, cu_seqlens)
+        return _ops.kv_append(*self._held, k, v, table, lengths, cu_seqlens)
+
+    def read(self, table, lengths, cu_seqlens=None, rows=None, dtype=None, stream=None):
+        """(k, v), [rows, kv_heads, head_dim]: the rows that an ``append`` with
+        these sequences writes, as the cache holds them; zeros where it would
+        write none.  ``rows``: how many there are, with cu_seqlens.  ``dtype``:
+        FP32, BF16 or FP16 (default: the cache's, BF16 for 8 bits)."""
+        if dtype is None:
+            dtype = torch.bfloat16 if self.k.dtype == torch.float8_e4m3fn else self.k.dtype
+        if stream is not None:
+            return self._on(stream, self.read, table, lengths, cu_seqlens, rows, dtype)
+        return _ops.kv_read(*self._held, table, lengths, cu_seqlens, rows, dtype)
+
+    def attend(self, q, table, lengths, scale=None, window: int = 0, stream=None) -> Attention:
+        """Attention of one query of each sequence, q [B, heads, head_dim] of the
+        cache's type (over 8 bits of BF16 or FP16; rows and heads of any pitch),
+        over the sequence's positions, its own among them: ``out`` of q's type
+        and ``lse``.  Query head i uses key head i // (heads // kv_heads).
+        ``scale``: of the scores (default head_dim ** -0.5).  ``window``: only the
+        last so many positions (0: all).  A sequence that sees nothing (a padded
+        slot of the batch, length 0) gives zeros and -inf."""
+        if stream is not None:
+            return self._on(stream, self.attend, q, table, lengths, scale, window)
+        return _ops.kv_attend(*self._held, q, table, lengths, scale, window)
+
+
 if not isinstance(_ops, _NoOps):
-    _ops.setup(PmpeError, RmsNorm, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
+    _ops.setup(PmpeError, RmsNorm, Attention, tuple(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
         "pmpe_rms_norm", "pmpe_rms_norm_backward_workspace_size", "pmpe_rms_norm_backward", "pmpe_route", "pmpe_route_backward",
-        "pmpe_clip_workspace_size", "pmpe_clip_grad_norm")))
+        "pmpe_clip_workspace_size", "pmpe_clip_grad_norm", "pmpe_kv_append", "pmpe_kv_read", "pmpe_kv_attend_workspace_size",
+        "pmpe_kv_attend")))

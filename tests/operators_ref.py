@@ -128,3 +128,54 @@ def route_backward(logits, policy, idx, dw, E_pub, E_priv, sigmoid=False, renorm
 
 def global_norm(grads):
     return float(np.sqrt(sum((g.astype(np.float64) ** 2).sum() for g in grads)))
+
+
+def e4m3(v):
+    """v rounded to the nearest e4m3 value, ties to even."""
+    _, ex = np.frexp(v)
+    step = np.exp2(np.maximum(ex - 1, -6) - 3.0)
+    return np.clip(np.round(v / step) * step, -E4M3_MAX, E4M3_MAX)
+
+
+def kv_entries(table, lengths, cu, rows, pages, page_size):
+    """(page, place) of each row's entry in the cache, None for a row that has none."""
+    B, width = table.shape
+    found = []
+    for r in range(rows):
+        at = None
+        for b in range(B):
+            first, last = (b, b + 1) if cu is None else (int(cu[b]), int(cu[b + 1]))
+            if first <= r < last:
+                pos = int(lengths[b]) - last + r
+                if 0 <= pos < width * page_size:
+                    page = int(table[b, pos // page_size])
+                    at = (page, pos % page_size) if 0 <= page < pages else None
+                break
+        found.append(at)
+    return found
+
+
+def kv_seen(table, length, window, pages, page_size):
+    """Pages and places of the positions that one sequence's query sees."""
+    n = min(max(int(length), 0), len(table) * page_size)
+    pos = np.arange(max(0, n - window) if window else 0, n)
+    page = np.asarray(table)[pos // page_size]
+    ok = (page >= 0) & (page < pages)
+    return page[ok], pos[ok] % page_size
+
+
+def attend(q, k, v, scale):
+    """(out, lse, size, scores) of one sequence: q [heads, D], k and v [n,
+    kv_heads, D]; size: the magnitude that errors of out are relative to, scores:
+    the largest sum of |q k| scale of each head."""
+    heads, n, group = q.shape[0], k.shape[0], q.shape[0] // k.shape[1]
+    if n == 0:
+        return np.zeros_like(q), np.full(heads, -np.inf), np.zeros_like(q), np.zeros(heads)
+    k, v = np.repeat(k, group, 1), np.repeat(v, group, 1)
+    s = np.einsum("hd,nhd->hn", q, k) * scale
+    top = s.max(1, keepdims=True)
+    e = np.exp(s - top)
+    a = e / e.sum(1, keepdims=True)
+    size = np.einsum("hn,nhd->hd", a, np.abs(v))
+    scores = np.einsum("hd,nhd->hn", np.abs(q), np.abs(k)).max(1) * abs(scale)
+    return np.einsum("hn,nhd->hd", a, v), (top + np.log(e.sum(1, keepdims=True)))[:, 0], size, scores
