@@ -601,6 +601,37 @@ typedef struct pmpe_kv_attend_desc {
 PMPE_API size_t pmpe_kv_attend_workspace_size(int B, int heads, int kv_heads, int head_dim); /* 0 for an invalid shape */
 PMPE_API int pmpe_kv_attend(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, const pmpe_kv_attend_desc *d, void *stream);
 
+#define PMPE_MAX_VOCABULARY (1 << 21)
+
+/* The next token of each row, from given random numbers:
+ *   r_i = exp((z_i - max z) / temperature); tokens with r below 2^-40, with a
+ *         logit of -inf or NaN are out, +inf counts as the largest finite one
+ *   kept: in the order (logit descending, id ascending) the first top_k
+ *         (0 or less: all); of those each with less than top_p of their sum
+ *         before it (the first always; 1 or more: all); of those r >= min_p
+ *         (0 or less, NaN: all; above 1: as 1)
+ *   drawn: the lowest kept id whose running sum of r, by id, is above u times
+ *         the kept sum; its probability is r over that sum
+ * A temperature that is not above 0 takes the largest logit (equal ones by the
+ * lower id) with probability 1.  u outside [0, 1) counts as its nearest end, NaN
+ * as 0; a top_p of NaN as 0.  A row without a token to draw gives -1 and 0.
+ * r is evaluated within 2^-32, relative, and sums of r are exact: where that
+ * leaves open which side of a border a token is on, either may be taken. */
+typedef struct pmpe_sample_desc {
+    int T, V;              /* rows >= 0, tokens 1 .. PMPE_MAX_VOCABULARY */
+    int logits_type;       /* PMPE_F32, PMPE_BF16, PMPE_F16 */
+    const void *logits;    /* [T, V], rows ld >= 0 elements apart (0: one row for all) */
+    int64_t ld;
+    const float *u;        /* [T] */
+    const float *temperatures, *top_ps, *min_ps; /* [T], or NULL: the value for all rows */
+    const int32_t *top_ks;
+    float temperature, top_p, min_p;
+    int top_k;
+    int32_t *token;        /* [T] */
+    float *prob;           /* [T] */
+} pmpe_sample_desc;
+PMPE_API int pmpe_sample(const pmpe_sample_desc *d, void *stream);
+
 /* Zero the audit buffer (pmpe_audit_words(T, E) words). */
 PMPE_API int pmpe_audit_reset(uint32_t *audit, int T, int E, void *stream);
 

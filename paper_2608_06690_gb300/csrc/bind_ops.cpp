@@ -42,8 +42,9 @@ decltype(&pmpe_kv_append) lib_kv_append;
 decltype(&pmpe_kv_read) lib_kv_read;
 decltype(&pmpe_kv_attend_workspace_size) lib_kv_attend_workspace_size;
 decltype(&pmpe_kv_attend) lib_kv_attend;
+decltype(&pmpe_sample) lib_sample;
 PyObject *g_error;           // PmpeError(code, what)
-PyTypeObject *g_rms_norm, *g_attention;  // RmsNorm and Attention, named tuples
+PyTypeObject *g_rms_norm, *g_attention, *g_sample;  // RmsNorm, Attention and Sample, named tuples
 
 struct Refused {
     int code;
@@ -573,11 +574,63 @@ PyObject *kv_attend(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (PmpeError, RmsNorm, Attention, the library's functions' addresses in the order below)
+// A setting of sample(): a number for all rows, or a tensor of one for each.
+// false: Python's error is set.
+bool setting(PyObject *o, int64_t T, at::Device dev, const char *what, const float *&each, float &all)
+{
+    if (THPVariable_Check(o)) {
+        const at::Tensor &t = THPVariable_Unpack(o);
+        want(is_vector(t, T, dev, at::kFloat), what);
+        each = (const float *)t.data_ptr();
+        return true;
+    }
+    const double v = PyFloat_AsDouble(o);
+    all = narrow(v);
+    return v != -1. || !PyErr_Occurred();
+}
+
+// (logits, u, temperature, top_k, top_p, min_p)
+PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        arguments(n, 6);
+        const at::Tensor &logits = tensor(a[0], "sample: logits are a CUDA tensor"), &u = tensor(a[1], "sample: u is a tensor");
+        const Where at(logits, "sample: logits are a CUDA tensor");
+        pmpe_sample_desc d = {};
+        d.logits_type = type_of(logits.scalar_type());
+        want(d.logits_type >= 0 && logits.dim() == 2, "sample: logits are [T, V] of FP32, BF16 or FP16");
+        d.T = count(logits.size(0));
+        d.V = count(logits.size(1));
+        d.ld = pitch(logits);
+        d.logits = logits.data_ptr();
+        want(is_vector(u, d.T, at.device, at::kFloat), "sample: u is FP32 [T] on the logits' device");
+        d.u = (const float *)u.data_ptr();
+        if (!setting(a[2], d.T, at.device, "sample: temperature is a number or FP32 [T] on the logits' device", d.temperatures, d.temperature) ||
+            !setting(a[4], d.T, at.device, "sample: top_p is a number or FP32 [T] on the logits' device", d.top_ps, d.top_p) ||
+            !setting(a[5], d.T, at.device, "sample: min_p is a number or FP32 [T] on the logits' device", d.min_ps, d.min_p))
+            return nullptr;
+        if (THPVariable_Check(a[3])) {
+            const at::Tensor &k = THPVariable_Unpack(a[3]);
+            want(is_vector(k, d.T, at.device, at::kInt), "sample: top_k is a number or int32 [T] on the logits' device");
+            d.top_ks = (const int32_t *)k.data_ptr();
+        } else {
+            const int64_t k = PyLong_AsLongLong(a[3]);
+            if (k == -1 && PyErr_Occurred()) return nullptr;
+            d.top_k = (int)std::max<int64_t>(-1, std::min<int64_t>(k, INT_MAX));
+        }
+        const at::Tensor token = empty(at.device, at::kInt, d.T), prob = empty(at.device, at::kFloat, d.T);
+        d.token = (int32_t *)token.data_ptr();
+        d.prob = (float *)prob.data_ptr();
+        run("pmpe_sample", [&, s = at.stream()] { return lib_sample(&d, s); });
+        return pack(g_sample, {token, prob});
+    });
+}
+
+// (PmpeError, RmsNorm, Attention, Sample, the library's functions' addresses in the order below)
 PyObject *setup(PyObject *, PyObject *args)
 {
-    PyObject *error, *norm, *attention, *at;
-    if (!PyArg_ParseTuple(args, "OO!O!O!", &error, &PyType_Type, &norm, &PyType_Type, &attention, &PyTuple_Type, &at)) return nullptr;
+    PyObject *error, *norm, *attention, *sample, *at;
+    if (!PyArg_ParseTuple(args, "OO!O!O!O!", &error, &PyType_Type, &norm, &PyType_Type, &attention, &PyType_Type, &sample, &PyTuple_Type, &at)) return nullptr;
     Py_ssize_t i = 0;
     auto next = [&](auto &f) {
         const unsigned long long v = i < PyTuple_GET_SIZE(at) ? PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(at, i)) : 0;
@@ -595,21 +648,23 @@ PyObject *setup(PyObject *, PyObject *args)
     next(lib_kv_read);
     next(lib_kv_attend_workspace_size);
     next(lib_kv_attend);
+    next(lib_sample);
     if (PyErr_Occurred()) return nullptr;
     if (i != PyTuple_GET_SIZE(at)) {
         PyErr_SetString(PyExc_TypeError, "setup: another number of functions");
         return nullptr;
     }
-    for (PyObject *o : {error, norm, attention}) Py_INCREF(o);
+    for (PyObject *o : {error, norm, attention, sample}) Py_INCREF(o);
     g_error = error;
     g_rms_norm = (PyTypeObject *)norm;
     g_attention = (PyTypeObject *)attention;
+    g_sample = (PyTypeObject *)sample;
     Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void *)name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(rms_norm), FAST(rms_norm_backward), FAST(route), FAST(route_backward), FAST(clip_grad_norm),
-                         FAST(kv_cache), FAST(kv_append), FAST(kv_read), FAST(kv_attend),
+                         FAST(kv_cache), FAST(kv_append), FAST(kv_read), FAST(kv_attend), FAST(sample),
                          {"router", router, METH_VARARGS, nullptr}, {"setup", setup, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods};

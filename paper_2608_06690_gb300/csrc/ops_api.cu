@@ -1,5 +1,6 @@
 // C ABI of the operators around the layer: checks of the descriptors, then
-// the launches of k_norm.cu, k_scores.cu, k_clip.cu, k_cache.cu and k_attend.cu.
+// the launches of k_norm.cu, k_scores.cu, k_clip.cu, k_cache.cu,
+// k_attend.cu and k_sample.cu.
 #include <cmath>
 #include <initializer_list>
 
@@ -273,6 +274,32 @@ int pmpe_kv_attend(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, co
     int sms = 0;
     if ((rc = sm_count(&sms)) != PMPE_OK) return rc;
     return done(launch_kv_attend(*cache, *seqs, *d, sms, (cudaStream_t)stream));
+}
+
+int pmpe_sample(const pmpe_sample_desc *d, void *stream)
+{
+    if (!d || d->T < 0 || d->V < 1 || !is_type(d->logits_type) || d->ld < 0) return PMPE_ERR_INVALID_ARG;
+    if (d->T > kMaxRows || d->V > PMPE_MAX_VOCABULARY || d->ld > ((int64_t)1 << 30)) return PMPE_ERR_UNSUPPORTED_SHAPE;
+    // settings for all rows are checked here
+    if ((!d->temperatures && !(d->temperature >= 0.f && std::isfinite(d->temperature))) || (!d->top_ps && !(d->top_p >= 0.f && d->top_p <= 1.f)) ||
+        (!d->min_ps && !(d->min_p >= 0.f && d->min_p <= 1.f)) || (!d->top_ks && d->top_k < 0))
+        return PMPE_ERR_INVALID_ARG;
+    if (d->T == 0) return PMPE_OK;
+    if (!d->logits || !d->u || !d->token || !d->prob) return PMPE_ERR_INVALID_ARG;
+    if (!fits(d->logits, d->logits_type) || !fits4(d->u) || !fits4(d->temperatures) || !fits4(d->top_ps) || !fits4(d->min_ps) || !fits4(d->top_ks) ||
+        !fits4(d->token) || !fits4(d->prob))
+        return PMPE_ERR_UNSUPPORTED_SHAPE;
+    // (a row's results are written while others are still read)
+    const int64_t rows = 4 * (int64_t)d->T, logits = ((d->T - 1) * d->ld + d->V) * (d->logits_type == PMPE_F32 ? 4 : 2);
+    for (const void *out : {(const void *)d->token, (const void *)d->prob}) {
+        if (!apart(out, rows, d->logits, logits)) return PMPE_ERR_INVALID_ARG;
+        for (const void *in : {(const void *)d->u, (const void *)d->temperatures, (const void *)d->top_ps, (const void *)d->min_ps, (const void *)d->top_ks})
+            if (!apart(out, rows, in, rows)) return PMPE_ERR_INVALID_ARG;
+    }
+    if (!apart(d->token, rows, d->prob, rows)) return PMPE_ERR_INVALID_ARG;
+    int sms = 0, rc;
+    if ((rc = sm_count(&sms)) != PMPE_OK) return rc;
+    return done(launch_sample(*d, sms, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -134,7 +134,7 @@ EXPORTED = ("pmpe_moe_workspace_size", "pmpe_moe_workspace_layout", "pmpe_audit_
             "pmpe_moe_forward_routed", "pmpe_moe_backward_routed",
             "pmpe_rms_norm", "pmpe_rms_norm_backward_workspace_size", "pmpe_rms_norm_backward", "pmpe_route",
             "pmpe_route_backward", "pmpe_clip_workspace_size", "pmpe_clip_grad_norm",
-            "pmpe_kv_append", "pmpe_kv_read", "pmpe_kv_attend_workspace_size", "pmpe_kv_attend")
+            "pmpe_kv_append", "pmpe_kv_read", "pmpe_kv_attend_workspace_size", "pmpe_kv_attend", "pmpe_sample")
 
 # Bytes of the library's static scratch array used by pmpe_moe_forward_noalloc.
 STATIC_SCRATCH_BYTES = 32 << 20
@@ -185,6 +185,8 @@ _lib.pmpe_kv_attend_workspace_size.restype = ctypes.c_size_t
 _lib.pmpe_kv_attend_workspace_size.argtypes = [ctypes.c_int] * 4
 _lib.pmpe_kv_attend.restype = ctypes.c_int
 _lib.pmpe_kv_attend.argtypes = [_vp, _vp, _vp, _vp]
+_lib.pmpe_sample.restype = ctypes.c_int
+_lib.pmpe_sample.argtypes = [_vp, _vp]
 _lib.pmpe_moe_workspace_size.restype = ctypes.c_size_t
 _lib.pmpe_moe_workspace_size.argtypes = [ctypes.c_int] * 7
 _lib.pmpe_moe_workspace_layout.restype = ctypes.c_int
@@ -809,8 +811,31 @@ class KvCache:
         return _ops.kv_attend(*self._held, q, table, lengths, scale, window)
 
 
+class Sample(NamedTuple):
+    token: torch.Tensor  # int32 [T], -1 where a row has no token to draw
+    prob: torch.Tensor   # FP32 [T], the probability with which the token was drawn
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=None) -> Sample:
+    """The next token of each row of logits ([T, V] of FP32, BF16 or FP16, rows
+    of any pitch, one row expanded to many among them) from the random numbers u (FP32 [T], uniform in [0, 1)).
+
+    temperature: 0 takes the largest logit.  top_k: only the k largest logits
+    (0: all; equal ones by the lower id).  top_p: of those only the largest that
+    together reach this share of their probability (1: all).  min_p: of those only
+    tokens with at least this share of the best one's probability.  Each is a
+    number for all rows, or a tensor of one for each (FP32 [T], top_k int32 [T]).
+    The token drawn is the lowest kept id whose cumulative probability, by id, is
+    above u: the same u gives the same token, whatever stands in the other rows.
+    Logits of -inf and NaN are never drawn, nor is what has less than 2^-40 of the
+    best token's probability.  V up to 2^21."""
+    if stream is not None:
+        return _on(stream, sample, logits, logits, u, temperature, top_k, top_p, min_p)
+    return _ops.sample(logits, u, temperature, top_k, top_p, min_p)
+
+
 if not isinstance(_ops, _NoOps):
-    _ops.setup(PmpeError, RmsNorm, Attention, tuple(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
+    _ops.setup(PmpeError, RmsNorm, Attention, Sample, tuple(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
         "pmpe_rms_norm", "pmpe_rms_norm_backward_workspace_size", "pmpe_rms_norm_backward", "pmpe_route", "pmpe_route_backward",
         "pmpe_clip_workspace_size", "pmpe_clip_grad_norm", "pmpe_kv_append", "pmpe_kv_read", "pmpe_kv_attend_workspace_size",
-        "pmpe_kv_attend")))
+        "pmpe_kv_attend", "pmpe_sample")))

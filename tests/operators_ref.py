@@ -179,3 +179,34 @@ def attend(q, k, v, scale):
     size = np.einsum("hn,nhd->hd", a, np.abs(v))
     scores = np.einsum("hd,nhd->hn", np.abs(q), np.abs(k)).max(1) * abs(scale)
     return np.einsum("hn,nhd->hd", a, v), (top + np.log(e.sum(1, keepdims=True)))[:, 0], size, scores
+
+
+def sample_row(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """(token, prob, kept ids) of one row, in 64 bits."""
+    z = np.asarray(z, np.float64)
+    ids = np.flatnonzero(z > -np.inf)
+    if len(ids) == 0:
+        return -1, 0.0, ids
+    z = np.minimum(z, FLT_MAX)
+    ids = ids[np.lexsort((ids, -z[ids]))]
+    if not temperature > 0:
+        return int(ids[0]), 1.0, ids[:1]
+    x = (z[ids[0]] - z[ids]) / np.float64(temperature)
+    r = np.exp(-x)
+    n = int((r >= 2.0 ** -40).sum())
+    if top_k > 0:
+        n = min(n, top_k)
+    ids, r, x = ids[:n], r[:n], x[:n]
+    if not top_p >= 1:
+        below = np.cumsum(r) - r
+        n = max(1, int((below < np.float64(top_p if top_p > 0 else 0.0) * r.sum()).sum()))
+        ids, r, x = ids[:n], r[:n], x[:n]
+    if min_p > 0:
+        keep = x <= -np.log(min(float(min_p), 1.0))  # (exp rounds to 1 what is next to it)
+        ids, r = ids[keep], r[keep]
+    order = np.argsort(ids)
+    ids, r = ids[order], r[order]
+    total = np.cumsum(r)
+    u = min(max(u, 0.0), 1.0 - 2.0 ** -24) if u == u else 0.0
+    at = min(int((total <= u * total[-1]).sum()), len(ids) - 1)
+    return int(ids[at]), r[at] / total[-1], ids

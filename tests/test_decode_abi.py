@@ -39,6 +39,12 @@ class Attend(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class SampleDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int), ("V", ctypes.c_int), ("logits_type", ctypes.c_int), ("logits", ctypes.c_void_p), ("ld", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("u", "temperatures", "top_ps", "min_ps", "top_ks")] + \
+               [(n, ctypes.c_float) for n in ("temperature", "top_p", "min_p")] + [("top_k", ctypes.c_int), ("token", ctypes.c_void_p), ("prob", ctypes.c_void_p)]
+
+
 CACHE = dict(pages=10, page_size=16, kv_heads=4, head_dim=128, type=1, k=P, v=P + FAR, k_scale=None, v_scale=None)
 SEQS = dict(B=3, table_width=5, table=P + 2 * FAR, table_ld=5, lengths=P + 2 * FAR + 4096, cu_seqlens=None)
 BAD_CACHE = [(-1, dict(pages=0)), (-1, dict(page_size=0)), (-1, dict(kv_heads=0)), (-1, dict(head_dim=0)), (-1, dict(type=0)), (-1, dict(type=4)),
@@ -134,6 +140,28 @@ def test_attend_refusals(pmpe):
     assert rc(seqs=dict(B=0, table=None, lengths=None), q=None, out=None, workspace=None) == pmpe.OK
 
 
+def test_sample_refusals(pmpe):
+    f = pmpe._lib.pmpe_sample
+    base = dict(T=3, V=1000, logits_type=0, logits=P, ld=1000, u=P + FAR, temperatures=None, top_ps=None, min_ps=None, top_ks=None, temperature=1.0, top_p=0.9,
+                min_p=0.1, top_k=5, token=P + 2 * FAR, prob=P + 3 * FAR)
+
+    def rc(**over):
+        return f(desc(SampleDesc, base, **over), None)
+
+    assert f(None, None) == pmpe.ERR_INVALID_ARG
+    for bad in (dict(T=-1), dict(V=0), dict(logits_type=3), dict(ld=-1), dict(logits=None), dict(u=None), dict(token=None), dict(prob=None),
+                dict(temperature=-0.5), dict(temperature=math.nan), dict(temperature=math.inf), dict(top_p=-0.1), dict(top_p=1.1), dict(top_p=math.nan),
+                dict(min_p=-0.1), dict(min_p=1.5), dict(min_p=math.nan), dict(top_k=-1), dict(token=P + 64), dict(prob=P + 11996), dict(token=P + FAR),
+                dict(prob=P + 2 * FAR + 8), dict(top_ks=P + 3 * FAR)):
+        assert rc(**bad) == pmpe.ERR_INVALID_ARG, bad
+    for bad in (dict(T=(1 << 30) + 1), dict(V=(1 << 21) + 1, ld=1 << 22), dict(ld=1 << 31), dict(logits=P + 2), dict(logits=P + 1, logits_type=1), dict(u=P + FAR + 2),
+                dict(token=P + 2 * FAR + 2), dict(prob=P + 3 * FAR + 1), dict(temperatures=P + 1), dict(top_ps=P + 2), dict(min_ps=P + 2), dict(top_ks=P + 2)):
+        assert rc(**bad) == pmpe.ERR_UNSUPPORTED_SHAPE, bad
+    assert rc(T=0, logits=None, u=None, token=None, prob=None) == pmpe.OK
+    # what rows have of their own is not the host's to check
+    assert rc(T=0, temperatures=P, top_ps=P, min_ps=P, top_ks=P, temperature=-1.0, top_p=7.0, min_p=-2.0, top_k=-4) == pmpe.OK
+
+
 def test_host_tensors_and_other_types_are_refused(pmpe):
     k = torch.zeros(4, 2, 8, 16, dtype=torch.bfloat16)
     with pytest.raises(pmpe.PmpeError, match="CUDA"):
@@ -143,6 +171,10 @@ def test_host_tensors_and_other_types_are_refused(pmpe):
                 (k8, k8, s, s[:3]), (k8, k8, s, s.double()), (k8, k8, s.transpose(1, 2).contiguous().transpose(1, 2), s), (k, k, 1.0)):
         with pytest.raises(pmpe.PmpeError):
             pmpe.KvCache(*bad)
+    z, u = torch.zeros(2, 8), torch.zeros(2)
+    for call in (lambda: pmpe.sample(z, u), lambda: pmpe.sample(None, u), lambda: pmpe.sample([[0.0]], u), lambda: pmpe._ops.sample(z, u)):
+        with pytest.raises(pmpe.PmpeError):
+            call()
 
 
 # ------------------------------------------------ the references themselves
@@ -176,3 +208,16 @@ def test_reference_e4m3():
     x = torch.cat([x, x * 2.0 ** -12, x * 2.0 ** -17])
     want = x.clamp(-448, 448).float().to(torch.float8_e4m3fn).double()
     assert np.array_equal(ref.e4m3(x.numpy()), want.numpy())
+
+
+def test_reference_sampling_by_hand():
+    z = np.log(np.array([0.1, 0.4, 0.1, 0.3, 0.1]))
+    assert ref.sample_row(z, 0.05)[:1] == (0,) and ref.sample_row(z, 0.11)[0] == 1 and ref.sample_row(z, 0.999)[0] == 4
+    assert ref.sample_row(z, 0.0, top_k=2)[2].tolist() == [1, 3] and ref.sample_row(z, 0.6, top_k=2)[0] == 3
+    assert ref.sample_row(z, 0.0, top_k=3)[2].tolist() == [0, 1, 3]  # equal ones by the lower id
+    assert ref.sample_row(z, 0.0, top_p=0.39)[2].tolist() == [1] and ref.sample_row(z, 0.0, top_p=0.41)[2].tolist() == [1, 3]
+    assert ref.sample_row(z, 0.0, top_k=2, top_p=0.5)[2].tolist() == [1]  # 4 / 7 of the two
+    assert ref.sample_row(z, 0.0, min_p=0.5)[2].tolist() == [1, 3] and ref.sample_row(z, 0.9, min_p=1.0)[2].tolist() == [1]
+    assert ref.sample_row(z, 0.9, temperature=0.0)[:2] == (1, 1.0) and ref.sample_row(z * 0 - np.inf, 0.9)[:2] == (-1, 0.0)
+    assert abs(ref.sample_row(z, 0.7, temperature=0.5)[1] - 0.09 / 0.28) < 1e-12
+    assert ref.sample_row([0.0, -28.0, np.nan], 0.0)[2].tolist() == [0]  # 40 ln 2 is 27.7
