@@ -615,7 +615,7 @@ PMPE_API int pmpe_kv_attend(const pmpe_kv_cache *cache, const pmpe_kv_sequences 
  * A temperature that is not above 0 takes the largest logit (equal ones by the
  * lower id) with probability 1.  u outside [0, 1) counts as its nearest end, NaN
  * as 0; a top_p of NaN as 0.  A row without a token to draw gives -1 and 0.
- * r is evaluated within 2^-32, relative, and sums of r are exact: where that
+ * r is evaluated within 2^-31, relative, and sums of r are exact: where that
  * leaves open which side of a border a token is on, either may be taken. */
 typedef struct pmpe_sample_desc {
     int T, V;              /* rows >= 0, tokens 1 .. PMPE_MAX_VOCABULARY */

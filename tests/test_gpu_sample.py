@@ -1,7 +1,7 @@
-"""Sampling against a 64-bit reference.  Tokens are equal: r is within 2^-32 and
+"""Sampling against a 64-bit reference.  Tokens are equal: r is within 2^-31 and
 its sums are exact, so that a border would have to lie that near to a draw (the
 seeds are fixed).  prob: r and the sum are rounded to FP32, and their quotient:
-three half steps and 2^-31."""
+three half steps, and a tenth of one for r."""
 import math
 
 import numpy as np
