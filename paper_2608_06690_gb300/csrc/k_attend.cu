@@ -26,16 +26,18 @@
 #include <algorithm>
 
 #include "kv_cache.cuh"
+#include "tc_ptx.cuh"
 
 namespace pmpe {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kKeys = 16;                // of a warp and tile
-constexpr int kTile = kKeys * kWarps;    // positions of a tile
-constexpr int kMaxCtas = 320;
-constexpr int kJoinThreads = 256;
+constexpr int kMaxCtas = 640;
+constexpr int kJoinThreads = 256, kFew = 4;  // parts that a warp joins by itself
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+constexpr float kAhead = 8.f;   // powers of two that a score may be above the maximum
+constexpr float kUp = 0x1p7f;   // 8 bits: weights up to 2^kAhead kUp stay inside FP16
 
 enum Kind { kBf16, kF16, kE4m3Bf16, kE4m3F16 };  // cache (and queries)
 
@@ -48,31 +50,50 @@ struct AttendParams {
     int heads, group, blocks;  // query heads of a key head, and blocks of 8 kNT of them
     int window;
     float scale_log2;
+    int box_rows;              // of a TMA copy: positions that lie one after another in a page; 0: copied one by one
+    CUtensorMap k_map, v_map;  // the keys and values as rows of 16-bit words
     float *part;               // [CTAs][2][8 kNT][kDP + 2]: sums, maxima, totals
-    long long *plan;           // [0] tiles a CTA, [1 + b] tiles before sequence b
 };
 
 template <int kDP, int kNT, int kKind> struct AttendShape {
     static constexpr bool k8 = kKind >= kE4m3Bf16;
     static constexpr int kE = k8 ? 1 : 2;
-    static constexpr int kRow = kDP * kE, kCpr = kRow / 16;  // bytes, 16-byte chunks of a row
-    static constexpr int kStage = 2 * kKeys * kRow + (k8 ? 2 * kKeys * 4 : 0) + 16;
-    static constexpr int kCtas = kDP * kE <= 256 ? 2 : 1;   // of an SM
+    // bytes of a row, its 16-byte chunks, and bytes of it in shared memory
+    static constexpr int kRow = kDP * kE, kUsed = kRow / 16, kPitch = kRow <= 64 ? 64 : (kRow + 127) / 128 * 128;
+    static constexpr int kBox = kPitch < 128 ? kPitch : 128, kBoxes = kPitch / kBox;  // bytes of a row that a TMA copy takes
     static constexpr int kHeads = 8 * kNT;
-    static constexpr int kBuf = kHeads * (kDP + 4) * 4, kStats = 2 * kWarps * kHeads * 4;
-    static constexpr int kRoom = 228 * 1024 / kCtas - 1024 - 128 - kBuf - kStats;  // 1 KB a CTA is the system's, 128 bytes static
-    static constexpr int kStages = kRoom / (kWarps * kStage) < 8 ? kRoom / (kWarps * kStage) : 8;
-    static constexpr int kSmem = kWarps * kStages * kStage + kBuf + kStats;
-    static_assert(kStages >= 3 && kStage % 16 == 0, "shared memory");
+    // rows of 16 keys that a warp takes at a time: a stage of them holds the
+    // warp's sums when a pair ends
+    static constexpr int kMT = 2 * 16 * kPitch >= kHeads * kDP * 4 ? 1 : 2;
+    static constexpr int kKeys = 16 * kMT, kTile = kKeys * kWarps;  // positions of a warp's part, of a tile
+    static constexpr uint32_t kAll = kMT == 2 ? 0xffffffffu : 0xffffu;
+    static constexpr int kData = 2 * kKeys * kPitch, kScales = k8 ? 2 * kKeys * 4 : 0;  // of a stage
+    static constexpr int kSmall = kScales + 16;  // scales, barrier, mask
+    static constexpr int kStats = 2 * kWarps * kHeads * 4;
+    // CTAs of an SM: what their registers and two stages a warp allow
+    static constexpr int kCtas = kDP * kNT <= 128 ? (kData <= 4096 ? 4 : 3) : kData <= 8192 ? (kDP <= 128 ? 3 : 2) : kData <= 12288 ? 2 : 1;
+    // 1 KB a CTA is the system's, 128 bytes static, up to 1 KB goes to the rings' alignment
+    static constexpr int kRoom = 228 * 1024 / kCtas - 2048 - 128 - kStats;
+    static constexpr int kStages = kRoom / (kWarps * (kData + kSmall)) < 8 ? kRoom / (kWarps * (kData + kSmall)) : 8;
+    static constexpr int kSmem = 1024 + kWarps * kStages * (kData + kSmall) + kStats;
+    static_assert(kStages >= 2 && kData % 1024 == 0 && kSmall % 16 == 0 && kData >= kHeads * kDP * 4, "shared memory");
+    // Chunk c of row r of a tile, as a TMA copy swizzles it: rows of kBox bytes,
+    // no two of eight rows' equal chunks in the same 16 bytes of a 128-byte line.
+    static __device__ __forceinline__ int chunk_at(int r, int c)
+    {
+        return kBox == 64 ? r * 4 + (c ^ ((r >> 1) & 3)) : (c >> 3) * kKeys * 8 + r * 8 + ((c & 7) ^ (r & 7));
+    }
 };
 
-// Chunk c of row r of a tile: no two of eight rows' equal chunks in the same
-// 16 bytes of a 128-byte bank line.
-template <int kCpr> __device__ __forceinline__ int chunk_at(int r, int c)
+// 16 bytes into shared memory, asynchronously; zeros for bytes = 0.
+__device__ __forceinline__ void fetch16(uint32_t dst, const void *src, int bytes)
 {
-    return r * kCpr + (kCpr % 8 == 0 ? c ^ (r & 7) : c ^ ((r >> 1) & 3));
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(bytes));
 }
-
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -122,7 +143,7 @@ template <bool kBf> __device__ __forceinline__ float2 unpack2(uint32_t u)
 
 // The positions of a sequence that its query sees, in tiles from a multiple of
 // kTile on.
-struct Span {
+template <int kTile> struct Span {
     int len, lo, first, tiles;
     __device__ __forceinline__ Span(const AttendParams &p, int b)
     {
@@ -135,9 +156,9 @@ struct Span {
 
 // A place in the row of all tiles: tile `tile` of the positions of sequence b,
 // for block `block` of the queries of key head `head`.
-struct Walk {
+template <int kTile> struct Walk {
     int b, head, block, tile;
-    Span s;
+    Span<kTile> s;
     __device__ __forceinline__ bool advance(const AttendParams &p)  // whether another pair begins
     {
         if (++tile < s.tiles) return false;
@@ -146,7 +167,7 @@ struct Walk {
             block = 0;
             if (++head == p.kv.kv_heads) {
                 head = 0;
-                do s = Span(p, ++b);
+                do s = Span<kTile>(p, ++b);
                 while (s.tiles == 0 && b < p.kv.B);
             }
         }
@@ -184,16 +205,25 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     constexpr bool k8 = S::k8, kBf = kKind == kBf16;  // kBf: of the products
     constexpr bool kQBf = kKind == kBf16 || kKind == kE4m3Bf16;
     using Q = typename std::conditional<kQBf, bf16, __half>::type;
-    constexpr int kSteps = kDP / 16;
-    extern __shared__ __align__(128) uint8_t smem[];
+    constexpr int kSteps = kDP / 16, kMT = S::kMT, kKeys = S::kKeys, kTile = S::kTile;
+    using Span = Span<kTile>;
+    extern __shared__ __align__(16) uint8_t smem[];
     __shared__ long long s_warp[kWarps], s_start;
     __shared__ int s_seq;
-    uint8_t *ring = smem + (threadIdx.x >> 5) * S::kStages * S::kStage;
-    float *all = (float *)(smem + kWarps * S::kStages * S::kStage);
-    float *s_m = all + S::kBuf / 4, *s_l = s_m + kWarps * S::kHeads;
+    __shared__ volatile int s_abort;
+    uint8_t *rings = smem + (-smem_u32(smem) & 1023u), *smalls = rings + kWarps * S::kStages * S::kData;
+    uint8_t *ring = rings + (threadIdx.x >> 5) * S::kStages * S::kData, *small = smalls + (threadIdx.x >> 5) * S::kStages * S::kSmall;
+    float *s_m = (float *)(smalls + kWarps * S::kStages * S::kSmall), *s_l = s_m + kWarps * S::kHeads;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane & 3, g = lane >> 2;
-    pdl_trigger();
+    const bool boxes = p.box_rows > 0;
+    auto barrier = [&](int stage) { return smem_u32(small + stage * S::kSmall + S::kScales); };
+    if (lane == 0) {  // a stage is full when its copies are: one arrival with their bytes, or every lane's
+        for (int i = 0; i < S::kStages; ++i) mbar_init(barrier(i), boxes ? 1 : 32);
+        if (warp == 0) s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
     pdl_wait();
+    pdl_trigger();  // not before: the second launch reads the lengths as soon as it starts
 
     // ---- this CTA's run of tiles
     const int pairs = p.kv.kv_heads * p.blocks;
@@ -204,14 +234,9 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
         long long all;
         const long long before = total + scan_before(n, s_warp, all);
         if (b0 == 0) mine = n, before0 = before;
-        if (blockIdx.x == 0 && b < p.kv.B) p.plan[1 + b] = before;
         total += all;
     }
     const long long per = (total + gridDim.x - 1) / gridDim.x;
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        p.plan[0] = per;
-        p.plan[1 + p.kv.B] = total;
-    }
     // sequences that see nothing
     for (int b = blockIdx.x; b < p.kv.B; b += gridDim.x) {
         if (Span(p, b).tiles > 0) continue;
@@ -241,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
         }
     }
     __syncthreads();
-    Walk at = {s_seq, 0, 0, 0, Span(p, s_seq)};
+    Walk<kTile> at = {s_seq, 0, 0, 0, Span(p, s_seq)};
     {
         const long long pair = s_start / at.s.tiles;
         at.tile = (int)(s_start - pair * at.s.tiles);
@@ -249,51 +274,90 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
         at.block = (int)(pair - (long long)at.head * p.blocks);
     }
 
-    // ---- copies: lane r < 16 (and r + 16) finds row r's entry, one tile ahead
-    Walk ahead = at;
+    // ---- copies
+    Walk<kTile> ahead = at;
     long long to_copy = left;
-    int page = -1, place = 0;
-    auto look_up = [&]() {
-        const int pos = ahead.s.first + ahead.tile * kTile + warp * kKeys + (lane & 15);
-        page = -1;
-        if (to_copy > 0 && pos >= ahead.s.lo && pos < ahead.s.len) {
-            const int j = p.kv.by_page.quotient(pos);
-            place = pos - j * p.kv.page_size;
-            page = __ldg(p.kv.table + ahead.b * p.kv.table_ld + j);
-        }
+    // The entry of position pos (the first of `n` in one page); -1: none of
+    // them is seen, or there is no page.
+    auto entry_at = [&](int pos, int n) -> long long {
+        if (pos + n <= ahead.s.lo || pos >= ahead.s.len) return -1;
+        const int j = p.kv.by_page.quotient(pos), page = __ldg(p.kv.table + ahead.b * p.kv.table_ld + j);
+        return (unsigned)page < (unsigned)p.kv.pages ? ((long long)page * p.kv.kv_heads + ahead.head) * p.kv.page_size + (pos - j * p.kv.page_size) : -1;
     };
-    const int row_bytes = p.kv.head_dim * S::kE;
+    // In boxes a lane looks up 16 positions, for the pair's next tiles together,
+    // so that the table's latency shows once in kBatch tiles.
+    constexpr int kBatch = 32 / kMT;
+    long long found = -1;  // boxes: of 16 positions of tile lane / kMT of the batch; else of one of the next tile's
+    int in_batch = kBatch;
+    auto look_up = [&]() {
+        if (to_copy > 0) found = entry_at(ahead.s.first + ahead.tile * kTile + warp * kKeys + (lane & (kKeys - 1)), 1);
+    };
     auto copy = [&](int stage) {
-        if (to_copy > 0) {
-            uint8_t *to = ring + stage * S::kStage;
-            const uint32_t to32 = smem_u32(to);
-            const bool there = (unsigned)page < (unsigned)p.kv.pages;
-            const uint32_t mask = __ballot_sync(~0u, there) & 0xffffu;
-            const long long entry = there ? ((long long)page * p.kv.kv_heads + ahead.head) * p.kv.page_size + place : 0;
-            if (mask) {
+        if (to_copy <= 0) return;
+        const uint32_t to = smem_u32(ring + stage * S::kData), bar = barrier(stage), scales = bar - S::kScales;
+        uint32_t mask = 0;
+        if (boxes) {
+            const int pos = ahead.s.first + ahead.tile * kTile + warp * kKeys;
+            if (in_batch == kBatch) {
+                found = entry_at(pos + lane / kMT * kTile + lane % kMT * 16, 16);
+                in_batch = 0;
+            }
+            long long entry[kMT];
+            uint32_t bytes = 0;
 #pragma unroll
-                for (int i = 0; i < S::kCpr / 2; ++i) {
-                    const int n = i * 32 + lane, r = n / S::kCpr, ch = n % S::kCpr;
-                    const long long off = __shfl_sync(~0u, entry, r) * row_bytes + ch * 16;
-                    const bool live = (mask >> r & 1) && ch * 16 < row_bytes;
-                    const uint32_t dst = to32 + chunk_at<S::kCpr>(r, ch) * 16;
-                    cp_async16(dst, p.kv.k + (live ? off : 0), live ? 16 : 0);
-                    cp_async16(dst + kKeys * S::kRow, p.kv.v + (live ? off : 0), live ? 16 : 0);
-                }
-                if constexpr (k8) {
-                    const float *src = lane < 16 ? p.kv.k_scale : p.kv.v_scale;
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(to32 + 2 * kKeys * S::kRow + lane * 4), "l"(src + entry),
-                                 "r"(there ? 4 : 0));
+            for (int h = 0; h < kMT; ++h) {
+                entry[h] = __shfl_sync(~0u, found, in_batch * kMT + h);
+                const int above = min(max(ahead.s.len - pos - 16 * h, 0), 16), below = min(max(ahead.s.lo - pos - 16 * h, 0), 16);
+                mask |= (entry[h] >= 0 ? ((1u << above) - 1) & ~((1u << below) - 1) : 0u) << (16 * h);
+                if (entry[h] >= 0) bytes += 2 * 16 * S::kPitch + S::kScales / kMT;
+            }
+            ++in_batch;
+            if (lane == 0) {
+                mbar_expect_tx(bar, bytes);
+#pragma unroll
+                for (int h = 0; h < kMT; ++h) {
+                    if (entry[h] < 0) continue;
+                    if (k8) {
+                        bulk_load(scales + 64 * h, p.kv.k_scale + entry[h], 64, bar);
+                        bulk_load(scales + kKeys * 4 + 64 * h, p.kv.v_scale + entry[h], 64, bar);
+                    }
+#pragma unroll
+                    for (int x = 0; x < S::kBoxes; ++x) {
+                        const uint32_t dst = to + x * kKeys * S::kBox + 16 * h * S::kBox;
+                        tma_load_2d(dst, &p.k_map, bar, x * (S::kBox / 2), (int)entry[h]);
+                        tma_load_2d(dst + kKeys * S::kPitch, &p.v_map, bar, x * (S::kBox / 2), (int)entry[h]);
+                    }
                 }
             }
-            if (lane == 0) *(uint32_t *)(to + S::kStage - 16) = mask;
-            --to_copy;
-            ahead.advance(p);
-            look_up();
+        } else {
+            const int row_bytes = p.kv.head_dim * S::kE;
+            mask = __ballot_sync(~0u, found >= 0) & S::kAll;
+            if (mask) {
+#pragma unroll
+                for (int i = 0; i < kKeys * S::kUsed / 32; ++i) {
+                    const int n = i * 32 + lane, r = n / S::kUsed, ch = n % S::kUsed;
+                    const long long off = __shfl_sync(~0u, found, r) * row_bytes + ch * 16;
+                    const bool live = (mask >> r & 1) && ch * 16 < row_bytes;
+                    const uint32_t dst = to + S::chunk_at(r, ch) * 16;
+                    fetch16(dst, p.kv.k + (live ? off : 0), live ? 16 : 0);
+                    fetch16(dst + kKeys * S::kPitch, p.kv.v + (live ? off : 0), live ? 16 : 0);
+                }
+                if constexpr (k8) {
+                    const uint32_t dst = scales + (lane & (kKeys - 1)) * 4;
+                    const long long e = max(found, 0ll);
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(p.kv.k_scale + e), "r"(found >= 0 ? 4 : 0));
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst + kKeys * 4), "l"(p.kv.v_scale + e), "r"(found >= 0 ? 4 : 0));
+                }
+            }
+            cp_async_arrive_noinc(bar);
         }
-        asm volatile("cp.async.commit_group;\n");
+        if (lane == 0) *(uint32_t *)(small + stage * S::kSmall + S::kScales + 8) = mask;
+        --to_copy;
+        if (ahead.advance(p)) in_batch = kBatch;
+        if (!boxes) look_up();
     };
-    look_up();
+    __syncwarp();
+    if (!boxes) look_up();
 #pragma unroll
     for (int i = 0; i < S::kStages - 1; ++i) copy(i);
 
@@ -302,7 +366,8 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     float o[kSteps][kNT][4], m[kNT][2], l[kNT][2], cs[kNT][2];
     float r_max = 0x1p-100f;  // 8 bits: the power of two that the weights are relative to
     int stage = 0, fill = S::kStages - 1, pieces = 0;
-    bool fresh = true;
+    uint32_t parity = 0;
+    bool fresh = true, lost = false;
     int first_tile = at.tile;
     for (long long t = 0; t < left; ++t) {
         if (fresh) {
@@ -348,22 +413,37 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[j][nt][i] = 0.f;
         }
-        cp_async_wait<S::kStages - 2>();
+        if (!lost && !mbar_wait(barrier(stage), parity, &s_abort, nullptr)) {
+            lost = true;  // (a copy that does not end: what this warp holds becomes NaN)
+            to_copy = 0;
+        }
         __syncwarp();
         copy(fill);
         fill = stage;
-        const uint8_t *from = ring + stage * S::kStage;
-        stage = stage + 1 == S::kStages ? 0 : stage + 1;
-        const uint32_t mask = *(const uint32_t *)(from + S::kStage - 16);
+        const uint8_t *from = ring + stage * S::kData;
+        const float *scales = (const float *)(small + stage * S::kSmall);
+        const uint32_t mask = lost ? 0u : *(const uint32_t *)(small + stage * S::kSmall + S::kScales + 8);
+        if (++stage == S::kStages) {
+            stage = 0;
+            parity ^= 1;
+        }
         if (mask) {
-            const uint32_t k_at = smem_u32(from), v_at = k_at + kKeys * S::kRow;
-            float s[kNT][4];
-            {
+            const uint32_t k_at = smem_u32(from), v_at = k_at + kKeys * S::kPitch;
+            if (boxes && mask != S::kAll) {  // values that are not seen become zeros: 0 NaN is NaN
+#pragma unroll 1
+                for (int r = 0; r < kKeys; ++r)
+                    if (!(mask >> r & 1) && lane < S::kUsed) st_shared_v4(v_at + S::chunk_at(r, lane) * 16, make_uint4(0u, 0u, 0u, 0u));
+                fence_proxy_async_smem();  // before the next copy into this stage
+                __syncwarp();
+            }
+            float s[kMT][kNT][4];
+#pragma unroll
+            for (int mt = 0; mt < kMT; ++mt) {
                 float a[2][kNT][4] = {};
 #pragma unroll
                 for (int ks = 0; ks < kSteps; ks += k8 ? 2 : 1) {
                     uint32_t f[4];
-                    ldsm4(f, k_at + chunk_at<S::kCpr>(lane & 15, (k8 ? ks : 2 * ks) + (lane >> 4)) * 16);
+                    ldsm4(f, k_at + S::chunk_at(16 * mt + (lane & 15), (k8 ? ks : 2 * ks) + (lane >> 4)) * 16);
 #pragma unroll
                     for (int nt = 0; nt < kNT; ++nt) {
                         if constexpr (k8) {
@@ -377,48 +457,49 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                 }
                 float k0 = 1.f, k1 = 1.f;
                 if constexpr (k8) {
-                    const float *sc = (const float *)(from + 2 * kKeys * S::kRow);
-                    k0 = sc[g];
-                    k1 = sc[g + 8];
+                    k0 = scales[16 * mt + g];
+                    k1 = scales[16 * mt + g + 8];
                 }
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[nt][i] = (a[0][nt][i] + a[1][nt][i]) * (cs[nt][i & 1] * (i < 2 ? k0 : k1));
+                    for (int i = 0; i < 4; ++i) s[mt][nt][i] = (a[0][nt][i] + a[1][nt][i]) * (cs[nt][i & 1] * (i < 2 ? k0 : k1));
             }
-            if (mask != 0xffffu) {
+            if (mask != S::kAll) {
 #pragma unroll
-                for (int nt = 0; nt < kNT; ++nt)
+                for (int mt = 0; mt < kMT; ++mt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!(mask >> (g + (i < 2 ? 0 : 8)) & 1)) s[nt][i] = -INFINITY;
+                    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!(mask >> (16 * mt + g + (i < 2 ? 0 : 8)) & 1)) s[mt][nt][i] = -INFINITY;
             }
-            float top[kNT][2];
+            // the maximum that powers are relative to follows the scores only
+            // where one is 2^kAhead above it: no shuffles for most tiles
             bool grown = false;
 #pragma unroll
-            for (int nt = 0; nt < kNT; ++nt)
+            for (int mt = 0; mt < kMT; ++mt)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    top[nt][i] = fmaxf(s[nt][i], s[nt][i + 2]);
+                for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-                    for (int off = 4; off < 32; off <<= 1) top[nt][i] = fmaxf(top[nt][i], __shfl_xor_sync(~0u, top[nt][i], off));
-                    grown |= top[nt][i] > m[nt][i];
-                }
-            float v0 = 1.f, v1 = 1.f;
+                    for (int i = 0; i < 4; ++i) grown |= s[mt][nt][i] > m[nt][i & 1] + kAhead;
+            float v0[kMT], v1[kMT], v_top = 0.f;
             if constexpr (k8) {
-                const float *sc = (const float *)(from + 2 * kKeys * S::kRow) + kKeys;
-                v0 = sc[g];
-                v1 = sc[g + 8];
-                grown |= fmaxf(v0, v1) > r_max;
+#pragma unroll
+                for (int mt = 0; mt < kMT; ++mt) {
+                    v0[mt] = mask >> (16 * mt + g) & 1 ? scales[kKeys + 16 * mt + g] : 0.f;
+                    v1[mt] = mask >> (16 * mt + g + 8) & 1 ? scales[kKeys + 16 * mt + g + 8] : 0.f;
+                    v_top = fmaxf(v_top, fmaxf(v0[mt], v1[mt]));
+                }
+                grown |= v_top > r_max;
             }
             if (__any_sync(~0u, grown)) {
                 float by = 1.f;
                 if constexpr (k8) {
-                    float r = fmaxf(v0, v1);
 #pragma unroll
-                    for (int off = 4; off < 32; off <<= 1) r = fmaxf(r, __shfl_xor_sync(~0u, r, off));
-                    if (r > r_max) {
-                        const float to = __uint_as_float(min((__float_as_uint(r) & 0x7f800000u) + 0x00800000u, 0x7f000000u));
+                    for (int off = 4; off < 32; off <<= 1) v_top = fmaxf(v_top, __shfl_xor_sync(~0u, v_top, off));
+                    if (v_top > r_max) {
+                        const float to = __uint_as_float(min((__float_as_uint(v_top) & 0x7f800000u) + 0x00800000u, 0x7f000000u));
                         by = r_max / to;
                         r_max = to;
                     }
@@ -428,7 +509,11 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                     float f[2];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float now = fmaxf(m[nt][i], top[nt][i]);
+                        float now = fmaxf(s[0][nt][i], s[0][nt][i + 2]);
+                        if (kMT == 2) now = fmaxf(now, fmaxf(s[kMT - 1][nt][i], s[kMT - 1][nt][i + 2]));
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) now = fmaxf(now, __shfl_xor_sync(~0u, now, off));
+                        now = fmaxf(now, m[nt][i]);
                         f[i] = ex2(m[nt][i] - (now == -INFINITY ? 0.f : now));
                         m[nt][i] = now;
                         l[nt][i] *= f[i];
@@ -440,56 +525,62 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                         for (int i = 0; i < 4; ++i) o[j][nt][i] *= f[i & 1];
                 }
             }
-            const float w0 = k8 ? v0 * (0x1p14f / r_max) : 1.f, w1 = k8 ? v1 * (0x1p14f / r_max) : 1.f;
-            uint32_t hi[kNT][2], lo[kNT][2];
+            uint32_t hi[kMT][kNT][2], lo[kMT][kNT][2];
 #pragma unroll
-            for (int nt = 0; nt < kNT; ++nt) {
-                float e[4];
+            for (int mt = 0; mt < kMT; ++mt) {
+                const float w0 = k8 ? v0[mt] * (kUp / r_max) : 1.f, w1 = k8 ? v1[mt] * (kUp / r_max) : 1.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float base = m[nt][i & 1] == -INFINITY ? 0.f : m[nt][i & 1];
-                    e[i] = ex2(s[nt][i] - base);
-                    l[nt][i & 1] += e[i];
-                    if (k8) e[i] *= i < 2 ? w0 : w1;
-                }
+                for (int nt = 0; nt < kNT; ++nt) {
+                    float e[4];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t h = pack2<kBf>(e[2 * i], e[2 * i + 1]);
-                    const float2 back = unpack2<kBf>(h);
-                    hi[nt][i] = transposed(h);
-                    lo[nt][i] = transposed(pack2<kBf>(e[2 * i] - back.x, e[2 * i + 1] - back.y));
+                    for (int i = 0; i < 4; ++i) {
+                        const float base = m[nt][i & 1] == -INFINITY ? 0.f : m[nt][i & 1];
+                        e[i] = ex2(s[mt][nt][i] - base);
+                        l[nt][i & 1] += e[i];
+                        if (k8) e[i] *= i < 2 ? w0 : w1;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t h = pack2<kBf>(e[2 * i], e[2 * i + 1]);
+                        const float2 back = unpack2<kBf>(h);
+                        hi[mt][nt][i] = transposed(h);
+                        lo[mt][nt][i] = transposed(pack2<kBf>(e[2 * i] - back.x, e[2 * i + 1] - back.y));
+                    }
                 }
             }
 #pragma unroll
-            for (int j = 0; j < kSteps; j += k8 ? 2 : 1) {
-                uint32_t f[4];
-                if constexpr (k8) {
-                    ldsm4t(f, v_at + chunk_at<S::kCpr>(lane & 15, j + (lane >> 4)) * 16);
+            for (int mt = 0; mt < kMT; ++mt)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {  // bytes of a register: two columns of one key, two of the next
-                        const uint32_t x = __byte_perm(f[2 * u], 0, 0x3120), y = __byte_perm(f[2 * u + 1], 0, 0x3120);
-                        const uint32_t a0 = widen(x & 0xffffu), a1 = widen(x >> 16), a2 = widen(y & 0xffffu), a3 = widen(y >> 16);
+                for (int j = 0; j < kSteps; j += k8 ? 2 : 1) {
+                    uint32_t f[4];
+                    if constexpr (k8) {
+                        ldsm4t(f, v_at + S::chunk_at(16 * mt + (lane & 15), j + (lane >> 4)) * 16);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {  // bytes of a register: two columns of one key, two of the next
+                            const uint32_t x = __byte_perm(f[2 * u], 0, 0x3120), y = __byte_perm(f[2 * u + 1], 0, 0x3120);
+                            const uint32_t a0 = widen(x & 0xffffu), a1 = widen(x >> 16), a2 = widen(y & 0xffffu), a3 = widen(y >> 16);
+#pragma unroll
+                            for (int nt = 0; nt < kNT; ++nt) {
+                                mma16816<kBf>(o[j + u][nt], a0, a1, a2, a3, hi[mt][nt][0], hi[mt][nt][1]);
+                                mma16816<kBf>(o[j + u][nt], a0, a1, a2, a3, lo[mt][nt][0], lo[mt][nt][1]);
+                            }
+                        }
+                    } else {
+                        ldsm4t(f, v_at + S::chunk_at(16 * mt + (lane & 7) + (lane >> 4) * 8, 2 * j + ((lane >> 3) & 1)) * 16);
 #pragma unroll
                         for (int nt = 0; nt < kNT; ++nt) {
-                            mma16816<kBf>(o[j + u][nt], a0, a1, a2, a3, hi[nt][0], hi[nt][1]);
-                            mma16816<kBf>(o[j + u][nt], a0, a1, a2, a3, lo[nt][0], lo[nt][1]);
+                            mma16816<kBf>(o[j][nt], f[0], f[1], f[2], f[3], hi[mt][nt][0], hi[mt][nt][1]);
+                            mma16816<kBf>(o[j][nt], f[0], f[1], f[2], f[3], lo[mt][nt][0], lo[mt][nt][1]);
                         }
                     }
-                } else {
-                    ldsm4t(f, v_at + chunk_at<S::kCpr>((lane & 7) + (lane >> 4) * 8, 2 * j + ((lane >> 3) & 1)) * 16);
-#pragma unroll
-                    for (int nt = 0; nt < kNT; ++nt) {
-                        mma16816<kBf>(o[j][nt], f[0], f[1], f[2], f[3], hi[nt][0], hi[nt][1]);
-                        mma16816<kBf>(o[j][nt], f[0], f[1], f[2], f[3], lo[nt][0], lo[nt][1]);
-                    }
                 }
-            }
         }
 
         // ---- the end of a pair, or of this CTA's part of it
         const int b = at.b, head = at.head, block = at.block, tile = at.tile, tiles = at.s.tiles;
         fresh = at.advance(p);
         if (!fresh && t + 1 < left) continue;
+        if (lost) l[0][0] = l[0][1] = m[0][0] = m[0][1] = NAN;
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
@@ -509,31 +600,34 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                 float top = -INFINITY;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w * S::kHeads + nt * 8 + 2 * c + i]);
-                const float f = ex2(m[nt][i] - (top == -INFINITY ? 0.f : top)) * (k8 ? r_max * 0x1p-14f : 1.f);
+                const float f = ex2(m[nt][i] - (top == -INFINITY ? 0.f : top)) * (k8 ? r_max / kUp : 1.f);
 #pragma unroll
                 for (int j = 0; j < kSteps; ++j) {
                     o[j][nt][i] *= f;
                     o[j][nt][i + 2] *= f;
                 }
             }
-        // the warps' sums, one warp after another
-        constexpr int kLd = kDP + 4;  // eight columns and four pairs of heads in different banks
-#pragma unroll 1
-        for (int w = 0; w < kWarps; ++w) {
-            if (warp == w) {
+        // the warps' sums, each in the stage that the warp has just read; a
+        // head's columns turned by its number, so that few share a bank
+        auto place = [](int h, int d) { return h * kDP + (d ^ ((h >> 1 & 3) << 3)); };
+        {
+            float *mine = (float *)const_cast<uint8_t *>(from);
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j)
+            for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-                    for (int nt = 0; nt < kNT; ++nt)
+                for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int d = j * 16 + (k8 ? 2 * g + (i >> 1) : g + 8 * (i >> 1));
-                            float *at_d = all + (nt * 8 + 2 * c + (i & 1)) * kLd + d;
-                            *at_d = w == 0 ? o[j][nt][i] : *at_d + o[j][nt][i];
-                        }
-            }
-            __syncthreads();
+                    for (int i = 0; i < 4; ++i)
+                        mine[place(nt * 8 + 2 * c + (i & 1), j * 16 + (k8 ? 2 * g + (i >> 1) : g + 8 * (i >> 1)))] = o[j][nt][i];
         }
+        __syncthreads();
+        const float *sums = (const float *)(rings + (from - ring));  // of warp 0; the others' are a ring apart
+        auto sum_of = [&](int h, int d) {
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) v += sums[w * (S::kStages * S::kData / 4) + place(h, d)];
+            return v;
+        };
         auto totals = [&](int h, float &top, float &sum) {
             top = -INFINITY;
             sum = 0.f;
@@ -549,7 +643,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                 float top, sum;
                 totals(h, top, sum);
                 const float f = sum == 0.f ? 0.f : 1.f / sum;
-                for (int d = lane; d < p.kv.head_dim; d += 32) ((Q *)p.out)[(h0 + h) * p.kv.head_dim + d] = from_f32<Q>(all[h * kLd + d] * f);
+                for (int d = lane; d < p.kv.head_dim; d += 32) ((Q *)p.out)[(h0 + h) * p.kv.head_dim + d] = from_f32<Q>(sum_of(h, d) * f);
                 if (p.lse && lane == 0) p.lse[h0 + h] = (top + log2f(sum)) * kLn2;
             }
         } else {
@@ -557,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
             for (int h = warp; h < live; h += kWarps) {
                 float top, sum;
                 totals(h, top, sum);
-                for (int d = lane; d < kDP; d += 32) part[h * kDP + d] = all[h * kLd + d];
+                for (int d = lane; d < kDP; d += 32) part[h * kDP + d] = sum_of(h, d);
                 if (lane == 0) {
                     part[S::kHeads * kDP + h] = top;
                     part[S::kHeads * (kDP + 1) + h] = sum;
@@ -565,33 +659,92 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
             }
         }
         ++pieces;
+        fence_proxy_async_smem();  // before the next copies into the stages
         __syncthreads();
     }
+    if (lost)  // no copy is left behind, as far as that can be waited for
+        for (int i = 0; i < S::kStages; ++i) mbar_wait(barrier(i), parity, &s_abort, nullptr);
     cp_async_wait<0>();
 }
 
-// The parts of one head of one sequence, in the CTAs' order.
-template <typename Q>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendParams p, int dp, int block_heads)
+// The parts of a pair's block of heads, joined in the CTAs' order: of a few, by
+// one CTA with a warp a head; of many, by a CTA a head.  Which, and where the
+// parts are, follows from the lengths, before the first launch is done.
+template <typename Q, int kTile>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendParams p, int dp, int block_heads, int ctas)
 {
     constexpr int kJoinWarps = kJoinThreads / 32;
     __shared__ float s_w[kMaxCtas], s_red[kJoinWarps], s_sum[kJoinWarps][PMPE_MAX_HEAD_DIM];
+    __shared__ long long s_all[kJoinWarps], s_before[kJoinWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int pairs = p.kv.kv_heads * p.blocks, b = blockIdx.y, pair = blockIdx.x / block_heads, own = blockIdx.x - pair * block_heads;
+    long long all = 0, first = 0;
+    for (int i = threadIdx.x; i < p.kv.B; i += kJoinThreads) {
+        const int n = Span<kTile>(p, i).tiles;
+        all += n;
+        if (i < b) first += n;
+    }
+    all = warp_sum(all);
+    first = warp_sum(first);
+    if (lane == 0) s_all[warp] = all, s_before[warp] = first;
+    __syncthreads();
+    all = first = 0;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) all += s_all[w], first += s_before[w];
+    const int tiles = Span<kTile>(p, b).tiles;
+    const long long per = max((all * pairs + ctas - 1) / ctas, 1ll), t0 = first * pairs + (long long)pair * tiles;
+    const int c0 = (int)(t0 / per), n = tiles == 0 ? 1 : (int)((t0 + tiles - 1) / per) - c0 + 1;
+    const bool few = n <= kFew;
+    if (own > 0 && (n == 1 || few)) return;
     pdl_trigger();
     pdl_wait();
-    const int head = blockIdx.x, b = blockIdx.y;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long per = p.plan[0], first = p.plan[1 + b], tiles = (p.plan[2 + b] - first) / (p.kv.kv_heads * p.blocks);
-    if (tiles == 0) return;
-    const int kv_head = head / p.group, in_group = head - kv_head * p.group, block = in_group / block_heads, h = in_group - block * block_heads;
-    const long long t0 = first + (long long)(kv_head * p.blocks + block) * tiles;
-    const int c0 = (int)(t0 / per), c1 = (int)((t0 + tiles - 1) / per), n = c1 - c0 + 1;
     if (n == 1) return;
+    const long long size = block_heads * (dp + 2);
     // a CTA's first piece is in its first place
-    auto part = [&](int i) { return p.part + ((c0 + i) * 2 + (i == 0 && t0 != c0 * per)) * (long long)(block_heads * (dp + 2)); };
-    float top = -INFINITY;
-    for (int i = threadIdx.x; i < n; i += kJoinThreads) {
-        s_w[i] = part(i)[block_heads * dp + h];
-        top = fmaxf(top, s_w[i]);
+    auto part = [&](int i) { return p.part + ((c0 + i) * 2 + (i == 0 && t0 != c0 * per)) * size; };
+    const int kv_head = pair / p.blocks, block = pair - kv_head * p.blocks, live = min(p.group - block * block_heads, block_heads);
+    const long long row0 = (long long)b * p.heads + kv_head * p.group + block * block_heads;
+    if (few) {
+        for (int h = warp; h < live; h += kJoinWarps) {
+            float v[kFew][PMPE_MAX_HEAD_DIM / 32], m[kFew], l[kFew], top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kFew; ++i) {
+                m[i] = -INFINITY;
+                l[i] = 0.f;
+                if (i < n) {
+                    m[i] = part(i)[block_heads * dp + h];
+                    l[i] = part(i)[block_heads * (dp + 1) + h];
+                }
+#pragma unroll
+                for (int k = 0; k < PMPE_MAX_HEAD_DIM / 32; ++k) v[i][k] = i < n && k * 32 < dp ? part(i)[h * dp + k * 32 + lane] : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < kFew; ++i) top = fmaxf(top, m[i]);
+            float out[PMPE_MAX_HEAD_DIM / 32] = {};
+#pragma unroll
+            for (int i = 0; i < kFew; ++i) {
+                const float w = ex2(m[i] - (top == -INFINITY ? 0.f : top));
+                sum += w * l[i];
+#pragma unroll
+                for (int k = 0; k < PMPE_MAX_HEAD_DIM / 32; ++k) out[k] += w * v[i][k];
+            }
+#pragma unroll
+            for (int k = 0; k < PMPE_MAX_HEAD_DIM / 32; ++k)
+                if (k * 32 + lane < p.kv.head_dim) ((Q *)p.out)[(row0 + h) * p.kv.head_dim + k * 32 + lane] = from_f32<Q>(sum == 0.f ? 0.f : out[k] / sum);
+            if (p.lse && lane == 0) p.lse[row0 + h] = (top + log2f(sum)) * kLn2;
+        }
+        return;
+    }
+    const int h = own;
+    if (h >= live) return;
+    float top = -INFINITY, sum = 0.f;
+    float m[(kMaxCtas + kJoinThreads - 1) / kJoinThreads], l[(kMaxCtas + kJoinThreads - 1) / kJoinThreads];
+#pragma unroll
+    for (int k = 0; k < (kMaxCtas + kJoinThreads - 1) / kJoinThreads; ++k) {
+        const int i = threadIdx.x + k * kJoinThreads;
+        m[k] = i < n ? part(i)[block_heads * dp + h] : -INFINITY;
+        l[k] = i < n ? part(i)[block_heads * (dp + 1) + h] : 0.f;
+        top = fmaxf(top, m[k]);
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, off));
@@ -599,17 +752,18 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_red[w]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-    for (int i = threadIdx.x; i < n; i += kJoinThreads) {
-        s_w[i] = ex2(s_w[i] - base);
-        sum += s_w[i] * part(i)[block_heads * (dp + 1) + h];
+#pragma unroll
+    for (int k = 0; k < (kMaxCtas + kJoinThreads - 1) / kJoinThreads; ++k) {
+        const int i = threadIdx.x + k * kJoinThreads;
+        const float w = ex2(m[k] - (top == -INFINITY ? 0.f : top));
+        if (i < n) s_w[i] = w;
+        sum += w * l[k];
     }
     sum = warp_sum(sum);
     __syncthreads();
     if (lane == 0) s_red[warp] = sum;
     float acc[PMPE_MAX_HEAD_DIM / 128][4] = {};
-#pragma unroll 4
+#pragma unroll 10
     for (int i = warp; i < n; i += kJoinWarps) {
         const float *from = part(i) + h * dp;
         const float w = s_w[i];
@@ -631,14 +785,13 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) sum += s_red[w];
-    const long long row = (long long)b * p.heads + head;
     for (int d = threadIdx.x; d < p.kv.head_dim; d += kJoinThreads) {
         float v = 0.f;
 #pragma unroll
         for (int w = 0; w < kJoinWarps; ++w) v += s_sum[w][d];
-        ((Q *)p.out)[row * p.kv.head_dim + d] = from_f32<Q>(sum == 0.f ? 0.f : v / sum);
+        ((Q *)p.out)[(row0 + h) * p.kv.head_dim + d] = from_f32<Q>(sum == 0.f ? 0.f : v / sum);
     }
-    if (p.lse && threadIdx.x == 0) p.lse[row] = (top + log2f(sum)) * kLn2;
+    if (p.lse && threadIdx.x == 0) p.lse[row0 + h] = (top + log2f(sum)) * kLn2;
 }
 
 // -------------------------------------------------------------- launches
@@ -648,16 +801,27 @@ int padded(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 
 // their sums fit the registers.
 int block_heads_for(int group, int head_dim) { return group > 8 && head_dim <= 128 ? 16 : 8; }
 
-template <int kDP, int kNT, int kKind> cudaError_t launch_shape(const AttendParams &p, int ctas, cudaStream_t st)
+template <int kDP, int kNT, int kKind> cudaError_t launch_shape(const AttendParams &p0, int ctas, cudaStream_t st)
 {
     using S = AttendShape<kDP, kNT, kKind>;
+    // copies in boxes: of kKeys rows, or of 16, that lie in one page
+    AttendParams p = p0;
+    const long long rows = (long long)p.kv.pages * p.kv.kv_heads * p.kv.page_size;
+    const uint64_t words = (uint64_t)p.kv.head_dim * S::kE / 2;
+    const CUtensorMapSwizzle swizzle = S::kBox == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
+    p.box_rows = 0;
+    if (p.kv.page_size % 16 == 0 && rows < (1ll << 31) && !(((uintptr_t)p.kv.k_scale | (uintptr_t)p.kv.v_scale) & 15u) &&
+        encode_2d_box(&p.k_map, p.kv.k, words, rows, S::kBox / 2, 16, swizzle) && encode_2d_box(&p.v_map, p.kv.v, words, rows, S::kBox / 2, 16, swizzle))
+        p.box_rows = 16;
     static std::atomic<int> limit[64];
     cudaError_t err = ensure_dynamic_smem(attend_kernel<kDP, kNT, kKind>, S::kSmem, limit);
     if (err != cudaSuccess) return err;
-    err = launch_pdl(attend_kernel<kDP, kNT, kKind>, dim3(std::min(ctas * S::kCtas, kMaxCtas)), dim3(kThreads), S::kSmem, st, p);
+    ctas = std::min(ctas * S::kCtas, kMaxCtas);
+    err = launch_pdl(attend_kernel<kDP, kNT, kKind>, dim3(ctas), dim3(kThreads), S::kSmem, st, p);
     if (err != cudaSuccess) return err;
     constexpr bool q_bf = kKind == kBf16 || kKind == kE4m3Bf16;
-    return launch_pdl(join_kernel<typename std::conditional<q_bf, bf16, __half>::type>, dim3(p.heads, p.kv.B), dim3(kJoinThreads), 0, st, p, kDP, S::kHeads);
+    return launch_pdl(join_kernel<typename std::conditional<q_bf, bf16, __half>::type, S::kTile>, dim3(p.kv.kv_heads * p.blocks * S::kHeads, p.kv.B),
+                      dim3(kJoinThreads), 0, st, p, kDP, S::kHeads, ctas);
 }
 template <int kKind> cudaError_t launch_kind(const AttendParams &p, int ctas, cudaStream_t st)
 {
@@ -674,14 +838,15 @@ size_t part_bytes(int group, int head_dim) { return (size_t)kMaxCtas * 2 * block
 
 size_t kv_attend_workspace_bytes(int B, int heads, int kv_heads, int head_dim)
 {
-    return part_bytes(heads / kv_heads, head_dim) + ((size_t)B + 2) * sizeof(long long);
+    (void)B;
+    return part_bytes(heads / kv_heads, head_dim);
 }
 
 cudaError_t launch_kv_attend(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, const pmpe_kv_attend_desc &d, int num_sms, cudaStream_t st)
 {
     const int group = d.heads / c.kv_heads, bh = block_heads_for(group, c.head_dim);
     AttendParams p = {KvView(c, s), d.q, d.out, d.lse, d.q_ld, d.q_head_ld, d.heads, group, (group + bh - 1) / bh, d.window, d.scale * kLog2e,
-                      (float *)d.workspace, (long long *)((uint8_t *)d.workspace + part_bytes(group, c.head_dim))};
+                      0, {}, {}, (float *)d.workspace};
     if (c.type == PMPE_BF16) return launch_kind<kBf16>(p, num_sms, st);
     if (c.type == PMPE_F16) return launch_kind<kF16>(p, num_sms, st);
     return d.type == PMPE_BF16 ? launch_kind<kE4m3Bf16>(p, num_sms, st) : launch_kind<kE4m3F16>(p, num_sms, st);
