@@ -47,6 +47,7 @@ struct AttendParams {
     void *out;
     float *lse;
     long long q_ld, q_head_ld;
+    int q_pairs;               // two elements of q an access
     int heads, group, blocks;  // query heads of a key head, and blocks of 8 kNT of them
     int window;
     float scale_log2;
@@ -117,11 +118,10 @@ template <bool kBf> __device__ __forceinline__ void mma16816(float (&d)[4], uint
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Two e4m3 (the low half) as two FP16.
-__device__ __forceinline__ uint32_t widen(uint32_t two)
+// Four e4m3 as two pairs of FP16.
+__device__ __forceinline__ void widen(uint32_t four, uint32_t &low, uint32_t &high)
 {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
-    return (uint32_t)h.x | (uint32_t)h.y << 16;
+    asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(low), "=r"(high) : "r"(four));
 }
 __device__ __forceinline__ float ex2(float x)
 {
@@ -175,28 +175,89 @@ template <int kTile> struct Walk {
     }
 };
 
+// Work as the CTAs share it: a tile counts one, and each pair of a sequence and
+// a block of heads one more, for its queries and its end (64 sequences of 0 to
+// 8192 positions in e4m3: CTAs of equal tiles ended 26 us apart, the ones with
+// many short sequences last).  Tile k of a pair that begins at cost P is at cost
+// P + 1 + k; CTA c has the costs c per .. (c + 1) per - 1.
+struct Cost {
+    long long cost, tiles;
+};
 // The sum over the CTA's threads before this one, and over all.
-__device__ __forceinline__ long long scan_before(long long v, long long *s_warp, long long &all)
+template <int kN> __device__ __forceinline__ Cost scan_before(Cost v, Cost (&s_warp)[kN], Cost &all)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long sum = v;
+    Cost sum = v;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const long long o = __shfl_up_sync(~0u, sum, off);
-        if (lane >= off) sum += o;
+        const long long c = __shfl_up_sync(~0u, sum.cost, off), t = __shfl_up_sync(~0u, sum.tiles, off);
+        if (lane >= off) sum.cost += c, sum.tiles += t;
     }
     __syncthreads();
     if (lane == 31) s_warp[warp] = sum;
     __syncthreads();
-    long long before = sum - v;
-    all = 0;
+    Cost before = {sum.cost - v.cost, sum.tiles - v.tiles};
+    all = {0, 0};
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) before += s_warp[w];
-        all += s_warp[w];
+    for (int w = 0; w < kN; ++w) {
+        if (w < warp) before.cost += s_warp[w].cost, before.tiles += s_warp[w].tiles;
+        all.cost += s_warp[w].cost, all.tiles += s_warp[w].tiles;
     }
     return before;
 }
+// Where a cost lies: the sequence, the pair of it, and what of it comes before;
+// b = B past the end.
+struct Spot {
+    int b, pair, tile;         // the first tile from there on
+    long long before, at;      // tiles before that one; the pair's cost
+};
+template <int kTile, int kN> struct Planner {
+    const AttendParams &p;
+    Cost (&s_warp)[kN];
+    Spot (&s_spot)[2];
+    int pairs;
+    Cost all;
+    __device__ __forceinline__ Cost of(int b) const
+    {
+        const int n = Span<kTile>(p, b).tiles;
+        return {n > 0 ? (n + 1ll) * pairs : 0, (long long)n * pairs};
+    }
+    // The spots of the costs where(cost of all), two of them, in every thread.
+    template <typename F> __device__ __forceinline__ void find(F where)
+    {
+        constexpr int kThreads = 32 * kN;
+        Cost sum = {0, 0}, mine = {0, 0}, first = {0, 0};
+        for (int b0 = 0; b0 < p.kv.B; b0 += kThreads) {
+            const Cost n = of(b0 + threadIdx.x);
+            Cost total;
+            const Cost before = scan_before(n, s_warp, total);
+            if (b0 == 0) mine = n, first = before;
+            sum.cost += total.cost, sum.tiles += total.tiles;
+        }
+        all = sum;
+        if (threadIdx.x < 2) s_spot[threadIdx.x] = {p.kv.B, 0, 0, all.tiles, all.cost};
+        __syncthreads();
+        sum = {0, 0};
+        for (int b0 = 0; b0 < p.kv.B; b0 += kThreads) {
+            if (b0 > 0 || p.kv.B > kThreads) {
+                Cost total;
+                mine = of(b0 + threadIdx.x);
+                first = scan_before(mine, s_warp, total);
+                first.cost += sum.cost, first.tiles += sum.tiles;
+                sum.cost += total.cost, sum.tiles += total.tiles;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const long long x = where(all.cost, i) - first.cost;
+                if (x >= 0 && x < mine.cost) {
+                    const int tiles = (int)(mine.tiles / pairs), pair = (int)(x / (tiles + 1)), tile = max((int)(x - pair * (tiles + 1ll)) - 1, 0);
+                    s_spot[i] = {b0 + (int)threadIdx.x, pair, tile, first.tiles + (long long)pair * tiles + tile, first.cost + pair * (tiles + 1ll)};
+                }
+            }
+        }
+        __syncthreads();
+    }
+};
 
 template <int kDP, int kNT, int kKind>
 __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas)) attend_kernel(const __grid_constant__ AttendParams p)
@@ -208,8 +269,8 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     constexpr int kSteps = kDP / 16, kMT = S::kMT, kKeys = S::kKeys, kTile = S::kTile;
     using Span = Span<kTile>;
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ long long s_warp[kWarps], s_start;
-    __shared__ int s_seq;
+    __shared__ Cost s_warp[kWarps];
+    __shared__ Spot s_spot[2];
     __shared__ volatile int s_abort;
     uint8_t *rings = smem + (-smem_u32(smem) & 1023u), *smalls = rings + kWarps * S::kStages * S::kData;
     uint8_t *ring = rings + (threadIdx.x >> 5) * S::kStages * S::kData, *small = smalls + (threadIdx.x >> 5) * S::kStages * S::kSmall;
@@ -226,17 +287,11 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     pdl_trigger();  // not before: the second launch reads the lengths as soon as it starts
 
     // ---- this CTA's run of tiles
-    const int pairs = p.kv.kv_heads * p.blocks;
-    long long total = 0, mine = 0, before0 = 0;
-    for (int b0 = 0; b0 < p.kv.B; b0 += kThreads) {
-        const int b = b0 + threadIdx.x;
-        const long long n = (long long)Span(p, b).tiles * pairs;
-        long long all;
-        const long long before = total + scan_before(n, s_warp, all);
-        if (b0 == 0) mine = n, before0 = before;
-        total += all;
-    }
-    const long long per = (total + gridDim.x - 1) / gridDim.x;
+    Planner<kTile, kWarps> plan = {p, s_warp, s_spot, p.kv.kv_heads * p.blocks, {0, 0}};
+    plan.find([&](long long all, int i) {
+        const long long per = max((all + gridDim.x - 1) / gridDim.x, 1ll);
+        return (blockIdx.x + i) * per;
+    });
     // sequences that see nothing
     for (int b = blockIdx.x; b < p.kv.B; b += gridDim.x) {
         if (Span(p, b).tiles > 0) continue;
@@ -245,34 +300,9 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
         if (p.lse)
             for (int i = threadIdx.x; i < p.heads; i += kThreads) p.lse[(long long)b * p.heads + i] = -INFINITY;
     }
-    const long long start = blockIdx.x * per, left = min(total, start + per) - start;
+    const long long left = s_spot[1].before - s_spot[0].before;
     if (left <= 0) return;
-    if (p.kv.B <= kThreads) {
-        if (start >= before0 && start < before0 + mine) {
-            s_seq = threadIdx.x;
-            s_start = start - before0;
-        }
-    } else {
-        long long sum = 0;
-        for (int b0 = 0; b0 < p.kv.B; b0 += kThreads) {
-            const long long n = (long long)Span(p, b0 + threadIdx.x).tiles * pairs;
-            long long all;
-            const long long before = sum + scan_before(n, s_warp, all);
-            if (start >= before && start < before + n) {
-                s_seq = b0 + threadIdx.x;
-                s_start = start - before;
-            }
-            sum += all;
-        }
-    }
-    __syncthreads();
-    Walk<kTile> at = {s_seq, 0, 0, 0, Span(p, s_seq)};
-    {
-        const long long pair = s_start / at.s.tiles;
-        at.tile = (int)(s_start - pair * at.s.tiles);
-        at.head = (int)(pair / p.blocks);
-        at.block = (int)(pair - (long long)at.head * p.blocks);
-    }
+    Walk<kTile> at = {s_spot[0].b, s_spot[0].pair / p.blocks, s_spot[0].pair % p.blocks, s_spot[0].tile, Span(p, s_spot[0].b)};
 
     // ---- copies
     Walk<kTile> ahead = at;
@@ -369,35 +399,53 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     uint32_t parity = 0;
     bool fresh = true, lost = false;
     int first_tile = at.tile;
+    // The queries of the pair at `at`, as stored: columns 2c, 2c + 1 and 8 on of
+    // each 16 (8 bits: 4c to 4c + 3) of head g of eight; zeros where there are none.
+    auto load_queries = [&]() {
+        const int live = min(p.group - at.block * S::kHeads, S::kHeads);
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+            const int h = nt * 8 + g;
+            const uint16_t *q = (const uint16_t *)p.q + at.b * p.q_ld + (long long)(at.head * p.group + at.block * S::kHeads + h) * p.q_head_ld;
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int d = ks * 16 + (k8 ? 4 * c + 2 * i : 2 * c + 8 * i);
+                    uint32_t w = 0;
+                    if (h < live && d < p.kv.head_dim) w = p.q_pairs ? *(const uint32_t *)(q + d) : q[d] | (uint32_t)q[d + 1] << 16;
+                    qf[ks][nt][i] = w;
+                }
+        }
+    };
     for (long long t = 0; t < left; ++t) {
         if (fresh) {
             fresh = false;
             first_tile = at.tile;
-            const int live = min(p.group - at.block * S::kHeads, S::kHeads);
+            if (t == 0) load_queries();
 #pragma unroll
             for (int nt = 0; nt < kNT; ++nt) {
-                const int h = nt * 8 + g;
-                const Q *q = (const Q *)p.q + at.b * p.q_ld + (long long)(at.head * p.group + at.block * S::kHeads + h) * p.q_head_ld;
-                float x[kSteps][4], top = 0.f;
-#pragma unroll
-                for (int ks = 0; ks < kSteps; ++ks)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int d = ks * 16 + (k8 ? 4 * c + i : 2 * c + (i & 1) + 8 * (i >> 1));
-                        x[ks][i] = h < live && d < p.kv.head_dim ? to_f32<Q>(q[d]) : 0.f;
-                        top = fmaxf(top, fabsf(x[ks][i]));
-                    }
                 float up = 1.f;
                 if constexpr (kKind == kE4m3Bf16) {  // into FP16's range, by a power of two
+                    float top = 0.f;
+#pragma unroll
+                    for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float2 x = unpack2<true>(qf[ks][nt][i]);
+                            top = fmaxf(top, fmaxf(fabsf(x.x), fabsf(x.y)));
+                        }
                     top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
                     top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
                     const int e = (int)(__float_as_uint(top) >> 23) - 127;  // -127 for zeros and subnormals, 128: not finite
                     if (e < 128) up = __uint_as_float((uint32_t)(min(14 - e, 100) + 127) << 23);
-                }
 #pragma unroll
-                for (int ks = 0; ks < kSteps; ++ks) {
-                    qf[ks][nt][0] = pack2<kBf>(x[ks][0] * up, x[ks][1] * up);
-                    qf[ks][nt][1] = pack2<kBf>(x[ks][2] * up, x[ks][3] * up);
+                    for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float2 x = unpack2<true>(qf[ks][nt][i]);
+                            qf[ks][nt][i] = pack2<false>(x.x * up, x.y * up);
+                        }
                 }
                 const float f = p.scale_log2 / up;
                 cs[nt][0] = k8 ? __shfl_sync(~0u, f, 8 * c) : f;  // of heads 2c and 2c + 1
@@ -444,12 +492,16 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                 for (int ks = 0; ks < kSteps; ks += k8 ? 2 : 1) {
                     uint32_t f[4];
                     ldsm4(f, k_at + S::chunk_at(16 * mt + (lane & 15), (k8 ? ks : 2 * ks) + (lane >> 4)) * 16);
+                    uint32_t w[8];
+                    if constexpr (k8) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) widen(f[i], w[2 * i], w[2 * i + 1]);
+                    }
 #pragma unroll
                     for (int nt = 0; nt < kNT; ++nt) {
                         if constexpr (k8) {
-                            mma16816<kBf>(a[0][nt], widen(f[0] & 0xffffu), widen(f[1] & 0xffffu), widen(f[0] >> 16), widen(f[1] >> 16), qf[ks][nt][0], qf[ks][nt][1]);
-                            mma16816<kBf>(a[1][nt], widen(f[2] & 0xffffu), widen(f[3] & 0xffffu), widen(f[2] >> 16), widen(f[3] >> 16), qf[ks + 1][nt][0],
-                                          qf[ks + 1][nt][1]);
+                            mma16816<kBf>(a[0][nt], w[0], w[2], w[1], w[3], qf[ks][nt][0], qf[ks][nt][1]);
+                            mma16816<kBf>(a[1][nt], w[4], w[6], w[5], w[7], qf[ks + 1][nt][0], qf[ks + 1][nt][1]);
                         } else {
                             mma16816<kBf>(a[ks & 1][nt], f[0], f[1], f[2], f[3], qf[ks][nt][0], qf[ks][nt][1]);
                         }
@@ -557,8 +609,9 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                         ldsm4t(f, v_at + S::chunk_at(16 * mt + (lane & 15), j + (lane >> 4)) * 16);
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {  // bytes of a register: two columns of one key, two of the next
-                            const uint32_t x = __byte_perm(f[2 * u], 0, 0x3120), y = __byte_perm(f[2 * u + 1], 0, 0x3120);
-                            const uint32_t a0 = widen(x & 0xffffu), a1 = widen(x >> 16), a2 = widen(y & 0xffffu), a3 = widen(y >> 16);
+                            uint32_t a0, a1, a2, a3;
+                            widen(__byte_perm(f[2 * u], 0, 0x3120), a0, a1);
+                            widen(__byte_perm(f[2 * u + 1], 0, 0x3120), a2, a3);
 #pragma unroll
                             for (int nt = 0; nt < kNT; ++nt) {
                                 mma16816<kBf>(o[j + u][nt], a0, a1, a2, a3, hi[mt][nt][0], hi[mt][nt][1]);
@@ -620,6 +673,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                     for (int i = 0; i < 4; ++i)
                         mine[place(nt * 8 + 2 * c + (i & 1), j * 16 + (k8 ? 2 * g + (i >> 1) : g + 8 * (i >> 1)))] = o[j][nt][i];
         }
+        if (t + 1 < left) load_queries();  // of the next pair: on the way while this one ends
         __syncthreads();
         const float *sums = (const float *)(rings + (from - ring));  // of warp 0; the others' are a ring apart
         auto sum_of = [&](int h, int d) {
@@ -667,41 +721,36 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     cp_async_wait<0>();
 }
 
-// The parts of a pair's block of heads, joined in the CTAs' order: of a few, by
-// one CTA with a warp a head; of many, by a CTA a head.  Which, and where the
-// parts are, follows from the lengths, before the first launch is done.
+// The parts of a pair, joined in the CTAs' order.  A CTA for each border between
+// two CTAs of the first launch; of a pair with a few parts the first border's
+// does all, a warp a head; of one with many each border's does some heads.
+// Which, and where the parts are, follows from the lengths, before the first
+// launch is done.
 template <typename Q, int kTile>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendParams p, int dp, int block_heads, int ctas)
 {
     constexpr int kJoinWarps = kJoinThreads / 32;
     __shared__ float s_w[kMaxCtas], s_red[kJoinWarps], s_sum[kJoinWarps][PMPE_MAX_HEAD_DIM];
-    __shared__ long long s_all[kJoinWarps], s_before[kJoinWarps];
+    __shared__ Cost s_warp[kJoinWarps];
+    __shared__ Spot s_spot[2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int pairs = p.kv.kv_heads * p.blocks, b = blockIdx.y, pair = blockIdx.x / block_heads, own = blockIdx.x - pair * block_heads;
-    long long all = 0, first = 0;
-    for (int i = threadIdx.x; i < p.kv.B; i += kJoinThreads) {
-        const int n = Span<kTile>(p, i).tiles;
-        all += n;
-        if (i < b) first += n;
-    }
-    all = warp_sum(all);
-    first = warp_sum(first);
-    if (lane == 0) s_all[warp] = all, s_before[warp] = first;
-    __syncthreads();
-    all = first = 0;
-#pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) all += s_all[w], first += s_before[w];
-    const int tiles = Span<kTile>(p, b).tiles;
-    const long long per = max((all * pairs + ctas - 1) / ctas, 1ll), t0 = first * pairs + (long long)pair * tiles;
-    const int c0 = (int)(t0 / per), n = tiles == 0 ? 1 : (int)((t0 + tiles - 1) / per) - c0 + 1;
+    Planner<kTile, kJoinWarps> plan = {p, s_warp, s_spot, p.kv.kv_heads * p.blocks, {0, 0}};
+    long long per = 1;
+    plan.find([&](long long all, int) {
+        per = max((all + ctas - 1) / ctas, 1ll);
+        return (blockIdx.x + 1) * per;
+    });
+    const Spot spot = s_spot[0];  // of what the border cuts
+    const int b = spot.b, pair = spot.pair, tiles = b < p.kv.B ? Span<kTile>(p, b).tiles : 0;
+    const int c0 = (int)((spot.at + 1) / per), n = tiles > 0 ? (int)((spot.at + tiles) / per) - c0 + 1 : 1;
+    const int own = (int)blockIdx.x - c0;  // the own-th border of the pair
     const bool few = n <= kFew;
-    if (own > 0 && (n == 1 || few)) return;
     pdl_trigger();
     pdl_wait();
-    if (n == 1) return;
+    if (n == 1 || own < 0 || (few && own > 0)) return;
     const long long size = block_heads * (dp + 2);
     // a CTA's first piece is in its first place
-    auto part = [&](int i) { return p.part + ((c0 + i) * 2 + (i == 0 && t0 != c0 * per)) * size; };
+    auto part = [&](int i) { return p.part + ((c0 + i) * 2 + (i == 0 && c0 * per < spot.at)) * size; };
     const int kv_head = pair / p.blocks, block = pair - kv_head * p.blocks, live = min(p.group - block * block_heads, block_heads);
     const long long row0 = (long long)b * p.heads + kv_head * p.group + block * block_heads;
     if (few) {
@@ -735,8 +784,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         }
         return;
     }
-    const int h = own;
-    if (h >= live) return;
+    for (int h = own; h < live; h += n - 1) {
     float top = -INFINITY, sum = 0.f;
     float m[(kMaxCtas + kJoinThreads - 1) / kJoinThreads], l[(kMaxCtas + kJoinThreads - 1) / kJoinThreads];
 #pragma unroll
@@ -792,6 +840,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         ((Q *)p.out)[(row0 + h) * p.kv.head_dim + d] = from_f32<Q>(sum == 0.f ? 0.f : v / sum);
     }
     if (p.lse && threadIdx.x == 0) p.lse[row0 + h] = (top + log2f(sum)) * kLn2;
+        __syncthreads();
+    }
 }
 
 // -------------------------------------------------------------- launches
@@ -820,8 +870,7 @@ template <int kDP, int kNT, int kKind> cudaError_t launch_shape(const AttendPara
     err = launch_pdl(attend_kernel<kDP, kNT, kKind>, dim3(ctas), dim3(kThreads), S::kSmem, st, p);
     if (err != cudaSuccess) return err;
     constexpr bool q_bf = kKind == kBf16 || kKind == kE4m3Bf16;
-    return launch_pdl(join_kernel<typename std::conditional<q_bf, bf16, __half>::type, S::kTile>, dim3(p.kv.kv_heads * p.blocks * S::kHeads, p.kv.B),
-                      dim3(kJoinThreads), 0, st, p, kDP, S::kHeads, ctas);
+    return launch_pdl(join_kernel<typename std::conditional<q_bf, bf16, __half>::type, S::kTile>, dim3(std::max(ctas - 1, 1)), dim3(kJoinThreads), 0, st, p, kDP, S::kHeads, ctas);
 }
 template <int kKind> cudaError_t launch_kind(const AttendParams &p, int ctas, cudaStream_t st)
 {
@@ -845,7 +894,8 @@ size_t kv_attend_workspace_bytes(int B, int heads, int kv_heads, int head_dim)
 cudaError_t launch_kv_attend(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, const pmpe_kv_attend_desc &d, int num_sms, cudaStream_t st)
 {
     const int group = d.heads / c.kv_heads, bh = block_heads_for(group, c.head_dim);
-    AttendParams p = {KvView(c, s), d.q, d.out, d.lse, d.q_ld, d.q_head_ld, d.heads, group, (group + bh - 1) / bh, d.window, d.scale * kLog2e,
+    AttendParams p = {KvView(c, s), d.q, d.out, d.lse, d.q_ld, d.q_head_ld,
+                      ((uintptr_t)d.q & 3u) == 0 && d.q_ld % 2 == 0 && d.q_head_ld % 2 == 0, d.heads, group, (group + bh - 1) / bh, d.window, d.scale * kLog2e,
                       0, {}, {}, (float *)d.workspace};
     if (c.type == PMPE_BF16) return launch_kind<kBf16>(p, num_sms, st);
     if (c.type == PMPE_F16) return launch_kind<kF16>(p, num_sms, st);
