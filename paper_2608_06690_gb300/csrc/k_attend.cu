@@ -176,10 +176,12 @@ template <int kTile> struct Walk {
 };
 
 // Work as the CTAs share it: a tile counts one, and each pair of a sequence and
-// a block of heads one more, for its queries and its end (64 sequences of 0 to
+// a block of heads kEnd more, for its queries and its end (64 sequences of 0 to
 // 8192 positions in e4m3: CTAs of equal tiles ended 26 us apart, the ones with
-// many short sequences last).  Tile k of a pair that begins at cost P is at cost
-// P + 1 + k; CTA c has the costs c per .. (c + 1) per - 1.
+// many short sequences last; kEnd = 1, 2, 3, 4: 63.1, 63.6, 57.2, 56.7 us, in
+// BF16 86.8 to 87.8).  Tile k of a pair that begins at cost P is at cost
+// P + kEnd + k; CTA c has the costs c per .. (c + 1) per - 1.
+constexpr long long kEnd = 3;
 struct Cost {
     long long cost, tiles;
 };
@@ -220,7 +222,7 @@ template <int kTile, int kN> struct Planner {
     __device__ __forceinline__ Cost of(int b) const
     {
         const int n = Span<kTile>(p, b).tiles;
-        return {n > 0 ? (n + 1ll) * pairs : 0, (long long)n * pairs};
+        return {n > 0 ? (n + kEnd) * pairs : 0, (long long)n * pairs};
     }
     // The spots of the costs where(cost of all), two of them, in every thread.
     template <typename F> __device__ __forceinline__ void find(F where)
@@ -250,8 +252,8 @@ template <int kTile, int kN> struct Planner {
             for (int i = 0; i < 2; ++i) {
                 const long long x = where(all.cost, i) - first.cost;
                 if (x >= 0 && x < mine.cost) {
-                    const int tiles = (int)(mine.tiles / pairs), pair = (int)(x / (tiles + 1)), tile = max((int)(x - pair * (tiles + 1ll)) - 1, 0);
-                    s_spot[i] = {b0 + (int)threadIdx.x, pair, tile, first.tiles + (long long)pair * tiles + tile, first.cost + pair * (tiles + 1ll)};
+                    const int tiles = (int)(mine.tiles / pairs), pair = (int)(x / (tiles + kEnd)), tile = max((int)(x - pair * (tiles + kEnd) - kEnd), 0);
+                    s_spot[i] = {b0 + (int)threadIdx.x, pair, tile, first.tiles + (long long)pair * tiles + tile, first.cost + pair * (tiles + kEnd)};
                 }
             }
         }
@@ -730,7 +732,8 @@ template <typename Q, int kTile>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendParams p, int dp, int block_heads, int ctas)
 {
     constexpr int kJoinWarps = kJoinThreads / 32;
-    __shared__ float s_w[kMaxCtas], s_red[kJoinWarps], s_sum[kJoinWarps][PMPE_MAX_HEAD_DIM];
+    __shared__ float s_top[kJoinWarps], s_total[kJoinWarps];
+    __shared__ __align__(16) float s_sum[kJoinWarps][PMPE_MAX_HEAD_DIM];
     __shared__ Cost s_warp[kJoinWarps];
     __shared__ Spot s_spot[2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -742,7 +745,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     });
     const Spot spot = s_spot[0];  // of what the border cuts
     const int b = spot.b, pair = spot.pair, tiles = b < p.kv.B ? Span<kTile>(p, b).tiles : 0;
-    const int c0 = (int)((spot.at + 1) / per), n = tiles > 0 ? (int)((spot.at + tiles) / per) - c0 + 1 : 1;
+    const int c0 = (int)((spot.at + kEnd) / per), n = tiles > 0 ? (int)((spot.at + kEnd + tiles - 1) / per) - c0 + 1 : 1;
     const int own = (int)blockIdx.x - c0;  // the own-th border of the pair
     const bool few = n <= kFew;
     pdl_trigger();
@@ -784,62 +787,72 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         }
         return;
     }
+    // every load of a part is on the way before one is waited for
     for (int h = own; h < live; h += n - 1) {
-    float top = -INFINITY, sum = 0.f;
-    float m[(kMaxCtas + kJoinThreads - 1) / kJoinThreads], l[(kMaxCtas + kJoinThreads - 1) / kJoinThreads];
+        constexpr int kAtOnce = 8;
+        float acc[PMPE_MAX_HEAD_DIM / 128][4] = {}, top = -INFINITY, sum = 0.f;
+        for (int i0 = warp; i0 < n; i0 += kJoinWarps * kAtOnce) {
+            float4 v[kAtOnce][PMPE_MAX_HEAD_DIM / 128];
+            float m[kAtOnce], l[kAtOnce], now = top;
 #pragma unroll
-    for (int k = 0; k < (kMaxCtas + kJoinThreads - 1) / kJoinThreads; ++k) {
-        const int i = threadIdx.x + k * kJoinThreads;
-        m[k] = i < n ? part(i)[block_heads * dp + h] : -INFINITY;
-        l[k] = i < n ? part(i)[block_heads * (dp + 1) + h] : 0.f;
-        top = fmaxf(top, m[k]);
-    }
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int i = i0 + j * kJoinWarps;
+                m[j] = -INFINITY;
+                l[j] = 0.f;
+                if (i < n) {
+                    m[j] = part(i)[block_heads * dp + h];
+                    l[j] = part(i)[block_heads * (dp + 1) + h];
+                }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, off));
-    if (lane == 0) s_red[warp] = top;
-    __syncthreads();
+                for (int k = 0; k < PMPE_MAX_HEAD_DIM / 128; ++k) {
+                    const int d = k * 128 + lane * 4;
+                    v[j][k] = i < n && d < dp ? *reinterpret_cast<const float4 *>(part(i) + h * dp + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+            }
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_red[w]);
+            for (int j = 0; j < kAtOnce; ++j) now = fmaxf(now, m[j]);
+            const float base = now == -INFINITY ? 0.f : now, f = ex2(top - base);
+            sum *= f;
 #pragma unroll
-    for (int k = 0; k < (kMaxCtas + kJoinThreads - 1) / kJoinThreads; ++k) {
-        const int i = threadIdx.x + k * kJoinThreads;
-        const float w = ex2(m[k] - (top == -INFINITY ? 0.f : top));
-        if (i < n) s_w[i] = w;
-        sum += w * l[k];
-    }
-    sum = warp_sum(sum);
-    __syncthreads();
-    if (lane == 0) s_red[warp] = sum;
-    float acc[PMPE_MAX_HEAD_DIM / 128][4] = {};
-#pragma unroll 10
-    for (int i = warp; i < n; i += kJoinWarps) {
-        const float *from = part(i) + h * dp;
-        const float w = s_w[i];
+            for (int k = 0; k < PMPE_MAX_HEAD_DIM / 128; ++k)
 #pragma unroll
-        for (int k = 0; k < PMPE_MAX_HEAD_DIM / 128; ++k) {
-            const int d = k * 128 + lane * 4;
-            if (d >= dp) break;
-            const float4 v = *reinterpret_cast<const float4 *>(from + d);
-            acc[k][0] += w * v.x;
-            acc[k][1] += w * v.y;
-            acc[k][2] += w * v.z;
-            acc[k][3] += w * v.w;
+                for (int e = 0; e < 4; ++e) acc[k][e] *= f;
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const float w = ex2(m[j] - base);
+                sum += w * l[j];
+#pragma unroll
+                for (int k = 0; k < PMPE_MAX_HEAD_DIM / 128; ++k) {
+                    acc[k][0] += w * v[j][k].x;
+                    acc[k][1] += w * v[j][k].y;
+                    acc[k][2] += w * v[j][k].z;
+                    acc[k][3] += w * v[j][k].w;
+                }
+            }
+            top = now;
         }
-    }
+        if (lane == 0) s_top[warp] = top, s_total[warp] = sum;
 #pragma unroll
-    for (int k = 0; k < PMPE_MAX_HEAD_DIM / 128; ++k)
-        if (k * 128 + lane * 4 < dp) *reinterpret_cast<float4 *>(&s_sum[warp][k * 128 + lane * 4]) = make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
-    __syncthreads();
-    sum = 0.f;
+        for (int k = 0; k < PMPE_MAX_HEAD_DIM / 128; ++k)
+            if (k * 128 + lane * 4 < dp) *reinterpret_cast<float4 *>(&s_sum[warp][k * 128 + lane * 4]) = make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
+        __syncthreads();
+        top = -INFINITY;
+        sum = 0.f;
+        float f[kJoinWarps];
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) sum += s_red[w];
-    for (int d = threadIdx.x; d < p.kv.head_dim; d += kJoinThreads) {
-        float v = 0.f;
+        for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_top[w]);
 #pragma unroll
-        for (int w = 0; w < kJoinWarps; ++w) v += s_sum[w][d];
-        ((Q *)p.out)[(row0 + h) * p.kv.head_dim + d] = from_f32<Q>(sum == 0.f ? 0.f : v / sum);
-    }
-    if (p.lse && threadIdx.x == 0) p.lse[row0 + h] = (top + log2f(sum)) * kLn2;
+        for (int w = 0; w < kJoinWarps; ++w) {
+            f[w] = ex2(s_top[w] - (top == -INFINITY ? 0.f : top));
+            sum += f[w] * s_total[w];
+        }
+        for (int d = threadIdx.x; d < p.kv.head_dim; d += kJoinThreads) {
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < kJoinWarps; ++w) v += f[w] * s_sum[w][d];
+            ((Q *)p.out)[(row0 + h) * p.kv.head_dim + d] = from_f32<Q>(sum == 0.f ? 0.f : v / sum);
+        }
+        if (p.lse && threadIdx.x == 0) p.lse[row0 + h] = (top + log2f(sum)) * kLn2;
         __syncthreads();
     }
 }
