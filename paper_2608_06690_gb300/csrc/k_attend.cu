@@ -53,7 +53,7 @@ struct AttendParams {
     float scale_log2;
     int box_rows;              // of a TMA copy: positions that lie one after another in a page; 0: copied one by one
     CUtensorMap k_map, v_map;  // the keys and values as rows of 16-bit words
-    float *part;               // [CTAs][2][8 kNT][kDP + 2]: sums, maxima, totals
+    float *part;               // [CTAs][2]: [8 kNT][kDP] sums, [8 kNT][2] maxima and totals
 };
 
 template <int kDP, int kNT, int kKind> struct AttendShape {
@@ -179,8 +179,9 @@ template <int kTile> struct Walk {
 // a block of heads kEnd more, for its queries and its end (64 sequences of 0 to
 // 8192 positions in e4m3: CTAs of equal tiles ended 26 us apart, the ones with
 // many short sequences last; kEnd = 1, 2, 3, 4: 63.1, 63.6, 57.2, 56.7 us, in
-// BF16 86.8 to 87.8).  Tile k of a pair that begins at cost P is at cost
-// P + kEnd + k; CTA c has the costs c per .. (c + 1) per - 1.
+// BF16 86.8 to 87.8, where a pair's end takes as long as 1.6 tiles).  Tile k of a
+// pair that begins at cost P is at cost P + kEnd + k; CTA c has the costs c per ..
+// (c + 1) per - 1.
 constexpr long long kEnd = 3;
 struct Cost {
     long long cost, tiles;
@@ -708,10 +709,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                 float top, sum;
                 totals(h, top, sum);
                 for (int d = lane; d < kDP; d += 32) part[h * kDP + d] = sum_of(h, d);
-                if (lane == 0) {
-                    part[S::kHeads * kDP + h] = top;
-                    part[S::kHeads * (kDP + 1) + h] = sum;
-                }
+                if (lane == 0) *reinterpret_cast<float2 *>(part + S::kHeads * kDP + 2 * h) = make_float2(top, sum);
             }
         }
         ++pieces;
@@ -758,31 +756,40 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     const long long row0 = (long long)b * p.heads + kv_head * p.group + block * block_heads;
     if (few) {
         for (int h = warp; h < live; h += kJoinWarps) {
-            float v[kFew][PMPE_MAX_HEAD_DIM / 32], m[kFew], l[kFew], top = -INFINITY, sum = 0.f;
+            float4 v[kFew][PMPE_MAX_HEAD_DIM / 128];
+            float2 ml[kFew];  // maximum and total
 #pragma unroll
             for (int i = 0; i < kFew; ++i) {
-                m[i] = -INFINITY;
-                l[i] = 0.f;
-                if (i < n) {
-                    m[i] = part(i)[block_heads * dp + h];
-                    l[i] = part(i)[block_heads * (dp + 1) + h];
+                ml[i] = i < n ? *reinterpret_cast<const float2 *>(part(i) + block_heads * dp + 2 * h) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+                for (int k = 0; k < PMPE_MAX_HEAD_DIM / 128; ++k) {
+                    const int d = k * 128 + lane * 4;
+                    v[i][k] = i < n && d < dp ? *reinterpret_cast<const float4 *>(part(i) + h * dp + d) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
-#pragma unroll
-                for (int k = 0; k < PMPE_MAX_HEAD_DIM / 32; ++k) v[i][k] = i < n && k * 32 < dp ? part(i)[h * dp + k * 32 + lane] : 0.f;
             }
+            float top = -INFINITY, sum = 0.f, acc[PMPE_MAX_HEAD_DIM / 128][4] = {};
 #pragma unroll
-            for (int i = 0; i < kFew; ++i) top = fmaxf(top, m[i]);
-            float out[PMPE_MAX_HEAD_DIM / 32] = {};
+            for (int i = 0; i < kFew; ++i) top = fmaxf(top, ml[i].x);
 #pragma unroll
             for (int i = 0; i < kFew; ++i) {
-                const float w = ex2(m[i] - (top == -INFINITY ? 0.f : top));
-                sum += w * l[i];
+                const float w = ex2(ml[i].x - (top == -INFINITY ? 0.f : top));
+                sum += w * ml[i].y;
 #pragma unroll
-                for (int k = 0; k < PMPE_MAX_HEAD_DIM / 32; ++k) out[k] += w * v[i][k];
+                for (int k = 0; k < PMPE_MAX_HEAD_DIM / 128; ++k) {
+                    acc[k][0] += w * v[i][k].x;
+                    acc[k][1] += w * v[i][k].y;
+                    acc[k][2] += w * v[i][k].z;
+                    acc[k][3] += w * v[i][k].w;
+                }
             }
+            const float f = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-            for (int k = 0; k < PMPE_MAX_HEAD_DIM / 32; ++k)
-                if (k * 32 + lane < p.kv.head_dim) ((Q *)p.out)[(row0 + h) * p.kv.head_dim + k * 32 + lane] = from_f32<Q>(sum == 0.f ? 0.f : out[k] / sum);
+            for (int k = 0; k < PMPE_MAX_HEAD_DIM / 128; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int d = k * 128 + lane * 4 + e;
+                    if (d < p.kv.head_dim) ((Q *)p.out)[(row0 + h) * p.kv.head_dim + d] = from_f32<Q>(acc[k][e] * f);
+                }
             if (p.lse && lane == 0) p.lse[row0 + h] = (top + log2f(sum)) * kLn2;
         }
         return;
@@ -800,8 +807,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
                 m[j] = -INFINITY;
                 l[j] = 0.f;
                 if (i < n) {
-                    m[j] = part(i)[block_heads * dp + h];
-                    l[j] = part(i)[block_heads * (dp + 1) + h];
+                    const float2 ml = *reinterpret_cast<const float2 *>(part(i) + block_heads * dp + 2 * h);
+                    m[j] = ml.x;
+                    l[j] = ml.y;
                 }
 #pragma unroll
                 for (int k = 0; k < PMPE_MAX_HEAD_DIM / 128; ++k) {
