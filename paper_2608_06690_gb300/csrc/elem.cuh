@@ -217,9 +217,10 @@ __device__ __forceinline__ uint32_t e4m3x2(float a, float b)
 {
     return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
-__device__ __forceinline__ float2 e4m3x2_to_f32(uint32_t two)
+// Four e4m3 as two pairs of FP16.
+__device__ __forceinline__ void e4m3x4_to_f16(uint32_t four, uint32_t &low, uint32_t &high)
 {
-    return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3)));
+    asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(low), "=r"(high) : "r"(four));
 }
 
 }  // namespace pmpe

@@ -118,11 +118,6 @@ template <bool kBf> __device__ __forceinline__ void mma16816(float (&d)[4], uint
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Four e4m3 as two pairs of FP16.
-__device__ __forceinline__ void widen(uint32_t four, uint32_t &low, uint32_t &high)
-{
-    asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(low), "=r"(high) : "r"(four));
-}
 __device__ __forceinline__ float ex2(float x)
 {
     float r;
@@ -498,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                     uint32_t w[8];
                     if constexpr (k8) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) widen(f[i], w[2 * i], w[2 * i + 1]);
+                        for (int i = 0; i < 4; ++i) e4m3x4_to_f16(f[i], w[2 * i], w[2 * i + 1]);
                     }
 #pragma unroll
                     for (int nt = 0; nt < kNT; ++nt) {
@@ -613,8 +608,8 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {  // bytes of a register: two columns of one key, two of the next
                             uint32_t a0, a1, a2, a3;
-                            widen(__byte_perm(f[2 * u], 0, 0x3120), a0, a1);
-                            widen(__byte_perm(f[2 * u + 1], 0, 0x3120), a2, a3);
+                            e4m3x4_to_f16(__byte_perm(f[2 * u], 0, 0x3120), a0, a1);
+                            e4m3x4_to_f16(__byte_perm(f[2 * u + 1], 0, 0x3120), a2, a3);
 #pragma unroll
                             for (int nt = 0; nt < kNT; ++nt) {
                                 mma16816<kBf>(o[j + u][nt], a0, a1, a2, a3, hi[mt][nt][0], hi[mt][nt][1]);

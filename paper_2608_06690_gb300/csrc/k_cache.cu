@@ -5,18 +5,23 @@
 //
 // A group of lanes holds one head of one row's key or value, eight elements a
 // lane, so that the largest magnitude is a few shuffles and both sides are
-// accessed 16 bytes a lane.  Where a row goes (its sequence by a search over
-// the offsets, its page by the table) is found once a CTA, by one thread a row,
-// while the rows' loads are on the way: four dependent loads that every group
-// would wait for otherwise.  Bytes bound both directions.
+// accessed 16 bytes a lane.  A CTA takes a run of rows.  Where they go (the
+// sequence by a search over the offsets, the page by the table: a chain of
+// loads) is found for all of them at once, a thread a row, while the first rows
+// are on the way; then the groups go through the rows' heads, the next ones'
+// loads ahead.  Bytes bound both directions.
+#include <string.h>
+
 #include <algorithm>
+#include <type_traits>
 
 #include "kv_cache.cuh"
 
 namespace pmpe {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kCtas = 8;  // kCtas: of an SM
+constexpr int kMaxRowsOfCta = 512;
 
 struct CacheParams {
     KvView kv;
@@ -24,13 +29,14 @@ struct CacheParams {
     void *k_out, *v_out;      // read: destination
     long long k_ld, k_head_ld, v_ld, v_head_ld;
     int T;
-    long long items;          // T * 2 * kv_heads
+    int rows, heads;          // of a CTA: rows, and of each as many of its keys' and values' heads
+    FastDiv by_heads;
 };
 
 // The entry (page * kv_heads * page_size + place: of head 0) of row r, -1 for none.
 __device__ __forceinline__ long long entry_of(const KvView &kv, int r)
 {
-    int b = r, pos;
+    int b = r, last = r + 1;
     if (kv.B == 0) return -1;
     if (kv.cu) {
         int lo = 0, hi = kv.B;  // the last b < B with cu[b] <= r; offsets that decrease lead to some b, checked below
@@ -40,131 +46,149 @@ __device__ __forceinline__ long long entry_of(const KvView &kv, int r)
             else hi = mid;
         }
         b = lo;
-        const int first = __ldg(kv.cu + b), last = __ldg(kv.cu + b + 1);
-        if (r < first || r >= last) return -1;
-        const long long at = (long long)__ldg(kv.lengths + b) - last + r;
-        if (at < 0 || at >= kv.capacity) return -1;
-        pos = (int)at;
-    } else {
-        pos = __ldg(kv.lengths + b) - 1;
-        if (pos < 0 || pos >= kv.capacity) return -1;
+        last = __ldg(kv.cu + b + 1);
+        if (r < __ldg(kv.cu + b) || r >= last) return -1;
     }
-    const int j = kv.by_page.quotient(pos), page = __ldg(kv.table + b * kv.table_ld + j);
+    const long long pos = (long long)__ldg(kv.lengths + b) - last + r;
+    if (pos < 0 || pos >= kv.capacity) return -1;
+    const int j = kv.by_page.quotient((int)pos), page = __ldg(kv.table + b * kv.table_ld + j);
     if ((unsigned)page >= (unsigned)kv.pages) return -1;
-    return (long long)page * kv.kv_heads * kv.page_size + (pos - j * kv.page_size);
+    return (long long)page * kv.kv_heads * kv.page_size + ((int)pos - j * kv.page_size);
 }
 
+// One head of one row.
+struct Item {
+    int row, head;  // row: of the CTA's
+    bool is_v, live;
+};
+
 // kBack: out of the cache.  kLanes: of a head, 8 elements each.  T: the rows'
-// type, C: the cache's (uint8_t: e4m3).  kVec: whole vectors.  kPer: heads of a group.
-template <typename T, typename C, int kLanes, bool kVec, bool kBack, int kPer>
-__global__ void __launch_bounds__(kThreads) cache_kernel(const __grid_constant__ CacheParams p)
+// type, C: the cache's (uint8_t: e4m3).  kVec: whole vectors.
+template <typename T, typename C, int kLanes, bool kVec, bool kBack>
+__global__ void __launch_bounds__(kThreads, kCtas) cache_kernel(const __grid_constant__ CacheParams p)
 {
-    constexpr int kGroups = kThreads / kLanes, kItems = kGroups * kPer;
+    constexpr int kGroups = kThreads / kLanes;
     constexpr bool k8 = sizeof(C) == 1;
-    __shared__ long long s_entry[kItems / 2 + 2];
+    __shared__ long long s_entry[kMaxRowsOfCta];
     pdl_trigger();
     pdl_wait();
-    const int per_row = 2 * p.kv.kv_heads, D = p.kv.head_dim;
-    const long long first = (long long)blockIdx.x * kItems;
-    const int r0 = (int)(first / per_row), rows = (int)((min(first + kItems, p.items) - 1) / per_row) - r0 + 1;
+    const int D = p.kv.head_dim, r0 = blockIdx.x * p.rows, rows = min(p.rows, p.T - r0), h0 = blockIdx.y * p.heads, items = rows * p.heads;
     const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, c = 8 * lane;
-    float x[kPer][8];
-    int row[kPer], head[kPer];
-    bool is_v[kPer], live[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const long long item = first + i * kGroups + group;
-        live[i] = item < p.items && c < D;
-        const int at = (int)(item - (long long)r0 * per_row);  // below kItems + per_row
-        row[i] = at / per_row;
-        const int h = at - row[i] * per_row;
-        is_v[i] = h >= p.kv.kv_heads;
-        head[i] = is_v[i] ? h - p.kv.kv_heads : h;
-        if (!kBack && live[i]) {
-            const T *src = is_v[i] ? (const T *)p.v + (r0 + row[i]) * p.v_ld + head[i] * p.v_head_ld
-                                   : (const T *)p.k + (r0 + row[i]) * p.k_ld + head[i] * p.k_head_ld;
+    auto item = [&](int n) {
+        Item it;
+        it.row = p.by_heads.quotient(n);
+        const int h = h0 + n - it.row * p.heads;
+        it.is_v = h >= p.kv.kv_heads;
+        it.head = it.is_v ? h - p.kv.kv_heads : h;
+        it.live = n < items && it.head < p.kv.kv_heads && c < D;
+        return it;
+    };
+    // an item's eight elements, and what scales them, as they lie in memory
+    struct Loaded {
+        typename std::conditional<kBack && k8, uint2, Raw8<typename std::conditional<kBack, typename std::conditional<k8, float, C>::type, T>::type>>::type raw;
+        float scale;
+    };
+    auto fetch = [&](int n, Loaded &l) {
+        const Item it = item(n);
+        memset(&l, 0, sizeof(l));
+        if (!it.live) return;
+        if constexpr (!kBack) {
+            const T *src = it.is_v ? (const T *)p.v + (r0 + it.row) * p.v_ld + it.head * p.v_head_ld
+                                   : (const T *)p.k + (r0 + it.row) * p.k_ld + it.head * p.k_head_ld;
             if (kVec) {
-                Raw8<T> raw;
-                load8<true>(raw, src + c, 8);
-                unpack(raw, x[i]);
+                load8<true>(l.raw, src + c, 8);
             } else {
+                T v[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[i][j] = to_f32<T>(src[c + j]);
+                for (int j = 0; j < 8; ++j) v[j] = src[c + j];
+                memcpy(&l.raw, v, sizeof(v));
             }
         } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
+            const long long e0 = s_entry[it.row], e = e0 + (long long)it.head * p.kv.page_size;
+            if (e0 < 0) return;
+            const C *at = (const C *)(it.is_v ? p.kv.v : p.kv.k) + e * D + c;
+            if constexpr (k8) {
+                l.raw = *reinterpret_cast<const uint2 *>(at);
+                l.scale = (it.is_v ? p.kv.v_scale : p.kv.k_scale)[e];
+            } else {
+                load8<true>(l.raw, at, 8);
+            }
         }
-    }
+    };
+    Loaded now, next;
+    if (!kBack) fetch(group, now);
     for (int i = threadIdx.x; i < rows; i += kThreads) s_entry[i] = entry_of(p.kv, r0 + i);
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const long long e0 = live[i] ? s_entry[row[i]] : -1;
-        const long long e = e0 + (long long)head[i] * p.kv.page_size;
-        C *at = (C *)(is_v[i] ? p.kv.v : p.kv.k) + e * D + c;
-        float *scale = (is_v[i] ? p.kv.v_scale : p.kv.k_scale) + e;
-        if (!kBack) {
+    if (kBack) fetch(group, now);
+    for (int n = group; n - group < items; n += kGroups) {
+        fetch(n + kGroups, next);
+        const Item it = item(n);
+        float x[8];
+        if constexpr (!kBack) {
+            unpack(now.raw, x);
+            const long long e0 = it.live ? s_entry[it.row] : -1, e = e0 + (long long)it.head * p.kv.page_size;
+            C *at = (C *)(it.is_v ? p.kv.v : p.kv.k) + e * D + c;
             if constexpr (k8) {
                 float amax = 0.f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) amax = max_magnitude(amax, x[i][j]);
+                for (int j = 0; j < 8; ++j) amax = max_magnitude(amax, x[j]);
 #pragma unroll
                 for (int off = kLanes / 2; off > 0; off >>= 1) amax = max_magnitude(amax, __shfl_xor_sync(~0u, amax, off));
                 float s;
                 const Divide by = divide_by(amax, 1.f, s);
-                if (e0 < 0) continue;
-                if (lane == 0) *scale = s;
-                float q[8];
+                if (e0 >= 0) {
+                    if (lane == 0) (it.is_v ? p.kv.v_scale : p.kv.k_scale)[e] = s;
+                    float q[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) q[j] = fmaf(x[i][j], by.hi, x[i][j] * by.lo);
-                *reinterpret_cast<uint2 *>(at) =
-                    make_uint2(e4m3x2(q[0], q[1]) | e4m3x2(q[2], q[3]) << 16, e4m3x2(q[4], q[5]) | e4m3x2(q[6], q[7]) << 16);
+                    for (int j = 0; j < 8; ++j) q[j] = fmaf(x[j], by.hi, x[j] * by.lo);
+                    *reinterpret_cast<uint2 *>(at) =
+                        make_uint2(e4m3x2(q[0], q[1]) | e4m3x2(q[2], q[3]) << 16, e4m3x2(q[4], q[5]) | e4m3x2(q[6], q[7]) << 16);
+                }
             } else {
-                if (e0 < 0) continue;
-                store8<true>(at, x[i], 8);
+                if (e0 >= 0) store8<true>(at, x, 8);
             }
         } else {
-            if (!live[i]) continue;
-            if (e0 >= 0) {
-                if constexpr (k8) {
-                    const uint2 u = *reinterpret_cast<const uint2 *>(at);
-                    const float s = *scale;
-                    const uint32_t w[2] = {u.x, u.y};
+            if constexpr (k8) {
+                uint32_t h[4];
+                e4m3x4_to_f16(now.raw.x, h[0], h[1]);
+                e4m3x4_to_f16(now.raw.y, h[2], h[3]);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 f = e4m3x2_to_f32(w[j >> 1] >> 16 * (j & 1));
-                        x[i][2 * j] = f.x * s;
-                        x[i][2 * j + 1] = f.y * s;
-                    }
+                for (int j = 0; j < 4; ++j) {
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[j]));
+                    x[2 * j] = f.x * now.scale;
+                    x[2 * j + 1] = f.y * now.scale;
+                }
+            } else {
+                unpack(now.raw, x);
+            }
+            if (it.live) {
+                T *to = (T *)(it.is_v ? p.v_out : p.k_out) + ((long long)(r0 + it.row) * p.kv.kv_heads + it.head) * D + c;
+                if (kVec) {
+                    store8<true>(to, x, 8);
                 } else {
-                    Raw8<C> raw;
-                    load8<true>(raw, at, 8);
-                    unpack(raw, x[i]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) to[j] = from_f32<T>(x[j]);
                 }
             }
-            T *to = (T *)(is_v[i] ? p.v_out : p.k_out) + ((long long)(r0 + row[i]) * p.kv.kv_heads + head[i]) * D + c;
-            if (kVec) {
-                store8<true>(to, x[i], 8);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) to[j] = from_f32<T>(x[i][j]);
-            }
         }
+        now = next;
     }
 }
 
-template <typename T, typename C, int kLanes, bool kVec, bool kBack> cudaError_t launch_l(const CacheParams &p, cudaStream_t st)
+template <typename T, typename C, int kLanes, bool kVec, bool kBack> cudaError_t launch_l(CacheParams &p, cudaStream_t st)
 {
-    // one head a group until the grid fills the GPU (152 SMs of eight CTAs), then four
+    // rows of a CTA: as many as fill its groups once, or more, so that the CTAs
+    // of 152 SMs take all rows at once
     constexpr int kGroups = kThreads / kLanes;
-    const long long one = (p.items + kGroups - 1) / kGroups;
-    if (one <= 152 * 8) return launch_pdl(cache_kernel<T, C, kLanes, kVec, kBack, 1>, dim3((unsigned)one), dim3(kThreads), 0, st, p);
-    const long long four = (p.items + 4 * kGroups - 1) / (4 * kGroups);
-    if (four > 0x7fffffff) return cudaErrorInvalidValue;
-    return launch_pdl(cache_kernel<T, C, kLanes, kVec, kBack, 4>, dim3((unsigned)four), dim3(kThreads), 0, st, p);
+    const int all = 2 * p.kv.kv_heads;
+    p.heads = std::min(all, kGroups);
+    const int parts = (all + p.heads - 1) / p.heads;
+    const long long share = ((long long)p.T * parts + kCtas * 152 - 1) / (kCtas * 152);
+    p.rows = (int)std::min<long long>(std::max<long long>(kGroups / p.heads, share), kMaxRowsOfCta);
+    p.by_heads = FastDiv(p.heads);
+    return launch_pdl(cache_kernel<T, C, kLanes, kVec, kBack>, dim3((p.T + p.rows - 1) / p.rows, parts), dim3(kThreads), 0, st, p);
 }
-template <typename T, typename C, bool kBack> cudaError_t launch_tc(const CacheParams &p, bool vec, cudaStream_t st)
+template <typename T, typename C, bool kBack> cudaError_t launch_tc(CacheParams &p, bool vec, cudaStream_t st)
 {
     const int lanes = (p.kv.head_dim + 7) / 8;
     if (!vec) return launch_l<T, C, 32, false, kBack>(p, st);
@@ -172,7 +196,7 @@ template <typename T, typename C, bool kBack> cudaError_t launch_tc(const CacheP
     if (lanes <= 16) return launch_l<T, C, 16, true, kBack>(p, st);
     return launch_l<T, C, 32, true, kBack>(p, st);
 }
-template <bool kBack> cudaError_t launch_types(const CacheParams &p, int type, int cache_type, bool vec, cudaStream_t st)
+template <bool kBack> cudaError_t launch_types(CacheParams p, int type, int cache_type, bool vec, cudaStream_t st)
 {
     auto by_cache = [&](auto t) {
         using T = decltype(t);
@@ -189,7 +213,7 @@ template <bool kBack> cudaError_t launch_types(const CacheParams &p, int type, i
 
 cudaError_t launch_kv_append(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, const pmpe_kv_append_desc &d, cudaStream_t st)
 {
-    CacheParams p = {KvView(c, s), d.k, d.v, nullptr, nullptr, d.k_ld, d.k_head_ld, d.v_ld, d.v_head_ld, d.T, (long long)d.T * 2 * c.kv_heads};
+    const CacheParams p = {KvView(c, s), d.k, d.v, nullptr, nullptr, d.k_ld, d.k_head_ld, d.v_ld, d.v_head_ld, d.T, 0, 0, FastDiv(1)};
     const bool f32 = d.type == PMPE_F32;
     const bool vec = aligned8(d.k, f32) && aligned8(d.v, f32) && d.k_ld % 8 == 0 && d.v_ld % 8 == 0 && d.k_head_ld % 8 == 0 && d.v_head_ld % 8 == 0;
     return launch_types<false>(p, d.type, c.type, vec, st);
@@ -197,7 +221,7 @@ cudaError_t launch_kv_append(const pmpe_kv_cache &c, const pmpe_kv_sequences &s,
 
 cudaError_t launch_kv_read(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, int T, int type, void *k, void *v, cudaStream_t st)
 {
-    CacheParams p = {KvView(c, s), nullptr, nullptr, k, v, 0, 0, 0, 0, T, (long long)T * 2 * c.kv_heads};
+    const CacheParams p = {KvView(c, s), nullptr, nullptr, k, v, 0, 0, 0, 0, T, 0, 0, FastDiv(1)};
     const bool f32 = type == PMPE_F32;
     return launch_types<true>(p, type, c.type, aligned8(k, f32) && aligned8(v, f32), st);
 }
