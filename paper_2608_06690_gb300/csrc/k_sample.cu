@@ -16,17 +16,18 @@
 //   q = 2^-f - 1 a cubic, |f| <= 2^-9:     its FP32 rounding is 2^-33 of r
 //
 // A cluster of CTAs takes a row, each a run of ids.  One pass finds the largest
-// logit; every thread's largest, in a histogram over x, tells how far down the
-// best top_k (without it: 1024) tokens reach at most, since each thread that
-// shows one there holds one: k threads' tokens at most, nearly k where ids are
-// random.  The second pass lists those tokens (and sums r over all where top_p
-// needs that), and one CTA finishes with the list in shared memory.  Rows whose
-// list would be too long, or holds less than top_p, go through the whole row
-// again instead.  Rows without top_k and top_p take one pass of sums.
-//
-// The filters' border is found in histograms of counts and sums, first over x,
-// then over the bits of z where the border lies, down to one value of z; of
-// equal ones the lowest ids stay.
+// logit.
+//   top_k up to 1024: every thread's largest logit, in a histogram over x, tells
+//     how far down the best top_k tokens reach at most, since each thread that
+//     shows one there holds one: k threads' tokens at most, nearly k where ids
+//     are random.  A second pass lists those, and one CTA finishes with the list.
+//   top_p alone, or a larger top_k: a second pass makes histograms of counts and
+//     sums over x; the bin where the border lies is listed in a third, which also
+//     sums what is above it by runs of ids; the border is found in the list.
+//   neither: the second pass sums by runs of ids.
+// A list that does not fit (many tokens of about the same logit) is replaced by
+// further passes, over the bits of the logits in the border's bin, down to one
+// value.  Of equal logits at the border the lowest ids stay.
 #include <algorithm>
 
 #include <cooperative_groups.h>
@@ -43,12 +44,10 @@ constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
 constexpr int kSegs = 8 * kWarps;    // runs of ids whose sums a CTA keeps
 constexpr int kBins = 2048;          // of a histogram
-constexpr int kBinsX = kThreads;     // of one over x
-constexpr float kPerX = 12.f;        // its bins for a step of one in x
 constexpr float kLeast = 40.f;       // log2 of the smallest r, negated
 constexpr int kFine = 46;            // bits of r behind the point
 constexpr int kList = 2048;          // tokens of a list
-constexpr int kWanted = 1024;        // tokens that it should reach down to
+constexpr int kWanted = 1024;        // top_k up to which threads' largest logits show the border
 constexpr float kLog2eHi = 1.44269502f, kLog2eLo = 1.92596303e-8f;  // log2(e) in two words
 constexpr float kFltMax = 3.402823466e38f;
 
@@ -99,10 +98,12 @@ __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float
 struct Slope {
     float top, hi, lo, pre, post;
     int shift;
+    bool plain;    // pre = post = 1
+    float bins;    // of a histogram, for a step of one in x
 };
 __device__ __forceinline__ Slope slope_of(float top, float temperature, int shift)
 {
-    Slope s = {top, 0.f, 0.f, 1.f, 1.f, shift};
+    Slope s = {top, 0.f, 0.f, 1.f, 1.f, shift, true, 0.f};
     // a power of two keeps the quotient among FP32's normal numbers
     if (temperature > 0x1p90f) {
         s.pre = 0x1p-100f;
@@ -111,6 +112,7 @@ __device__ __forceinline__ Slope slope_of(float top, float temperature, int shif
         s.post = 0x1p100f;
         temperature *= 0x1p100f;
     }
+    s.plain = s.pre == 1.f && s.post == 1.f;
     s.hi = kLog2eHi / temperature;
     if (s.hi > 0.f) s.lo = (fmaf(-s.hi, temperature, kLog2eHi) + kLog2eLo) / temperature;
     return s;
@@ -150,33 +152,105 @@ __device__ __forceinline__ u64 weight_of(const Slope &s, float z, const Power *p
     n += s.shift - (kFine - 31);
     return n <= 0 ? (u64)w << -n : (u64)(w >> n);
 }
-// The smallest logit with x <= (hi, lo), by 32 tries at a time; the same in every lane.
-__device__ float lowest(const Slope &s, float hi, float lo)
+// The smallest logit for which `in` holds, as it does for the largest and does
+// not again further down, by 32 tries at a time; the same in every lane.
+template <typename F> __device__ float lowest(float top, F in)
 {
-    uint32_t below = key_of(-kFltMax) - 1, at = key_of(s.top);  // x is above at `below` (or that is no logit), within at `at`
+    uint32_t below = key_of(-kFltMax) - 1, at = key_of(top);  // not in at `below` (or that is no logit), in at `at`
     while (at - below > 1) {
         const uint32_t step = (at - below + 32) / 33, k = min(at, below + step * ((threadIdx.x & 31) + 1));
-        const Ratio x = x_of(s, logit_of(k));
-        const uint32_t in = __ballot_sync(~0u, (x.hi - hi) + (x.lo - lo) <= 0.f);  // (not of infinities)
-        const int first = in ? __ffs(in) - 1 : 32;
+        const uint32_t is = __ballot_sync(~0u, in(logit_of(k)));
+        const int first = is ? __ffs(is) - 1 : 32;
         const uint32_t from = below;
         if (first < 32) at = min(at, from + step * (first + 1));
         below = min(at - 1, from + step * first);
     }
     return logit_of(at);
 }
+// Whether r is at least min_p, 2^-40 < min_p < 1.
+__device__ __forceinline__ bool at_least(const Slope &s, float z, float min_p, const Power *powers)
+{
+    const Ratio x = x_of(s, z);
+    if (!(x.hi <= kLeast + 1.f)) return false;
+    int n;
+    const uint32_t w = power_of(x, powers, n), m = (__float_as_uint(min_p) & 0x7fffffu) | 0x800000u;
+    const int sh = 31 + n - (150 - (int)(__float_as_uint(min_p) >> 23));  // r >= min_p: w >= m 2^sh
+    return sh > 8 ? false : sh >= 0 ? w >= (uint64_t)m << sh : sh < -31 || (uint64_t)w << -sh >= m;
+}
+
+// Two values to an instruction.
+struct Two {
+    uint64_t v;
+    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ explicit Two(uint64_t w) : v(w) {}
+    __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return Two(r);
+}
+__device__ __forceinline__ Two add2(Two a, Two b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a.v), "l"(b.v));
+    return Two(r);
+}
+__device__ __forceinline__ Two mul2(Two a, Two b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a.v), "l"(b.v));
+    return Two(r);
+}
+// weight_of() of two logits, the same arithmetic; 0 where `in` is false.
+__device__ __forceinline__ void weights_of(const Slope &s, float z0, float z1, bool in0, bool in1, const Power *powers, u64 &w0, u64 &w1)
+{
+    if (!s.plain) {
+        w0 = in0 ? weight_of(s, z0, powers) : 0;
+        w1 = in1 ? weight_of(s, z1, powers) : 0;
+        return;
+    }
+    const Two minus(-1.f, -1.f), a(s.top, s.top), z(z0, z1), c(s.hi, s.hi);
+    const Two d = fma2(z, minus, a), bb = fma2(d, minus, a);
+    const Two e = add2(fma2(add2(d, bb), minus, a), fma2(z, minus, bb));
+    const Two hi = mul2(d, c), lo = fma2(d, c, mul2(hi, minus)), lo2 = add2(lo, fma2(d, Two(s.lo, s.lo), mul2(e, c)));
+    const Two kf = fma2(hi, Two(256.f, 256.f), Two(12582912.f, 12582912.f));
+    const Two f = add2(fma2(add2(kf, Two(-12582912.f, -12582912.f)), Two(-1.f / 256.f, -1.f / 256.f), hi), lo2);
+    const Two q = mul2(f, fma2(f, fma2(f, Two(-0.055504109f, -0.055504109f), Two(0.240226507f, 0.240226507f)), Two(-0.693147181f, -0.693147181f)));
+    float k[2], qs[2];
+    kf.get(k[0], k[1]);
+    q.get(qs[0], qs[1]);
+    u64 w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int bits = __float_as_int(k[i]);
+        const Power p = powers[bits & 255];
+        const uint32_t v = p.fixed + __float2int_rn(p.value * qs[i]);
+        const bool in = i ? in1 : in0;
+        const int down = in ? (bits >> 8) - (0x4b400000 >> 8) + s.shift - (kFine - 31) : 0;  // v 2^-down
+        w[i] = (u64)(v >> max(down, 0)) * (in ? 1u << max(-down, 0) : 0u);
+    }
+    w0 = w[0];
+    w1 = w[1];
+}
 
 struct Shared {
     Power powers[256];
     uint32_t mass_lo[kBins], mass_hi[kBins], count[kBins];
-    u64 mass_x[kBinsX];      // merged: of the histogram over x
-    uint32_t count_x[kBinsX];
+    u64 mass_x[kBins];       // merged: of the histogram over x
+    uint32_t count_x[kBins];
     float list_z[kList];
     int list_id[kList];
     u64 list_w[kList];
     u64 seg[kSegs], warp_mass[kWarps], total[3][kMaxCluster], found_mass;
     uint32_t warp_count[kWarps], found_count, found_bin, range_lo, range_hi, listed;
     int id;
+    // what the first CTA found in a list: the border, and the sum up to it
+    float logit;
+    int last;
+    u64 upto;
+    float floors[2];
 };
 
 template <typename T> constexpr int kChunk = 16 / sizeof(T);  // logits of a load
@@ -188,46 +262,52 @@ template <typename T> struct Sampler {
     const T *z;
     bool vec;                 // whole loads: rows are aligned for them
     Slope slope;
-    float floor;              // the lowest logit that the sums take
+    float floor;              // the lowest logit that sums and counts take
     int rank, ranks, lo, hi;  // this CTA's ids (runs begin at whole loads)
     int listed;               // tokens in the list
 
-    // f(z, id) of this CTA's logits from `begin` to `end`, `step` loads apart; NaN where there are none.
-    template <typename F> __device__ __forceinline__ void each(int begin, int end, int step, F f) const
+    // f(values, id of the first) of kChunk logits a load, `step` loads apart; NaN where there are none.
+    template <typename F> __device__ __forceinline__ void loads(int begin, int end, int step, F f) const
     {
-        for (int i = begin; i < end; i += step * kChunk<T>) load(i, end, f);
-    }
-    template <typename F> __device__ __forceinline__ void load(int i, int end, F f) const
-    {
-        if (vec && i + kChunk<T> <= end) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(z + i));
-            if constexpr (sizeof(T) == 4) {
-                f(__uint_as_float(u.x), i);
-                f(__uint_as_float(u.y), i + 1);
-                f(__uint_as_float(u.z), i + 2);
-                f(__uint_as_float(u.w), i + 3);
+#pragma unroll 2
+        for (int i = begin; i < end; i += step * kChunk<T>) {
+            float v[kChunk<T>];
+            if (vec && i + kChunk<T> <= end) {
+                const uint4 u = __ldg(reinterpret_cast<const uint4 *>(z + i));
+                if constexpr (sizeof(T) == 4) {
+                    v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
+                } else {
+                    unpack8(u, v, T());
+                }
             } else {
-                float v[8];
-                unpack8(u, v, T());
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f(v[j], i + j);
+                for (int j = 0; j < kChunk<T>; ++j) v[j] = i + j < end ? to_f32<T>(z[i + j]) : NAN;
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < kChunk<T>; ++j)
-                if (i + j < end) f(to_f32<T>(z[i + j]), i + j);
+            f(v, i);
         }
     }
-    // f(z, id, w) of what the sums take: of the list, or of the row.
+    template <typename F> __device__ __forceinline__ void each(F f) const  // f(z, id) of this CTA's
+    {
+        loads(lo + threadIdx.x * kChunk<T>, hi, kThreads, [&](const float (&v)[kChunk<T>], int i) {
+#pragma unroll
+            for (int j = 0; j < kChunk<T>; ++j) f(v[j], i + j);
+        });
+    }
+    // f(z, id, w) of what the sums take: of the list, or of this CTA's part of the row.
     template <bool kOfList, typename F> __device__ __forceinline__ void each_weight(F f) const
     {
         if constexpr (kOfList) {
             for (int i = threadIdx.x; i < listed; i += kThreads) f(s.list_z[i], s.list_id[i], s.list_w[i]);
         } else {
-            each(lo + threadIdx.x * kChunk<T>, hi, kThreads, [&](float v, int i) {
-                if (v >= floor) {
-                    v = fminf(v, kFltMax);
-                    f(v, i, weight_of(slope, v, s.powers));
+            loads(lo + threadIdx.x * kChunk<T>, hi, kThreads, [&](const float (&v)[kChunk<T>], int i) {
+#pragma unroll
+                for (int j = 0; j < kChunk<T>; j += 2) {
+                    const float a = fminf(v[j], kFltMax), b = fminf(v[j + 1], kFltMax);  // (NaN becomes the largest: told apart by v)
+                    const bool in0 = v[j] >= floor, in1 = v[j + 1] >= floor;
+                    u64 w0, w1;
+                    weights_of(slope, a, b, in0, in1, s.powers, w0, w1);
+                    if (in0) f(a, i + j, w0);
+                    if (in1) f(b, i + j + 1, w1);
                 }
             });
         }
@@ -242,27 +322,34 @@ template <typename T> struct Sampler {
         for (int b = threadIdx.x; b < kBins; b += kThreads) s.mass_lo[b] = 0, s.mass_hi[b] = 0, s.count[b] = 0;
         __syncthreads();
     }
-    __device__ __forceinline__ void add(int bin, u64 w) const
+    __device__ __forceinline__ void add_mass(int bin, u64 w) const
     {
-        atomicAdd(&s.count[bin], 1u);
         const uint32_t low = (uint32_t)w, old = atomicAdd(&s.mass_lo[bin], low), high = (uint32_t)(w >> 32) + (old > ~low);
         if (high) atomicAdd(&s.mass_hi[bin], high);
     }
-    // The histogram of all CTAs in place of each one's, kN bins.
-    template <bool kOfList, int kN> __device__ void merge() const
+    __device__ __forceinline__ void add(int bin, u64 w) const
+    {
+        atomicAdd(&s.count[bin], 1u);
+        add_mass(bin, w);
+    }
+    __device__ __forceinline__ u64 mass_at(int b) const { return ((u64)s.mass_hi[b] << 32) + s.mass_lo[b]; }
+    // The histogram of all CTAs in place of each one's.
+    template <bool kOfList> __device__ void merge() const
     {
         meet<kOfList>();
         if (kOfList || ranks == 1) return;
-        constexpr int kPer = kN / kThreads;
+        constexpr int kPer = kBins / kThreads;
         u64 m[kPer];
         uint32_t c[kPer];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const int b = threadIdx.x + j * kThreads;
-            m[j] = 0, c[j] = 0;
-            for (int r = 0; r < ranks; ++r) {
-                m[j] += ((u64)cluster.map_shared_rank(s.mass_hi, r)[b] << 32) + cluster.map_shared_rank(s.mass_lo, r)[b];
-                c[j] += cluster.map_shared_rank(s.count, r)[b];
+        for (int j = 0; j < kPer; ++j) m[j] = 0, c[j] = 0;
+        for (int r = 0; r < ranks; ++r) {
+            const uint32_t *hi32 = cluster.map_shared_rank(s.mass_hi, r), *lo32 = cluster.map_shared_rank(s.mass_lo, r), *n = cluster.map_shared_rank(s.count, r);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const int b = threadIdx.x + j * kThreads;
+                m[j] += ((u64)hi32[b] << 32) + lo32[b];
+                c[j] += n[b];
             }
         }
         cluster.sync();
@@ -274,19 +361,19 @@ template <typename T> struct Sampler {
         __syncthreads();
     }
 
-    // In kN bins with mass(b) and count(b), the first whose running count (or
+    // In kBins bins with mass(b) and count(b), the first whose running count (or
     // mass) reaches `want`: its number, and what comes before it.  false: none.
-    template <int kN, typename M, typename C>
-    __device__ bool crossing(M mass_at, C count_at, bool by_mass, u64 want, uint32_t &bin, u64 &before_mass, uint32_t &before_count) const
+    template <typename M, typename C>
+    __device__ bool crossing(M mass_of, C count_of, bool by_mass, u64 want, uint32_t &bin, u64 &before_mass, uint32_t &before_count) const
     {
-        constexpr int kPer = kN / kThreads;
+        constexpr int kPer = kBins / kThreads;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         u64 m[kPer], mass = 0;
         uint32_t c[kPer], count = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            m[j] = mass_at(threadIdx.x * kPer + j);
-            c[j] = count_at(threadIdx.x * kPer + j);
+            m[j] = mass_of(threadIdx.x * kPer + j);
+            c[j] = count_of(threadIdx.x * kPer + j);
             mass += m[j], count += c[j];
         }
         u64 im = mass;
@@ -323,41 +410,48 @@ template <typename T> struct Sampler {
         __syncthreads();
         return bin != ~0u;
     }
-    __device__ __forceinline__ int bin_of(float v) const { return (int)(x_near(slope, v) * kPerX); }
+    // The bin of a histogram over x; the same number as it is compared with.
+    __device__ __forceinline__ float place_of(float v) const { return x_near(slope, v) * slope.bins; }
 
-    // The histogram over x, into mass_x and count_x; the sum of all.
-    template <bool kOfList> __device__ u64 over_x() const
+    // The histogram over x, into mass_x and count_x (counts only where they are wanted); the sum of all.
+    __device__ u64 over_x(bool counts) const
     {
         clear();
-        each_weight<kOfList>([&](float v, int, u64 w) { add(bin_of(v), w); });
-        merge<kOfList, kBinsX>();
-        u64 sum = ((u64)s.mass_hi[threadIdx.x] << 32) + s.mass_lo[threadIdx.x];
-        s.mass_x[threadIdx.x] = sum;
-        s.count_x[threadIdx.x] = s.count[threadIdx.x];
-        sum = warp_sum(sum);
-        if ((threadIdx.x & 31) == 0) s.warp_mass[threadIdx.x >> 5] = sum;
-        __syncthreads();
-        sum = 0;
-        for (int w = 0; w < kWarps; ++w) sum += s.warp_mass[w];
-        __syncthreads();
-        return sum;
+        each_weight<false>([&](float v, int, u64 w) {
+            const int b = (int)place_of(v);
+            if (counts) atomicAdd(&s.count[b], 1u);
+            add_mass(b, w);
+        });
+        merge<false>();
+        u64 sum = 0;
+        for (int b = threadIdx.x; b < kBins; b += kThreads) {
+            sum += s.mass_x[b] = mass_at(b);
+            s.count_x[b] = s.count[b];
+        }
+        return cta_sum(sum);
+    }
+    __device__ __forceinline__ bool crossing_x(bool by_mass, u64 want, uint32_t &bin, u64 &mass, uint32_t &count) const
+    {
+        return crossing([&](int b) { return s.mass_x[b]; }, [&](int b) { return s.count_x[b]; }, by_mass, want, bin, mass, count);
     }
 
-    // The logit at which the running count (or sum) reaches `want`, by the
-    // histogram over x: how many of that logit are wanted, and the sum up to
-    // them.  false: there is less than that.
-    template <bool kOfList> __device__ bool border(bool by_mass, u64 want, float &logit, u64 &ties, u64 &upto) const
+    // The logit at which the running count (or sum) reaches `want`, after what
+    // comes before (mass, count), among those of bin `bin` over x (of a list:
+    // among all): how many of that logit are wanted, and the sum up to them.
+    template <bool kOfList> __device__ void border(bool by_mass, u64 want, uint32_t bin, u64 mass, uint32_t count, float &logit, u64 &ties, u64 &upto) const
     {
-        uint32_t bin, count;
-        u64 mass;
-        if (!crossing<kBinsX>([&](int b) { return s.mass_x[b]; }, [&](int b) { return s.count_x[b]; }, by_mass, want, bin, mass, count)) return false;
-        // that bin's logits, from the largest on
+        // the logits' range
         if (threadIdx.x == 0) s.range_lo = ~0u, s.range_hi = 0;
         __syncthreads();
         uint32_t klo = ~0u, khi = 0;
-        each_weight<kOfList>([&](float v, int, u64) {
-            if ((uint32_t)bin_of(v) == bin) klo = min(klo, key_of(v)), khi = max(khi, key_of(v));
-        });
+        auto take = [&](float v) { klo = min(klo, key_of(v)), khi = max(khi, key_of(v)); };
+        if constexpr (kOfList) {
+            each_weight<true>([&](float v, int, u64) { take(v); });
+        } else {
+            each([&](float v, int) {
+                if (v >= floor && (uint32_t)place_of(fminf(v, kFltMax)) == bin) take(fminf(v, kFltMax));
+            });
+        }
         klo = __reduce_min_sync(~0u, klo);
         khi = __reduce_max_sync(~0u, khi);
         if ((threadIdx.x & 31) == 0) atomicMin(&s.range_lo, klo), atomicMax(&s.range_hi, khi);
@@ -372,120 +466,143 @@ template <typename T> struct Sampler {
         while (width > 0) {
             const int sh = max(0, 21 - __clz(width));  // width >> sh < kBins
             clear();
-            each_weight<kOfList>([&](float v, int, u64 w) {
+            auto bin_it = [&](float v, u64 w) {
                 const uint32_t k = key_of(v);
                 if (k <= khi && khi - k <= width) add((khi - k) >> sh, w);
-            });
-            merge<kOfList, kBins>();
+            };
+            if constexpr (kOfList) {
+                each_weight<true>([&](float v, int, u64 w) { bin_it(v, w); });
+            } else {
+                const float least = logit_of(khi - width), most = logit_of(khi);
+                each([&](float v, int) {
+                    v = v >= floor ? fminf(v, kFltMax) : NAN;
+                    if (v >= least && v <= most) bin_it(v, weight_of(slope, v, s.powers));
+                });
+            }
+            merge<kOfList>();
             u64 bm;
             uint32_t bc, b;
-            crossing<kBins>([&](int i) { return ((u64)s.mass_hi[i] << 32) + s.mass_lo[i]; }, [&](int i) { return s.count[i]; }, by_mass,
-                            want - (by_mass ? mass : count), b, bm, bc);
+            crossing([&](int i) { return mass_at(i); }, [&](int i) { return s.count[i]; }, by_mass, want - (by_mass ? mass : count), b, bm, bc);
             mass += bm;
             count += bc;
             khi -= b << sh;
             width = min(width - (b << sh), (1u << sh) - 1);
         }
-        if (!kOfList) cluster.sync();  // before another search sets the range
+        meet<kOfList>();  // before another search sets the range
         logit = logit_of(khi);
         const u64 w = weight_of(slope, logit, s.powers);
         ties = by_mass ? (want - mass + w - 1) / w : want - count;
         upto = mass + ties * w;
-        return true;
     }
 
-    // The first id whose running sum of f(z, id, w) is above target(sum of
-    // all); -1 for none.  The same in every CTA.
-    template <bool kOfList, typename F, typename G> __device__ int locate(F f, G target, u64 &all) const
+    // The id in the list at which the running sum of f(z, id, w), by id, passes `want`.
+    template <typename F> __device__ int locate_in_list(F f, u64 want) const
     {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        if constexpr (kOfList) {
-            u64 sum = 0;
-            each_weight<true>([&](float v, int i, u64 w) { sum += f(v, i, w); });
-            sum = warp_sum(sum);
-            if (lane == 0) s.warp_mass[warp] = sum;
-            __syncthreads();
-            all = 0;
-            for (int w = 0; w < kWarps; ++w) all += s.warp_mass[w];
-            u64 want = target(all) + 1, bm;
-            uint32_t high, low, bc;
-            clear();
-            each_weight<true>([&](float v, int i, u64 w) {
-                w = f(v, i, w);
-                if (w) add(i >> 10, w);
-            });
-            __syncthreads();
-            auto mass_at = [&](int i) { return ((u64)s.mass_hi[i] << 32) + s.mass_lo[i]; };
-            auto count_at = [&](int i) { return s.count[i]; };
-            if (!crossing<kBins>(mass_at, count_at, true, want, high, bm, bc)) return -1;
-            want -= bm;
-            clear();
-            each_weight<true>([&](float v, int i, u64 w) {
-                w = (uint32_t)(i >> 10) == high ? f(v, i, w) : 0;
-                if (w) add(i & 1023, w);
-            });
-            __syncthreads();
-            crossing<kBins>(mass_at, count_at, true, want, low, bm, bc);
-            return (int)(high << 10 | low);
-        } else {
-            auto taken = [&](float v, int i) {
-                if (!(v >= floor)) return 0ull;
-                v = fminf(v, kFltMax);
-                return f(v, i, weight_of(slope, v, s.powers));
-            };
-            constexpr int kStep = 32 * kChunk<T>;
-            const int seg = ((hi - lo + kSegs - 1) / kSegs + kStep - 1) / kStep * kStep;
-            for (int g = warp; g < kSegs; g += kWarps) {
-                u64 sum = 0;
-                each(lo + g * seg + lane * kChunk<T>, min(hi, lo + (g + 1) * seg), 32, [&](float v, int i) { sum += taken(v, i); });
-                sum = warp_sum(sum);
-                if (lane == 0) s.seg[g] = sum;
-            }
-            if (threadIdx.x == 0) s.id = -1;
-            __syncthreads();
-            if (warp == 0) {
-                u64 sum = 0;
-                for (int g = lane; g < kSegs; g += 32) sum += s.seg[g];
-                sum = warp_sum(sum);
-                if (lane < ranks) cluster.map_shared_rank(s.total[0], lane)[rank] = sum;
-            }
-            cluster.sync();
-            u64 before = 0;
-            all = 0;
-            for (int r = 0; r < ranks; ++r) {
-                if (r < rank) before += s.total[0][r];
-                all += s.total[0][r];
-            }
-            const u64 want = target(all);
-            if (warp == 0 && all > 0 && before <= want && want < before + s.total[0][rank]) {
-                int g = 0;
-                while (before + s.seg[g] <= want) before += s.seg[g++];
-                for (int i = lo + g * seg + lane;; i += 32) {
-                    u64 sum = i < hi ? taken(to_f32<T>(z[i]), i) : 0;
-                    for (int off = 1; off < 32; off <<= 1) {
-                        const u64 o = __shfl_up_sync(~0u, sum, off);
-                        if (lane >= off) sum += o;
-                    }
-                    const uint32_t past = __ballot_sync(~0u, before + sum > want);
-                    if (past) {
-                        if (lane < ranks) *cluster.map_shared_rank(&s.id, lane) = i - lane + __ffs(past) - 1;
-                        break;
-                    }
-                    before += __shfl_sync(~0u, sum, 31);
-                }
-            }
-            cluster.sync();
-            const int id = s.id;
-            __syncthreads();  // before the next search resets it
-            return id;
-        }
+        u64 bm;
+        uint32_t high, low, bc;
+        auto mass = [&](int i) { return mass_at(i); };
+        auto count = [&](int) { return 0u; };
+        clear();
+        each_weight<true>([&](float v, int i, u64 w) {
+            w = f(v, i, w);
+            if (w) add_mass(i >> 10, w);
+        });
+        __syncthreads();
+        ++want;
+        if (!crossing(mass, count, true, want, high, bm, bc)) return -1;
+        want -= bm;
+        clear();
+        each_weight<true>([&](float v, int i, u64 w) {
+            w = (uint32_t)(i >> 10) == high ? f(v, i, w) : 0;
+            if (w) add_mass(i & 1023, w);
+        });
+        __syncthreads();
+        crossing(mass, count, true, want, low, bm, bc);
+        return (int)(high << 10 | low);
     }
-    // Values of the CTAs (one each, from thread 0's point of view) to all of them.
+
+    // Runs of ids: a warp's, kSegs of a CTA, of whole loads.
+    __device__ __forceinline__ int run_length() const
+    {
+        constexpr int kStep = 32 * kChunk<T>;
+        return ((hi - lo + kSegs - 1) / kSegs + kStep - 1) / kStep * kStep;
+    }
+    // Their sums of f(z, w, id), into s.seg.
+    template <typename F> __device__ __forceinline__ void sum_runs(F f) const
+    {
+        const int lane = threadIdx.x & 31, seg = run_length();
+        for (int g = threadIdx.x >> 5; g < kSegs; g += kWarps) {
+            u64 sum = 0;
+            loads(lo + g * seg + lane * kChunk<T>, min(hi, lo + (g + 1) * seg), 32, [&](const float (&v)[kChunk<T>], int i) { sum += f(v, i); });
+            sum = warp_sum(sum);
+            if (lane == 0) s.seg[g] = sum;
+        }
+        __syncthreads();
+    }
+    // The first id whose running sum is above target(sum of all), with the runs'
+    // sums in s.seg and one(z, id) of single tokens; -1 for none.  The same in
+    // every CTA.
+    template <typename F, typename G> __device__ int locate(F one, G target, u64 &all) const
+    {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seg = run_length();
+        if (threadIdx.x == 0) s.id = -1;
+        if (warp == 0) {
+            u64 sum = 0;
+            for (int g = lane; g < kSegs; g += 32) sum += s.seg[g];
+            sum = warp_sum(sum);
+            if (lane < ranks) cluster.map_shared_rank(s.total[0], lane)[rank] = sum;
+        }
+        cluster.sync();
+        u64 before = 0;
+        all = 0;
+        for (int r = 0; r < ranks; ++r) {
+            if (r < rank) before += s.total[0][r];
+            all += s.total[0][r];
+        }
+        const u64 want = target(all);
+        if (warp == 0 && all > 0 && before <= want && want < before + s.total[0][rank]) {
+            // 32 runs at a time, then 32 tokens
+            int g = 0;
+            for (;; g += 32) {
+                u64 sum = g + lane < kSegs ? s.seg[g + lane] : 0;
+                for (int off = 1; off < 32; off <<= 1) {
+                    const u64 o = __shfl_up_sync(~0u, sum, off);
+                    if (lane >= off) sum += o;
+                }
+                const uint32_t past = __ballot_sync(~0u, before + sum > want);
+                if (past) {
+                    const int first = __ffs(past) - 1;
+                    if (first > 0) before += __shfl_sync(~0u, sum, first - 1);
+                    g += first;
+                    break;
+                }
+                before += __shfl_sync(~0u, sum, 31);
+            }
+            for (int i = lo + g * seg + lane;; i += 32) {
+                u64 sum = i < hi ? one(to_f32<T>(z[i]), i) : 0;
+                for (int off = 1; off < 32; off <<= 1) {
+                    const u64 o = __shfl_up_sync(~0u, sum, off);
+                    if (lane >= off) sum += o;
+                }
+                const uint32_t past = __ballot_sync(~0u, before + sum > want);
+                if (past) {
+                    if (lane < ranks) *cluster.map_shared_rank(&s.id, lane) = i - lane + __ffs(past) - 1;
+                    break;
+                }
+                before += __shfl_sync(~0u, sum, 31);
+            }
+        }
+        cluster.sync();
+        const int id = s.id;
+        __syncthreads();  // before the next search resets it
+        return id;
+    }
+    // A value of each CTA to all of them, in total[slot].
     __device__ __forceinline__ void share(int slot, u64 v) const
     {
         if ((int)threadIdx.x < ranks) cluster.map_shared_rank(s.total[slot], threadIdx.x)[rank] = v;
     }
-    // A warp's values' sum over the CTA, in every thread.
+    // The sum over the CTA's threads, in every one.
     __device__ __forceinline__ u64 cta_sum(u64 v) const
     {
         v = warp_sum(v);
@@ -496,39 +613,41 @@ template <typename T> struct Sampler {
         __syncthreads();
         return v;
     }
-
-    // The filters' border and the draw.
-    template <bool kOfList> __device__ void finish(int t, int top_k, float top_p, float min_p, float u)
+    // The lists of all CTAs (their lengths in total[2]) in the first one's, if
+    // they fit; in all CTAs whether they do.  The others' parts stay theirs.
+    __device__ bool gather()
     {
-        float logit = -INFINITY;  // kept: above it, and of those equal to it up to id `last`
-        u64 ties = ~0ull, all;
-        int last = 0x7fffffff;
-        if (top_k > 0 || !(top_p >= 1.f)) {
-            u64 sum = over_x<kOfList>(), upto;
-            if (top_k > 0) {
-                if (border<kOfList>(false, (u64)top_k, logit, ties, upto)) sum = upto;
-            } else if (kOfList) {  // the list is not all
-                sum = 0;
-                for (int r = 0; r < ranks; ++r) sum += s.total[1][r];
+        int n = 0;
+        for (int r = 0; r < ranks; ++r) n += (int)min(s.total[2][r], (u64)kList + 1);
+        if (n > kList) return false;
+        if (rank == 0) {
+            const int own = (int)s.total[2][0];
+            for (int i = threadIdx.x + own; i < n; i += kThreads) {
+                int r = 0, at = i;
+                while (at >= (int)s.total[2][r]) at -= (int)s.total[2][r++];
+                s.list_z[i] = cluster.map_shared_rank(s.list_z, r)[at];
+                s.list_id[i] = cluster.map_shared_rank(s.list_id, r)[at];
+                s.list_w[i] = cluster.map_shared_rank(s.list_w, r)[at];
             }
-            if (!(top_p >= 1.f)) border<kOfList>(true, max(share_of(sum, top_p, true), 1ull), logit, ties, upto);
+            listed = n;
+        } else {
+            listed = (int)s.total[2][rank];
         }
-        // of equal logits at the border the lowest ids stay
-        if (ties != ~0ull)
-            last = locate<kOfList>([&](float v, int, u64) { return (u64)(v == logit); }, [&](u64) { return ties - 1; }, all);
-        if (min_p > 0.f) {
-            const double lim = -log2((double)min_p);
-            if (lim < kLeast) floor = lowest(slope, (float)lim, (float)(lim - (float)lim));
-        }
-        const float least = floor;
-        const int id = locate<kOfList>([&](float v, int i, u64 w) { return v >= least && (v > logit || (v == logit && i <= last)) ? w : 0ull; },
-                                       [&](u64 sum) { return share_of(sum, u, false); }, all);
-        if (rank == 0 && threadIdx.x == 0) {
-            p.token[t] = id;
-            int n;  // (r itself: of small ones the sums take few bits)
-            const uint32_t w = power_of(x_of(slope, fminf(to_f32<T>(z[id]), kFltMax)), s.powers, n);
-            p.prob[t] = (float)w * __int_as_float((127 - n) << 23) * (float)(1 << (kFine - 31)) / ((float)all * (float)(1 << slope.shift));
-        }
+        __syncthreads();
+        return true;
+    }
+    __device__ __forceinline__ void list(float v, int i, u64 w) const
+    {
+        const uint32_t at = atomicAdd(&s.listed, 1u);
+        if (at < kList) s.list_z[at] = v, s.list_id[at] = i, s.list_w[at] = w;
+    }
+
+    __device__ void answer(int t, int id, u64 all) const
+    {
+        p.token[t] = id;
+        int n;  // (r itself: of small ones the sums take few bits)
+        const uint32_t w = power_of(x_of(slope, fminf(to_f32<T>(z[id]), kFltMax)), s.powers, n);
+        p.prob[t] = (float)w * __int_as_float((127 - n) << 23) * (float)(1 << (kFine - 31)) / ((float)all * (float)(1 << slope.shift));
     }
     // floor(sum f) for 0 <= f < 1 (above: as the largest such), or its ceiling.
     static __device__ __forceinline__ u64 share_of(u64 sum, float f, bool up)
@@ -544,6 +663,119 @@ template <typename T> struct Sampler {
         if (down >= 128) return up && v ? 1 : 0;
         const unsigned __int128 q = v >> down;
         return (u64)q + (up && (q << down) != v);
+    }
+
+    // A row whose best top_k are in the list: the first CTA by itself.
+    __device__ void from_list(int t, int top_k, float top_p, float least, float u)
+    {
+        u64 sum = 0, ties = ~0ull, upto;
+        float logit = -INFINITY;
+        int last = 0x7fffffff;
+        each_weight<true>([&](float, int, u64 w) { sum += w; });
+        sum = cta_sum(sum);
+        if (listed > top_k) {
+            border<true>(false, (u64)top_k, 0, 0, 0, logit, ties, upto);
+            sum = upto;
+        }
+        if (!(top_p >= 1.f)) border<true>(true, max(share_of(sum, top_p, true), 1ull), 0, 0, 0, logit, ties, upto);
+        if (ties != ~0ull) last = locate_in_list([&](float v, int, u64) { return (u64)(v == logit); }, ties - 1);
+        auto kept = [&](float v, int i, u64 w) { return v >= least && (v > logit || (v == logit && i <= last)) ? w : 0ull; };
+        sum = 0;
+        each_weight<true>([&](float v, int i, u64 w) { sum += kept(v, i, w); });
+        sum = cta_sum(sum);
+        const int id = locate_in_list(kept, share_of(sum, u, false));
+        if (threadIdx.x == 0) answer(t, id, sum);
+    }
+
+    // Any other row, by all CTAs.
+    __device__ void from_row(int t, int top_k, float top_p, float least, float u)
+    {
+        const bool by_sum = !(top_p >= 1.f);
+        float logit = -INFINITY;  // kept: above it, and of those equal to it up to id `last`
+        int last = 0x7fffffff;
+        bool summed = false;      // s.seg holds the kept ones' sums
+        if (top_k > 0 || by_sum) {
+            u64 sum = over_x(top_k > 0);
+            for (int turn = 0; turn < 2; ++turn) {  // top_k's border, then top_p's
+                if (turn == 0 ? top_k <= 0 : !by_sum) continue;
+                const u64 want = turn == 0 ? (u64)top_k : max(share_of(sum, top_p, true), 1ull);
+                uint32_t bin, count;
+                u64 mass, ties, upto;
+                if (!crossing_x(turn == 1, want, bin, mass, count)) continue;
+                // that bin's tokens into the list; the sums of what lies above it
+                if (threadIdx.x == 0) s.listed = 0;
+                __syncthreads();
+                const float from = (float)bin, to = (float)(bin + 1);
+                sum_runs([&](const float (&v)[kChunk<T>], int i) {
+                    u64 run = 0;
+#pragma unroll
+                    for (int j = 0; j < kChunk<T>; j += 2) {
+                        const float a = fminf(v[j], kFltMax), b = fminf(v[j + 1], kFltMax), x0 = place_of(a), x1 = place_of(b);
+                        const bool in0 = v[j] >= floor && x0 < to, in1 = v[j + 1] >= floor && x1 < to;
+                        if (!(in0 || in1)) continue;
+                        u64 w0, w1;
+                        weights_of(slope, a, b, in0, in1, s.powers, w0, w1);
+                        if (in0 && x0 >= from) list(a, i + j, w0), w0 = 0;
+                        if (in1 && x1 >= from) list(b, i + j + 1, w1), w1 = 0;
+                        run += (a >= least ? w0 : 0) + (b >= least ? w1 : 0);
+                    }
+                    return run;
+                });
+                share(2, s.listed);
+                cluster.sync();
+                summed = gather();
+                if (summed) {
+                    if (rank == 0) {
+                        border<true>(turn == 1, want, 0, mass, count, logit, ties, upto);
+                        last = locate_in_list([&](float v, int, u64) { return (u64)(v == logit); }, ties - 1);
+                        if ((int)threadIdx.x < ranks) {
+                            Shared *o = cluster.map_shared_rank(&s, threadIdx.x);
+                            o->logit = logit, o->last = last, o->upto = upto;
+                        }
+                        listed = (int)s.total[2][0];
+                    }
+                    cluster.sync();
+                    logit = s.logit, last = s.last, sum = s.upto;
+                } else {
+                    cluster.sync();  // the lengths have been read
+                    border<false>(turn == 1, want, bin, mass, count, logit, ties, upto);
+                    sum_runs([&](const float (&v)[kChunk<T>], int) {
+                        u64 n = 0;
+#pragma unroll
+                        for (int j = 0; j < kChunk<T>; ++j) n += fminf(v[j], kFltMax) == logit && v[j] == v[j];
+                        return n;
+                    });
+                    u64 all;
+                    last = locate([&](float v, int) { return (u64)(fminf(v, kFltMax) == logit && v == v); }, [&](u64) { return ties - 1; }, all);
+                    sum = upto;
+                }
+            }
+        }
+        auto kept = [&](float v, int i) { return v >= floor && v >= least && (v > logit || (v == logit && i <= last)); };
+        if (summed) {  // the border's bin, from this CTA's list
+            const int seg = run_length();
+            for (int i = threadIdx.x; i < listed; i += kThreads)
+                if (kept(s.list_z[i], s.list_id[i])) atomicAdd(&s.seg[(s.list_id[i] - lo) / seg], s.list_w[i]);
+            __syncthreads();
+        } else {
+            sum_runs([&](const float (&v)[kChunk<T>], int i) {
+                u64 run = 0;
+#pragma unroll
+                for (int j = 0; j < kChunk<T>; j += 2) {
+                    const float a = fminf(v[j], kFltMax), b = fminf(v[j + 1], kFltMax);
+                    u64 w0, w1;
+                    weights_of(slope, a, b, v[j] == v[j] && kept(a, i + j), v[j + 1] == v[j + 1] && kept(b, i + j + 1), s.powers, w0, w1);
+                    run += w0 + w1;
+                }
+                return run;
+            });
+        }
+        u64 all;
+        const int id = locate([&](float v, int i) {
+            const float a = fminf(v, kFltMax);
+            return v == v && kept(a, i) ? weight_of(slope, a, s.powers) : 0ull;
+        }, [&](u64 sum) { return share_of(sum, u, false); }, all);
+        if (rank == 0 && threadIdx.x == 0) answer(t, id, all);
     }
 };
 
@@ -561,31 +793,38 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
     Sampler<T> m = {p, s, cluster, row, ((uintptr_t)row & 15u) == 0, Slope(), -INFINITY, rank, ranks, min(p.V, rank * slice), min(p.V, (rank + 1) * slice), 0};
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 
-    // ---- the largest logit
-    float mine = -INFINITY;  // of this thread (NaN is passed over)
-    m.each(m.lo + threadIdx.x * kChunk<T>, m.hi, kThreads, [&](float v, int) { mine = fmaxf(mine, v); });
+    // ---- the largest logit, and the smallest
+    float mine = -INFINITY, least_of = INFINITY;  // of this thread (NaN is passed over)
+    m.each([&](float v, int) {
+        mine = fmaxf(mine, v);
+        least_of = fminf(least_of, v);
+    });
     mine = fminf(mine, kFltMax);
     float top = mine;
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, off));
-    if (lane == 0) s.warp_mass[warp] = (u64)__float_as_uint(top);
+    for (int off = 16; off > 0; off >>= 1) {
+        top = fmaxf(top, __shfl_xor_sync(~0u, top, off));
+        least_of = fminf(least_of, __shfl_xor_sync(~0u, least_of, off));
+    }
+    if (lane == 0) s.warp_mass[warp] = (u64)__float_as_uint(top) << 32 | __float_as_uint(least_of);
     __syncthreads();
-    top = __uint_as_float((uint32_t)s.warp_mass[lane < kWarps ? lane : 0]);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, off));
-    m.share(2, (u64)__float_as_uint(top));  // (a place of its own: no barrier stands between this and the next)
+    auto join = [&](u64 v) {
+        top = fmaxf(top, __uint_as_float((uint32_t)(v >> 32)));
+        least_of = fminf(least_of, __uint_as_float((uint32_t)v));
+    };
+    for (int w = 0; w < kWarps; ++w) join(s.warp_mass[w]);
+    m.share(2, (u64)__float_as_uint(top) << 32 | __float_as_uint(least_of));  // (a place that the next to share does not use)
     cluster.sync();
-    for (int r = 0; r < ranks; ++r) top = fmaxf(top, __uint_as_float((uint32_t)s.total[2][r]));
+    for (int r = 0; r < ranks; ++r) join(s.total[2][r]);
 
     const float temperature = p.temperature ? p.temperature[t] : p.temperature1, top_p = p.top_p ? p.top_p[t] : p.top_p1;
-    float min_p = p.min_p ? p.min_p[t] : p.min_p1;
-    if (min_p > 1.f) min_p = 1.f;  // (NaN stays, and limits nothing)
-    const int top_k = p.top_k ? p.top_k[t] : p.top_k1;
+    const float min_p = p.min_p ? p.min_p[t] : p.min_p1;  // (NaN limits nothing)
+    int top_k = p.top_k ? p.top_k[t] : p.top_k1;
     if (top == -INFINITY || !(temperature > 0.f) || top_k == 1) {  // nothing to draw, or no choice
         int first = 0x7fffffff;
         if (top > -INFINITY)
-            m.each(m.lo + threadIdx.x * kChunk<T>, m.hi, kThreads, [&](float v, int i) {
-                if (fminf(v, kFltMax) == top) first = min(first, i);
+            m.each([&](float v, int i) {
+                if (fminf(v, kFltMax) == top && v == v) first = min(first, i);
             });
         first = (int)__reduce_min_sync(~0u, (uint32_t)first);
         if (threadIdx.x == 0) s.id = 0x7fffffff;
@@ -601,68 +840,57 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
         }
         return;
     }
-    m.slope = slope_of(top, temperature, p.shift);
-    m.floor = lowest(m.slope, kLeast, 0.f);
     const float u = p.u[t];
-    const bool by_sum = !(top_p >= 1.f);
-    if (top_k <= kWanted && (top_k > 0 || by_sum)) {
-        // ---- how far down the wanted tokens reach, by the threads' largest
+    m.slope = slope_of(top, temperature, p.shift);
+    // what is too small for the sums, and for min_p; all that is a number where
+    // the smallest is not
+    const float far = x_near(m.slope, least_of);
+    if (warp == 0) {
+        const float f0 = far < kLeast - 1.f ? -kFltMax : lowest(top, [&](float z) {
+            const Ratio x = x_of(m.slope, z);
+            return (x.hi - kLeast) + x.lo <= 0.f;  // (not of infinities)
+        });
+        if (lane == 0) s.floors[0] = f0;
+    } else if (warp == 1) {
+        const float f1 = !(min_p > 0x1p-40f) ? -kFltMax : min_p >= 1.f ? top : lowest(top, [&](float z) { return at_least(m.slope, z, min_p, s.powers); });
+        if (lane == 0) s.floors[1] = f1;
+    }
+    m.slope.bins = (float)(kBins - 2) / fminf(fmaxf(far, 0x1p-60f), kLeast + 1.f);  // (a NaN or infinity: 41)
+    if (top_k >= p.V) top_k = 0;
+    __syncthreads();
+    m.floor = s.floors[0];
+    const float least = s.floors[1];
+    if (top_k > 0 && top_k <= kWanted) {
+        // ---- how far down top_k tokens reach, by the threads' largest
         m.clear();
         if (threadIdx.x == 0) s.listed = 0;
-        if (mine >= m.floor) atomicAdd(&s.count[m.bin_of(mine)], 1u);
+        if (mine >= m.floor) atomicAdd(&s.count[(int)m.place_of(mine)], 1u);
         cluster.sync();
-        uint32_t c = 0, bin, bc;
-        for (int r = 0; r < ranks; ++r) c += cluster.map_shared_rank(s.count, r)[threadIdx.x];
+        uint32_t c[kBins / kThreads] = {}, bin, bc;
+        for (int r = 0; r < ranks; ++r) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(cluster.map_shared_rank(s.count, r) + 4 * threadIdx.x);
+            c[0] += v.x, c[1] += v.y, c[2] += v.z, c[3] += v.w;
+        }
         u64 bm;
-        const bool whole = !m.template crossing<kBinsX>([&](int) { return 0ull; }, [&](int) { return c; }, false, (u64)(top_k > 0 ? top_k : kWanted), bin, bm, bc);
-        const float lim = whole ? INFINITY : (float)(bin + 1);
-        // ---- their list; r of those, and of all
-        u64 in_list = 0, in_all = 0;
-        m.each(m.lo + threadIdx.x * kChunk<T>, m.hi, kThreads, [&](float v, int i) {
+        const bool some = m.crossing([&](int) { return 0ull; }, [&](int b) { return b & 2 ? (b & 1 ? c[3] : c[2]) : (b & 1 ? c[1] : c[0]); }, false, (u64)top_k, bin, bm, bc);
+        const float lim = some ? (float)(bin + 1) : INFINITY;
+        // ---- their list
+        m.each([&](float v, int i) {
             if (!(v >= m.floor)) return;
             v = fminf(v, kFltMax);
-            const bool in = x_near(m.slope, v) * kPerX < lim;
-            u64 w = 0;
-            if (in || top_k <= 0) w = weight_of(m.slope, v, s.powers);
-            if (in) {
-                const uint32_t at = atomicAdd(&s.listed, 1u);
-                if (at < kList) s.list_z[at] = v, s.list_id[at] = i, s.list_w[at] = w;
-                in_list += w;
-            }
-            in_all += w;
+            if (m.place_of(v) < lim) m.list(v, i, weight_of(m.slope, v, s.powers));
         });
-        in_list = m.cta_sum(in_list);
-        in_all = m.cta_sum(in_all);
-        m.share(0, in_list);
-        m.share(1, in_all);
+        __syncthreads();
         m.share(2, s.listed);
         cluster.sync();
-        u64 n = 0, before = 0;
-        in_list = in_all = 0;
-        for (int r = 0; r < ranks; ++r) in_list += s.total[0][r], in_all += s.total[1][r], n += s.total[2][r];
-        if (n <= kList && (top_k > 0 || in_list >= Sampler<T>::share_of(in_all, top_p, true))) {
-            // ---- the first CTA goes on by itself
-            if (rank == 0) {
-                before = s.total[2][0];
-                for (int r = 1; r < ranks; ++r) {
-                    const int part = (int)s.total[2][r];
-                    for (int i = threadIdx.x; i < part; i += kThreads) {
-                        s.list_z[before + i] = cluster.map_shared_rank(s.list_z, r)[i];
-                        s.list_id[before + i] = cluster.map_shared_rank(s.list_id, r)[i];
-                        s.list_w[before + i] = cluster.map_shared_rank(s.list_w, r)[i];
-                    }
-                    before += part;
-                }
-            }
-            cluster.sync();
-            if (rank != 0) return;
-            m.listed = (int)n;
-            m.template finish<true>(t, top_k, top_p, min_p, u);
+        const bool fits = m.gather();
+        cluster.sync();  // the lists and their lengths have been read
+        if (fits) {
+            if (rank == 0) m.from_list(t, top_k, top_p, least, u);
             return;
         }
-        cluster.sync();  // the totals have been read
     }
-    m.template finish<false>(t, top_k, top_p, min_p, u);
+    m.from_row(t, top_k, top_p, least, u);
     cluster.sync();  // (no CTA ends while another reads from it)
 }
 
