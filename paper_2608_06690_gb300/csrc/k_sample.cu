@@ -41,12 +41,13 @@ namespace cg = cooperative_groups;
 typedef unsigned long long u64;
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kMaxCluster = 16;
+constexpr int kMaxCluster = 8;
 constexpr int kSegs = 8 * kWarps;    // runs of ids whose sums a CTA keeps
 constexpr int kBins = 2048;          // of a histogram
 constexpr float kLeast = 40.f;       // log2 of the smallest r, negated
 constexpr int kFine = 46;            // bits of r behind the point
 constexpr int kList = 2048;          // tokens of a list
+constexpr int kShort = 192;          // of one that each token is compared with all of
 constexpr int kWanted = 1024;        // top_k up to which threads' largest logits show the border
 constexpr float kLog2eHi = 1.44269502f, kLog2eLo = 1.92596303e-8f;  // log2(e) in two words
 constexpr float kFltMax = 3.402823466e38f;
@@ -93,6 +94,20 @@ __device__ __forceinline__ uint32_t key_of(float z)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+// The value below a finite logit.
+__device__ __forceinline__ float below(float z)
+{
+    const uint32_t key = key_of(z);
+    return logit_of(key - (key == 0x80000000u ? 2 : 1));  // (the key before that of 0 is -0)
+}
+
+// +inf counts as the largest finite logit; NaN stays, and is above and below nothing.
+__device__ __forceinline__ float clip(float z)
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(z), "f"(kFltMax));
+    return r;
+}
 
 // What turns logits into x = (pre top - pre z) post (hi + lo).
 struct Slope {
@@ -266,23 +281,30 @@ template <typename T> struct Sampler {
     int rank, ranks, lo, hi;  // this CTA's ids (runs begin at whole loads)
     int listed;               // tokens in the list
 
-    // f(values, id of the first) of kChunk logits a load, `step` loads apart; NaN where there are none.
+    // kChunk logits from id i on, clipped; NaN from `end` on.
+    __device__ __forceinline__ void load(int i, int end, float (&v)[kChunk<T>]) const
+    {
+        if (vec && i + kChunk<T> <= end) {
+            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(z + i));
+            if constexpr (sizeof(T) == 4) {
+                v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
+            } else {
+                unpack8(u, v, T());
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kChunk<T>; ++j) v[j] = i + j < end ? to_f32<T>(z[i + j]) : NAN;
+        }
+#pragma unroll
+        for (int j = 0; j < kChunk<T>; ++j) v[j] = clip(v[j]);
+    }
+    // f(values, id of the first) of kChunk logits a load, `step` loads apart.
     template <typename F> __device__ __forceinline__ void loads(int begin, int end, int step, F f) const
     {
-#pragma unroll 2
+#pragma unroll 4
         for (int i = begin; i < end; i += step * kChunk<T>) {
             float v[kChunk<T>];
-            if (vec && i + kChunk<T> <= end) {
-                const uint4 u = __ldg(reinterpret_cast<const uint4 *>(z + i));
-                if constexpr (sizeof(T) == 4) {
-                    v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
-                } else {
-                    unpack8(u, v, T());
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < kChunk<T>; ++j) v[j] = i + j < end ? to_f32<T>(z[i + j]) : NAN;
-            }
+            load(i, end, v);
             f(v, i);
         }
     }
@@ -302,20 +324,25 @@ template <typename T> struct Sampler {
             loads(lo + threadIdx.x * kChunk<T>, hi, kThreads, [&](const float (&v)[kChunk<T>], int i) {
 #pragma unroll
                 for (int j = 0; j < kChunk<T>; j += 2) {
-                    const float a = fminf(v[j], kFltMax), b = fminf(v[j + 1], kFltMax);  // (NaN becomes the largest: told apart by v)
                     const bool in0 = v[j] >= floor, in1 = v[j + 1] >= floor;
                     u64 w0, w1;
-                    weights_of(slope, a, b, in0, in1, s.powers, w0, w1);
-                    if (in0) f(a, i + j, w0);
-                    if (in1) f(b, i + j + 1, w1);
+                    weights_of(slope, v[j], v[j + 1], in0, in1, s.powers, w0, w1);
+                    if (in0) f(v[j], i + j, w0);
+                    if (in1) f(v[j + 1], i + j + 1, w1);
                 }
             });
         }
     }
+    // All CTAs of the row.
+    __device__ __forceinline__ void all_meet() const
+    {
+        if (ranks > 1) cluster.sync();
+        else __syncthreads();
+    }
     template <bool kOfList> __device__ __forceinline__ void meet() const
     {
         if constexpr (kOfList) __syncthreads();
-        else cluster.sync();
+        else all_meet();
     }
     __device__ __forceinline__ void clear() const
     {
@@ -449,7 +476,7 @@ template <typename T> struct Sampler {
             each_weight<true>([&](float v, int, u64) { take(v); });
         } else {
             each([&](float v, int) {
-                if (v >= floor && (uint32_t)place_of(fminf(v, kFltMax)) == bin) take(fminf(v, kFltMax));
+                if (v >= floor && (uint32_t)place_of(v) == bin) take(v);
             });
         }
         klo = __reduce_min_sync(~0u, klo);
@@ -475,8 +502,7 @@ template <typename T> struct Sampler {
             } else {
                 const float least = logit_of(khi - width), most = logit_of(khi);
                 each([&](float v, int) {
-                    v = v >= floor ? fminf(v, kFltMax) : NAN;
-                    if (v >= least && v <= most) bin_it(v, weight_of(slope, v, s.powers));
+                    if (v >= least && v <= most && v >= floor) bin_it(v, weight_of(slope, v, s.powers));
                 });
             }
             merge<kOfList>();
@@ -527,15 +553,38 @@ template <typename T> struct Sampler {
         constexpr int kStep = 32 * kChunk<T>;
         return ((hi - lo + kSegs - 1) / kSegs + kStep - 1) / kStep * kStep;
     }
-    // Their sums of f(z, w, id), into s.seg.
+    // Their sums of f(values, id of the first), into s.seg.
     template <typename F> __device__ __forceinline__ void sum_runs(F f) const
     {
-        const int lane = threadIdx.x & 31, seg = run_length();
-        for (int g = threadIdx.x >> 5; g < kSegs; g += kWarps) {
-            u64 sum = 0;
-            loads(lo + g * seg + lane * kChunk<T>, min(hi, lo + (g + 1) * seg), 32, [&](const float (&v)[kChunk<T>], int i) { sum += f(v, i); });
-            sum = warp_sum(sum);
-            if (lane == 0) s.seg[g] = sum;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seg = run_length();
+        if (seg == 32 * kChunk<T>) {  // a load each: some at a time, so that their latencies overlap
+            constexpr int kRuns = kSegs / kWarps, kAtOnce = 16 / kChunk<T>;
+            for (int g = warp * kRuns; g < (warp + 1) * kRuns; g += kAtOnce) {
+                if (lo + g * seg >= hi) {
+                    if (lane < kAtOnce) s.seg[g + lane] = 0;
+                    continue;
+                }
+                float v[kAtOnce][kChunk<T>];
+                u64 sum[kAtOnce];
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) load(lo + (g + k) * seg + lane * kChunk<T>, hi, v[k]);
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) sum[k] = f(v[k], lo + (g + k) * seg + lane * kChunk<T>);
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+                    for (int k = 0; k < kAtOnce; ++k) sum[k] += __shfl_xor_sync(~0u, sum[k], off);
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k)
+                    if (lane == k) s.seg[g + k] = sum[k];
+            }
+        } else {
+            for (int g = warp; g < kSegs; g += kWarps) {
+                u64 sum = 0;
+                loads(lo + g * seg + lane * kChunk<T>, min(hi, lo + (g + 1) * seg), 32, [&](const float (&v)[kChunk<T>], int i) { sum += f(v, i); });
+                sum = warp_sum(sum);
+                if (lane == 0) s.seg[g] = sum;
+            }
         }
         __syncthreads();
     }
@@ -552,7 +601,7 @@ template <typename T> struct Sampler {
             sum = warp_sum(sum);
             if (lane < ranks) cluster.map_shared_rank(s.total[0], lane)[rank] = sum;
         }
-        cluster.sync();
+        all_meet();
         u64 before = 0;
         all = 0;
         for (int r = 0; r < ranks; ++r) {
@@ -578,21 +627,36 @@ template <typename T> struct Sampler {
                 }
                 before += __shfl_sync(~0u, sum, 31);
             }
-            for (int i = lo + g * seg + lane;; i += 32) {
-                u64 sum = i < hi ? one(to_f32<T>(z[i]), i) : 0;
+            // (a load of each lane, then that lane's values one after another)
+            for (int i = lo + g * seg + lane * kChunk<T>;; i += 32 * kChunk<T>) {
+                float v[kChunk<T>];
+                u64 w[kChunk<T>], sum = 0;
+                load(i, hi, v);
+#pragma unroll
+                for (int j = 0; j < kChunk<T>; ++j) sum += w[j] = one(v[j], i + j);
+                u64 upto = sum;
+#pragma unroll
                 for (int off = 1; off < 32; off <<= 1) {
-                    const u64 o = __shfl_up_sync(~0u, sum, off);
-                    if (lane >= off) sum += o;
+                    const u64 o = __shfl_up_sync(~0u, upto, off);
+                    if (lane >= off) upto += o;
                 }
-                const uint32_t past = __ballot_sync(~0u, before + sum > want);
+                const uint32_t past = __ballot_sync(~0u, before + upto > want);
                 if (past) {
-                    if (lane < ranks) *cluster.map_shared_rank(&s.id, lane) = i - lane + __ffs(past) - 1;
+                    u64 run = before + upto - sum;
+                    int id = -1;
+#pragma unroll
+                    for (int j = 0; j < kChunk<T>; ++j) {
+                        run += w[j];
+                        if (id < 0 && run > want) id = i + j;
+                    }
+                    id = __shfl_sync(~0u, id, __ffs(past) - 1);
+                    if (lane < ranks) *cluster.map_shared_rank(&s.id, lane) = id;
                     break;
                 }
-                before += __shfl_sync(~0u, sum, 31);
+                before += __shfl_sync(~0u, upto, 31);
             }
         }
-        cluster.sync();
+        all_meet();
         const int id = s.id;
         __syncthreads();  // before the next search resets it
         return id;
@@ -646,7 +710,7 @@ template <typename T> struct Sampler {
     {
         p.token[t] = id;
         int n;  // (r itself: of small ones the sums take few bits)
-        const uint32_t w = power_of(x_of(slope, fminf(to_f32<T>(z[id]), kFltMax)), s.powers, n);
+        const uint32_t w = power_of(x_of(slope, clip(to_f32<T>(z[id]))), s.powers, n);
         p.prob[t] = (float)w * __int_as_float((127 - n) << 23) * (float)(1 << (kFine - 31)) / ((float)all * (float)(1 << slope.shift));
     }
     // floor(sum f) for 0 <= f < 1 (above: as the largest such), or its ceiling.
@@ -665,9 +729,43 @@ template <typename T> struct Sampler {
         return (u64)q + (up && (q << down) != v);
     }
 
+    // The same for a short list, a thread a token: what is before it in the order
+    // of the logits, and in that of the ids, by comparison with each other one.
+    __device__ void from_short_list(int t, int top_k, float top_p, float least, float u)
+    {
+        const bool is = (int)threadIdx.x < listed;
+        const float v = is ? s.list_z[threadIdx.x] : 0.f;
+        const int id = is ? s.list_id[threadIdx.x] : 0;
+        const u64 w = is ? s.list_w[threadIdx.x] : 0;
+        u64 before = 0;
+        int place = 0;
+        if (is)
+            for (int j = 0; j < listed; ++j) {
+                const float o = s.list_z[j];
+                if (o > v || (o == v && s.list_id[j] < id)) before += s.list_w[j], ++place;
+            }
+        __syncthreads();  // the list has been read
+        bool in = is && place < top_k;
+        if (!(top_p >= 1.f)) {
+            const u64 sum = cta_sum(in ? w : 0);
+            in = in && before < max(share_of(sum, top_p, true), 1ull);
+        }
+        in = in && v >= least;
+        if (is && !in) s.list_w[threadIdx.x] = 0;  // (read again behind the sum's barriers)
+        const u64 all = cta_sum(in ? w : 0), want = share_of(all, u, false);
+        u64 upto = 0;
+        if (in)
+            for (int j = 0; j < listed; ++j)
+                if (s.list_id[j] <= id) upto += s.list_w[j];
+        if (in && upto > want && upto - w <= want) answer(t, id, all);
+    }
     // A row whose best top_k are in the list: the first CTA by itself.
     __device__ void from_list(int t, int top_k, float top_p, float least, float u)
     {
+        if (listed <= kShort) {
+            from_short_list(t, top_k, top_p, least, u);
+            return;
+        }
         u64 sum = 0, ties = ~0ull, upto;
         float logit = -INFINITY;
         int last = 0x7fffffff;
@@ -710,8 +808,8 @@ template <typename T> struct Sampler {
                     u64 run = 0;
 #pragma unroll
                     for (int j = 0; j < kChunk<T>; j += 2) {
-                        const float a = fminf(v[j], kFltMax), b = fminf(v[j + 1], kFltMax), x0 = place_of(a), x1 = place_of(b);
-                        const bool in0 = v[j] >= floor && x0 < to, in1 = v[j + 1] >= floor && x1 < to;
+                        const float a = v[j], b = v[j + 1], x0 = place_of(a), x1 = place_of(b);
+                        const bool in0 = a >= floor && x0 < to, in1 = b >= floor && x1 < to;
                         if (!(in0 || in1)) continue;
                         u64 w0, w1;
                         weights_of(slope, a, b, in0, in1, s.powers, w0, w1);
@@ -722,7 +820,7 @@ template <typename T> struct Sampler {
                     return run;
                 });
                 share(2, s.listed);
-                cluster.sync();
+                all_meet();
                 summed = gather();
                 if (summed) {
                     if (rank == 0) {
@@ -734,47 +832,51 @@ template <typename T> struct Sampler {
                         }
                         listed = (int)s.total[2][0];
                     }
-                    cluster.sync();
+                    all_meet();
                     logit = s.logit, last = s.last, sum = s.upto;
                 } else {
-                    cluster.sync();  // the lengths have been read
+                    all_meet();  // the lengths have been read
                     border<false>(turn == 1, want, bin, mass, count, logit, ties, upto);
                     sum_runs([&](const float (&v)[kChunk<T>], int) {
                         u64 n = 0;
 #pragma unroll
-                        for (int j = 0; j < kChunk<T>; ++j) n += fminf(v[j], kFltMax) == logit && v[j] == v[j];
+                        for (int j = 0; j < kChunk<T>; ++j) n += v[j] == logit;
                         return n;
                     });
                     u64 all;
-                    last = locate([&](float v, int) { return (u64)(fminf(v, kFltMax) == logit && v == v); }, [&](u64) { return ties - 1; }, all);
+                    last = locate([&](float v, int) { return (u64)(v == logit); }, [&](u64) { return ties - 1; }, all);
                     sum = upto;
                 }
             }
         }
-        auto kept = [&](float v, int i) { return v >= floor && v >= least && (v > logit || (v == logit && i <= last)); };
+        // without a border above them, what the limits leave
+        const float limit = fmaxf(floor, least);
+        const bool bordered = logit >= limit;
+        if (!bordered) logit = below(limit), last = -1;
+        auto kept = [&](float v, int i) { return v > logit || (v == logit && i <= last); };
         if (summed) {  // the border's bin, from this CTA's list
             const int seg = run_length();
             for (int i = threadIdx.x; i < listed; i += kThreads)
                 if (kept(s.list_z[i], s.list_id[i])) atomicAdd(&s.seg[(s.list_id[i] - lo) / seg], s.list_w[i]);
             __syncthreads();
         } else {
-            sum_runs([&](const float (&v)[kChunk<T>], int i) {
-                u64 run = 0;
+            auto sums = [&](auto in) {
+                sum_runs([&](const float (&v)[kChunk<T>], int i) {
+                    u64 run = 0;
 #pragma unroll
-                for (int j = 0; j < kChunk<T>; j += 2) {
-                    const float a = fminf(v[j], kFltMax), b = fminf(v[j + 1], kFltMax);
-                    u64 w0, w1;
-                    weights_of(slope, a, b, v[j] == v[j] && kept(a, i + j), v[j + 1] == v[j + 1] && kept(b, i + j + 1), s.powers, w0, w1);
-                    run += w0 + w1;
-                }
-                return run;
-            });
+                    for (int j = 0; j < kChunk<T>; j += 2) {
+                        u64 w0, w1;
+                        weights_of(slope, v[j], v[j + 1], in(v[j], i + j), in(v[j + 1], i + j + 1), s.powers, w0, w1);
+                        run += w0 + w1;
+                    }
+                    return run;
+                });
+            };
+            if (bordered) sums(kept);
+            else sums([&](float v, int) { return v > logit; });
         }
         u64 all;
-        const int id = locate([&](float v, int i) {
-            const float a = fminf(v, kFltMax);
-            return v == v && kept(a, i) ? weight_of(slope, a, s.powers) : 0ull;
-        }, [&](u64 sum) { return share_of(sum, u, false); }, all);
+        const int id = locate([&](float v, int i) { return kept(v, i) ? weight_of(slope, v, s.powers) : 0ull; }, [&](u64 sum) { return share_of(sum, u, false); }, all);
         if (rank == 0 && threadIdx.x == 0) answer(t, id, all);
     }
 };
@@ -799,7 +901,6 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
         mine = fmaxf(mine, v);
         least_of = fminf(least_of, v);
     });
-    mine = fminf(mine, kFltMax);
     float top = mine;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
@@ -814,7 +915,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
     };
     for (int w = 0; w < kWarps; ++w) join(s.warp_mass[w]);
     m.share(2, (u64)__float_as_uint(top) << 32 | __float_as_uint(least_of));  // (a place that the next to share does not use)
-    cluster.sync();
+    m.all_meet();
     for (int r = 0; r < ranks; ++r) join(s.total[2][r]);
 
     const float temperature = p.temperature ? p.temperature[t] : p.temperature1, top_p = p.top_p ? p.top_p[t] : p.top_p1;
@@ -824,7 +925,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
         int first = 0x7fffffff;
         if (top > -INFINITY)
             m.each([&](float v, int i) {
-                if (fminf(v, kFltMax) == top && v == v) first = min(first, i);
+                if (v == top) first = min(first, i);
             });
         first = (int)__reduce_min_sync(~0u, (uint32_t)first);
         if (threadIdx.x == 0) s.id = 0x7fffffff;
@@ -832,7 +933,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
         if (lane == 0) atomicMin(&s.id, first);
         __syncthreads();
         m.share(1, (u64)s.id);
-        cluster.sync();
+        m.all_meet();
         if (rank == 0 && threadIdx.x == 0) {
             for (int r = 0; r < ranks; ++r) first = min(first, (int)s.total[1][r]);
             p.token[t] = top > -INFINITY ? first : -1;
@@ -865,7 +966,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
         m.clear();
         if (threadIdx.x == 0) s.listed = 0;
         if (mine >= m.floor) atomicAdd(&s.count[(int)m.place_of(mine)], 1u);
-        cluster.sync();
+        m.all_meet();
         uint32_t c[kBins / kThreads] = {}, bin, bc;
         for (int r = 0; r < ranks; ++r) {
             const uint4 v = *reinterpret_cast<const uint4 *>(cluster.map_shared_rank(s.count, r) + 4 * threadIdx.x);
@@ -876,22 +977,20 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
         const float lim = some ? (float)(bin + 1) : INFINITY;
         // ---- their list
         m.each([&](float v, int i) {
-            if (!(v >= m.floor)) return;
-            v = fminf(v, kFltMax);
-            if (m.place_of(v) < lim) m.list(v, i, weight_of(m.slope, v, s.powers));
+            if (v >= m.floor && m.place_of(v) < lim) m.list(v, i, weight_of(m.slope, v, s.powers));
         });
         __syncthreads();
         m.share(2, s.listed);
-        cluster.sync();
+        m.all_meet();
         const bool fits = m.gather();
-        cluster.sync();  // the lists and their lengths have been read
+        m.all_meet();  // the lists and their lengths have been read
         if (fits) {
             if (rank == 0) m.from_list(t, top_k, top_p, least, u);
             return;
         }
     }
     m.from_row(t, top_k, top_p, least, u);
-    cluster.sync();  // (no CTA ends while another reads from it)
+    m.all_meet();  // (no CTA ends while another reads from it)
 }
 
 template <typename T> cudaError_t launch_typed(const SampleParams &p, int num_sms, cudaStream_t st)
@@ -901,7 +1000,6 @@ template <typename T> cudaError_t launch_typed(const SampleParams &p, int num_sm
     while (ranks < kMaxCluster && 2 * ranks * (long long)p.T <= 2 * num_sms && p.V >= 8192 * ranks) ranks *= 2;
     static std::atomic<int> limit[64];
     cudaError_t err = ensure_dynamic_smem(sample_kernel<T>, sizeof(Shared), limit);
-    if (err == cudaSuccess && ranks > 8) err = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (err != cudaSuccess) return err;
     return launch_cluster_pdl(sample_kernel<T>, ranks, dim3((unsigned)(p.T * (long long)ranks)), dim3(kThreads), sizeof(Shared), st, p);
 }
