@@ -47,7 +47,7 @@ constexpr int kBins = 2048;          // of a histogram
 constexpr float kLeast = 40.f;       // log2 of the smallest r, negated
 constexpr int kFine = 46;            // bits of r behind the point
 constexpr int kList = 2048;          // tokens of a list
-constexpr int kShort = 192;          // of one that each token is compared with all of
+constexpr int kShort = 384;          // of one that each token is compared with all of
 constexpr int kWanted = 1024;        // top_k up to which threads' largest logits show the border
 constexpr float kLog2eHi = 1.44269502f, kLog2eLo = 1.92596303e-8f;  // log2(e) in two words
 constexpr float kFltMax = 3.402823466e38f;
@@ -361,7 +361,7 @@ template <typename T> struct Sampler {
     }
     __device__ __forceinline__ u64 mass_at(int b) const { return ((u64)s.mass_hi[b] << 32) + s.mass_lo[b]; }
     // The histogram of all CTAs in place of each one's.
-    template <bool kOfList> __device__ void merge() const
+    template <bool kOfList> __device__ void merge(bool counts = true) const
     {
         meet<kOfList>();
         if (kOfList || ranks == 1) return;
@@ -376,7 +376,7 @@ template <typename T> struct Sampler {
             for (int j = 0; j < kPer; ++j) {
                 const int b = threadIdx.x + j * kThreads;
                 m[j] += ((u64)hi32[b] << 32) + lo32[b];
-                c[j] += n[b];
+                if (counts) c[j] += n[b];
             }
         }
         cluster.sync();
@@ -438,18 +438,34 @@ template <typename T> struct Sampler {
         return bin != ~0u;
     }
     // The bin of a histogram over x; the same number as it is compared with.
-    __device__ __forceinline__ float place_of(float v) const { return x_near(slope, v) * slope.bins; }
+    __device__ __forceinline__ float place_of(float v) const { return __fmul_rn(x_near(slope, v), slope.bins); }
 
     // The histogram over x, into mass_x and count_x (counts only where they are wanted); the sum of all.
     __device__ u64 over_x(bool counts) const
     {
         clear();
-        each_weight<false>([&](float v, int, u64 w) {
-            const int b = (int)place_of(v);
-            if (counts) atomicAdd(&s.count[b], 1u);
-            add_mass(b, w);
+        loads(lo + threadIdx.x * kChunk<T>, hi, kThreads, [&](const float (&v)[kChunk<T>], int) {
+            constexpr int kN = kChunk<T>;
+            u64 w[kN];
+            uint32_t old[kN];
+            int b[kN];
+#pragma unroll
+            for (int j = 0; j < kN; j += 2) {
+                weights_of(slope, v[j], v[j + 1], v[j] >= floor, v[j + 1] >= floor, s.powers, w[j], w[j + 1]);
+                b[j] = w[j] ? (int)place_of(v[j]) : 0;
+                b[j + 1] = w[j + 1] ? (int)place_of(v[j + 1]) : 0;
+            }
+            // (one after another, each waiting for its carry, they took twice as long)
+#pragma unroll
+            for (int j = 0; j < kN; ++j) old[j] = w[j] ? atomicAdd(&s.mass_lo[b[j]], (uint32_t)w[j]) : 0;
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                const uint32_t high = (uint32_t)(w[j] >> 32) + (old[j] > ~(uint32_t)w[j]);
+                if (high) atomicAdd(&s.mass_hi[b[j]], high);
+                if (counts && w[j]) atomicAdd(&s.count[b[j]], 1u);
+            }
         });
-        merge<false>();
+        merge<false>(counts);
         u64 sum = 0;
         for (int b = threadIdx.x; b < kBins; b += kThreads) {
             sum += s.mass_x[b] = mass_at(b);
@@ -729,8 +745,38 @@ template <typename T> struct Sampler {
         return (u64)q + (up && (q << down) != v);
     }
 
-    // The same for a short list, a thread a token: what is before it in the order
-    // of the logits, and in that of the ids, by comparison with each other one.
+    // What stands before a token in the order of the logits: the sum, and how many.
+    // (Without branches: with one for each other token 104 took 12 us.)
+    __device__ __forceinline__ u64 before_in_list(float v, int id, uint32_t &place) const
+    {
+        u64 sum = 0;
+        place = 0;
+#pragma unroll 8
+        for (int j = 0; j < listed; ++j) {
+            const float o = s.list_z[j];
+            const int i = s.list_id[j];
+            const u64 w = s.list_w[j];
+            const bool before = o > v || (o == v && i < id);
+            sum += before ? w : 0;
+            place += before;
+        }
+        return sum;
+    }
+    // The border in a short list: the last token that is kept, and the sum up to
+    // it, into s; a thread a token, by comparison with each other one.
+    __device__ void short_border(bool by_mass, u64 want, u64 mass, uint32_t count) const
+    {
+        if ((int)threadIdx.x >= listed) return;
+        const float v = s.list_z[threadIdx.x];
+        const int id = s.list_id[threadIdx.x];
+        const u64 w = s.list_w[threadIdx.x];
+        uint32_t place;
+        mass += before_in_list(v, id, place);
+        count += place;
+        if (by_mass ? mass < want && mass + w >= want : count + 1 == want) s.logit = v, s.last = id, s.upto = mass + w;
+    }
+    // A row whose best top_k are in a short list, a thread a token: what is before
+    // it in the order of the logits, and in that of the ids, in the same way.
     __device__ void from_short_list(int t, int top_k, float top_p, float least, float u)
     {
         const bool is = (int)threadIdx.x < listed;
@@ -738,14 +784,10 @@ template <typename T> struct Sampler {
         const int id = is ? s.list_id[threadIdx.x] : 0;
         const u64 w = is ? s.list_w[threadIdx.x] : 0;
         u64 before = 0;
-        int place = 0;
-        if (is)
-            for (int j = 0; j < listed; ++j) {
-                const float o = s.list_z[j];
-                if (o > v || (o == v && s.list_id[j] < id)) before += s.list_w[j], ++place;
-            }
+        uint32_t place = 0;
+        if (is) before = before_in_list(v, id, place);
         __syncthreads();  // the list has been read
-        bool in = is && place < top_k;
+        bool in = is && place < (uint32_t)top_k;
         if (!(top_p >= 1.f)) {
             const u64 sum = cta_sum(in ? w : 0);
             in = in && before < max(share_of(sum, top_p, true), 1ull);
@@ -754,9 +796,13 @@ template <typename T> struct Sampler {
         if (is && !in) s.list_w[threadIdx.x] = 0;  // (read again behind the sum's barriers)
         const u64 all = cta_sum(in ? w : 0), want = share_of(all, u, false);
         u64 upto = 0;
-        if (in)
-            for (int j = 0; j < listed; ++j)
-                if (s.list_id[j] <= id) upto += s.list_w[j];
+        if (in) {
+#pragma unroll 8
+            for (int j = 0; j < listed; ++j) {
+                const u64 o = s.list_w[j];
+                upto += s.list_id[j] <= id ? o : 0;
+            }
+        }
         if (in && upto > want && upto - w <= want) answer(t, id, all);
     }
     // A row whose best top_k are in the list: the first CTA by itself.
@@ -824,11 +870,17 @@ template <typename T> struct Sampler {
                 summed = gather();
                 if (summed) {
                     if (rank == 0) {
-                        border<true>(turn == 1, want, 0, mass, count, logit, ties, upto);
-                        last = locate_in_list([&](float v, int, u64) { return (u64)(v == logit); }, ties - 1);
-                        if ((int)threadIdx.x < ranks) {
+                        if (listed <= kShort) {
+                            short_border(turn == 1, want, mass, count);
+                        } else {
+                            border<true>(turn == 1, want, 0, mass, count, logit, ties, upto);
+                            last = locate_in_list([&](float v, int, u64) { return (u64)(v == logit); }, ties - 1);
+                            if (threadIdx.x == 0) s.logit = logit, s.last = last, s.upto = upto;
+                        }
+                        __syncthreads();
+                        if (threadIdx.x > 0 && (int)threadIdx.x < ranks) {
                             Shared *o = cluster.map_shared_rank(&s, threadIdx.x);
-                            o->logit = logit, o->last = last, o->upto = upto;
+                            o->logit = s.logit, o->last = s.last, o->upto = s.upto;
                         }
                         listed = (int)s.total[2][0];
                     }
