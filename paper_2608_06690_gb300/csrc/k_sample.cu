@@ -28,6 +28,8 @@
 // A list that does not fit (many tokens of about the same logit) is replaced by
 // further passes, over the bits of the logits in the border's bin, down to one
 // value.  Of equal logits at the border the lowest ids stay.
+#include <string.h>
+
 #include <algorithm>
 
 #include <cooperative_groups.h>
@@ -218,12 +220,16 @@ __device__ __forceinline__ Two mul2(Two a, Two b)
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a.v), "l"(b.v));
     return Two(r);
 }
+// (For temperatures far from 1: out of line, where rows seldom go.  A row runs
+// each of its passes once: their code is fetched as they run, and time is lost
+// with what is skipped as well.)
+__device__ __noinline__ u64 weight_apart(Slope s, float z, const Power *powers) { return weight_of(s, z, powers); }
 // weight_of() of two logits, the same arithmetic; 0 where `in` is false.
 __device__ __forceinline__ void weights_of(const Slope &s, float z0, float z1, bool in0, bool in1, const Power *powers, u64 &w0, u64 &w1)
 {
     if (!s.plain) {
-        w0 = in0 ? weight_of(s, z0, powers) : 0;
-        w1 = in1 ? weight_of(s, z1, powers) : 0;
+        w0 = in0 ? weight_apart(s, z0, powers) : 0;
+        w1 = in1 ? weight_apart(s, z1, powers) : 0;
         return;
     }
     const Two minus(-1.f, -1.f), a(s.top, s.top), z(z0, z1), c(s.hi, s.hi);
@@ -274,37 +280,51 @@ template <typename T> struct Sampler {
     const SampleParams &p;
     Shared &s;
     cg::cluster_group cluster;
-    const T *z;
-    bool vec;                 // whole loads: rows are aligned for them
+    const T *z;               // the row from the 16-byte boundary before it on: token i is at position i + head
+    int head;
     Slope slope;
     float floor;              // the lowest logit that sums and counts take
-    int rank, ranks, lo, hi;  // this CTA's ids (runs begin at whole loads)
+    int rank, ranks, lo, hi;  // this CTA's positions, from whole loads on; what is called id below is a position too
     int listed;               // tokens in the list
 
-    // kChunk logits from id i on, clipped; NaN from `end` on.
-    __device__ __forceinline__ void load(int i, int end, float (&v)[kChunk<T>]) const
+    // kChunk logits from id i on, as they lie in memory; NaN from `end` on.
+    __device__ __forceinline__ uint4 fetch(int i, int end) const
     {
-        if (vec && i + kChunk<T> <= end) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(z + i));
-            if constexpr (sizeof(T) == 4) {
-                v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
-            } else {
-                unpack8(u, v, T());
-            }
-        } else {
+        return i >= head && i + kChunk<T> <= end ? __ldg(reinterpret_cast<const uint4 *>(z + i)) : fetch_apart(z, i, end, head);
+    }
+    static __device__ __noinline__ uint4 fetch_apart(const T *z, int i, int end, int head)
+    {
+        uint4 u;
+        T v[kChunk<T>];
 #pragma unroll
-            for (int j = 0; j < kChunk<T>; ++j) v[j] = i + j < end ? to_f32<T>(z[i + j]) : NAN;
+        for (int j = 0; j < kChunk<T>; ++j) v[j] = i + j >= head && i + j < end ? z[i + j] : from_f32<T>(NAN);
+        memcpy(&u, v, sizeof(u));
+        return u;
+    }
+    // As FP32, clipped.
+    static __device__ __forceinline__ void spread(const uint4 &u, float (&v)[kChunk<T>])
+    {
+        if constexpr (sizeof(T) == 4) {
+            v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
+        } else {
+            unpack8(u, v, T());
         }
 #pragma unroll
         for (int j = 0; j < kChunk<T>; ++j) v[j] = clip(v[j]);
     }
-    // f(values, id of the first) of kChunk logits a load, `step` loads apart.
+    __device__ __forceinline__ void load(int i, int end, float (&v)[kChunk<T>]) const { spread(fetch(i, end), v); }
+    // f(values, id of the first) of kChunk logits a load, `step` loads apart, the
+    // next load ahead.
     template <typename F> __device__ __forceinline__ void loads(int begin, int end, int step, F f) const
     {
-#pragma unroll 4
+        if (begin >= end) return;
+        uint4 next = fetch(begin, end);
+#pragma unroll 1
         for (int i = begin; i < end; i += step * kChunk<T>) {
+            const uint4 now = next;
+            if (i + step * kChunk<T> < end) next = fetch(i + step * kChunk<T>, end);
             float v[kChunk<T>];
-            load(i, end, v);
+            spread(now, v);
             f(v, i);
         }
     }
@@ -547,7 +567,7 @@ template <typename T> struct Sampler {
         clear();
         each_weight<true>([&](float v, int i, u64 w) {
             w = f(v, i, w);
-            if (w) add_mass(i >> 10, w);
+            if (w) add_mass((i - head) >> 10, w);
         });
         __syncthreads();
         ++want;
@@ -555,12 +575,12 @@ template <typename T> struct Sampler {
         want -= bm;
         clear();
         each_weight<true>([&](float v, int i, u64 w) {
-            w = (uint32_t)(i >> 10) == high ? f(v, i, w) : 0;
-            if (w) add_mass(i & 1023, w);
+            w = (uint32_t)((i - head) >> 10) == high ? f(v, i, w) : 0;
+            if (w) add_mass((i - head) & 1023, w);
         });
         __syncthreads();
         crossing(mass, count, true, want, low, bm, bc);
-        return (int)(high << 10 | low);
+        return (int)(high << 10 | low) + head;
     }
 
     // Runs of ids: a warp's, kSegs of a CTA, of whole loads.
@@ -573,34 +593,11 @@ template <typename T> struct Sampler {
     template <typename F> __device__ __forceinline__ void sum_runs(F f) const
     {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seg = run_length();
-        if (seg == 32 * kChunk<T>) {  // a load each: some at a time, so that their latencies overlap
-            constexpr int kRuns = kSegs / kWarps, kAtOnce = 16 / kChunk<T>;
-            for (int g = warp * kRuns; g < (warp + 1) * kRuns; g += kAtOnce) {
-                if (lo + g * seg >= hi) {
-                    if (lane < kAtOnce) s.seg[g + lane] = 0;
-                    continue;
-                }
-                float v[kAtOnce][kChunk<T>];
-                u64 sum[kAtOnce];
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) load(lo + (g + k) * seg + lane * kChunk<T>, hi, v[k]);
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) sum[k] = f(v[k], lo + (g + k) * seg + lane * kChunk<T>);
-#pragma unroll
-                for (int off = 16; off > 0; off >>= 1)
-#pragma unroll
-                    for (int k = 0; k < kAtOnce; ++k) sum[k] += __shfl_xor_sync(~0u, sum[k], off);
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k)
-                    if (lane == k) s.seg[g + k] = sum[k];
-            }
-        } else {
-            for (int g = warp; g < kSegs; g += kWarps) {
-                u64 sum = 0;
-                loads(lo + g * seg + lane * kChunk<T>, min(hi, lo + (g + 1) * seg), 32, [&](const float (&v)[kChunk<T>], int i) { sum += f(v, i); });
-                sum = warp_sum(sum);
-                if (lane == 0) s.seg[g] = sum;
-            }
+        for (int g = warp; g < kSegs; g += kWarps) {
+            u64 sum = 0;
+            loads(lo + g * seg + lane * kChunk<T>, min(hi, lo + (g + 1) * seg), 32, [&](const float (&v)[kChunk<T>], int i) { sum += f(v, i); });
+            sum = warp_sum(sum);
+            if (lane == 0) s.seg[g] = sum;
         }
         __syncthreads();
     }
@@ -724,7 +721,7 @@ template <typename T> struct Sampler {
 
     __device__ void answer(int t, int id, u64 all) const
     {
-        p.token[t] = id;
+        p.token[t] = id - head;
         int n;  // (r itself: of small ones the sums take few bits)
         const uint32_t w = power_of(x_of(slope, clip(to_f32<T>(z[id]))), s.powers, n);
         p.prob[t] = (float)w * __int_as_float((127 - n) << 23) * (float)(1 << (kFine - 31)) / ((float)all * (float)(1 << slope.shift));
@@ -942,17 +939,31 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
     pdl_wait();
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), t = blockIdx.x / ranks;
-    const int slice = ((p.V + ranks - 1) / ranks + 31) / 32 * 32;
     const T *row = (const T *)p.logits + t * p.ld;
-    Sampler<T> m = {p, s, cluster, row, ((uintptr_t)row & 15u) == 0, Slope(), -INFINITY, rank, ranks, min(p.V, rank * slice), min(p.V, (rank + 1) * slice), 0};
+    const int head = (int)((uintptr_t)row & 15u) / (int)sizeof(T), end = head + p.V, slice = ((end + ranks - 1) / ranks + 31) / 32 * 32;
+    Sampler<T> m = {p, s, cluster, row - head, head, Slope(), -INFINITY, rank, ranks, min(end, rank * slice), min(end, (rank + 1) * slice), 0};
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 
     // ---- the largest logit, and the smallest
     float mine = -INFINITY, least_of = INFINITY;  // of this thread (NaN is passed over)
-    m.each([&](float v, int) {
-        mine = fmaxf(mine, v);
-        least_of = fminf(least_of, v);
-    });
+    for (int i = m.lo + threadIdx.x * kChunk<T>; i < m.hi; i += 4 * kThreads * kChunk<T>) {
+        uint4 raw[4];  // four loads at a time, past the end the first again
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int at = i + k * kThreads * kChunk<T>;
+            raw[k] = m.fetch(at < m.hi ? at : i, m.hi);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float v[kChunk<T>];
+            m.spread(raw[k], v);
+#pragma unroll
+            for (int j = 0; j < kChunk<T>; ++j) {
+                mine = fmaxf(mine, v[j]);
+                least_of = fminf(least_of, v[j]);
+            }
+        }
+    }
     float top = mine;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
@@ -988,7 +999,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
         m.all_meet();
         if (rank == 0 && threadIdx.x == 0) {
             for (int r = 0; r < ranks; ++r) first = min(first, (int)s.total[1][r]);
-            p.token[t] = top > -INFINITY ? first : -1;
+            p.token[t] = top > -INFINITY ? first - m.head : -1;
             p.prob[t] = top > -INFINITY ? 1.f : 0.f;
         }
         return;
