@@ -259,8 +259,11 @@ __device__ __forceinline__ void weights_of(const Slope &s, float z0, float z1, b
 struct Shared {
     Power powers[256];
     uint32_t mass_lo[kBins], mass_hi[kBins], count[kBins];
-    u64 mass_x[kBins];       // merged: of the histogram over x
+    u64 mass_x[kBins];       // of the histogram over x, all CTAs': each CTA has a share of the bins
     uint32_t count_x[kBins];
+    u64 mass_of[kMaxCluster], count_of[kMaxCluster];  // of the CTAs' shares
+    u64 border_mass;         // before the bin of the border
+    uint32_t border_bin, border_count;
     float list_z[kList];
     int list_id[kList];
     u64 list_w[kList];
@@ -381,7 +384,7 @@ template <typename T> struct Sampler {
     }
     __device__ __forceinline__ u64 mass_at(int b) const { return ((u64)s.mass_hi[b] << 32) + s.mass_lo[b]; }
     // The histogram of all CTAs in place of each one's.
-    template <bool kOfList> __device__ void merge(bool counts = true) const
+    template <bool kOfList> __device__ void merge() const
     {
         meet<kOfList>();
         if (kOfList || ranks == 1) return;
@@ -396,7 +399,7 @@ template <typename T> struct Sampler {
             for (int j = 0; j < kPer; ++j) {
                 const int b = threadIdx.x + j * kThreads;
                 m[j] += ((u64)hi32[b] << 32) + lo32[b];
-                if (counts) c[j] += n[b];
+                c[j] += n[b];
             }
         }
         cluster.sync();
@@ -485,17 +488,59 @@ template <typename T> struct Sampler {
                 if (counts && w[j]) atomicAdd(&s.count[b[j]], 1u);
             }
         });
-        merge<false>(counts);
-        u64 sum = 0;
-        for (int b = threadIdx.x; b < kBins; b += kThreads) {
-            sum += s.mass_x[b] = mass_at(b);
-            s.count_x[b] = s.count[b];
+        all_meet();
+        // each CTA adds up its share of the bins (every CTA all of them: 6 us)
+        const int share_bins = kBins / ranks, first = rank * share_bins;
+        u64 sum = 0, n = 0;
+        for (int b = first + threadIdx.x; b < first + share_bins; b += kThreads) {
+            u64 m = 0;
+            uint32_t c = 0;
+            for (int r = 0; r < ranks; ++r) {
+                const Shared *o = cluster.map_shared_rank(&s, r);
+                m += ((u64)o->mass_hi[b] << 32) + o->mass_lo[b];
+                if (counts) c += o->count[b];
+            }
+            s.mass_x[b] = m;
+            s.count_x[b] = c;
+            sum += m;
+            n += c;
         }
-        return cta_sum(sum);
+        sum = cta_sum(sum);
+        n = cta_sum(n);
+        if ((int)threadIdx.x < ranks) {
+            Shared *o = cluster.map_shared_rank(&s, threadIdx.x);
+            o->mass_of[rank] = sum;
+            o->count_of[rank] = n;
+        }
+        all_meet();
+        sum = 0;
+        for (int r = 0; r < ranks; ++r) sum += s.mass_of[r];
+        return sum;
     }
-    __device__ __forceinline__ bool crossing_x(bool by_mass, u64 want, uint32_t &bin, u64 &mass, uint32_t &count) const
+    // The bin over x where the running count (or sum) reaches `want`, and what
+    // comes before it; found by the CTA that has it.  false: none does.
+    __device__ bool crossing_x(bool by_mass, u64 want, uint32_t &bin, u64 &mass, uint32_t &count) const
     {
-        return crossing([&](int b) { return s.mass_x[b]; }, [&](int b) { return s.count_x[b]; }, by_mass, want, bin, mass, count);
+        u64 m = 0, c = 0;
+        int r = 0;
+        for (; r < ranks && (by_mass ? m + s.mass_of[r] : c + s.count_of[r]) < want; ++r) m += s.mass_of[r], c += s.count_of[r];
+        if (r == ranks) return false;
+        if (r == rank) {
+            const int share_bins = kBins / ranks, first = rank * share_bins;
+            auto mine = [&](int b) { return b >= first && b < first + share_bins; };
+            crossing([&](int b) { return mine(b) ? s.mass_x[b] : 0ull; }, [&](int b) { return mine(b) ? s.count_x[b] : 0u; }, by_mass, want - (by_mass ? m : c), bin, mass, count);
+            if ((int)threadIdx.x < ranks) {
+                Shared *o = cluster.map_shared_rank(&s, threadIdx.x);
+                o->border_bin = bin;
+                o->border_mass = mass + m;
+                o->border_count = count + (uint32_t)c;
+            }
+        }
+        all_meet();
+        bin = s.border_bin;
+        mass = s.border_mass;
+        count = s.border_count;
+        return true;
     }
 
     // The logit at which the running count (or sum) reaches `want`, after what
@@ -589,16 +634,34 @@ template <typename T> struct Sampler {
         constexpr int kStep = 32 * kChunk<T>;
         return ((hi - lo + kSegs - 1) / kSegs + kStep - 1) / kStep * kStep;
     }
-    // Their sums of f(values, id of the first), into s.seg.
+    // Their sums of f(values, id of the first), into s.seg; a warp's runs lie one
+    // after another, the next load ahead across them.
     template <typename F> __device__ __forceinline__ void sum_runs(F f) const
     {
+        constexpr int kStep = 32 * kChunk<T>, kRuns = kSegs / kWarps;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seg = run_length();
-        for (int g = warp; g < kSegs; g += kWarps) {
-            u64 sum = 0;
-            loads(lo + g * seg + lane * kChunk<T>, min(hi, lo + (g + 1) * seg), 32, [&](const float (&v)[kChunk<T>], int i) { sum += f(v, i); });
-            sum = warp_sum(sum);
-            if (lane == 0) s.seg[g] = sum;
+        const int begin = lo + warp * kRuns * seg, finish = min(hi, begin + kRuns * seg);
+        int g = warp * kRuns, left = seg;
+        u64 sum = 0;
+        uint4 next = make_uint4(0, 0, 0, 0);
+        if (begin < finish) next = fetch(begin + lane * kChunk<T>, hi);
+#pragma unroll 1
+        for (int i = begin; i < finish; i += kStep) {
+            const uint4 now = next;
+            if (i + kStep < finish) next = fetch(i + kStep + lane * kChunk<T>, hi);
+            float v[kChunk<T>];
+            spread(now, v);
+            sum += f(v, i + lane * kChunk<T>);
+            left -= kStep;
+            if (left == 0 || i + kStep >= finish) {
+                sum = warp_sum(sum);
+                if (lane == 0) s.seg[g] = sum;
+                ++g;
+                sum = 0;
+                left = seg;
+            }
         }
+        for (g += lane; g < (warp + 1) * kRuns; g += 32) s.seg[g] = 0;
         __syncthreads();
     }
     // The first id whose running sum is above target(sum of all), with the runs'
