@@ -584,8 +584,9 @@ PMPE_API int pmpe_kv_read(const pmpe_kv_cache *cache, const pmpe_kv_sequences *s
  * more).  A sequence that sees nothing gives out = 0, lse = -inf.  What the
  * cache holds at positions that are not seen, NaN say, does not matter.  The
  * order of the sums goes by the lengths of all sequences of the call, so the same
- * call gives the same bits.  With 8 bits a value whose scale is below 2^-24 of
- * the largest seen loses bits. */
+ * call gives the same bits.  With 8 bits a value loses bits where its scale times
+ * its weight is below 2^-20 of the largest scale, and an element of q where it is
+ * below 2^-31 of the largest of its head. */
 typedef struct pmpe_kv_attend_desc {
     int heads;             /* a multiple of kv_heads, at most 65535 */
     int type;              /* of q and out: the cache's; over 8 bits PMPE_BF16 or PMPE_F16 */

@@ -631,7 +631,10 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
         const int b = at.b, head = at.head, block = at.block, tile = at.tile, tiles = at.s.tiles;
         fresh = at.advance(p);
         if (!fresh && t + 1 < left) continue;
-        if (lost) l[0][0] = l[0][1] = m[0][0] = m[0][1] = NAN;
+        if (lost) {
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt) l[nt][0] = l[nt][1] = m[nt][0] = m[nt][1] = NAN;
+        }
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll

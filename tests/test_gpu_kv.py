@@ -527,6 +527,9 @@ def test_refusals_on_the_gpu(pmpe):
             print("not refused:", i)
     with pytest.raises(TypeError):
         c.attend(q, table, n, scale="x")
+    rows = c.read(table[:0], n[:0], cu_seqlens=cu[:1], rows=3)  # rows of no sequence
+    assert rows[0].shape == (3, 2, 64) and not rows[0].any() and not rows[1].any()
+    c.append(k, k, table[:0], n[:0], cu_seqlens=cu[:1])
     empty = c.attend(q[:0], table[:0], n[:0])
     assert empty.out.shape == (0, 4, 64) and empty.lse.shape == (0, 4)
     v = c.k._version
