@@ -3,12 +3,20 @@
 //   s_p = scale q . k_p,   out = sum_p e^(s_p - m) v_p / sum_p e^(s_p - m),   lse = m + ln sum_p e^(s_p - m)
 //
 // in one pass over the cache with the running maximum m.  The cache's bytes
-// bound it: of a key and its value (512 bytes with 128 columns of 16 bits)
-// every query head of a group takes 512 operations, 8 an octet of heads and
-// byte, a tenth of what mma.sync gives at the rate of DRAM.  (tcgen05 would
-// hold 128 keys by eight heads in TMEM; there is no product here whose time
-// shows.)  So each warp works by itself: it copies 16 keys and their values
-// into a ring of its own, asynchronously, and no barrier stands between tiles.
+// bound it (64 sequences of up to 8192 positions, 32 over 4 heads of 128, 538 MB
+// of BF16: 87.8 us, 6.1 TB/s; 131072 positions of one sequence 49.5 us; in e4m3
+// the 278 MB 58 us).  Of a key and its value (512 bytes in 16 bits) every query
+// head of a group takes 512 operations: mma.sync is busy an eighth of the time
+// (a fifth in e4m3).  tcgen05 would hold 128 keys by eight heads in TMEM and
+// read them back for the maximum; no product here is long enough to show.
+//
+// Each warp works by itself, so that no barrier stands between tiles: it copies
+// 16 keys and their values (32 of narrow ones) ahead into a ring of its own, by
+// TMA where 16 positions lie one after another in a page (pages of a multiple of
+// 16), by 16-byte copies of each row otherwise.  (The copies alone take 81 us of
+// the 87.8, with the ones of each row 95.)  The more warps an SM has, the less
+// each one's chain of dependent steps shows: 12 or 16 of them with two or three
+// stages each; 8 with three took 107 us, and 97 in e4m3.
 //
 //   S^T = K Q^T    16 keys by 8 heads: keys are the rows, so that a group of up
 //                  to eight heads fills the tile; FP32
@@ -18,11 +26,13 @@
 //                  S, a value's scale its weight, over the largest scale so far
 //                  (a power of two) to stay inside FP16
 //
-// Work is cut by length, not by sequence: tiles of 64 positions of all
-// (sequence, key head) pairs in a row, an equal run of them for each CTA (two
-// an SM), whose bounds each CTA derives from the lengths on the device.  A pair
-// that one CTA holds whole is finished there; of the others each CTA leaves its
-// sums (FP32) in the workspace, and a second launch joins them in order.
+// Work is cut by length, not by sequence: tiles of 64 or 128 positions of all
+// (sequence, block of heads) pairs in a row, an equal run of them for each CTA,
+// whose bounds each CTA derives from the lengths on the device.  A pair that one
+// CTA holds whole is finished there; of the others each CTA leaves its sums
+// (FP32) in the workspace, and a second launch joins them in order.  That launch
+// costs 2 to 5 us; sums joined by the last CTA of a pair would need counters that
+// are zero before the call.
 #include <algorithm>
 
 #include "kv_cache.cuh"

@@ -9,7 +9,10 @@
 // sequence by a search over the offsets, the page by the table: a chain of
 // loads) is found for all of them at once, a thread a row, while the first rows
 // are on the way; then the groups go through the rows' heads, the next ones'
-// loads ahead.  Bytes bound both directions.
+// loads ahead.  Bytes bound the way back (65533 positions of 4 heads of 128 out
+// of e4m3, 203 MB: 37.5 us, 5.4 TB/s); into e4m3 instructions do (16377 rows, 51
+// MB: 16.0 us; 180 a warp and two heads, of which 16 for the products by the
+// two-word reciprocal).
 #include <string.h>
 
 #include <algorithm>
@@ -20,6 +23,8 @@
 namespace pmpe {
 namespace {
 
+// Two heads on the way for each group at 4 CTAs an SM took 16.0 and 51 us for the
+// two, four without the CTAs' runs of rows 22 and 39.
 constexpr int kThreads = 256, kCtas = 8;  // kCtas: of an SM
 constexpr int kMaxRowsOfCta = 512;
 
