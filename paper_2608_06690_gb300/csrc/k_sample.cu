@@ -191,16 +191,8 @@ template <typename F> __device__ float lowest(float top, F in)
     }
     return logit_of(at);
 }
-// Whether r is at least min_p, 2^-40 < min_p < 1.
-__device__ __forceinline__ bool at_least(const Slope &s, float z, float min_p, const Power *powers)
-{
-    const Ratio x = x_of(s, z);
-    if (!(x.hi <= kLeast + 1.f)) return false;
-    int n;
-    const uint32_t w = power_of(x, powers, n), m = (__float_as_uint(min_p) & 0x7fffffu) | 0x800000u;
-    const int sh = 31 + n - (150 - (int)(__float_as_uint(min_p) >> 23));  // r >= min_p: w >= m 2^sh
-    return sh > 8 ? false : sh >= 0 ? w >= (uint64_t)m << sh : sh < -31 || (uint64_t)w << -sh >= m;
-}
+// Whether x <= (hi, lo).  (Not of infinities.)
+__device__ __forceinline__ bool within(const Ratio &x, float hi, float lo) { return (x.hi - hi) + (x.lo - lo) <= 0.f; }
 
 // Two values to an instruction.
 struct Two {
@@ -1080,13 +1072,17 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
     // the smallest is not
     const float far = x_near(m.slope, least_of);
     if (warp == 0) {
-        const float f0 = far < kLeast - 1.f ? -kFltMax : lowest(top, [&](float z) {
-            const Ratio x = x_of(m.slope, z);
-            return (x.hi - kLeast) + x.lo <= 0.f;  // (not of infinities)
-        });
+        const float f0 = far < kLeast - 1.f ? -kFltMax : lowest(top, [&](float z) { return within(x_of(m.slope, z), kLeast, 0.f); });
         if (lane == 0) s.floors[0] = f0;
     } else if (warp == 1) {
-        const float f1 = !(min_p > 0x1p-40f) ? -kFltMax : min_p >= 1.f ? top : lowest(top, [&](float z) { return at_least(m.slope, z, min_p, s.powers); });
+        float f1 = -kFltMax;
+        if (min_p >= 1.f) {
+            f1 = top;
+        } else if (min_p > 0x1p-40f) {  // x's own limit, in two words: as near as x is, nearer than r
+            const double x = -log2((double)min_p);
+            const float hi = (float)x, lo = (float)(x - hi);
+            f1 = lowest(top, [&](float z) { return within(x_of(m.slope, z), hi, lo); });
+        }
         if (lane == 0) s.floors[1] = f1;
     }
     m.slope.bins = (float)(kBins - 2) / fminf(fmaxf(far, 0x1p-60f), kLeast + 1.f);  // (a NaN or infinity: 41)
