@@ -10,9 +10,8 @@
 // loads) is found for all of them at once, a thread a row, while the first rows
 // are on the way; then the groups go through the rows' heads, the next ones'
 // loads ahead.  Bytes bound the way back (65533 positions of 4 heads of 128 out
-// of e4m3, 203 MB: 37.5 us, 5.4 TB/s); into e4m3 instructions do (16377 rows, 51
-// MB: 16.0 us; 180 a warp and two heads, of which 16 for the products by the
-// two-word reciprocal).
+// of e4m3, 203 MB: 37.5 us, 5.4 TB/s); into e4m3 instructions count as much (16377
+// rows, 51 MB: 13.4 us, 3.8 TB/s), so that a lane takes 16 elements there.
 #include <string.h>
 
 #include <algorithm>
@@ -23,9 +22,11 @@
 namespace pmpe {
 namespace {
 
-// Two heads on the way for each group at 4 CTAs an SM took 16.0 and 51 us for the
-// two, four without the CTAs' runs of rows 22 and 39.
-constexpr int kThreads = 256, kCtas = 8;  // kCtas: of an SM
+// CTAs of an SM.  8 bits back: eight with a head on the way for each group 37.5
+// us, four with two 51.  Into 8 bits with 16 elements a lane: four 13.4 us, eight
+// (32 registers) 16.9; with eight elements a lane 16.0.
+constexpr int kThreads = 256;
+constexpr int ctas_of_sm(int wide) { return wide == 2 ? 4 : 8; }
 constexpr int kMaxRowsOfCta = 512;
 
 struct CacheParams {
@@ -67,10 +68,10 @@ struct Item {
     bool is_v, live;
 };
 
-// kBack: out of the cache.  kLanes: of a head, 8 elements each.  T: the rows'
-// type, C: the cache's (uint8_t: e4m3).  kVec: whole vectors.
-template <typename T, typename C, int kLanes, bool kVec, bool kBack>
-__global__ void __launch_bounds__(kThreads, kCtas) cache_kernel(const __grid_constant__ CacheParams p)
+// kBack: out of the cache.  kLanes: of a head, 8 kWide elements each.  T: the
+// rows' type, C: the cache's (uint8_t: e4m3).  kVec: whole vectors.
+template <typename T, typename C, int kLanes, bool kVec, bool kBack, int kWide>
+__global__ void __launch_bounds__(kThreads, ctas_of_sm(kWide)) cache_kernel(const __grid_constant__ CacheParams p)
 {
     constexpr int kGroups = kThreads / kLanes;
     constexpr bool k8 = sizeof(C) == 1;
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) cache_kernel(const __grid_con
     pdl_trigger();
     pdl_wait();
     const int D = p.kv.head_dim, r0 = blockIdx.x * p.rows, rows = min(p.rows, p.T - r0), h0 = blockIdx.y * p.heads, items = rows * p.heads;
-    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, c = 8 * lane;
+    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, c = 8 * kWide * lane;
     auto item = [&](int n) {
         Item it;
         it.row = p.by_heads.quotient(n);
@@ -90,7 +91,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) cache_kernel(const __grid_con
     };
     // an item's eight elements, and what scales them, as they lie in memory
     struct Loaded {
-        typename std::conditional<kBack && k8, uint2, Raw8<typename std::conditional<kBack, typename std::conditional<k8, float, C>::type, T>::type>>::type raw;
+        typename std::conditional<kBack && k8, uint2, Raw8<typename std::conditional<kBack, typename std::conditional<k8, float, C>::type, T>::type>>::type raw[kWide];
         float scale;
     };
     auto fetch = [&](int n, Loaded &l) {
@@ -100,8 +101,13 @@ __global__ void __launch_bounds__(kThreads, kCtas) cache_kernel(const __grid_con
         if constexpr (!kBack) {
             const T *src = it.is_v ? (const T *)p.v + (r0 + it.row) * p.v_ld + it.head * p.v_head_ld
                                    : (const T *)p.k + (r0 + it.row) * p.k_ld + it.head * p.k_head_ld;
-            if (kVec) {
-                load8<true>(l.raw, src + c, 8);
+            if (kVec && kWide == 2 && sizeof(T) == 2) {  // 32 bytes at once
+                Raw8<float> both;
+                load8<true>(both, (const float *)(src + c), 8);
+                memcpy(&l.raw, &both, sizeof(l.raw));
+            } else if (kVec) {
+#pragma unroll
+                for (int w = 0; w < kWide; ++w) load8<true>(l.raw[w], src + c + 8 * w, 8);
             } else {
                 T v[8];
 #pragma unroll
@@ -113,10 +119,10 @@ __global__ void __launch_bounds__(kThreads, kCtas) cache_kernel(const __grid_con
             if (e0 < 0) return;
             const C *at = (const C *)(it.is_v ? p.kv.v : p.kv.k) + e * D + c;
             if constexpr (k8) {
-                l.raw = *reinterpret_cast<const uint2 *>(at);
+                l.raw[0] = *reinterpret_cast<const uint2 *>(at);
                 l.scale = (it.is_v ? p.kv.v_scale : p.kv.k_scale)[e];
             } else {
-                load8<true>(l.raw, at, 8);
+                load8<true>(l.raw[0], at, 8);
             }
         }
     };
@@ -128,35 +134,48 @@ __global__ void __launch_bounds__(kThreads, kCtas) cache_kernel(const __grid_con
     for (int n = group; n - group < items; n += kGroups) {
         fetch(n + kGroups, next);
         const Item it = item(n);
-        float x[8];
         if constexpr (!kBack) {
-            unpack(now.raw, x);
+            float x[kWide][8];
+#pragma unroll
+            for (int w = 0; w < kWide; ++w) unpack(now.raw[w], x[w]);
             const long long e0 = it.live ? s_entry[it.row] : -1, e = e0 + (long long)it.head * p.kv.page_size;
             C *at = (C *)(it.is_v ? p.kv.v : p.kv.k) + e * D + c;
             if constexpr (k8) {
                 float amax = 0.f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) amax = max_magnitude(amax, x[j]);
+                for (int w = 0; w < kWide; ++w)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) amax = max_magnitude(amax, x[w][j]);
 #pragma unroll
                 for (int off = kLanes / 2; off > 0; off >>= 1) amax = max_magnitude(amax, __shfl_xor_sync(~0u, amax, off));
                 float s;
                 const Divide by = divide_by(amax, 1.f, s);
                 if (e0 >= 0) {
                     if (lane == 0) (it.is_v ? p.kv.v_scale : p.kv.k_scale)[e] = s;
-                    float q[8];
+                    uint32_t q[2 * kWide];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) q[j] = fmaf(x[j], by.hi, x[j] * by.lo);
-                    *reinterpret_cast<uint2 *>(at) =
-                        make_uint2(e4m3x2(q[0], q[1]) | e4m3x2(q[2], q[3]) << 16, e4m3x2(q[4], q[5]) | e4m3x2(q[6], q[7]) << 16);
+                    for (int w = 0; w < kWide; ++w)
+#pragma unroll
+                        for (int j = 0; j < 8; j += 4) {
+                            float y[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) y[k] = fmaf(x[w][j + k], by.hi, x[w][j + k] * by.lo);
+                            q[2 * w + j / 4] = e4m3x2(y[0], y[1]) | e4m3x2(y[2], y[3]) << 16;
+                        }
+                    if constexpr (kWide == 2)
+                        *reinterpret_cast<uint4 *>(at) = make_uint4(q[0], q[1], q[2], q[3]);
+                    else
+                        *reinterpret_cast<uint2 *>(at) = make_uint2(q[0], q[1]);
                 }
             } else {
-                if (e0 >= 0) store8<true>(at, x, 8);
+                if (e0 >= 0) store8<true>(at, x[0], 8);
             }
         } else {
+            float x[8];
             if constexpr (k8) {
                 uint32_t h[4];
-                e4m3x4_to_f16(now.raw.x, h[0], h[1]);
-                e4m3x4_to_f16(now.raw.y, h[2], h[3]);
+                e4m3x4_to_f16(now.raw[0].x, h[0], h[1]);
+                e4m3x4_to_f16(now.raw[0].y, h[2], h[3]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[j]));
@@ -164,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) cache_kernel(const __grid_con
                     x[2 * j + 1] = f.y * now.scale;
                 }
             } else {
-                unpack(now.raw, x);
+                unpack(now.raw[0], x);
             }
             if (it.live) {
                 T *to = (T *)(it.is_v ? p.v_out : p.k_out) + ((long long)(r0 + it.row) * p.kv.kv_heads + it.head) * D + c;
@@ -180,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) cache_kernel(const __grid_con
     }
 }
 
-template <typename T, typename C, int kLanes, bool kVec, bool kBack> cudaError_t launch_l(CacheParams &p, cudaStream_t st)
+template <typename T, typename C, int kLanes, bool kVec, bool kBack, int kWide = 1> cudaError_t launch_l(CacheParams &p, cudaStream_t st)
 {
     // rows of a CTA: as many as fill its groups once, or more, so that the CTAs
     // of 152 SMs take all rows at once
@@ -188,20 +207,25 @@ template <typename T, typename C, int kLanes, bool kVec, bool kBack> cudaError_t
     const int all = 2 * p.kv.kv_heads;
     p.heads = std::min(all, kGroups);
     const int parts = (all + p.heads - 1) / p.heads;
-    const long long share = ((long long)p.T * parts + kCtas * 152 - 1) / (kCtas * 152);
+    const long long ctas = 152 * ctas_of_sm(kWide), share = ((long long)p.T * parts + ctas - 1) / ctas;
     p.rows = (int)std::min<long long>(std::max<long long>(kGroups / p.heads, share), kMaxRowsOfCta);
     p.by_heads = FastDiv(p.heads);
-    return launch_pdl(cache_kernel<T, C, kLanes, kVec, kBack>, dim3((p.T + p.rows - 1) / p.rows, parts), dim3(kThreads), 0, st, p);
+    return launch_pdl(cache_kernel<T, C, kLanes, kVec, kBack, kWide>, dim3((p.T + p.rows - 1) / p.rows, parts), dim3(kThreads), 0, st, p);
 }
-template <typename T, typename C, bool kBack> cudaError_t launch_tc(CacheParams &p, bool vec, cudaStream_t st)
+// vec: 0 single elements, 1 vectors of eight, 2 pairs of those.
+template <typename T, typename C, bool kBack> cudaError_t launch_tc(CacheParams &p, int vec, cudaStream_t st)
 {
     const int lanes = (p.kv.head_dim + 7) / 8;
-    if (!vec) return launch_l<T, C, 32, false, kBack>(p, st);
+    if (vec == 0) return launch_l<T, C, 32, false, kBack>(p, st);
+    if constexpr (!kBack && sizeof(C) == 1) {
+        // into 8 bits, where instructions bound it, 16 elements a lane
+        if (vec == 2) return lanes <= 16 ? launch_l<T, C, 8, true, kBack, 2>(p, st) : launch_l<T, C, 16, true, kBack, 2>(p, st);
+    }
     if (lanes <= 8) return launch_l<T, C, 8, true, kBack>(p, st);
     if (lanes <= 16) return launch_l<T, C, 16, true, kBack>(p, st);
     return launch_l<T, C, 32, true, kBack>(p, st);
 }
-template <bool kBack> cudaError_t launch_types(CacheParams p, int type, int cache_type, bool vec, cudaStream_t st)
+template <bool kBack> cudaError_t launch_types(CacheParams p, int type, int cache_type, int vec, cudaStream_t st)
 {
     auto by_cache = [&](auto t) {
         using T = decltype(t);
@@ -220,7 +244,9 @@ cudaError_t launch_kv_append(const pmpe_kv_cache &c, const pmpe_kv_sequences &s,
 {
     const CacheParams p = {KvView(c, s), d.k, d.v, nullptr, nullptr, d.k_ld, d.k_head_ld, d.v_ld, d.v_head_ld, d.T, 0, 0, FastDiv(1)};
     const bool f32 = d.type == PMPE_F32;
-    const bool vec = aligned8(d.k, f32) && aligned8(d.v, f32) && d.k_ld % 8 == 0 && d.v_ld % 8 == 0 && d.k_head_ld % 8 == 0 && d.v_head_ld % 8 == 0;
+    const int64_t ld = d.k_ld | d.v_ld | d.k_head_ld | d.v_head_ld;
+    int vec = aligned8(d.k, f32) && aligned8(d.v, f32) && ld % 8 == 0;
+    if (vec && (f32 || (((uintptr_t)d.k | (uintptr_t)d.v) % 32 == 0 && ld % 16 == 0))) vec = 2;
     return launch_types<false>(p, d.type, c.type, vec, st);
 }
 
