@@ -663,6 +663,73 @@ template <typename T> struct Sampler {
         for (g += lane; g < (warp + 1) * kRuns; g += 32) s.seg[g] = 0;
         __syncthreads();
     }
+    // The runs' sums of r of the tokens from `above` on, the ones below `least` left
+    // out; those from `from` on and below `above` go into the list.  Where a fifth
+    // of the tokens is from `from` on, nearly every warp's load has one: they are
+    // packed together in a queue of the warp's before r is evaluated, 64 at a time.
+    __device__ __forceinline__ void sum_runs_above(float from, float above, float least) const
+    {
+        constexpr int kStep = 32 * kChunk<T>, kRuns = kSegs / kWarps;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seg = run_length();
+        const int begin = lo + warp * kRuns * seg, finish = min(hi, begin + kRuns * seg);
+        float *q_z = (float *)(s.mass_lo + warp * (kBins / kWarps));  // (the histogram's place: 128 of each)
+        int *q_id = (int *)(s.mass_hi + warp * (kBins / kWarps)), queued = 0;
+        int g = warp * kRuns, left = seg;
+        u64 sum = 0;
+        auto evaluate = [&](int n) {  // of the queue's first n <= 64
+            __syncwarp();
+            u64 w[2];
+            const float z0 = q_z[lane], z1 = q_z[lane + 32];
+            weights_of(slope, z0, z1, lane < n, lane + 32 < n, s.powers, w[0], w[1]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float z = k ? z1 : z0;
+                if (lane + 32 * k >= n) continue;
+                if (z < above) list(z, q_id[lane + 32 * k], w[k]);
+                else if (z >= least) sum += w[k];
+            }
+            __syncwarp();
+        };
+        uint4 next = make_uint4(0, 0, 0, 0);
+        if (begin < finish) next = fetch(begin + lane * kChunk<T>, hi);
+#pragma unroll 1
+        for (int i = begin; i < finish; i += kStep) {
+            const uint4 now = next;
+            if (i + kStep < finish) next = fetch(i + kStep + lane * kChunk<T>, hi);
+            float v[kChunk<T>];
+            spread(now, v);
+#pragma unroll
+            for (int j = 0; j < kChunk<T>; ++j) {
+                const uint32_t in = __ballot_sync(~0u, v[j] >= from);
+                if (v[j] >= from) {
+                    const int at = queued + __popc(in & ((1u << lane) - 1));
+                    q_z[at] = v[j];
+                    q_id[at] = i + lane * kChunk<T> + j;
+                }
+                queued += __popc(in);
+                if (queued >= 64) {
+                    evaluate(64);
+                    queued -= 64;
+                    const float z = q_z[64 + lane];
+                    const int id = q_id[64 + lane];
+                    if (lane < queued) q_z[lane] = z, q_id[lane] = id;
+                    __syncwarp();
+                }
+            }
+            left -= kStep;
+            if (left == 0 || i + kStep >= finish) {
+                evaluate(queued);
+                queued = 0;
+                sum = warp_sum(sum);
+                if (lane == 0) s.seg[g] = sum;
+                ++g;
+                sum = 0;
+                left = seg;
+            }
+        }
+        for (g += lane; g < (warp + 1) * kRuns; g += 32) s.seg[g] = 0;
+        __syncthreads();
+    }
     // The first id whose running sum is above target(sum of all), with the runs'
     // sums in s.seg and one(z, id) of single tokens; -1 for none.  The same in
     // every CTA.
@@ -907,23 +974,13 @@ template <typename T> struct Sampler {
                 if (!crossing_x(turn == 1, want, bin, mass, count)) continue;
                 // that bin's tokens into the list; the sums of what lies above it
                 if (threadIdx.x == 0) s.listed = 0;
+                const int warp = threadIdx.x >> 5;
+                if (warp < 2) {  // the lowest logit of the bin, and the lowest above it
+                    const float to = (float)(int)(bin + 1 - warp), z = to > 0.f ? lowest(slope.top, [&](float v) { return place_of(v) < to; }) : INFINITY;
+                    if ((threadIdx.x & 31) == 0) s.floors[warp] = z;
+                }
                 __syncthreads();
-                const float from = (float)bin, to = (float)(bin + 1);
-                sum_runs([&](const float (&v)[kChunk<T>], int i) {
-                    u64 run = 0;
-#pragma unroll
-                    for (int j = 0; j < kChunk<T>; j += 2) {
-                        const float a = v[j], b = v[j + 1], x0 = place_of(a), x1 = place_of(b);
-                        const bool in0 = a >= floor && x0 < to, in1 = b >= floor && x1 < to;
-                        if (!(in0 || in1)) continue;
-                        u64 w0, w1;
-                        weights_of(slope, a, b, in0, in1, s.powers, w0, w1);
-                        if (in0 && x0 >= from) list(a, i + j, w0), w0 = 0;
-                        if (in1 && x1 >= from) list(b, i + j + 1, w1), w1 = 0;
-                        run += (a >= least ? w0 : 0) + (b >= least ? w1 : 0);
-                    }
-                    return run;
-                });
+                sum_runs_above(fmaxf(s.floors[0], floor), s.floors[1], least);
                 share(2, s.listed);
                 all_meet();
                 summed = gather();
