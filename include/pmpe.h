@@ -538,8 +538,8 @@ typedef struct pmpe_kv_cache {
 
 /* The sequences of a call.  Position p of sequence b lies in page
  * table[b][p / page_size], place p % page_size.  A sequence holds lengths[b]
- * positions, those of the call included; a length is taken as between 0 and
- * table_width * page_size.  A table entry outside [0, pages) is no page: its
+ * positions, those of the call included; the attention takes a length as between
+ * 0 and table_width * page_size.  A table entry outside [0, pages) is no page: its
  * positions are not written, read as zeros and not attended.  Entries that no
  * position below the length needs are not read. */
 typedef struct pmpe_kv_sequences {
@@ -616,8 +616,10 @@ PMPE_API int pmpe_kv_attend(const pmpe_kv_cache *cache, const pmpe_kv_sequences 
  * A temperature that is not above 0 takes the largest logit (equal ones by the
  * lower id) with probability 1.  u outside [0, 1) counts as its nearest end, NaN
  * as 0; a top_p of NaN as 0.  A row without a token to draw gives -1 and 0.
- * r is evaluated within 2^-31, relative, and sums of r are exact: where that
- * leaves open which side of a border a token is on, either may be taken. */
+ * r is evaluated within 2^-31, relative, and rounded to a multiple of 2^-(63 - l)
+ * with l = ceil(log2 V), 3 at least (of 2^-46 for 131072 tokens); sums are exact:
+ * where that leaves open which side of a border a token is on, either may be
+ * taken. */
 typedef struct pmpe_sample_desc {
     int T, V;              /* rows >= 0, tokens 1 .. PMPE_MAX_VOCABULARY */
     int logits_type;       /* PMPE_F32, PMPE_BF16, PMPE_F16 */

@@ -9,7 +9,8 @@
 // A token is an integer, so that sums that differ in their last bits would give
 // another one now and then.  Therefore r is evaluated to 2^-31 (not FP32's
 // 2^-22; FP64 has a sixty-fourth of its rate here) and held as an integer of
-// 2^-46 of the best: sums of integers do not depend on their order.
+// 2^-46 of the best (finer in short rows): sums of integers do not depend on
+// their order.
 //
 //   x = (z_max - z) log2(e) / temperature  in two words, x = k / 256 + f
 //   r = 2^-x = 2^(-k / 256) (1 + q(f)),    the power from a table (Tang 1989),
@@ -54,7 +55,7 @@ constexpr int kMaxCluster = 8;
 constexpr int kSegs = 8 * kWarps;    // runs of ids whose sums a CTA keeps
 constexpr int kBins = 2048;          // of a histogram
 constexpr float kLeast = 40.f;       // log2 of the smallest r, negated
-constexpr int kFine = 46;            // bits of r behind the point
+constexpr int kFine = 46;            // bits of r behind the point, for 2^17 tokens
 constexpr int kList = 2048;          // tokens of a list
 constexpr int kShort = 384;          // of one that each token is compared with all of
 constexpr int kWanted = 1024;        // top_k up to which threads' largest logits show the border
@@ -168,13 +169,16 @@ __device__ __forceinline__ uint32_t power_of(const Ratio &x, const Power *powers
     n = k >> 8;
     return p.fixed + __float2int_rn(p.value * q);
 }
-// r as the sums take it.
+// r as the sums take it, of a row of up to 2^17 tokens a multiple of 2^-46 or finer:
+// rounded to nearest, so that what small ones lose has no direction.  (Cut off,
+// 16000 tokens together lost what one of 2^-33 of the sum weighs, and with the
+// logits in descending order u = 1 - 2^-24 drew a neighbour.)
 __device__ __forceinline__ u64 weight_of(const Slope &s, float z, const Power *powers)
 {
     int n;
     const uint32_t w = power_of(x_of(s, z), powers, n);
     n += s.shift - (kFine - 31);
-    return n <= 0 ? (u64)w << -n : (u64)(w >> n);
+    return n <= 0 ? (u64)w << -n : (u64)((w + ((1u << n) >> 1)) >> n);
 }
 // The smallest logit for which `in` holds, as it does for the largest and does
 // not again further down, by 32 tries at a time; the same in every lane.
@@ -249,7 +253,8 @@ __device__ __forceinline__ void weights_of(const Slope &s, float z0, float z1, b
         const uint32_t v = p.fixed + __float2int_rn(p.value * qs[i]);
         const bool in = i ? in1 : in0;
         const int down = in ? (bits >> 8) - (0x4b400000 >> 8) + s.shift - (kFine - 31) : 0;  // v 2^-down
-        w[i] = (u64)(v >> max(down, 0)) * (in ? 1u << max(-down, 0) : 0u);
+        const int by = max(down, 0);
+        w[i] = (u64)((v + ((1u << by) >> 1)) >> by) * (in ? 1u << max(-down, 0) : 0u);
     }
     w0 = w[0];
     w1 = w[1];
@@ -853,7 +858,7 @@ template <typename T> struct Sampler {
         p.token[t] = id - head;
         int n;  // (r itself: of small ones the sums take few bits)
         const uint32_t w = power_of(x_of(slope, clip(to_f32<T>(z[id]))), s.powers, n);
-        p.prob[t] = (float)w * __int_as_float((127 - n) << 23) * (float)(1 << (kFine - 31)) / ((float)all * (float)(1 << slope.shift));
+        p.prob[t] = (float)w * __int_as_float((127 - n + kFine - 31 - slope.shift) << 23) / (float)all;
     }
     // floor(sum f) for 0 <= f < 1 (above: as the largest such), or its ceiling.
     static __device__ __forceinline__ u64 share_of(u64 sum, float f, bool up)
@@ -1202,3 +1207,5 @@ cudaError_t launch_sample(const pmpe_sample_desc &d, int num_sms, cudaStream_t s
 }
 
 }  // namespace pmpe
+    // as fine as sums of V tokens below 2^63 allow; a weight's shift to the left stays below 32
+    p.shift = -14;

@@ -747,8 +747,8 @@ class KvCache:
     lies in page table[b, p // page_size]; rows of any pitch), and ``lengths``,
     int32 [B]: the positions that each holds, those of the call included.  Which
     pages are whose is the caller's business; an entry outside [0, pages) is no
-    page: its positions are not written, read as zeros and not attended, and
-    lengths are taken as between 0 and width * page_size."""
+    page: its positions are not written, read as zeros and not attended.  Nor are
+    positions below 0 or past width * page_size.  Nothing here has a gradient."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         _ops.kv_cache(k, v, k_scale, v_scale)
@@ -828,7 +828,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=Non
     The token drawn is the lowest kept id whose cumulative probability, by id, is
     above u: the same u gives the same token, whatever stands in the other rows.
     Logits of -inf and NaN are never drawn, nor is what has less than 2^-40 of the
-    best token's probability.  V up to 2^21."""
+    best token's probability.  V up to 2^21.  No gradient."""
     if stream is not None:
         return _on(stream, sample, logits, logits, u, temperature, top_k, top_p, min_p)
     return _ops.sample(logits, u, temperature, top_k, top_p, min_p)

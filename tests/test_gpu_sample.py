@@ -1,6 +1,6 @@
-"""Sampling against a 64-bit reference.  Tokens are equal: r is within 2^-31 and
-its sums are exact, so that a border would have to lie that near to a draw (the
-seeds are fixed).  prob: r and the sum are rounded to FP32, and their quotient:
+"""Sampling against a 64-bit reference.  Tokens are equal: r is within 2^-31, its
+sums of multiples of 2^-46 or finer, so that a border would have to lie that near
+to a draw (the seeds are fixed).  prob: r and the sum are rounded to FP32, and their quotient:
 three half steps, and a tenth of one for r."""
 import math
 
@@ -102,6 +102,29 @@ def test_the_ends_of_u(pmpe, dtype):
     u = torch.tensor([0.0, 1 - 2.0 ** -24, 2.0 ** -24, 1e-30, 1e-45, 0.5, 0.25, 2.0 ** -100])
     for kw in SETTINGS:
         check(pmpe, z, u, **kw)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("descending", [True, False])
+def test_sorted_logits(pmpe, dtype, descending):
+    """The draw lies among the smallest tokens, whose sum R is 2^-24 of all, S, and of which one is about
+    2^-31.  Of 16491 tokens r is rounded to a multiple of 2^-48: up to 2^-49 each, n of them below the
+    border, and 2^-31 of r.  The border itself, 2^-24 S, is off by 2^-24 (2^-31 S + V 2^-49)."""
+    T, V, low = 48, 16491, 2.0 ** -24
+    z = torch.sort(randn((T, V), 6, F32, 5.0), dim=1, descending=descending).values.to(dtype)
+    u = torch.full((T,), 1 - low if descending else low)
+    rows = np.sort(z.double().cpu().numpy(), axis=1)  # the smallest first
+    for kw in SETTINGS[:2]:
+        s = pmpe.sample(z, u.cuda(), **kw)
+        for t, token in enumerate(s.token.tolist()):
+            r = np.exp((rows[t] - rows[t, -1]) / np.float64(np.float32(kw.get("temperature", 1.0))))
+            r[r < 2.0 ** -40] = 0
+            upto = np.cumsum(r)
+            at = V - 1 - token if descending else token
+            n, border = int((r[:at + 1] > 0).sum()), low * upto[-1]
+            off = n * 2.0 ** -49 + 2.0 ** -31 * upto[at] + low * (2.0 ** -31 * upto[-1] + V * 2.0 ** -49)
+            assert r[at] > 0 and off < r[at], (t, off, r[at])
+            assert upto[at] - r[at] - off <= border <= upto[at] + off, (t, token, border, upto[at], off)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
