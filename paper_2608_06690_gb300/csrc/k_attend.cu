@@ -469,8 +469,8 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[j][nt][i] = 0.f;
         }
-        if (!lost && !mbar_wait(barrier(stage), parity, &s_abort, nullptr)) {
-            lost = true;  // (a copy that does not end: what this warp holds becomes NaN)
+        if (!lost && __any_sync(~0u, !mbar_wait(barrier(stage), parity, &s_abort, nullptr))) {
+            lost = true;  // (a copy that does not end: what this warp, all lanes of it, holds becomes NaN)
             to_copy = 0;
         }
         __syncwarp();

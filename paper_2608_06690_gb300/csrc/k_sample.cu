@@ -759,7 +759,7 @@ template <typename T> struct Sampler {
         if (warp == 0 && all > 0 && before <= want && want < before + s.total[0][rank]) {
             // 32 runs at a time, then 32 tokens
             int g = 0;
-            for (;; g += 32) {
+            for (; g < kSegs; g += 32) {
                 u64 sum = g + lane < kSegs ? s.seg[g + lane] : 0;
                 for (int off = 1; off < 32; off <<= 1) {
                     const u64 o = __shfl_up_sync(~0u, sum, off);
@@ -775,7 +775,8 @@ template <typename T> struct Sampler {
                 before += __shfl_sync(~0u, sum, 31);
             }
             // (a load of each lane, then that lane's values one after another)
-            for (int i = lo + g * seg + lane * kChunk<T>;; i += 32 * kChunk<T>) {
+            for (int i0 = lo + g * seg; i0 < hi; i0 += 32 * kChunk<T>) {
+                const int i = i0 + lane * kChunk<T>;
                 float v[kChunk<T>];
                 u64 w[kChunk<T>], sum = 0;
                 load(i, hi, v);
@@ -855,6 +856,10 @@ template <typename T> struct Sampler {
 
     __device__ void answer(int t, int id, u64 all) const
     {
+        if (id < head) {  // (none: what stands for a row without a token)
+            p.token[t] = -1, p.prob[t] = 0.f;
+            return;
+        }
         p.token[t] = id - head;
         int n;  // (r itself: of small ones the sums take few bits)
         const uint32_t w = power_of(x_of(slope, clip(to_f32<T>(z[id]))), s.powers, n);
