@@ -18,10 +18,12 @@
 //
 // A cluster of CTAs takes a row, each a run of ids.  One pass finds the largest
 // logit.
-//   top_k up to 1024: every thread's largest logit, in a histogram over x, tells
-//     how far down the best top_k tokens reach at most, since each thread that
-//     shows one there holds one: k threads' tokens at most, nearly k where ids
-//     are random.  A second pass lists those, and one CTA finishes with the list.
+//   top_k up to 1024: the largest logits of every thread's four runs of loads, in
+//     a histogram over x, tell how far down the best top_k tokens reach at most,
+//     since each run that shows one there holds one: k runs' tokens at most,
+//     nearly k where ids are random.  A second pass lists those, and one CTA
+//     finishes with the list.  (With one a thread, top_k 1000 in rows of one CTA
+//     had no border and listed all: 400 rows of 32003 119 us, with four 61.)
 //   top_p alone, or a larger top_k: a second pass makes histograms of counts and
 //     sums over x; the bin where the border lies is listed in a third, which also
 //     sums what is above it by runs of ids; the border is found in the list.
@@ -30,11 +32,11 @@
 // further passes, over the bits of the logits in the border's bin, down to one
 // value.  Of equal logits at the border the lowest ids stay.
 //
-// Latency bounds a single row (131072 tokens, top_k 50, top_p 0.95: 13.5 us, the
-// largest logit and the list 5 and 3 of them), instructions many rows: r takes 36
-// a token, two tokens at a time (400 rows of 32003: 37 us; 64 rows of 131072
-// 22 us with top_k, 29 with neither, 75 with top_p over as many as a fifth of the
-// tokens).  A row's passes run a few times each, so that fetching their code
+// Latency bounds a single row (131072 tokens, top_k 50, top_p 0.95: 13.2 us, the
+// largest logit and the list 5 and 3 of them), instructions many rows: r takes 39
+// a token, two tokens at a time (400 rows of 32003: 37 us, of two CTAs each 58;
+// 64 rows of 131072 22 us with top_k, 29 with neither, 67 with top_p over as many
+// as a fifth of the tokens).  A row's passes run a few times each, so that fetching their code
 // counts: they are not unrolled, and what is seldom needed is out of line.
 #include <string.h>
 
@@ -58,7 +60,7 @@ constexpr float kLeast = 40.f;       // log2 of the smallest r, negated
 constexpr int kFine = 46;            // bits of r behind the point, for 2^17 tokens
 constexpr int kList = 2048;          // tokens of a list
 constexpr int kShort = 384;          // of one that each token is compared with all of
-constexpr int kWanted = 1024;        // top_k up to which threads' largest logits show the border
+constexpr int kWanted = 1024;        // top_k up to which runs' largest logits show the border
 constexpr float kLog2eHi = 1.44269502f, kLog2eLo = 1.92596303e-8f;  // log2(e) in two words
 constexpr float kFltMax = 3.402823466e38f;
 
@@ -250,7 +252,6 @@ __device__ __forceinline__ void weights_of(const Slope &s, float z0, float z1, b
     for (int i = 0; i < 2; ++i) {
         const int bits = __float_as_int(k[i]);
         const Power p = powers[bits & 255];
-        const uint32_t v = p.fixed + __float2int_rn(p.value * qs[i]);
         const bool in = i ? in1 : in0;
         const int down = in ? (bits >> 8) - (0x4b400000 >> 8) + s.shift - (kFine - 31) : 0;  // v 2^-down
         const int by = max(down, 0);
@@ -1074,7 +1075,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 
     // ---- the largest logit, and the smallest
-    float mine = -INFINITY, least_of = INFINITY;  // of this thread (NaN is passed over)
+    float mine[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, least_of = INFINITY;  // of this thread's four runs of loads (NaN is passed over)
     for (int i = m.lo + threadIdx.x * kChunk<T>; i < m.hi; i += 4 * kThreads * kChunk<T>) {
         uint4 raw[4];  // four loads at a time, past the end the first again
 #pragma unroll
@@ -1088,12 +1089,14 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
             m.spread(raw[k], v);
 #pragma unroll
             for (int j = 0; j < kChunk<T>; ++j) {
-                mine = fmaxf(mine, v[j]);
+            float most = v[0];
+                most = fmaxf(most, v[j]);
                 least_of = fminf(least_of, v[j]);
             }
         }
     }
-    float top = mine;
+            if (i + k * kThreads * kChunk<T> < m.hi) mine[k] = fmaxf(mine[k], most);
+    float top = fmaxf(fmaxf(mine[0], mine[1]), fmaxf(mine[2], mine[3]));
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(~0u, top, off));
@@ -1158,10 +1161,12 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
     m.floor = s.floors[0];
     const float least = s.floors[1];
     if (top_k > 0 && top_k <= kWanted) {
-        // ---- how far down top_k tokens reach, by the threads' largest
+        // ---- how far down top_k tokens reach, by the runs' largest
         m.clear();
         if (threadIdx.x == 0) s.listed = 0;
-        if (mine >= m.floor) atomicAdd(&s.count[(int)m.place_of(mine)], 1u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (mine[k] >= m.floor) atomicAdd(&s.count[(int)m.place_of(mine[k])], 1u);
         m.all_meet();
         uint32_t c[kBins / kThreads] = {}, bin, bc;
         for (int r = 0; r < ranks; ++r) {
@@ -1170,19 +1175,26 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
         }
         u64 bm;
         const bool some = m.crossing([&](int) { return 0ull; }, [&](int b) { return b & 2 ? (b & 1 ? c[3] : c[2]) : (b & 1 ? c[1] : c[0]); }, false, (u64)top_k, bin, bm, bc);
-        const float lim = some ? (float)(bin + 1) : INFINITY;
-        // ---- their list
-        m.each([&](float v, int i) {
-            if (v >= m.floor && m.place_of(v) < lim) m.list(v, i, weight_of(m.slope, v, s.powers));
-        });
-        __syncthreads();
-        m.share(2, s.listed);
-        m.all_meet();
-        const bool fits = m.gather();
-        m.all_meet();  // the lists and their lengths have been read
-        if (fits) {
-            if (rank == 0) m.from_list(t, top_k, top_p, least, u);
-            return;
+        // Where fewer runs than top_k show a token the row has few, or top_k is
+        // more than there are runs: most show one then, and a list would not fit.
+        const bool few = some || p.V <= kList || 2 * m.cta_sum(c[0] + c[1] + c[2] + c[3]) < 4ull * ranks * kThreads;
+        if (few) {
+            const float lim = some ? (float)(bin + 1) : INFINITY;
+            // ---- their list
+            m.each([&](float v, int i) {
+                if (v >= m.floor && m.place_of(v) < lim) m.list(v, i, weight_of(m.slope, v, s.powers));
+            });
+            __syncthreads();
+            m.share(2, s.listed);
+            m.all_meet();
+            const bool fits = m.gather();
+            m.all_meet();  // the lists and their lengths have been read
+            if (fits) {
+                if (rank == 0) m.from_list(t, top_k, top_p, least, u);
+                return;
+            }
+        } else {
+            m.all_meet();  // the histograms have been read
         }
     }
     m.from_row(t, top_k, top_p, least, u);
@@ -1207,10 +1219,10 @@ cudaError_t launch_sample(const pmpe_sample_desc &d, int num_sms, cudaStream_t s
     SampleParams p = {d.logits, d.ld, d.u, d.temperatures, d.top_ps, d.min_ps, d.top_ks, d.temperature, d.top_p, d.min_p, d.top_k, d.T, d.V, 0, d.token, d.prob};
     while (p.shift < kFine && (int64_t)d.V > ((int64_t)1 << (63 - kFine + p.shift))) ++p.shift;
     if (d.logits_type == PMPE_F32) return launch_typed<float>(p, num_sms, st);
+    // as fine as sums of V tokens below 2^63 allow; a weight's shift to the left stays below 32
+    p.shift = -14;
     if (d.logits_type == PMPE_BF16) return launch_typed<bf16>(p, num_sms, st);
     return launch_typed<__half>(p, num_sms, st);
 }
 
 }  // namespace pmpe
-    // as fine as sums of V tokens below 2^63 allow; a weight's shift to the left stays below 32
-    p.shift = -14;

@@ -104,6 +104,19 @@ def test_the_ends_of_u(pmpe, dtype):
         check(pmpe, z, u, **kw)
 
 
+@pytest.mark.parametrize("T,V", [(3, 131072), (200, 2048), (200, 2049), (200, 9000)])
+def test_large_top_k(pmpe, T, V):
+    """As many as there are runs of loads, more, and less; rows of which a mask leaves about as many."""
+    g = torch.Generator().manual_seed(V)
+    z, u = randn((T, V), V, BF16, 2.0), rand(T, V + 1)
+    top_k = torch.tensor(np.random.default_rng(V).choice([400, 511, 512, 513, 800, 1000, 1023, 1024, 1025, 2047, 2048], T), dtype=torch.int32)
+    check(pmpe, z, u, top_k=top_k, top_p=0.98)
+    left = torch.tensor([1, 10, 300, 1000, 1024, 1500, 2500])[torch.arange(T) % 7]
+    z = z.masked_fill(torch.rand((T, V), generator=g).argsort(1).argsort(1).ge(left[:, None]).cuda(), -math.inf)
+    check(pmpe, z, u, top_k=top_k)
+    check(pmpe, z.sort(1).values, u, top_k=top_k, top_p=0.9)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("descending", [True, False])
 def test_sorted_logits(pmpe, dtype, descending):
