@@ -252,6 +252,7 @@ __device__ __forceinline__ void weights_of(const Slope &s, float z0, float z1, b
     for (int i = 0; i < 2; ++i) {
         const int bits = __float_as_int(k[i]);
         const Power p = powers[bits & 255];
+        const uint32_t v = p.fixed + __float2int_rn(p.value * qs[i]);
         const bool in = i ? in1 : in0;
         const int down = in ? (bits >> 8) - (0x4b400000 >> 8) + s.shift - (kFine - 31) : 0;  // v 2^-down
         const int by = max(down, 0);
@@ -1087,15 +1088,15 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
         for (int k = 0; k < 4; ++k) {
             float v[kChunk<T>];
             m.spread(raw[k], v);
+            float most = v[0];
 #pragma unroll
             for (int j = 0; j < kChunk<T>; ++j) {
-            float most = v[0];
                 most = fmaxf(most, v[j]);
                 least_of = fminf(least_of, v[j]);
             }
+            if (i + k * kThreads * kChunk<T> < m.hi) mine[k] = fmaxf(mine[k], most);
         }
     }
-            if (i + k * kThreads * kChunk<T> < m.hi) mine[k] = fmaxf(mine[k], most);
     float top = fmaxf(fmaxf(mine[0], mine[1]), fmaxf(mine[2], mine[3]));
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
@@ -1217,10 +1218,10 @@ template <typename T> cudaError_t launch_typed(const SampleParams &p, int num_sm
 cudaError_t launch_sample(const pmpe_sample_desc &d, int num_sms, cudaStream_t st)
 {
     SampleParams p = {d.logits, d.ld, d.u, d.temperatures, d.top_ps, d.min_ps, d.top_ks, d.temperature, d.top_p, d.min_p, d.top_k, d.T, d.V, 0, d.token, d.prob};
-    while (p.shift < kFine && (int64_t)d.V > ((int64_t)1 << (63 - kFine + p.shift))) ++p.shift;
-    if (d.logits_type == PMPE_F32) return launch_typed<float>(p, num_sms, st);
     // as fine as sums of V tokens below 2^63 allow; a weight's shift to the left stays below 32
     p.shift = -14;
+    while (p.shift < kFine && (int64_t)d.V > ((int64_t)1 << (63 - kFine + p.shift))) ++p.shift;
+    if (d.logits_type == PMPE_F32) return launch_typed<float>(p, num_sms, st);
     if (d.logits_type == PMPE_BF16) return launch_typed<bf16>(p, num_sms, st);
     return launch_typed<__half>(p, num_sms, st);
 }
