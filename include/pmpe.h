@@ -580,8 +580,8 @@ PMPE_API int pmpe_kv_read(const pmpe_kv_cache *cache, const pmpe_kv_sequences *s
  *   out = sum_p a_p v_p,  lse = ln sum_p exp(s_p)
  * for the last `window` positions (0: all).  Query head i uses the keys and
  * values of head i / (heads / kv_heads).  Products are exact in FP32, sums FP32;
- * a weight enters the sum over the values in two 16-bit words (16 bits or
- * more).  A sequence that sees nothing gives out = 0, lse = -inf.  What the
+ * a weight enters the sum over the values in three BF16 words, which hold FP32's
+ * 24 bits, or in two FP16 words.  A sequence that sees nothing gives out = 0, lse = -inf.  What the
  * cache holds at positions that are not seen, NaN say, does not matter.  The
  * order of the sums goes by the lengths of all sequences of the call, so the same
  * call gives the same bits.  With 8 bits a value loses bits where its scale times

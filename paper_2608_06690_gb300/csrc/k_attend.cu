@@ -20,8 +20,9 @@
 //
 //   S^T = K Q^T    16 keys by 8 heads: keys are the rows, so that a group of up
 //                  to eight heads fills the tile; FP32
-//   O^T += V^T P^T 16 columns by 8 heads; P in two 16-bit words (hi + lo), so
-//                  that its rounding (2^-17 or less) vanishes beside the output's
+//   O^T += V^T P^T 16 columns by 8 heads; P in three BF16 words, which hold all
+//                  24 bits of an FP32 weight, or in two FP16 words.  (Two words of
+//                  BF16, 2^-17 off, turned the rounding of one output in a thousand.)
 //   8 bits         e4m3 to FP16 is exact; a key's scale multiplies its row of
 //                  S, a value's scale its weight, over the largest scale so far
 //                  (a power of two) to stay inside FP16
@@ -275,6 +276,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     constexpr bool kQBf = kKind == kBf16 || kKind == kE4m3Bf16;
     using Q = typename std::conditional<kQBf, bf16, __half>::type;
     constexpr int kSteps = kDP / 16, kMT = S::kMT, kKeys = S::kKeys, kTile = S::kTile;
+    constexpr int kWords = kBf ? 3 : 2;  // of a weight: all of its 24 bits, or 22
     using Span = Span<kTile>;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Cost s_warp[kWarps];
@@ -585,7 +587,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                         for (int i = 0; i < 4; ++i) o[j][nt][i] *= f[i & 1];
                 }
             }
-            uint32_t hi[kMT][kNT][2], lo[kMT][kNT][2];
+            uint32_t pw[kMT][kNT][kWords][2];  // the weights' words, the largest first
 #pragma unroll
             for (int mt = 0; mt < kMT; ++mt) {
                 const float w0 = k8 ? v0[mt] * (kUp / r_max) : 1.f, w1 = k8 ? v1[mt] * (kUp / r_max) : 1.f;
@@ -600,12 +602,15 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                         if (k8) e[i] *= i < 2 ? w0 : w1;
                     }
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const uint32_t h = pack2<kBf>(e[2 * i], e[2 * i + 1]);
-                        const float2 back = unpack2<kBf>(h);
-                        hi[mt][nt][i] = transposed(h);
-                        lo[mt][nt][i] = transposed(pack2<kBf>(e[2 * i] - back.x, e[2 * i + 1] - back.y));
-                    }
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int w = 0; w < kWords; ++w) {
+                            const uint32_t h = pack2<kBf>(e[2 * i], e[2 * i + 1]);
+                            const float2 back = unpack2<kBf>(h);
+                            pw[mt][nt][w][i] = transposed(h);
+                            e[2 * i] -= back.x;  // exactly
+                            e[2 * i + 1] -= back.y;
+                        }
                 }
             }
 #pragma unroll
@@ -621,18 +626,16 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                             e4m3x4_to_f16(__byte_perm(f[2 * u], 0, 0x3120), a0, a1);
                             e4m3x4_to_f16(__byte_perm(f[2 * u + 1], 0, 0x3120), a2, a3);
 #pragma unroll
-                            for (int nt = 0; nt < kNT; ++nt) {
-                                mma16816<kBf>(o[j + u][nt], a0, a1, a2, a3, hi[mt][nt][0], hi[mt][nt][1]);
-                                mma16816<kBf>(o[j + u][nt], a0, a1, a2, a3, lo[mt][nt][0], lo[mt][nt][1]);
-                            }
+                            for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                                for (int w = 0; w < kWords; ++w) mma16816<kBf>(o[j + u][nt], a0, a1, a2, a3, pw[mt][nt][w][0], pw[mt][nt][w][1]);
                         }
                     } else {
                         ldsm4t(f, v_at + S::chunk_at(16 * mt + (lane & 7) + (lane >> 4) * 8, 2 * j + ((lane >> 3) & 1)) * 16);
 #pragma unroll
-                        for (int nt = 0; nt < kNT; ++nt) {
-                            mma16816<kBf>(o[j][nt], f[0], f[1], f[2], f[3], hi[mt][nt][0], hi[mt][nt][1]);
-                            mma16816<kBf>(o[j][nt], f[0], f[1], f[2], f[3], lo[mt][nt][0], lo[mt][nt][1]);
-                        }
+                        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                            for (int w = 0; w < kWords; ++w) mma16816<kBf>(o[j][nt], f[0], f[1], f[2], f[3], pw[mt][nt][w][0], pw[mt][nt][w][1]);
                     }
                 }
         }
