@@ -581,12 +581,13 @@ PMPE_API int pmpe_kv_read(const pmpe_kv_cache *cache, const pmpe_kv_sequences *s
  * for the last `window` positions (0: all).  Query head i uses the keys and
  * values of head i / (heads / kv_heads).  Products are exact in FP32, sums FP32;
  * a weight enters the sum over the values in three BF16 words, which hold FP32's
- * 24 bits, or in two FP16 words.  A sequence that sees nothing gives out = 0, lse = -inf.  What the
- * cache holds at positions that are not seen, NaN say, does not matter.  The
- * order of the sums goes by the lengths of all sequences of the call, so the same
- * call gives the same bits.  With 8 bits a value loses bits where its scale times
- * its weight is below 2^-20 of the largest scale, and an element of q where it is
- * below 2^-31 of the largest of its head. */
+ * 24 bits, or in two FP16 words: 16 bits or more from 2^-22 of the largest weight
+ * on, below that within 2^-39 of the largest.  (With 8 bits 2^-19 and 2^-36, of a
+ * weight times its value's scale and of the largest weight times the largest scale;
+ * an element of q loses bits where it is below 2^-31 of the largest of its head.)
+ * A sequence that sees nothing gives out = 0, lse = -inf.  What the cache holds at
+ * positions that are not seen, NaN say, does not matter.  The order of the sums goes
+ * by the lengths of all sequences of the call, so the same call gives the same bits. */
 typedef struct pmpe_kv_attend_desc {
     int heads;             /* a multiple of kv_heads, at most 65535 */
     int type;              /* of q and out: the cache's; over 8 bits PMPE_BF16 or PMPE_F16 */

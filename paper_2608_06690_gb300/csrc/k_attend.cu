@@ -47,8 +47,6 @@ constexpr int kMaxCtas = 640;
 constexpr int kJoinThreads = 256, kFew = 4;  // parts that a warp joins by itself
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-constexpr float kAhead = 8.f;   // powers of two that a score may be above the maximum
-constexpr float kUp = 0x1p7f;   // 8 bits: weights up to 2^kAhead kUp stay inside FP16
 
 enum Kind { kBf16, kF16, kE4m3Bf16, kE4m3F16 };  // cache (and queries)
 
@@ -277,6 +275,13 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     using Q = typename std::conditional<kQBf, bf16, __half>::type;
     constexpr int kSteps = kDP / 16, kMT = S::kMT, kKeys = S::kKeys, kTile = S::kTile;
     constexpr int kWords = kBf ? 3 : 2;  // of a weight: all of its 24 bits, or 22
+    // Powers of two that a score may be above the maximum that the weights are
+    // relative to, and what they are multiplied by.  FP16's words end at 2^-24: they
+    // use its range up to 2^15, so that a weight of 2^-22 of the largest keeps 16
+    // bits and a smaller one is off by 2^-39 of the largest at most (over 8 bits, where
+    // following the maximum more often costs time, 2^-19 and 2^-36: the 64 ragged
+    // sequences take 58.1, 58.6, 59.0, 59.6 us with 8, 4, 3, 1 powers).
+    constexpr float kAhead = kBf ? 8.f : k8 ? 3.f : 1.f, kUp = kBf ? 1.f : k8 ? 0x1p12f : 0x1p14f;
     using Span = Span<kTile>;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Cost s_warp[kWarps];
@@ -590,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
             uint32_t pw[kMT][kNT][kWords][2];  // the weights' words, the largest first
 #pragma unroll
             for (int mt = 0; mt < kMT; ++mt) {
-                const float w0 = k8 ? v0[mt] * (kUp / r_max) : 1.f, w1 = k8 ? v1[mt] * (kUp / r_max) : 1.f;
+                const float w0 = k8 ? v0[mt] * (kUp / r_max) : kUp, w1 = k8 ? v1[mt] * (kUp / r_max) : kUp;
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
                     float e[4];
@@ -599,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                         const float base = m[nt][i & 1] == -INFINITY ? 0.f : m[nt][i & 1];
                         e[i] = ex2(s[mt][nt][i] - base);
                         l[nt][i & 1] += e[i];
-                        if (k8) e[i] *= i < 2 ? w0 : w1;
+                        if (!kBf) e[i] *= i < 2 ? w0 : w1;
                     }
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
@@ -667,7 +672,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                 float top = -INFINITY;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w * S::kHeads + nt * 8 + 2 * c + i]);
-                const float f = ex2(m[nt][i] - (top == -INFINITY ? 0.f : top)) * (k8 ? r_max / kUp : 1.f);
+                const float f = ex2(m[nt][i] - (top == -INFINITY ? 0.f : top)) * ((k8 ? r_max : 1.f) / kUp);
 #pragma unroll
                 for (int j = 0; j < kSteps; ++j) {
                     o[j][nt][i] *= f;

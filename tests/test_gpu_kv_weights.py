@@ -1,14 +1,19 @@
 """What the attention's weights hold to.
 
 u = 2^-24.  Scores here are one product q k and its factors: off by 2 u of
-themselves (log2 e, and one product).  2^x by the hardware is within 2^-22; a weight
-in BF16 words is exact, in FP16 words within 2^-22.  A matrix instruction's sums may
-be cut off instead of rounded: 2 u of the largest term each."""
+themselves in 16 bits (log2 e, and one product), 6 u in 8 bits (the scale, the key's
+scale and their products besides).  2^x by the hardware is within 2^-22; a weight
+in BF16 words is exact, in FP16 words within 2^-22, or 2^-39 of the largest weight
+where it is below 2^-22 of it (a step of 2^-24 halved, the largest at 2^14 or above; over
+8 bits at 2^12).  A matrix instruction's sums may be cut off instead of rounded: 2 u
+of the largest term each."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_kv import BF16, F16, U, close, f64, half_eps, smallest
+from test_gpu_kv import BF16, E4M3, F16, KINDS, U, close, f64, half_eps, smallest
 
 pytestmark = pytest.mark.gpu
 
@@ -42,3 +47,48 @@ def test_weights_have_the_bits_of_fp32(pmpe, dtype):
     # the score's and the power's errors; three instructions' sums of terms up to 1, the four warps', the quotient's
     bound = (w * (2 * U * x + 2.0 ** -22) + (0 if dtype == BF16 else 2.0 ** -22) + 2 * 3 * U + 6 * U * np.abs(rest)) / (2 + w)
     close(f64(a.out[:, 0]), want[:, None], (bound + half_eps(dtype) * (np.abs(want) + bound) + smallest(dtype))[:, None])
+
+
+@pytest.mark.parametrize("cache,dtype", KINDS)
+@pytest.mark.parametrize("others", ["equal", "random"])
+@pytest.mark.parametrize("page", [16, 24])
+def test_what_is_far_below_a_position_without_value(pmpe, cache, dtype, others, page):
+    """Positions of large scores and zero values (one for each warp of a tile),
+    and thousands of others up to 2^-29 of their weight: the output is theirs alone."""
+    n, D, H, G = 4000, 32, 4, 12
+    g = torch.Generator().manual_seed(3)
+    k, v = torch.zeros((n, 1, D)), (torch.rand((n, 1, D), generator=g) + 0.5) * 1000
+    if others == "random":
+        k[:, 0, 0] = torch.randn(n, generator=g)
+    first = [0, 16, 32, 48, 64, 80, 96, 112]
+    k[first, 0, 0], v[first] = 16.0, 0.0
+    need = -(-n // page)
+    c = pmpe.KvCache.empty(need, page, 1, D, cache)
+    one = torch.arange(need, dtype=torch.int32, device="cuda").view(1, need)
+    rows = BF16 if cache == E4M3 else cache
+    c.append(k.to(rows).cuda(), v.to(rows).cuda(), one, torch.tensor([n], dtype=torch.int32, device="cuda"), cu_seqlens=torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    # enough sequences that a CTA has whole ones; G of them differ
+    B = 57 * G
+    q1 = torch.zeros((G, H, D))
+    q1[..., 0] = torch.linspace(4.0, 20.0, G * H).view(G, H) / 16
+    q = q1.to(dtype).cuda().repeat(B // G, 1, 1)
+    a = c.attend(q, one.expand(B, need).contiguous(), torch.full((B,), n, dtype=torch.int32, device="cuda"), scale=1.0)
+    pos = np.arange(n)
+    pools = [f64(t) if s is None else f64(t) * f64(s)[..., None] for t, s in ((c.k, c.k_scale), (c.v, c.v_scale))]
+    kk, vv = (x[pos // page, 0, pos % page] for x in pools)
+    s = np.einsum("ghd,nd->ghn", f64(q[:G]), kk)
+    top = s.max(2, keepdims=True)
+    e = np.exp(s - top)
+    p = e / e.sum(2, keepdims=True)
+    want = np.einsum("ghn,nd->ghd", p, vv)  # (values are not negative: also what errors are relative to)
+    # a score and its scale's rounding in 8 bits, the power, the words, the sums of 64 positions a step; each twice, the total has them too
+    rel = 2 * (6 * U * np.abs(s).max(2) + 2.0 ** -22 + 2.0 ** -22 + (n / 64 + 32) * 2 * U)
+    bound = rel[..., None] * want
+    if cache != BF16:
+        # each below 2^-22 of the largest (in 8 bits 2^-19, with the values' scales, relative to a power of two up to twice the largest)
+        bound = bound + n * p.max(2)[..., None] * vv.max() * (2.0 ** -39 if cache == F16 else 2.0 ** -36)
+    bound = bound + half_eps(dtype) * (want + bound) + smallest(dtype)
+    close(f64(a.out).reshape(B // G, G, H, D), want[None], bound[None])
+    lse = (top + np.log(e.sum(2, keepdims=True)))[..., 0]
+    close(f64(a.lse).reshape(B // G, G, H), lse[None], (rel / 2 + 2 * U * np.abs(lse) + 2.0 ** -22)[None])
+    assert math.isfinite(float(a.out.float().sum()))
