@@ -45,6 +45,7 @@
 #include <cooperative_groups.h>
 
 #include "elem.cuh"
+#include "tc_ptx.cuh"
 
 namespace pmpe {
 namespace {
@@ -1066,6 +1067,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
     extern __shared__ __align__(16) uint8_t smem[];
     Shared &s = *reinterpret_cast<Shared *>(smem);
     pdl_trigger();
+    cluster_arrive();
     if (threadIdx.x < 256) s.powers[threadIdx.x] = g_powers.at[threadIdx.x];
     pdl_wait();
     cg::cluster_group cluster = cg::this_cluster();
@@ -1110,6 +1112,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) sample_kern
         least_of = fminf(least_of, __uint_as_float((uint32_t)v));
     };
     for (int w = 0; w < kWarps; ++w) join(s.warp_mass[w]);
+    cluster_wait();  // all CTAs have started: only now may their shared memory be written to
     m.share(2, (u64)__float_as_uint(top) << 32 | __float_as_uint(least_of));  // (a place that the next to share does not use)
     m.all_meet();
     for (int r = 0; r < ranks; ++r) join(s.total[2][r]);

@@ -364,6 +364,11 @@ __device__ __forceinline__ void cluster_sync_all()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
 }
+// The two halves of a cluster barrier that only says that every CTA of the
+// cluster has started, as the first access to another one's shared memory
+// needs: what lies between them hides it.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;\n" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;\n" ::: "memory"); }
 // The shared::cluster address of CTA `rank`'s copy of this CTA's shared address.
 __device__ __forceinline__ uint32_t dsmem_addr(uint32_t local, uint32_t rank)
 {
