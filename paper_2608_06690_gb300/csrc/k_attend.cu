@@ -159,7 +159,7 @@ template <int kTile> struct Span {
 };
 
 // A place in the row of all tiles: tile `tile` of the positions of sequence b,
-// for block `block` of the queries of key head `head`.
+// for block `block` of the queries of key head `head`.  A warp's lanes go together.
 template <int kTile> struct Walk {
     int b, head, block, tile;
     Span<kTile> s;
@@ -171,8 +171,17 @@ template <int kTile> struct Walk {
             block = 0;
             if (++head == p.kv.kv_heads) {
                 head = 0;
-                do s = Span<kTile>(p, ++b);
-                while (s.tiles == 0 && b < p.kv.B);
+                // the next sequence that sees something, by a look at 32 lengths
+                // at once; B for none
+                for (++b; b < p.kv.B; b += 32) {
+                    const uint32_t any = __ballot_sync(~0u, Span<kTile>(p, b + (threadIdx.x & 31)).tiles > 0);
+                    if (any) {
+                        b += __ffs(any) - 1;
+                        break;
+                    }
+                }
+                b = min(b, p.kv.B);
+                s = Span<kTile>(p, b);
             }
         }
         return true;
