@@ -587,7 +587,9 @@ PMPE_API int pmpe_kv_read(const pmpe_kv_cache *cache, const pmpe_kv_sequences *s
  * an element of q loses bits where it is below 2^-31 of the largest of its head.)
  * A sequence that sees nothing gives out = 0, lse = -inf.  What the cache holds at
  * positions that are not seen, NaN say, does not matter.  The order of the sums goes
- * by the lengths of all sequences of the call, so the same call gives the same bits. */
+ * by the lengths of all sequences of the call, so the same call gives the same bits.
+ * Should a copy out of the cache not end within 4 s, the heads that wait for it become
+ * NaN; there is no other sign of that. */
 typedef struct pmpe_kv_attend_desc {
     int heads;             /* a multiple of kv_heads, at most 65535 */
     int type;              /* of q and out: the cache's; over 8 bits PMPE_BF16 or PMPE_F16 */

@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Cost s_warp[kWarps];
     __shared__ Spot s_spot[2];
-    __shared__ volatile int s_abort;
+    __shared__ volatile int s_abort, s_left;  // a wait ran out; one for what was left behind did too
     uint8_t *rings = smem + (-smem_u32(smem) & 1023u), *smalls = rings + kWarps * S::kStages * S::kData;
     uint8_t *ring = rings + (threadIdx.x >> 5) * S::kStages * S::kData, *small = smalls + (threadIdx.x >> 5) * S::kStages * S::kSmall;
     float *s_m = (float *)(smalls + kWarps * S::kStages * S::kSmall), *s_l = s_m + kWarps * S::kHeads;
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     auto barrier = [&](int stage) { return smem_u32(small + stage * S::kSmall + S::kScales); };
     if (lane == 0) {  // a stage is full when its copies are: one arrival with their bytes, or every lane's
         for (int i = 0; i < S::kStages; ++i) mbar_init(barrier(i), boxes ? 1 : 32);
-        if (warp == 0) s_abort = 0;
+        if (warp == 0) s_abort = 0, s_left = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     pdl_wait();
@@ -331,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     // ---- copies
     Walk<kTile> ahead = at;
     long long to_copy = left;
+    int copied = 0;
     // The entry of position pos (the first of `n` in one page); -1: none of
     // them is seen, or there is no page.
     auto entry_at = [&](int pos, int n) -> long long {
@@ -407,6 +408,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
         }
         if (lane == 0) *(uint32_t *)(small + stage * S::kSmall + S::kScales + 8) = mask;
         --to_copy;
+        ++copied;
         if (ahead.advance(p)) in_batch = kBatch;
         if (!boxes) look_up();
     };
@@ -741,8 +743,8 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
         fence_proxy_async_smem();  // before the next copies into the stages
         __syncthreads();
     }
-    if (lost)  // no copy is left behind, as far as that can be waited for
-        for (int i = 0; i < S::kStages; ++i) mbar_wait(barrier(i), parity, &s_abort, nullptr);
+    if (lost)  // no copy is left behind: each stage's last one is waited for, again with a limit
+        for (int n = max(copied - S::kStages, 0); n < copied; ++n) mbar_wait(barrier(n % S::kStages), n / S::kStages & 1, &s_left, nullptr);
     cp_async_wait<0>();
 }
 
