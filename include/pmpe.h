@@ -579,7 +579,8 @@ PMPE_API int pmpe_kv_read(const pmpe_kv_cache *cache, const pmpe_kv_sequences *s
  *   s_p = scale q . k_p,  a = softmax of s over the positions seen
  *   out = sum_p a_p v_p,  lse = ln sum_p exp(s_p)
  * for the last `window` positions (0: all).  Query head i uses the keys and
- * values of head i / (heads / kv_heads).  Products are exact in FP32, sums FP32;
+ * values of head i / (heads / kv_heads).  Products are exact in FP32, sums FP32, so
+ * that 2^8 times (over 8 bits 2^3 times) the sum of all |v_p| has to be finite in it;
  * a weight enters the sum over the values in three BF16 words, which hold FP32's
  * 24 bits, or in two FP16 words: 16 bits or more from 2^-22 of the largest weight
  * on, below that within 2^-39 of the largest.  (With 8 bits 2^-19 and 2^-36, of a

@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
     // ---- tiles
     uint32_t qf[kSteps][kNT][2];
     float o[kSteps][kNT][4], m[kNT][2], l[kNT][2], cs[kNT][2];
-    float r_max = 0x1p-100f;  // 8 bits: the power of two that the weights are relative to
+    float v_up = 0x1p126f;  // 8 bits: one over the power of two that the weights are relative to
     int stage = 0, fill = S::kStages - 1, pieces = 0;
     uint32_t parity = 0;
     bool fresh = true, lost = false;
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                 m[nt][0] = m[nt][1] = -INFINITY;
                 l[nt][0] = l[nt][1] = 0.f;
             }
-            r_max = 0x1p-100f;
+            v_up = 0x1p126f;
 #pragma unroll
             for (int j = 0; j < kSteps; ++j)
 #pragma unroll
@@ -569,17 +569,17 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                     v1[mt] = mask >> (16 * mt + g + 8) & 1 ? scales[kKeys + 16 * mt + g + 8] : 0.f;
                     v_top = fmaxf(v_top, fmaxf(v0[mt], v1[mt]));
                 }
-                grown |= v_top > r_max;
+                grown |= v_top * v_up > 1.f;
             }
             if (__any_sync(~0u, grown)) {
                 float by = 1.f;
                 if constexpr (k8) {
 #pragma unroll
                     for (int off = 4; off < 32; off <<= 1) v_top = fmaxf(v_top, __shfl_xor_sync(~0u, v_top, off));
-                    if (v_top > r_max) {
-                        const float to = __uint_as_float(min((__float_as_uint(v_top) & 0x7f800000u) + 0x00800000u, 0x7f000000u));
-                        by = r_max / to;
-                        r_max = to;
+                    if (v_top * v_up > 1.f) {
+                        const float to = 1.f / __uint_as_float(min((__float_as_uint(v_top) & 0x7f800000u) + 0x00800000u, 0x7f000000u));
+                        by = to / v_up;
+                        v_up = to;
                     }
                 }
 #pragma unroll
@@ -606,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
             uint32_t pw[kMT][kNT][kWords][2];  // the weights' words, the largest first
 #pragma unroll
             for (int mt = 0; mt < kMT; ++mt) {
-                const float w0 = k8 ? v0[mt] * (kUp / r_max) : kUp, w1 = k8 ? v1[mt] * (kUp / r_max) : kUp;
+                const float w0 = k8 ? v0[mt] * v_up * kUp : kUp, w1 = k8 ? v1[mt] * v_up * kUp : kUp;
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
                     float e[4];
@@ -683,11 +683,11 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                 float top = -INFINITY;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w * S::kHeads + nt * 8 + 2 * c + i]);
-                const float f = ex2(m[nt][i] - (top == -INFINITY ? 0.f : top)) * ((k8 ? r_max : 1.f) / kUp);
+                const float f = ex2(m[nt][i] - (top == -INFINITY ? 0.f : top)) / kUp, down = k8 ? 1.f / v_up : 1.f;
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) {
-                    o[j][nt][i] *= f;
-                    o[j][nt][i + 2] *= f;
+                for (int j = 0; j < kSteps; ++j) {  // (two factors: their product may be too small)
+                    o[j][nt][i] = o[j][nt][i] * f * down;
+                    o[j][nt][i + 2] = o[j][nt][i + 2] * f * down;
                 }
             }
         // the warps' sums, each in the stage that the warp has just read; a

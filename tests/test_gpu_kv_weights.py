@@ -13,6 +13,7 @@ import numpy as np
 import pytest
 import torch
 
+import operators_ref as ref
 from test_gpu_kv import BF16, E4M3, F16, KINDS, U, close, f64, half_eps, smallest
 
 pytestmark = pytest.mark.gpu
@@ -92,3 +93,29 @@ def test_what_is_far_below_a_position_without_value(pmpe, cache, dtype, others, 
     lse = (top + np.log(e.sum(2, keepdims=True)))[..., 0]
     close(f64(a.lse).reshape(B // G, G, H), lse[None], (rel / 2 + 2 * U * np.abs(lse) + 2.0 ** -22)[None])
     assert math.isfinite(float(a.out.float().sum()))
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 70])
+@pytest.mark.parametrize("base", [2.0 ** -126, 2.0 ** -125, 2.0 ** -123, 2.0 ** -110, 2.0 ** 118])
+def test_values_of_the_smallest_scales(pmpe, base, n):
+    """Eight bits: scales down to 2^-126, the least that an append writes, and near FP32's end."""
+    D, page = 32, 16
+    need = -(-n // page)
+    g = torch.Generator().manual_seed(4)
+    c = pmpe.KvCache.empty(need, page, 1, D, E4M3)
+    c.k.copy_(torch.randn(c.k.shape, generator=g).to(E4M3))
+    c.v.copy_((1 + 255 * torch.rand(c.v.shape, generator=g)).to(E4M3))
+    c.k_scale.fill_(0.25)
+    c.v_scale.copy_(base * (1 + torch.rand(c.v_scale.shape, generator=g)))
+    q = torch.randn((1, 4, D), generator=g).to(BF16).cuda()
+    table = torch.arange(need, dtype=torch.int32, device="cuda").view(1, need)
+    a = c.attend(q, table, torch.tensor([n], dtype=torch.int32, device="cuda"))
+    pos = np.arange(n)
+    k, v = (x[pos // page, :, pos % page] for x in (f64(c.k) * f64(c.k_scale)[..., None], f64(c.v) * f64(c.v_scale)[..., None]))
+    want, _, size, scores = ref.attend(f64(q[0]), k, v, 1 / math.sqrt(D))
+    # as in the other file's, FP16's words in place of 2^-17
+    bound = (2 * (136 * U * scores[:, None] + 2.0 ** -22 + 2.0 ** -22) + (n / 64 + 32) * 4 * U) * size
+    bound = bound + n * 2.0 ** -36 * v.max() + half_eps(BF16) * (np.abs(want) + bound) + smallest(BF16)
+    # the sum over the values before it is divided, up to 2^3 n of the largest value, is FP32's: 2^128 ends it
+    ok = np.full(want.shape, 8 * n * v.max() < 2.0 ** 128) | (n == 1)
+    close(f64(a.out[0])[ok], want[ok], bound[ok])
