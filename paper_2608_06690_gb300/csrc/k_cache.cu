@@ -4,7 +4,7 @@
 //   8 bits:  s = max(amax |x| / 448, 2^-126),  q = e4m3(x / s),  x ~ q s
 //
 // A group of lanes holds one head of one row's key or value, eight elements a
-// lane, so that the largest magnitude is a few shuffles and both sides are
+// lane (into 8 bits 16 where the rows' alignment allows), so that the largest magnitude is a few shuffles and both sides are
 // accessed 16 bytes a lane.  A CTA takes a run of rows.  Where they go (the
 // sequence by a search over the offsets, the page by the table: a chain of
 // loads) is found for all of them at once, a thread a row, while the first rows
@@ -35,6 +35,7 @@ struct CacheParams {
     void *k_out, *v_out;      // read: destination
     long long k_ld, k_head_ld, v_ld, v_head_ld;
     int T;
+    int sms;                  // of the device
     int rows, heads;          // of a CTA: rows, and of each as many of its keys' and values' heads
     FastDiv by_heads;
 };
@@ -202,12 +203,12 @@ __global__ void __launch_bounds__(kThreads, ctas_of_sm(kWide)) cache_kernel(cons
 template <typename T, typename C, int kLanes, bool kVec, bool kBack, int kWide = 1> cudaError_t launch_l(CacheParams &p, cudaStream_t st)
 {
     // rows of a CTA: as many as fill its groups once, or more, so that the CTAs
-    // of 152 SMs take all rows at once
+    // of all SMs take all rows at once
     constexpr int kGroups = kThreads / kLanes;
     const int all = 2 * p.kv.kv_heads;
     p.heads = std::min(all, kGroups);
     const int parts = (all + p.heads - 1) / p.heads;
-    const long long ctas = 152 * ctas_of_sm(kWide), share = ((long long)p.T * parts + ctas - 1) / ctas;
+    const long long ctas = p.sms * ctas_of_sm(kWide), share = ((long long)p.T * parts + ctas - 1) / ctas;
     p.rows = (int)std::min<long long>(std::max<long long>(kGroups / p.heads, share), kMaxRowsOfCta);
     p.by_heads = FastDiv(p.heads);
     return launch_pdl(cache_kernel<T, C, kLanes, kVec, kBack, kWide>, dim3((p.T + p.rows - 1) / p.rows, parts), dim3(kThreads), 0, st, p);
@@ -240,9 +241,9 @@ template <bool kBack> cudaError_t launch_types(CacheParams p, int type, int cach
 
 }  // namespace
 
-cudaError_t launch_kv_append(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, const pmpe_kv_append_desc &d, cudaStream_t st)
+cudaError_t launch_kv_append(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, const pmpe_kv_append_desc &d, int num_sms, cudaStream_t st)
 {
-    const CacheParams p = {KvView(c, s), d.k, d.v, nullptr, nullptr, d.k_ld, d.k_head_ld, d.v_ld, d.v_head_ld, d.T, 0, 0, FastDiv(1)};
+    const CacheParams p = {KvView(c, s), d.k, d.v, nullptr, nullptr, d.k_ld, d.k_head_ld, d.v_ld, d.v_head_ld, d.T, num_sms, 0, 0, FastDiv(1)};
     const bool f32 = d.type == PMPE_F32;
     const int64_t ld = d.k_ld | d.v_ld | d.k_head_ld | d.v_head_ld;
     int vec = aligned8(d.k, f32) && aligned8(d.v, f32) && ld % 8 == 0;
@@ -250,9 +251,9 @@ cudaError_t launch_kv_append(const pmpe_kv_cache &c, const pmpe_kv_sequences &s,
     return launch_types<false>(p, d.type, c.type, vec, st);
 }
 
-cudaError_t launch_kv_read(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, int T, int type, void *k, void *v, cudaStream_t st)
+cudaError_t launch_kv_read(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, int T, int type, void *k, void *v, int num_sms, cudaStream_t st)
 {
-    const CacheParams p = {KvView(c, s), nullptr, nullptr, k, v, 0, 0, 0, 0, T, 0, 0, FastDiv(1)};
+    const CacheParams p = {KvView(c, s), nullptr, nullptr, k, v, 0, 0, 0, 0, T, num_sms, 0, 0, FastDiv(1)};
     const bool f32 = type == PMPE_F32;
     return launch_types<true>(p, type, c.type, aligned8(k, f32) && aligned8(v, f32), st);
 }

@@ -228,7 +228,9 @@ int pmpe_kv_append(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, co
     if (!apart_from_cache(d->k, (last * d->k_ld + heads * d->k_head_ld + cache->head_dim) * e, *cache) ||
         !apart_from_cache(d->v, (last * d->v_ld + heads * d->v_head_ld + cache->head_dim) * e, *cache))
         return PMPE_ERR_INVALID_ARG;
-    return done(launch_kv_append(*cache, *seqs, *d, (cudaStream_t)stream));
+    int sms = 0;
+    if ((rc = sm_count(&sms)) != PMPE_OK) return rc;
+    return done(launch_kv_append(*cache, *seqs, *d, sms, (cudaStream_t)stream));
 }
 
 int pmpe_kv_read(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, int T, int type, void *k, void *v, void *stream)
@@ -242,7 +244,9 @@ int pmpe_kv_read(const pmpe_kv_cache *cache, const pmpe_kv_sequences *seqs, int 
     if (!fits(k, type) || !fits(v, type)) return PMPE_ERR_UNSUPPORTED_SHAPE;
     const int64_t bytes = (int64_t)T * cache->kv_heads * cache->head_dim * (type == PMPE_F32 ? 4 : 2);
     if (!apart(k, bytes, v, bytes) || !apart_from_cache(k, bytes, *cache) || !apart_from_cache(v, bytes, *cache)) return PMPE_ERR_INVALID_ARG;
-    return done(launch_kv_read(*cache, *seqs, T, type, k, v, (cudaStream_t)stream));
+    int sms = 0;
+    if ((rc = sm_count(&sms)) != PMPE_OK) return rc;
+    return done(launch_kv_read(*cache, *seqs, T, type, k, v, sms, (cudaStream_t)stream));
 }
 
 size_t pmpe_kv_attend_workspace_size(int B, int heads, int kv_heads, int head_dim)

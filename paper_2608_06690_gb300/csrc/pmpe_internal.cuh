@@ -188,8 +188,8 @@ size_t clip_workspace_bytes(int n);
 int clip_tensors_ok(const pmpe_grad *g, int n);
 cudaError_t launch_clip(const pmpe_grad *g, int n, float max_norm, float *norm_out, void *workspace, cudaStream_t st);
 // The decoding loop's operators (k_cache.cu, k_attend.cu, k_sample.cu).
-cudaError_t launch_kv_append(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, const pmpe_kv_append_desc &d, cudaStream_t st);
-cudaError_t launch_kv_read(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, int T, int type, void *k, void *v, cudaStream_t st);
+cudaError_t launch_kv_append(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, const pmpe_kv_append_desc &d, int num_sms, cudaStream_t st);
+cudaError_t launch_kv_read(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, int T, int type, void *k, void *v, int num_sms, cudaStream_t st);
 size_t kv_attend_workspace_bytes(int B, int heads, int kv_heads, int head_dim);
 cudaError_t launch_kv_attend(const pmpe_kv_cache &c, const pmpe_kv_sequences &s, const pmpe_kv_attend_desc &d, int num_sms, cudaStream_t st);
 cudaError_t launch_sample(const pmpe_sample_desc &d, int num_sms, cudaStream_t st);
