@@ -629,6 +629,11 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                         }
                 }
             }
+            // 16 positions' sums, the smallest words first, then to the running
+            // ones by additions that round: the matrix instructions cut their sums
+            // off, always towards zero, which in running sums grew with the run
+            // (1e-3 over 2^20 positions; without them 0.7 us of the 88, over
+            // 8 bits 1.3 of the 60).
 #pragma unroll
             for (int mt = 0; mt < kMT; ++mt)
 #pragma unroll
@@ -642,16 +647,24 @@ __global__ void __launch_bounds__(kThreads, (AttendShape<kDP, kNT, kKind>::kCtas
                             e4m3x4_to_f16(__byte_perm(f[2 * u], 0, 0x3120), a0, a1);
                             e4m3x4_to_f16(__byte_perm(f[2 * u + 1], 0, 0x3120), a2, a3);
 #pragma unroll
-                            for (int nt = 0; nt < kNT; ++nt)
+                            for (int nt = 0; nt < kNT; ++nt) {
+                                float sum[4] = {};
 #pragma unroll
-                                for (int w = 0; w < kWords; ++w) mma16816<kBf>(o[j + u][nt], a0, a1, a2, a3, pw[mt][nt][w][0], pw[mt][nt][w][1]);
+                                for (int w = kWords - 1; w >= 0; --w) mma16816<kBf>(sum, a0, a1, a2, a3, pw[mt][nt][w][0], pw[mt][nt][w][1]);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) o[j + u][nt][i] += sum[i];
+                            }
                         }
                     } else {
                         ldsm4t(f, v_at + S::chunk_at(16 * mt + (lane & 7) + (lane >> 4) * 8, 2 * j + ((lane >> 3) & 1)) * 16);
 #pragma unroll
-                        for (int nt = 0; nt < kNT; ++nt)
+                        for (int nt = 0; nt < kNT; ++nt) {
+                            float sum[4] = {};
 #pragma unroll
-                            for (int w = 0; w < kWords; ++w) mma16816<kBf>(o[j][nt], f[0], f[1], f[2], f[3], pw[mt][nt][w][0], pw[mt][nt][w][1]);
+                            for (int w = kWords - 1; w >= 0; --w) mma16816<kBf>(sum, f[0], f[1], f[2], f[3], pw[mt][nt][w][0], pw[mt][nt][w][1]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[j][nt][i] += sum[i];
+                        }
                     }
                 }
         }

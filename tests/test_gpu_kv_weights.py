@@ -14,7 +14,7 @@ import pytest
 import torch
 
 import operators_ref as ref
-from test_gpu_kv import BF16, E4M3, F16, KINDS, U, close, f64, half_eps, smallest
+from test_gpu_kv import BF16, E4M3, F16, KINDS, U, cache_of, close, f64, half_eps, smallest
 
 pytestmark = pytest.mark.gpu
 
@@ -119,3 +119,21 @@ def test_values_of_the_smallest_scales(pmpe, base, n):
     # the sum over the values before it is divided, up to 2^3 n of the largest value, is FP32's: 2^128 ends it
     ok = np.full(want.shape, 8 * n * v.max() < 2.0 ** 128) | (n == 1)
     close(f64(a.out[0])[ok], want[ok], bound[ok])
+
+
+@pytest.mark.parametrize("cache,dtype,n", [(BF16, BF16, 1 << 22), (F16, F16, 1 << 20), (E4M3, F16, 1 << 20), (E4M3, BF16, 1 << 22)])
+def test_long_sums_are_not_cut_off(pmpe, cache, dtype, n):
+    """Enough long sequences that a CTA has whole ones, all values 1: the weights'
+    sum over the weights' sum.  A warp adds a quarter of them, 16 at a time: roundings
+    of half a step each, in any direction, ten standard deviations of which are
+    10 sqrt(n / 64) u, for both sums."""
+    B, H, D, page, pages = 480, 8, 32, 1024, 8
+    c = cache_of(pmpe, pages, page, 1, D, cache, 1)
+    c.v.copy_(torch.ones(c.v.shape).to(cache))
+    if cache == E4M3:
+        c.v_scale.fill_(1.0)
+    g = torch.Generator().manual_seed(2)
+    table = torch.randint(0, pages, (1, n // page), generator=g, dtype=torch.int32).cuda().expand(B, -1).contiguous()
+    q = torch.randn((B, H, D), generator=g).to(dtype).cuda()
+    a = c.attend(q, table, torch.full((B,), n, dtype=torch.int32, device="cuda"))
+    close(f64(a.out), 1.0, 2 * 10 * math.sqrt(n / 64) * U + half_eps(dtype))
