@@ -586,6 +586,8 @@ PMPE_API int pmpe_kv_read(const pmpe_kv_cache *cache, const pmpe_kv_sequences *s
  * on, below that within 2^-39 of the largest.  (With 8 bits 2^-19 and 2^-36, of a
  * weight times its value's scale and of the largest weight times the largest scale;
  * an element of q loses bits where it is below 2^-31 of the largest of its head.)
+ * A NaN that is seen shows; an infinite value that is seen makes its column of out an
+ * infinity or NaN (a weight's smaller words may be 0 or negative).
  * A sequence that sees nothing gives out = 0, lse = -inf.  What the cache holds at
  * positions that are not seen, NaN say, does not matter.  The order of the sums goes
  * by the lengths of all sequences of the call, so the same call gives the same bits.

@@ -137,3 +137,19 @@ def test_long_sums_are_not_cut_off(pmpe, cache, dtype, n):
     q = torch.randn((B, H, D), generator=g).to(dtype).cuda()
     a = c.attend(q, table, torch.full((B,), n, dtype=torch.int32, device="cuda"))
     close(f64(a.out), 1.0, 2 * 10 * math.sqrt(n / 64) * U + half_eps(dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_an_infinite_value_shows_in_its_column_alone(pmpe, dtype):
+    c = cache_of(pmpe, 8, 16, 2, 64, dtype, 1)
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(2, 4)
+    n = torch.tensor([64, 50], dtype=torch.int32, device="cuda")
+    g = torch.Generator().manual_seed(3)
+    q = torch.randn((2, 8, 64), generator=g).to(dtype).cuda()
+    want = c.attend(q, table, n)
+    c.v[5, 1, 3, 7] = math.inf
+    got = c.attend(q, table, n)
+    at = torch.zeros((2, 8, 64), dtype=torch.bool, device="cuda")
+    at[1, 4:, 7] = True
+    assert not torch.isfinite(got.out[at]).any()
+    assert torch.equal(got.out[~at], want.out[~at]) and torch.equal(got.lse, want.lse)
