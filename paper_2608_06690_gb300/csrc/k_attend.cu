@@ -4,9 +4,9 @@
 //
 // in one pass over the cache with the running maximum m.  The cache's bytes
 // bound it (64 sequences of up to 8192 positions, 32 over 4 heads of 128, 538 MB
-// of BF16: 87.8 us, 6.1 TB/s; 131072 positions of one sequence 49.5 us; in e4m3
-// the 278 MB 58 us).  Of a key and its value (512 bytes in 16 bits) every query
-// head of a group takes 512 operations: mma.sync is busy an eighth of the time
+// of BF16: 87.6 us, 6.1 TB/s; 131072 positions of one sequence 50.2 us; in e4m3
+// the 278 MB 60.2 us, where instructions count as much).  Of a key and its value (512 bytes in 16 bits) every query
+// head of a group takes 512 operations: mma.sync is busy a sixth of the time
 // (a fifth in e4m3).  tcgen05 would hold 128 keys by eight heads in TMEM and
 // read them back for the maximum; no product here is long enough to show.
 //
@@ -14,7 +14,7 @@
 // 16 keys and their values (32 of narrow ones) ahead into a ring of its own, by
 // TMA where 16 positions lie one after another in a page (pages of a multiple of
 // 16), by 16-byte copies of each row otherwise.  (The copies alone take 81 us of
-// the 87.8, with the ones of each row 95.)  The more warps an SM has, the less
+// the 87.6, with the ones of each row 95.)  The more warps an SM has, the less
 // each one's chain of dependent steps shows: 12 or 16 of them with two or three
 // stages each; 8 with three took 107 us, and 97 in e4m3.
 //
@@ -34,6 +34,12 @@
 // (FP32) in the workspace, and a second launch joins them in order.  That launch
 // costs 2 to 5 us; sums joined by the last CTA of a pair would need counters that
 // are zero before the call.
+//
+// Groups of more than 8 heads (16 up to 128 columns) are several blocks, each of
+// which reads the keys and values again, and 16 heads side by side cost registers:
+// the 64 ragged sequences with 16, 24, 64 heads a key head of 128 take 96, 159, 305
+// us in BF16, 86, 146, 275 in e4m3 (102 bytes a thread spilled, 40 with heads of 64,
+// 28 in 16 bits); with 24 heads of 256 246 and 146.
 #include <algorithm>
 
 #include "kv_cache.cuh"
@@ -191,8 +197,8 @@ template <int kTile> struct Walk {
 // Work as the CTAs share it: a tile counts one, and each pair of a sequence and
 // a block of heads kEnd more, for its queries and its end (64 sequences of 0 to
 // 8192 positions in e4m3: CTAs of equal tiles ended 26 us apart, the ones with
-// many short sequences last; kEnd = 1, 2, 3, 4: 63.1, 63.6, 57.2, 56.7 us, in
-// BF16 86.8 to 87.8, where a pair's end takes as long as 1.6 tiles).  Tile k of a
+// many short sequences last; kEnd = 1, 2, 3, 4 took 63.1, 63.6, 57.2, 56.7 us
+// when 3 was chosen, in BF16 86.8 to 87.8, where a pair's end takes as long as 1.6 tiles).  Tile k of a
 // pair that begins at cost P is at cost P + kEnd + k; CTA c has the costs c per ..
 // (c + 1) per - 1.
 constexpr long long kEnd = 3;

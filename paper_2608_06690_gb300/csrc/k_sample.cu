@@ -32,11 +32,12 @@
 // further passes, over the bits of the logits in the border's bin, down to one
 // value.  Of equal logits at the border the lowest ids stay.
 //
-// Latency bounds a single row (131072 tokens, top_k 50, top_p 0.95: 13.2 us, the
-// largest logit and the list 5 and 3 of them), instructions many rows: r takes 39
-// a token, two tokens at a time (400 rows of 32003: 37 us, of two CTAs each 58;
-// 64 rows of 131072 22 us with top_k, 29 with neither, 67 with top_p over as many
-// as a fifth of the tokens).  A row's passes run a few times each, so that fetching their code
+// Latency bounds a single row (131072 tokens, top_k 50, top_p 0.95: 13.3 us, the
+// largest logit and the list 5 and 3 of them).  Many rows: r takes 39 instructions a
+// token, two tokens at a time, whose issue is half of the 41.5 us of 400 rows of
+// 32003; the other half is the grid, 400 CTAs on 304 places (two CTAs a row: 58).
+// (64 rows of 131072 22 us with top_k, 29 with neither, 67 with top_p over as many as
+// a fifth of the tokens.  16-bit logits spill 36 bytes a thread.)  A row's passes run a few times each, so that fetching their code
 // counts: they are not unrolled, and what is seldom needed is out of line.
 #include <string.h>
 
