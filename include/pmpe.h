@@ -618,7 +618,8 @@ PMPE_API int pmpe_kv_attend(const pmpe_kv_cache *cache, const pmpe_kv_sequences 
  *         before it (the first always; 1 or more: all); of those r >= min_p
  *         (0 or less, NaN: all; above 1: as 1)
  *   drawn: the lowest kept id whose running sum of r, by id, is above u times
- *         the kept sum; its probability is r over that sum
+ *         the kept sum; its probability is r over that sum, both rounded to FP32
+ *         before the quotient is
  * A temperature that is not above 0 takes the largest logit (equal ones by the
  * lower id) with probability 1.  u outside [0, 1) counts as its nearest end, NaN
  * as 0; a top_p of NaN as 0.  A row without a token to draw gives -1 and 0.
